@@ -570,6 +570,104 @@ spv_status spv_devoxelize(void* stream, void* ws, size_t ws_bytes,
                           const float* scale_p, const float* shift_p, int32_t relu_p,
                           void* out, spv_dtype dt, int32_t* corner_idx, float* corner_w);
 
+/*
+ * spv_layer_norm -- normalization of each feature row over its channels:
+ *   out[i][c] = (x[i][c] - mu_i) * r_i * gamma[c] + beta[c],
+ *   mu_i = mean_c x[i][c],  r_i = 1 / sqrt(mean_c (x[i][c] - mu_i)^2 + eps)
+ * float32 statistics (the deviations are squared after the mean is taken off),
+ * one rounding to dt.  A row of equal values gives beta.
+ * In:  x [m_cap][C] (dt); m_dev: device row count (NULL = m_cap); gamma, beta
+ *      [C] f32 or NULL (1, 0); eps > 0, finite.
+ * Out: out [m_cap][C] (dt; rows < count written); may be x itself.
+ * 16-byte aligned rows of a multiple of 8 (16-bit) or 4 (f32) channels are moved
+ * 16 bytes at a time; other widths and pointers element by element.  No workspace.
+ * Errors: SPV_ERR_INVALID_ARG (null pointers, sizes, eps).
+ *
+ * spv_layer_norm_backward -- with h = dy * gamma and xh = (x - mu) r, from x itself
+ * (the statistics are formed again; nothing of the forward call is kept):
+ *   dx = r (h - mean_c h - xh mean_c(h xh)) (+ dres),
+ *   dgamma[c] = sum_i dy xh,  dbeta[c] = sum_i dy
+ * (float32 sums over a workgroup's rows, added in fp64 in a fixed order: the same
+ * bits on every call).
+ * In:  dy, x [m_cap][C] (dt); dres [m_cap][C] (dt) or NULL: a gradient added to dx
+ *      before its one rounding (the residual branch around a pre-norm layer).
+ * Out: dx [m_cap][C] (dt; may be dy or dres), dgamma, dbeta [C] f32; any may be
+ *      NULL.  ws: spv_layer_norm_backward_workspace_bytes(m_cap, C) bytes, 256-byte
+ *      aligned, needed only with dgamma or dbeta.
+ * Errors: SPV_ERR_INVALID_ARG, SPV_ERR_CAPACITY.
+ */
+spv_status spv_layer_norm(void* stream, const void* x, const int64_t* m_dev, int64_t m_cap, int32_t C,
+                          const float* gamma, const float* beta, float eps, void* out, spv_dtype dt);
+size_t spv_layer_norm_backward_workspace_bytes(int64_t m_cap, int32_t C);
+spv_status spv_layer_norm_backward(void* stream, void* ws, size_t ws_bytes, const void* dy, const void* x,
+                                   const int64_t* m_dev, int64_t m_cap, int32_t C, const float* gamma, float eps,
+                                   const void* dres, void* dx, float* dgamma, float* dbeta, spv_dtype dt);
+
+/* Parameters of an attention over packed scans.  Rows of scan b are q_off[b] ..
+ * q_off[b+1] - 1 of the queries and k_off[b] .. k_off[b+1] - 1 of the keys and
+ * values; either range may be empty.  A voxel list in canonical order holds its
+ * scans one after the other. */
+typedef struct spv_attention_params {
+    int32_t H;   /* query heads */
+    int32_t Hkv; /* key / value heads; query head h reads head h / (H / Hkv) */
+    int32_t D;   /* channels of a head: a multiple of 8 in 8 .. 128 */
+    int32_t B;   /* scans */
+    float scale; /* of the products q . k, in [1e-9, 1e9] */
+    float cap;   /* > 0: a product z counts as cap * tanh(z / cap); 0: as z; else in [1e-6, 1e6] */
+    const int32_t* q_off;    /* [B + 1] device, ascending */
+    const int32_t* k_off;    /* [B + 1] device, ascending (may be q_off) */
+    const int32_t* q_coords; /* [nq][4] voxel coordinates (b, x, y, z), or NULL: no distance bias */
+    const int32_t* k_coords; /* [nk][4], given with q_coords (may be the same) */
+    const float* slopes;     /* [H] f32, given with q_coords; finite, at most 1e9 in magnitude */
+} spv_attention_params;
+
+/*
+ * spv_attention -- attention of every query over the keys of its scan:
+ *   z_ij = scale * (q_i . k_j),  t_ij = cap > 0 ? cap * tanh(z_ij / cap) : z_ij,
+ *   s_ij = t_ij - slopes[h] * (|dx| + |dy| + |dz|)   (d = c_i - c_j, the voxels' coordinates),
+ *   out_i = sum_j p_ij v_j,  p_ij = exp(s_ij - lse_i),  lse_i = log sum_j exp(s_ij)
+ * for each head h, j over the scan's keys.  A query whose scan has no key gets
+ * out = 0 and lse = -inf.  With coordinates (b, i, 0, 0) the bias is the one of
+ * token distances in a sequence.  Softmax statistics and sums are float32; 16-bit
+ * types multiply on matrix cores with the weights p rounded to the type.
+ * In:  q [nq][ldq], k [nk][ldk], v [nk][ldv] (dt): row i, head h at
+ *      q + i * ldq + h * D; row strides in elements, multiples of 8 (16-bit) or 4
+ *      (f32), at least the row's channels; 16-byte aligned, so q, k and v may be
+ *      parts of one wider buffer.  Coordinates outside the voxel range count as its
+ *      nearest end.  Offsets are clamped to [0, nq] / [0, nk].
+ * Out: out [nq][ldo] (dt), no input; lse [nq][H] f32 or NULL (the backward's
+ *      input).  Rows of no scan are not written.
+ *      ws: spv_attention_workspace_bytes(p, nq, nk, dt) bytes, 256-byte aligned
+ *      (NULL where that is 0): few queries split their keys over the chip, and the
+ *      parts are joined from there in a fixed order.
+ * Errors: SPV_ERR_INVALID_ARG (null or misaligned pointers, sizes, strides, scale,
+ *      cap, aliasing), SPV_ERR_UNSUPPORTED (D; more than 2^22 workgroups),
+ *      SPV_ERR_CAPACITY (ws too small).
+ *
+ * spv_attention_backward -- its gradients, with delta_i = dout_i . out_i:
+ *   dv_j = sum_i p_ij dout_i,  ds_ij = p_ij (dout_i . v_j - delta_i),
+ *   dz_ij = ds_ij (1 - (t_ij / cap)^2) (or ds_ij),
+ *   dq_i = scale sum_j dz_ij k_j,  dk_j = scale sum_i dz_ij q_i
+ * (shared key heads sum over their query heads; scale, cap and slopes are
+ * constants).  Deterministic: no atomics, every sum in a fixed order.
+ * In:  the forward's inputs, out and lse; dout [nq][lddo] (dt).
+ * Out: dq [nq][lddq], dk [nk][lddk], dv [nk][lddv] (dt), no input, rows strided and
+ *      aligned as the inputs'.  A key of a scan without queries gets 0; rows of no
+ *      scan are not written.
+ *      ws: spv_attention_backward_workspace_bytes(p, nq, nk, dt) bytes.
+ * Errors: as spv_attention.
+ */
+size_t spv_attention_workspace_bytes(const spv_attention_params* p, int64_t nq, int64_t nk, spv_dtype dt);
+spv_status spv_attention(void* stream, void* ws, size_t ws_bytes, const spv_attention_params* p,
+                         const void* q, int64_t ldq, int64_t nq, const void* k, int64_t ldk,
+                         const void* v, int64_t ldv, int64_t nk, void* out, int64_t ldo, float* lse, spv_dtype dt);
+size_t spv_attention_backward_workspace_bytes(const spv_attention_params* p, int64_t nq, int64_t nk, spv_dtype dt);
+spv_status spv_attention_backward(void* stream, void* ws, size_t ws_bytes, const spv_attention_params* p,
+                                  const void* q, int64_t ldq, int64_t nq, const void* k, int64_t ldk,
+                                  const void* v, int64_t ldv, int64_t nk, const void* out, int64_t ldo,
+                                  const float* lse, const void* dout, int64_t lddo, void* dq, int64_t lddq,
+                                  void* dk, int64_t lddk, void* dv, int64_t lddv, spv_dtype dt);
+
 /* Parameters of the SPVConv block (Fig. 2): voxel branch = voxelize, n_convs
  * submanifold 3x3x3 convs C->C, each act(scale * conv + shift); point branch =
  * act(scale_p * (f @ Wp) + shift_p); fused by addition after devoxelization. */

@@ -735,6 +735,157 @@ spv_status spv_linear_backward(void* stream, void* ws, size_t ws_bytes, const vo
     return hip_check();
 }
 
+spv_status spv_layer_norm(void* stream, const void* x, const int64_t* m_dev, int64_t m_cap, int32_t C,
+                          const float* gamma, const float* beta, float eps, void* out, spv_dtype dt) {
+    if (m_cap < 0 || m_cap >= ((int64_t)1 << 31) || C <= 0 || !valid_dt(dt) || !valid_v(eps))
+        return SPV_ERR_INVALID_ARG;
+    if (m_cap == 0) return SPV_OK;
+    if (!x || !out) return SPV_ERR_INVALID_ARG;
+    launch_layer_norm((hipStream_t)stream, NormArgs{x, m_dev, m_cap, C, (int)dt, gamma, beta, eps, out});
+    return hip_check();
+}
+
+size_t spv_layer_norm_backward_workspace_bytes(int64_t m_cap, int32_t C) {
+    if (m_cap < 0 || m_cap >= ((int64_t)1 << 31) || C <= 0) return 0;
+    Arena a(nullptr, 0);
+    plan_norm_ws(a, m_cap, C);
+    return a.used;
+}
+
+spv_status spv_layer_norm_backward(void* stream, void* ws, size_t ws_bytes, const void* dy, const void* x,
+                                   const int64_t* m_dev, int64_t m_cap, int32_t C, const float* gamma, float eps,
+                                   const void* dres, void* dx, float* dgamma, float* dbeta, spv_dtype dt) {
+    if (m_cap < 0 || m_cap >= ((int64_t)1 << 31) || C <= 0 || !valid_dt(dt) || !valid_v(eps))
+        return SPV_ERR_INVALID_ARG;
+    if (m_cap > 0 && (!dy || !x || (dx && dx == x))) return SPV_ERR_INVALID_ARG;
+    const bool sums = dgamma || dbeta;
+    NormWs w{nullptr, nullptr};
+    if (sums) {
+        if (!ws_ok(ws)) return SPV_ERR_INVALID_ARG;
+        if (need(spv_layer_norm_backward_workspace_bytes(m_cap, C), ws_bytes)) return SPV_ERR_CAPACITY;
+        Arena a(ws, ws_bytes);
+        w = plan_norm_ws(a, m_cap, C);
+    }
+    if (m_cap == 0 && !sums) return SPV_OK;
+    if (!dx && !sums) return SPV_OK;
+    launch_layer_norm_backward((hipStream_t)stream,
+                               NormBwdArgs{dy, x, m_dev, m_cap, C, (int)dt, gamma, eps, dres, dx, dgamma, dbeta}, w);
+    return hip_check();
+}
+
+// a row stride (in elements) that holds the row's channels and keeps every row 16-byte aligned
+static bool row_stride_ok(int64_t ld, int64_t channels, spv_dtype dt) {
+    return ld >= channels && ld % (int64_t)(16 / esize(dt)) == 0 && ld < ((int64_t)1 << 31);
+}
+
+// the checks of both directions; fills t with everything but the gradients
+static spv_status attention_args(const spv_attention_params* p, const void* q, int64_t ldq, int64_t nq, const void* k,
+                                 int64_t ldk, const void* v, int64_t ldv, int64_t nk, const void* out, int64_t ldo,
+                                 const float* lse, spv_dtype dt, AttnArgs& t) {
+    if (!p || !valid_dt(dt) || p->H <= 0 || p->Hkv <= 0 || p->H > 65535 || p->H % p->Hkv || p->D <= 0 || p->B < 0 ||
+        nq < 0 || nk < 0 || nq >= ((int64_t)1 << 31) || nk >= ((int64_t)1 << 31))
+        return SPV_ERR_INVALID_ARG;
+    if (!(p->scale >= 1e-9f && p->scale <= 1e9f) || !(p->cap == 0.f || (p->cap >= 1e-6f && p->cap <= 1e6f)))
+        return SPV_ERR_INVALID_ARG;
+    const bool bias = p->q_coords || p->k_coords || p->slopes;
+    if (p->B > 0 && (!p->q_off || !p->k_off)) return SPV_ERR_INVALID_ARG;
+    if (bias && (!p->slopes || (nq > 0 && !p->q_coords) || (nk > 0 && !p->k_coords))) return SPV_ERR_INVALID_ARG;
+    if (!aligned16(p->q_coords) || !aligned16(p->k_coords)) return SPV_ERR_INVALID_ARG;
+    if (p->D % 8 || p->D > 128) return SPV_ERR_UNSUPPORTED;
+    const int64_t hd = (int64_t)p->H * p->D, kd = (int64_t)p->Hkv * p->D;
+    if (!row_stride_ok(ldq, hd, dt) || !row_stride_ok(ldo, hd, dt) || !row_stride_ok(ldk, kd, dt) ||
+        !row_stride_ok(ldv, kd, dt))
+        return SPV_ERR_INVALID_ARG;
+    if ((nq > 0 && (!q || !out)) || (nk > 0 && (!k || !v))) return SPV_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return SPV_ERR_INVALID_ARG;
+    t = AttnArgs{};
+    t.q = q, t.k = k, t.v = v, t.out = const_cast<void*>(out), t.lse = const_cast<float*>(lse);
+    t.ldq = ldq, t.ldk = ldk, t.ldv = ldv, t.ldo = ldo, t.nq = nq, t.nk = nk;
+    t.q_off = p->q_off, t.k_off = p->k_off;
+    if (bias) t.q_coords = p->q_coords, t.k_coords = p->k_coords, t.slopes = p->slopes;
+    t.H = p->H, t.K = p->Hkv, t.D = p->D, t.B = p->B, t.dt = (int)dt, t.scale = p->scale, t.cap = p->cap;
+    return attention_supported(t) ? SPV_OK : SPV_ERR_UNSUPPORTED;
+}
+
+// sizes alone, for the workspace queries; false where the calls would refuse them
+static bool attention_sizes(const spv_attention_params* p, int64_t nq, int64_t nk, spv_dtype dt, AttnArgs& t) {
+    if (!p || !valid_dt(dt) || p->H <= 0 || p->Hkv <= 0 || p->H > 65535 || p->H % p->Hkv || p->D <= 0 || p->D % 8 ||
+        p->D > 128 || p->B < 0 || nq < 0 || nk < 0 || nq >= ((int64_t)1 << 31) || nk >= ((int64_t)1 << 31))
+        return false;
+    t = AttnArgs{};
+    t.nq = nq, t.nk = nk, t.H = p->H, t.K = p->Hkv, t.D = p->D, t.B = p->B, t.dt = (int)dt;
+    return attention_supported(t);
+}
+
+size_t spv_attention_workspace_bytes(const spv_attention_params* p, int64_t nq, int64_t nk, spv_dtype dt) {
+    AttnArgs t;
+    if (!attention_sizes(p, nq, nk, dt, t)) return 0;
+    Arena a(nullptr, 0);
+    plan_attention_ws(a, t);
+    return a.used;
+}
+
+spv_status spv_attention(void* stream, void* ws, size_t ws_bytes, const spv_attention_params* p, const void* q,
+                         int64_t ldq, int64_t nq, const void* k, int64_t ldk, const void* v, int64_t ldv, int64_t nk,
+                         void* out, int64_t ldo, float* lse, spv_dtype dt) {
+    AttnArgs t;
+    const spv_status st = attention_args(p, q, ldq, nq, k, ldk, v, ldv, nk, out, ldo, lse, dt, t);
+    if (st != SPV_OK) return st;
+    if (out && (out == q || out == k || out == v)) return SPV_ERR_INVALID_ARG;
+    Arena a(nullptr, 0);
+    plan_attention_ws(a, t);
+    if (a.used) {
+        if (!ws_ok(ws)) return SPV_ERR_INVALID_ARG;
+        if (need(a.used, ws_bytes)) return SPV_ERR_CAPACITY;
+        Arena b(ws, ws_bytes);
+        plan_attention_ws(b, t);
+    }
+    if (nq == 0 || t.B == 0) return SPV_OK;
+    launch_attention((hipStream_t)stream, t);
+    return hip_check();
+}
+
+size_t spv_attention_backward_workspace_bytes(const spv_attention_params* p, int64_t nq, int64_t nk, spv_dtype dt) {
+    AttnArgs t;
+    if (!attention_sizes(p, nq, nk, dt, t)) return 0;
+    Arena a(nullptr, 0);
+    plan_attention_backward_ws(a, t);
+    return a.used;
+}
+
+spv_status spv_attention_backward(void* stream, void* ws, size_t ws_bytes, const spv_attention_params* p,
+                                  const void* q, int64_t ldq, int64_t nq, const void* k, int64_t ldk, const void* v,
+                                  int64_t ldv, int64_t nk, const void* out, int64_t ldo, const float* lse,
+                                  const void* dout, int64_t lddo, void* dq, int64_t lddq, void* dk, int64_t lddk,
+                                  void* dv, int64_t lddv, spv_dtype dt) {
+    AttnArgs t;
+    const spv_status st = attention_args(p, q, ldq, nq, k, ldk, v, ldv, nk, out, ldo, lse, dt, t);
+    if (st != SPV_OK) return st;
+    if ((nq > 0 && (!dout || !lse || !dq)) || (nk > 0 && (!dk || !dv))) return SPV_ERR_INVALID_ARG;
+    if (!aligned16(dout) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv)) return SPV_ERR_INVALID_ARG;
+    const int64_t hd = (int64_t)t.H * t.D, kd = (int64_t)t.K * t.D;
+    if (!row_stride_ok(lddo, hd, dt) || !row_stride_ok(lddq, hd, dt) || !row_stride_ok(lddk, kd, dt) ||
+        !row_stride_ok(lddv, kd, dt))
+        return SPV_ERR_INVALID_ARG;
+    // both passes read every input, so no gradient may be one
+    for (const void* g : {(const void*)dq, (const void*)dk, (const void*)dv})
+        if (g && (g == q || g == k || g == v || g == out || g == dout)) return SPV_ERR_INVALID_ARG;
+    if ((dq && (dq == dk || dq == dv)) || (dk && dk == dv)) return SPV_ERR_INVALID_ARG;
+    t.dout = dout, t.dq = dq, t.dk = dk, t.dv = dv;
+    t.lddo = lddo, t.lddq = lddq, t.lddk = lddk, t.lddv = lddv;
+    Arena a(nullptr, 0);
+    plan_attention_backward_ws(a, t);
+    if (a.used) {
+        if (!ws_ok(ws)) return SPV_ERR_INVALID_ARG;
+        if (need(a.used, ws_bytes)) return SPV_ERR_CAPACITY;
+        Arena b(ws, ws_bytes);
+        plan_attention_backward_ws(b, t);
+    }
+    if (t.B == 0 || (nq == 0 && nk == 0)) return SPV_OK;
+    launch_attention_backward((hipStream_t)stream, t);
+    return hip_check();
+}
+
 size_t spv_devoxelize_backward_workspace_bytes(int64_t n, int64_t m) {
     if (n < 0 || m < 0) return 0;
     Arena a(nullptr, 0);

@@ -450,6 +450,63 @@ DvbWs plan_devox_backward_ws(Arena& a, int64_t n, int64_t m);
 void launch_devoxelize_backward(hipStream_t s, const DvbWs& w, const int32_t* cidx, const float* cw, const void* dout,
                                 int64_t n, int C, float* dv, int64_t m, int dt);
 
+// --- layer norm (norm.hip) -------------------------------------------------------
+struct NormArgs {
+    const void* x;          // [m][C]
+    const int64_t* m_dev;   // device row count (nullptr = m_cap)
+    int64_t m_cap;
+    int C, dt;
+    const float* gamma;     // [C] or nullptr (1)
+    const float* beta;      // [C] or nullptr (0)
+    float eps;
+    void* out;              // [m][C]
+};
+void launch_layer_norm(hipStream_t s, const NormArgs& a);
+struct NormBwdArgs {
+    const void* dy;         // [m][C]
+    const void* x;          // [m][C]
+    const int64_t* m_dev;
+    int64_t m_cap;
+    int C, dt;
+    const float* gamma;
+    float eps;
+    const void* dres;       // [m][C] or nullptr, added to dx
+    void* dx;               // [m][C] or nullptr
+    float* dgamma;          // [C] or nullptr
+    float* dbeta;           // [C] or nullptr
+};
+// the workgroups' column sums (float32) and the rows' statistics
+struct NormWs {
+    float* part;            // [workgroups][2][C]
+    float* stat;            // [m][2] mean and 1 / deviation
+};
+NormWs plan_norm_ws(Arena& a, int64_t m_cap, int C);
+void launch_layer_norm_backward(hipStream_t s, const NormBwdArgs& a, const NormWs& w);
+
+// --- attention over packed scans (attention.hip) ------------------------------------
+struct AttnArgs {
+    const void *q, *k, *v;      // [n][ld], head h at h * D
+    int64_t ldq, ldk, ldv, ldo; // row strides in elements
+    int64_t nq, nk;
+    const int32_t *q_off, *k_off;        // [B + 1] first row of each scan
+    const int32_t *q_coords, *k_coords;  // [n][4] or nullptr
+    const float* slopes;                 // [H]
+    int H, K, D, B, dt;                  // K key heads, H / K query heads on each
+    float scale, cap;
+    void* out;                  // [nq][ldo]; the backward's input
+    float* lse;                 // [nq][H] or nullptr
+    // backward
+    const void* dout;           // [nq][lddo]
+    void *dq, *dk, *dv;         // [n][lddq / lddk / lddv]
+    int64_t lddo, lddq, lddk, lddv;
+    float* delta;               // [nq][H] dout . out
+};
+bool attention_supported(const AttnArgs& a);
+void plan_attention_ws(Arena& a, AttnArgs& t);
+void launch_attention(hipStream_t s, const AttnArgs& a);
+void plan_attention_backward_ws(Arena& a, AttnArgs& t);
+void launch_attention_backward(hipStream_t s, const AttnArgs& a);
+
 // weight packings a block call runs inside its voxelization's first launch
 constexpr int kMaxPackJobs = 3;
 // the convolution itself (one kernel); wpack must have been packed from W

@@ -38,6 +38,9 @@ EXPORTS = ("spv_workspace_bytes", "spv_voxelize", "spv_voxelize_onto", "spv_pack
            "spv_devoxelize_backward_workspace_bytes", "spv_devoxelize_backward", "spv_devoxelize",
            "spv_epilogue_backward_workspace_bytes", "spv_epilogue_backward",
            "spv_linear_backward_workspace_bytes", "spv_linear_backward",
+           "spv_layer_norm", "spv_layer_norm_backward_workspace_bytes", "spv_layer_norm_backward",
+           "spv_attention_workspace_bytes", "spv_attention", "spv_attention_backward_workspace_bytes",
+           "spv_attention_backward",
            "spv_block_workspace_bytes", "spv_block", "spv_lookup", "spv_voxel_lookup", "spv_conv_kernel",
            "spv_sparse_conv_nbr_noalloc",
            "spv_block_conv_kernel", "spv_status_check", "spv_status_string", "spv_last_hip_error")
@@ -57,6 +60,12 @@ class BlockParams(ct.Structure):
                 ("relu_p", ct.c_int32), ("devox_mode", ct.c_int32), ("residual", ct.c_int32),
                 ("events", ct.POINTER(ct.c_void_p)),
                 ("n_events", ct.c_int32)]
+
+
+class AttentionParams(ct.Structure):
+    _fields_ = [("H", ct.c_int32), ("Hkv", ct.c_int32), ("D", ct.c_int32), ("B", ct.c_int32), ("scale", ct.c_float),
+                ("cap", ct.c_float), ("q_off", ct.c_void_p), ("k_off", ct.c_void_p), ("q_coords", ct.c_void_p),
+                ("k_coords", ct.c_void_p), ("slopes", ct.c_void_p)]
 
 
 _lib = None
@@ -111,6 +120,17 @@ def lib():
         L.spv_linear_backward_workspace_bytes.restype = sz
         L.spv_linear_backward.argtypes = [vp, vp, sz, vp, i64, i32, vp, i32, vp, vp, vp, i32]
         L.spv_devoxelize_backward_workspace_bytes.restype = sz
+        L.spv_layer_norm.argtypes = [vp, vp, vp, i64, i32, vp, vp, f32, vp, i32]
+        L.spv_layer_norm_backward_workspace_bytes.argtypes = [i64, i32]
+        L.spv_layer_norm_backward_workspace_bytes.restype = sz
+        L.spv_layer_norm_backward.argtypes = [vp, vp, sz, vp, vp, vp, i64, i32, vp, f32, vp, vp, vp, vp, i32]
+        ap = ct.POINTER(AttentionParams)
+        for f in ("spv_attention_workspace_bytes", "spv_attention_backward_workspace_bytes"):
+            getattr(L, f).argtypes = [ap, i64, i64, i32]
+            getattr(L, f).restype = sz
+        L.spv_attention.argtypes = [vp, vp, sz, ap, vp, i64, i64, vp, i64, vp, i64, i64, vp, i64, vp, i32]
+        L.spv_attention_backward.argtypes = [vp, vp, sz, ap, vp, i64, i64, vp, i64, vp, i64, i64, vp, i64, vp, vp, i64,
+                                             vp, i64, vp, i64, vp, i64, i32]
         L.spv_devoxelize.argtypes = [vp, vp, sz, vp, vp, i64, i32, vp, vp, i64, f32, i32, vp, i32, vp, i32, vp, vp,
                                      vp, i32, vp, i32, vp, vp]
         L.spv_devoxelize_nbr.argtypes = [vp, vp, sz, vp, vp, i64, vp, vp, i32, vp, vp, i64, f32, i32, vp, i32, vp,
@@ -134,6 +154,7 @@ def lib():
                   "spv_sparse_conv_dgrad", "spv_sparse_conv_dgrad_nbr", "spv_sparse_conv_wgrad",
                   "spv_voxelize_backward",
                   "spv_devoxelize_backward", "spv_epilogue_backward", "spv_linear_backward", "spv_devoxelize",
+                  "spv_layer_norm", "spv_layer_norm_backward", "spv_attention", "spv_attention_backward",
                   "spv_block", "spv_lookup", "spv_voxel_lookup",
                   "spv_sparse_conv_nbr_noalloc", "spv_status_check"):
             getattr(L, f).restype = ct.c_int
@@ -188,6 +209,21 @@ class Workspace:
     @classmethod
     def for_linear_backward(cls, Cin: int, Cout: int, device="cuda"):
         return cls(lib().spv_linear_backward_workspace_bytes(Cin, Cout), device)
+
+    @classmethod
+    def for_layer_norm_backward(cls, m: int, C: int, device="cuda"):
+        return cls(lib().spv_layer_norm_backward_workspace_bytes(m, C), device)
+
+    @classmethod
+    def for_attention(cls, params: "AttentionParams", nq: int, nk: int, dtype: torch.dtype, device="cuda"):
+        return cls(lib().spv_attention_workspace_bytes(ct.byref(params), nq, nk, _DT[dtype]), device)
+
+    @classmethod
+    def for_attention_backward(cls, params: "AttentionParams", nq: int, nk: int, dtype: torch.dtype, device="cuda"):
+        """Serves the forward call of the same sizes too."""
+        need = max(lib().spv_attention_workspace_bytes(ct.byref(params), nq, nk, _DT[dtype]),
+                   lib().spv_attention_backward_workspace_bytes(ct.byref(params), nq, nk, _DT[dtype]))
+        return cls(need, device)
 
     @classmethod
     def for_block(cls, max_points: int, C: int, device="cuda"):
@@ -595,6 +631,143 @@ def spv_linear_backward(ws: Workspace, x: torch.Tensor, W: torch.Tensor, da: tor
                                    _ptr(dW), _DT[x.dtype])
     _chk(st, "spv_linear_backward")
     return dx, dW
+
+
+def spv_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                   eps: float = 1e-5, m_dev: Optional[torch.Tensor] = None,
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """(x - mean) / sqrt(var + eps) * gamma + beta over the channels of each row of x [m][C]."""
+    m, C = x.shape
+    _check_vec(gamma, C, "gamma")
+    _check_vec(beta, C, "beta")
+    if out is None:
+        out = torch.empty((m, C), dtype=x.dtype, device=x.device)
+    elif out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("out must have x's shape and type")
+    st = lib().spv_layer_norm(_stream(), _ptr(x), _ptr(m_dev), m, C, _ptr(gamma), _ptr(beta), eps, _ptr(out),
+                              _DT[x.dtype])
+    _chk(st, "spv_layer_norm")
+    return out
+
+
+def spv_layer_norm_backward(ws: Workspace, dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                            eps: float = 1e-5, dres: Optional[torch.Tensor] = None,
+                            m_dev: Optional[torch.Tensor] = None):
+    """(dx, dgamma, dbeta) of spv_layer_norm; dres: a gradient added to dx (the residual branch's)."""
+    m, C = x.shape
+    _check_vec(gamma, C, "gamma")
+    for t, name in ((dy, "dy"), (dres, "dres")):
+        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
+            raise ValueError(f"{name} must have x's shape and type")
+    dx = torch.empty((m, C), dtype=x.dtype, device=x.device)
+    dg = torch.empty((2, C), dtype=torch.float32, device=x.device)
+    st = lib().spv_layer_norm_backward(_stream(), ws.ptr, ws.nbytes, _ptr(dy), _ptr(x), _ptr(m_dev), m, C, _ptr(gamma),
+                                       eps, _ptr(dres), _ptr(dx), _ptr(dg[0]), _ptr(dg[1]), _DT[x.dtype])
+    _chk(st, "spv_layer_norm_backward")
+    return dx, dg[0], dg[1]
+
+
+def _check_vec(t: Optional[torch.Tensor], C: int, name: str):
+    if t is not None and (t.dtype != torch.float32 or t.shape != (C,)):
+        raise ValueError(f"{name} must be float32 [{C}]")
+
+
+def make_attention_params(H: int, Hkv: int, D: int, q_off: torch.Tensor, k_off: Optional[torch.Tensor] = None,
+                          scale: Optional[float] = None, cap: float = 0.0, q_coords: Optional[torch.Tensor] = None,
+                          k_coords: Optional[torch.Tensor] = None,
+                          slopes: Optional[torch.Tensor] = None) -> AttentionParams:
+    """Parameters of an attention over packed scans: scan b's queries are rows q_off[b] .. q_off[b+1] - 1 and
+    its keys rows k_off[b] .. k_off[b+1] - 1 (int32 device tensors [B + 1]; k_off None: the queries' own).
+    scale None: 1 / sqrt(D).  With slopes [H] and the rows' voxel coordinates [n][4] (k_coords None: the
+    queries' own) a score falls by its head's slope times the L1 distance.
+
+    The struct holds raw device pointers; it also keeps references to every tensor it points into, so
+    they stay allocated as long as the struct lives."""
+    if k_off is None:
+        k_off = q_off
+    if slopes is not None and k_coords is None:
+        k_coords = q_coords
+    for t, name in ((q_off, "q_off"), (k_off, "k_off")):
+        if t.dtype != torch.int32 or t.dim() != 1 or t.shape != q_off.shape or t.shape[0] < 1:
+            raise ValueError(f"{name} must be int32 [scans + 1]")
+    for t, name in ((q_coords, "q_coords"), (k_coords, "k_coords")):
+        if (t is None) != (slopes is None):
+            raise ValueError("coordinates and slopes go together")
+        if t is not None and (t.dtype != torch.int32 or t.dim() != 2 or t.shape[1] != 4):
+            raise ValueError(f"{name} must be int32 [rows][4]")
+    _check_vec(slopes, H, "slopes")
+
+    def ptr(t):
+        return None if t is None else _ptr(t).value
+    p = AttentionParams(H, Hkv, D, q_off.shape[0] - 1, D ** -0.5 if scale is None else scale, cap, ptr(q_off),
+                        ptr(k_off), ptr(q_coords), ptr(k_coords), ptr(slopes))
+    p._keep = (q_off, k_off, q_coords, k_coords, slopes)
+    return p
+
+
+def _heads(t: torch.Tensor, heads: int, D: int, like: torch.Tensor, name: str):
+    """(pointer, row stride) of t [n][heads][D], whose rows may be parts of wider ones."""
+    n, h, d = t.shape
+    if h != heads or d != D or t.dtype != like.dtype:
+        raise ValueError(f"{name} must be [rows][{heads}][{D}] of q's type")
+    if not t.is_cuda:
+        raise ValueError("libspv takes device tensors")
+    s = t.stride()
+    if n and ((d > 1 and s[2] != 1) or (h > 1 and s[1] != d)):
+        raise ValueError(f"the channels of a row of {name} must be contiguous")
+    return t.data_ptr(), s[0] if n > 1 else h * d
+
+
+def _attention_tensors(p: AttentionParams, q, k, v):
+    if k.shape[0] != v.shape[0]:
+        raise ValueError("k and v must have the same rows")
+    for t, c, name in ((q, p._keep[2], "q_coords"), (k, p._keep[3], "k_coords")):
+        if c is not None and c.shape[0] < t.shape[0]:
+            raise ValueError(f"{name} must have a row for each of its side's")
+    return _heads(q, p.H, p.D, q, "q") + _heads(k, p.Hkv, p.D, q, "k") + _heads(v, p.Hkv, p.D, q, "v")
+
+
+def spv_attention(ws: Workspace, params: AttentionParams, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                  want_lse: bool = False, out: Optional[torch.Tensor] = None):
+    """Attention of q [nq][H][D] over k, v [nk][Hkv][D] of the same scan; with want_lse (out, lse [nq][H])."""
+    qp, ldq, kp, ldk, vp, ldv = _attention_tensors(params, q, k, v)
+    nq, nk = q.shape[0], k.shape[0]
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    op, ldo = _heads(out, params.H, params.D, q, "out")
+    if out.shape[0] != nq:
+        raise ValueError("out must have q's rows")
+    lse = torch.empty((nq, params.H), dtype=torch.float32, device=q.device) if want_lse else None
+    st = lib().spv_attention(_stream(), ws.ptr, ws.nbytes, ct.byref(params), qp, ldq, nq, kp, ldk, vp, ldv, nk, op, ldo,
+                             _ptr(lse), _DT[q.dtype])
+    _chk(st, "spv_attention")
+    return (out, lse) if want_lse else out
+
+
+def spv_attention_backward(ws: Workspace, params: AttentionParams, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                           out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                           grads: Optional[Sequence[torch.Tensor]] = None):
+    """(dq, dk, dv) of spv_attention, given its out and lse [nq][H] and the gradient dout of out; grads: the
+    tensors to write (which may be parts of one wider buffer), else new dense ones."""
+    qp, ldq, kp, ldk, vp, ldv = _attention_tensors(params, q, k, v)
+    nq, nk = q.shape[0], k.shape[0]
+    op, ldo = _heads(out, params.H, params.D, q, "out")
+    dop, lddo = _heads(dout, params.H, params.D, q, "dout")
+    if out.shape[0] != nq or dout.shape[0] != nq:
+        raise ValueError("out and dout must have q's rows")
+    if lse.dtype != torch.float32 or lse.shape != (nq, params.H):
+        raise ValueError("lse must be float32 [rows][heads]")
+    if grads is None:
+        grads = [torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v)]
+    elif any(g.shape[0] != t.shape[0] for g, t in zip(grads, (q, k, v))):
+        raise ValueError("the gradients must have their inputs' rows")
+    dq, lddq = _heads(grads[0], params.H, params.D, q, "dq")
+    dk, lddk = _heads(grads[1], params.Hkv, params.D, q, "dk")
+    dv, lddv = _heads(grads[2], params.Hkv, params.D, q, "dv")
+    st = lib().spv_attention_backward(_stream(), ws.ptr, ws.nbytes, ct.byref(params), qp, ldq, nq, kp, ldk, vp, ldv, nk,
+                                      op, ldo, _ptr(lse), dop, lddo, dq, lddq, dk, lddk, dv, lddv, _DT[q.dtype])
+    _chk(st, "spv_attention_backward")
+    return tuple(grads)
 
 
 def spv_devoxelize(ws: Workspace, grid_coords: torch.Tensor, vfeat: torch.Tensor, xyz: torch.Tensor,
