@@ -575,7 +575,7 @@ spv_status spv_devoxelize(void* stream, void* ws, size_t ws_bytes,
  *   out[i][c] = (x[i][c] - mu_i) * r_i * gamma[c] + beta[c],
  *   mu_i = mean_c x[i][c],  r_i = 1 / sqrt(mean_c (x[i][c] - mu_i)^2 + eps)
  * float32 statistics (the deviations are squared after the mean is taken off),
- * one rounding to dt.  A row of equal values gives beta.
+ * one rounding to dt.  A row of equal values gives beta, up to the mean's rounding.
  * In:  x [m_cap][C] (dt); m_dev: device row count (NULL = m_cap); gamma, beta
  *      [C] f32 or NULL (1, 0); eps > 0, finite.
  * Out: out [m_cap][C] (dt; rows < count written); may be x itself.

@@ -4,6 +4,8 @@
 //   dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy
 // The variance is the mean square of the deviations, taken after the mean: no
 // cancellation where a row sits far from zero.
+#include <type_traits>
+
 #include "conv_common.hpp"
 
 namespace spv {
@@ -78,8 +80,8 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_norm_bwd_any(NormBwdArgs a,
     }
 }
 
-// the column sums of 64 channels over a run of rows: part[blockIdx.x][2][C].  dx may
-// be dy itself, so this runs before k_norm_bwd_any overwrites it and forms xh from x.
+// the column sums of 64 channels over a run of rows: part[blockIdx.x][2][C].  It reads
+// dy, so it runs before k_norm_bwd_any writes dx, which may be dy.
 template <int DT>
 __global__ __launch_bounds__(64 * kNormWaves) void k_norm_cols_any(NormBwdArgs a, const float* stat, float* part) {
     __shared__ float red[kNormWaves][2][64];
@@ -105,32 +107,270 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_norm_cols_any(NormBwdArgs a
     }
 }
 
-// a thread per channel and half adds the workgroups' sums in order
-__global__ __launch_bounds__(64) void k_norm_join(const float* __restrict__ part, int nblk, int C,
-                                                  float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    const int c = blockIdx.x * 64 + threadIdx.x;
-    float* out = blockIdx.y ? dbeta : dgamma;
-    if (c >= C || !out) return;
-    double s = 0.0;
-    for (int b = 0; b < nblk; ++b) s += (double)part[((int64_t)b * 2 + blockIdx.y) * C + c];
-    out[c] = (float)s;
+// ---------------------------------------------------------------------------
+// 16 bytes at a time: L lanes hold a row, NV vectors of VEC channels each (vector v of lane l is number
+// v * L + l of the row), 64 / L rows a wave.  A row is read once: the mean, the deviations and, in the
+// backward, both of its means are formed in registers.  What bounds it is memory, so each wave's next rows
+// are loaded before the present ones are reduced, and gamma, beta and the column sums stay in registers
+// over a workgroup's rows.
+// ---------------------------------------------------------------------------
+template <int DT>
+constexpr int kVec = DT == SPV_F32 ? 4 : 8;
+
+template <int DT>
+__device__ inline void unpack(const uint4& u, float (&x)[kVec<DT>]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (DT == SPV_F32) {
+            x[j] = __uint_as_float(w[j]);
+        } else {
+            x[2 * j] = from16<DT>(w[j] & 0xFFFF);
+            x[2 * j + 1] = from16<DT>(w[j] >> 16);
+        }
+    }
+}
+template <int DT>
+__device__ inline uint4 pack(const float (&x)[kVec<DT>]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (DT == SPV_F32) w[j] = __float_as_uint(x[j]);
+        else w[j] = (uint32_t)to16<DT>(x[2 * j]) | ((uint32_t)to16<DT>(x[2 * j + 1]) << 16);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// sum over the L lanes of a row
+template <int L>
+__device__ inline float row_sum(float v) {
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) v += __shfl_xor(v, o, 64);
+    return v;
 }
 
-static unsigned norm_grid(int64_t m_cap) {
-    const int64_t g = (m_cap + kNormWaves - 1) / kNormWaves;
+template <int DT, int L, int NV>
+struct Rows {
+    static constexpr int V = kVec<DT>;
+    int l, nvec, C;
+    float inv;  // 1 / C
+    bool live[NV];
+    __device__ Rows(int lane, int C) : l(lane & (L - 1)), nvec(C / V), C(C), inv(1.f / (float)C) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) live[v] = v * L + l < nvec;
+    }
+    __device__ int chan(int v) const { return (v * L + l) * V; }
+    __device__ void load(const void* p, int64_t row, bool on, uint4 (&u)[NV]) const {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            u[v] = on && live[v] ? *(const uint4*)((const char*)p + (row * C + chan(v)) * (16 / V))
+                                 : make_uint4(0, 0, 0, 0);
+    }
+    __device__ void channels(const float* p, float other, float (&g)[NV][V]) const {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < V; ++e) g[v][e] = p && live[v] ? p[chan(v) + e] : other;
+    }
+    // x -> (x - mean) / deviation in place (0 in idle vectors); returns 1 / deviation
+    __device__ float normalize(float (&x)[NV][V], float eps) const {
+        float s = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < V; ++e) s += x[v][e];
+        const float mu = row_sum<L>(s) / (float)C;  // exact where the sum is
+        float ss = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                x[v][e] = live[v] ? x[v][e] - mu : 0.f;
+                ss = fmaf(x[v][e], x[v][e], ss);
+            }
+        const float r = 1.f / sqrtf(row_sum<L>(ss) * inv + eps);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[v][e] *= r;
+        return r;
+    }
+};
+
+template <int DT, int L, int NV>
+__global__ __launch_bounds__(64 * kNormWaves) void k_norm(NormArgs a) {
+    constexpr int V = kVec<DT>, R = 64 / L;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Rows<DT, L, NV> t(lane, a.C);
+    float g[NV][V], b[NV][V];
+    t.channels(a.gamma, 1.f, g);
+    t.channels(a.beta, 0.f, b);
+    const int64_t m = clamp_rows(a.m_dev, a.m_cap), step = (int64_t)gridDim.x * kNormWaves * R;
+    int64_t i = ((int64_t)blockIdx.x * kNormWaves + wave) * R + lane / L;
+    uint4 u[NV], nu[NV];
+    t.load(a.x, i, i < m, u);
+    // the row groups of a wave leave the loop together: the row sums take the whole wave
+    for (int64_t i0 = i - lane / L; i0 < m; i0 += step, i += step) {
+        t.load(a.x, i + step, i + step < m, nu);
+        float x[NV][V];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) unpack<DT>(u[v], x[v]);
+        t.normalize(x, a.eps);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[v][e] = fmaf(x[v][e], g[v][e], b[v][e]);
+            if (i < m && t.live[v]) *(uint4*)((char*)a.out + (i * a.C + t.chan(v)) * (16 / V)) = pack<DT>(x[v]);
+            u[v] = nu[v];
+        }
+    }
+}
+
+// dx, and (part given) the workgroup's column sums: each lane's over its rows in float32, then the lanes
+// of a channel in a fixed order
+template <int DT, int L, int NV>
+__global__ __launch_bounds__(64 * kNormWaves) void k_norm_bwd(NormBwdArgs a, float* part) {
+    constexpr int V = kVec<DT>, R = 64 / L;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Rows<DT, L, NV> t(lane, a.C);
+    float g[NV][V], sg[NV][V], sb[NV][V];
+    t.channels(a.gamma, 1.f, g);
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sg[v][e] = sb[v][e] = 0.f;
+    const int64_t m = clamp_rows(a.m_dev, a.m_cap), step = (int64_t)gridDim.x * kNormWaves * R;
+    int64_t i = ((int64_t)blockIdx.x * kNormWaves + wave) * R + lane / L;
+    uint4 ux[NV], ud[NV], ur[NV];
+    t.load(a.x, i, i < m, ux);
+    t.load(a.dy, i, i < m, ud);
+    for (int64_t i0 = i - lane / L; i0 < m; i0 += step, i += step) {
+        float x[NV][V], h[NV][V];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            unpack<DT>(ux[v], x[v]);
+            unpack<DT>(ud[v], h[v]);
+        }
+        if (a.dres) t.load(a.dres, i, i < m, ur);
+        t.load(a.x, i + step, i + step < m, ux);
+        t.load(a.dy, i + step, i + step < m, ud);
+        const float r = t.normalize(x, a.eps);
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                sg[v][e] = fmaf(h[v][e], x[v][e], sg[v][e]);  // a row past the end adds 0 * 0
+                sb[v][e] += h[v][e];
+                h[v][e] *= g[v][e];
+                s1 += h[v][e];
+                s2 = fmaf(h[v][e], x[v][e], s2);
+            }
+        if (!a.dx) continue;
+        s1 = row_sum<L>(s1) * t.inv;
+        s2 = row_sum<L>(s2) * t.inv;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float q[V] = {};
+            if (a.dres) unpack<DT>(ur[v], q);
+#pragma unroll
+            for (int e = 0; e < V; ++e) h[v][e] = fmaf(r, h[v][e] - s1 - x[v][e] * s2, q[e]);
+            if (i < m && t.live[v]) *(uint4*)((char*)a.dx + (i * a.C + t.chan(v)) * (16 / V)) = pack<DT>(h[v]);
+        }
+    }
+    if (!part) return;  // the whole workgroup
+    __shared__ float red[kNormWaves][2][L * NV * V];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+#pragma unroll
+            for (int o = L; o < 64; o <<= 1) {
+                sg[v][e] += __shfl_xor(sg[v][e], o, 64);
+                sb[v][e] += __shfl_xor(sb[v][e], o, 64);
+            }
+            if (lane < L) {
+                red[wave][0][t.chan(v) + e] = sg[v][e];
+                red[wave][1][t.chan(v) + e] = sb[v][e];
+            }
+        }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * a.C; c += 64 * kNormWaves) {
+        const int half = c >= a.C, cc = half ? c - a.C : c;
+        float s = red[0][half][cc];
+        for (int w = 1; w < kNormWaves; ++w) s += red[w][half][cc];
+        part[(int64_t)blockIdx.x * 2 * a.C + c] = s;
+    }
+}
+
+// adds the workgroups' column sums in 64 bits in a fixed order: 32 columns of part [nblk][cols] a workgroup,
+// each in 32 runs of consecutive workgroups
+__global__ __launch_bounds__(1024) void k_norm_join(const float* __restrict__ part, int nblk, int C,
+                                                    float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    __shared__ double red[32][33];
+    const int col = threadIdx.x & 31, run = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
+    const int len = (nblk + 31) / 32, b0 = run * len, b1 = b0 + len < nblk ? b0 + len : nblk;
+    double s = 0.0;
+    if (c < 2 * C)
+        for (int b = b0; b < b1; ++b) s += (double)part[(int64_t)b * 2 * C + c];
+    red[run][col] = s;
+    __syncthreads();
+    if (run || c >= 2 * C) return;
+    for (int q = 1; q < 32; ++q) s += red[q][col];
+    if (c < C) {
+        if (dgamma) dgamma[c] = (float)s;
+    } else if (dbeta) {
+        dbeta[c - C] = (float)s;
+    }
+}
+
+// workgroups, each with rows_wg rows at a time
+static unsigned norm_grid(int64_t m_cap, int rows_wg) {
+    const int64_t g = (m_cap + rows_wg - 1) / rows_wg;
     return (unsigned)(g < 1 ? 1 : g > kNormGrid ? kNormGrid : g);
 }
 
 NormWs plan_norm_ws(Arena& a, int64_t m_cap, int C) {
     NormWs w;
-    w.part = a.take<float>((size_t)norm_grid(m_cap) * 2 * (size_t)C);
+    w.part = a.take<float>((size_t)norm_grid(m_cap, kNormWaves) * 2 * (size_t)C);
     w.stat = a.take<float>((size_t)2 * (size_t)m_cap);
     return w;
 }
 
+// Calls f(L, NV) for the first shape of the list that holds the row's C / VEC vectors (the fewest idle ones), or
+// returns false where the vector kernel has none: unaligned rows, odd widths, over 256 vectors.
+template <int L, int NV>
+struct NormShape {
+    static constexpr int lanes = L, vectors = NV;
+};
+template <class F>
+static bool norm_pick(int, F&&) {
+    return false;
+}
+template <class S, class... More, class F>
+static bool norm_pick(int n, F&& f) {
+    if (n > S::lanes * S::vectors) return norm_pick<More...>(n, f);
+    f(std::integral_constant<int, S::lanes>{}, std::integral_constant<int, S::vectors>{});
+    return true;
+}
+template <int DT, class F>
+static bool norm_shape(int C, bool aligned, F&& f) {
+    if (!aligned || C % kVec<DT>) return false;
+    return norm_pick<NormShape<1, 1>, NormShape<2, 1>, NormShape<1, 3>, NormShape<4, 1>, NormShape<2, 3>,
+                     NormShape<8, 1>, NormShape<4, 3>, NormShape<16, 1>, NormShape<8, 3>, NormShape<32, 1>,
+                     NormShape<16, 3>, NormShape<64, 1>, NormShape<32, 3>, NormShape<64, 2>, NormShape<64, 3>,
+                     NormShape<64, 4>>(C / kVec<DT>, f);
+}
+static bool norm_aligned(const void* p, const void* q, const void* r = nullptr, const void* t = nullptr) {
+    return (((uintptr_t)p | (uintptr_t)q | (uintptr_t)r | (uintptr_t)t) & 15u) == 0;
+}
+
 template <int DT>
 static void norm_dt(hipStream_t s, const NormArgs& a) {
-    k_norm_any<DT><<<norm_grid(a.m_cap), 64 * kNormWaves, 0, s>>>(a);
+    const bool vec = norm_shape<DT>(a.C, norm_aligned(a.x, a.out), [&](auto l, auto nv) {
+        constexpr int L = decltype(l)::value, NV = decltype(nv)::value;
+        k_norm<DT, L, NV><<<norm_grid(a.m_cap, kNormWaves * (64 / L)), 64 * kNormWaves, 0, s>>>(a);
+    });
+    if (!vec) k_norm_any<DT><<<norm_grid(a.m_cap, kNormWaves), 64 * kNormWaves, 0, s>>>(a);
 }
 void launch_layer_norm(hipStream_t s, const NormArgs& a) {
     if (a.dt == SPV_F32) norm_dt<SPV_F32>(s, a);
@@ -140,17 +380,26 @@ void launch_layer_norm(hipStream_t s, const NormArgs& a) {
 
 template <int DT>
 static void norm_bwd_dt(hipStream_t s, const NormBwdArgs& a, const NormWs& w) {
-    const unsigned g = norm_grid(a.m_cap);
     const bool sums = a.dgamma || a.dbeta;
-    if (sums) {
-        // the statistics alone, then the column sums, then dx (which may overwrite dy)
-        NormBwdArgs st = a;
-        st.dx = nullptr;
-        k_norm_bwd_any<DT><<<g, 64 * kNormWaves, 0, s>>>(st, w.stat);
-        k_norm_cols_any<DT><<<dim3(g, (unsigned)((a.C + 63) / 64)), 64 * kNormWaves, 0, s>>>(a, w.stat, w.part);
-        k_norm_join<<<dim3((unsigned)((a.C + 63) / 64), 2), 64, 0, s>>>(w.part, (int)g, a.C, a.dgamma, a.dbeta);
+    unsigned g = 0;
+    const bool vec = norm_shape<DT>(a.C, norm_aligned(a.x, a.dy, a.dres, a.dx), [&](auto l, auto nv) {
+        constexpr int L = decltype(l)::value, NV = decltype(nv)::value;
+        g = norm_grid(a.m_cap, kNormWaves * (64 / L));
+        k_norm_bwd<DT, L, NV><<<g, 64 * kNormWaves, 0, s>>>(a, sums ? w.part : nullptr);
+    });
+    if (!vec) {
+        g = norm_grid(a.m_cap, kNormWaves);
+        if (sums) {
+            // the statistics alone, then the column sums, then dx (which may overwrite dy)
+            NormBwdArgs st = a;
+            st.dx = nullptr;
+            k_norm_bwd_any<DT><<<g, 64 * kNormWaves, 0, s>>>(st, w.stat);
+            k_norm_cols_any<DT><<<dim3(g, (unsigned)((a.C + 63) / 64)), 64 * kNormWaves, 0, s>>>(a, w.stat, w.part);
+        }
+        if (a.dx) k_norm_bwd_any<DT><<<g, 64 * kNormWaves, 0, s>>>(a, nullptr);
     }
-    if (a.dx) k_norm_bwd_any<DT><<<g, 64 * kNormWaves, 0, s>>>(a, nullptr);
+    if (sums)
+        k_norm_join<<<(unsigned)((2 * a.C + 31) / 32), 1024, 0, s>>>(w.part, (int)g, a.C, a.dgamma, a.dbeta);
 }
 void launch_layer_norm_backward(hipStream_t s, const NormBwdArgs& a, const NormWs& w) {
     if (a.dt == SPV_F32) norm_bwd_dt<SPV_F32>(s, a, w);
