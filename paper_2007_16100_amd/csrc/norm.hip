@@ -11,7 +11,8 @@
 namespace spv {
 
 constexpr int kNormWaves = 4;
-constexpr unsigned kNormGrid = 1024;  // workgroups at most (four per CU): their column sums are joined
+constexpr unsigned kNormGrid = 2048;    // workgroups of the forward at most
+constexpr unsigned kNormBwdGrid = 512;  // of the backward: two per CU, whose column sums are joined
 
 __device__ inline float wave_sum(float v) {
 #pragma unroll
@@ -136,7 +137,7 @@ __device__ inline uint4 pack(const float (&x)[kVec<DT>]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         if constexpr (DT == SPV_F32) w[j] = __float_as_uint(x[j]);
-        else w[j] = (uint32_t)to16<DT>(x[2 * j]) | ((uint32_t)to16<DT>(x[2 * j + 1]) << 16);
+        else w[j] = pack2<DT>(x[2 * j], x[2 * j + 1]);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
@@ -167,9 +168,11 @@ struct Rows {
     }
     __device__ void channels(const float* p, float other, float (&g)[NV][V]) const {
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+        for (int v = 0; v < NV; ++v) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) g[v][e] = p && live[v] ? p[chan(v) + e] : other;
+            for (int e = 0; e < V; ++e) g[v][e] = other;
+            if (p && live[v]) __builtin_memcpy(g[v], p + chan(v), sizeof(g[v]));
+        }
     }
     // x -> (x - mean) / deviation in place (0 in idle vectors); returns 1 / deviation
     __device__ float normalize(float (&x)[NV][V], float eps) const {
@@ -201,13 +204,13 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_norm(NormArgs a) {
     constexpr int V = kVec<DT>, R = 64 / L;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Rows<DT, L, NV> t(lane, a.C);
-    float g[NV][V], b[NV][V];
-    t.channels(a.gamma, 1.f, g);
-    t.channels(a.beta, 0.f, b);
     const int64_t m = clamp_rows(a.m_dev, a.m_cap), step = (int64_t)gridDim.x * kNormWaves * R;
     int64_t i = ((int64_t)blockIdx.x * kNormWaves + wave) * R + lane / L;
     uint4 u[NV], nu[NV];
     t.load(a.x, i, i < m, u);
+    float g[NV][V], b[NV][V];
+    t.channels(a.gamma, 1.f, g);
+    t.channels(a.beta, 0.f, b);
     // the row groups of a wave leave the loop together: the row sums take the whole wave
     for (int64_t i0 = i - lane / L; i0 < m; i0 += step, i += step) {
         t.load(a.x, i + step, i + step < m, nu);
@@ -302,20 +305,33 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_norm_bwd(NormBwdArgs a, flo
     }
 }
 
-// adds the workgroups' column sums in 64 bits in a fixed order: 32 columns of part [nblk][cols] a workgroup,
-// each in 32 runs of consecutive workgroups
+// adds the workgroups' column sums in 64 bits in a fixed order: 16 columns of part [nblk][cols] a workgroup,
+// each in 64 runs of consecutive workgroups, eight of a run's loads in flight
 __global__ __launch_bounds__(1024) void k_norm_join(const float* __restrict__ part, int nblk, int C,
                                                     float* __restrict__ dgamma, float* __restrict__ dbeta) {
-    __shared__ double red[32][33];
-    const int col = threadIdx.x & 31, run = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
-    const int len = (nblk + 31) / 32, b0 = run * len, b1 = b0 + len < nblk ? b0 + len : nblk;
+    __shared__ double red[64][17];
+    const int col = threadIdx.x & 15, run = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
+    const int len = (nblk + 63) / 64, b0 = run * len, b1 = b0 + len < nblk ? b0 + len : nblk;
     double s = 0.0;
     if (c < 2 * C)
-        for (int b = b0; b < b1; ++b) s += (double)part[(int64_t)b * 2 * C + c];
+        for (int b = b0; b < b1; b += 8) {
+            float f[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f[q] = b + q < b1 ? part[(int64_t)(b + q) * 2 * C + c] : 0.f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s += (double)f[q];
+        }
     red[run][col] = s;
     __syncthreads();
+    // eight runs of eight, then one of those
+    if (run < 8) {
+        s = red[run * 8][col];
+        for (int q = 1; q < 8; ++q) s += red[run * 8 + q][col];
+        red[run * 8][col] = s;
+    }
+    __syncthreads();
     if (run || c >= 2 * C) return;
-    for (int q = 1; q < 32; ++q) s += red[q][col];
+    for (int q = 1; q < 8; ++q) s += red[q * 8][col];
     if (c < C) {
         if (dgamma) dgamma[c] = (float)s;
     } else if (dbeta) {
@@ -324,14 +340,17 @@ __global__ __launch_bounds__(1024) void k_norm_join(const float* __restrict__ pa
 }
 
 // workgroups, each with rows_wg rows at a time
-static unsigned norm_grid(int64_t m_cap, int rows_wg) {
-    const int64_t g = (m_cap + rows_wg - 1) / rows_wg;
-    return (unsigned)(g < 1 ? 1 : g > kNormGrid ? kNormGrid : g);
+static unsigned norm_grid(int64_t m_cap, int rows_wg, unsigned most) {
+    const int64_t tiles = (m_cap + rows_wg - 1) / rows_wg;
+    if (tiles <= (int64_t)most) return (unsigned)(tiles < 1 ? 1 : tiles);
+    const int64_t rounds = (tiles + most - 1) / most;  // as many rounds with the fewest workgroups: none runs one more
+    return (unsigned)((tiles + rounds - 1) / rounds);
 }
 
 NormWs plan_norm_ws(Arena& a, int64_t m_cap, int C) {
     NormWs w;
-    w.part = a.take<float>((size_t)norm_grid(m_cap, kNormWaves) * 2 * (size_t)C);
+    const int64_t wgs = (m_cap + kNormWaves - 1) / kNormWaves;  // no kernel takes fewer rows a workgroup
+    w.part = a.take<float>((size_t)(wgs < 1 ? 1 : wgs > kNormBwdGrid ? kNormBwdGrid : wgs) * 2 * (size_t)C);
     w.stat = a.take<float>((size_t)2 * (size_t)m_cap);
     return w;
 }
@@ -368,9 +387,9 @@ template <int DT>
 static void norm_dt(hipStream_t s, const NormArgs& a) {
     const bool vec = norm_shape<DT>(a.C, norm_aligned(a.x, a.out), [&](auto l, auto nv) {
         constexpr int L = decltype(l)::value, NV = decltype(nv)::value;
-        k_norm<DT, L, NV><<<norm_grid(a.m_cap, kNormWaves * (64 / L)), 64 * kNormWaves, 0, s>>>(a);
+        k_norm<DT, L, NV><<<norm_grid(a.m_cap, kNormWaves * (64 / L), kNormGrid), 64 * kNormWaves, 0, s>>>(a);
     });
-    if (!vec) k_norm_any<DT><<<norm_grid(a.m_cap, kNormWaves), 64 * kNormWaves, 0, s>>>(a);
+    if (!vec) k_norm_any<DT><<<norm_grid(a.m_cap, kNormWaves, kNormGrid), 64 * kNormWaves, 0, s>>>(a);
 }
 void launch_layer_norm(hipStream_t s, const NormArgs& a) {
     if (a.dt == SPV_F32) norm_dt<SPV_F32>(s, a);
@@ -384,11 +403,11 @@ static void norm_bwd_dt(hipStream_t s, const NormBwdArgs& a, const NormWs& w) {
     unsigned g = 0;
     const bool vec = norm_shape<DT>(a.C, norm_aligned(a.x, a.dy, a.dres, a.dx), [&](auto l, auto nv) {
         constexpr int L = decltype(l)::value, NV = decltype(nv)::value;
-        g = norm_grid(a.m_cap, kNormWaves * (64 / L));
+        g = norm_grid(a.m_cap, kNormWaves * (64 / L), kNormBwdGrid);
         k_norm_bwd<DT, L, NV><<<g, 64 * kNormWaves, 0, s>>>(a, sums ? w.part : nullptr);
     });
     if (!vec) {
-        g = norm_grid(a.m_cap, kNormWaves);
+        g = norm_grid(a.m_cap, kNormWaves, kNormBwdGrid);
         if (sums) {
             // the statistics alone, then the column sums, then dx (which may overwrite dy)
             NormBwdArgs st = a;
@@ -399,7 +418,7 @@ static void norm_bwd_dt(hipStream_t s, const NormBwdArgs& a, const NormWs& w) {
         if (a.dx) k_norm_bwd_any<DT><<<g, 64 * kNormWaves, 0, s>>>(a, nullptr);
     }
     if (sums)
-        k_norm_join<<<(unsigned)((2 * a.C + 31) / 32), 1024, 0, s>>>(w.part, (int)g, a.C, a.dgamma, a.dbeta);
+        k_norm_join<<<(unsigned)((2 * a.C + 15) / 16), 1024, 0, s>>>(w.part, (int)g, a.C, a.dgamma, a.dbeta);
 }
 void launch_layer_norm_backward(hipStream_t s, const NormBwdArgs& a, const NormWs& w) {
     if (a.dt == SPV_F32) norm_bwd_dt<SPV_F32>(s, a, w);

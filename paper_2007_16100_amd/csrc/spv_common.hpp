@@ -260,6 +260,19 @@ __device__ inline uint16_t to16(float v) {
     if constexpr (DT == SPV_BF16) return f32_to_bf16(v);
     else return f32_to_f16(v);
 }
+// two values, round to nearest even, in one 32-bit word (low half first), in the hardware's conversions
+template <int DT>
+__device__ inline uint32_t pack2(float lo, float hi) {
+    typedef float f32x2_ __attribute__((ext_vector_type(2)));
+    const f32x2_ f{lo, hi};
+    if constexpr (DT == SPV_BF16) {
+        typedef __bf16 bf16x2_ __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_));
+    } else {
+        typedef _Float16 f16x2_ __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, f16x2_));
+    }
+}
 // fp64 -> fp32 rounding to odd: a following round-to-nearest-even to a format
 // with at most 22 fraction bits then rounds the fp64 value exactly once
 __device__ inline float f64_to_f32_odd(double d) {
