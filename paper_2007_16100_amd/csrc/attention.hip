@@ -1,208 +1,290 @@
-// attention.hip -- attention over packed scans and its backward:
+// attention.hip -- attention over packed scans, forward:
 //   s_ij = cap(scale q_i . k_j) - slope_h |c_i - c_j|_1,  j over the keys of i's scan,
-//   out_i = sum_j p_ij v_j,  p_ij = exp(s_ij - lse_i)
-// One wave per (row, head): a first version that is right for every shape.
-#include "conv_common.hpp"
+//   out_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(s_ij - m_i)
+// in one pass over the keys with a running reference m and a running sum.
+#include "attn_common.hpp"
 
 namespace spv {
 
-constexpr int kAttnWaves = 4;
+// Columns are (query, head of a key head's group) pairs, so shared key heads are staged once for all of their query
+// heads; a workgroup takes 32 NW columns of one scan and one key head.  Scores are kept in units of log 2 and
+// relative to the column's reference; the reference moves (and the sums are scaled) only when a score passes it by
+// more than kLead: weights of up to 2^kLead lose nothing in float32 sums or 16-bit weights, and after the first
+// tiles the reference hardly ever moves.
+constexpr float kLead = 8.f;
 
-__device__ inline int clamp_off(int32_t o, int64_t n) { return o < 0 ? 0 : (o > n ? (int)n : o); }
+template <int DT, int DP, int NW, bool BIAS, bool CAP>
+__global__ __launch_bounds__(64 * NW) void k_attn(AttnArgs a) {
+    using T = Tile<DT, DP>;
+    constexpr int KT = attn_rows(DT, DP), KS = KT / 32, TH = 64 * NW, BM = 32 * NW;
+    // the reference goes into the products' accumulator, where no tanh stands between them
+    constexpr bool FOLD = DT != SPV_F32 && !CAP;
+    __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
+    __shared__ __align__(16) uint32_t lc[2][2][BIAS ? KT : 4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
+    const int G = a.H / a.K, kh = (int)(blockIdx.x % (unsigned)a.K);
+    const ScanTile t = find_tile(a.q_off, a.B, a.nq, G, BM, blockIdx.x / (unsigned)a.K);
+    if (t.col0 >= t.cols) return;  // the whole workgroup
+    const int64_t k0 = uniform(clamp_off(a.k_off[t.b], a.nk)), k1 = uniform(clamp_off(a.k_off[t.b + 1], a.nk));
+    const int64_t tiles = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0, per = (tiles + gridDim.y - 1) / gridDim.y;
+    const int64_t t0 = blockIdx.y * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
-// the scan of a row of `off`'s side: the last b with off[b] <= row, or -1 when the row is in none
-__device__ inline int scan_of(const int32_t* off, int B, int64_t row) {
-    int lo = 0, hi = B;  // off[lo] <= row < off[hi]
-    if (row < off[0] || row >= off[B]) return -1;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (off[mid] <= row) lo = mid;
-        else hi = mid;
+    // the lane's column
+    const int64_t q0 = t.col0 / G;
+    const int x = (int)(t.col0 - q0 * G) + 32 * wave + c;
+    const bool live = t.col0 + 32 * wave + c < t.cols, busy = t.col0 + 32 * wave < t.cols;
+    const int64_t qi = t.first + q0 + x / G;
+    const int head = kh * G + x % G;
+    uint4 qf[T::NF];
+    T::load_cols(a.q, qi * a.ldq + (int64_t)head * a.D, live, a.D, h, qf);
+    const float cs = a.scale * kLog2e, inv_cs = 1.f / cs;
+    const float cz = CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
+    Voxel qc{0, 0};
+    float slope = 0.f, lift = 0.f;
+    if constexpr (BIAS) {
+        if (live) {
+            qc = voxel_of(*(const int4*)(a.q_coords + 4 * qi));
+            slope = a.slopes[head] * kLog2e;
+            lift = slope * 8388608.f;  // what 2^23 + distance brings too much
+        }
     }
-    return lo;
-}
 
-__device__ inline int voxel_coord(int c) { return c < kCoordMin ? kCoordMin : (c > kCoordMax ? kCoordMax : c); }
-__device__ inline float voxel_dist(const int32_t* a, const int32_t* b) {
-    int d = 0;
+    Stage<DT, DP, KT, TH> sk, sv;
+    int4 ck{0, 0, 0, 0};
+    auto load = [&](int64_t i) __attribute__((always_inline)) {
+        const int64_t r = k0 + i * KT;
+        sk.load(a.k, a.ldk, (int64_t)kh * a.D, r, k1, a.D, tid);
+        sv.load(a.v, a.ldv, (int64_t)kh * a.D, r, k1, a.D, tid);
+        if constexpr (BIAS)
+            if (tid < KT && r + tid < k1) ck = *(const int4*)(a.k_coords + 4 * (r + tid));
+    };
+    auto store = [&](int s) __attribute__((always_inline)) {
+        sk.store(lk[s], tid);
+        sv.store(lv[s], tid);
+        if constexpr (BIAS)
+            if (tid < KT) {
+                const Voxel v = voxel_of(ck);
+                lc[s][0][tid] = v.xy;
+                lc[s][1][tid] = v.z;
+            }
+    };
+
+    f32x16 o[T::NB];
 #pragma unroll
-    for (int e = 1; e < 4; ++e) d += abs(voxel_coord(a[e]) - voxel_coord(b[e]));
-    return (float)d;
+    for (int b = 0; b < T::NB; ++b) o[b] = f32x16{};
+    f32x16 ref{};      // -reference / cs in every register (FOLD)
+    float m = 0.f, l = 0.f;
+    if (t0 < t1) {
+        load(t0);
+        store(0);
+        if (t0 + 1 < t1) load(t0 + 1);
+    }
+    __syncthreads();
+    for (int64_t i = t0; i < t1; ++i) {
+        const int s = (int)(i - t0) & 1;
+        if (busy) {
+            f32x16 z[KS];
+#pragma unroll
+            for (int u = 0; u < KS; ++u) z[u] = T::rows_dot(lk[s] + 32 * u * T::LD, lane, qf, FOLD ? ref : f32x16{});
+            float d = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < KS; ++u)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t xy[4] = {}, zz[4] = {};
+                    if constexpr (BIAS) {
+                        const uint4 p = *(const uint4*)&lc[s][0][32 * u + 8 * q + 4 * h];
+                        const uint4 r = *(const uint4*)&lc[s][1][32 * u + 8 * q + 4 * h];
+                        xy[0] = p.x, xy[1] = p.y, xy[2] = p.z, xy[3] = p.w;
+                        zz[0] = r.x, zz[1] = r.y, zz[2] = r.z, zz[3] = r.w;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float b = 0.f;
+                        if constexpr (BIAS) b = fmaf(voxel_dist(xy[e], zz[e], qc.xy, qc.z), -slope, lift);
+                        float y = z[u][4 * q + e];
+                        if constexpr (CAP && DT == SPV_F32) {
+                            y = fmaf(cap2, tanhf(y * (a.scale / a.cap)), b - m);
+                        } else if constexpr (CAP) {
+                            // cap tanh(w) = cap - 2 cap / (exp(2 w) + 1)
+                            const float ex = __builtin_amdgcn_exp2f(y * cz);
+                            y = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(ex + 1.f), b + (cap2 - m));
+                        } else if constexpr (FOLD) {
+                            y = BIAS ? fmaf(y, cs, b) : y * cs;
+                        } else {
+                            y = fmaf(y, cs, b) - m;
+                        }
+                        z[u][4 * q + e] = y;
+                    }
+                }
+            if (k0 + (i + 1) * KT > k1) {  // keys past the scan's end
+                const int n = (int)(k1 - k0 - i * KT);
+#pragma unroll
+                for (int u = 0; u < KS; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (32 * u + 8 * (r / 4) + 4 * h + r % 4 >= n) z[u][r] = -INFINITY;
+            }
+#pragma unroll
+            for (int u = 0; u < KS; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) d = fmaxf(d, z[u][r]);
+            const bool first = i == t0;
+            if (first || __any(d > kLead)) {
+                d = half_max(d);
+                const float up = first || d > kLead ? d : 0.f;
+                const float f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
+                m += up;
+                l *= f;
+#pragma unroll
+                for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[b][r] *= f;
+#pragma unroll
+                for (int u = 0; u < KS; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) z[u][r] -= up;
+                if constexpr (FOLD)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) ref[r] = -m * inv_cs;
+            }
+#pragma unroll
+            for (int u = 0; u < KS; ++u) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) z[u][r] = __builtin_amdgcn_exp2f(z[u][r]);
+                const typename T::Weights w = T::weights(z[u]);
+                l = T::sum(w, l);
+                T::add_weighted(lv[s] + 32 * u * T::LD, lane, w, o);
+            }
+        }
+        if (i + 1 < t1) {
+            store(s ^ 1);
+            if (i + 2 < t1) load(i + 2);
+        }
+        __syncthreads();
+    }
+    l = half_sum(l);
+    if (!live) return;
+    const int64_t row = qi * a.H + head;
+    if (a.part) {
+        // one of gridDim.y parts: sums as they are, in float32
+        const int64_t at = (int64_t)blockIdx.y * a.nq * a.H + row;
+        if (h == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m, l);
+        if (l == 0.f) return;  // no key: not read
+        Tile<SPV_F32, DP>::store_cols(a.part, at * a.D, a.D, h, o, 1.f);
+        return;
+    }
+    T::store_cols(a.out, qi * a.ldo + (int64_t)head * a.D, a.D, h, o, tiles ? 1.f / l : 0.f);
+    if (a.lse && h == 0) a.lse[row] = tiles ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
+// the parts of a row, added in their order under the largest reference; four channels a thread
 template <int DT>
-__device__ inline float head_dot(const void* a, int64_t i, const void* b, int64_t j, int D) {
-    float s = 0.f;
-    for (int d = 0; d < D; ++d) s = fmaf(ld_feat<DT>(a, i + d), ld_feat<DT>(b, j + d), s);
+__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int parts) {
+    const int D4 = a.D / 4;
+    const int64_t id = blockIdx.x * (int64_t)256 + threadIdx.x, rows = a.nq * a.H, row = id / D4;
+    if (row >= rows) return;
+    const int d = (int)(id - row * D4) * 4;
+    const int64_t qi = row / a.H;
+    if (qi < a.q_off[0] || qi >= a.q_off[a.B]) return;  // a row of no scan
+    float m = -INFINITY;
+    for (int s = 0; s < parts; ++s) {
+        const float2 ml = *(const float2*)(a.part_ml + 2 * (s * rows + row));
+        if (ml.y != 0.f) m = fmaxf(m, ml.x);
+    }
+    float l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < parts; ++s) {
+        const float2 ml = *(const float2*)(a.part_ml + 2 * (s * rows + row));
+        if (ml.y == 0.f) continue;
+        const float f = __builtin_amdgcn_exp2f(ml.x - m);
+        const float4 p = *(const float4*)(a.part + (s * rows + row) * a.D + d);
+        l = fmaf(f, ml.y, l);
+        o.x = fmaf(f, p.x, o.x);
+        o.y = fmaf(f, p.y, o.y);
+        o.z = fmaf(f, p.z, o.z);
+        o.w = fmaf(f, p.w, o.w);
+    }
+    const float f = l != 0.f ? 1.f / l : 0.f;
+    const int64_t at = qi * a.ldo + (row - qi * a.H) * a.D + d;
+    if constexpr (DT == SPV_F32)
+        *(float4*)((float*)a.out + at) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+    else
+        *(uint2*)((uint16_t*)a.out + at) = make_uint2(pack2<DT>(o.x * f, o.y * f), pack2<DT>(o.z * f, o.w * f));
+    if (a.lse && d == 0) a.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+}
+
+// ---------------------------------------------------------------------------
+// host: the shape of a launch
+// ---------------------------------------------------------------------------
+static int attn_dp(int D) { return (D + 31) / 32 * 32; }
+
+// waves of a workgroup and parts of a scan's keys
+struct AttnShape {
+    int nw, parts;
+    int64_t tiles;
+};
+static AttnShape attn_shape(const AttnArgs& a) {
+    const int G = a.H / a.K, B = a.B < 1 ? 1 : a.B;
+    AttnShape s{4, 1, attn_tiles(a.nq, a.B, G, 128)};
+    // 128 columns a workgroup while that gives every CU one and the scans fill them
+    if (s.tiles * a.K < 256 || a.nq * G / B < 64) s = AttnShape{1, 1, attn_tiles(a.nq, a.B, G, 32)};
+    // keys in parts of at least four tiles (of the average scan) while there are under four waves a CU
+    const int KT = attn_rows(a.dt, attn_dp(a.D));
+    const int64_t wgs = s.tiles * a.K * s.nw, key_tiles = a.nk / B / KT;
+    if (s.nw == 1 && wgs < 1024) {
+        int64_t p = (2048 + wgs - 1) / (wgs < 1 ? 1 : wgs);
+        if (p > key_tiles / 4) p = key_tiles / 4;
+        if (p > 256) p = 256;
+        s.parts = p < 2 ? 1 : (int)p;
+    }
     return s;
 }
 
-// the score of query row i (head h) and key row j; *slope receives d score / d product
+constexpr int64_t kMaxWorkgroups = (int64_t)1 << 22;
+
+bool attention_supported(const AttnArgs& a) {
+    const int G = a.H / a.K;
+    return attn_tiles(a.nq, a.B, G, 32) * a.K <= kMaxWorkgroups && attn_tiles(a.nk, a.B, G, 32) * a.K <= kMaxWorkgroups;
+}
+
+void plan_attention_ws(Arena& a, AttnArgs& t) {
+    const AttnShape s = attn_shape(t);
+    if (s.parts < 2) return;
+    const size_t rows = (size_t)s.parts * (size_t)t.nq * (size_t)t.H;
+    t.part_ml = a.take<float>(2 * rows);
+    t.part = a.take<float>(rows * (size_t)t.D);
+}
+
+template <int DT, int DP, int NW>
+static void attn_launch(hipStream_t s, const AttnArgs& a, const AttnShape& sh) {
+    const dim3 g((unsigned)(sh.tiles * a.K), (unsigned)sh.parts);
+    if (a.slopes && a.cap > 0.f) k_attn<DT, DP, NW, true, true><<<g, 64 * NW, 0, s>>>(a);
+    else if (a.slopes) k_attn<DT, DP, NW, true, false><<<g, 64 * NW, 0, s>>>(a);
+    else if (a.cap > 0.f) k_attn<DT, DP, NW, false, true><<<g, 64 * NW, 0, s>>>(a);
+    else k_attn<DT, DP, NW, false, false><<<g, 64 * NW, 0, s>>>(a);
+}
+template <int DT, int DP>
+static void attn_dp_launch(hipStream_t s, const AttnArgs& a, const AttnShape& sh) {
+    if (sh.nw == 4) attn_launch<DT, DP, 4>(s, a, sh);
+    else attn_launch<DT, DP, 1>(s, a, sh);
+}
 template <int DT>
-__device__ inline float score(const AttnArgs& a, int64_t i, int64_t j, int h, float* slope) {
-    const int g = h / (a.H / a.K);
-    float z = a.scale * head_dot<DT>(a.q, i * a.ldq + (int64_t)h * a.D, a.k, j * a.ldk + (int64_t)g * a.D, a.D);
-    *slope = a.scale;
-    if (a.cap > 0.f) {
-        const float t = tanhf(z / a.cap);
-        z = a.cap * t;
-        *slope = a.scale * (1.f - t * t);
+static void attn_dt(hipStream_t s, const AttnArgs& a) {
+    const AttnShape sh = attn_shape(a);
+    switch (attn_dp(a.D)) {
+        case 32: attn_dp_launch<DT, 32>(s, a, sh); break;
+        case 64: attn_dp_launch<DT, 64>(s, a, sh); break;
+        case 96: attn_dp_launch<DT, 96>(s, a, sh); break;
+        case 128: attn_dp_launch<DT, 128>(s, a, sh); break;
     }
-    if (a.slopes) z -= a.slopes[h] * voxel_dist(a.q_coords + 4 * i, a.k_coords + 4 * j);
-    return z;
-}
-
-__device__ inline float wave_add(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-__device__ inline float wave_max(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
-}
-
-template <int DT>
-__global__ __launch_bounds__(64 * kAttnWaves) void k_attn(AttnArgs a) {
-    const int lane = threadIdx.x & 63, h = blockIdx.y, g = h / (a.H / a.K);
-    for (int64_t i = (int64_t)blockIdx.x * kAttnWaves + (threadIdx.x >> 6); i < a.nq;
-         i += (int64_t)gridDim.x * kAttnWaves) {
-        const int b = scan_of(a.q_off, a.B, i);
-        if (b < 0) continue;
-        const int64_t j0 = clamp_off(a.k_off[b], a.nk), j1 = clamp_off(a.k_off[b + 1], a.nk);
-        float m = -1e30f, l = 0.f, o0 = 0.f, o1 = 0.f;
-        for (int64_t j = j0; j < j1; j += 64) {
-            float sl;
-            const float s = j + lane < j1 ? score<DT>(a, i, j + lane, h, &sl) : -INFINITY;
-            const float mn = fmaxf(m, wave_max(s));
-            const float p = expf(s - mn), f = expf(m - mn);
-            m = mn;
-            l = l * f + wave_add(p);
-            o0 *= f;
-            o1 *= f;
-            const int n = (int)(j1 - j < 64 ? j1 - j : 64);
-            for (int u = 0; u < n; ++u) {
-                const float pu = __shfl(p, u, 64);
-                const int64_t t = (j + u) * a.ldv + (int64_t)g * a.D;
-                if (lane < a.D) o0 = fmaf(pu, ld_feat<DT>(a.v, t + lane), o0);
-                if (lane + 64 < a.D) o1 = fmaf(pu, ld_feat<DT>(a.v, t + lane + 64), o1);
-            }
-        }
-        const int64_t t = i * a.ldo + (int64_t)h * a.D;
-        const float f = l > 0.f || l != l ? 1.f / l : 0.f;
-        if (lane < a.D) st_feat<DT>(a.out, t + lane, o0 * f);
-        if (lane + 64 < a.D) st_feat<DT>(a.out, t + lane + 64, o1 * f);
-        if (a.lse && lane == 0) a.lse[i * a.H + h] = j1 > j0 ? m + logf(l) : -INFINITY;
-    }
-}
-
-template <int DT>
-__global__ __launch_bounds__(64 * kAttnWaves) void k_attn_dq(AttnArgs a) {
-    const int lane = threadIdx.x & 63, h = blockIdx.y, g = h / (a.H / a.K);
-    for (int64_t i = (int64_t)blockIdx.x * kAttnWaves + (threadIdx.x >> 6); i < a.nq;
-         i += (int64_t)gridDim.x * kAttnWaves) {
-        const int b = scan_of(a.q_off, a.B, i);
-        if (b < 0) continue;
-        const int64_t j0 = clamp_off(a.k_off[b], a.nk), j1 = clamp_off(a.k_off[b + 1], a.nk);
-        const int64_t to = i * a.ldo + (int64_t)h * a.D;
-        const int64_t td = i * a.lddo + (int64_t)h * a.D;
-        const float delta = head_dot<DT>(a.dout, td, a.out, to, a.D), lse = a.lse[i * a.H + h];
-        if (lane == 0) a.delta[i * a.H + h] = delta;
-        float o0 = 0.f, o1 = 0.f;
-        for (int64_t j = j0; j < j1; j += 64) {
-            float dz = 0.f;
-            if (j + lane < j1) {
-                float sl;
-                const float s = score<DT>(a, i, j + lane, h, &sl);
-                const float dp = head_dot<DT>(a.dout, td, a.v, (j + lane) * a.ldv + (int64_t)g * a.D, a.D);
-                dz = expf(s - lse) * (dp - delta) * sl;
-            }
-            const int n = (int)(j1 - j < 64 ? j1 - j : 64);
-            for (int u = 0; u < n; ++u) {
-                const float du = __shfl(dz, u, 64);
-                const int64_t t = (j + u) * a.ldk + (int64_t)g * a.D;
-                if (lane < a.D) o0 = fmaf(du, ld_feat<DT>(a.k, t + lane), o0);
-                if (lane + 64 < a.D) o1 = fmaf(du, ld_feat<DT>(a.k, t + lane + 64), o1);
-            }
-        }
-        const int64_t t = i * a.lddq + (int64_t)h * a.D;
-        if (lane < a.D) st_feat<DT>(a.dq, t + lane, o0);
-        if (lane + 64 < a.D) st_feat<DT>(a.dq, t + lane + 64, o1);
-    }
-}
-
-template <int DT>
-__global__ __launch_bounds__(64 * kAttnWaves) void k_attn_dkv(AttnArgs a) {
-    const int lane = threadIdx.x & 63, g = blockIdx.y, G = a.H / a.K;
-    for (int64_t j = (int64_t)blockIdx.x * kAttnWaves + (threadIdx.x >> 6); j < a.nk;
-         j += (int64_t)gridDim.x * kAttnWaves) {
-        const int b = scan_of(a.k_off, a.B, j);
-        if (b < 0) continue;
-        const int64_t i0 = clamp_off(a.q_off[b], a.nq), i1 = clamp_off(a.q_off[b + 1], a.nq);
-        const int64_t tv = j * a.ldv + (int64_t)g * a.D, tk = j * a.ldk + (int64_t)g * a.D;
-        float k0 = 0.f, k1 = 0.f, v0 = 0.f, v1 = 0.f;
-        for (int h = g * G; h < (g + 1) * G; ++h)
-            for (int64_t i = i0; i < i1; i += 64) {
-                float p = 0.f, dz = 0.f;
-                if (i + lane < i1) {
-                    float sl;
-                    const int64_t r = i + lane;
-                    p = expf(score<DT>(a, r, j, h, &sl) - a.lse[r * a.H + h]);
-                    dz = p * (head_dot<DT>(a.dout, r * a.lddo + (int64_t)h * a.D, a.v, tv, a.D) - a.delta[r * a.H + h]) *
-                         sl;
-                }
-                const int n = (int)(i1 - i < 64 ? i1 - i : 64);
-                for (int u = 0; u < n; ++u) {
-                    const float pu = __shfl(p, u, 64), du = __shfl(dz, u, 64);
-                    const int64_t to = (i + u) * a.lddo + (int64_t)h * a.D, tq = (i + u) * a.ldq + (int64_t)h * a.D;
-                    if (lane < a.D) {
-                        v0 = fmaf(pu, ld_feat<DT>(a.dout, to + lane), v0);
-                        k0 = fmaf(du, ld_feat<DT>(a.q, tq + lane), k0);
-                    }
-                    if (lane + 64 < a.D) {
-                        v1 = fmaf(pu, ld_feat<DT>(a.dout, to + lane + 64), v1);
-                        k1 = fmaf(du, ld_feat<DT>(a.q, tq + lane + 64), k1);
-                    }
-                }
-            }
-        const int64_t ok = j * a.lddk + (int64_t)g * a.D, ov = j * a.lddv + (int64_t)g * a.D;
-        if (lane < a.D) {
-            st_feat<DT>(a.dk, ok + lane, k0);
-            st_feat<DT>(a.dv, ov + lane, v0);
-        }
-        if (lane + 64 < a.D) {
-            st_feat<DT>(a.dk, ok + lane + 64, k1);
-            st_feat<DT>(a.dv, ov + lane + 64, v1);
-        }
-    }
-}
-
-bool attention_supported(const AttnArgs&) { return true; }
-void plan_attention_ws(Arena&, AttnArgs&) {}
-void plan_attention_backward_ws(Arena& a, AttnArgs& t) { t.delta = a.take<float>((size_t)t.nq * (size_t)t.H); }
-
-static unsigned attn_grid(int64_t n) {
-    const int64_t g = (n + kAttnWaves - 1) / kAttnWaves;
-    return (unsigned)(g > 65536 ? 65536 : g);
+    if (sh.parts > 1) k_attn_join<DT><<<blocks_for(a.nq * a.H * (a.D / 4), 256), 256, 0, s>>>(a, sh.parts);
 }
 
 void launch_attention(hipStream_t s, const AttnArgs& a) {
-    const dim3 g(attn_grid(a.nq), (unsigned)a.H);
-    if (a.dt == SPV_F32) k_attn<SPV_F32><<<g, 64 * kAttnWaves, 0, s>>>(a);
-    else if (a.dt == SPV_BF16) k_attn<SPV_BF16><<<g, 64 * kAttnWaves, 0, s>>>(a);
-    else k_attn<SPV_F16><<<g, 64 * kAttnWaves, 0, s>>>(a);
-}
-
-template <int DT>
-static void attn_bwd_dt(hipStream_t s, const AttnArgs& a) {
-    if (a.nq > 0) k_attn_dq<DT><<<dim3(attn_grid(a.nq), (unsigned)a.H), 64 * kAttnWaves, 0, s>>>(a);
-    if (a.nk > 0) k_attn_dkv<DT><<<dim3(attn_grid(a.nk), (unsigned)a.K), 64 * kAttnWaves, 0, s>>>(a);
-}
-void launch_attention_backward(hipStream_t s, const AttnArgs& a) {
-    if (a.dt == SPV_F32) attn_bwd_dt<SPV_F32>(s, a);
-    else if (a.dt == SPV_BF16) attn_bwd_dt<SPV_BF16>(s, a);
-    else attn_bwd_dt<SPV_F16>(s, a);
+    if (a.dt == SPV_F32) attn_dt<SPV_F32>(s, a);
+    else if (a.dt == SPV_BF16) attn_dt<SPV_BF16>(s, a);
+    else attn_dt<SPV_F16>(s, a);
 }
 
 }  // namespace spv

@@ -1,0 +1,264 @@
+// attn_common.hpp -- what the attention kernels share: matrix-core tiles of 32 rows by 32 columns, the staging of
+// rows in LDS, the scans' ranges and the scores.
+//
+// A wave owns 32 columns, one to each pair of lanes (c, c + 32), and takes 32 rows at a time from LDS as the A
+// operand.  The accumulator of a tile holds, in lane (c, h), rows 8 (i / 4) + 4 h + i % 4 of column c (i = 0 .. 15):
+// sums and maxima down a column stay in a lane and one exchange between the halves.  Those same registers are the
+// B operand of the product that follows (weights times values): the k index of a product may be numbered in any
+// order as long as both operands agree, so k slot (h, j) is given the row that lane half h already holds, and the A
+// operand is gathered to match by transposing LDS reads (16-bit types: ds_read_b64_tr_b16 hands each lane four
+// rows of one channel) or plain ones (float32).  Weights never move between lanes.
+#pragma once
+
+#include "conv_common.hpp"
+
+namespace spv {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ inline int64_t clamp_off(int32_t o, int64_t n) { return o < 0 ? 0 : ((int64_t)o > n ? n : (int64_t)o); }
+
+// wave-uniform values, in scalar registers
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline int64_t uniform(int64_t v) {
+    return (int64_t)(((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32) | (uint32_t)uniform((int)v));
+}
+
+// The tiles of a side: scan b's rows * per columns are cut into tiles of BM from its own start, and its first tile
+// is number floor(off[b] * per / BM) + b: ascending in b, with room for every scan's tiles and known without a
+// pass over the scans.  attn_tiles bounds their number.
+__device__ inline int64_t scan_tile(const int32_t* off, int b, int64_t n, int per, int BM) {
+    return clamp_off(off[b], n) * per / BM + b;
+}
+inline int64_t attn_tiles(int64_t n, int B, int per, int BM) { return n * per / BM + B; }
+
+struct ScanTile {
+    int b;           // scan
+    int64_t first;   // its first row
+    int64_t cols;    // its columns (rows * per)
+    int64_t col0;    // the tile's first column; at least cols: nothing to do
+};
+// the scan of tile t: a search with 64 probes a step
+__device__ inline ScanTile find_tile(const int32_t* off, int B, int64_t n, int per, int BM, int64_t t) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = B;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) >> 6, at = lo + step * lane;
+        const bool le = at < hi && scan_tile(off, at, n, per, BM) <= t;
+        const int k = __popcll(__ballot(le));
+        lo += step * (k > 0 ? k - 1 : 0);
+        hi = lo + step < hi ? lo + step : hi;
+    }
+    ScanTile s;
+    s.b = uniform(lo);
+    s.first = uniform(clamp_off(off[s.b], n));
+    const int64_t end = uniform(clamp_off(off[s.b + 1], n)), mine = t - uniform(scan_tile(off, s.b, n, per, BM));
+    s.cols = end > s.first ? (end - s.first) * per : 0;
+    s.col0 = mine >= 0 ? mine * BM : s.cols;
+    return s;
+}
+
+// the voxels' L1 distance: 16-bit coordinates in two words, so that a score's distance is two sums of absolute
+// differences onto the bits of 2^23, which read as a float are 2^23 + distance
+struct Voxel {
+    uint32_t xy, z;
+};
+constexpr uint32_t kDistBits = 0x4B000000u;  // 2^23
+__device__ inline uint32_t voxel_coord(int c) {
+    return (uint32_t)((c < kCoordMin ? kCoordMin : (c > kCoordMax ? kCoordMax : c)) + 32768);
+}
+__device__ inline Voxel voxel_of(const int4& c) {
+    return Voxel{voxel_coord(c.y) | (voxel_coord(c.z) << 16), voxel_coord(c.w)};
+}
+__device__ inline float voxel_dist(uint32_t axy, uint32_t az, uint32_t bxy, uint32_t bz) {
+    return __uint_as_float(__builtin_amdgcn_sad_u16(az, bz, __builtin_amdgcn_sad_u16(axy, bxy, kDistBits)));
+}
+
+// the other half's value of a column: (max, sum) over both
+__device__ inline f32x2 both_halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f32x2{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ inline float half_sum(float v) {
+    const f32x2 r = both_halves(v);
+    return r.x + r.y;
+}
+__device__ inline float half_max(float v) {
+    const f32x2 r = both_halves(v);
+    return fmaxf(r.x, r.y);
+}
+
+// Rows of up to DP channels (a multiple of 32; D <= DP of them real, the rest zero) in LDS, and products with them.
+template <int DT, int DP>
+struct Tile {
+    static constexpr bool W = DT == SPV_F32;
+    static constexpr int SZ = W ? 4 : 2;       // bytes of an element
+    static constexpr int E = 16 / SZ;          // elements of 16 bytes
+    static constexpr int LD = DP * SZ + 16;    // bytes from row to row: 16 of padding spread the rows over the banks
+    static constexpr int NF = DP / (2 * E);    // 16-byte fragments of a row that a lane holds
+    static constexpr int CH = DP / E;          // 16-byte chunks of a row
+    static constexpr int NB = DP / 32;         // blocks of 32 channels
+
+    // B operand: a lane's fragments of its column's row (channels 2 E s + E h ..), zeros past D
+    static __device__ inline void load_cols(const void* p, int64_t at, bool live, int D, int h, uint4 (&f)[NF]) {
+#pragma unroll
+        for (int s = 0; s < NF; ++s) {
+            const int d = 2 * E * s + E * h;
+            f[s] = live && d < D ? *(const uint4*)((const char*)p + (at + d) * SZ) : make_uint4(0, 0, 0, 0);
+        }
+    }
+
+    // c + rows (32 of them, at lds) . columns
+    static __device__ inline f32x16 rows_dot(const char* lds, int lane, const uint4 (&f)[NF], f32x16 c) {
+        const char* a = lds + (lane & 31) * LD + (lane >> 5) * 16;
+#pragma unroll
+        for (int s = 0; s < NF; ++s) {
+            const uint4 x = *(const uint4*)(a + 32 * s);
+            if constexpr (W) {
+                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.x), __uint_as_float(f[s].x), c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.y), __uint_as_float(f[s].y), c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.z), __uint_as_float(f[s].z), c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.w), __uint_as_float(f[s].w), c, 0, 0, 0);
+            } else if constexpr (DT == SPV_BF16) {
+                c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
+                                                            __builtin_bit_cast(bf16x8, f[s]), c, 0, 0, 0);
+            } else {
+                c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x),
+                                                           __builtin_bit_cast(f16x8, f[s]), c, 0, 0, 0);
+            }
+        }
+        return c;
+    }
+
+    // the weights of 32 rows (accumulator registers) as B operands
+    struct Weights {
+        uint4 f[W ? 4 : 2];
+    };
+    static __device__ inline Weights weights(const f32x16& p) {
+        Weights w;
+        if constexpr (W) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                w.f[t] = make_uint4(__float_as_uint(p[4 * t]), __float_as_uint(p[4 * t + 1]),
+                                    __float_as_uint(p[4 * t + 2]), __float_as_uint(p[4 * t + 3]));
+        } else {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                w.f[t] = make_uint4(pack2<DT>(p[8 * t], p[8 * t + 1]), pack2<DT>(p[8 * t + 2], p[8 * t + 3]),
+                                    pack2<DT>(p[8 * t + 4], p[8 * t + 5]), pack2<DT>(p[8 * t + 6], p[8 * t + 7]));
+        }
+        return w;
+    }
+    // s + the sum of the lane's 16 weights as they are multiplied
+    static __device__ inline float sum(const Weights& w, float s) {
+#pragma unroll
+        for (int t = 0; t < (W ? 4 : 2); ++t) {
+            const uint32_t u[4] = {w.f[t].x, w.f[t].y, w.f[t].z, w.f[t].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (W)
+                    s += __uint_as_float(u[e]);
+                else if constexpr (DT == SPV_BF16)
+                    s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, u[e]),
+                                                        __builtin_bit_cast(bf16x2, 0x3F803F80u), s, false);
+                else
+                    s = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, u[e]), __builtin_bit_cast(f16x2, 0x3C003C00u),
+                                               s, false);
+            }
+        }
+        return s;
+    }
+
+    // o[b] + (channels 32 b .. 32 b + 31 of the 32 rows at lds, transposed) . weights: lane (c, h) of o[b] holds
+    // channels 32 b + 8 (i / 4) + 4 h + i % 4 of column c
+    static __device__ inline void add_weighted(const char* lds, int lane, const Weights& w, f32x16 (&o)[NB]) {
+        if constexpr (W) {
+            const char* a = lds + (lane >> 5) * 4 * LD + (lane & 31) * 4;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t u[4] = {w.f[i / 4].x, w.f[i / 4].y, w.f[i / 4].z, w.f[i / 4].w};
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float*)(a + (8 * (i / 4) + i % 4) * LD + 128 * b),
+                                                                __uint_as_float(u[i % 4]), o[b], 0, 0, 0);
+            }
+        } else {
+            // lanes 16 g .. 16 g + 15 read four rows of 16 channels, and each gets its channel of the four
+            const int t = lane & 15, g = lane >> 4;
+            const char* a = lds + (4 * (g >> 1) + (t >> 2)) * LD + (16 * (g & 1) + 4 * (t & 3)) * 2;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    typedef __attribute__((address_space(3))) i16x4 lds4;
+                    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds4*)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)(a + 16 * k * LD + 64 * b));
+                    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds4*)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)(a + (16 * k + 8) * LD + 64 * b));
+                    typedef short i16x8 __attribute__((ext_vector_type(8)));
+                    const i16x8 x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    if constexpr (DT == SPV_BF16)
+                        o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
+                                                                       __builtin_bit_cast(bf16x8, w.f[k]), o[b], 0, 0, 0);
+                    else
+                        o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x),
+                                                                      __builtin_bit_cast(f16x8, w.f[k]), o[b], 0, 0, 0);
+                }
+        }
+    }
+
+    // a lane's sums of its column, times f, to channels of row `at` (elements) of dst
+    static __device__ inline void store_cols(void* dst, int64_t at, int D, int h, const f32x16 (&o)[NB], float f) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int d = 32 * b + 8 * q + 4 * h;
+                if (d >= D) continue;
+                char* p = (char*)dst + (at + d) * SZ;
+                if constexpr (W)
+                    *(float4*)p = make_float4(o[b][4 * q] * f, o[b][4 * q + 1] * f, o[b][4 * q + 2] * f,
+                                              o[b][4 * q + 3] * f);
+                else
+                    *(uint2*)p = make_uint2(pack2<DT>(o[b][4 * q] * f, o[b][4 * q + 1] * f),
+                                            pack2<DT>(o[b][4 * q + 2] * f, o[b][4 * q + 3] * f));
+            }
+    }
+};
+
+// KT rows of DP channels on their way from memory to LDS by TH threads: loaded to registers a tile ahead, zeros for
+// rows past `end` and channels past D
+template <int DT, int DP, int KT, int TH>
+struct Stage {
+    using T = Tile<DT, DP>;
+    static constexpr int N = KT * T::CH / TH;
+    static_assert(KT * T::CH % TH == 0, "every thread moves as many chunks");
+    uint4 u[N];
+    __device__ inline void load(const void* p, int64_t ld, int64_t head, int64_t row0, int64_t end, int D, int tid) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int id = tid + i * TH, r = id / T::CH, ch = id % T::CH;
+            u[i] = row0 + r < end && ch * T::E < D
+                       ? *(const uint4*)((const char*)p + ((row0 + r) * ld + head + ch * T::E) * T::SZ)
+                       : make_uint4(0, 0, 0, 0);
+        }
+    }
+    __device__ inline void store(char* lds, int tid) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int id = tid + i * TH;
+            *(uint4*)(lds + (id / T::CH) * T::LD + (id % T::CH) * 16) = u[i];
+        }
+    }
+};
+
+// rows that the kernels stage at a time
+constexpr int attn_rows(int dt, int DP) { return dt == SPV_F32 || DP > 96 ? 32 : 64; }
+
+}  // namespace spv
