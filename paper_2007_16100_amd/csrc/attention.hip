@@ -13,10 +13,14 @@ namespace spv {
 // tiles the reference hardly ever moves.
 constexpr float kLead = 8.f;
 
+
+// waves per SIMD that the registers have to leave room for
+constexpr int attn_waves(int dt, int DP, int nw) { return nw == 1 || dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? 4 : 3; }
+
 template <int DT, int DP, int NW, bool BIAS, bool CAP>
-__global__ __launch_bounds__(64 * NW) void k_attn(AttnArgs a) {
+__global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnArgs a) {
     using T = Tile<DT, DP>;
-    constexpr int KT = attn_rows(DT, DP), KS = KT / 32, TH = 64 * NW, BM = 32 * NW;
+    constexpr int KT = attn_rows(DT, DP), KS = KT / 32, TH = 64 * NW, CB = 1, WC = 32 * CB, BM = WC * NW;
     // the reference goes into the products' accumulator, where no tanh stands between them
     constexpr bool FOLD = DT != SPV_F32 && !CAP;
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
@@ -29,23 +33,30 @@ __global__ __launch_bounds__(64 * NW) void k_attn(AttnArgs a) {
     const int64_t tiles = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0, per = (tiles + gridDim.y - 1) / gridDim.y;
     const int64_t t0 = blockIdx.y * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
-    // the lane's column
-    const int64_t q0 = t.col0 / G;
-    const int x = (int)(t.col0 - q0 * G) + 32 * wave + c;
-    const bool live = t.col0 + 32 * wave + c < t.cols, busy = t.col0 + 32 * wave < t.cols;
-    const int64_t qi = t.first + q0 + x / G;
-    const int head = kh * G + x % G;
-    uint4 qf[T::NF];
-    T::load_cols(a.q, qi * a.ldq + (int64_t)head * a.D, live, a.D, h, qf);
+    // the lane's columns
     const float cs = a.scale * kLog2e, inv_cs = 1.f / cs;
     const float cz = CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
-    Voxel qc{0, 0};
-    float slope = 0.f, lift = 0.f;
-    if constexpr (BIAS) {
-        if (live) {
-            qc = voxel_of(*(const int4*)(a.q_coords + 4 * qi));
-            slope = a.slopes[head] * kLog2e;
-            lift = slope * 8388608.f;  // what 2^23 + distance brings too much
+    const bool busy = t.col0 + WC * wave < t.cols;
+    const int64_t q0 = t.col0 / G;
+    int64_t qi[CB];
+    int head[CB];
+    bool live[CB];
+    uint4 qf[CB][T::NF];
+    Voxel qc[CB];
+    float slope[CB], lift[CB];  // lift: what the 2^23 of a distance brings too much
+#pragma unroll
+    for (int n = 0; n < CB; ++n) {
+        const int x = WC * wave + 32 * n + c, y = (int)(t.col0 - q0 * G) + x;
+        live[n] = t.col0 + x < t.cols;
+        qi[n] = t.first + q0 + y / G;
+        head[n] = kh * G + y % G;
+        T::load_cols(a.q, qi[n] * a.ldq + (int64_t)head[n] * a.D, live[n], a.D, h, qf[n]);
+        qc[n] = Voxel{0, 0};
+        slope[n] = lift[n] = 0.f;
+        if (BIAS && live[n]) {
+            qc[n] = voxel_of(*(const int4*)(a.q_coords + 4 * qi[n]));
+            slope[n] = a.slopes[head[n]] * kLog2e;
+            lift[n] = slope[n] * 8388608.f;
         }
     }
 
@@ -69,11 +80,15 @@ __global__ __launch_bounds__(64 * NW) void k_attn(AttnArgs a) {
             }
     };
 
-    f32x16 o[T::NB];
+    f32x16 o[CB][T::NB], ref[CB];  // ref: -reference / cs in every register (FOLD)
+    float m[CB], l[CB];
 #pragma unroll
-    for (int b = 0; b < T::NB; ++b) o[b] = f32x16{};
-    f32x16 ref{};      // -reference / cs in every register (FOLD)
-    float m = 0.f, l = 0.f;
+    for (int n = 0; n < CB; ++n) {
+#pragma unroll
+        for (int b = 0; b < T::NB; ++b) o[n][b] = f32x16{};
+        ref[n] = f32x16{};
+        m[n] = l[n] = 0.f;
+    }
     if (t0 < t1) {
         load(t0);
         store(0);
@@ -83,77 +98,97 @@ __global__ __launch_bounds__(64 * NW) void k_attn(AttnArgs a) {
     for (int64_t i = t0; i < t1; ++i) {
         const int s = (int)(i - t0) & 1;
         if (busy) {
-            f32x16 z[KS];
+            f32x16 z[KS][CB];
+            float d[CB];
 #pragma unroll
-            for (int u = 0; u < KS; ++u) z[u] = T::rows_dot(lk[s] + 32 * u * T::LD, lane, qf, FOLD ? ref : f32x16{});
-            float d = -INFINITY;
+            for (int u = 0; u < KS; ++u) {
+#pragma unroll
+                for (int n = 0; n < CB; ++n) z[u][n] = FOLD ? ref[n] : f32x16{};
+                T::rows_dot(lk[s] + 32 * u * T::LD, lane, qf, z[u]);
+            }
 #pragma unroll
             for (int u = 0; u < KS; ++u)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     uint32_t xy[4] = {}, zz[4] = {};
                     if constexpr (BIAS) {
-                        const uint4 p = *(const uint4*)&lc[s][0][32 * u + 8 * q + 4 * h];
-                        const uint4 r = *(const uint4*)&lc[s][1][32 * u + 8 * q + 4 * h];
-                        xy[0] = p.x, xy[1] = p.y, xy[2] = p.z, xy[3] = p.w;
-                        zz[0] = r.x, zz[1] = r.y, zz[2] = r.z, zz[3] = r.w;
+                        lds_words(&lc[s][0][32 * u + 8 * q + 4 * h], xy);
+                        lds_words(&lc[s][1][32 * u + 8 * q + 4 * h], zz);
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float b = 0.f;
-                        if constexpr (BIAS) b = fmaf(voxel_dist(xy[e], zz[e], qc.xy, qc.z), -slope, lift);
-                        float y = z[u][4 * q + e];
-                        if constexpr (CAP && DT == SPV_F32) {
-                            y = fmaf(cap2, tanhf(y * (a.scale / a.cap)), b - m);
-                        } else if constexpr (CAP) {
-                            // cap tanh(w) = cap - 2 cap / (exp(2 w) + 1)
-                            const float ex = __builtin_amdgcn_exp2f(y * cz);
-                            y = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(ex + 1.f), b + (cap2 - m));
-                        } else if constexpr (FOLD) {
-                            y = BIAS ? fmaf(y, cs, b) : y * cs;
-                        } else {
-                            y = fmaf(y, cs, b) - m;
+                    for (int n = 0; n < CB; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float b = 0.f;
+                            if constexpr (BIAS)
+                                b = fmaf(voxel_dist(xy[e], zz[e], qc[n].xy, qc[n].z), -slope[n], lift[n]);
+                            float y = z[u][n][4 * q + e];
+                            if constexpr (CAP && DT == SPV_F32) {
+                                y = fmaf(cap2, tanhf(y * (a.scale / a.cap)), b - m[n]);
+                            } else if constexpr (CAP) {
+                                // cap tanh(w) = cap - 2 cap / (exp(2 w) + 1)
+                                const float ex = __builtin_amdgcn_exp2f(y * cz);
+                                y = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(ex + 1.f), b + (cap2 - m[n]));
+                            } else if constexpr (FOLD) {
+                                y = BIAS ? fmaf(y, cs, b) : y * cs;
+                            } else {
+                                y = fmaf(y, cs, b) - m[n];
+                            }
+                            z[u][n][4 * q + e] = y;
                         }
-                        z[u][4 * q + e] = y;
-                    }
                 }
             if (k0 + (i + 1) * KT > k1) {  // keys past the scan's end
-                const int n = (int)(k1 - k0 - i * KT);
+                const int end = (int)(k1 - k0 - i * KT);
+                asm volatile("");  // a branch: selects on every tile cost two instructions a score
 #pragma unroll
                 for (int u = 0; u < KS; ++u)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (32 * u + 8 * (r / 4) + 4 * h + r % 4 >= n) z[u][r] = -INFINITY;
+                    for (int n = 0; n < CB; ++n)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (32 * u + 8 * (r / 4) + 4 * h + r % 4 >= end) z[u][n][r] = -INFINITY;
             }
+            bool ahead = i == t0;
 #pragma unroll
-            for (int u = 0; u < KS; ++u)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) d = fmaxf(d, z[u][r]);
-            const bool first = i == t0;
-            if (first || __any(d > kLead)) {
-                d = half_max(d);
-                const float up = first || d > kLead ? d : 0.f;
-                const float f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
-                m += up;
-                l *= f;
-#pragma unroll
-                for (int b = 0; b < T::NB; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[b][r] *= f;
+            for (int n = 0; n < CB; ++n) {
+                d[n] = -INFINITY;
 #pragma unroll
                 for (int u = 0; u < KS; ++u)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) z[u][r] -= up;
-                if constexpr (FOLD)
+                    for (int r = 0; r < 16; ++r) d[n] = fmaxf(d[n], z[u][n][r]);
+                ahead = ahead || d[n] > kLead;
+            }
+            if (__any(ahead)) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) ref[r] = -m * inv_cs;
+                for (int n = 0; n < CB; ++n) {
+                    const bool first = i == t0;
+                    const float dn = half_max(d[n]), up = first || dn > kLead ? dn : 0.f;
+                    const float f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
+                    m[n] += up;
+                    l[n] *= f;
+#pragma unroll
+                    for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) o[n][b][r] *= f;
+#pragma unroll
+                    for (int u = 0; u < KS; ++u)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) z[u][n][r] -= up;
+                    if constexpr (FOLD)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) ref[n][r] = -m[n] * inv_cs;
+                }
             }
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
+                typename T::Weights w[CB];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) z[u][r] = __builtin_amdgcn_exp2f(z[u][r]);
-                const typename T::Weights w = T::weights(z[u]);
-                l = T::sum(w, l);
+                for (int n = 0; n < CB; ++n) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) z[u][n][r] = __builtin_amdgcn_exp2f(z[u][n][r]);
+                    w[n] = T::weights(z[u][n]);
+                    l[n] = T::sum(w[n], l[n]);
+                }
                 T::add_weighted(lv[s] + 32 * u * T::LD, lane, w, o);
             }
         }
@@ -163,19 +198,22 @@ __global__ __launch_bounds__(64 * NW) void k_attn(AttnArgs a) {
         }
         __syncthreads();
     }
-    l = half_sum(l);
-    if (!live) return;
-    const int64_t row = qi * a.H + head;
-    if (a.part) {
-        // one of gridDim.y parts: sums as they are, in float32
-        const int64_t at = (int64_t)blockIdx.y * a.nq * a.H + row;
-        if (h == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m, l);
-        if (l == 0.f) return;  // no key: not read
-        Tile<SPV_F32, DP>::store_cols(a.part, at * a.D, a.D, h, o, 1.f);
-        return;
+#pragma unroll
+    for (int n = 0; n < CB; ++n) {
+        const float ln = half_sum(l[n]);
+        if (!live[n]) continue;
+        const int64_t row = qi[n] * a.H + head[n];
+        if (a.part) {
+            // one of gridDim.y parts: sums as they are, in float32
+            const int64_t at = (int64_t)blockIdx.y * a.nq * a.H + row;
+            if (h == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m[n], ln);
+            // without a key they are not read
+            if (ln != 0.f) Tile<SPV_F32, DP>::store_cols(a.part, at * a.D, a.D, h, o[n], 1.f);
+            continue;
+        }
+        T::store_cols(a.out, qi[n] * a.ldo + (int64_t)head[n] * a.D, a.D, h, o[n], tiles ? 1.f / ln : 0.f);
+        if (a.lse && h == 0) a.lse[row] = tiles ? (m[n] + __builtin_amdgcn_logf(ln)) * kLn2 : -INFINITY;
     }
-    T::store_cols(a.out, qi * a.ldo + (int64_t)head * a.D, a.D, h, o, tiles ? 1.f / l : 0.f);
-    if (a.lse && h == 0) a.lse[row] = tiles ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // the parts of a row, added in their order under the largest reference; four channels a thread
@@ -217,13 +255,6 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int parts) {
 // ---------------------------------------------------------------------------
 // host: the shape of a launch
 // ---------------------------------------------------------------------------
-static int attn_dp(int D) { return (D + 31) / 32 * 32; }
-
-// waves of a workgroup and parts of a scan's keys
-struct AttnShape {
-    int nw, parts;
-    int64_t tiles;
-};
 static AttnShape attn_shape(const AttnArgs& a) {
     const int G = a.H / a.K, B = a.B < 1 ? 1 : a.B;
     AttnShape s{4, 1, attn_tiles(a.nq, a.B, G, 128)};
@@ -240,8 +271,6 @@ static AttnShape attn_shape(const AttnArgs& a) {
     }
     return s;
 }
-
-constexpr int64_t kMaxWorkgroups = (int64_t)1 << 22;
 
 bool attention_supported(const AttnArgs& a) {
     const int G = a.H / a.K;

@@ -114,32 +114,50 @@ struct Tile {
         }
     }
 
-    // c + rows (32 of them, at lds) . columns
-    static __device__ inline f32x16 rows_dot(const char* lds, int lane, const uint4 (&f)[NF], f32x16 c) {
+    // c[n] + rows (32 of them, at lds) . columns f[n]: a fragment of the rows is read once for all CB column blocks
+    template <int CB>
+    static __device__ inline void rows_dot(const char* lds, int lane, const uint4 (&f)[CB][NF], f32x16 (&c)[CB]) {
         const char* a = lds + (lane & 31) * LD + (lane >> 5) * 16;
 #pragma unroll
         for (int s = 0; s < NF; ++s) {
             const uint4 x = *(const uint4*)(a + 32 * s);
-            if constexpr (W) {
-                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.x), __uint_as_float(f[s].x), c, 0, 0, 0);
-                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.y), __uint_as_float(f[s].y), c, 0, 0, 0);
-                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.z), __uint_as_float(f[s].z), c, 0, 0, 0);
-                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.w), __uint_as_float(f[s].w), c, 0, 0, 0);
-            } else if constexpr (DT == SPV_BF16) {
-                c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
-                                                            __builtin_bit_cast(bf16x8, f[s]), c, 0, 0, 0);
-            } else {
-                c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x),
-                                                           __builtin_bit_cast(f16x8, f[s]), c, 0, 0, 0);
+#pragma unroll
+            for (int n = 0; n < CB; ++n) {
+                const uint4 y = f[n][s];
+                if constexpr (W) {
+                    c[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.x), __uint_as_float(y.x), c[n], 0, 0, 0);
+                    c[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.y), __uint_as_float(y.y), c[n], 0, 0, 0);
+                    c[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.z), __uint_as_float(y.z), c[n], 0, 0, 0);
+                    c[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.w), __uint_as_float(y.w), c[n], 0, 0, 0);
+                } else if constexpr (DT == SPV_BF16) {
+                    c[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
+                                                                   __builtin_bit_cast(bf16x8, y), c[n], 0, 0, 0);
+                } else {
+                    c[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x),
+                                                                  __builtin_bit_cast(f16x8, y), c[n], 0, 0, 0);
+                }
             }
         }
-        return c;
     }
 
     // the weights of 32 rows (accumulator registers) as B operands
     struct Weights {
         uint4 f[W ? 4 : 2];
     };
+    // the dot product of two fragments' channels, added to s
+    static __device__ inline float frag_dot(const uint4& a, const uint4& b, float s) {
+        const uint32_t u[4] = {a.x, a.y, a.z, a.w}, v[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (W) {
+                s = fmaf(__uint_as_float(u[e]), __uint_as_float(v[e]), s);
+            } else {
+                s = fmaf(from16<DT>(u[e] & 0xFFFF), from16<DT>(v[e] & 0xFFFF), s);
+                s = fmaf(from16<DT>(u[e] >> 16), from16<DT>(v[e] >> 16), s);
+            }
+        }
+        return s;
+    }
     static __device__ inline Weights weights(const f32x16& p) {
         Weights w;
         if constexpr (W) {
@@ -175,40 +193,45 @@ struct Tile {
         return s;
     }
 
-    // o[b] + (channels 32 b .. 32 b + 31 of the 32 rows at lds, transposed) . weights: lane (c, h) of o[b] holds
-    // channels 32 b + 8 (i / 4) + 4 h + i % 4 of column c
-    static __device__ inline void add_weighted(const char* lds, int lane, const Weights& w, f32x16 (&o)[NB]) {
+    // o[n][b] + (channels 32 b .. 32 b + 31 of the 32 rows at lds, transposed) . weights w[n]: lane (c, h) of
+    // o[n][b] holds channels 32 b + 8 (i / 4) + 4 h + i % 4 of column c
+    template <int CB>
+    static __device__ inline void add_weighted(const char* lds, int lane, const Weights (&w)[CB], f32x16 (&o)[CB][NB]) {
         if constexpr (W) {
             const char* a = lds + (lane >> 5) * 4 * LD + (lane & 31) * 4;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t u[4] = {w.f[i / 4].x, w.f[i / 4].y, w.f[i / 4].z, w.f[i / 4].w};
+            for (int i = 0; i < 16; ++i)
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
-                    o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float*)(a + (8 * (i / 4) + i % 4) * LD + 128 * b),
-                                                                __uint_as_float(u[i % 4]), o[b], 0, 0, 0);
-            }
+                for (int b = 0; b < NB; ++b) {
+                    const float x = *(const float*)(a + (8 * (i / 4) + i % 4) * LD + 128 * b);
+#pragma unroll
+                    for (int n = 0; n < CB; ++n) {
+                        const uint32_t u[4] = {w[n].f[i / 4].x, w[n].f[i / 4].y, w[n].f[i / 4].z, w[n].f[i / 4].w};
+                        o[n][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, __uint_as_float(u[i % 4]), o[n][b], 0, 0, 0);
+                    }
+                }
         } else {
+            typedef short i16x8 __attribute__((ext_vector_type(8)));
+            typedef __attribute__((address_space(3))) i16x4 lds4;
             // lanes 16 g .. 16 g + 15 read four rows of 16 channels, and each gets its channel of the four
             const int t = lane & 15, g = lane >> 4;
-            const char* a = lds + (4 * (g >> 1) + (t >> 2)) * LD + (16 * (g & 1) + 4 * (t & 3)) * 2;
+            const uint32_t a = lds_addr(lds) + (4 * (g >> 1) + (t >> 2)) * LD + (16 * (g & 1) + 4 * (t & 3)) * 2;
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
-                    typedef __attribute__((address_space(3))) i16x4 lds4;
-                    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds4*)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)(a + 16 * k * LD + 64 * b));
-                    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds4*)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)(a + (16 * k + 8) * LD + 64 * b));
-                    typedef short i16x8 __attribute__((ext_vector_type(8)));
+                    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(a + 16 * k * LD + 64 * b));
+                    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(a + (16 * k + 8) * LD + 64 * b));
                     const i16x8 x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    if constexpr (DT == SPV_BF16)
-                        o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
-                                                                       __builtin_bit_cast(bf16x8, w.f[k]), o[b], 0, 0, 0);
-                    else
-                        o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x),
-                                                                      __builtin_bit_cast(f16x8, w.f[k]), o[b], 0, 0, 0);
+#pragma unroll
+                    for (int n = 0; n < CB; ++n) {
+                        if constexpr (DT == SPV_BF16)
+                            o[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                                __builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, w[n].f[k]), o[n][b], 0, 0, 0);
+                        else
+                            o[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                                __builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, w[n].f[k]), o[n][b], 0, 0, 0);
+                    }
                 }
         }
     }
@@ -232,19 +255,25 @@ struct Tile {
     }
 };
 
+// the four words of rows 8 q + 4 h .. + 3
+__device__ inline void lds_words(const uint32_t* p, uint32_t (&w)[4]) {
+    const uint4 v = *(const uint4*)p;
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+}
+
 // KT rows of DP channels on their way from memory to LDS by TH threads: loaded to registers a tile ahead, zeros for
 // rows past `end` and channels past D
 template <int DT, int DP, int KT, int TH>
 struct Stage {
     using T = Tile<DT, DP>;
-    static constexpr int N = KT * T::CH / TH;
-    static_assert(KT * T::CH % TH == 0, "every thread moves as many chunks");
+    static constexpr int N = (KT * T::CH + TH - 1) / TH;  // chunks of a thread; past the last: none
+    
     uint4 u[N];
     __device__ inline void load(const void* p, int64_t ld, int64_t head, int64_t row0, int64_t end, int D, int tid) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int id = tid + i * TH, r = id / T::CH, ch = id % T::CH;
-            u[i] = row0 + r < end && ch * T::E < D
+            u[i] = (KT * T::CH % TH == 0 || id < KT * T::CH) && row0 + r < end && ch * T::E < D
                        ? *(const uint4*)((const char*)p + ((row0 + r) * ld + head + ch * T::E) * T::SZ)
                        : make_uint4(0, 0, 0, 0);
         }
@@ -253,12 +282,22 @@ struct Stage {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int id = tid + i * TH;
-            *(uint4*)(lds + (id / T::CH) * T::LD + (id % T::CH) * 16) = u[i];
+            if (KT * T::CH % TH == 0 || id < KT * T::CH)
+                *(uint4*)(lds + (id / T::CH) * T::LD + (id % T::CH) * 16) = u[i];
         }
     }
 };
 
 // rows that the kernels stage at a time
-constexpr int attn_rows(int dt, int DP) { return dt == SPV_F32 || DP > 96 ? 32 : 64; }
+constexpr int attn_rows(int dt, int DP) { return dt == SPV_F32 || DP > 32 ? 32 : 64; }
+// channels a head's rows are padded to
+constexpr int attn_dp(int D) { return (D + 31) / 32 * 32; }
+
+// a launch: waves of a workgroup, parts that the rows of a scan are taken in, tiles of columns
+struct AttnShape {
+    int nw, parts;
+    int64_t tiles;
+};
+constexpr int64_t kMaxWorkgroups = (int64_t)1 << 22;
 
 }  // namespace spv
