@@ -26,12 +26,13 @@ __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnAr
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
     __shared__ __align__(16) uint32_t lc[2][2][BIAS ? KT : 4];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
-    const int G = a.H / a.K, kh = (int)(blockIdx.x % (unsigned)a.K);
-    const ScanTile t = find_tile(a.q_off, a.B, a.nq, G, BM, blockIdx.x / (unsigned)a.K);
+    const Share sh = attn_share(a);
+    const int G = a.H / a.K, kh = sh.kh;
+    const ScanTile t = find_tile(a.q_off, a.B, a.nq, G, BM, sh.tile);
     if (t.col0 >= t.cols) return;  // the whole workgroup
     const int64_t k0 = uniform(clamp_off(a.k_off[t.b], a.nk)), k1 = uniform(clamp_off(a.k_off[t.b + 1], a.nk));
-    const int64_t tiles = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0, per = (tiles + gridDim.y - 1) / gridDim.y;
-    const int64_t t0 = blockIdx.y * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+    const int64_t tiles = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0, per = (tiles + sh.parts - 1) / sh.parts;
+    const int64_t t0 = sh.part * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
     // the lane's columns
     const float cs = a.scale * kLog2e, inv_cs = 1.f / cs;
@@ -123,10 +124,8 @@ __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnAr
                             if constexpr (BIAS)
                                 b = fmaf(voxel_dist(xy[e], zz[e], qc[n].xy, qc[n].z), -slope[n], lift[n]);
                             float y = z[u][n][4 * q + e];
-                            if constexpr (CAP && DT == SPV_F32) {
-                                y = fmaf(cap2, tanhf(y * (a.scale / a.cap)), b - m[n]);
-                            } else if constexpr (CAP) {
-                                // cap tanh(w) = cap - 2 cap / (exp(2 w) + 1)
+                            if constexpr (CAP) {
+                                // cap tanh(w) = cap - 2 cap / (exp(2 w) + 1), to an absolute error of 2^-22 cap
                                 const float ex = __builtin_amdgcn_exp2f(y * cz);
                                 y = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(ex + 1.f), b + (cap2 - m[n]));
                             } else if constexpr (FOLD) {
@@ -204,8 +203,8 @@ __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnAr
         if (!live[n]) continue;
         const int64_t row = qi[n] * a.H + head[n];
         if (a.part) {
-            // one of gridDim.y parts: sums as they are, in float32
-            const int64_t at = (int64_t)blockIdx.y * a.nq * a.H + row;
+            // one of the parts: sums as they are, in float32
+            const int64_t at = (int64_t)sh.part * a.nq * a.H + row;
             if (h == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m[n], ln);
             // without a key they are not read
             if (ln != 0.f) Tile<SPV_F32, DP>::store_cols(a.part, at * a.D, a.D, h, o[n], 1.f);
@@ -216,60 +215,91 @@ __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnAr
     }
 }
 
-// the parts of a row, added in their order under the largest reference; four channels a thread
-template <int DT>
+// The parts of a row joined under their largest reference: WR waves a row, a lane for each four channels of one of
+// every NP parts, added in a fixed order.
+template <int DT, int WR>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int parts) {
-    const int D4 = a.D / 4;
-    const int64_t id = blockIdx.x * (int64_t)256 + threadIdx.x, rows = a.nq * a.H, row = id / D4;
-    if (row >= rows) return;
-    const int d = (int)(id - row * D4) * 4;
-    const int64_t qi = row / a.H;
-    if (qi < a.q_off[0] || qi >= a.q_off[a.B]) return;  // a row of no scan
+    constexpr int RW = 4 / WR;  // rows a workgroup
+    __shared__ float so[4][64][4], sl[4][64], sm[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rw = wave / WR, w = wave % WR;
+    const int P4 = a.D <= 32 ? 8 : a.D <= 64 ? 16 : 32, NP = 64 / P4 * WR;
+    const int64_t rows = a.nq * a.H, row = (int64_t)blockIdx.x * RW + rw, qi = row / a.H;
+    // a row of no scan has no parts
+    const bool on = row < rows && qi >= a.q_off[0] && qi < a.q_off[a.B];
+    const float2* ml = (const float2*)a.part_ml + row;
     float m = -INFINITY;
-    for (int s = 0; s < parts; ++s) {
-        const float2 ml = *(const float2*)(a.part_ml + 2 * (s * rows + row));
-        if (ml.y != 0.f) m = fmaxf(m, ml.x);
+    if (on)
+        for (int s = lane + 64 * w; s < parts; s += 64 * WR) {
+            const float2 v = ml[s * rows];
+            if (v.y != 0.f) m = fmaxf(m, v.x);
+        }
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
+    if constexpr (WR > 1) {
+        if (lane == 0) sm[wave] = m;
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < WR; ++x) m = fmaxf(m, sm[rw * WR + x]);
     }
+    const int d = lane % P4 * 4;
     float l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < parts; ++s) {
-        const float2 ml = *(const float2*)(a.part_ml + 2 * (s * rows + row));
-        if (ml.y == 0.f) continue;
-        const float f = __builtin_amdgcn_exp2f(ml.x - m);
-        const float4 p = *(const float4*)(a.part + (s * rows + row) * a.D + d);
-        l = fmaf(f, ml.y, l);
-        o.x = fmaf(f, p.x, o.x);
-        o.y = fmaf(f, p.y, o.y);
-        o.z = fmaf(f, p.z, o.z);
-        o.w = fmaf(f, p.w, o.w);
+    float o[4] = {};
+    if (on && d < a.D) {
+        constexpr int U = 4;  // parts in flight
+        for (int s0 = lane / P4 + 64 / P4 * w; s0 < parts; s0 += U * NP) {
+            float2 v[U];
+            float4 p[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int s = s0 + u * NP;
+                v[u] = s < parts ? ml[s * rows] : make_float2(0.f, 0.f);
+                // sums of no key are not written
+                p[u] = v[u].y != 0.f ? *(const float4*)(a.part + (s * rows + row) * a.D + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (v[u].y == 0.f) continue;
+                const float f = __builtin_amdgcn_exp2f(v[u].x - m);
+                l = fmaf(f, v[u].y, l);
+                o[0] = fmaf(f, p[u].x, o[0]);
+                o[1] = fmaf(f, p[u].y, o[1]);
+                o[2] = fmaf(f, p[u].z, o[2]);
+                o[3] = fmaf(f, p[u].w, o[3]);
+            }
+        }
     }
+    for (int x = P4; x < 64; x <<= 1) {
+        l += __shfl_xor(l, x, 64);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], x, 64);
+    }
+    if constexpr (WR > 1) {
+        sl[wave][lane] = l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) so[wave][lane][e] = o[e];
+        __syncthreads();
+        if (w) return;
+        for (int x = 1; x < WR; ++x) {
+            l += sl[rw * WR + x][lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += so[rw * WR + x][lane][e];
+        }
+    }
+    if (!on || lane >= P4 || d >= a.D) return;
     const float f = l != 0.f ? 1.f / l : 0.f;
     const int64_t at = qi * a.ldo + (row - qi * a.H) * a.D + d;
     if constexpr (DT == SPV_F32)
-        *(float4*)((float*)a.out + at) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+        *(float4*)((float*)a.out + at) = make_float4(o[0] * f, o[1] * f, o[2] * f, o[3] * f);
     else
-        *(uint2*)((uint16_t*)a.out + at) = make_uint2(pack2<DT>(o.x * f, o.y * f), pack2<DT>(o.z * f, o.w * f));
-    if (a.lse && d == 0) a.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+        *(uint2*)((uint16_t*)a.out + at) = make_uint2(pack2<DT>(o[0] * f, o[1] * f), pack2<DT>(o[2] * f, o[3] * f));
+    if (a.lse && lane == 0) a.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
-// host: the shape of a launch
+// host
 // ---------------------------------------------------------------------------
-static AttnShape attn_shape(const AttnArgs& a) {
-    const int G = a.H / a.K, B = a.B < 1 ? 1 : a.B;
-    AttnShape s{4, 1, attn_tiles(a.nq, a.B, G, 128)};
-    // 128 columns a workgroup while that gives every CU one and the scans fill them
-    if (s.tiles * a.K < 256 || a.nq * G / B < 64) s = AttnShape{1, 1, attn_tiles(a.nq, a.B, G, 32)};
-    // keys in parts of at least four tiles (of the average scan) while there are under four waves a CU
-    const int KT = attn_rows(a.dt, attn_dp(a.D));
-    const int64_t wgs = s.tiles * a.K * s.nw, key_tiles = a.nk / B / KT;
-    if (s.nw == 1 && wgs < 1024) {
-        int64_t p = (2048 + wgs - 1) / (wgs < 1 ? 1 : wgs);
-        if (p > key_tiles / 4) p = key_tiles / 4;
-        if (p > 256) p = 256;
-        s.parts = p < 2 ? 1 : (int)p;
-    }
-    return s;
+static AttnShape forward_shape(const AttnArgs& a) {
+    return attn_shape(a.nq, a.H / a.K, a.B, a.K, a.nk / (a.B < 1 ? 1 : a.B) / attn_rows(a.dt, attn_dp(a.D)));
 }
 
 bool attention_supported(const AttnArgs& a) {
@@ -278,7 +308,7 @@ bool attention_supported(const AttnArgs& a) {
 }
 
 void plan_attention_ws(Arena& a, AttnArgs& t) {
-    const AttnShape s = attn_shape(t);
+    const AttnShape s = forward_shape(t);
     if (s.parts < 2) return;
     const size_t rows = (size_t)s.parts * (size_t)t.nq * (size_t)t.H;
     t.part_ml = a.take<float>(2 * rows);
@@ -287,7 +317,7 @@ void plan_attention_ws(Arena& a, AttnArgs& t) {
 
 template <int DT, int DP, int NW>
 static void attn_launch(hipStream_t s, const AttnArgs& a, const AttnShape& sh) {
-    const dim3 g((unsigned)(sh.tiles * a.K), (unsigned)sh.parts);
+    const dim3 g = attn_grid(sh, a.K);
     if (a.slopes && a.cap > 0.f) k_attn<DT, DP, NW, true, true><<<g, 64 * NW, 0, s>>>(a);
     else if (a.slopes) k_attn<DT, DP, NW, true, false><<<g, 64 * NW, 0, s>>>(a);
     else if (a.cap > 0.f) k_attn<DT, DP, NW, false, true><<<g, 64 * NW, 0, s>>>(a);
@@ -300,14 +330,15 @@ static void attn_dp_launch(hipStream_t s, const AttnArgs& a, const AttnShape& sh
 }
 template <int DT>
 static void attn_dt(hipStream_t s, const AttnArgs& a) {
-    const AttnShape sh = attn_shape(a);
+    const AttnShape sh = forward_shape(a);
     switch (attn_dp(a.D)) {
         case 32: attn_dp_launch<DT, 32>(s, a, sh); break;
         case 64: attn_dp_launch<DT, 64>(s, a, sh); break;
         case 96: attn_dp_launch<DT, 96>(s, a, sh); break;
         case 128: attn_dp_launch<DT, 128>(s, a, sh); break;
     }
-    if (sh.parts > 1) k_attn_join<DT><<<blocks_for(a.nq * a.H * (a.D / 4), 256), 256, 0, s>>>(a, sh.parts);
+    if (sh.parts > 16) k_attn_join<DT, 4><<<blocks_for(a.nq * a.H, 1), 256, 0, s>>>(a, sh.parts);
+    else if (sh.parts > 1) k_attn_join<DT, 1><<<blocks_for(a.nq * a.H, 4), 256, 0, s>>>(a, sh.parts);
 }
 
 void launch_attention(hipStream_t s, const AttnArgs& a) {

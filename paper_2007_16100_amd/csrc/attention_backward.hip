@@ -13,18 +13,13 @@ namespace spv {
 // score (log 2 units, less the row's lse) and its slope by the product, from a product y
 template <int DT, bool CAP>
 struct Score {
-    float cs, cz, cap2, w;
+    float cs, cz, cap2;
     __device__ explicit Score(const AttnArgs& a)
-        : cs(a.scale * kLog2e), cz(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f), cap2(a.cap * kLog2e),
-          w(CAP ? a.scale / a.cap : 0.f) {}
+        : cs(a.scale * kLog2e), cz(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f), cap2(a.cap * kLog2e) {}
     static constexpr bool kFold = DT != SPV_F32 && !CAP;  // the products already hold -lse / cs
     // x: the score; the return value times kBend is d score / d (scale * product)
     __device__ float operator()(float y, float bias, float lse, float& x) const {
-        if constexpr (CAP && DT == SPV_F32) {
-            const float t = tanhf(y * w);
-            x = fmaf(cap2, t, bias - lse);
-            return fmaf(-t, t, 1.f);
-        } else if constexpr (CAP) {
+        if constexpr (CAP) {
             // t = 1 - 2 r with r = 1 / (exp(2 w) + 1): 1 - t^2 = 4 (r - r^2)
             const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * cz) + 1.f);
             x = fmaf(-2.f * cap2, r, bias + (cap2 - lse));
@@ -34,7 +29,7 @@ struct Score {
             return 1.f;
         }
     }
-    static constexpr float kBend = CAP && DT != SPV_F32 ? 4.f : 1.f;
+    static constexpr float kBend = CAP ? 4.f : 1.f;
 };
 
 // waves per SIMD that the registers have to leave room for
@@ -49,12 +44,13 @@ __global__ __launch_bounds__(64 * NW, dq_waves(DT, DP, NW)) void k_attn_dq(AttnA
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
     __shared__ __align__(16) uint32_t lc[2][2][BIAS ? KT : 4];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
-    const int G = a.H / a.K, kh = (int)(blockIdx.x % (unsigned)a.K);
-    const ScanTile t = find_tile(a.q_off, a.B, a.nq, G, BM, blockIdx.x / (unsigned)a.K);
+    const Share sh = attn_share(a);
+    const int G = a.H / a.K, kh = sh.kh;
+    const ScanTile t = find_tile(a.q_off, a.B, a.nq, G, BM, sh.tile);
     if (t.col0 >= t.cols) return;  // the whole workgroup
     const int64_t k0 = uniform(clamp_off(a.k_off[t.b], a.nk)), k1 = uniform(clamp_off(a.k_off[t.b + 1], a.nk));
-    const int64_t tiles = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0, per = (tiles + gridDim.y - 1) / gridDim.y;
-    const int64_t t0 = blockIdx.y * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+    const int64_t tiles = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0, per = (tiles + sh.parts - 1) / sh.parts;
+    const int64_t t0 = sh.part * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
     const S score(a);
     const bool busy = t.col0 + 32 * wave < t.cols;
@@ -76,7 +72,7 @@ __global__ __launch_bounds__(64 * NW, dq_waves(DT, DP, NW)) void k_attn_dq(AttnA
     }
     if (live) {
         lse = a.lse[qi * a.H + head] * kLog2e;
-        if (h == 0 && blockIdx.y == 0) a.delta[qi * a.H + head] = delta;
+        if (h == 0 && sh.part == 0) a.delta[qi * a.H + head] = delta;
     }
     Voxel qc{0, 0};
     float slope = 0.f, lift = 0.f;
@@ -162,7 +158,7 @@ __global__ __launch_bounds__(64 * NW, dq_waves(DT, DP, NW)) void k_attn_dq(AttnA
     if (!live) return;
     const float f = a.scale * S::kBend;
     if (a.part)
-        Tile<SPV_F32, DP>::store_cols(a.part, (((int64_t)blockIdx.y * a.nq + qi) * a.H + head) * a.D, a.D, h, o[0], f);
+        Tile<SPV_F32, DP>::store_cols(a.part, (((int64_t)sh.part * a.nq + qi) * a.H + head) * a.D, a.D, h, o[0], f);
     else
         T::store_cols(a.dq, qi * a.lddq + (int64_t)head * a.D, a.D, h, o[0], f);
 }
@@ -182,13 +178,14 @@ __global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(Att
     __shared__ __align__(16) uint32_t lc[2][2][BIAS ? KT : 4];
     __shared__ __align__(16) float lr[2][2][KT];  // the rows' lse (as the score wants it) and -delta
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
-    const int G = a.H / a.K, kh = (int)(blockIdx.x % (unsigned)a.K);
-    const ScanTile t = find_tile(a.k_off, a.B, a.nk, 1, BM, blockIdx.x / (unsigned)a.K);
+    const Share sh = attn_share(a);
+    const int G = a.H / a.K, kh = sh.kh;
+    const ScanTile t = find_tile(a.k_off, a.B, a.nk, 1, BM, sh.tile);
     if (t.col0 >= t.cols) return;  // the whole workgroup
     const int64_t q0 = uniform(clamp_off(a.q_off[t.b], a.nq)), q1 = uniform(clamp_off(a.q_off[t.b + 1], a.nq));
     const int64_t tiles = q1 > q0 ? (q1 - q0 + KT - 1) / KT : 0, all = tiles * G;
-    const int64_t per = (all + gridDim.y - 1) / gridDim.y;
-    const int64_t t0 = blockIdx.y * per, t1 = t0 + per < all ? t0 + per : all;
+    const int64_t per = (all + sh.parts - 1) / sh.parts;
+    const int64_t t0 = sh.part * per, t1 = t0 + per < all ? t0 + per : all;
 
     const S score(a);
     const bool busy = t.col0 + 32 * wave < t.cols, live = t.col0 + 32 * wave + c < t.cols;
@@ -293,8 +290,8 @@ __global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(Att
     if (!live) return;
     const float f = a.scale * S::kBend;
     if (a.part) {
-        const int64_t at = (((int64_t)blockIdx.y * a.nk + kj) * a.K + kh) * a.D;
-        const int64_t half = (int64_t)gridDim.y * a.nk * a.K * a.D;
+        const int64_t at = (((int64_t)sh.part * a.nk + kj) * a.K + kh) * a.D;
+        const int64_t half = (int64_t)sh.parts * a.nk * a.K * a.D;
         Tile<SPV_F32, DP>::store_cols(a.part, at, a.D, h, ok[0], f);
         Tile<SPV_F32, DP>::store_cols(a.part, half + at, a.D, h, ov[0], down);
     } else {
@@ -324,27 +321,13 @@ __global__ __launch_bounds__(256) void k_attn_add_parts(const float* __restrict_
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
-// the shape of one side: n rows of `per` columns over the other side's `work` tiles of 32 in the average scan
-static AttnShape side_shape(int64_t n, int per, int B, int K, int64_t work) {
-    AttnShape s{4, 1, attn_tiles(n, B, per, 128)};
-    const int scans = B < 1 ? 1 : B;
-    if (s.tiles * K < 256 || n * per / scans < 64) s = AttnShape{1, 1, attn_tiles(n, B, per, 32)};
-    const int64_t wgs = s.tiles * K;
-    if (s.nw == 1 && wgs < 1024) {
-        int64_t p = (2048 + wgs - 1) / (wgs < 1 ? 1 : wgs);
-        if (p > work / 4) p = work / 4;
-        if (p > 256) p = 256;
-        s.parts = p < 2 ? 1 : (int)p;
-    }
-    return s;
-}
 static AttnShape dq_shape(const AttnArgs& a) {
     const int G = a.H / a.K;
-    return side_shape(a.nq, G, a.B, a.K, a.nk / (a.B < 1 ? 1 : a.B) / 32);
+    return attn_shape(a.nq, G, a.B, a.K, a.nk / (a.B < 1 ? 1 : a.B) / 32);
 }
 static AttnShape dkv_shape(const AttnArgs& a) {
     const int G = a.H / a.K;
-    return side_shape(a.nk, 1, a.B, a.K, a.nq / (a.B < 1 ? 1 : a.B) / 32 * G);
+    return attn_shape(a.nk, 1, a.B, a.K, a.nq / (a.B < 1 ? 1 : a.B) / 32 * G);
 }
 
 void plan_attention_backward_ws(Arena& a, AttnArgs& t) {
@@ -358,7 +341,7 @@ void plan_attention_backward_ws(Arena& a, AttnArgs& t) {
 
 template <int DT, int DP, int NW, bool BIAS, bool CAP>
 static void launch_side(hipStream_t s, const AttnArgs& a, const AttnShape& sh, bool keys) {
-    const dim3 g((unsigned)(sh.tiles * a.K), (unsigned)sh.parts);
+    const dim3 g = attn_grid(sh, a.K);
     if (keys) k_attn_dkv<DT, DP, NW, BIAS, CAP><<<g, 64 * NW, 0, s>>>(a);
     else k_attn_dq<DT, DP, NW, BIAS, CAP><<<g, 64 * NW, 0, s>>>(a);
 }

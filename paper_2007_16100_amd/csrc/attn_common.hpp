@@ -38,6 +38,18 @@ __device__ inline int64_t scan_tile(const int32_t* off, int b, int64_t n, int pe
 }
 inline int64_t attn_tiles(int64_t n, int B, int per, int BM) { return n * per / BM + B; }
 
+// What a workgroup takes: a key head, a tile of columns and one of `parts` shares of the rows.  In one part the heads
+// come first in the grid, so that the eight dies (which take workgroups in turn) each keep to few heads' rows in
+// their L2.  In parts those come first: the heads of one part, which share its cache lines, then run on one die.
+struct Share {
+    int kh, part, parts;
+    int64_t tile;
+};
+__device__ inline Share attn_share(const AttnArgs& a) {
+    if (a.part) return Share{(int)blockIdx.y, (int)blockIdx.x, (int)gridDim.x, (int64_t)blockIdx.z};
+    return Share{(int)(blockIdx.x % (unsigned)a.K), 0, 1, (int64_t)(blockIdx.x / (unsigned)a.K)};
+}
+
 struct ScanTile {
     int b;           // scan
     int64_t first;   // its first row
@@ -298,6 +310,26 @@ struct AttnShape {
     int nw, parts;
     int64_t tiles;
 };
+inline dim3 attn_grid(const AttnShape& s, int K) {
+    return s.parts > 1 ? dim3((unsigned)s.parts, (unsigned)K, (unsigned)s.tiles) : dim3((unsigned)(s.tiles * K));
+}
+// 128 columns a workgroup while that gives every CU one and the scans fill them, else 32; rows in parts of at least
+// four tiles of the average scan's `work` while there are under four waves a CU (1,024 workgroups: grids of parts
+// stay within the limits of their dimensions)
+inline AttnShape attn_shape(int64_t n, int per, int B, int K, int64_t work) {
+    const int scans = B < 1 ? 1 : B;
+    AttnShape s{4, 1, attn_tiles(n, B, per, 128)};
+    if (s.tiles * K < 256 || n * per / scans < 64) s = AttnShape{1, 1, attn_tiles(n, B, per, 32)};
+    const int64_t wgs = s.tiles * K;
+    if (s.nw == 1 && wgs < 1024) {
+        int64_t p = 2048 / (wgs < 1 ? 1 : wgs);
+        if (p > work / 4) p = work / 4;
+        if (p > 256) p = 256;
+        if (p > 8) p &= ~(int64_t)7;  // a part's heads on one die
+        s.parts = p < 2 ? 1 : (int)p;
+    }
+    return s;
+}
 constexpr int64_t kMaxWorkgroups = (int64_t)1 << 22;
 
 }  // namespace spv
