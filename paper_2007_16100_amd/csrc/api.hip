@@ -775,7 +775,7 @@ spv_status spv_layer_norm_backward(void* stream, void* ws, size_t ws_bytes, cons
 
 // a row stride (in elements) that holds the row's channels and keeps every row 16-byte aligned
 static bool row_stride_ok(int64_t ld, int64_t channels, spv_dtype dt) {
-    return ld >= channels && ld % (int64_t)(16 / esize(dt)) == 0 && ld < ((int64_t)1 << 31);
+    return ld >= channels && ld % (int64_t)(16 / esize(dt)) == 0 && ld < ((int64_t)1 << 24);
 }
 
 // the checks of both directions; fills t with everything but the gradients

@@ -7,22 +7,27 @@
 namespace spv {
 
 // Columns are (query, head of a key head's group) pairs, so shared key heads are staged once for all of their query
-// heads; a workgroup takes 32 NW columns of one scan and one key head.  Scores are kept in units of log 2 and
-// relative to the column's reference; the reference moves (and the sums are scaled) only when a score passes it by
-// more than kLead: weights of up to 2^kLead lose nothing in float32 sums or 16-bit weights, and after the first
-// tiles the reference hardly ever moves.
+// heads; a workgroup takes 32 NW columns of one scan and one key head.  Scores are kept in units of log 2.  A column's
+// reference m moves (and the sums are scaled) only when a score passes it by more than kLead: weights of up to
+// 2^kLead lose nothing in float32 sums or 16-bit weights, and after the first tiles m hardly ever moves.
+// The bias, over scale, is what the products are added to; a cap's tanh stands between them, so it is added after.
 constexpr float kLead = 8.f;
 
-
 // waves per SIMD that the registers have to leave room for
-constexpr int attn_waves(int dt, int DP, int nw) { return nw == 1 || dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? 4 : 3; }
+#ifndef OCC32
+#define OCC32 3
+#endif
+#ifndef OCC64
+#define OCC64 4
+#endif
+constexpr int attn_waves(int dt, int DP, int nw) {
+    return nw == 1 || dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? OCC64 : OCC32;
+}
 
 template <int DT, int DP, int NW, bool BIAS, bool CAP>
 __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnArgs a) {
     using T = Tile<DT, DP>;
-    constexpr int KT = attn_rows(DT, DP), KS = KT / 32, TH = 64 * NW, CB = 1, WC = 32 * CB, BM = WC * NW;
-    // the reference goes into the products' accumulator, where no tanh stands between them
-    constexpr bool FOLD = DT != SPV_F32 && !CAP;
+    constexpr int KT = attn_rows(DT, DP), KS = KT / 32, TH = 64 * NW, BM = 32 * NW;
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
     __shared__ __align__(16) uint32_t lc[2][2][BIAS ? KT : 4];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
@@ -31,44 +36,35 @@ __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnAr
     const ScanTile t = find_tile(a.q_off, a.B, a.nq, G, BM, sh.tile);
     if (t.col0 >= t.cols) return;  // the whole workgroup
     const int64_t k0 = uniform(clamp_off(a.k_off[t.b], a.nk)), k1 = uniform(clamp_off(a.k_off[t.b + 1], a.nk));
-    const int64_t tiles = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0, per = (tiles + sh.parts - 1) / sh.parts;
-    const int64_t t0 = sh.part * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+    const int keys = (int)(k1 > k0 ? k1 - k0 : 0), tiles = keys / KT + (keys % KT != 0);
+    const int per = (tiles + sh.parts - 1) / sh.parts, t0 = sh.part * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
-    // the lane's columns
-    const float cs = a.scale * kLog2e, inv_cs = 1.f / cs;
-    const float cz = CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
-    const bool busy = t.col0 + WC * wave < t.cols;
+    // the lane's column
+    const bool busy = t.col0 + 32 * wave < t.cols, live = t.col0 + 32 * wave + c < t.cols;
     const int64_t q0 = t.col0 / G;
-    int64_t qi[CB];
-    int head[CB];
-    bool live[CB];
-    uint4 qf[CB][T::NF];
-    Voxel qc[CB];
-    float slope[CB], lift[CB];  // lift: what the 2^23 of a distance brings too much
-#pragma unroll
-    for (int n = 0; n < CB; ++n) {
-        const int x = WC * wave + 32 * n + c, y = (int)(t.col0 - q0 * G) + x;
-        live[n] = t.col0 + x < t.cols;
-        qi[n] = t.first + q0 + y / G;
-        head[n] = kh * G + y % G;
-        T::load_cols(a.q, qi[n] * a.ldq + (int64_t)head[n] * a.D, live[n], a.D, h, qf[n]);
-        qc[n] = Voxel{0, 0};
-        slope[n] = lift[n] = 0.f;
-        if (BIAS && live[n]) {
-            qc[n] = voxel_of(*(const int4*)(a.q_coords + 4 * qi[n]));
-            slope[n] = a.slopes[head[n]] * kLog2e;
-            lift[n] = slope[n] * 8388608.f;
-        }
+    const int x = (int)(t.col0 - q0 * G) + 32 * wave + c, head = kh * G + x % G;
+    const int64_t qi = t.first + q0 + x / G;
+    uint4 qf[T::NF];
+    T::load_cols(a.q, qi * a.ldq + (int64_t)head * a.D, live, a.D, h, qf);
+    const float cs = a.scale * kLog2e, cz = CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
+    Voxel qc{0, 0};
+    float slope = 0.f;  // of the scores where there is a cap, else of the products
+    if (BIAS && live) {
+        qc = voxel_of(*(const int4*)(a.q_coords + 4 * qi));
+        slope = CAP ? a.slopes[head] * kLog2e : a.slopes[head] / a.scale;
     }
+    const float lift = slope * 8388608.f;  // what the 2^23 of a distance brings too much
 
-    Stage<DT, DP, KT, TH> sk, sv;
+    Stage<DT, DP, KT, TH> sk(tid, a.ldk, a.D), sv(tid, a.ldv, a.D);
     int4 ck{0, 0, 0, 0};
-    auto load = [&](int64_t i) __attribute__((always_inline)) {
-        const int64_t r = k0 + i * KT;
-        sk.load(a.k, a.ldk, (int64_t)kh * a.D, r, k1, a.D, tid);
-        sv.load(a.v, a.ldv, (int64_t)kh * a.D, r, k1, a.D, tid);
+    auto load = [&](int i) __attribute__((always_inline)) {
+        const int64_t r = k0 + (int64_t)i * KT, n = k1 - r;
+        sk.load(rows_buffer((const char*)a.k + (r * a.ldk + kh * a.D) * T::SZ, a.ldk * T::SZ, n, KT, a.D * T::SZ));
+        sv.load(rows_buffer((const char*)a.v + (r * a.ldv + kh * a.D) * T::SZ, a.ldv * T::SZ, n, KT, a.D * T::SZ));
         if constexpr (BIAS)
-            if (tid < KT && r + tid < k1) ck = *(const int4*)(a.k_coords + 4 * (r + tid));
+            if (tid < KT)
+                ck = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                  rows_buffer(a.k_coords + 4 * r, 16, n, KT, 16), tid * 16, 0, 0));
     };
     auto store = [&](int s) __attribute__((always_inline)) {
         sk.store(lk[s], tid);
@@ -81,113 +77,76 @@ __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnAr
             }
     };
 
-    f32x16 o[CB][T::NB], ref[CB];  // ref: -reference / cs in every register (FOLD)
-    float m[CB], l[CB];
+    f32x16 o[T::NB];
 #pragma unroll
-    for (int n = 0; n < CB; ++n) {
-#pragma unroll
-        for (int b = 0; b < T::NB; ++b) o[n][b] = f32x16{};
-        ref[n] = f32x16{};
-        m[n] = l[n] = 0.f;
-    }
+    for (int b = 0; b < T::NB; ++b) o[b] = f32x16{};
+    float m = 0.f, l = 0.f;
     if (t0 < t1) {
         load(t0);
         store(0);
         if (t0 + 1 < t1) load(t0 + 1);
     }
     __syncthreads();
-    for (int64_t i = t0; i < t1; ++i) {
-        const int s = (int)(i - t0) & 1;
+    for (int i = t0; i < t1; ++i) {
+        const int s = (i - t0) & 1;
         if (busy) {
-            f32x16 z[KS][CB];
-            float d[CB];
+            f32x16 z[KS], bias[CAP && BIAS ? KS : 1];
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
+                f32x16 b{};
+                if constexpr (BIAS)
 #pragma unroll
-                for (int n = 0; n < CB; ++n) z[u][n] = FOLD ? ref[n] : f32x16{};
-                T::rows_dot(lk[s] + 32 * u * T::LD, lane, qf, z[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < KS; ++u)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t xy[4] = {}, zz[4] = {};
-                    if constexpr (BIAS) {
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t xy[4], zz[4];
                         lds_words(&lc[s][0][32 * u + 8 * q + 4 * h], xy);
                         lds_words(&lc[s][1][32 * u + 8 * q + 4 * h], zz);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            b[4 * q + e] = fmaf(voxel_dist(xy[e], zz[e], qc.xy, qc.z), -slope, lift);
                     }
+                if constexpr (CAP && BIAS) bias[u] = b;
+                z[u] = T::rows_dot(lk[s] + 32 * u * T::LD, lane, qf, CAP ? f32x16{} : b);
+            }
 #pragma unroll
-                    for (int n = 0; n < CB; ++n)
+            for (int u = 0; u < KS; ++u) {
+                if constexpr (CAP)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float b = 0.f;
-                            if constexpr (BIAS)
-                                b = fmaf(voxel_dist(xy[e], zz[e], qc[n].xy, qc[n].z), -slope[n], lift[n]);
-                            float y = z[u][n][4 * q + e];
-                            if constexpr (CAP) {
-                                // cap tanh(w) = cap - 2 cap / (exp(2 w) + 1), to an absolute error of 2^-22 cap
-                                const float ex = __builtin_amdgcn_exp2f(y * cz);
-                                y = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(ex + 1.f), b + (cap2 - m[n]));
-                            } else if constexpr (FOLD) {
-                                y = BIAS ? fmaf(y, cs, b) : y * cs;
-                            } else {
-                                y = fmaf(y, cs, b) - m[n];
-                            }
-                            z[u][n][4 * q + e] = y;
-                        }
+                    for (int r = 0; r < 16; ++r) {
+                        // cap tanh(w) = cap - 2 cap / (exp(2 w) + 1), to an absolute error of 2^-22 cap
+                        const float ex = __builtin_amdgcn_exp2f(z[u][r] * cz);
+                        z[u][r] = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(ex + 1.f),
+                                       BIAS ? bias[BIAS ? u : 0][r] + (cap2 - m) : cap2 - m);
+                    }
+                const int end = keys - i * KT - 32 * u;
+                if (end < 32) {  // keys past the scan's end
+                    asm volatile("");  // a branch: selects on every tile cost two instructions a score
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (8 * (r / 4) + 4 * h + r % 4 >= end) z[u][r] = -INFINITY;
                 }
-            if (k0 + (i + 1) * KT > k1) {  // keys past the scan's end
-                const int end = (int)(k1 - k0 - i * KT);
-                asm volatile("");  // a branch: selects on every tile cost two instructions a score
+                float d = z[u][0];
 #pragma unroll
-                for (int u = 0; u < KS; ++u)
-#pragma unroll
-                    for (int n = 0; n < CB; ++n)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (32 * u + 8 * (r / 4) + 4 * h + r % 4 >= end) z[u][n][r] = -INFINITY;
-            }
-            bool ahead = i == t0;
-#pragma unroll
-            for (int n = 0; n < CB; ++n) {
-                d[n] = -INFINITY;
-#pragma unroll
-                for (int u = 0; u < KS; ++u)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) d[n] = fmaxf(d[n], z[u][n][r]);
-                ahead = ahead || d[n] > kLead;
-            }
-            if (__any(ahead)) {
-#pragma unroll
-                for (int n = 0; n < CB; ++n) {
-                    const bool first = i == t0;
-                    const float dn = half_max(d[n]), up = first || dn > kLead ? dn : 0.f;
+                for (int r = 1; r < 16; ++r) d = fmaxf(d, z[u][r]);
+                if constexpr (!CAP) d = fmaf(d, cs, -m);
+                const bool first = i == t0 && u == 0;
+                if (first || __any(d > kLead)) {
+                    d = half_max(d);
+                    const float up = first || d > kLead ? d : 0.f;
                     const float f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
-                    m[n] += up;
-                    l[n] *= f;
+                    m += up;
+                    l *= f;
 #pragma unroll
                     for (int b = 0; b < T::NB; ++b)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) o[n][b][r] *= f;
+                        for (int r = 0; r < 16; ++r) o[b][r] *= f;
+                    if constexpr (CAP)
 #pragma unroll
-                    for (int u = 0; u < KS; ++u)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) z[u][n][r] -= up;
-                    if constexpr (FOLD)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) ref[n][r] = -m[n] * inv_cs;
+                        for (int r = 0; r < 16; ++r) z[u][r] -= up;
                 }
-            }
 #pragma unroll
-            for (int u = 0; u < KS; ++u) {
-                typename T::Weights w[CB];
-#pragma unroll
-                for (int n = 0; n < CB; ++n) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) z[u][n][r] = __builtin_amdgcn_exp2f(z[u][n][r]);
-                    w[n] = T::weights(z[u][n]);
-                    l[n] = T::sum(w[n], l[n]);
-                }
+                for (int r = 0; r < 16; ++r) z[u][r] = __builtin_amdgcn_exp2f(CAP ? z[u][r] : fmaf(z[u][r], cs, -m));
+                const typename T::Weights w = T::weights(z[u]);
+                l = T::sum(w, l);
                 T::add_weighted(lv[s] + 32 * u * T::LD, lane, w, o);
             }
         }
@@ -197,22 +156,18 @@ __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnAr
         }
         __syncthreads();
     }
-#pragma unroll
-    for (int n = 0; n < CB; ++n) {
-        const float ln = half_sum(l[n]);
-        if (!live[n]) continue;
-        const int64_t row = qi[n] * a.H + head[n];
-        if (a.part) {
-            // one of the parts: sums as they are, in float32
-            const int64_t at = (int64_t)sh.part * a.nq * a.H + row;
-            if (h == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m[n], ln);
-            // without a key they are not read
-            if (ln != 0.f) Tile<SPV_F32, DP>::store_cols(a.part, at * a.D, a.D, h, o[n], 1.f);
-            continue;
-        }
-        T::store_cols(a.out, qi[n] * a.ldo + (int64_t)head[n] * a.D, a.D, h, o[n], tiles ? 1.f / ln : 0.f);
-        if (a.lse && h == 0) a.lse[row] = tiles ? (m[n] + __builtin_amdgcn_logf(ln)) * kLn2 : -INFINITY;
+    l = half_sum(l);
+    if (!live) return;
+    const int64_t row = qi * a.H + head;
+    if (a.part) {
+        // one of the parts: sums as they are, in float32
+        const int64_t at = (int64_t)sh.part * a.nq * a.H + row;
+        if (h == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m, l);
+        if (l != 0.f) Tile<SPV_F32, DP>::store_cols(a.part, at * a.D, a.D, h, o, 1.f);  // else they are not read
+        return;
     }
+    T::store_cols(a.out, qi * a.ldo + (int64_t)head * a.D, a.D, h, o, tiles ? 1.f / l : 0.f);
+    if (a.lse && h == 0) a.lse[row] = tiles ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // The parts of a row joined under their largest reference: WR waves a row, a lane for each four channels of one of

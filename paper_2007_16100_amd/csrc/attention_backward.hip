@@ -4,42 +4,39 @@
 // Two kernels, each of which forms the weights anew: dq with the queries in the columns, as the forward has them (it
 // also forms delta), and dk, dv with the keys in the columns.  One kernel for all three would save two products of
 // seven, but either add dq in the order that workgroups happen to run in, or hold it for every part of the keys.
-// lse and delta enter as the products' accumulators (dout . v - delta and, where no tanh stands between,
-// q . k - lse / scale come out of the matrix cores).
+// -delta is what the products dout . v are added to; the bias, over scale, or (keys in the columns) the rows' -lse are
+// what the products q . k are added to, unless a cap's tanh stands between.
 #include "attn_common.hpp"
 
 namespace spv {
 
-// score (log 2 units, less the row's lse) and its slope by the product, from a product y
-template <int DT, bool CAP>
-struct Score {
-    float cs, cz, cap2;
-    __device__ explicit Score(const AttnArgs& a)
-        : cs(a.scale * kLog2e), cz(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f), cap2(a.cap * kLog2e) {}
-    static constexpr bool kFold = DT != SPV_F32 && !CAP;  // the products already hold -lse / cs
-    // x: the score; the return value times kBend is d score / d (scale * product)
-    __device__ float operator()(float y, float bias, float lse, float& x) const {
-        if constexpr (CAP) {
-            // t = 1 - 2 r with r = 1 / (exp(2 w) + 1): 1 - t^2 = 4 (r - r^2)
-            const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * cz) + 1.f);
-            x = fmaf(-2.f * cap2, r, bias + (cap2 - lse));
-            return fmaf(-r, r, r);
-        } else {
-            x = kFold ? fmaf(y, cs, bias) : fmaf(y, cs, bias - lse);
-            return 1.f;
-        }
+// d score / d product, over scale and kBend, and the score itself from a product under a cap
+struct Capped {
+    float cz, cap2;
+    __device__ explicit Capped(const AttnArgs& a) : cz(2.f * kLog2e * a.scale / a.cap), cap2(a.cap * kLog2e) {}
+    // t = tanh(w) = 1 - 2 r with r = 1 / (exp(2 w) + 1): 1 - t^2 = 4 (r - r^2)
+    __device__ float operator()(float y, float rest, float& x) const {
+        const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * cz) + 1.f);
+        x = fmaf(-2.f * cap2, r, rest);
+        return fmaf(-r, r, r);
     }
-    static constexpr float kBend = CAP ? 4.f : 1.f;
 };
+template <bool CAP>
+constexpr float kBend = CAP ? 4.f : 1.f;
 
 // waves per SIMD that the registers have to leave room for
-constexpr int dq_waves(int dt, int DP, int nw) { return nw == 1 || dt == SPV_F32 || DP > 64 ? 1 : 2; }
-constexpr int dkv_waves(int dt, int DP, int nw) { return nw == 1 || dt == SPV_F32 || DP > 64 ? 1 : 2; }
+#ifndef OCQ
+#define OCQ 2
+#endif
+#ifndef OCK
+#define OCK 2
+#endif
+constexpr int dq_waves(int dt, int DP, int nw) { return nw == 1 || dt == SPV_F32 || DP > 64 ? 1 : OCQ; }
+constexpr int dkv_waves(int dt, int DP, int nw) { return nw == 1 || dt == SPV_F32 || DP > 64 ? 1 : OCK; }
 
 template <int DT, int DP, int NW, bool BIAS, bool CAP>
 __global__ __launch_bounds__(64 * NW, dq_waves(DT, DP, NW)) void k_attn_dq(AttnArgs a) {
     using T = Tile<DT, DP>;
-    using S = Score<DT, CAP>;
     constexpr int KT = 32, TH = 64 * NW, BM = 32 * NW;
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
     __shared__ __align__(16) uint32_t lc[2][2][BIAS ? KT : 4];
@@ -49,53 +46,51 @@ __global__ __launch_bounds__(64 * NW, dq_waves(DT, DP, NW)) void k_attn_dq(AttnA
     const ScanTile t = find_tile(a.q_off, a.B, a.nq, G, BM, sh.tile);
     if (t.col0 >= t.cols) return;  // the whole workgroup
     const int64_t k0 = uniform(clamp_off(a.k_off[t.b], a.nk)), k1 = uniform(clamp_off(a.k_off[t.b + 1], a.nk));
-    const int64_t tiles = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0, per = (tiles + sh.parts - 1) / sh.parts;
-    const int64_t t0 = sh.part * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+    const int keys = (int)(k1 > k0 ? k1 - k0 : 0), tiles = keys / KT + (keys % KT != 0);
+    const int per = (tiles + sh.parts - 1) / sh.parts, t0 = sh.part * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
-    const S score(a);
-    const bool busy = t.col0 + 32 * wave < t.cols;
+    const bool busy = t.col0 + 32 * wave < t.cols, live = t.col0 + 32 * wave + c < t.cols;
     const int64_t q0 = t.col0 / G;
-    const int col = 32 * wave + c, y0 = (int)(t.col0 - q0 * G) + col;
-    const bool live = t.col0 + col < t.cols;
+    const int y0 = (int)(t.col0 - q0 * G) + 32 * wave + c, head = kh * G + y0 % G;
     const int64_t qi = t.first + q0 + y0 / G;
-    const int head = kh * G + y0 % G;
-    uint4 qf[1][T::NF], df[1][T::NF];
-    T::load_cols(a.q, qi * a.ldq + (int64_t)head * a.D, live, a.D, h, qf[0]);
-    T::load_cols(a.dout, qi * a.lddo + (int64_t)head * a.D, live, a.D, h, df[0]);
+    uint4 qf[T::NF], df[T::NF];
+    T::load_cols(a.q, qi * a.ldq + (int64_t)head * a.D, live, a.D, h, qf);
+    T::load_cols(a.dout, qi * a.lddo + (int64_t)head * a.D, live, a.D, h, df);
     float lse = 0.f, delta = 0.f;
     {
         uint4 of[T::NF];
         T::load_cols(a.out, qi * a.ldo + (int64_t)head * a.D, live, a.D, h, of);
 #pragma unroll
-        for (int s = 0; s < T::NF; ++s) delta = T::frag_dot(df[0][s], of[s], delta);
+        for (int s = 0; s < T::NF; ++s) delta = T::frag_dot(df[s], of[s], delta);
         delta = half_sum(delta);
     }
+    Voxel qc{0, 0};
+    float slope = 0.f;  // of the scores where there is a cap, else of the products
     if (live) {
         lse = a.lse[qi * a.H + head] * kLog2e;
         if (h == 0 && sh.part == 0) a.delta[qi * a.H + head] = delta;
+        if constexpr (BIAS) {
+            qc = voxel_of(*(const int4*)(a.q_coords + 4 * qi));
+            slope = CAP ? a.slopes[head] * kLog2e : a.slopes[head] / a.scale;
+        }
     }
-    Voxel qc{0, 0};
-    float slope = 0.f, lift = 0.f;
-    if (BIAS && live) {
-        qc = voxel_of(*(const int4*)(a.q_coords + 4 * qi));
-        slope = a.slopes[head] * kLog2e;
-        lift = slope * 8388608.f;
-    }
-    f32x16 zref, dref;
+    const float lift = slope * 8388608.f;  // what the 2^23 of a distance brings too much
+    const float cs = a.scale * kLog2e;
+    const Capped capped(a);
+    f32x16 dref;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        zref[r] = S::kFold ? -lse / score.cs : 0.f;
-        dref[r] = -delta;
-    }
+    for (int r = 0; r < 16; ++r) dref[r] = -delta;
 
-    Stage<DT, DP, KT, TH> sk, sv;
+    Stage<DT, DP, KT, TH> sk(tid, a.ldk, a.D), sv(tid, a.ldv, a.D);
     int4 ck{0, 0, 0, 0};
-    auto load = [&](int64_t i) __attribute__((always_inline)) {
-        const int64_t r = k0 + i * KT;
-        sk.load(a.k, a.ldk, (int64_t)kh * a.D, r, k1, a.D, tid);
-        sv.load(a.v, a.ldv, (int64_t)kh * a.D, r, k1, a.D, tid);
+    auto load = [&](int i) __attribute__((always_inline)) {
+        const int64_t r = k0 + (int64_t)i * KT, n = k1 - r;
+        sk.load(rows_buffer((const char*)a.k + (r * a.ldk + kh * a.D) * T::SZ, a.ldk * T::SZ, n, KT, a.D * T::SZ));
+        sv.load(rows_buffer((const char*)a.v + (r * a.ldv + kh * a.D) * T::SZ, a.ldv * T::SZ, n, KT, a.D * T::SZ));
         if constexpr (BIAS)
-            if (tid < KT && r + tid < k1) ck = *(const int4*)(a.k_coords + 4 * (r + tid));
+            if (tid < KT)
+                ck = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                  rows_buffer(a.k_coords + 4 * r, 16, n, KT, 16), tid * 16, 0, 0));
     };
     auto store = [&](int s) __attribute__((always_inline)) {
         sk.store(lk[s], tid);
@@ -107,47 +102,49 @@ __global__ __launch_bounds__(64 * NW, dq_waves(DT, DP, NW)) void k_attn_dq(AttnA
                 lc[s][1][tid] = v.z;
             }
     };
-    f32x16 o[1][T::NB];
+    f32x16 o[T::NB];
 #pragma unroll
-    for (int b = 0; b < T::NB; ++b) o[0][b] = f32x16{};
+    for (int b = 0; b < T::NB; ++b) o[b] = f32x16{};
     if (t0 < t1) {
         load(t0);
         store(0);
         if (t0 + 1 < t1) load(t0 + 1);
     }
     __syncthreads();
-    for (int64_t i = t0; i < t1; ++i) {
-        const int s = (int)(i - t0) & 1;
+    for (int i = t0; i < t1; ++i) {
+        const int s = (i - t0) & 1;
         if (busy) {
-            f32x16 z[1] = {zref}, d[1] = {dref};
-            T::rows_dot(lk[s], lane, qf, z);
-            T::rows_dot(lv[s], lane, df, d);
+            f32x16 b{};
+            const f32x16 d = T::rows_dot(lv[s], lane, df, dref);
+            if constexpr (BIAS)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                uint32_t xy[4] = {}, zz[4] = {};
-                if constexpr (BIAS) {
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t xy[4], zz[4];
                     lds_words(&lc[s][0][8 * q + 4 * h], xy);
                     lds_words(&lc[s][1][8 * q + 4 * h], zz);
-                }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float b = 0.f, x;
-                    if constexpr (BIAS) b = fmaf(voxel_dist(xy[e], zz[e], qc.xy, qc.z), -slope, lift);
-                    const float bend = score(z[0][4 * q + e], b, lse, x);
-                    float g = __builtin_amdgcn_exp2f(x) * d[0][4 * q + e];
-                    if constexpr (CAP) g *= bend;
-                    z[0][4 * q + e] = g;
+                    for (int e = 0; e < 4; ++e)
+                        b[4 * q + e] = fmaf(voxel_dist(xy[e], zz[e], qc.xy, qc.z), -slope, lift);
+                }
+            f32x16 z = T::rows_dot(lk[s], lane, qf, CAP ? f32x16{} : b);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                if constexpr (CAP) {
+                    float x;
+                    const float bend = capped(z[r], BIAS ? b[r] + (capped.cap2 - lse) : capped.cap2 - lse, x);
+                    z[r] = __builtin_amdgcn_exp2f(x) * d[r] * bend;
+                } else {
+                    z[r] = __builtin_amdgcn_exp2f(fmaf(z[r], cs, -lse)) * d[r];
                 }
             }
-            if (k0 + (i + 1) * KT > k1) {  // keys past the scan's end: their rows are zero, but not their weights
-                const int end = (int)(k1 - k0 - i * KT);
+            const int end = keys - i * KT;
+            if (end < KT) {  // keys past the scan's end: their rows are zero, but not their weights
                 asm volatile("");  // a branch, not selects on every tile
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (8 * (r / 4) + 4 * h + r % 4 >= end) z[0][r] = 0.f;
+                    if (8 * (r / 4) + 4 * h + r % 4 >= end) z[r] = 0.f;
             }
-            const typename T::Weights w[1] = {T::weights(z[0])};
-            T::add_weighted(lk[s], lane, w, o);
+            T::add_weighted(lk[s], lane, T::weights(z), o);
         }
         if (i + 1 < t1) {
             store(s ^ 1);
@@ -156,27 +153,27 @@ __global__ __launch_bounds__(64 * NW, dq_waves(DT, DP, NW)) void k_attn_dq(AttnA
         __syncthreads();
     }
     if (!live) return;
-    const float f = a.scale * S::kBend;
+    const float f = a.scale * kBend<CAP>;
     if (a.part)
-        Tile<SPV_F32, DP>::store_cols(a.part, (((int64_t)sh.part * a.nq + qi) * a.H + head) * a.D, a.D, h, o[0], f);
+        Tile<SPV_F32, DP>::store_cols(a.part, (((int64_t)sh.part * a.nq + qi) * a.H + head) * a.D, a.D, h, o, f);
     else
-        T::store_cols(a.dq, qi * a.lddq + (int64_t)head * a.D, a.D, h, o[0], f);
+        T::store_cols(a.dq, qi * a.lddq + (int64_t)head * a.D, a.D, h, o, f);
 }
 
-// Columns are keys; the rows are the scan's queries, once for each head of the key head's group, in that order.
 // The weights are at most 1 and, over long scans, far below float16's smallest normal number (6e-5): in that type they
-// are multiplied as 2^12 p (and may be some times 1 where scores of millions round).  dz is not scaled: its size is that of dout, which a caller may have scaled up.
+// are multiplied as 2^12 p (and may be some times 1 where scores of millions round).  dz is not scaled: its size is
+// that of dout, which a caller may have scaled up.
 template <int DT>
 constexpr float kUp = DT == SPV_F16 ? 12.f : 0.f;
 
+// Columns are keys; the rows are the scan's queries, once for each head of the key head's group, in that order.
 template <int DT, int DP, int NW, bool BIAS, bool CAP>
 __global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(AttnArgs a) {
     using T = Tile<DT, DP>;
-    using S = Score<DT, CAP>;
     constexpr int KT = 32, TH = 64 * NW, BM = 32 * NW;
     __shared__ __align__(16) char lq[2][KT * T::LD], ld[2][KT * T::LD];
     __shared__ __align__(16) uint32_t lc[2][2][BIAS ? KT : 4];
-    __shared__ __align__(16) float lr[2][2][KT];  // the rows' lse (as the score wants it) and -delta
+    __shared__ float lr[2][2][64];  // the rows' -lse (see below) and -delta, then zeros
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
     const int G = a.H / a.K, kh = sh.kh;
@@ -187,38 +184,42 @@ __global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(Att
     const int64_t per = (all + sh.parts - 1) / sh.parts;
     const int64_t t0 = sh.part * per, t1 = t0 + per < all ? t0 + per : all;
 
-    const S score(a);
     const bool busy = t.col0 + 32 * wave < t.cols, live = t.col0 + 32 * wave + c < t.cols;
     const int64_t kj = t.first + t.col0 + 32 * wave + c;
-    uint4 kf[1][T::NF], vf[1][T::NF];
-    T::load_cols(a.k, kj * a.ldk + (int64_t)kh * a.D, live, a.D, h, kf[0]);
-    T::load_cols(a.v, kj * a.ldv + (int64_t)kh * a.D, live, a.D, h, vf[0]);
+    uint4 kf[T::NF], vf[T::NF];
+    T::load_cols(a.k, kj * a.ldk + (int64_t)kh * a.D, live, a.D, h, kf);
+    T::load_cols(a.v, kj * a.ldv + (int64_t)kh * a.D, live, a.D, h, vf);
     Voxel kc{0, 0};
     if (BIAS && live) kc = voxel_of(*(const int4*)(a.k_coords + 4 * kj));
+    const float cs = a.scale * kLog2e, inv_cs = 1.f / cs;
+    const Capped capped(a);
+    if (tid < 128) lr[tid >> 6][0][tid & 63] = lr[tid >> 6][1][tid & 63] = 0.f;
+    if (NW == 1) lr[1][0][lane] = lr[1][1][lane] = 0.f;
 
-    Stage<DT, DP, KT, TH> sq, sd;
+    Stage<DT, DP, KT, TH> sq(tid, a.ldq, a.D), sd(tid, a.lddo, a.D);
     int4 cq{0, 0, 0, 0};
     float rl = 0.f, rd = 0.f;
-    // tile i is number i % tiles of head i / tiles of the group
-    auto load = [&](int64_t i) __attribute__((always_inline)) {
-        const int64_t g = i / tiles, r = q0 + (i - g * tiles) * KT;
-        const int64_t head = (int64_t)kh * G + g;
-        sq.load(a.q, a.ldq, head * a.D, r, q1, a.D, tid);
-        sd.load(a.dout, a.lddo, head * a.D, r, q1, a.D, tid);
+    int64_t next = t0, g_next = tiles ? t0 / tiles : 0, i_next = t0 - g_next * tiles;  // the tile to load: head, tile of its rows
+    auto load = [&]() __attribute__((always_inline)) {
+        const int64_t r = q0 + i_next * KT, n = q1 - r, head = (int64_t)kh * G + g_next;
+        sq.load(rows_buffer((const char*)a.q + (r * a.ldq + head * a.D) * T::SZ, a.ldq * T::SZ, n, KT, a.D * T::SZ));
+        sd.load(rows_buffer((const char*)a.dout + (r * a.lddo + head * a.D) * T::SZ, a.lddo * T::SZ, n, KT, a.D * T::SZ));
         if (tid < KT) {
-            const bool in = r + tid < q1;
+            const bool in = tid < n;
             // a row past the end has no weight: its lse is infinite
-            rl = in ? a.lse[(r + tid) * a.H + head] * kLog2e - kUp<DT> : INFINITY;
+            rl = in ? kUp<DT> - a.lse[(r + tid) * a.H + head] * kLog2e : -INFINITY;
             rd = in ? -a.delta[(r + tid) * a.H + head] : 0.f;
             if constexpr (BIAS)
                 if (in) cq = *(const int4*)(a.q_coords + 4 * (r + tid));
         }
+        ++next;
+        if (++i_next == tiles) i_next = 0, ++g_next;
     };
     auto store = [&](int s) __attribute__((always_inline)) {
         sq.store(lq[s], tid);
         sd.store(ld[s], tid);
         if (tid < KT) {
-            lr[s][0][tid] = S::kFold ? -rl / score.cs : rl;
+            lr[s][0][tid] = CAP ? rl + capped.cap2 : rl * inv_cs;
             lr[s][1][tid] = rd;
             if constexpr (BIAS) {
                 const Voxel v = voxel_of(cq);
@@ -228,13 +229,15 @@ __global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(Att
         }
     };
     constexpr float down = DT == SPV_F16 ? 1.f / 4096.f : 1.f;  // 2^-kUp
-    f32x16 ok[1][T::NB], ov[1][T::NB];
+    f32x16 ok[T::NB], ov[T::NB];
 #pragma unroll
-    for (int b = 0; b < T::NB; ++b) ok[0][b] = ov[0][b] = f32x16{};
+    for (int b = 0; b < T::NB; ++b) ok[b] = ov[b] = f32x16{};
+    int64_t i_now = i_next, g_now = g_next;
+    __syncthreads();
     if (t0 < t1) {
-        load(t0);
+        load();
         store(0);
-        if (t0 + 1 < t1) load(t0 + 1);
+        if (t0 + 1 < t1) load();
     }
     __syncthreads();
     for (int64_t i = t0; i < t1; ++i) {
@@ -242,21 +245,12 @@ __global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(Att
         if (busy) {
             float slope = 0.f, lift = 0.f;
             if constexpr (BIAS) {
-                slope = a.slopes[(int64_t)kh * G + i / tiles] * kLog2e;
+                slope = a.slopes[(int64_t)kh * G + g_now] * kLog2e;
                 lift = slope * 8388608.f;
             }
-            f32x16 z[1], d[1];
-            float lse[16];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float4 x = *(const float4*)&lr[s][0][8 * q + 4 * h], y = *(const float4*)&lr[s][1][8 * q + 4 * h];
-                lse[4 * q] = x.x, lse[4 * q + 1] = x.y, lse[4 * q + 2] = x.z, lse[4 * q + 3] = x.w;
-                d[0][4 * q] = y.x, d[0][4 * q + 1] = y.y, d[0][4 * q + 2] = y.z, d[0][4 * q + 3] = y.w;
-            }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) z[0][r] = S::kFold ? lse[r] : 0.f;
-            T::rows_dot(lq[s], lane, kf, z);
-            T::rows_dot(ld[s], lane, vf, d);
+            f32x16 z = spread_rows(lr[s][0][lane]), rest = z;
+            f32x16 d = T::rows_dot(ld[s], lane, vf, spread_rows(lr[s][1][lane]));
+            z = T::rows_dot(lq[s], lane, kf, CAP ? f32x16{} : z);
             f32x16 p;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -268,35 +262,40 @@ __global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(Att
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = 4 * q + e;
-                    float b = 0.f, x;
+                    float b = 0.f;
                     if constexpr (BIAS) b = fmaf(voxel_dist(xy[e], zz[e], kc.xy, kc.z), -slope, lift);
-                    const float bend = score(z[0][r], b, lse[r], x);
-                    p[r] = __builtin_amdgcn_exp2f(x);
-                    z[0][r] = p[r] * d[0][r];
-                    if constexpr (CAP) z[0][r] *= bend;
-                    if constexpr (DT == SPV_F16) z[0][r] *= down;
+                    if constexpr (CAP) {
+                        float x;
+                        const float bend = capped(z[r], BIAS ? b + rest[r] : rest[r], x);
+                        p[r] = __builtin_amdgcn_exp2f(x);
+                        z[r] = p[r] * d[r] * bend;
+                    } else {
+                        p[r] = __builtin_amdgcn_exp2f(BIAS ? fmaf(z[r], cs, b) : z[r] * cs);
+                        z[r] = p[r] * d[r];
+                    }
+                    if constexpr (DT == SPV_F16) z[r] *= down;
                 }
             }
-            const typename T::Weights wp[1] = {T::weights(p)}, wz[1] = {T::weights(z[0])};
-            T::add_weighted(ld[s], lane, wp, ov);
-            T::add_weighted(lq[s], lane, wz, ok);
+            T::add_weighted(ld[s], lane, T::weights(p), ov);
+            T::add_weighted(lq[s], lane, T::weights(z), ok);
         }
+        if (++i_now == tiles) i_now = 0, ++g_now;
         if (i + 1 < t1) {
             store(s ^ 1);
-            if (i + 2 < t1) load(i + 2);
+            if (next < t1) load();
         }
         __syncthreads();
     }
     if (!live) return;
-    const float f = a.scale * S::kBend;
+    const float f = a.scale * kBend<CAP>;
     if (a.part) {
         const int64_t at = (((int64_t)sh.part * a.nk + kj) * a.K + kh) * a.D;
         const int64_t half = (int64_t)sh.parts * a.nk * a.K * a.D;
-        Tile<SPV_F32, DP>::store_cols(a.part, at, a.D, h, ok[0], f);
-        Tile<SPV_F32, DP>::store_cols(a.part, half + at, a.D, h, ov[0], down);
+        Tile<SPV_F32, DP>::store_cols(a.part, at, a.D, h, ok, f);
+        Tile<SPV_F32, DP>::store_cols(a.part, half + at, a.D, h, ov, down);
     } else {
-        T::store_cols(a.dk, kj * a.lddk + (int64_t)kh * a.D, a.D, h, ok[0], f);
-        T::store_cols(a.dv, kj * a.lddv + (int64_t)kh * a.D, a.D, h, ov[0], down);
+        T::store_cols(a.dk, kj * a.lddk + (int64_t)kh * a.D, a.D, h, ok, f);
+        T::store_cols(a.dv, kj * a.lddv + (int64_t)kh * a.D, a.D, h, ov, down);
     }
 }
 

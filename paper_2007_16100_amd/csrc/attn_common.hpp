@@ -106,6 +106,16 @@ __device__ inline float half_max(float v) {
     return fmaxf(r.x, r.y);
 }
 
+template <int DT>
+__device__ inline f32x16 mfma32x32x16(uint4 a, uint4 b, f32x16 c) {
+    if constexpr (DT == SPV_BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+                                                       0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
+                                                      0, 0);
+}
+
 // Rows of up to DP channels (a multiple of 32; D <= DP of them real, the rest zero) in LDS, and products with them.
 template <int DT, int DP>
 struct Tile {
@@ -126,30 +136,22 @@ struct Tile {
         }
     }
 
-    // c[n] + rows (32 of them, at lds) . columns f[n]: a fragment of the rows is read once for all CB column blocks
-    template <int CB>
-    static __device__ inline void rows_dot(const char* lds, int lane, const uint4 (&f)[CB][NF], f32x16 (&c)[CB]) {
+    // c + rows (32 of them, at lds) . columns
+    static __device__ inline f32x16 rows_dot(const char* lds, int lane, const uint4 (&f)[NF], f32x16 c) {
         const char* a = lds + (lane & 31) * LD + (lane >> 5) * 16;
 #pragma unroll
         for (int s = 0; s < NF; ++s) {
-            const uint4 x = *(const uint4*)(a + 32 * s);
-#pragma unroll
-            for (int n = 0; n < CB; ++n) {
-                const uint4 y = f[n][s];
-                if constexpr (W) {
-                    c[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.x), __uint_as_float(y.x), c[n], 0, 0, 0);
-                    c[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.y), __uint_as_float(y.y), c[n], 0, 0, 0);
-                    c[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.z), __uint_as_float(y.z), c[n], 0, 0, 0);
-                    c[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.w), __uint_as_float(y.w), c[n], 0, 0, 0);
-                } else if constexpr (DT == SPV_BF16) {
-                    c[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
-                                                                   __builtin_bit_cast(bf16x8, y), c[n], 0, 0, 0);
-                } else {
-                    c[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x),
-                                                                  __builtin_bit_cast(f16x8, y), c[n], 0, 0, 0);
-                }
+            const uint4 x = *(const uint4*)(a + 32 * s), y = f[s];
+            if constexpr (W) {
+                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.x), __uint_as_float(y.x), c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.y), __uint_as_float(y.y), c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.z), __uint_as_float(y.z), c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x.w), __uint_as_float(y.w), c, 0, 0, 0);
+            } else {
+                c = mfma32x32x16<DT>(x, y, c);
             }
         }
+        return c;
     }
 
     // the weights of 32 rows (accumulator registers) as B operands
@@ -205,23 +207,19 @@ struct Tile {
         return s;
     }
 
-    // o[n][b] + (channels 32 b .. 32 b + 31 of the 32 rows at lds, transposed) . weights w[n]: lane (c, h) of
-    // o[n][b] holds channels 32 b + 8 (i / 4) + 4 h + i % 4 of column c
-    template <int CB>
-    static __device__ inline void add_weighted(const char* lds, int lane, const Weights (&w)[CB], f32x16 (&o)[CB][NB]) {
+    // o[b] + (channels 32 b .. 32 b + 31 of the 32 rows at lds, transposed) . weights: lane (c, h) of o[b] holds
+    // channels 32 b + 8 (i / 4) + 4 h + i % 4 of column c
+    static __device__ inline void add_weighted(const char* lds, int lane, const Weights& w, f32x16 (&o)[NB]) {
         if constexpr (W) {
             const char* a = lds + (lane >> 5) * 4 * LD + (lane & 31) * 4;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t u[4] = {w.f[i / 4].x, w.f[i / 4].y, w.f[i / 4].z, w.f[i / 4].w};
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    const float x = *(const float*)(a + (8 * (i / 4) + i % 4) * LD + 128 * b);
-#pragma unroll
-                    for (int n = 0; n < CB; ++n) {
-                        const uint32_t u[4] = {w[n].f[i / 4].x, w[n].f[i / 4].y, w[n].f[i / 4].z, w[n].f[i / 4].w};
-                        o[n][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, __uint_as_float(u[i % 4]), o[n][b], 0, 0, 0);
-                    }
-                }
+                for (int b = 0; b < NB; ++b)
+                    o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float*)(a + (8 * (i / 4) + i % 4) * LD + 128 * b),
+                                                                __uint_as_float(u[i % 4]), o[b], 0, 0, 0);
+            }
         } else {
             typedef short i16x8 __attribute__((ext_vector_type(8)));
             typedef __attribute__((address_space(3))) i16x4 lds4;
@@ -235,15 +233,7 @@ struct Tile {
                     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(a + 16 * k * LD + 64 * b));
                     const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(a + (16 * k + 8) * LD + 64 * b));
                     const i16x8 x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-                    for (int n = 0; n < CB; ++n) {
-                        if constexpr (DT == SPV_BF16)
-                            o[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                                __builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, w[n].f[k]), o[n][b], 0, 0, 0);
-                        else
-                            o[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                                __builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, w[n].f[k]), o[n][b], 0, 0, 0);
-                    }
+                    o[b] = mfma32x32x16<DT>(__builtin_bit_cast(uint4, x), w.f[k], o[b]);
                 }
         }
     }
@@ -273,30 +263,44 @@ __device__ inline void lds_words(const uint32_t* p, uint32_t (&w)[4]) {
     w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
 }
 
-// KT rows of DP channels on their way from memory to LDS by TH threads: loaded to registers a tile ahead, zeros for
-// rows past `end` and channels past D
+// a value of each of 32 rows (in lanes 0 .. 31; 0 in the others) to every column of that row's accumulators, exactly:
+// a product with ones, where reading them from LDS would take eight times the LDS cycles of all else in a score
+__device__ inline f32x16 spread_rows(float v) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(v, 1.f, f32x16{}, 0, 0, 0);
+}
+
+// n (at most KT) rows from p, ld bytes apart and D bytes each, as a buffer: what lies outside reads as zero
+__device__ inline __amdgpu_buffer_rsrc_t rows_buffer(const void* p, int64_t ld, int64_t n, int KT, int D) {
+    const int64_t r = n < KT ? n : KT;
+    return make_rsrc(p, r > 0 ? (uint32_t)((r - 1) * ld + D) : 0u);
+}
+
+// KT rows of DP channels on their way from memory to LDS by TH threads: 16 bytes at a time, loaded to registers a tile
+// ahead; zeros for rows past the buffer's and channels past D.  The offsets within a tile stay the same.
 template <int DT, int DP, int KT, int TH>
 struct Stage {
     using T = Tile<DT, DP>;
-    static constexpr int N = (KT * T::CH + TH - 1) / TH;  // chunks of a thread; past the last: none
-    
+    static constexpr int RP = TH / T::CH, N = (KT + RP - 1) / RP;  // rows a pass, passes
+    uint32_t off[N];
     uint4 u[N];
-    __device__ inline void load(const void* p, int64_t ld, int64_t head, int64_t row0, int64_t end, int D, int tid) {
+    __device__ Stage(int tid, int64_t ld, int D) {
+        const int r = tid / T::CH, ch = tid % T::CH;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int id = tid + i * TH, r = id / T::CH, ch = id % T::CH;
-            u[i] = (KT * T::CH % TH == 0 || id < KT * T::CH) && row0 + r < end && ch * T::E < D
-                       ? *(const uint4*)((const char*)p + ((row0 + r) * ld + head + ch * T::E) * T::SZ)
-                       : make_uint4(0, 0, 0, 0);
-        }
+        for (int i = 0; i < N; ++i)
+            off[i] = r < RP && r + i * RP < KT && ch * T::E < D ? (uint32_t)((r + i * RP) * ld + ch * T::E) * T::SZ
+                                                                 : kOutOfRange;
+    }
+    __device__ inline void load(__amdgpu_buffer_rsrc_t rows) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            u[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rows, off[i], 0, 0));
     }
     __device__ inline void store(char* lds, int tid) const {
+        const int r = tid / T::CH, ch = tid % T::CH;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int id = tid + i * TH;
-            if (KT * T::CH % TH == 0 || id < KT * T::CH)
-                *(uint4*)(lds + (id / T::CH) * T::LD + (id % T::CH) * 16) = u[i];
-        }
+        for (int i = 0; i < N; ++i)
+            if ((TH % T::CH == 0 || r < RP) && (KT % RP == 0 || r + i * RP < KT))
+                *(uint4*)(lds + (r + i * RP) * T::LD + ch * 16) = u[i];
     }
 };
 
