@@ -7,7 +7,7 @@
 namespace spv {
 
 // Columns are (query, head of a key head's group) pairs, so shared key heads are staged once for all of their query
-// heads; a workgroup takes 32 NW columns of one scan and one key head.  Scores are kept in units of log 2.  A column's
+// heads; a workgroup takes the columns of one scan and one key head.  Scores are kept in units of log 2.  A column's
 // reference m moves (and the sums are scaled) only when a score passes it by more than kLead: weights of up to
 // 2^kLead lose nothing in float32 sums or 16-bit weights, and after the first tiles m hardly ever moves.
 // The bias, over scale, is what the products are added to; a cap's tanh stands between them, so it is added after.
@@ -18,19 +18,19 @@ constexpr float kLead = 8.f;
 #define OCC32 3
 #endif
 #ifndef OCC64
-#define OCC64 4
+#define OCC64 3
 #endif
-constexpr int attn_waves(int dt, int DP, int nw) {
-    return nw == 1 || dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? OCC64 : OCC32;
-}
+constexpr int attn_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? OCC64 : OCC32; }
 
-template <int DT, int DP, int NW, bool BIAS, bool CAP>
-__global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnArgs a) {
+template <int DT, int DP, int KW, bool BIAS, bool CAP>
+__global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     using T = Tile<DT, DP>;
-    constexpr int KT = attn_rows(DT, DP), KS = KT / 32, TH = 64 * NW, BM = 32 * NW;
+    constexpr int RT = attn_rows(DT, DP, KW), KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
-    __shared__ __align__(16) uint32_t lc[2][2][BIAS ? KT : 4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
+    __shared__ __align__(16) Places<BIAS ? KT : 32> lc;
+    __shared__ int box[4][6];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), cw = wave / KW, kw = wave % KW;
+    const int c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
     const int G = a.H / a.K, kh = sh.kh;
     const ScanTile t = find_tile(a.q_off, a.B, a.nq, G, BM, sh.tile);
@@ -40,72 +40,81 @@ __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnAr
     const int per = (tiles + sh.parts - 1) / sh.parts, t0 = sh.part * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
     // the lane's column
-    const bool busy = t.col0 + 32 * wave < t.cols, live = t.col0 + 32 * wave + c < t.cols;
+    const bool busy = t.col0 + 32 * cw < t.cols, live = t.col0 + 32 * cw + c < t.cols;
     const int64_t q0 = t.col0 / G;
-    const int x = (int)(t.col0 - q0 * G) + 32 * wave + c, head = kh * G + x % G;
+    const int x = (int)(t.col0 - q0 * G) + 32 * cw + c, head = kh * G + x % G;
     const int64_t qi = t.first + q0 + x / G;
     uint4 qf[T::NF];
     T::load_cols(a.q, qi * a.ldq + (int64_t)head * a.D, live, a.D, h, qf);
     const float cs = a.scale * kLog2e, cz = CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
-    Voxel qc{0, 0};
+    Words far{0, 0};
+    uint32_t place = 0;
+    Cube cube{};
     float slope = 0.f;  // of the scores where there is a cap, else of the products
-    if (BIAS && live) {
-        qc = voxel_of(*(const int4*)(a.q_coords + 4 * qi));
-        slope = CAP ? a.slopes[head] * kLog2e : a.slopes[head] / a.scale;
+    if constexpr (BIAS) {
+        int4 qc{0, 0, 0, 0};
+        if (live) {
+            qc = voxel_clamp(*(const int4*)(a.q_coords + 4 * qi));
+            slope = CAP ? a.slopes[head] * kLog2e : a.slopes[head] / a.scale;
+        }
+        cube = columns_cube(qc, live, box);
+        cube.place(qc, place);
+        far = voxel_words(qc);
     }
-    const float lift = slope * 8388608.f;  // what the 2^23 of a distance brings too much
+    const float lift = slope * 8388608.f;
 
-    Stage<DT, DP, KT, TH> sk(tid, a.ldk, a.D), sv(tid, a.ldv, a.D);
+    Stage<DT, DP, KT, 256> sk(tid, a.ldk, a.D), sv(tid, a.ldv, a.D);
+    const int64_t first = k0 + (int64_t)t0 * KT;
+    RowTiles<KT> rk((const char*)a.k + kh * a.D * T::SZ, first, k1, a.ldk * T::SZ, a.D * T::SZ);
+    RowTiles<KT> rv((const char*)a.v + kh * a.D * T::SZ, first, k1, a.ldv * T::SZ, a.D * T::SZ);
+    RowTiles<KT> rc(a.k_coords, first, k1, 16, 16);
     int4 ck{0, 0, 0, 0};
-    auto load = [&](int i) __attribute__((always_inline)) {
-        const int64_t r = k0 + (int64_t)i * KT, n = k1 - r;
-        sk.load(rows_buffer((const char*)a.k + (r * a.ldk + kh * a.D) * T::SZ, a.ldk * T::SZ, n, KT, a.D * T::SZ));
-        sv.load(rows_buffer((const char*)a.v + (r * a.ldv + kh * a.D) * T::SZ, a.ldv * T::SZ, n, KT, a.D * T::SZ));
-        if constexpr (BIAS)
-            if (tid < KT)
-                ck = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                  rows_buffer(a.k_coords + 4 * r, 16, n, KT, 16), tid * 16, 0, 0));
+    int64_t ck_left = 0;
+    auto load = [&]() __attribute__((always_inline)) {
+        sk.load(rk.next());
+        sv.load(rv.next());
+        if constexpr (BIAS) {
+            ck_left = rc.left;
+            const __amdgpu_buffer_rsrc_t r = rc.next();
+            if (tid < KT) ck = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(r, tid * 16, 0, 0));
+        }
     };
     auto store = [&](int s) __attribute__((always_inline)) {
         sk.store(lk[s], tid);
         sv.store(lv[s], tid);
         if constexpr (BIAS)
-            if (tid < KT) {
-                const Voxel v = voxel_of(ck);
-                lc[s][0][tid] = v.xy;
-                lc[s][1][tid] = v.z;
-            }
+            if (tid < KT) lc.put(s, tid, ck, tid < ck_left, cube);
     };
 
+    // weights of scores (relative to m already under a cap)
+    auto weights = [](const f32x16& z, float cs, float m) __attribute__((always_inline)) {
+        f32x16 p;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(CAP ? z[r] : fmaf(z[r], cs, -m));
+        return T::weights(p);
+    };
     f32x16 o[T::NB];
 #pragma unroll
     for (int b = 0; b < T::NB; ++b) o[b] = f32x16{};
     float m = 0.f, l = 0.f;
     if (t0 < t1) {
-        load(t0);
+        load();
         store(0);
-        if (t0 + 1 < t1) load(t0 + 1);
+        if (t0 + 1 < t1) load();
     }
     __syncthreads();
+    bool first_rows = true;
     for (int i = t0; i < t1; ++i) {
         const int s = (i - t0) & 1;
-        if (busy) {
+        const int row0 = RT * kw, left = keys - i * KT - row0;  // the wave's rows of the tile, keys from there on
+        if (busy && left > 0) {
             f32x16 z[KS], bias[CAP && BIAS ? KS : 1];
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
                 f32x16 b{};
-                if constexpr (BIAS)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t xy[4], zz[4];
-                        lds_words(&lc[s][0][32 * u + 8 * q + 4 * h], xy);
-                        lds_words(&lc[s][1][32 * u + 8 * q + 4 * h], zz);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            b[4 * q + e] = fmaf(voxel_dist(xy[e], zz[e], qc.xy, qc.z), -slope, lift);
-                    }
+                if constexpr (BIAS) lc.bias(s, row0 + 32 * u, h, far, place, slope, lift, b);
                 if constexpr (CAP && BIAS) bias[u] = b;
-                z[u] = T::rows_dot(lk[s] + 32 * u * T::LD, lane, qf, CAP ? f32x16{} : b);
+                z[u] = T::rows_dot(lk[s] + (row0 + 32 * u) * T::LD, lane, qf, CAP ? f32x16{} : b);
             }
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
@@ -117,7 +126,7 @@ __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnAr
                         z[u][r] = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(ex + 1.f),
                                        BIAS ? bias[BIAS ? u : 0][r] + (cap2 - m) : cap2 - m);
                     }
-                const int end = keys - i * KT - 32 * u;
+                const int end = left - 32 * u;
                 if (end < 32) {  // keys past the scan's end
                     asm volatile("");  // a branch: selects on every tile cost two instructions a score
 #pragma unroll
@@ -128,11 +137,11 @@ __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnAr
 #pragma unroll
                 for (int r = 1; r < 16; ++r) d = fmaxf(d, z[u][r]);
                 if constexpr (!CAP) d = fmaf(d, cs, -m);
-                const bool first = i == t0 && u == 0;
-                if (first || __any(d > kLead)) {
+                if (first_rows || __any(d > kLead)) {
                     d = half_max(d);
-                    const float up = first || d > kLead ? d : 0.f;
-                    const float f = first ? 1.f : __builtin_amdgcn_exp2f(-up);
+                    const float up = first_rows || d > kLead ? d : 0.f;
+                    const float f = first_rows ? 1.f : __builtin_amdgcn_exp2f(-up);
+                    first_rows = false;
                     m += up;
                     l *= f;
 #pragma unroll
@@ -143,20 +152,52 @@ __global__ __launch_bounds__(64 * NW, attn_waves(DT, DP, NW)) void k_attn(AttnAr
 #pragma unroll
                         for (int r = 0; r < 16; ++r) z[u][r] -= up;
                 }
-#pragma unroll
-                for (int r = 0; r < 16; ++r) z[u][r] = __builtin_amdgcn_exp2f(CAP ? z[u][r] : fmaf(z[u][r], cs, -m));
-                const typename T::Weights w = T::weights(z[u]);
+                const typename T::Weights w = weights(z[u], cs, m);
                 l = T::sum(w, l);
-                T::add_weighted(lv[s] + 32 * u * T::LD, lane, w, o);
+                T::add_weighted(lv[s] + (row0 + 32 * u) * T::LD, lane, w, o);
             }
         }
         if (i + 1 < t1) {
             store(s ^ 1);
-            if (i + 2 < t1) load(i + 2);
+            if (i + 2 < t1) load();
         }
         __syncthreads();
     }
     l = half_sum(l);
+    if constexpr (KW > 1) {
+        // the waves of a block of columns join under their largest reference (the tiles' LDS is free by now)
+        static_assert(2 * KT * T::LD >= CW * (KW - 1) * (T::NB * 16 + 2) * 256, "a wave's sums have room");
+        constexpr int N = (T::NB * 16 + 2) * 64;
+        float* p = (float*)&lk[0][0] + (cw * (KW - 1) + kw - 1) * N;
+        if (kw) {
+            lds_put(p + 128, lane, o);
+            p[lane] = m;
+            p[64 + lane] = l;
+        }
+        __syncthreads();
+        if (kw) return;
+        p += N;
+        float top = l != 0.f ? m : -INFINITY;
+#pragma unroll
+        for (int w = 1; w < KW; ++w)
+            if (p[(w - 1) * N + 64 + lane] != 0.f) top = fmaxf(top, p[(w - 1) * N + lane]);
+        const float f = l != 0.f ? __builtin_amdgcn_exp2f(m - top) : 0.f;
+        l *= f;
+#pragma unroll
+        for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[b][r] *= f;
+#pragma unroll
+        for (int w = 1; w < KW; ++w) {
+            const float* pw = p + (w - 1) * N;
+            const float lw = pw[64 + lane];
+            if (lw == 0.f) continue;  // both lanes of a column: no key among the wave's
+            const float fw = __builtin_amdgcn_exp2f(pw[lane] - top);
+            l = fmaf(fw, lw, l);
+            lds_add(pw + 128, lane, fw, o);
+        }
+        m = l != 0.f ? top : 0.f;
+    }
     if (!live) return;
     const int64_t row = qi * a.H + head;
     if (a.part) {
@@ -254,7 +295,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int parts) {
 // host
 // ---------------------------------------------------------------------------
 static AttnShape forward_shape(const AttnArgs& a) {
-    return attn_shape(a.nq, a.H / a.K, a.B, a.K, a.nk / (a.B < 1 ? 1 : a.B) / attn_rows(a.dt, attn_dp(a.D)));
+    return attn_shape(a.dt, attn_dp(a.D), a.nq, a.H / a.K, a.B, a.K, a.nk / (a.B < 1 ? 1 : a.B));
 }
 
 bool attention_supported(const AttnArgs& a) {
@@ -270,17 +311,19 @@ void plan_attention_ws(Arena& a, AttnArgs& t) {
     t.part = a.take<float>(rows * (size_t)t.D);
 }
 
-template <int DT, int DP, int NW>
+template <int DT, int DP, int KW>
 static void attn_launch(hipStream_t s, const AttnArgs& a, const AttnShape& sh) {
     const dim3 g = attn_grid(sh, a.K);
-    if (a.slopes && a.cap > 0.f) k_attn<DT, DP, NW, true, true><<<g, 64 * NW, 0, s>>>(a);
-    else if (a.slopes) k_attn<DT, DP, NW, true, false><<<g, 64 * NW, 0, s>>>(a);
-    else if (a.cap > 0.f) k_attn<DT, DP, NW, false, true><<<g, 64 * NW, 0, s>>>(a);
-    else k_attn<DT, DP, NW, false, false><<<g, 64 * NW, 0, s>>>(a);
+    if (a.slopes && a.cap > 0.f) k_attn<DT, DP, KW, true, true><<<g, 256, 0, s>>>(a);
+    else if (a.slopes) k_attn<DT, DP, KW, true, false><<<g, 256, 0, s>>>(a);
+    else if (a.cap > 0.f) k_attn<DT, DP, KW, false, true><<<g, 256, 0, s>>>(a);
+    else k_attn<DT, DP, KW, false, false><<<g, 256, 0, s>>>(a);
 }
 template <int DT, int DP>
 static void attn_dp_launch(hipStream_t s, const AttnArgs& a, const AttnShape& sh) {
-    if (sh.nw == 4) attn_launch<DT, DP, 4>(s, a, sh);
+    constexpr int K1 = attn_kw(DT, DP, 1), K2 = attn_kw(DT, DP, 2);
+    if (K2 > 1 && sh.mode == 2) attn_launch<DT, DP, K2>(s, a, sh);
+    else if (K1 > 1 && sh.mode == 1) attn_launch<DT, DP, K1>(s, a, sh);
     else attn_launch<DT, DP, 1>(s, a, sh);
 }
 template <int DT>

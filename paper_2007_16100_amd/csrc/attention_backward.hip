@@ -31,16 +31,18 @@ constexpr float kBend = CAP ? 4.f : 1.f;
 #ifndef OCK
 #define OCK 2
 #endif
-constexpr int dq_waves(int dt, int DP, int nw) { return nw == 1 || dt == SPV_F32 || DP > 64 ? 1 : OCQ; }
-constexpr int dkv_waves(int dt, int DP, int nw) { return nw == 1 || dt == SPV_F32 || DP > 64 ? 1 : OCK; }
+constexpr int dq_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? 2 : OCQ; }
+constexpr int dkv_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? 2 : OCK; }
 
-template <int DT, int DP, int NW, bool BIAS, bool CAP>
-__global__ __launch_bounds__(64 * NW, dq_waves(DT, DP, NW)) void k_attn_dq(AttnArgs a) {
+template <int DT, int DP, int KW, bool BIAS, bool CAP>
+__global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     using T = Tile<DT, DP>;
-    constexpr int KT = 32, TH = 64 * NW, BM = 32 * NW;
+    constexpr int KT = 32 * KW, CW = 4 / KW, BM = 32 * CW;
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
-    __shared__ __align__(16) uint32_t lc[2][2][BIAS ? KT : 4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
+    __shared__ __align__(16) Places<BIAS ? KT : 32> lc;
+    __shared__ int box[4][6];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), cw = wave / KW, kw = wave % KW;
+    const int c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
     const int G = a.H / a.K, kh = sh.kh;
     const ScanTile t = find_tile(a.q_off, a.B, a.nq, G, BM, sh.tile);
@@ -49,9 +51,9 @@ __global__ __launch_bounds__(64 * NW, dq_waves(DT, DP, NW)) void k_attn_dq(AttnA
     const int keys = (int)(k1 > k0 ? k1 - k0 : 0), tiles = keys / KT + (keys % KT != 0);
     const int per = (tiles + sh.parts - 1) / sh.parts, t0 = sh.part * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
-    const bool busy = t.col0 + 32 * wave < t.cols, live = t.col0 + 32 * wave + c < t.cols;
+    const bool busy = t.col0 + 32 * cw < t.cols, live = t.col0 + 32 * cw + c < t.cols;
     const int64_t q0 = t.col0 / G;
-    const int y0 = (int)(t.col0 - q0 * G) + 32 * wave + c, head = kh * G + y0 % G;
+    const int y0 = (int)(t.col0 - q0 * G) + 32 * cw + c, head = kh * G + y0 % G;
     const int64_t qi = t.first + q0 + y0 / G;
     uint4 qf[T::NF], df[T::NF];
     T::load_cols(a.q, qi * a.ldq + (int64_t)head * a.D, live, a.D, h, qf);
@@ -64,69 +66,70 @@ __global__ __launch_bounds__(64 * NW, dq_waves(DT, DP, NW)) void k_attn_dq(AttnA
         for (int s = 0; s < T::NF; ++s) delta = T::frag_dot(df[s], of[s], delta);
         delta = half_sum(delta);
     }
-    Voxel qc{0, 0};
+    Words far{0, 0};
+    uint32_t place = 0;
+    Cube cube{};
     float slope = 0.f;  // of the scores where there is a cap, else of the products
     if (live) {
         lse = a.lse[qi * a.H + head] * kLog2e;
-        if (h == 0 && sh.part == 0) a.delta[qi * a.H + head] = delta;
-        if constexpr (BIAS) {
-            qc = voxel_of(*(const int4*)(a.q_coords + 4 * qi));
+        if (h == 0 && sh.part == 0 && kw == 0) a.delta[qi * a.H + head] = delta;
+    }
+    if constexpr (BIAS) {
+        int4 qc{0, 0, 0, 0};
+        if (live) {
+            qc = voxel_clamp(*(const int4*)(a.q_coords + 4 * qi));
             slope = CAP ? a.slopes[head] * kLog2e : a.slopes[head] / a.scale;
         }
+        cube = columns_cube(qc, live, box);
+        cube.place(qc, place);
+        far = voxel_words(qc);
     }
-    const float lift = slope * 8388608.f;  // what the 2^23 of a distance brings too much
+    const float lift = slope * 8388608.f;
     const float cs = a.scale * kLog2e;
     const Capped capped(a);
     f32x16 dref;
 #pragma unroll
     for (int r = 0; r < 16; ++r) dref[r] = -delta;
 
-    Stage<DT, DP, KT, TH> sk(tid, a.ldk, a.D), sv(tid, a.ldv, a.D);
+    Stage<DT, DP, KT, 256> sk(tid, a.ldk, a.D), sv(tid, a.ldv, a.D);
+    const int64_t first = k0 + (int64_t)t0 * KT;
+    RowTiles<KT> rk((const char*)a.k + kh * a.D * T::SZ, first, k1, a.ldk * T::SZ, a.D * T::SZ);
+    RowTiles<KT> rv((const char*)a.v + kh * a.D * T::SZ, first, k1, a.ldv * T::SZ, a.D * T::SZ);
+    RowTiles<KT> rc(a.k_coords, first, k1, 16, 16);
     int4 ck{0, 0, 0, 0};
-    auto load = [&](int i) __attribute__((always_inline)) {
-        const int64_t r = k0 + (int64_t)i * KT, n = k1 - r;
-        sk.load(rows_buffer((const char*)a.k + (r * a.ldk + kh * a.D) * T::SZ, a.ldk * T::SZ, n, KT, a.D * T::SZ));
-        sv.load(rows_buffer((const char*)a.v + (r * a.ldv + kh * a.D) * T::SZ, a.ldv * T::SZ, n, KT, a.D * T::SZ));
-        if constexpr (BIAS)
-            if (tid < KT)
-                ck = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                  rows_buffer(a.k_coords + 4 * r, 16, n, KT, 16), tid * 16, 0, 0));
+    int64_t ck_left = 0;
+    auto load = [&]() __attribute__((always_inline)) {
+        sk.load(rk.next());
+        sv.load(rv.next());
+        if constexpr (BIAS) {
+            ck_left = rc.left;
+            const __amdgpu_buffer_rsrc_t r = rc.next();
+            if (tid < KT) ck = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(r, tid * 16, 0, 0));
+        }
     };
     auto store = [&](int s) __attribute__((always_inline)) {
         sk.store(lk[s], tid);
         sv.store(lv[s], tid);
         if constexpr (BIAS)
-            if (tid < KT) {
-                const Voxel v = voxel_of(ck);
-                lc[s][0][tid] = v.xy;
-                lc[s][1][tid] = v.z;
-            }
+            if (tid < KT) lc.put(s, tid, ck, tid < ck_left, cube);
     };
     f32x16 o[T::NB];
 #pragma unroll
     for (int b = 0; b < T::NB; ++b) o[b] = f32x16{};
     if (t0 < t1) {
-        load(t0);
+        load();
         store(0);
-        if (t0 + 1 < t1) load(t0 + 1);
+        if (t0 + 1 < t1) load();
     }
     __syncthreads();
     for (int i = t0; i < t1; ++i) {
         const int s = (i - t0) & 1;
-        if (busy) {
+        const int row0 = 32 * kw, end = keys - i * KT - row0;  // the wave's rows of the tile, keys from there on
+        if (busy && end > 0) {
             f32x16 b{};
-            const f32x16 d = T::rows_dot(lv[s], lane, df, dref);
-            if constexpr (BIAS)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t xy[4], zz[4];
-                    lds_words(&lc[s][0][8 * q + 4 * h], xy);
-                    lds_words(&lc[s][1][8 * q + 4 * h], zz);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        b[4 * q + e] = fmaf(voxel_dist(xy[e], zz[e], qc.xy, qc.z), -slope, lift);
-                }
-            f32x16 z = T::rows_dot(lk[s], lane, qf, CAP ? f32x16{} : b);
+            const f32x16 d = T::rows_dot(lv[s] + row0 * T::LD, lane, df, dref);
+            if constexpr (BIAS) lc.bias(s, row0, h, far, place, slope, lift, b);
+            f32x16 z = T::rows_dot(lk[s] + row0 * T::LD, lane, qf, CAP ? f32x16{} : b);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 if constexpr (CAP) {
@@ -137,20 +140,30 @@ __global__ __launch_bounds__(64 * NW, dq_waves(DT, DP, NW)) void k_attn_dq(AttnA
                     z[r] = __builtin_amdgcn_exp2f(fmaf(z[r], cs, -lse)) * d[r];
                 }
             }
-            const int end = keys - i * KT;
-            if (end < KT) {  // keys past the scan's end: their rows are zero, but not their weights
+            if (end < 32) {  // keys past the scan's end: their rows are zero, but not their weights
                 asm volatile("");  // a branch, not selects on every tile
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (8 * (r / 4) + 4 * h + r % 4 >= end) z[r] = 0.f;
             }
-            T::add_weighted(lk[s], lane, T::weights(z), o);
+            T::add_weighted(lk[s] + row0 * T::LD, lane, T::weights(z), o);
         }
         if (i + 1 < t1) {
             store(s ^ 1);
-            if (i + 2 < t1) load(i + 2);
+            if (i + 2 < t1) load();
         }
         __syncthreads();
+    }
+    if constexpr (KW > 1) {
+        // the waves of a block of columns add up (the tiles' LDS is free by now)
+        static_assert(2 * KT * T::LD >= CW * (KW - 1) * T::NB * 16 * 256, "a wave's sums have room");
+        constexpr int N = T::NB * 16 * 64;
+        float* p = (float*)&lk[0][0] + cw * (KW - 1) * N;
+        if (kw) lds_put(p + (kw - 1) * N, lane, o);
+        __syncthreads();
+        if (kw) return;
+#pragma unroll
+        for (int w = 1; w < KW; ++w) lds_add(p + (w - 1) * N, lane, 1.f, o);
     }
     if (!live) return;
     const float f = a.scale * kBend<CAP>;
@@ -167,14 +180,16 @@ template <int DT>
 constexpr float kUp = DT == SPV_F16 ? 12.f : 0.f;
 
 // Columns are keys; the rows are the scan's queries, once for each head of the key head's group, in that order.
-template <int DT, int DP, int NW, bool BIAS, bool CAP>
-__global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(AttnArgs a) {
+template <int DT, int DP, int KW, bool BIAS, bool CAP>
+__global__ __launch_bounds__(256, dkv_waves(DT, DP)) void k_attn_dkv(AttnArgs a) {
     using T = Tile<DT, DP>;
-    constexpr int KT = 32, TH = 64 * NW, BM = 32 * NW;
+    constexpr int KT = 32 * KW, CW = 4 / KW, BM = 32 * CW;
     __shared__ __align__(16) char lq[2][KT * T::LD], ld[2][KT * T::LD];
-    __shared__ __align__(16) uint32_t lc[2][2][BIAS ? KT : 4];
-    __shared__ float lr[2][2][64];  // the rows' -lse (see below) and -delta, then zeros
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, h = lane >> 5;
+    __shared__ __align__(16) Places<BIAS ? KT : 32> lc;
+    __shared__ int box[4][6];
+    __shared__ float lr[2][2][KW][64];  // each 32 rows' -lse (see below) and -delta, then zeros
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), cw = wave / KW, kw = wave % KW;
+    const int c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
     const int G = a.H / a.K, kh = sh.kh;
     const ScanTile t = find_tile(a.k_off, a.B, a.nk, 1, BM, sh.tile);
@@ -184,28 +199,37 @@ __global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(Att
     const int64_t per = (all + sh.parts - 1) / sh.parts;
     const int64_t t0 = sh.part * per, t1 = t0 + per < all ? t0 + per : all;
 
-    const bool busy = t.col0 + 32 * wave < t.cols, live = t.col0 + 32 * wave + c < t.cols;
-    const int64_t kj = t.first + t.col0 + 32 * wave + c;
+    const bool busy = t.col0 + 32 * cw < t.cols, live = t.col0 + 32 * cw + c < t.cols;
+    const int64_t kj = t.first + t.col0 + 32 * cw + c;
     uint4 kf[T::NF], vf[T::NF];
     T::load_cols(a.k, kj * a.ldk + (int64_t)kh * a.D, live, a.D, h, kf);
     T::load_cols(a.v, kj * a.ldv + (int64_t)kh * a.D, live, a.D, h, vf);
-    Voxel kc{0, 0};
-    if (BIAS && live) kc = voxel_of(*(const int4*)(a.k_coords + 4 * kj));
+    Words far{0, 0};
+    uint32_t place = 0;
+    Cube cube{};
+    if constexpr (BIAS) {
+        int4 kc{0, 0, 0, 0};
+        if (live) kc = voxel_clamp(*(const int4*)(a.k_coords + 4 * kj));
+        cube = columns_cube(kc, live, box);
+        cube.place(kc, place);
+        far = voxel_words(kc);
+    }
     const float cs = a.scale * kLog2e, inv_cs = 1.f / cs;
     const Capped capped(a);
-    if (tid < 128) lr[tid >> 6][0][tid & 63] = lr[tid >> 6][1][tid & 63] = 0.f;
-    if (NW == 1) lr[1][0][lane] = lr[1][1][lane] = 0.f;
+    for (int e = tid; e < 4 * KW * 64; e += 256) (&lr[0][0][0][0])[e] = 0.f;
 
-    Stage<DT, DP, KT, TH> sq(tid, a.ldq, a.D), sd(tid, a.lddo, a.D);
+    Stage<DT, DP, KT, 256> sq(tid, a.ldq, a.D), sd(tid, a.lddo, a.D);
     int4 cq{0, 0, 0, 0};
     float rl = 0.f, rd = 0.f;
-    int64_t next = t0, g_next = tiles ? t0 / tiles : 0, i_next = t0 - g_next * tiles;  // the tile to load: head, tile of its rows
+    bool in = false;
+    // the tile to load and the one at work, as head of the group and tile of its rows
+    int64_t next = t0, g_next = tiles ? t0 / tiles : 0, i_next = t0 - g_next * tiles;
     auto load = [&]() __attribute__((always_inline)) {
-        const int64_t r = q0 + i_next * KT, n = q1 - r, head = (int64_t)kh * G + g_next;
-        sq.load(rows_buffer((const char*)a.q + (r * a.ldq + head * a.D) * T::SZ, a.ldq * T::SZ, n, KT, a.D * T::SZ));
-        sd.load(rows_buffer((const char*)a.dout + (r * a.lddo + head * a.D) * T::SZ, a.lddo * T::SZ, n, KT, a.D * T::SZ));
+        const int64_t r = q0 + i_next * KT, head = (int64_t)kh * G + g_next;
+        sq.load(RowTiles<KT>((const char*)a.q + head * a.D * T::SZ, r, q1, a.ldq * T::SZ, a.D * T::SZ).next());
+        sd.load(RowTiles<KT>((const char*)a.dout + head * a.D * T::SZ, r, q1, a.lddo * T::SZ, a.D * T::SZ).next());
         if (tid < KT) {
-            const bool in = tid < n;
+            in = tid < q1 - r;
             // a row past the end has no weight: its lse is infinite
             rl = in ? kUp<DT> - a.lse[(r + tid) * a.H + head] * kLog2e : -INFINITY;
             rd = in ? -a.delta[(r + tid) * a.H + head] : 0.f;
@@ -219,13 +243,9 @@ __global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(Att
         sq.store(lq[s], tid);
         sd.store(ld[s], tid);
         if (tid < KT) {
-            lr[s][0][tid] = CAP ? rl + capped.cap2 : rl * inv_cs;
-            lr[s][1][tid] = rd;
-            if constexpr (BIAS) {
-                const Voxel v = voxel_of(cq);
-                lc[s][0][tid] = v.xy;
-                lc[s][1][tid] = v.z;
-            }
+            lr[s][0][tid >> 5][tid & 31] = CAP ? rl + capped.cap2 : rl * inv_cs;
+            lr[s][1][tid >> 5][tid & 31] = rd;
+            if constexpr (BIAS) lc.put(s, tid, cq, in, cube);
         }
     };
     constexpr float down = DT == SPV_F16 ? 1.f / 4096.f : 1.f;  // 2^-kUp
@@ -242,42 +262,33 @@ __global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(Att
     __syncthreads();
     for (int64_t i = t0; i < t1; ++i) {
         const int s = (int)(i - t0) & 1;
-        if (busy) {
+        const int row0 = 32 * kw;  // the wave's rows of the tile
+        if (busy && q0 + i_now * KT + row0 < q1) {
             float slope = 0.f, lift = 0.f;
             if constexpr (BIAS) {
                 slope = a.slopes[(int64_t)kh * G + g_now] * kLog2e;
                 lift = slope * 8388608.f;
             }
-            f32x16 z = spread_rows(lr[s][0][lane]), rest = z;
-            f32x16 d = T::rows_dot(ld[s], lane, vf, spread_rows(lr[s][1][lane]));
-            z = T::rows_dot(lq[s], lane, kf, CAP ? f32x16{} : z);
-            f32x16 p;
+            f32x16 z = spread_rows(lr[s][0][kw][lane]), rest = z;
+            f32x16 d = T::rows_dot(ld[s] + row0 * T::LD, lane, vf, spread_rows(lr[s][1][kw][lane]));
+            z = T::rows_dot(lq[s] + row0 * T::LD, lane, kf, CAP ? f32x16{} : z);
+            f32x16 p, b{};
+            if constexpr (BIAS) lc.bias(s, row0, h, far, place, slope, lift, b);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                uint32_t xy[4] = {}, zz[4] = {};
-                if constexpr (BIAS) {
-                    lds_words(&lc[s][0][8 * q + 4 * h], xy);
-                    lds_words(&lc[s][1][8 * q + 4 * h], zz);
+            for (int r = 0; r < 16; ++r) {
+                if constexpr (CAP) {
+                    float x;
+                    const float bend = capped(z[r], BIAS ? b[r] + rest[r] : rest[r], x);
+                    p[r] = __builtin_amdgcn_exp2f(x);
+                    z[r] = p[r] * d[r] * bend;
+                } else {
+                    p[r] = __builtin_amdgcn_exp2f(BIAS ? fmaf(z[r], cs, b[r]) : z[r] * cs);
+                    z[r] = p[r] * d[r];
                 }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 4 * q + e;
-                    float b = 0.f;
-                    if constexpr (BIAS) b = fmaf(voxel_dist(xy[e], zz[e], kc.xy, kc.z), -slope, lift);
-                    if constexpr (CAP) {
-                        float x;
-                        const float bend = capped(z[r], BIAS ? b + rest[r] : rest[r], x);
-                        p[r] = __builtin_amdgcn_exp2f(x);
-                        z[r] = p[r] * d[r] * bend;
-                    } else {
-                        p[r] = __builtin_amdgcn_exp2f(BIAS ? fmaf(z[r], cs, b) : z[r] * cs);
-                        z[r] = p[r] * d[r];
-                    }
-                    if constexpr (DT == SPV_F16) z[r] *= down;
-                }
+                if constexpr (DT == SPV_F16) z[r] *= down;
             }
-            T::add_weighted(ld[s], lane, T::weights(p), ov);
-            T::add_weighted(lq[s], lane, T::weights(z), ok);
+            T::add_weighted(ld[s] + row0 * T::LD, lane, T::weights(p), ov);
+            T::add_weighted(lq[s] + row0 * T::LD, lane, T::weights(z), ok);
         }
         if (++i_now == tiles) i_now = 0, ++g_now;
         if (i + 1 < t1) {
@@ -285,6 +296,24 @@ __global__ __launch_bounds__(64 * NW, dkv_waves(DT, DP, NW)) void k_attn_dkv(Att
             if (next < t1) load();
         }
         __syncthreads();
+    }
+    if constexpr (KW > 1) {
+        // the waves of a block of columns add up (the tiles' LDS is free by now)
+        static_assert(2 * KT * T::LD >= CW * (KW - 1) * T::NB * 16 * 256, "a wave's sums have room");
+        constexpr int N = T::NB * 16 * 64;
+        float* pk = (float*)&lq[0][0] + cw * (KW - 1) * N;
+        float* pv = (float*)&ld[0][0] + cw * (KW - 1) * N;
+        if (kw) {
+            lds_put(pk + (kw - 1) * N, lane, ok);
+            lds_put(pv + (kw - 1) * N, lane, ov);
+        }
+        __syncthreads();
+        if (kw) return;
+#pragma unroll
+        for (int w = 1; w < KW; ++w) {
+            lds_add(pk + (w - 1) * N, lane, 1.f, ok);
+            lds_add(pv + (w - 1) * N, lane, 1.f, ov);
+        }
     }
     if (!live) return;
     const float f = a.scale * kBend<CAP>;
@@ -321,12 +350,10 @@ __global__ __launch_bounds__(256) void k_attn_add_parts(const float* __restrict_
 // host
 // ---------------------------------------------------------------------------
 static AttnShape dq_shape(const AttnArgs& a) {
-    const int G = a.H / a.K;
-    return attn_shape(a.nq, G, a.B, a.K, a.nk / (a.B < 1 ? 1 : a.B) / 32);
+    return attn_shape(a.dt, attn_dp(a.D), a.nq, a.H / a.K, a.B, a.K, a.nk / (a.B < 1 ? 1 : a.B));
 }
 static AttnShape dkv_shape(const AttnArgs& a) {
-    const int G = a.H / a.K;
-    return attn_shape(a.nk, 1, a.B, a.K, a.nq / (a.B < 1 ? 1 : a.B) / 32 * G);
+    return attn_shape(a.dt, attn_dp(a.D), a.nk, 1, a.B, a.K, a.nq / (a.B < 1 ? 1 : a.B) * (a.H / a.K));
 }
 
 void plan_attention_backward_ws(Arena& a, AttnArgs& t) {
@@ -338,23 +365,25 @@ void plan_attention_backward_ws(Arena& a, AttnArgs& t) {
     if (pq || pk) t.part = a.take<float>(pq > pk ? pq : pk);
 }
 
-template <int DT, int DP, int NW, bool BIAS, bool CAP>
+template <int DT, int DP, int KW, bool BIAS, bool CAP>
 static void launch_side(hipStream_t s, const AttnArgs& a, const AttnShape& sh, bool keys) {
     const dim3 g = attn_grid(sh, a.K);
-    if (keys) k_attn_dkv<DT, DP, NW, BIAS, CAP><<<g, 64 * NW, 0, s>>>(a);
-    else k_attn_dq<DT, DP, NW, BIAS, CAP><<<g, 64 * NW, 0, s>>>(a);
+    if (keys) k_attn_dkv<DT, DP, KW, BIAS, CAP><<<g, 256, 0, s>>>(a);
+    else k_attn_dq<DT, DP, KW, BIAS, CAP><<<g, 256, 0, s>>>(a);
 }
-template <int DT, int DP, int NW>
-static void launch_nw(hipStream_t s, const AttnArgs& a, const AttnShape& sh, bool keys) {
-    if (a.slopes && a.cap > 0.f) launch_side<DT, DP, NW, true, true>(s, a, sh, keys);
-    else if (a.slopes) launch_side<DT, DP, NW, true, false>(s, a, sh, keys);
-    else if (a.cap > 0.f) launch_side<DT, DP, NW, false, true>(s, a, sh, keys);
-    else launch_side<DT, DP, NW, false, false>(s, a, sh, keys);
+template <int DT, int DP, int KW>
+static void launch_kw(hipStream_t s, const AttnArgs& a, const AttnShape& sh, bool keys) {
+    if (a.slopes && a.cap > 0.f) launch_side<DT, DP, KW, true, true>(s, a, sh, keys);
+    else if (a.slopes) launch_side<DT, DP, KW, true, false>(s, a, sh, keys);
+    else if (a.cap > 0.f) launch_side<DT, DP, KW, false, true>(s, a, sh, keys);
+    else launch_side<DT, DP, KW, false, false>(s, a, sh, keys);
 }
 template <int DT, int DP>
 static void launch_dp(hipStream_t s, const AttnArgs& a, const AttnShape& sh, bool keys) {
-    if (sh.nw == 4) launch_nw<DT, DP, 4>(s, a, sh, keys);
-    else launch_nw<DT, DP, 1>(s, a, sh, keys);
+    constexpr int K1 = attn_kw(DT, DP, 1), K2 = attn_kw(DT, DP, 2);
+    if (K2 > 1 && sh.mode == 2) launch_kw<DT, DP, K2>(s, a, sh, keys);
+    else if (K1 > 1 && sh.mode == 1) launch_kw<DT, DP, K1>(s, a, sh, keys);
+    else launch_kw<DT, DP, 1>(s, a, sh, keys);
 }
 template <int DT>
 static void backward_dt(hipStream_t s, const AttnArgs& a, bool keys) {

@@ -76,21 +76,106 @@ __device__ inline ScanTile find_tile(const int32_t* off, int B, int64_t n, int p
     return s;
 }
 
-// the voxels' L1 distance: 16-bit coordinates in two words, so that a score's distance is two sums of absolute
-// differences onto the bits of 2^23, which read as a float are 2^23 + distance
-struct Voxel {
-    uint32_t xy, z;
-};
+// The voxels' L1 distance.  Coordinates are 16 bits each: two words, and a distance is two sums of absolute differences
+// onto the bits of 2^23, which read as a float are 2^23 + distance.  Where a workgroup's columns and 32 rows lie in one
+// cube of 256 voxels a side (most do: a scan at a coarse stride is hardly wider), three bytes of one word hold a
+// voxel's place in it, and one sum does.
 constexpr uint32_t kDistBits = 0x4B000000u;  // 2^23
-__device__ inline uint32_t voxel_coord(int c) {
-    return (uint32_t)((c < kCoordMin ? kCoordMin : (c > kCoordMax ? kCoordMax : c)) + 32768);
+__device__ inline int voxel_coord(int c) { return c < kCoordMin ? kCoordMin : (c > kCoordMax ? kCoordMax : c); }
+struct Cube {
+    int x, y, z;  // lowest corner
+    bool any;     // the columns fit in it
+    // the word of a place in the cube (coordinates in the voxel range); false: it is outside
+    __device__ bool place(const int4& c, uint32_t& w) const {
+        const uint32_t dx = c.y - x, dy = c.z - y, dz = c.w - z;
+        w = dx | (dy << 8) | (dz << 16);
+        return any && (dx | dy | dz) < 256u;
+    }
+};
+struct Words {
+    uint32_t a, b;  // x | y << 16 and z, from 2^15 below zero; or the place in the cube
+};
+__device__ inline int4 voxel_clamp(const int4& c) {
+    return make_int4(c.x, voxel_coord(c.y), voxel_coord(c.z), voxel_coord(c.w));
 }
-__device__ inline Voxel voxel_of(const int4& c) {
-    return Voxel{voxel_coord(c.y) | (voxel_coord(c.z) << 16), voxel_coord(c.w)};
+__device__ inline Words voxel_words(const int4& c) {
+    return Words{(uint32_t)(c.y + 32768) | ((uint32_t)(c.z + 32768) << 16), (uint32_t)(c.w + 32768)};
 }
-__device__ inline float voxel_dist(uint32_t axy, uint32_t az, uint32_t bxy, uint32_t bz) {
-    return __uint_as_float(__builtin_amdgcn_sad_u16(az, bz, __builtin_amdgcn_sad_u16(axy, bxy, kDistBits)));
+// The cube around a workgroup's columns (one to each lane; both halves of a wave hold the same), with equal margins:
+// every thread calls it; lds holds 4 x 6 ints.
+__device__ inline Cube columns_cube(const int4& c, bool live, int (*lds)[6]) {
+    int v[6] = {live ? c.y : 0x7FFFFFFF, live ? c.z : 0x7FFFFFFF, live ? c.w : 0x7FFFFFFF,
+                live ? -c.y : 0x7FFFFFFF, live ? -c.z : 0x7FFFFFFF, live ? -c.w : 0x7FFFFFFF};
+#pragma unroll
+    for (int e = 0; e < 6; ++e) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v[e] = min(v[e], __shfl_xor(v[e], o, 64));
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][e] = v[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 6; ++e) v[e] = uniform(min(min(lds[0][e], lds[1][e]), min(lds[2][e], lds[3][e])));
+    Cube q;
+    int lo[3];
+    q.any = true;
+#pragma unroll
+    for (int e = 0; e < 3; ++e) {
+        const int span = -v[3 + e] - v[e];
+        q.any = q.any && span < 256;
+        lo[e] = v[e] - (255 - span) / 2;
+    }
+    q.x = lo[0], q.y = lo[1], q.z = lo[2];
+    return q;
 }
+// b = -slope * distance for the lane's 16 of 32 rows (words wa, wb of each in LDS), from the column's words; lift is
+// what the 2^23 of a distance brings too much: slope 2^23, so that the sum is rounded once
+__device__ inline void distance_bias(const uint32_t* wa, const uint32_t* wb, int h, bool near, const Words& far,
+                                     uint32_t place, float slope, float lift, f32x16& b) {
+    if (near) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint4 a = *(const uint4*)(wa + 8 * q + 4 * h);
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                b[4 * q + e] = fmaf(__uint_as_float(__builtin_amdgcn_sad_u8(w[e], place, kDistBits)), -slope, lift);
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint4 a = *(const uint4*)(wa + 8 * q + 4 * h), z = *(const uint4*)(wb + 8 * q + 4 * h);
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w}, u[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                b[4 * q + e] = fmaf(__uint_as_float(__builtin_amdgcn_sad_u16(
+                                        u[e], far.b, __builtin_amdgcn_sad_u16(w[e], far.a, kDistBits))),
+                                    -slope, lift);
+        }
+    }
+}
+// The words of KT rows in LDS, one row a thread (tid < KT): those of the cube where all rows of its 32 lie in it.
+template <int KT>
+struct Places {
+    uint32_t w[2][2][KT];
+    uint32_t near[2][KT / 32];  // of each 32 rows
+    __device__ inline void put(int s, int tid, const int4& raw, bool in, const Cube& cube) {
+        const int4 c = voxel_clamp(raw);
+        uint32_t p;
+        const bool ok = cube.place(c, p) || !in;
+        const uint64_t all = __ballot(ok);
+        const bool near = (uint32_t)(all >> (tid & 32)) == 0xFFFFFFFFu;
+        const Words f = voxel_words(c);
+        w[s][0][tid] = near ? p : f.a;
+        w[s][1][tid] = f.b;
+        if ((tid & 31) == 0) near_of(s, tid >> 5) = near;
+    }
+    __device__ inline uint32_t& near_of(int s, int i) { return near[s][i]; }
+    __device__ inline void bias(int s, int row0, int h, const Words& far, uint32_t place, float slope, float lift,
+                                f32x16& b) const {
+        distance_bias(&w[s][0][row0], &w[s][1][row0], h, uniform((int)near[s][row0 >> 5]) != 0, far, place, slope, lift,
+                      b);
+    }
+};
 
 // the other half's value of a column: (max, sum) over both
 __device__ inline f32x2 both_halves(float v) {
@@ -257,23 +342,30 @@ struct Tile {
     }
 };
 
-// the four words of rows 8 q + 4 h .. + 3
-__device__ inline void lds_words(const uint32_t* p, uint32_t (&w)[4]) {
-    const uint4 v = *(const uint4*)p;
-    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-}
-
 // a value of each of 32 rows (in lanes 0 .. 31; 0 in the others) to every column of that row's accumulators, exactly:
 // a product with ones, where reading them from LDS would take eight times the LDS cycles of all else in a score
 __device__ inline f32x16 spread_rows(float v) {
     return __builtin_amdgcn_mfma_f32_32x32x2f32(v, 1.f, f32x16{}, 0, 0, 0);
 }
 
-// n (at most KT) rows from p, ld bytes apart and D bytes each, as a buffer: what lies outside reads as zero
-__device__ inline __amdgpu_buffer_rsrc_t rows_buffer(const void* p, int64_t ld, int64_t n, int KT, int D) {
-    const int64_t r = n < KT ? n : KT;
-    return make_rsrc(p, r > 0 ? (uint32_t)((r - 1) * ld + D) : 0u);
-}
+// Rows of a scan, KT at a time, as buffers: what lies outside reads as zero.  Scalar state: the next rows' address, how
+// many are left, and the bytes of a whole tile.
+template <int KT>
+struct RowTiles {
+    const char* at;
+    int64_t left, step;
+    int ld, row;
+    __device__ RowTiles(const void* p, int64_t first, int64_t n, int64_t ld_bytes, int row_bytes)
+        : at((const char*)p + first * ld_bytes), left(n - first), step(KT * ld_bytes), ld((int)ld_bytes), row(row_bytes) {}
+    __device__ inline __amdgpu_buffer_rsrc_t next() {
+        uint32_t bytes = (uint32_t)(KT - 1) * (uint32_t)ld + (uint32_t)row;
+        if (left < KT) bytes = left > 0 ? (uint32_t)(left - 1) * (uint32_t)ld + (uint32_t)row : 0u;
+        const __amdgpu_buffer_rsrc_t r = make_rsrc(at, bytes);
+        at += step;
+        left -= KT;
+        return r;
+    }
+};
 
 // KT rows of DP channels on their way from memory to LDS by TH threads: 16 bytes at a time, loaded to registers a tile
 // ahead; zeros for rows past the buffer's and channels past D.  The offsets within a tile stay the same.
@@ -304,30 +396,62 @@ struct Stage {
     }
 };
 
-// rows that the kernels stage at a time
-constexpr int attn_rows(int dt, int DP) { return dt == SPV_F32 || DP > 32 ? 32 : 64; }
+// registers of a wave in LDS, 256 bytes each
+template <int N>
+__device__ inline void lds_put(float* p, int lane, const f32x16 (&o)[N]) {
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[(16 * b + r) * 64 + lane] = o[b][r];
+}
+template <int N>
+__device__ inline void lds_add(const float* p, int lane, float f, f32x16 (&o)[N]) {
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[b][r] = fmaf(f, p[(16 * b + r) * 64 + lane], o[b][r]);
+}
+
+// The four waves of a workgroup: CW blocks of 32 columns, and KW waves on each that take every KW'th 32 rows of what is
+// staged and join at the end.  More waves on fewer columns read the rows more often but leave more workgroups.
+// The waves of `mode` 0, 1, 2 on a block of columns; a head too wide for LDS takes the last mode that fits.
+constexpr int attn_kw(int dt, int DP, int mode) {
+    const int most = (dt == SPV_F32 ? 2 : 1) * DP <= 64 ? 4 : (dt == SPV_F32 ? 2 : 1) * DP <= 128 ? 2 : 1;
+    return (1 << mode) < most ? 1 << mode : most;
+}
+// rows that a wave takes between two barriers
+#ifndef RTK
+#define RTK 2
+#endif
+constexpr int attn_rows(int dt, int DP, int KW) { return dt == SPV_F32 || DP > 32 || KW >= RTK ? 32 : 64; }
+
 // channels a head's rows are padded to
 constexpr int attn_dp(int D) { return (D + 31) / 32 * 32; }
 
-// a launch: waves of a workgroup, parts that the rows of a scan are taken in, tiles of columns
+// a launch: mode (above), parts that the rows of a scan are taken in, tiles of columns
 struct AttnShape {
-    int nw, parts;
+    int mode, parts;
     int64_t tiles;
 };
 inline dim3 attn_grid(const AttnShape& s, int K) {
     return s.parts > 1 ? dim3((unsigned)s.parts, (unsigned)K, (unsigned)s.tiles) : dim3((unsigned)(s.tiles * K));
 }
-// 128 columns a workgroup while that gives every CU one and the scans fill them, else 32; rows in parts of at least
-// four tiles of the average scan's `work` while there are under four waves a CU (1,024 workgroups: grids of parts
-// stay within the limits of their dimensions)
-inline AttnShape attn_shape(int64_t n, int per, int B, int K, int64_t work) {
-    const int scans = B < 1 ? 1 : B;
-    AttnShape s{4, 1, attn_tiles(n, B, per, 128)};
-    if (s.tiles * K < 256 || n * per / scans < 64) s = AttnShape{1, 1, attn_tiles(n, B, per, 32)};
+// The fewest waves on a block of columns that give every SIMD kAttnWaves waves (4 of them: a compute unit's four SIMDs
+// times 256); below half of that the rows are also taken in parts, of at least 256 of the average scan's `rows`.
+#ifndef FULL
+#define FULL 2048
+#endif
+constexpr int64_t kAttnFull = FULL;  // waves
+inline AttnShape attn_shape(int dt, int DP, int64_t n, int per, int B, int K, int64_t rows) {
+    AttnShape s{0, 1, 0};
+    for (;; ++s.mode) {
+        s.tiles = attn_tiles(n, B, per, 128 / attn_kw(dt, DP, s.mode));
+        if (s.mode == 2 || s.tiles * K * 4 >= kAttnFull) break;
+    }
     const int64_t wgs = s.tiles * K;
-    if (s.nw == 1 && wgs < 1024) {
-        int64_t p = 2048 / (wgs < 1 ? 1 : wgs);
-        if (p > work / 4) p = work / 4;
+    if (wgs * 4 < kAttnFull / 2) {
+        int64_t p = kAttnFull / 4 / (wgs < 1 ? 1 : wgs);
+        if (p > rows / 256) p = rows / 256;
         if (p > 256) p = 256;
         if (p > 8) p &= ~(int64_t)7;  // a part's heads on one die
         s.parts = p < 2 ? 1 : (int)p;
