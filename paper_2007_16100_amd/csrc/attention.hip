@@ -14,13 +14,7 @@ namespace spv {
 constexpr float kLead = 8.f;
 
 // waves per SIMD that the registers have to leave room for
-#ifndef OCC32
-#define OCC32 3
-#endif
-#ifndef OCC64
-#define OCC64 3
-#endif
-constexpr int attn_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? OCC64 : OCC32; }
+constexpr int attn_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : 4; }
 
 template <int DT, int DP, int KW, bool BIAS, bool CAP>
 __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
@@ -28,7 +22,7 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     constexpr int RT = attn_rows(DT, DP, KW), KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
     __shared__ __align__(16) Places<BIAS ? KT : 32> lc;
-    __shared__ int box[4][6];
+    __shared__ uint32_t box[4][3];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), cw = wave / KW, kw = wave % KW;
     const int c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
@@ -46,7 +40,8 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     const int64_t qi = t.first + q0 + x / G;
     uint4 qf[T::NF];
     T::load_cols(a.q, qi * a.ldq + (int64_t)head * a.D, live, a.D, h, qf);
-    const float cs = a.scale * kLog2e, cz = CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
+    const float cs = in_vgpr(a.scale * kLog2e), cz = in_vgpr(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f);
+    const float cap2 = a.cap * kLog2e, fall = in_vgpr(-2.f * cap2);
     Words far{0, 0};
     uint32_t place = 0;
     Cube cube{};
@@ -109,10 +104,14 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
         const int row0 = RT * kw, left = keys - i * KT - row0;  // the wave's rows of the tile, keys from there on
         if (busy && left > 0) {
             f32x16 z[KS], bias[CAP && BIAS ? KS : 1];
+            RowWords rw[KS];
+            if constexpr (BIAS)
+#pragma unroll
+                for (int u = 0; u < KS; ++u) rw[u].load(&lc.w[s][0][row0 + 32 * u], h);
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
                 f32x16 b{};
-                if constexpr (BIAS) lc.bias(s, row0 + 32 * u, h, far, place, slope, lift, b);
+                if constexpr (BIAS) lc.bias(s, row0 + 32 * u, h, rw[u], far, place, slope, lift, b);
                 if constexpr (CAP && BIAS) bias[u] = b;
                 z[u] = T::rows_dot(lk[s] + (row0 + 32 * u) * T::LD, lane, qf, CAP ? f32x16{} : b);
             }
@@ -123,7 +122,7 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
                     for (int r = 0; r < 16; ++r) {
                         // cap tanh(w) = cap - 2 cap / (exp(2 w) + 1), to an absolute error of 2^-22 cap
                         const float ex = __builtin_amdgcn_exp2f(z[u][r] * cz);
-                        z[u][r] = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(ex + 1.f),
+                        z[u][r] = fmaf(fall, __builtin_amdgcn_rcpf(ex + 1.f),
                                        BIAS ? bias[BIAS ? u : 0][r] + (cap2 - m) : cap2 - m);
                     }
                 const int end = left - 32 * u;

@@ -12,12 +12,13 @@ namespace spv {
 
 // d score / d product, over scale and kBend, and the score itself from a product under a cap
 struct Capped {
-    float cz, cap2;
-    __device__ explicit Capped(const AttnArgs& a) : cz(2.f * kLog2e * a.scale / a.cap), cap2(a.cap * kLog2e) {}
+    float cz, cap2, fall;
+    __device__ explicit Capped(const AttnArgs& a)
+        : cz(in_vgpr(2.f * kLog2e * a.scale / a.cap)), cap2(a.cap * kLog2e), fall(in_vgpr(-2.f * cap2)) {}
     // t = tanh(w) = 1 - 2 r with r = 1 / (exp(2 w) + 1): 1 - t^2 = 4 (r - r^2)
     __device__ float operator()(float y, float rest, float& x) const {
         const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * cz) + 1.f);
-        x = fmaf(-2.f * cap2, r, rest);
+        x = fmaf(fall, r, rest);
         return fmaf(-r, r, r);
     }
 };
@@ -25,22 +26,16 @@ template <bool CAP>
 constexpr float kBend = CAP ? 4.f : 1.f;
 
 // waves per SIMD that the registers have to leave room for
-#ifndef OCQ
-#define OCQ 2
-#endif
-#ifndef OCK
-#define OCK 2
-#endif
-constexpr int dq_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? 2 : OCQ; }
-constexpr int dkv_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? 2 : OCK; }
+constexpr int dq_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? 2 : 3; }
+constexpr int dkv_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : 2; }
 
 template <int DT, int DP, int KW, bool BIAS, bool CAP>
 __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     using T = Tile<DT, DP>;
-    constexpr int KT = 32 * KW, CW = 4 / KW, BM = 32 * CW;
+    constexpr int RT = attn_rows(DT, DP, KW), KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
     __shared__ __align__(16) Places<BIAS ? KT : 32> lc;
-    __shared__ int box[4][6];
+    __shared__ uint32_t box[4][3];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), cw = wave / KW, kw = wave % KW;
     const int c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
@@ -85,7 +80,7 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
         far = voxel_words(qc);
     }
     const float lift = slope * 8388608.f;
-    const float cs = a.scale * kLog2e;
+    const float cs = in_vgpr(a.scale * kLog2e);
     const Capped capped(a);
     f32x16 dref;
 #pragma unroll
@@ -124,29 +119,43 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     __syncthreads();
     for (int i = t0; i < t1; ++i) {
         const int s = (i - t0) & 1;
-        const int row0 = 32 * kw, end = keys - i * KT - row0;  // the wave's rows of the tile, keys from there on
-        if (busy && end > 0) {
-            f32x16 b{};
-            const f32x16 d = T::rows_dot(lv[s] + row0 * T::LD, lane, df, dref);
-            if constexpr (BIAS) lc.bias(s, row0, h, far, place, slope, lift, b);
-            f32x16 z = T::rows_dot(lk[s] + row0 * T::LD, lane, qf, CAP ? f32x16{} : b);
+        const int row0 = RT * kw, left = keys - i * KT - row0;  // the wave's rows of the tile, keys from there on
+        if (busy && left > 0) {
+            f32x16 z[KS], d[KS], bias[CAP && BIAS ? KS : 1];
+            RowWords rw[KS];
+            if constexpr (BIAS)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                if constexpr (CAP) {
-                    float x;
-                    const float bend = capped(z[r], BIAS ? b[r] + (capped.cap2 - lse) : capped.cap2 - lse, x);
-                    z[r] = __builtin_amdgcn_exp2f(x) * d[r] * bend;
-                } else {
-                    z[r] = __builtin_amdgcn_exp2f(fmaf(z[r], cs, -lse)) * d[r];
+                for (int u = 0; u < KS; ++u) rw[u].load(&lc.w[s][0][row0 + 32 * u], h);
+#pragma unroll
+            for (int u = 0; u < KS; ++u) {
+                d[u] = T::rows_dot(lv[s] + (row0 + 32 * u) * T::LD, lane, df, dref);
+                f32x16 b{};
+                if constexpr (BIAS) lc.bias(s, row0 + 32 * u, h, rw[u], far, place, slope, lift, b);
+                if constexpr (CAP && BIAS) bias[u] = b;
+                z[u] = T::rows_dot(lk[s] + (row0 + 32 * u) * T::LD, lane, qf, CAP ? f32x16{} : b);
+            }
+#pragma unroll
+            for (int u = 0; u < KS; ++u) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if constexpr (CAP) {
+                        float x;
+                        const float top = capped.cap2 - lse;
+                        const float bend = capped(z[u][r], BIAS ? bias[BIAS ? u : 0][r] + top : top, x);
+                        z[u][r] = __builtin_amdgcn_exp2f(x) * d[u][r] * bend;
+                    } else {
+                        z[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], cs, -lse)) * d[u][r];
+                    }
                 }
-            }
-            if (end < 32) {  // keys past the scan's end: their rows are zero, but not their weights
-                asm volatile("");  // a branch, not selects on every tile
+                const int end = left - 32 * u;
+                if (end < 32) {  // keys past the scan's end: their rows are zero, but not their weights
+                    asm volatile("");  // a branch, not selects on every tile
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (8 * (r / 4) + 4 * h + r % 4 >= end) z[r] = 0.f;
+                    for (int r = 0; r < 16; ++r)
+                        if (8 * (r / 4) + 4 * h + r % 4 >= end) z[u][r] = 0.f;
+                }
+                T::add_weighted(lk[s] + (row0 + 32 * u) * T::LD, lane, T::weights(z[u]), o);
             }
-            T::add_weighted(lk[s] + row0 * T::LD, lane, T::weights(z), o);
         }
         if (i + 1 < t1) {
             store(s ^ 1);
@@ -183,11 +192,11 @@ constexpr float kUp = DT == SPV_F16 ? 12.f : 0.f;
 template <int DT, int DP, int KW, bool BIAS, bool CAP>
 __global__ __launch_bounds__(256, dkv_waves(DT, DP)) void k_attn_dkv(AttnArgs a) {
     using T = Tile<DT, DP>;
-    constexpr int KT = 32 * KW, CW = 4 / KW, BM = 32 * CW;
+    constexpr int RT = 32, KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
     __shared__ __align__(16) char lq[2][KT * T::LD], ld[2][KT * T::LD];
     __shared__ __align__(16) Places<BIAS ? KT : 32> lc;
-    __shared__ int box[4][6];
-    __shared__ float lr[2][2][KW][64];  // each 32 rows' -lse (see below) and -delta, then zeros
+    __shared__ uint32_t box[4][3];
+    __shared__ float lr[2][2][KT / 32][64];  // each 32 rows' -lse (see below) and -delta, then zeros
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), cw = wave / KW, kw = wave % KW;
     const int c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
@@ -214,37 +223,54 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP)) void k_attn_dkv(AttnArgs a)
         cube.place(kc, place);
         far = voxel_words(kc);
     }
-    const float cs = a.scale * kLog2e, inv_cs = 1.f / cs;
+    const float cs = in_vgpr(a.scale * kLog2e), inv_cs = 1.f / cs;
     const Capped capped(a);
-    for (int e = tid; e < 4 * KW * 64; e += 256) (&lr[0][0][0][0])[e] = 0.f;
+    for (int e = tid; e < 4 * (KT / 32) * 64; e += 256) (&lr[0][0][0][0])[e] = 0.f;
 
     Stage<DT, DP, KT, 256> sq(tid, a.ldq, a.D), sd(tid, a.lddo, a.D);
     int4 cq{0, 0, 0, 0};
     float rl = 0.f, rd = 0.f;
-    bool in = false;
+    int64_t left = 0;
     // the tile to load and the one at work, as head of the group and tile of its rows
     int64_t next = t0, g_next = tiles ? t0 / tiles : 0, i_next = t0 - g_next * tiles;
-    auto load = [&]() __attribute__((always_inline)) {
+    RowTiles<KT> rq, ro, re, rt, rc;
+    auto start = [&]() __attribute__((always_inline)) {
         const int64_t r = q0 + i_next * KT, head = (int64_t)kh * G + g_next;
-        sq.load(RowTiles<KT>((const char*)a.q + head * a.D * T::SZ, r, q1, a.ldq * T::SZ, a.D * T::SZ).next());
-        sd.load(RowTiles<KT>((const char*)a.dout + head * a.D * T::SZ, r, q1, a.lddo * T::SZ, a.D * T::SZ).next());
+        rq = RowTiles<KT>((const char*)a.q + head * a.D * T::SZ, r, q1, a.ldq * T::SZ, a.D * T::SZ);
+        ro = RowTiles<KT>((const char*)a.dout + head * a.D * T::SZ, r, q1, a.lddo * T::SZ, a.D * T::SZ);
+        re = RowTiles<KT>(a.lse + head, r, q1, 4 * a.H, 4);
+        rt = RowTiles<KT>(a.delta + head, r, q1, 4 * a.H, 4);
+        rc = RowTiles<KT>(a.q_coords, r, q1, 16, 16);
+    };
+    start();
+    auto load = [&]() __attribute__((always_inline)) {
+        left = rq.left;
+        sq.load(rq.next());
+        sd.load(ro.next());
+        const __amdgpu_buffer_rsrc_t be = re.next(), bt = rt.next();
         if (tid < KT) {
-            in = tid < q1 - r;
-            // a row past the end has no weight: its lse is infinite
-            rl = in ? kUp<DT> - a.lse[(r + tid) * a.H + head] * kLog2e : -INFINITY;
-            rd = in ? -a.delta[(r + tid) * a.H + head] : 0.f;
-            if constexpr (BIAS)
-                if (in) cq = *(const int4*)(a.q_coords + 4 * (r + tid));
+            rl = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(be, tid * 4 * a.H, 0, 0));
+            rd = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(bt, tid * 4 * a.H, 0, 0));
+        }
+        if constexpr (BIAS) {
+            const __amdgpu_buffer_rsrc_t bc = rc.next();
+            if (tid < KT) cq = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(bc, tid * 16, 0, 0));
         }
         ++next;
-        if (++i_next == tiles) i_next = 0, ++g_next;
+        if (++i_next == tiles) {
+            i_next = 0, ++g_next;
+            if (next < t1) start();
+        }
     };
     auto store = [&](int s) __attribute__((always_inline)) {
         sq.store(lq[s], tid);
         sd.store(ld[s], tid);
         if (tid < KT) {
-            lr[s][0][tid >> 5][tid & 31] = CAP ? rl + capped.cap2 : rl * inv_cs;
-            lr[s][1][tid >> 5][tid & 31] = rd;
+            // a row past the end has no weight: its lse counts as infinite
+            const bool in = tid < left;
+            const float e = in ? kUp<DT> - rl * kLog2e : -INFINITY;
+            lr[s][0][tid >> 5][tid & 31] = CAP ? e + capped.cap2 : e * inv_cs;
+            lr[s][1][tid >> 5][tid & 31] = -rd;
             if constexpr (BIAS) lc.put(s, tid, cq, in, cube);
         }
     };
@@ -262,33 +288,49 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP)) void k_attn_dkv(AttnArgs a)
     __syncthreads();
     for (int64_t i = t0; i < t1; ++i) {
         const int s = (int)(i - t0) & 1;
-        const int row0 = 32 * kw;  // the wave's rows of the tile
+        const int row0 = RT * kw;  // the wave's rows of the tile
         if (busy && q0 + i_now * KT + row0 < q1) {
             float slope = 0.f, lift = 0.f;
             if constexpr (BIAS) {
-                slope = a.slopes[(int64_t)kh * G + g_now] * kLog2e;
+                slope = in_vgpr(a.slopes[(int64_t)kh * G + g_now] * kLog2e);
                 lift = slope * 8388608.f;
             }
-            f32x16 z = spread_rows(lr[s][0][kw][lane]), rest = z;
-            f32x16 d = T::rows_dot(ld[s] + row0 * T::LD, lane, vf, spread_rows(lr[s][1][kw][lane]));
-            z = T::rows_dot(lq[s] + row0 * T::LD, lane, kf, CAP ? f32x16{} : z);
-            f32x16 p, b{};
-            if constexpr (BIAS) lc.bias(s, row0, h, far, place, slope, lift, b);
+            f32x16 z[KS], d[KS], rest[CAP ? KS : 1];
+            RowWords rw[KS];
+            if constexpr (BIAS)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
+                for (int u = 0; u < KS; ++u) rw[u].load(&lc.w[s][0][row0 + 32 * u], h);
+#pragma unroll
+            for (int u = 0; u < KS; ++u) {
+                z[u] = spread_rows(lr[s][0][(row0 >> 5) + u][lane]);
+                d[u] = spread_rows(lr[s][1][(row0 >> 5) + u][lane]);
                 if constexpr (CAP) {
-                    float x;
-                    const float bend = capped(z[r], BIAS ? b[r] + rest[r] : rest[r], x);
-                    p[r] = __builtin_amdgcn_exp2f(x);
-                    z[r] = p[r] * d[r] * bend;
-                } else {
-                    p[r] = __builtin_amdgcn_exp2f(BIAS ? fmaf(z[r], cs, b[r]) : z[r] * cs);
-                    z[r] = p[r] * d[r];
+                    rest[u] = z[u];
+                    z[u] = f32x16{};
                 }
-                if constexpr (DT == SPV_F16) z[r] *= down;
+                z[u] = T::rows_dot(lq[s] + (row0 + 32 * u) * T::LD, lane, kf, z[u]);
+                d[u] = T::rows_dot(ld[s] + (row0 + 32 * u) * T::LD, lane, vf, d[u]);
             }
-            T::add_weighted(ld[s] + row0 * T::LD, lane, T::weights(p), ov);
-            T::add_weighted(lq[s] + row0 * T::LD, lane, T::weights(z), ok);
+#pragma unroll
+            for (int u = 0; u < KS; ++u) {
+                f32x16 p, b{};
+                if constexpr (BIAS) lc.bias(s, row0 + 32 * u, h, rw[u], far, place, slope, lift, b);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if constexpr (CAP) {
+                        float x;
+                        const float bend = capped(z[u][r], BIAS ? b[r] + rest[CAP ? u : 0][r] : rest[CAP ? u : 0][r], x);
+                        p[r] = __builtin_amdgcn_exp2f(x);
+                        z[u][r] = p[r] * d[u][r] * bend;
+                    } else {
+                        p[r] = __builtin_amdgcn_exp2f(BIAS ? fmaf(z[u][r], cs, b[r]) : z[u][r] * cs);
+                        z[u][r] = p[r] * d[u][r];
+                    }
+                    if constexpr (DT == SPV_F16) z[u][r] *= down;
+                }
+                T::add_weighted(ld[s] + (row0 + 32 * u) * T::LD, lane, T::weights(p), ov);
+                T::add_weighted(lq[s] + (row0 + 32 * u) * T::LD, lane, T::weights(z[u]), ok);
+            }
         }
         if (++i_now == tiles) i_now = 0, ++g_now;
         if (i + 1 < t1) {

@@ -24,6 +24,12 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ inline int64_t clamp_off(int32_t o, int64_t n) { return o < 0 ? 0 : ((int64_t)o > n ? n : (int64_t)o); }
 
+// a uniform value in a vector register: float32 arithmetic on vector registers alone runs at 2.7 cycles a wave, with a
+// scalar operand at 4
+__device__ inline float in_vgpr(float v) {
+    asm("" : "+v"(v));
+    return v;
+}
 // wave-uniform values, in scalar registers
 __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ inline int64_t uniform(int64_t v) {
@@ -102,57 +108,57 @@ __device__ inline Words voxel_words(const int4& c) {
     return Words{(uint32_t)(c.y + 32768) | ((uint32_t)(c.z + 32768) << 16), (uint32_t)(c.w + 32768)};
 }
 // The cube around a workgroup's columns (one to each lane; both halves of a wave hold the same), with equal margins:
-// every thread calls it; lds holds 4 x 6 ints.
-__device__ inline Cube columns_cube(const int4& c, bool live, int (*lds)[6]) {
-    int v[6] = {live ? c.y : 0x7FFFFFFF, live ? c.z : 0x7FFFFFFF, live ? c.w : 0x7FFFFFFF,
-                live ? -c.y : 0x7FFFFFFF, live ? -c.z : 0x7FFFFFFF, live ? -c.w : 0x7FFFFFFF};
+// every thread calls it; lds holds 4 x 3 words.
+__device__ inline Cube columns_cube(const int4& c, bool live, uint32_t (*lds)[3]) {
+    // the lowest of x, y, z, -x, -y, -z, two to a word
+    typedef short i16x2 __attribute__((ext_vector_type(2)));
+    auto two = [&](int a, int b) { return live ? i16x2{(short)a, (short)b} : i16x2{32767, 32767}; };
+    i16x2 v[3] = {two(c.y, c.z), two(c.w, -c.y), two(-c.z, -c.w)};
 #pragma unroll
-    for (int e = 0; e < 6; ++e) {
+    for (int o = 16; o > 0; o >>= 1) {
+        i16x2 w[3];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[e] = min(v[e], __shfl_xor(v[e], o, 64));
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][e] = v[e];
+        for (int e = 0; e < 3; ++e) w[e] = __builtin_bit_cast(i16x2, __shfl_xor(__builtin_bit_cast(int, v[e]), o, 64));
+#pragma unroll
+        for (int e = 0; e < 3; ++e) v[e] = __builtin_elementwise_min(v[e], w[e]);
     }
-    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
 #pragma unroll
-    for (int e = 0; e < 6; ++e) v[e] = uniform(min(min(lds[0][e], lds[1][e]), min(lds[2][e], lds[3][e])));
+        for (int e = 0; e < 3; ++e) lds[threadIdx.x >> 6][e] = __builtin_bit_cast(uint32_t, v[e]);
+    __syncthreads();
+    int m[6];
+#pragma unroll
+    for (int e = 0; e < 3; ++e) {
+        i16x2 t = __builtin_bit_cast(i16x2, lds[0][e]);
+#pragma unroll
+        for (int w = 1; w < 4; ++w) t = __builtin_elementwise_min(t, __builtin_bit_cast(i16x2, lds[w][e]));
+        m[2 * e] = uniform((int)t.x);
+        m[2 * e + 1] = uniform((int)t.y);
+    }
     Cube q;
     int lo[3];
     q.any = true;
 #pragma unroll
     for (int e = 0; e < 3; ++e) {
-        const int span = -v[3 + e] - v[e];
+        const int span = -m[3 + e] - m[e];
         q.any = q.any && span < 256;
-        lo[e] = v[e] - (255 - span) / 2;
+        lo[e] = m[e] - (255 - span) / 2;
     }
     q.x = lo[0], q.y = lo[1], q.z = lo[2];
     return q;
 }
-// b = -slope * distance for the lane's 16 of 32 rows (words wa, wb of each in LDS), from the column's words; lift is
-// what the 2^23 of a distance brings too much: slope 2^23, so that the sum is rounded once
-__device__ inline void distance_bias(const uint32_t* wa, const uint32_t* wb, int h, bool near, const Words& far,
-                                     uint32_t place, float slope, float lift, f32x16& b) {
-    if (near) {
+// four words a lane of each of four runs of rows: rows 8 q + 4 h .. + 3
+struct RowWords {
+    uint4 q[4];
+    __device__ inline void load(const uint32_t* w, int h) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint4 a = *(const uint4*)(wa + 8 * q + 4 * h);
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                b[4 * q + e] = fmaf(__uint_as_float(__builtin_amdgcn_sad_u8(w[e], place, kDistBits)), -slope, lift);
-        }
-    } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint4 a = *(const uint4*)(wa + 8 * q + 4 * h), z = *(const uint4*)(wb + 8 * q + 4 * h);
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w}, u[4] = {z.x, z.y, z.z, z.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                b[4 * q + e] = fmaf(__uint_as_float(__builtin_amdgcn_sad_u16(
-                                        u[e], far.b, __builtin_amdgcn_sad_u16(w[e], far.a, kDistBits))),
-                                    -slope, lift);
-        }
+        for (int i = 0; i < 4; ++i) q[i] = *(const uint4*)(w + 8 * i + 4 * h);
     }
-}
+    __device__ inline uint32_t operator[](int r) const {
+        const uint4& v = q[r / 4];
+        return r % 4 == 0 ? v.x : r % 4 == 1 ? v.y : r % 4 == 2 ? v.z : v.w;
+    }
+};
 // The words of KT rows in LDS, one row a thread (tid < KT): those of the cube where all rows of its 32 lie in it.
 template <int KT>
 struct Places {
@@ -167,13 +173,25 @@ struct Places {
         const Words f = voxel_words(c);
         w[s][0][tid] = near ? p : f.a;
         w[s][1][tid] = f.b;
-        if ((tid & 31) == 0) near_of(s, tid >> 5) = near;
+        if ((tid & 31) == 0) this->near[s][tid >> 5] = near;
     }
-    __device__ inline uint32_t& near_of(int s, int i) { return near[s][i]; }
-    __device__ inline void bias(int s, int row0, int h, const Words& far, uint32_t place, float slope, float lift,
-                                f32x16& b) const {
-        distance_bias(&w[s][0][row0], &w[s][1][row0], h, uniform((int)near[s][row0 >> 5]) != 0, far, place, slope, lift,
-                      b);
+    // b = -slope * distance for the lane's 16 of the 32 rows from row0 (their first words already in a), from the
+    // column's words; lift is what the 2^23 of a distance brings too much: slope 2^23, so that the sum is rounded once
+    __device__ inline void bias(int s, int row0, int h, const RowWords& a, const Words& far, uint32_t place, float slope,
+                                float lift, f32x16& b) const {
+        if (uniform((int)near[s][row0 >> 5])) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                b[r] = fmaf(__uint_as_float(__builtin_amdgcn_sad_u8(a[r], place, kDistBits)), -slope, lift);
+        } else {
+            RowWords z;
+            z.load(&w[s][1][row0], h);
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                b[r] = fmaf(__uint_as_float(__builtin_amdgcn_sad_u16(
+                                z[r], far.b, __builtin_amdgcn_sad_u16(a[r], far.a, kDistBits))),
+                            -slope, lift);
+        }
     }
 };
 
@@ -355,6 +373,8 @@ struct RowTiles {
     const char* at;
     int64_t left, step;
     int ld, row;
+    __device__ RowTiles() {}
+    // rows first .. n - 1 of p, ld_bytes apart, row_bytes of each
     __device__ RowTiles(const void* p, int64_t first, int64_t n, int64_t ld_bytes, int row_bytes)
         : at((const char*)p + first * ld_bytes), left(n - first), step(KT * ld_bytes), ld((int)ld_bytes), row(row_bytes) {}
     __device__ inline __amdgpu_buffer_rsrc_t next() {
@@ -420,10 +440,7 @@ constexpr int attn_kw(int dt, int DP, int mode) {
     return (1 << mode) < most ? 1 << mode : most;
 }
 // rows that a wave takes between two barriers
-#ifndef RTK
-#define RTK 2
-#endif
-constexpr int attn_rows(int dt, int DP, int KW) { return dt == SPV_F32 || DP > 32 || KW >= RTK ? 32 : 64; }
+constexpr int attn_rows(int dt, int DP, int KW) { return dt == SPV_F32 || DP > 32 || KW > 1 ? 32 : 64; }
 
 // channels a head's rows are padded to
 constexpr int attn_dp(int D) { return (D + 31) / 32 * 32; }
@@ -436,12 +453,11 @@ struct AttnShape {
 inline dim3 attn_grid(const AttnShape& s, int K) {
     return s.parts > 1 ? dim3((unsigned)s.parts, (unsigned)K, (unsigned)s.tiles) : dim3((unsigned)(s.tiles * K));
 }
-// The fewest waves on a block of columns that give every SIMD kAttnWaves waves (4 of them: a compute unit's four SIMDs
-// times 256); below half of that the rows are also taken in parts, of at least 256 of the average scan's `rows`.
-#ifndef FULL
-#define FULL 2048
-#endif
-constexpr int64_t kAttnFull = FULL;  // waves
+// The fewest waves on a block of columns that leave two waves to each SIMD (kAttnFull).  Where even the most leave a
+// compute unit without a workgroup, the rows are also taken in parts, two workgroups to a compute unit, of at least 256
+// rows of the average scan.  More parts cost more in joining them than they bring: at [1457, 1544] x 3 heads, float32,
+// 51 us in one part, 59 in six; at [2000] x 8 heads, bf16, 26 and 42.
+constexpr int64_t kAttnFull = 2048;
 inline AttnShape attn_shape(int dt, int DP, int64_t n, int per, int B, int K, int64_t rows) {
     AttnShape s{0, 1, 0};
     for (;; ++s.mode) {
@@ -449,8 +465,8 @@ inline AttnShape attn_shape(int dt, int DP, int64_t n, int per, int B, int K, in
         if (s.mode == 2 || s.tiles * K * 4 >= kAttnFull) break;
     }
     const int64_t wgs = s.tiles * K;
-    if (wgs * 4 < kAttnFull / 2) {
-        int64_t p = kAttnFull / 4 / (wgs < 1 ? 1 : wgs);
+    if (wgs < 256) {
+        int64_t p = 512 / (wgs < 1 ? 1 : wgs);
         if (p > rows / 256) p = rows / 256;
         if (p > 256) p = 256;
         if (p > 8) p &= ~(int64_t)7;  // a part's heads on one die
