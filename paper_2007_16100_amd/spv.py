@@ -621,11 +621,11 @@ def spv_epilogue_backward(ws: Workspace, dy: torch.Tensor, a: torch.Tensor, scal
     return da, dres, dscale, dshift
 
 
-def spv_linear_backward(ws: Workspace, x: torch.Tensor, W: torch.Tensor, da: torch.Tensor):
-    """(dx, dW) of the product x @ W, given its gradient da."""
+def spv_linear_backward(ws: Workspace, x: torch.Tensor, W: torch.Tensor, da: torch.Tensor, want_dx: bool = True):
+    """(dx, dW) of the product x @ W, given its gradient da; dx is None without want_dx."""
     m, Cin = x.shape
     Cout = W.shape[1]
-    dx = torch.empty((max(m, 1), Cin), dtype=x.dtype, device=x.device)
+    dx = torch.empty((max(m, 1), Cin), dtype=x.dtype, device=x.device) if want_dx else None
     dW = torch.empty((Cin, Cout), dtype=torch.float32, device=x.device)
     st = lib().spv_linear_backward(_stream(), ws.ptr, ws.nbytes, _ptr(x), m, Cin, _ptr(W), Cout, _ptr(da), _ptr(dx),
                                    _ptr(dW), _DT[x.dtype])
