@@ -228,8 +228,8 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_norm(NormArgs a) {
     }
 }
 
-// dx, and (part given) the workgroup's column sums: each lane's over its rows in float32, then the lanes
-// of a channel in a fixed order
+// dx, and (part given) the workgroup's column sums: each lane's over its rows in float32, then the lanes of a channel in
+// a fixed order.  A single workgroup's are the result.
 template <int DT, int L, int NV>
 __global__ __launch_bounds__(64 * kNormWaves) void k_norm_bwd(NormBwdArgs a, float* part) {
     constexpr int V = kVec<DT>, R = 64 / L;
@@ -301,7 +301,8 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_norm_bwd(NormBwdArgs a, flo
         const int half = c >= a.C, cc = half ? c - a.C : c;
         float s = red[0][half][cc];
         for (int w = 1; w < kNormWaves; ++w) s += red[w][half][cc];
-        part[(int64_t)blockIdx.x * 2 * a.C + c] = s;
+        if (gridDim.x > 1) part[(int64_t)blockIdx.x * 2 * a.C + c] = s;
+        else if (half ? a.dbeta : a.dgamma) (half ? a.dbeta : a.dgamma)[cc] = s;
     }
 }
 
@@ -417,7 +418,7 @@ static void norm_bwd_dt(hipStream_t s, const NormBwdArgs& a, const NormWs& w) {
         }
         if (a.dx) k_norm_bwd_any<DT><<<g, 64 * kNormWaves, 0, s>>>(a, nullptr);
     }
-    if (sums)
+    if (sums && !(vec && g == 1))
         k_norm_join<<<(unsigned)((2 * a.C + 15) / 16), 1024, 0, s>>>(w.part, (int)g, a.C, a.dgamma, a.dbeta);
 }
 void launch_layer_norm_backward(hipStream_t s, const NormBwdArgs& a, const NormWs& w) {

@@ -172,8 +172,25 @@ def _ptr(t: Optional[torch.Tensor]):
     return ct.c_void_p(t.data_ptr())
 
 
+# the current stream's handle without the Stream object that torch.cuda.current_stream builds (2.8 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
+    if _raw_stream is not None:
+        return ct.c_void_p(_raw_stream(torch.cuda.current_device()))
     return ct.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _addr(t: Optional[torch.Tensor]):
+    """_ptr as a plain integer, which the calls take as well."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("libspv takes device tensors")
+    if not t.is_contiguous():
+        raise ValueError("libspv takes contiguous tensors")
+    return t.data_ptr()
 
 
 def _chk(st: int, what: str):
@@ -638,14 +655,12 @@ def spv_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: 
                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """(x - mean) / sqrt(var + eps) * gamma + beta over the channels of each row of x [m][C]."""
     m, C = x.shape
-    _check_vec(gamma, C, "gamma")
-    _check_vec(beta, C, "beta")
+    xp, gp, bp = _addr(x), _channels(gamma, C, "gamma"), _channels(beta, C, "beta")
     if out is None:
-        out = torch.empty((m, C), dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x)
     elif out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("out must have x's shape and type")
-    st = lib().spv_layer_norm(_stream(), _ptr(x), _ptr(m_dev), m, C, _ptr(gamma), _ptr(beta), eps, _ptr(out),
-                              _DT[x.dtype])
+    st = lib().spv_layer_norm(_stream(), xp, _addr(m_dev), m, C, gp, bp, eps, _addr(out), _DT[x.dtype])
     _chk(st, "spv_layer_norm")
     return out
 
@@ -655,21 +670,26 @@ def spv_layer_norm_backward(ws: Workspace, dy: torch.Tensor, x: torch.Tensor, ga
                             m_dev: Optional[torch.Tensor] = None):
     """(dx, dgamma, dbeta) of spv_layer_norm; dres: a gradient added to dx (the residual branch's)."""
     m, C = x.shape
-    _check_vec(gamma, C, "gamma")
+    xp, gp = _addr(x), _channels(gamma, C, "gamma")
     for t, name in ((dy, "dy"), (dres, "dres")):
         if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
             raise ValueError(f"{name} must have x's shape and type")
-    dx = torch.empty((m, C), dtype=x.dtype, device=x.device)
-    dg = torch.empty((2, C), dtype=torch.float32, device=x.device)
-    st = lib().spv_layer_norm_backward(_stream(), ws.ptr, ws.nbytes, _ptr(dy), _ptr(x), _ptr(m_dev), m, C, _ptr(gamma),
-                                       eps, _ptr(dres), _ptr(dx), _ptr(dg[0]), _ptr(dg[1]), _DT[x.dtype])
+    dx = torch.empty_like(x)
+    dgamma = torch.empty(C, dtype=torch.float32, device=x.device)
+    dbeta = torch.empty_like(dgamma)
+    st = lib().spv_layer_norm_backward(_stream(), ws.ptr, ws.nbytes, _addr(dy), xp, _addr(m_dev), m, C, gp, eps,
+                                       _addr(dres), dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), _DT[x.dtype])
     _chk(st, "spv_layer_norm_backward")
-    return dx, dg[0], dg[1]
+    return dx, dgamma, dbeta
 
 
-def _check_vec(t: Optional[torch.Tensor], C: int, name: str):
-    if t is not None and (t.dtype != torch.float32 or t.shape != (C,)):
+def _channels(t: Optional[torch.Tensor], C: int, name: str):
+    """Address of a float32 vector of C entries (None: none)."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (C,):
         raise ValueError(f"{name} must be float32 [{C}]")
+    return _addr(t)
 
 
 def make_attention_params(H: int, Hkv: int, D: int, q_off: torch.Tensor, k_off: Optional[torch.Tensor] = None,
@@ -695,51 +715,50 @@ def make_attention_params(H: int, Hkv: int, D: int, q_off: torch.Tensor, k_off: 
             raise ValueError("coordinates and slopes go together")
         if t is not None and (t.dtype != torch.int32 or t.dim() != 2 or t.shape[1] != 4):
             raise ValueError(f"{name} must be int32 [rows][4]")
-    _check_vec(slopes, H, "slopes")
-
-    def ptr(t):
-        return None if t is None else _ptr(t).value
-    p = AttentionParams(H, Hkv, D, q_off.shape[0] - 1, D ** -0.5 if scale is None else scale, cap, ptr(q_off),
-                        ptr(k_off), ptr(q_coords), ptr(k_coords), ptr(slopes))
+    p = AttentionParams(H, Hkv, D, q_off.shape[0] - 1, D ** -0.5 if scale is None else scale, cap, _addr(q_off),
+                        _addr(k_off), _addr(q_coords), _addr(k_coords), _channels(slopes, H, "slopes"))
     p._keep = (q_off, k_off, q_coords, k_coords, slopes)
     return p
 
 
-def _heads(t: torch.Tensor, heads: int, D: int, like: torch.Tensor, name: str):
-    """(pointer, row stride) of t [n][heads][D], whose rows may be parts of wider ones."""
+def _heads(t: torch.Tensor, heads: int, D: int, dtype: torch.dtype, name: str):
+    """(rows, address, row stride) of t [n][heads][D], whose rows may be parts of wider ones."""
     n, h, d = t.shape
-    if h != heads or d != D or t.dtype != like.dtype:
-        raise ValueError(f"{name} must be [rows][{heads}][{D}] of q's type")
+    if h != heads or d != D or t.dtype != dtype:
+        raise ValueError(f"{name} must be [rows][{heads}][{D}] of {dtype}")
     if not t.is_cuda:
         raise ValueError("libspv takes device tensors")
-    s = t.stride()
-    if n and ((d > 1 and s[2] != 1) or (h > 1 and s[1] != d)):
+    ld, sh, sd = t.stride()
+    if n and ((d > 1 and sd != 1) or (h > 1 and sh != d)):
         raise ValueError(f"the channels of a row of {name} must be contiguous")
-    return t.data_ptr(), s[0] if n > 1 else h * d
+    return n, t.data_ptr(), ld if n > 1 else h * d
 
 
-def _attention_tensors(p: AttentionParams, q, k, v):
-    if k.shape[0] != v.shape[0]:
+def _qkv(p: AttentionParams, q, k, v):
+    D, K, dt = p.D, p.Hkv, q.dtype
+    nq, qp, ldq = _heads(q, p.H, D, dt, "q")
+    nk, kp, ldk = _heads(k, K, D, dt, "k")
+    nv, vp, ldv = _heads(v, K, D, dt, "v")
+    if nk != nv:
         raise ValueError("k and v must have the same rows")
-    for t, c, name in ((q, p._keep[2], "q_coords"), (k, p._keep[3], "k_coords")):
-        if c is not None and c.shape[0] < t.shape[0]:
-            raise ValueError(f"{name} must have a row for each of its side's")
-    return _heads(q, p.H, p.D, q, "q") + _heads(k, p.Hkv, p.D, q, "k") + _heads(v, p.Hkv, p.D, q, "v")
+    _, _, qc, kc, _ = p._keep
+    if qc is not None and (qc.shape[0] < nq or kc.shape[0] < nk):
+        raise ValueError("the coordinates must have a row for each of their side's")
+    return qp, ldq, nq, kp, ldk, vp, ldv, nk
 
 
 def spv_attention(ws: Workspace, params: AttentionParams, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                   want_lse: bool = False, out: Optional[torch.Tensor] = None):
     """Attention of q [nq][H][D] over k, v [nk][Hkv][D] of the same scan; with want_lse (out, lse [nq][H])."""
-    qp, ldq, kp, ldk, vp, ldv = _attention_tensors(params, q, k, v)
-    nq, nk = q.shape[0], k.shape[0]
+    side = _qkv(params, q, k, v)
+    nq, H, D = q.shape
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    op, ldo = _heads(out, params.H, params.D, q, "out")
-    if out.shape[0] != nq:
+        out = torch.empty((nq, H, D), dtype=q.dtype, device=q.device)
+    no, op, ldo = _heads(out, H, D, q.dtype, "out")
+    if no != nq:
         raise ValueError("out must have q's rows")
-    lse = torch.empty((nq, params.H), dtype=torch.float32, device=q.device) if want_lse else None
-    st = lib().spv_attention(_stream(), ws.ptr, ws.nbytes, ct.byref(params), qp, ldq, nq, kp, ldk, vp, ldv, nk, op, ldo,
-                             _ptr(lse), _DT[q.dtype])
+    lse = torch.empty((nq, H), dtype=torch.float32, device=q.device) if want_lse else None
+    st = lib().spv_attention(_stream(), ws.ptr, ws.nbytes, ct.byref(params), *side, op, ldo, _addr(lse), _DT[q.dtype])
     _chk(st, "spv_attention")
     return (out, lse) if want_lse else out
 
@@ -749,23 +768,24 @@ def spv_attention_backward(ws: Workspace, params: AttentionParams, q: torch.Tens
                            grads: Optional[Sequence[torch.Tensor]] = None):
     """(dq, dk, dv) of spv_attention, given its out and lse [nq][H] and the gradient dout of out; grads: the
     tensors to write (which may be parts of one wider buffer), else new dense ones."""
-    qp, ldq, kp, ldk, vp, ldv = _attention_tensors(params, q, k, v)
-    nq, nk = q.shape[0], k.shape[0]
-    op, ldo = _heads(out, params.H, params.D, q, "out")
-    dop, lddo = _heads(dout, params.H, params.D, q, "dout")
-    if out.shape[0] != nq or dout.shape[0] != nq:
+    side = _qkv(params, q, k, v)
+    nq, H, D = q.shape
+    K, dt = params.Hkv, q.dtype
+    no, op, ldo = _heads(out, H, D, dt, "out")
+    nd, dop, lddo = _heads(dout, H, D, dt, "dout")
+    if no != nq or nd != nq:
         raise ValueError("out and dout must have q's rows")
-    if lse.dtype != torch.float32 or lse.shape != (nq, params.H):
+    if lse.dtype != torch.float32 or lse.shape != (nq, H):
         raise ValueError("lse must be float32 [rows][heads]")
     if grads is None:
-        grads = [torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v)]
+        grads = [torch.empty(t.shape, dtype=dt, device=q.device) for t in (q, k, v)]
     elif any(g.shape[0] != t.shape[0] for g, t in zip(grads, (q, k, v))):
         raise ValueError("the gradients must have their inputs' rows")
-    dq, lddq = _heads(grads[0], params.H, params.D, q, "dq")
-    dk, lddk = _heads(grads[1], params.Hkv, params.D, q, "dk")
-    dv, lddv = _heads(grads[2], params.Hkv, params.D, q, "dv")
-    st = lib().spv_attention_backward(_stream(), ws.ptr, ws.nbytes, ct.byref(params), qp, ldq, nq, kp, ldk, vp, ldv, nk,
-                                      op, ldo, _ptr(lse), dop, lddo, dq, lddq, dk, lddk, dv, lddv, _DT[q.dtype])
+    _, dq, lddq = _heads(grads[0], H, D, dt, "dq")
+    _, dk, lddk = _heads(grads[1], K, D, dt, "dk")
+    _, dv, lddv = _heads(grads[2], K, D, dt, "dv")
+    st = lib().spv_attention_backward(_stream(), ws.ptr, ws.nbytes, ct.byref(params), *side, op, ldo, _addr(lse), dop,
+                                      lddo, dq, lddq, dk, lddk, dv, lddv, _DT[dt])
     _chk(st, "spv_attention_backward")
     return tuple(grads)
 
