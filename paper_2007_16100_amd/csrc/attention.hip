@@ -14,7 +14,13 @@ namespace spv {
 constexpr float kLead = 8.f;
 
 // waves per SIMD that the registers have to leave room for
-constexpr int attn_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : 4; }
+#ifndef O64
+#define O64 4
+#endif
+constexpr int attn_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? O64 : 4; }
+#ifndef O64
+#define O64 4
+#endif
 
 template <int DT, int DP, int KW, bool BIAS, bool CAP>
 __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
@@ -103,28 +109,27 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
         const int s = (i - t0) & 1;
         const int row0 = RT * kw, left = keys - i * KT - row0;  // the wave's rows of the tile, keys from there on
         if (busy && left > 0) {
-            f32x16 z[KS], bias[CAP && BIAS ? KS : 1];
-            RowWords rw[KS];
-            if constexpr (BIAS)
-#pragma unroll
-                for (int u = 0; u < KS; ++u) rw[u].load(&lc.w[s][0][row0 + 32 * u], h);
+            f32x16 z[KS];
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
                 f32x16 b{};
-                if constexpr (BIAS) lc.bias(s, row0 + 32 * u, h, rw[u], far, place, slope, lift, b);
-                if constexpr (CAP && BIAS) bias[u] = b;
-                z[u] = T::rows_dot(lk[s] + (row0 + 32 * u) * T::LD, lane, qf, CAP ? f32x16{} : b);
+                if constexpr (BIAS && !CAP)
+                    lc.bias(s, row0 + 32 * u, h, far, place, slope, lift,
+                            [&](int r, float x) __attribute__((always_inline)) { b[r] = x; });
+                z[u] = T::rows_dot(lk[s] + (row0 + 32 * u) * T::LD, lane, qf, b);
             }
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
-                if constexpr (CAP)
+                // cap tanh(w) = cap - 2 cap / (exp(2 w) + 1), to an absolute error of 2^-22 cap
+                auto bend = [&](int r, float b) __attribute__((always_inline)) {
+                    const float ex = __builtin_amdgcn_exp2f(z[u][r] * cz);
+                    z[u][r] = fmaf(fall, __builtin_amdgcn_rcpf(ex + 1.f), b + (cap2 - m));
+                };
+                if constexpr (CAP && BIAS)
+                    lc.bias(s, row0 + 32 * u, h, far, place, slope, lift, bend);
+                else if constexpr (CAP)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        // cap tanh(w) = cap - 2 cap / (exp(2 w) + 1), to an absolute error of 2^-22 cap
-                        const float ex = __builtin_amdgcn_exp2f(z[u][r] * cz);
-                        z[u][r] = fmaf(fall, __builtin_amdgcn_rcpf(ex + 1.f),
-                                       BIAS ? bias[BIAS ? u : 0][r] + (cap2 - m) : cap2 - m);
-                    }
+                    for (int r = 0; r < 16; ++r) bend(r, 0.f);
                 const int end = left - 32 * u;
                 if (end < 32) {  // keys past the scan's end
                     asm volatile("");  // a branch: selects on every tile cost two instructions a score

@@ -121,32 +121,32 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
         const int s = (i - t0) & 1;
         const int row0 = RT * kw, left = keys - i * KT - row0;  // the wave's rows of the tile, keys from there on
         if (busy && left > 0) {
-            f32x16 z[KS], d[KS], bias[CAP && BIAS ? KS : 1];
-            RowWords rw[KS];
-            if constexpr (BIAS)
-#pragma unroll
-                for (int u = 0; u < KS; ++u) rw[u].load(&lc.w[s][0][row0 + 32 * u], h);
+            f32x16 z[KS], d[KS];
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
                 d[u] = T::rows_dot(lv[s] + (row0 + 32 * u) * T::LD, lane, df, dref);
                 f32x16 b{};
-                if constexpr (BIAS) lc.bias(s, row0 + 32 * u, h, rw[u], far, place, slope, lift, b);
-                if constexpr (CAP && BIAS) bias[u] = b;
-                z[u] = T::rows_dot(lk[s] + (row0 + 32 * u) * T::LD, lane, qf, CAP ? f32x16{} : b);
+                if constexpr (BIAS && !CAP)
+                    lc.bias(s, row0 + 32 * u, h, far, place, slope, lift,
+                            [&](int r, float x) __attribute__((always_inline)) { b[r] = x; });
+                z[u] = T::rows_dot(lk[s] + (row0 + 32 * u) * T::LD, lane, qf, b);
             }
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
+                auto grad = [&](int r, float b) __attribute__((always_inline)) {
                     if constexpr (CAP) {
                         float x;
-                        const float top = capped.cap2 - lse;
-                        const float bend = capped(z[u][r], BIAS ? bias[BIAS ? u : 0][r] + top : top, x);
+                        const float bend = capped(z[u][r], b + (capped.cap2 - lse), x);
                         z[u][r] = __builtin_amdgcn_exp2f(x) * d[u][r] * bend;
                     } else {
                         z[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], cs, -lse)) * d[u][r];
                     }
-                }
+                };
+                if constexpr (CAP && BIAS)
+                    lc.bias(s, row0 + 32 * u, h, far, place, slope, lift, grad);
+                else
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) grad(r, 0.f);
                 const int end = left - 32 * u;
                 if (end < 32) {  // keys past the scan's end: their rows are zero, but not their weights
                     asm volatile("");  // a branch, not selects on every tile
@@ -296,10 +296,6 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP)) void k_attn_dkv(AttnArgs a)
                 lift = slope * 8388608.f;
             }
             f32x16 z[KS], d[KS], rest[CAP ? KS : 1];
-            RowWords rw[KS];
-            if constexpr (BIAS)
-#pragma unroll
-                for (int u = 0; u < KS; ++u) rw[u].load(&lc.w[s][0][row0 + 32 * u], h);
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
                 z[u] = spread_rows(lr[s][0][(row0 >> 5) + u][lane]);
@@ -313,21 +309,24 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP)) void k_attn_dkv(AttnArgs a)
             }
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
-                f32x16 p, b{};
-                if constexpr (BIAS) lc.bias(s, row0 + 32 * u, h, rw[u], far, place, slope, lift, b);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
+                f32x16 p;
+                auto grad = [&](int r, float b) __attribute__((always_inline)) {
                     if constexpr (CAP) {
                         float x;
-                        const float bend = capped(z[u][r], BIAS ? b[r] + rest[CAP ? u : 0][r] : rest[CAP ? u : 0][r], x);
+                        const float bend = capped(z[u][r], b + rest[CAP ? u : 0][r], x);
                         p[r] = __builtin_amdgcn_exp2f(x);
                         z[u][r] = p[r] * d[u][r] * bend;
                     } else {
-                        p[r] = __builtin_amdgcn_exp2f(BIAS ? fmaf(z[u][r], cs, b[r]) : z[u][r] * cs);
+                        p[r] = __builtin_amdgcn_exp2f(BIAS ? fmaf(z[u][r], cs, b) : z[u][r] * cs);
                         z[u][r] = p[r] * d[u][r];
                     }
                     if constexpr (DT == SPV_F16) z[u][r] *= down;
-                }
+                };
+                if constexpr (BIAS)
+                    lc.bias(s, row0 + 32 * u, h, far, place, slope, lift, grad);
+                else
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) grad(r, 0.f);
                 T::add_weighted(ld[s] + (row0 + 32 * u) * T::LD, lane, T::weights(p), ov);
                 T::add_weighted(lq[s] + (row0 + 32 * u) * T::LD, lane, T::weights(z[u]), ok);
             }

@@ -147,18 +147,6 @@ __device__ inline Cube columns_cube(const int4& c, bool live, uint32_t (*lds)[3]
     q.x = lo[0], q.y = lo[1], q.z = lo[2];
     return q;
 }
-// four words a lane of each of four runs of rows: rows 8 q + 4 h .. + 3
-struct RowWords {
-    uint4 q[4];
-    __device__ inline void load(const uint32_t* w, int h) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = *(const uint4*)(w + 8 * i + 4 * h);
-    }
-    __device__ inline uint32_t operator[](int r) const {
-        const uint4& v = q[r / 4];
-        return r % 4 == 0 ? v.x : r % 4 == 1 ? v.y : r % 4 == 2 ? v.z : v.w;
-    }
-};
 // The words of KT rows in LDS, one row a thread (tid < KT): those of the cube where all rows of its 32 lie in it.
 template <int KT>
 struct Places {
@@ -175,22 +163,32 @@ struct Places {
         w[s][1][tid] = f.b;
         if ((tid & 31) == 0) this->near[s][tid >> 5] = near;
     }
-    // b = -slope * distance for the lane's 16 of the 32 rows from row0 (their first words already in a), from the
-    // column's words; lift is what the 2^23 of a distance brings too much: slope 2^23, so that the sum is rounded once
-    __device__ inline void bias(int s, int row0, int h, const RowWords& a, const Words& far, uint32_t place, float slope,
-                                float lift, f32x16& b) const {
+    // f(r, -slope * distance) for the lane's 16 of the 32 rows from row0, from the column's words; lift is what the 2^23
+    // of a distance brings too much: slope 2^23, so that the sum is rounded once
+    template <class F>
+    __device__ inline void bias(int s, int row0, int h, const Words& far, uint32_t place, float slope, float lift,
+                                F&& f) const {
+        const uint32_t *wa = &w[s][0][row0 + 4 * h], *wb = &w[s][1][row0 + 4 * h];
         if (uniform((int)near[s][row0 >> 5])) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                b[r] = fmaf(__uint_as_float(__builtin_amdgcn_sad_u8(a[r], place, kDistBits)), -slope, lift);
-        } else {
-            RowWords z;
-            z.load(&w[s][1][row0], h);
+            for (int q = 0; q < 4; ++q) {
+                const uint4 v = *(const uint4*)(wa + 8 * q);
+                const uint32_t a[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                b[r] = fmaf(__uint_as_float(__builtin_amdgcn_sad_u16(
-                                z[r], far.b, __builtin_amdgcn_sad_u16(a[r], far.a, kDistBits))),
-                            -slope, lift);
+                for (int e = 0; e < 4; ++e)
+                    f(4 * q + e, fmaf(__uint_as_float(__builtin_amdgcn_sad_u8(a[e], place, kDistBits)), -slope, lift));
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint4 v = *(const uint4*)(wa + 8 * q), y = *(const uint4*)(wb + 8 * q);
+                const uint32_t a[4] = {v.x, v.y, v.z, v.w}, z[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    f(4 * q + e, fmaf(__uint_as_float(__builtin_amdgcn_sad_u16(
+                                          z[e], far.b, __builtin_amdgcn_sad_u16(a[e], far.a, kDistBits))),
+                                      -slope, lift));
+            }
         }
     }
 };
@@ -457,7 +455,10 @@ inline dim3 attn_grid(const AttnShape& s, int K) {
 // compute unit without a workgroup, the rows are also taken in parts, two workgroups to a compute unit, of at least 256
 // rows of the average scan.  More parts cost more in joining them than they bring: at [1457, 1544] x 3 heads, float32,
 // 51 us in one part, 59 in six; at [2000] x 8 heads, bf16, 26 and 42.
-constexpr int64_t kAttnFull = 2048;
+#ifndef FULL
+#define FULL 2048
+#endif
+constexpr int64_t kAttnFull = FULL;
 inline AttnShape attn_shape(int dt, int DP, int64_t n, int per, int B, int K, int64_t rows) {
     AttnShape s{0, 1, 0};
     for (;; ++s.mode) {
