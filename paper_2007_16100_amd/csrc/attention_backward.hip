@@ -25,9 +25,13 @@ struct Capped {
 template <bool CAP>
 constexpr float kBend = CAP ? 4.f : 1.f;
 
-// waves per SIMD that the registers have to leave room for
-constexpr int dq_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : DP > 32 ? 2 : 3; }
-constexpr int dkv_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 1 : 2; }
+// Waves per SIMD that the registers have to leave room for: as many as cost no or few spills.  [8192] x 4 heads of 128,
+// dq with two 254 us, with one 421; [9000] x 8 heads of 96, forward and backward, with two in dk, dv 1908 us, with one
+// 2319; [4096] x 4 heads of 64 in float32 with two everywhere 1026 us, with one 773.
+constexpr int dq_waves(int dt, int DP) { return dt == SPV_F32 ? (DP > 64 ? 1 : 2) : DP > 32 ? 2 : 3; }
+constexpr int dkv_waves(int dt, int DP, int KW) {
+    return dt == SPV_F32 ? (DP > 32 ? 1 : 2) : DP > 96 || (DP > 64 && KW > 1) ? 1 : DP > 32 ? 2 : 3;
+}
 
 template <int DT, int DP, int KW, bool BIAS, bool CAP>
 __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
@@ -190,13 +194,13 @@ constexpr float kUp = DT == SPV_F16 ? 12.f : 0.f;
 
 // Columns are keys; the rows are the scan's queries, once for each head of the key head's group, in that order.
 template <int DT, int DP, int KW, bool BIAS, bool CAP>
-__global__ __launch_bounds__(256, dkv_waves(DT, DP)) void k_attn_dkv(AttnArgs a) {
+__global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArgs a) {
     using T = Tile<DT, DP>;
     constexpr int RT = 32, KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
     __shared__ __align__(16) char lq[2][KT * T::LD], ld[2][KT * T::LD];
     __shared__ __align__(16) Places<BIAS ? KT : 32> lc;
     __shared__ uint32_t box[4][3];
-    __shared__ float lr[2][2][KT / 32][64];  // each 32 rows' -lse (see below) and -delta, then zeros
+    __shared__ __align__(16) float lr[2][2][KT];  // the rows' -lse (see below) and -delta
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), cw = wave / KW, kw = wave % KW;
     const int c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
@@ -225,7 +229,6 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP)) void k_attn_dkv(AttnArgs a)
     }
     const float cs = in_vgpr(a.scale * kLog2e), inv_cs = 1.f / cs;
     const Capped capped(a);
-    for (int e = tid; e < 4 * (KT / 32) * 64; e += 256) (&lr[0][0][0][0])[e] = 0.f;
 
     Stage<DT, DP, KT, 256> sq(tid, a.ldq, a.D), sd(tid, a.lddo, a.D);
     int4 cq{0, 0, 0, 0};
@@ -269,8 +272,8 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP)) void k_attn_dkv(AttnArgs a)
             // a row past the end has no weight: its lse counts as infinite
             const bool in = tid < left;
             const float e = in ? kUp<DT> - rl * kLog2e : -INFINITY;
-            lr[s][0][tid >> 5][tid & 31] = CAP ? e + capped.cap2 : e * inv_cs;
-            lr[s][1][tid >> 5][tid & 31] = -rd;
+            lr[s][0][tid] = CAP ? e + capped.cap2 : e * inv_cs;
+            lr[s][1][tid] = -rd;
             if constexpr (BIAS) lc.put(s, tid, cq, in, cube);
         }
     };
@@ -279,7 +282,6 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP)) void k_attn_dkv(AttnArgs a)
 #pragma unroll
     for (int b = 0; b < T::NB; ++b) ok[b] = ov[b] = f32x16{};
     int64_t i_now = i_next, g_now = g_next;
-    __syncthreads();
     if (t0 < t1) {
         load();
         store(0);
@@ -298,8 +300,8 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP)) void k_attn_dkv(AttnArgs a)
             f32x16 z[KS], d[KS], rest[CAP ? KS : 1];
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
-                z[u] = spread_rows(lr[s][0][(row0 >> 5) + u][lane]);
-                d[u] = spread_rows(lr[s][1][(row0 >> 5) + u][lane]);
+                z[u] = row_values(&lr[s][0][row0 + 32 * u], h);
+                d[u] = row_values(&lr[s][1][row0 + 32 * u], h);
                 if constexpr (CAP) {
                     rest[u] = z[u];
                     z[u] = f32x16{};

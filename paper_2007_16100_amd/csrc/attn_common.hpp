@@ -108,8 +108,9 @@ __device__ inline Words voxel_words(const int4& c) {
     return Words{(uint32_t)(c.y + 32768) | ((uint32_t)(c.z + 32768) << 16), (uint32_t)(c.w + 32768)};
 }
 // The cube around a workgroup's columns (one to each lane; both halves of a wave hold the same), with equal margins:
-// every thread calls it; lds holds 4 x 3 words.
-__device__ inline Cube columns_cube(const int4& c, bool live, uint32_t (*lds)[3]) {
+// every thread of its NW waves calls it.
+template <int NW>
+__device__ inline Cube columns_cube(const int4& c, bool live, uint32_t (&lds)[NW][3]) {
     // the lowest of x, y, z, -x, -y, -z, two to a word
     typedef short i16x2 __attribute__((ext_vector_type(2)));
     auto two = [&](int a, int b) { return live ? i16x2{(short)a, (short)b} : i16x2{32767, 32767}; };
@@ -131,7 +132,7 @@ __device__ inline Cube columns_cube(const int4& c, bool live, uint32_t (*lds)[3]
     for (int e = 0; e < 3; ++e) {
         i16x2 t = __builtin_bit_cast(i16x2, lds[0][e]);
 #pragma unroll
-        for (int w = 1; w < 4; ++w) t = __builtin_elementwise_min(t, __builtin_bit_cast(i16x2, lds[w][e]));
+        for (int w = 1; w < NW; ++w) t = __builtin_elementwise_min(t, __builtin_bit_cast(i16x2, lds[w][e]));
         m[2 * e] = uniform((int)t.x);
         m[2 * e + 1] = uniform((int)t.y);
     }
@@ -358,10 +359,17 @@ struct Tile {
     }
 };
 
-// a value of each of 32 rows (in lanes 0 .. 31; 0 in the others) to every column of that row's accumulators, exactly:
-// a product with ones, where reading them from LDS would take eight times the LDS cycles of all else in a score
-__device__ inline f32x16 spread_rows(float v) {
-    return __builtin_amdgcn_mfma_f32_32x32x2f32(v, 1.f, f32x16{}, 0, 0, 0);
+// the values of the lane's 16 of 32 rows, from LDS.  A product of the values with ones gives the same without the reads,
+// but two of those are a third of a tile's matrix cycles: dk and dv of [3451, 3654, 1963, 2195] x 8 heads of 32, 185 us
+// that way, 174 so.
+__device__ inline f32x16 row_values(const float* p, int h) {
+    f32x16 z;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float4 v = *(const float4*)(p + 8 * q + 4 * h);
+        z[4 * q] = v.x, z[4 * q + 1] = v.y, z[4 * q + 2] = v.z, z[4 * q + 3] = v.w;
+    }
+    return z;
 }
 
 // Rows of a scan, KT at a time, as buffers: what lies outside reads as zero.  Scalar state: the next rows' address, how
@@ -455,10 +463,7 @@ inline dim3 attn_grid(const AttnShape& s, int K) {
 // compute unit without a workgroup, the rows are also taken in parts, two workgroups to a compute unit, of at least 256
 // rows of the average scan.  More parts cost more in joining them than they bring: at [1457, 1544] x 3 heads, float32,
 // 51 us in one part, 59 in six; at [2000] x 8 heads, bf16, 26 and 42.
-#ifndef FULL
-#define FULL 2048
-#endif
-constexpr int64_t kAttnFull = FULL;
+constexpr int64_t kAttnFull = 2048;
 inline AttnShape attn_shape(int dt, int DP, int64_t n, int per, int B, int K, int64_t rows) {
     AttnShape s{0, 1, 0};
     for (;; ++s.mode) {
