@@ -632,7 +632,7 @@ typedef struct spv_attention_params {
  * types multiply on matrix cores with the weights p rounded to the type.
  * In:  q [nq][ldq], k [nk][ldk], v [nk][ldv] (dt): row i, head h at
  *      q + i * ldq + h * D; row strides in elements, multiples of 8 (16-bit) or 4
- *      (f32), at least the row's channels, below 2^24; 16-byte aligned, so q, k and v may be
+ *      (f32), at least the row's channels, under 32 MiB; 16-byte aligned, so q, k and v may be
  *      parts of one wider buffer.  Coordinates outside the voxel range count as its
  *      nearest end.  Offsets are clamped to [0, nq] / [0, nk].
  * Out: out [nq][ldo] (dt), no input; lse [nq][H] f32 or NULL (the backward's
@@ -641,7 +641,7 @@ typedef struct spv_attention_params {
  *      (NULL where that is 0): few queries split their keys over the chip, and the
  *      parts are joined from there in a fixed order.
  * Errors: SPV_ERR_INVALID_ARG (null or misaligned pointers, sizes, strides, scale,
- *      cap, aliasing), SPV_ERR_UNSUPPORTED (D; more than 2^22 workgroups),
+ *      cap, aliasing), SPV_ERR_UNSUPPORTED (D; over 2^22 workgroups of 32 rows),
  *      SPV_ERR_CAPACITY (ws too small).
  *
  * spv_attention_backward -- its gradients, with delta_i = dout_i . out_i:

@@ -773,9 +773,10 @@ spv_status spv_layer_norm_backward(void* stream, void* ws, size_t ws_bytes, cons
     return hip_check();
 }
 
-// a row stride (in elements) that holds the row's channels and keeps every row 16-byte aligned
+// a row stride (in elements) that holds the row's channels, keeps every row 16-byte aligned and lets 32 bits address the
+// 128 rows that the kernels stage at a time
 static bool row_stride_ok(int64_t ld, int64_t channels, spv_dtype dt) {
-    return ld >= channels && ld % (int64_t)(16 / esize(dt)) == 0 && ld < ((int64_t)1 << 24);
+    return ld >= channels && ld % (int64_t)(16 / esize(dt)) == 0 && ld < ((int64_t)1 << 25) / (int64_t)esize(dt);
 }
 
 // the checks of both directions; fills t with everything but the gradients

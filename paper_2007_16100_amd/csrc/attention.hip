@@ -299,7 +299,7 @@ static AttnShape forward_shape(const AttnArgs& a) {
 
 bool attention_supported(const AttnArgs& a) {
     const int G = a.H / a.K;
-    return attn_tiles(a.nq, a.B, G, 32) * a.K <= kMaxWorkgroups && attn_tiles(a.nk, a.B, G, 32) * a.K <= kMaxWorkgroups;
+    return attn_tiles(a.nq, a.B, G, 32) * a.K <= kMaxWorkgroups && attn_tiles(a.nk, a.B, 1, 32) * a.K <= kMaxWorkgroups;
 }
 
 void plan_attention_ws(Arena& a, AttnArgs& t) {

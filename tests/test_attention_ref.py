@@ -109,6 +109,11 @@ def test_attention_refusals():
         assert fwd(D=D, ldq=4 * 256, ldk=2 * 256, ldv=2 * 256, ldo=4 * 256) == unsup
     assert fwd(nq=0, q=None, out=None) == spv.SPV_OK
     assert fwd(B=0, q_off=None, k_off=None) == spv.SPV_OK
+    # rows of 32 MiB and more, and more workgroups than a grid is given
+    for dt, ld in ((0, 1 << 23), (1, 1 << 24), (2, 1 << 24)):
+        for name in ("ldq", "ldk", "ldv", "ldo"):
+            assert fwd(dt=dt, **{name: ld}) == bad, (dt, name)
+    assert fwd(nq=(1 << 31) - 1) == unsup and fwd(nk=(1 << 31) - 1) == unsup
 
     def bwd(dq=5 * P, dk=6 * P, dv=7 * P, lse=8 * P, dout=9 * P, lddo=128, lddq=128, lddk=64, lddv=64, w=ws, nb=big,
             nq=4):
