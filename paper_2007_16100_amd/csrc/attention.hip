@@ -28,9 +28,9 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     const int c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
     const int G = a.H / a.K, kh = sh.kh;
-    const ScanTile t = find_tile(a.q_off, a.B, a.nq, G, BM, sh.tile);
+    const ScanTile t = find_tile(a.q_off, a.nq, a.k_off, a.nk, a.B, G, BM, sh.tile);
     if (t.col0 >= t.cols) return;  // the whole workgroup
-    const int64_t k0 = uniform(clamp_off(a.k_off[t.b], a.nk)), k1 = uniform(clamp_off(a.k_off[t.b + 1], a.nk));
+    const int64_t k0 = t.r0, k1 = t.r1;
     const int keys = (int)(k1 > k0 ? k1 - k0 : 0), tiles = keys / KT + (keys % KT != 0);
     const int per = (tiles + sh.parts - 1) / sh.parts, t0 = sh.part * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
@@ -43,21 +43,13 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     T::load_cols(a.q, qi * a.ldq + (int64_t)head * a.D, live, a.D, h, qf);
     const float cs = in_vgpr(a.scale * kLog2e), cz = in_vgpr(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f);
     const float cap2 = a.cap * kLog2e, fall = in_vgpr(-2.f * cap2);
-    Words far{0, 0};
-    uint32_t place = 0;
-    Cube cube{};
+    int4 qc{0, 0, 0, 0};
     float slope = 0.f;  // of the scores where there is a cap, else of the products
-    if constexpr (BIAS) {
-        int4 qc{0, 0, 0, 0};
+    if constexpr (BIAS)
         if (live) {
-            qc = voxel_clamp(*(const int4*)(a.q_coords + 4 * qi));
-            slope = CAP ? a.slopes[head] * kLog2e : a.slopes[head] / a.scale;
+            qc = *(const int4*)(a.q_coords + 4 * qi);
+            slope = a.slopes[head];
         }
-        cube = columns_cube(qc, live, box);
-        cube.place(qc, place);
-        far = voxel_words(qc);
-    }
-    const float lift = slope * 8388608.f;
 
     Stage<DT, DP, KT, 256> sk(tid, a.ldk, a.D), sv(tid, a.ldv, a.D);
     const int64_t first = k0 + (int64_t)t0 * KT;
@@ -75,6 +67,21 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
             if (tid < KT) ck = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(r, tid * 16, 0, 0));
         }
     };
+    // the first rows are asked for before anything waits for the columns'
+    if (t0 < t1) load();
+
+    Words far{0, 0};
+    uint32_t place = 0;
+    Cube cube{};
+    if constexpr (BIAS) {
+        qc = voxel_clamp(qc);
+        slope = CAP ? slope * kLog2e : slope / a.scale;
+        cube = columns_cube(qc, live, box);
+        cube.place(qc, place);
+        far = voxel_words(qc);
+    }
+    const float lift = slope * 8388608.f;
+
     auto store = [&](int s) __attribute__((always_inline)) {
         sk.store(lk[s], tid);
         sv.store(lv[s], tid);
@@ -94,7 +101,6 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     for (int b = 0; b < T::NB; ++b) o[b] = f32x16{};
     float m = 0.f, l = 0.f;
     if (t0 < t1) {
-        load();
         store(0);
         if (t0 + 1 < t1) load();
     }

@@ -44,9 +44,9 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     const int c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
     const int G = a.H / a.K, kh = sh.kh;
-    const ScanTile t = find_tile(a.q_off, a.B, a.nq, G, BM, sh.tile);
+    const ScanTile t = find_tile(a.q_off, a.nq, a.k_off, a.nk, a.B, G, BM, sh.tile);
     if (t.col0 >= t.cols) return;  // the whole workgroup
-    const int64_t k0 = uniform(clamp_off(a.k_off[t.b], a.nk)), k1 = uniform(clamp_off(a.k_off[t.b + 1], a.nk));
+    const int64_t k0 = t.r0, k1 = t.r1;
     const int keys = (int)(k1 > k0 ? k1 - k0 : 0), tiles = keys / KT + (keys % KT != 0);
     const int per = (tiles + sh.parts - 1) / sh.parts, t0 = sh.part * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
@@ -58,37 +58,17 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     T::load_cols(a.q, qi * a.ldq + (int64_t)head * a.D, live, a.D, h, qf);
     T::load_cols(a.dout, qi * a.lddo + (int64_t)head * a.D, live, a.D, h, df);
     float lse = 0.f, delta = 0.f;
-    {
-        uint4 of[T::NF];
-        T::load_cols(a.out, qi * a.ldo + (int64_t)head * a.D, live, a.D, h, of);
-#pragma unroll
-        for (int s = 0; s < T::NF; ++s) delta = T::frag_dot(df[s], of[s], delta);
-        delta = half_sum(delta);
-    }
-    Words far{0, 0};
-    uint32_t place = 0;
-    Cube cube{};
+    uint4 of[T::NF];
+    T::load_cols(a.out, qi * a.ldo + (int64_t)head * a.D, live, a.D, h, of);
+    int4 qc{0, 0, 0, 0};
     float slope = 0.f;  // of the scores where there is a cap, else of the products
     if (live) {
-        lse = a.lse[qi * a.H + head] * kLog2e;
-        if (h == 0 && sh.part == 0 && kw == 0) a.delta[qi * a.H + head] = delta;
-    }
-    if constexpr (BIAS) {
-        int4 qc{0, 0, 0, 0};
-        if (live) {
-            qc = voxel_clamp(*(const int4*)(a.q_coords + 4 * qi));
-            slope = CAP ? a.slopes[head] * kLog2e : a.slopes[head] / a.scale;
+        lse = a.lse[qi * a.H + head];
+        if constexpr (BIAS) {
+            qc = *(const int4*)(a.q_coords + 4 * qi);
+            slope = a.slopes[head];
         }
-        cube = columns_cube(qc, live, box);
-        cube.place(qc, place);
-        far = voxel_words(qc);
     }
-    const float lift = slope * 8388608.f;
-    const float cs = in_vgpr(a.scale * kLog2e);
-    const Capped capped(a);
-    f32x16 dref;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dref[r] = -delta;
 
     Stage<DT, DP, KT, 256> sk(tid, a.ldk, a.D), sv(tid, a.ldv, a.D);
     const int64_t first = k0 + (int64_t)t0 * KT;
@@ -106,6 +86,31 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
             if (tid < KT) ck = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(r, tid * 16, 0, 0));
         }
     };
+    // the first rows are asked for before anything waits for the columns'
+    if (t0 < t1) load();
+
+    lse *= kLog2e;
+#pragma unroll
+    for (int s = 0; s < T::NF; ++s) delta = T::frag_dot(df[s], of[s], delta);
+    delta = half_sum(delta);
+    if (live && h == 0 && sh.part == 0 && kw == 0) a.delta[qi * a.H + head] = delta;
+    Words far{0, 0};
+    uint32_t place = 0;
+    Cube cube{};
+    if constexpr (BIAS) {
+        qc = voxel_clamp(qc);
+        slope = CAP ? slope * kLog2e : slope / a.scale;
+        cube = columns_cube(qc, live, box);
+        cube.place(qc, place);
+        far = voxel_words(qc);
+    }
+    const float lift = slope * 8388608.f;
+    const float cs = in_vgpr(a.scale * kLog2e);
+    const Capped capped(a);
+    f32x16 dref;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dref[r] = -delta;
+
     auto store = [&](int s) __attribute__((always_inline)) {
         sk.store(lk[s], tid);
         sv.store(lv[s], tid);
@@ -116,7 +121,6 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
 #pragma unroll
     for (int b = 0; b < T::NB; ++b) o[b] = f32x16{};
     if (t0 < t1) {
-        load();
         store(0);
         if (t0 + 1 < t1) load();
     }
@@ -205,9 +209,9 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
     const int c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
     const int G = a.H / a.K, kh = sh.kh;
-    const ScanTile t = find_tile(a.k_off, a.B, a.nk, 1, BM, sh.tile);
+    const ScanTile t = find_tile(a.k_off, a.nk, a.q_off, a.nq, a.B, 1, BM, sh.tile);
     if (t.col0 >= t.cols) return;  // the whole workgroup
-    const int64_t q0 = uniform(clamp_off(a.q_off[t.b], a.nq)), q1 = uniform(clamp_off(a.q_off[t.b + 1], a.nq));
+    const int64_t q0 = t.r0, q1 = t.r1;
     const int64_t tiles = q1 > q0 ? (q1 - q0 + KT - 1) / KT : 0, all = tiles * G;
     const int64_t per = (all + sh.parts - 1) / sh.parts;
     const int64_t t0 = sh.part * per, t1 = t0 + per < all ? t0 + per : all;
@@ -217,18 +221,9 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
     uint4 kf[T::NF], vf[T::NF];
     T::load_cols(a.k, kj * a.ldk + (int64_t)kh * a.D, live, a.D, h, kf);
     T::load_cols(a.v, kj * a.ldv + (int64_t)kh * a.D, live, a.D, h, vf);
-    Words far{0, 0};
-    uint32_t place = 0;
-    Cube cube{};
-    if constexpr (BIAS) {
-        int4 kc{0, 0, 0, 0};
-        if (live) kc = voxel_clamp(*(const int4*)(a.k_coords + 4 * kj));
-        cube = columns_cube(kc, live, box);
-        cube.place(kc, place);
-        far = voxel_words(kc);
-    }
-    const float cs = in_vgpr(a.scale * kLog2e), inv_cs = 1.f / cs;
-    const Capped capped(a);
+    int4 kc{0, 0, 0, 0};
+    if constexpr (BIAS)
+        if (live) kc = *(const int4*)(a.k_coords + 4 * kj);
 
     Stage<DT, DP, KT, 256> sq(tid, a.ldq, a.D), sd(tid, a.lddo, a.D);
     int4 cq{0, 0, 0, 0};
@@ -265,6 +260,21 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
             if (next < t1) start();
         }
     };
+    int64_t i_now = i_next, g_now = g_next;
+    // the first rows are asked for before anything waits for the columns'
+    if (t0 < t1) load();
+
+    const float cs = in_vgpr(a.scale * kLog2e), inv_cs = 1.f / cs;
+    const Capped capped(a);
+    Words far{0, 0};
+    uint32_t place = 0;
+    Cube cube{};
+    if constexpr (BIAS) {
+        kc = voxel_clamp(kc);
+        cube = columns_cube(kc, live, box);
+        cube.place(kc, place);
+        far = voxel_words(kc);
+    }
     auto store = [&](int s) __attribute__((always_inline)) {
         sq.store(lq[s], tid);
         sd.store(ld[s], tid);
@@ -281,9 +291,7 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
     f32x16 ok[T::NB], ov[T::NB];
 #pragma unroll
     for (int b = 0; b < T::NB; ++b) ok[b] = ov[b] = f32x16{};
-    int64_t i_now = i_next, g_now = g_next;
     if (t0 < t1) {
-        load();
         store(0);
         if (t0 + 1 < t1) load();
     }

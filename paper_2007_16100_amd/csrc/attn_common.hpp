@@ -39,8 +39,8 @@ __device__ inline int64_t uniform(int64_t v) {
 // The tiles of a side: scan b's rows * per columns are cut into tiles of BM from its own start, and its first tile
 // is number floor(off[b] * per / BM) + b: ascending in b, with room for every scan's tiles and known without a
 // pass over the scans.  attn_tiles bounds their number.
-__device__ inline int64_t scan_tile(const int32_t* off, int b, int64_t n, int per, int BM) {
-    return clamp_off(off[b], n) * per / BM + b;
+__device__ inline int64_t scan_tile(int32_t off, int b, int64_t n, int per, int BM) {
+    return clamp_off(off, n) * per / BM + b;
 }
 inline int64_t attn_tiles(int64_t n, int B, int per, int BM) { return n * per / BM + B; }
 
@@ -61,24 +61,33 @@ struct ScanTile {
     int64_t first;   // its first row
     int64_t cols;    // its columns (rows * per)
     int64_t col0;    // the tile's first column; at least cols: nothing to do
+    int64_t r0, r1;  // the scan's rows of the other side
 };
-// the scan of tile t: a search with 64 probes a step
-__device__ inline ScanTile find_tile(const int32_t* off, int B, int64_t n, int per, int BM, int64_t t) {
+// The scan of tile t, by a search with 63 intervals a step.  Both sides' offsets are read in the same step and handed
+// over between lanes: one wait for memory (up to 63 scans) before the rows themselves can be asked for.
+__device__ inline ScanTile find_tile(const int32_t* off, int64_t n, const int32_t* other, int64_t n_other, int B, int per,
+                                     int BM, int64_t t) {
     const int lane = threadIdx.x & 63;
-    int lo = 0, hi = B;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) >> 6, at = lo + step * lane;
-        const bool le = at < hi && scan_tile(off, at, n, per, BM) <= t;
-        const int k = __popcll(__ballot(le));
-        lo += step * (k > 0 ? k - 1 : 0);
+    int lo = 0, hi = B, step, k, o, r;
+    do {
+        step = (hi - lo + 62) / 63;
+        const int at = lo + step * lane;
+        o = r = 0;
+        if (at <= hi) o = off[at], r = other[at];
+        k = __popcll(__ballot(at < hi && scan_tile(o, at, n, per, BM) <= t));
+        k = uniform(k > 0 ? k - 1 : 0);
+        lo += step * k;
         hi = lo + step < hi ? lo + step : hi;
-    }
+    } while (step > 1);
     ScanTile s;
     s.b = uniform(lo);
-    s.first = uniform(clamp_off(off[s.b], n));
-    const int64_t end = uniform(clamp_off(off[s.b + 1], n)), mine = t - uniform(scan_tile(off, s.b, n, per, BM));
+    const int32_t first = __builtin_amdgcn_readlane(o, k);
+    s.first = clamp_off(first, n);
+    const int64_t end = clamp_off(__builtin_amdgcn_readlane(o, k + 1), n), mine = t - scan_tile(first, s.b, n, per, BM);
     s.cols = end > s.first ? (end - s.first) * per : 0;
     s.col0 = mine >= 0 ? mine * BM : s.cols;
+    s.r0 = clamp_off(__builtin_amdgcn_readlane(r, k), n_other);
+    s.r1 = clamp_off(__builtin_amdgcn_readlane(r, k + 1), n_other);
     return s;
 }
 
