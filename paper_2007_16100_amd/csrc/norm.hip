@@ -12,7 +12,9 @@ namespace spv {
 
 constexpr int kNormWaves = 4;
 constexpr unsigned kNormGrid = 2048;    // workgroups of the forward at most
-constexpr unsigned kNormBwdGrid = 512;  // of the backward: two per CU, whose column sums are joined
+// of the backward: two per CU, whose column sums are joined.  Forward and backward of 300,007 x 96 in bf16 with the
+// residual's gradient take 65 us with 512, 77 with 768, 73 with 1024.
+constexpr unsigned kNormBwdGrid = 512;
 
 __device__ inline float wave_sum(float v) {
 #pragma unroll
@@ -113,7 +115,10 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_norm_cols_any(NormBwdArgs a
 // v * L + l of the row), 64 / L rows a wave.  A row is read once: the mean, the deviations and, in the
 // backward, both of its means are formed in registers.  What bounds it is memory, so each wave's next rows
 // are loaded before the present ones are reduced, and gamma, beta and the column sums stay in registers
-// over a workgroup's rows.
+// over a workgroup's rows.  Three vectors a lane hold rows of 96, 192, 384 .. without idle lanes.
+// 300,007 x 96 in bf16: 23.8 us, 4.8 TB/s (a copy of 1 GiB reaches 5.1).  Forward and backward of 88,119 x 96
+// in bf16 with the residual's gradient: 29 us, of which the join of the column sums 4; of 26,881 x 256 in
+// f16: 25 us.  701 x 96 in float32: 3.4 us on the GPU, 7.4 a call.
 // ---------------------------------------------------------------------------
 template <int DT>
 constexpr int kVec = DT == SPV_F32 ? 4 : 8;
