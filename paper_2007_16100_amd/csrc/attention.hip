@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     RowTiles<KT> rv((const char*)a.v + kh * a.D * T::SZ, first, k1, a.ldv * T::SZ, a.D * T::SZ);
     RowTiles<KT> rc(a.k_coords, first, k1, 16, 16);
     int4 ck{0, 0, 0, 0};
-    int64_t ck_left = 0;
+    int ck_left = 0;
     auto load = [&]() __attribute__((always_inline)) {
         sk.load(rk.next());
         sv.load(rv.next());

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     RowTiles<KT> rv((const char*)a.v + kh * a.D * T::SZ, first, k1, a.ldv * T::SZ, a.D * T::SZ);
     RowTiles<KT> rc(a.k_coords, first, k1, 16, 16);
     int4 ck{0, 0, 0, 0};
-    int64_t ck_left = 0;
+    int ck_left = 0;
     auto load = [&]() __attribute__((always_inline)) {
         sk.load(rk.next());
         sv.load(rv.next());
@@ -221,9 +221,8 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
     const ScanTile t = find_tile(a.k_off, a.nk, a.q_off, a.nq, a.B, 1, BM, sh.tile);
     if (t.col0 >= t.cols) return;  // the whole workgroup
     const int64_t q0 = t.r0, q1 = t.r1;
-    const int64_t tiles = q1 > q0 ? (q1 - q0 + KT - 1) / KT : 0, all = tiles * G;
-    const int64_t per = (all + sh.parts - 1) / sh.parts;
-    const int64_t t0 = sh.part * per, t1 = t0 + per < all ? t0 + per : all;
+    const int rows = (int)(q1 > q0 ? q1 - q0 : 0), tiles = rows / KT + (rows % KT != 0), all = tiles * G;
+    const int per = (all + sh.parts - 1) / sh.parts, t0 = sh.part * per, t1 = t0 + per < all ? t0 + per : all;
 
     const bool busy = t.col0 + 32 * cw < t.cols, live = t.col0 + 32 * cw + c < t.cols;
     const int64_t kj = t.first + t.col0 + 32 * cw + c;
@@ -237,12 +236,12 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
     Stage<DT, DP, KT, 256> sq(tid, a.ldq, a.D), sd(tid, a.lddo, a.D);
     int4 cq{0, 0, 0, 0};
     float rl = 0.f, rd = 0.f;
-    int64_t left = 0;
+    int left = 0;
     // the tile to load and the one at work, as head of the group and tile of its rows
-    int64_t next = t0, g_next = tiles ? t0 / tiles : 0, i_next = t0 - g_next * tiles;
+    int next = t0, g_next = tiles ? t0 / tiles : 0, i_next = t0 - g_next * tiles;
     RowTiles<KT> rq, ro, re, rt, rc;
     auto start = [&]() __attribute__((always_inline)) {
-        const int64_t r = q0 + i_next * KT, head = (int64_t)kh * G + g_next;
+        const int64_t r = q0 + (int64_t)i_next * KT, head = (int64_t)kh * G + g_next;
         rq = RowTiles<KT>((const char*)a.q + head * a.D * T::SZ, r, q1, a.ldq * T::SZ, a.D * T::SZ);
         ro = RowTiles<KT>((const char*)a.dout + head * a.D * T::SZ, r, q1, a.lddo * T::SZ, a.D * T::SZ);
         re = RowTiles<KT>(a.lse + head, r, q1, 4 * a.H, 4);
@@ -269,7 +268,7 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
             if (next < t1) start();
         }
     };
-    int64_t i_now = i_next, g_now = g_next;
+    int i_now = i_next, g_now = g_next;
     // the first rows are asked for before anything waits for the columns'
     if (t0 < t1) load();
 
@@ -305,13 +304,13 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
         if (t0 + 1 < t1) load();
     }
     __syncthreads();
-    for (int64_t i = t0; i < t1; ++i) {
-        const int s = (int)(i - t0) & 1;
+    for (int i = t0; i < t1; ++i) {
+        const int s = (i - t0) & 1;
         const int row0 = RT * kw;  // the wave's rows of the tile
-        if (busy && q0 + i_now * KT + row0 < q1) {
+        if (busy && i_now * KT + row0 < rows) {
             float slope = 0.f, lift = 0.f;
             if constexpr (BIAS) {
-                slope = in_vgpr(a.slopes[(int64_t)kh * G + g_now] * kLog2e);
+                slope = in_vgpr(a.slopes[kh * G + g_now] * kLog2e);
                 lift = slope * 8388608.f;
             }
             f32x16 z[KS], d[KS], rest[CAP ? KS : 1];

@@ -386,15 +386,19 @@ __device__ inline f32x16 row_values(const float* p, int h) {
 template <int KT>
 struct RowTiles {
     const char* at;
-    int64_t left, step;
-    int ld, row;
+    int64_t step;
+    int left, ld, row;
     __device__ RowTiles() {}
-    // rows first .. n - 1 of p, ld_bytes apart, row_bytes of each
+    // rows first .. n - 1 of p (offsets of 32 bits), ld_bytes apart, row_bytes of each
     __device__ RowTiles(const void* p, int64_t first, int64_t n, int64_t ld_bytes, int row_bytes)
-        : at((const char*)p + first * ld_bytes), left(n - first), step(KT * ld_bytes), ld((int)ld_bytes), row(row_bytes) {}
+        : at((const char*)p + first * ld_bytes), step(KT * ld_bytes), left((int)(n - first)), ld((int)ld_bytes),
+          row(row_bytes) {}
     __device__ inline __amdgpu_buffer_rsrc_t next() {
         uint32_t bytes = (uint32_t)(KT - 1) * (uint32_t)ld + (uint32_t)row;
-        if (left < KT) bytes = left > 0 ? (uint32_t)(left - 1) * (uint32_t)ld + (uint32_t)row : 0u;
+        if (left < KT) {
+            asm volatile("");  // a branch: the last tile alone needs the products
+            bytes = left > 0 ? (uint32_t)(left - 1) * (uint32_t)ld + (uint32_t)row : 0u;
+        }
         const __amdgpu_buffer_rsrc_t r = make_rsrc(at, bytes);
         at += step;
         left -= KT;
@@ -489,6 +493,8 @@ inline AttnShape attn_shape(int dt, int DP, int64_t n, int per, int B, int K, in
     }
     return s;
 }
+// of a launch, in tiles of 32 columns; a scan's tiles of rows, each once for a key head's query heads, are no more, so
+// 32 bits count them
 constexpr int64_t kMaxWorkgroups = (int64_t)1 << 22;
 
 }  // namespace spv
