@@ -63,17 +63,18 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
 
     Stage<DT, DP, KT, 256> sk(tid, a.ldk, a.D), sv(tid, a.ldv, a.D);
     const int64_t first = k0 + (int64_t)t0 * KT;
-    RowTiles<KT> rk((const char*)a.k + kh * a.D * T::SZ, first, k1, a.ldk * T::SZ, a.D * T::SZ);
-    RowTiles<KT> rv((const char*)a.v + kh * a.D * T::SZ, first, k1, a.ldv * T::SZ, a.D * T::SZ);
-    RowTiles<KT> rc(a.k_coords, first, k1, 16, 16);
+    RowTiles<KT> rk((const char*)a.k + kh * a.D * T::SZ, first, a.ldk * T::SZ, a.D * T::SZ);
+    RowTiles<KT> rv((const char*)a.v + kh * a.D * T::SZ, first, a.ldv * T::SZ, a.D * T::SZ);
+    RowTiles<KT> rc(a.k_coords, first, 16, 16);
     int4 ck{0, 0, 0, 0};
-    int ck_left = 0;
+    int ahead = keys - t0 * KT, got = 0;  // keys to load, and how many of them the tile loaded last has
     auto load = [&]() __attribute__((always_inline)) {
-        sk.load(rk.next());
-        sv.load(rv.next());
+        got = ahead < KT ? ahead : KT;
+        ahead -= KT;
+        sk.load(rk.next(got));
+        sv.load(rv.next(got));
         if constexpr (BIAS) {
-            ck_left = rc.left;
-            const __amdgpu_buffer_rsrc_t r = rc.next();
+            const __amdgpu_buffer_rsrc_t r = rc.next(got);
             if (tid < KT) ck = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(r, tid * 16, 0, 0));
         }
     };
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
         sk.store(lk[s], tid);
         sv.store(lv[s], tid);
         if constexpr (BIAS)
-            if (tid < KT) lc.put(s, tid, ck, tid < ck_left, cube);
+            if (tid < KT) lc.put(s, tid, ck, tid < got, cube);
     };
 
     // weights of scores (relative to m already under a cap)

@@ -81,17 +81,18 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
 
     Stage<DT, DP, KT, 256> sk(tid, a.ldk, a.D), sv(tid, a.ldv, a.D);
     const int64_t first = k0 + (int64_t)t0 * KT;
-    RowTiles<KT> rk((const char*)a.k + kh * a.D * T::SZ, first, k1, a.ldk * T::SZ, a.D * T::SZ);
-    RowTiles<KT> rv((const char*)a.v + kh * a.D * T::SZ, first, k1, a.ldv * T::SZ, a.D * T::SZ);
-    RowTiles<KT> rc(a.k_coords, first, k1, 16, 16);
+    RowTiles<KT> rk((const char*)a.k + kh * a.D * T::SZ, first, a.ldk * T::SZ, a.D * T::SZ);
+    RowTiles<KT> rv((const char*)a.v + kh * a.D * T::SZ, first, a.ldv * T::SZ, a.D * T::SZ);
+    RowTiles<KT> rc(a.k_coords, first, 16, 16);
     int4 ck{0, 0, 0, 0};
-    int ck_left = 0;
+    int ahead = keys - t0 * KT, got = 0;  // keys to load, and how many of them the tile loaded last has
     auto load = [&]() __attribute__((always_inline)) {
-        sk.load(rk.next());
-        sv.load(rv.next());
+        got = ahead < KT ? ahead : KT;
+        ahead -= KT;
+        sk.load(rk.next(got));
+        sv.load(rv.next(got));
         if constexpr (BIAS) {
-            ck_left = rc.left;
-            const __amdgpu_buffer_rsrc_t r = rc.next();
+            const __amdgpu_buffer_rsrc_t r = rc.next(got);
             if (tid < KT) ck = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(r, tid * 16, 0, 0));
         }
     };
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
         sk.store(lk[s], tid);
         sv.store(lv[s], tid);
         if constexpr (BIAS)
-            if (tid < KT) lc.put(s, tid, ck, tid < ck_left, cube);
+            if (tid < KT) lc.put(s, tid, ck, tid < got, cube);
     };
     f32x16 o[T::NB];
 #pragma unroll
@@ -236,30 +237,30 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
     Stage<DT, DP, KT, 256> sq(tid, a.ldq, a.D), sd(tid, a.lddo, a.D);
     int4 cq{0, 0, 0, 0};
     float rl = 0.f, rd = 0.f;
-    int left = 0;
+    int got = 0;  // rows of the tile loaded last
     // the tile to load and the one at work, as head of the group and tile of its rows
     int next = t0, g_next = tiles ? t0 / tiles : 0, i_next = t0 - g_next * tiles;
     RowTiles<KT> rq, ro, re, rt, rc;
     auto start = [&]() __attribute__((always_inline)) {
         const int64_t r = q0 + (int64_t)i_next * KT, head = (int64_t)kh * G + g_next;
-        rq = RowTiles<KT>((const char*)a.q + head * a.D * T::SZ, r, q1, a.ldq * T::SZ, a.D * T::SZ);
-        ro = RowTiles<KT>((const char*)a.dout + head * a.D * T::SZ, r, q1, a.lddo * T::SZ, a.D * T::SZ);
-        re = RowTiles<KT>(a.lse + head, r, q1, 4 * a.H, 4);
-        rt = RowTiles<KT>(a.delta + head, r, q1, 4 * a.H, 4);
-        rc = RowTiles<KT>(a.q_coords, r, q1, 16, 16);
+        rq = RowTiles<KT>((const char*)a.q + head * a.D * T::SZ, r, a.ldq * T::SZ, a.D * T::SZ);
+        ro = RowTiles<KT>((const char*)a.dout + head * a.D * T::SZ, r, a.lddo * T::SZ, a.D * T::SZ);
+        re = RowTiles<KT>(a.lse + head, r, 4 * a.H, 4);
+        rt = RowTiles<KT>(a.delta + head, r, 4 * a.H, 4);
+        rc = RowTiles<KT>(a.q_coords, r, 16, 16);
     };
     start();
     auto load = [&]() __attribute__((always_inline)) {
-        left = rq.left;
-        sq.load(rq.next());
-        sd.load(ro.next());
-        const __amdgpu_buffer_rsrc_t be = re.next(), bt = rt.next();
+        got = rows - i_next * KT < KT ? rows - i_next * KT : KT;
+        sq.load(rq.next(got));
+        sd.load(ro.next(got));
+        const __amdgpu_buffer_rsrc_t be = re.next(got), bt = rt.next(got);
         if (tid < KT) {
             rl = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(be, tid * 4 * a.H, 0, 0));
             rd = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(bt, tid * 4 * a.H, 0, 0));
         }
         if constexpr (BIAS) {
-            const __amdgpu_buffer_rsrc_t bc = rc.next();
+            const __amdgpu_buffer_rsrc_t bc = rc.next(got);
             if (tid < KT) cq = __builtin_bit_cast(int4, __builtin_amdgcn_raw_buffer_load_b128(bc, tid * 16, 0, 0));
         }
         ++next;
@@ -288,7 +289,7 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
         sd.store(ld[s], tid);
         if (tid < KT) {
             // a row past the end has no weight: its lse counts as infinite
-            const bool in = tid < left;
+            const bool in = tid < got;
             const float e = in ? kUp<DT> - rl * kLog2e : -INFINITY;
             lr[s][0][tid] = CAP ? e + capped.cap2 : e * inv_cs;
             lr[s][1][tid] = -rd;

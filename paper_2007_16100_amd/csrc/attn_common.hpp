@@ -381,27 +381,21 @@ __device__ inline f32x16 row_values(const float* p, int h) {
     return z;
 }
 
-// Rows of a scan, KT at a time, as buffers: what lies outside reads as zero.  Scalar state: the next rows' address, how
-// many are left, and the bytes of a whole tile.
+// Rows of a scan, KT at a time, as buffers: what lies outside reads as zero.  Scalar state: the next rows' address and
+// the bytes of a whole tile.
 template <int KT>
 struct RowTiles {
     const char* at;
     int64_t step;
-    int left, ld, row;
+    int ld, row;
     __device__ RowTiles() {}
-    // rows first .. n - 1 of p (offsets of 32 bits), ld_bytes apart, row_bytes of each
-    __device__ RowTiles(const void* p, int64_t first, int64_t n, int64_t ld_bytes, int row_bytes)
-        : at((const char*)p + first * ld_bytes), step(KT * ld_bytes), left((int)(n - first)), ld((int)ld_bytes),
-          row(row_bytes) {}
-    __device__ inline __amdgpu_buffer_rsrc_t next() {
-        uint32_t bytes = (uint32_t)(KT - 1) * (uint32_t)ld + (uint32_t)row;
-        if (left < KT) {
-            asm volatile("");  // a branch: the last tile alone needs the products
-            bytes = left > 0 ? (uint32_t)(left - 1) * (uint32_t)ld + (uint32_t)row : 0u;
-        }
-        const __amdgpu_buffer_rsrc_t r = make_rsrc(at, bytes);
+    // of p from row `first` on, ld_bytes apart, row_bytes of each
+    __device__ RowTiles(const void* p, int64_t first, int64_t ld_bytes, int row_bytes)
+        : at((const char*)p + first * ld_bytes), step(KT * ld_bytes), ld((int)ld_bytes), row(row_bytes) {}
+    // the next 1 .. KT of them
+    __device__ inline __amdgpu_buffer_rsrc_t next(int rows) {
+        const __amdgpu_buffer_rsrc_t r = make_rsrc(at, (uint32_t)(rows - 1) * (uint32_t)ld + (uint32_t)row);
         at += step;
-        left -= KT;
         return r;
     }
 };
