@@ -15,11 +15,11 @@ namespace spv {
 // In 16 bits at 32 channels a score costs two matrix products of 32 channels but seven vector instructions (distance,
 // bias, reference, exponential, maximum, sum, rounding), of which the exponential counts double: those bound it, not the
 // products.  They keep the vector units busy 82% of the time at [16384] x 8 heads.
-// [3451, 3654, 1963, 2195] x 8 heads of 32, bf16, bias: 91 us (scores alone: 50 - 60; products: 29); the rest is what
-// 720 workgroups leave of 256 compute units at the end, and the waits at the barriers of two to three workgroups a unit.
-// Four scans of 26,881 in all x 4 heads of 64 on 2, f16, cap and bias: 481 us; a cap adds an exponential, a reciprocal
+// [3451, 3654, 1963, 2195] x 8 heads of 32, bf16, bias: 90 us (scores alone: 50 - 60; products: 29); its 720 workgroups
+// leave two to three waves a SIMD, which wait at barriers and for each other's products.
+// Four scans of 26,881 in all x 4 heads of 64 on 2, f16, cap and bias: 474 us; a cap adds an exponential, a reciprocal
 // and three more instructions.  One query over 88,119 keys x 8 heads of 32: 18 us in 64 parts, 3.8 TB/s with the join.
-// 211 x 3 heads in float32: 9.4 us a call.  In float32 the products (64 cycles each) bound it: [1457, 1544] x 3 heads,
+// 211 x 3 heads in float32: 9.5 us a call.  In float32 the products (64 cycles each) bound it: [1457, 1544] x 3 heads,
 // cap and bias, 47 us, where 288 workgroups lie on 256 units.
 constexpr float kLead = 8.f;
 

@@ -11,9 +11,9 @@
 // dq and dk of bf16 are off by 2.6e-3 (root of the mean square against 64 bits), their own last rounding alone by 1.7e-3.
 // An exact delta takes one more product of p and k, and brings 2.4e-3.
 //
-// [3451, 3654, 1963, 2195] x 8 heads of 32, bf16, bias: dq 111 us, dk and dv 175.  As in the forward the vector
+// [3451, 3654, 1963, 2195] x 8 heads of 32, bf16, bias: dq 106 us, dk and dv 141.  As in the forward the vector
 // instructions of a score bound dq; dk and dv have two accumulators of a column, so two or three waves a SIMD, and wait
-// for LDS and the matrix unit in turn.  [1457, 1544] x 3 heads in float32, cap and bias: dq 63 us, dk and dv 82, by the
+// for LDS and the matrix unit in turn.  [1457, 1544] x 3 heads in float32, cap and bias: dq 61 us, dk and dv 75, by the
 // products, with 288 workgroups on 256 units.
 #include "attn_common.hpp"
 
