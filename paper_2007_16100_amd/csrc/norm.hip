@@ -16,35 +16,40 @@ constexpr unsigned kNormGrid = 2048;    // workgroups of the forward at most
 // residual's gradient take 65 us with 512, 77 with 768, 73 with 1024.
 constexpr unsigned kNormBwdGrid = 512;
 
-__device__ inline float wave_sum(float v) {
+// sum over the L lanes of a row
+template <int L>
+__device__ inline float row_sum(float v) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    for (int o = 1; o < L; o <<= 1) v += __shfl_xor(v, o, 64);
     return v;
 }
 
-// mean and 1 / deviation of row x[0 .. C), the whole wave
-template <int DT>
-__device__ inline void row_stats(const void* x, int64_t base, int C, float eps, int lane, float& mu, float& r) {
+// mean and 1 / deviation of row x[0 .. C) (on: there is one), from the L lanes that hold it
+template <int DT, int L>
+__device__ inline void row_stats(const void* x, int64_t base, int C, float eps, int l, bool on, float& mu, float& r) {
     float s = 0.f;
-    for (int c = lane; c < C; c += 64) s += ld_feat<DT>(x, base + c);
-    mu = wave_sum(s) / (float)C;
+    for (int c = l; on && c < C; c += L) s += ld_feat<DT>(x, base + c);
+    mu = row_sum<L>(s) / (float)C;
     float ss = 0.f;
-    for (int c = lane; c < C; c += 64) {
+    for (int c = l; on && c < C; c += L) {
         const float d = ld_feat<DT>(x, base + c) - mu;
         ss = fmaf(d, d, ss);
     }
-    r = 1.f / sqrtf(wave_sum(ss) / (float)C + eps);
+    r = 1.f / sqrtf(row_sum<L>(ss) / (float)C + eps);
 }
 
-// a wave per row, any width and alignment
-template <int DT>
+// any width and alignment: L lanes a row, 64 / L rows a wave, which leave the loop together
+template <int DT, int L>
 __global__ __launch_bounds__(64 * kNormWaves) void k_norm_any(NormArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t m = clamp_rows(a.m_dev, a.m_cap);
-    for (int64_t i = (int64_t)blockIdx.x * kNormWaves + wave; i < m; i += (int64_t)gridDim.x * kNormWaves) {
+    constexpr int R = 64 / L;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & (L - 1);
+    const int64_t m = clamp_rows(a.m_dev, a.m_cap), step = (int64_t)gridDim.x * kNormWaves * R;
+    for (int64_t i0 = ((int64_t)blockIdx.x * kNormWaves + wave) * R; i0 < m; i0 += step) {
+        const int64_t i = i0 + lane / L;
+        const bool on = i < m;
         float mu, r;
-        row_stats<DT>(a.x, i * a.C, a.C, a.eps, lane, mu, r);
-        for (int c = lane; c < a.C; c += 64) {
+        row_stats<DT, L>(a.x, i * a.C, a.C, a.eps, l, on, mu, r);
+        for (int c = l; on && c < a.C; c += L) {
             const float xh = (ld_feat<DT>(a.x, i * a.C + c) - mu) * r;
             st_feat<DT>(a.out, i * a.C + c, fmaf(xh, a.gamma ? a.gamma[c] : 1.f, a.beta ? a.beta[c] : 0.f));
         }
@@ -52,27 +57,30 @@ __global__ __launch_bounds__(64 * kNormWaves) void k_norm_any(NormArgs a) {
 }
 
 // dx, and each row's statistics for the column sums
-template <int DT>
+template <int DT, int L>
 __global__ __launch_bounds__(64 * kNormWaves) void k_norm_bwd_any(NormBwdArgs a, float* stat) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t m = clamp_rows(a.m_dev, a.m_cap);
-    for (int64_t i = (int64_t)blockIdx.x * kNormWaves + wave; i < m; i += (int64_t)gridDim.x * kNormWaves) {
+    constexpr int R = 64 / L;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & (L - 1);
+    const int64_t m = clamp_rows(a.m_dev, a.m_cap), step = (int64_t)gridDim.x * kNormWaves * R;
+    for (int64_t i0 = ((int64_t)blockIdx.x * kNormWaves + wave) * R; i0 < m; i0 += step) {
+        const int64_t i = i0 + lane / L;
+        const bool on = i < m;
         float mu, r;
-        row_stats<DT>(a.x, i * a.C, a.C, a.eps, lane, mu, r);
-        if (stat && lane == 0) {
+        row_stats<DT, L>(a.x, i * a.C, a.C, a.eps, l, on, mu, r);
+        if (stat && on && l == 0) {
             stat[2 * i] = mu;
             stat[2 * i + 1] = r;
         }
         if (!a.dx) continue;
         float s1 = 0.f, s2 = 0.f;
-        for (int c = lane; c < a.C; c += 64) {
+        for (int c = l; on && c < a.C; c += L) {
             const float h = ld_feat<DT>(a.dy, i * a.C + c) * (a.gamma ? a.gamma[c] : 1.f);
             s1 += h;
             s2 = fmaf(h, (ld_feat<DT>(a.x, i * a.C + c) - mu) * r, s2);
         }
-        s1 = wave_sum(s1) / (float)a.C;
-        s2 = wave_sum(s2) / (float)a.C;
-        for (int c = lane; c < a.C; c += 64) {
+        s1 = row_sum<L>(s1) / (float)a.C;
+        s2 = row_sum<L>(s2) / (float)a.C;
+        for (int c = l; on && c < a.C; c += L) {
             const int64_t t = i * a.C + c;
             const float h = ld_feat<DT>(a.dy, t) * (a.gamma ? a.gamma[c] : 1.f);
             const float xh = (ld_feat<DT>(a.x, t) - mu) * r;
@@ -145,13 +153,6 @@ __device__ inline uint4 pack(const float (&x)[kVec<DT>]) {
         else w[j] = pack2<DT>(x[2 * j], x[2 * j + 1]);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
-}
-// sum over the L lanes of a row
-template <int L>
-__device__ inline float row_sum(float v) {
-#pragma unroll
-    for (int o = 1; o < L; o <<= 1) v += __shfl_xor(v, o, 64);
-    return v;
 }
 
 template <int DT, int L, int NV>
@@ -389,13 +390,19 @@ static bool norm_aligned(const void* p, const void* q, const void* r = nullptr, 
     return (((uintptr_t)p | (uintptr_t)q | (uintptr_t)r | (uintptr_t)t) & 15u) == 0;
 }
 
+// Channels up to which the plain kernels give a row 8 lanes, not 64.  Forward and backward of 88,119 x 19 in float32 take
+// 42 us with 8, 145 with 64; of 20,011 x 131 54 and 74; of 5003 x 511 in f16 86 and 50.
+constexpr int kNarrow = 256;
+
 template <int DT>
 static void norm_dt(hipStream_t s, const NormArgs& a) {
     const bool vec = norm_shape<DT>(a.C, norm_aligned(a.x, a.out), [&](auto l, auto nv) {
         constexpr int L = decltype(l)::value, NV = decltype(nv)::value;
         k_norm<DT, L, NV><<<norm_grid(a.m_cap, kNormWaves * (64 / L), kNormGrid), 64 * kNormWaves, 0, s>>>(a);
     });
-    if (!vec) k_norm_any<DT><<<norm_grid(a.m_cap, kNormWaves, kNormGrid), 64 * kNormWaves, 0, s>>>(a);
+    if (vec) return;
+    if (a.C <= kNarrow) k_norm_any<DT, 8><<<norm_grid(a.m_cap, kNormWaves * 8, kNormGrid), 64 * kNormWaves, 0, s>>>(a);
+    else k_norm_any<DT, 64><<<norm_grid(a.m_cap, kNormWaves, kNormGrid), 64 * kNormWaves, 0, s>>>(a);
 }
 void launch_layer_norm(hipStream_t s, const NormArgs& a) {
     if (a.dt == SPV_F32) norm_dt<SPV_F32>(s, a);
@@ -413,15 +420,19 @@ static void norm_bwd_dt(hipStream_t s, const NormBwdArgs& a, const NormWs& w) {
         k_norm_bwd<DT, L, NV><<<g, 64 * kNormWaves, 0, s>>>(a, sums ? w.part : nullptr);
     });
     if (!vec) {
+        const bool narrow = a.C <= kNarrow;
+        const unsigned g8 = norm_grid(a.m_cap, kNormWaves * 8, kNormGrid);
         g = norm_grid(a.m_cap, kNormWaves, kNormBwdGrid);
         if (sums) {
             // the statistics alone, then the column sums, then dx (which may overwrite dy)
             NormBwdArgs st = a;
             st.dx = nullptr;
-            k_norm_bwd_any<DT><<<g, 64 * kNormWaves, 0, s>>>(st, w.stat);
+            if (narrow) k_norm_bwd_any<DT, 8><<<g8, 64 * kNormWaves, 0, s>>>(st, w.stat);
+            else k_norm_bwd_any<DT, 64><<<g, 64 * kNormWaves, 0, s>>>(st, w.stat);
             k_norm_cols_any<DT><<<dim3(g, (unsigned)((a.C + 63) / 64)), 64 * kNormWaves, 0, s>>>(a, w.stat, w.part);
         }
-        if (a.dx) k_norm_bwd_any<DT><<<g, 64 * kNormWaves, 0, s>>>(a, nullptr);
+        if (a.dx && narrow) k_norm_bwd_any<DT, 8><<<g8, 64 * kNormWaves, 0, s>>>(a, nullptr);
+        else if (a.dx) k_norm_bwd_any<DT, 64><<<g, 64 * kNormWaves, 0, s>>>(a, nullptr);
     }
     if (sums && !(vec && g == 1))
         k_norm_join<<<(unsigned)((2 * a.C + 15) / 16), 1024, 0, s>>>(w.part, (int)g, a.C, a.dgamma, a.dbeta);
