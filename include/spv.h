@@ -626,8 +626,9 @@ typedef struct spv_attention_params {
  *   z_ij = scale * (q_i . k_j),  t_ij = cap > 0 ? cap * tanh(z_ij / cap) : z_ij,
  *   s_ij = t_ij - slopes[h] * (|dx| + |dy| + |dz|)   (d = c_i - c_j, the voxels' coordinates),
  *   out_i = sum_j p_ij v_j,  p_ij = exp(s_ij - lse_i),  lse_i = log sum_j exp(s_ij)
- * for each head h, j over the scan's keys.  A query whose scan has no key gets
- * out = 0 and lse = -inf.  With coordinates (b, i, 0, 0) the bias is the one of
+ * for each head h, j over the scan's keys.  A query whose scan has no key, or none
+ * whose score is above minus infinity, gets out = 0 and lse = -inf (and no
+ * gradient).  With coordinates (b, i, 0, 0) the bias is the one of
  * token distances in a sequence.  Softmax statistics and sums are float32; 16-bit
  * types multiply on matrix cores with the weights p rounded to the type.
  * In:  q [nq][ldq], k [nk][ldk], v [nk][ldv] (dt): row i, head h at

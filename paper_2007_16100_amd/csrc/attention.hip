@@ -22,6 +22,9 @@ namespace spv {
 // 211 x 3 heads in float32: 9.5 us a call.  In float32 the products (64 cycles each) bound it: [1457, 1544] x 3 heads,
 // cap and bias, 47 us, where 288 workgroups lie on 256 units.
 constexpr float kLead = 8.f;
+// the reference of a column without a finite score so far: one of minus infinity has no weight under it, and any finite
+// one passes it
+constexpr float kNoScore = -1e38f;
 
 // Waves per SIMD that the registers have to leave room for.  [8192] x 4 heads of 128 with two 217 us, with one 350;
 // [16384] x 8 heads of 32 with four 621 us, with three 685.
@@ -110,7 +113,7 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     f32x16 o[T::NB];
 #pragma unroll
     for (int b = 0; b < T::NB; ++b) o[b] = f32x16{};
-    float m = 0.f, l = 0.f;
+    float m = CAP ? 0.f : kNoScore, l = 0.f;  // capped scores are finite: theirs starts at the first rows' maximum
     if (t0 < t1) {
         store(0);
         if (t0 + 1 < t1) load();
@@ -152,13 +155,21 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
                 float d = z[u][0];
 #pragma unroll
                 for (int r = 1; r < 16; ++r) d = fmaxf(d, z[u][r]);
-                if constexpr (!CAP) d = fmaf(d, cs, -m);
-                if (first_rows || __any(d > kLead)) {
-                    d = half_max(d);
-                    const float up = first_rows || d > kLead ? d : 0.f;
-                    const float f = first_rows ? 1.f : __builtin_amdgcn_exp2f(-up);
-                    first_rows = false;
-                    m += up;
+                const float top = d;
+                if constexpr (!CAP) d = fmaf(top, cs, -m);
+                if ((CAP && first_rows) || __any(d > kLead)) {
+                    float up, f;
+                    if constexpr (CAP) {
+                        d = half_max(d);
+                        up = first_rows || d > kLead ? d : 0.f;
+                        f = first_rows ? 1.f : __builtin_amdgcn_exp2f(-up);
+                        first_rows = false;
+                        m += up;
+                    } else {
+                        const float to = half_max(top) * cs, now = to - m > kLead ? to : m;
+                        f = __builtin_amdgcn_exp2f(m - now);
+                        m = now;
+                    }
                     l *= f;
 #pragma unroll
                     for (int b = 0; b < T::NB; ++b)
@@ -223,8 +234,8 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
         if (l != 0.f) Tile<SPV_F32, DP>::store_cols(a.part, at * a.D, a.D, h, o, 1.f);  // else they are not read
         return;
     }
-    T::store_cols(a.out, qi * a.ldo + (int64_t)head * a.D, a.D, h, o, tiles ? 1.f / l : 0.f);
-    if (a.lse && h == 0) a.lse[row] = tiles ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    T::store_cols(a.out, qi * a.ldo + (int64_t)head * a.D, a.D, h, o, l != 0.f ? 1.f / l : 0.f);
+    if (a.lse && h == 0) a.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // The parts of a row joined under their largest reference: WR waves a row, a lane for each four channels of one of

@@ -34,6 +34,9 @@ struct Capped {
 template <bool CAP>
 constexpr float kBend = CAP ? 4.f : 1.f;
 
+// a row's lse in units of log 2, as the weights are formed from it: a row whose scores are all minus infinity has none
+__device__ inline float row_lse(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
 // Waves per SIMD that the registers have to leave room for: as many as cost no or few spills.  [8192] x 4 heads of 128,
 // dq with two 254 us, with one 421; [9000] x 8 heads of 96, forward and backward, with two in dk, dv 1908 us, with one
 // 2319; [4096] x 4 heads of 64 in float32 with two everywhere 1026 us, with one 773.
@@ -99,7 +102,7 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     // the first rows are asked for before anything waits for the columns'
     if (t0 < t1) load();
 
-    lse *= kLog2e;
+    lse = row_lse(lse);
 #pragma unroll
     for (int s = 0; s < T::NF; ++s) delta = T::frag_dot(df[s], of[s], delta);
     delta = half_sum(delta);
@@ -290,7 +293,7 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
         if (tid < KT) {
             // a row past the end has no weight: its lse counts as infinite
             const bool in = tid < got;
-            const float e = in ? kUp<DT> - rl * kLog2e : -INFINITY;
+            const float e = in ? kUp<DT> - row_lse(rl) : -INFINITY;
             lr[s][0][tid] = CAP ? e + capped.cap2 : e * inv_cs;
             lr[s][1][tid] = -rd;
             if constexpr (BIAS) lc.put(s, tid, cq, in, cube);
