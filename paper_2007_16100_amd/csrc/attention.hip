@@ -22,9 +22,28 @@ namespace spv {
 // 211 x 3 heads in float32: 9.5 us a call.  In float32 the products (64 cycles each) bound it: [1457, 1544] x 3 heads,
 // cap and bias, 47 us, where 288 workgroups lie on 256 units.
 constexpr float kLead = 8.f;
-// the reference of a column without a finite score so far: one of minus infinity has no weight under it, and any finite
-// one passes it
-constexpr float kNoScore = -1e38f;
+// A reference is base + m: base in the units that the products come in (of the scores, under a cap), m in units of log 2.
+// One of up to kNear is all in m, and weights are exp2(z cs - m) in one step.  A larger one is a base, the largest z
+// itself, and is taken off z first: rounded to a float, m = base cs would be off by more than the weights' range, the
+// same for every key but enough to overflow or lose them all.
+constexpr float kNear = 1024.f;
+// the base of a column without a finite score so far: one of minus infinity has no weight under it, and any finite one
+// passes it
+constexpr float kNoScore = -3.402823466e38f;
+// what sums under several references are joined under, from the largest (in units of log 2) and the largest base
+struct Reference {
+    float base, m;
+    __device__ Reference(float top, float top_base) {
+        const bool near = fabsf(top) <= kNear;
+        base = near ? 0.f : top_base;
+        m = near ? top : 0.f;
+    }
+    __device__ float factor(float b, float mm, float unit) const {
+        return __builtin_amdgcn_exp2f(fmaf(b - base, unit, mm - m));
+    }
+};
+// units of log 2 in one of the base's
+__device__ inline float attn_unit(const AttnArgs& a) { return a.cap > 0.f ? 1.f : a.scale * kLog2e; }
 
 // Waves per SIMD that the registers have to leave room for.  [8192] x 4 heads of 128 with two 217 us, with one 350;
 // [16384] x 8 heads of 32 with four 621 us, with three 685.
@@ -103,7 +122,7 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
             if (tid < KT) lc.put(s, tid, ck, tid < got, cube);
     };
 
-    // weights of scores (relative to m already under a cap)
+    // weights of scores (relative to m already under a cap) over their base
     auto weights = [](const f32x16& z, float cs, float m) __attribute__((always_inline)) {
         f32x16 p;
 #pragma unroll
@@ -113,13 +132,13 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     f32x16 o[T::NB];
 #pragma unroll
     for (int b = 0; b < T::NB; ++b) o[b] = f32x16{};
-    float m = CAP ? 0.f : kNoScore, l = 0.f;  // capped scores are finite: theirs starts at the first rows' maximum
+    float m = 0.f, base = kNoScore, l = 0.f;
+    bool based = true;  // a column of the wave has a base
     if (t0 < t1) {
         store(0);
         if (t0 + 1 < t1) load();
     }
     __syncthreads();
-    bool first_rows = true;
     for (int i = t0; i < t1; ++i) {
         const int s = (i - t0) & 1;
         const int row0 = RT * kw, left = keys - i * KT - row0;  // the wave's rows of the tile, keys from there on
@@ -152,24 +171,20 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
                     for (int r = 0; r < 16; ++r)
                         if (8 * (r / 4) + 4 * h + r % 4 >= end) z[u][r] = -INFINITY;
                 }
-                float d = z[u][0];
+                float top = z[u][0];
 #pragma unroll
-                for (int r = 1; r < 16; ++r) d = fmaxf(d, z[u][r]);
-                const float top = d;
-                if constexpr (!CAP) d = fmaf(top, cs, -m);
-                if ((CAP && first_rows) || __any(d > kLead)) {
-                    float up, f;
-                    if constexpr (CAP) {
-                        d = half_max(d);
-                        up = first_rows || d > kLead ? d : 0.f;
-                        f = first_rows ? 1.f : __builtin_amdgcn_exp2f(-up);
-                        first_rows = false;
-                        m += up;
-                    } else {
-                        const float to = half_max(top) * cs, now = to - m > kLead ? to : m;
-                        f = __builtin_amdgcn_exp2f(m - now);
-                        m = now;
+                for (int r = 1; r < 16; ++r) top = fmaxf(top, z[u][r]);
+                if (__any((CAP ? top - base : fmaf(top - base, cs, -m)) > kLead)) {
+                    top = half_max(top);
+                    const float past = CAP ? top - base : fmaf(top - base, cs, -m), old_m = m, old_base = base;
+                    if (past > kLead) {
+                        const float to = CAP ? top + m : top * cs;
+                        const bool near = fabsf(to) <= kNear;
+                        m = near ? to : 0.f;
+                        base = near ? 0.f : CAP ? to : top;
                     }
+                    const float f = __builtin_amdgcn_exp2f(fmaf(old_base - base, CAP ? 1.f : cs, old_m - m));
+                    based = __any(base != 0.f);
                     l *= f;
 #pragma unroll
                     for (int b = 0; b < T::NB; ++b)
@@ -177,7 +192,12 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
                         for (int r = 0; r < 16; ++r) o[b][r] *= f;
                     if constexpr (CAP)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) z[u][r] -= up;
+                        for (int r = 0; r < 16; ++r) z[u][r] += old_m - m;
+                }
+                if (based) {
+                    asm volatile("");  // a branch: it is hardly ever taken after the first rows
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) z[u][r] -= base;
                 }
                 const typename T::Weights w = weights(z[u], cs, m);
                 l = T::sum(w, l);
@@ -193,49 +213,56 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     l = half_sum(l);
     if constexpr (KW > 1) {
         // the waves of a block of columns join under their largest reference (the tiles' LDS is free by now)
-        static_assert(2 * KT * T::LD >= CW * (KW - 1) * (T::NB * 16 + 2) * 256, "a wave's sums have room");
-        constexpr int N = (T::NB * 16 + 2) * 64;
+        static_assert(2 * KT * T::LD >= CW * (KW - 1) * (T::NB * 16 + 3) * 256, "a wave's sums have room");
+        constexpr int N = (T::NB * 16 + 3) * 64;
         float* p = (float*)&lk[0][0] + (cw * (KW - 1) + kw - 1) * N;
         if (kw) {
-            lds_put(p + 128, lane, o);
+            lds_put(p + 192, lane, o);
             p[lane] = m;
             p[64 + lane] = l;
+            p[128 + lane] = base;
         }
         __syncthreads();
         if (kw) return;
         p += N;
-        float top = l != 0.f ? m : -INFINITY;
+        const float unit = CAP ? 1.f : cs;
+        float top = -INFINITY, top_base = kNoScore;
+        auto count = [&](float m, float l, float base) __attribute__((always_inline)) {
+            if (l != 0.f) top = fmaxf(top, fmaf(base, unit, m)), top_base = fmaxf(top_base, base);
+        };
+        count(m, l, base);
 #pragma unroll
-        for (int w = 1; w < KW; ++w)
-            if (p[(w - 1) * N + 64 + lane] != 0.f) top = fmaxf(top, p[(w - 1) * N + lane]);
-        const float f = l != 0.f ? __builtin_amdgcn_exp2f(m - top) : 0.f;
+        for (int w = 0; w < KW - 1; ++w) count(p[w * N + lane], p[w * N + 64 + lane], p[w * N + 128 + lane]);
+        const Reference to(top, top_base);
+        const float f = l != 0.f ? to.factor(base, m, unit) : 0.f;
         l *= f;
 #pragma unroll
         for (int b = 0; b < T::NB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[b][r] *= f;
 #pragma unroll
-        for (int w = 1; w < KW; ++w) {
-            const float* pw = p + (w - 1) * N;
+        for (int w = 0; w < KW - 1; ++w) {
+            const float* pw = p + w * N;
             const float lw = pw[64 + lane];
             if (lw == 0.f) continue;  // both lanes of a column: no key among the wave's
-            const float fw = __builtin_amdgcn_exp2f(pw[lane] - top);
+            const float fw = to.factor(pw[128 + lane], pw[lane], unit);
             l = fmaf(fw, lw, l);
-            lds_add(pw + 128, lane, fw, o);
+            lds_add(pw + 192, lane, fw, o);
         }
-        m = l != 0.f ? top : 0.f;
+        m = to.m, base = to.base;
     }
     if (!live) return;
     const int64_t row = qi * a.H + head;
     if (a.part) {
         // one of the parts: sums as they are, in float32
         const int64_t at = (int64_t)sh.part * a.nq * a.H + row;
-        if (h == 0) *(float2*)(a.part_ml + 2 * at) = make_float2(m, l);
+        if (h == 0) *(float4*)(a.part_ml + 4 * at) = make_float4(m, l, base, 0.f);
         if (l != 0.f) Tile<SPV_F32, DP>::store_cols(a.part, at * a.D, a.D, h, o, 1.f);  // else they are not read
         return;
     }
     T::store_cols(a.out, qi * a.ldo + (int64_t)head * a.D, a.D, h, o, l != 0.f ? 1.f / l : 0.f);
-    if (a.lse && h == 0) a.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if (a.lse && h == 0)
+        a.lse[row] = l != 0.f ? fmaf(base, CAP ? 1.f : cs, m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // The parts of a row joined under their largest reference: WR waves a row, a lane for each four channels of one of
@@ -249,12 +276,13 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int parts) {
     const int64_t rows = a.nq * a.H, row = (int64_t)blockIdx.x * RW + rw, qi = row / a.H;
     // a row of no scan has no parts
     const bool on = row < rows && qi >= a.q_off[0] && qi < a.q_off[a.B];
-    const float2* ml = (const float2*)a.part_ml + row;
-    float m = -INFINITY;
+    const float4* ml = (const float4*)a.part_ml + row;  // m, sum of weights, base
+    const float unit = attn_unit(a);
+    float m = -INFINITY, base = kNoScore;
     if (on)
         for (int s = lane + 64 * w; s < parts; s += 64 * WR) {
-            const float2 v = ml[s * rows];
-            if (v.y != 0.f) m = fmaxf(m, v.x);
+            const float4 v = ml[s * rows];
+            if (v.y != 0.f) m = fmaxf(m, fmaf(v.z, unit, v.x)), base = fmaxf(base, v.z);
         }
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
@@ -264,25 +292,37 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int parts) {
 #pragma unroll
         for (int x = 0; x < WR; ++x) m = fmaxf(m, sm[rw * WR + x]);
     }
+    if (fabsf(m) > kNear) {  // the same in all of a row's waves
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) base = fmaxf(base, __shfl_xor(base, x, 64));
+        if constexpr (WR > 1) {
+            __syncthreads();
+            if (lane == 0) sm[wave] = base;
+            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < WR; ++x) base = fmaxf(base, sm[rw * WR + x]);
+        }
+    }
+    const Reference to(m, base);
     const int d = lane % P4 * 4;
     float l = 0.f;
     float o[4] = {};
     if (on && d < a.D) {
         constexpr int U = 4;  // parts in flight
         for (int s0 = lane / P4 + 64 / P4 * w; s0 < parts; s0 += U * NP) {
-            float2 v[U];
+            float4 v[U];
             float4 p[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int s = s0 + u * NP;
-                v[u] = s < parts ? ml[s * rows] : make_float2(0.f, 0.f);
+                v[u] = s < parts ? ml[s * rows] : make_float4(0.f, 0.f, 0.f, 0.f);
                 // sums of no key are not written
                 p[u] = v[u].y != 0.f ? *(const float4*)(a.part + (s * rows + row) * a.D + d) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (v[u].y == 0.f) continue;
-                const float f = __builtin_amdgcn_exp2f(v[u].x - m);
+                const float f = to.factor(v[u].z, v[u].x, unit);
                 l = fmaf(f, v[u].y, l);
                 o[0] = fmaf(f, p[u].x, o[0]);
                 o[1] = fmaf(f, p[u].y, o[1]);
@@ -315,7 +355,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int parts) {
         *(float4*)((float*)a.out + at) = make_float4(o[0] * f, o[1] * f, o[2] * f, o[3] * f);
     else
         *(uint2*)((uint16_t*)a.out + at) = make_uint2(pack2<DT>(o[0] * f, o[1] * f), pack2<DT>(o[2] * f, o[3] * f));
-    if (a.lse && lane == 0) a.lse[row] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    if (a.lse && lane == 0)
+        a.lse[row] = l != 0.f ? fmaf(to.base, unit, to.m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
@@ -334,7 +375,7 @@ void plan_attention_ws(Arena& a, AttnArgs& t) {
     const AttnShape s = forward_shape(t);
     if (s.parts < 2) return;
     const size_t rows = (size_t)s.parts * (size_t)t.nq * (size_t)t.H;
-    t.part_ml = a.take<float>(2 * rows);
+    t.part_ml = a.take<float>(4 * rows);
     t.part = a.take<float>(rows * (size_t)t.D);
 }
 

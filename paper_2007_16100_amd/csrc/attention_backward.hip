@@ -34,8 +34,14 @@ struct Capped {
 template <bool CAP>
 constexpr float kBend = CAP ? 4.f : 1.f;
 
-// a row's lse in units of log 2, as the weights are formed from it: a row whose scores are all minus infinity has none
-__device__ inline float row_lse(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+// A row's lse in units of log 2, as the weights are formed from it.  A float32 holds it to 2^-24 of itself, and a weight
+// exp2(s - lse) is off by as much: past kMaxLse by a factor, up to overflow.  Such a row, and one whose scores are all
+// minus infinity, has no gradient.
+constexpr float kMaxLse = 4194304.f;  // 2^22
+__device__ inline float row_lse(float lse) {
+    const float e = lse * kLog2e;
+    return fabsf(e) > kMaxLse ? INFINITY : e;
+}
 
 // Waves per SIMD that the registers have to leave room for: as many as cost no or few spills.  [8192] x 4 heads of 128,
 // dq with two 254 us, with one 421; [9000] x 8 heads of 96, forward and backward, with two in dk, dv 1908 us, with one

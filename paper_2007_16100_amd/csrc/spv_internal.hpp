@@ -496,7 +496,7 @@ struct AttnArgs {
     void* out;                  // [nq][ldo]; the backward's input
     float* lse;                 // [nq][H] or nullptr
     float* part;                // [parts][nq][H][D] sums of the keys' parts, or nullptr: the keys are in one part
-    float* part_ml;             // [parts][nq][H][2] their reference and sum of weights
+    float* part_ml;             // [parts][nq][H][4] their m, sum of weights and base
     // backward
     const void* dout;           // [nq][lddo]
     void *dq, *dk, *dv;         // [n][lddq / lddk / lddv]

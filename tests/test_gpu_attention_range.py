@@ -100,3 +100,65 @@ def test_infinite_keys_and_rows_without_a_finite_score(spv, nq, nk, dtype):
     k[..., 0] = float("-inf")
     got = run(spv, q, k, v)
     assert not got["out"].any() and bool((got["lse"] == -float("inf")).all())
+
+
+# -- large scores --------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+@pytest.mark.parametrize("slope", [2.0 ** 4, 2.0 ** 9, 2.0 ** 17, 2.0 ** 20])
+@pytest.mark.parametrize("nq,nk", [(33, 700), (1, 6000), (300, 40)])
+def test_tokens_far_from_every_key(spv, nq, nk, slope, cap, dtype):
+    """Distances of some ten thousand under steep slopes: only the nearest keys have weight, each as much.  The scores are
+    products of zero minus a distance, equal where the distances are, so the mean of the nearest keys' values is exact
+    but for its own roundings; gradients are finite."""
+    print(f"{nq}x{nk} slope={slope} cap={cap} {dtype}", flush=True)
+    g = torch.Generator().manual_seed(11)
+    q, k = torch.zeros(nq, 2, 32, dtype=TD[dtype]).cuda(), rnd(1, nk, 2, 32, dtype=dtype)
+    v, do = rnd(2, nk, 2, 32, dtype=dtype), rnd(3, nq, 2, 32, dtype=dtype)
+    kc = torch.randint(-30, 30, (nk, 4), generator=g).to(torch.int32).cuda()
+    qc = torch.randint(-30, 30, (nq, 4), generator=g).to(torch.int32).cuda()
+    qc[:, 1] += 20000
+    qc[:, 2] -= 30000
+    got = run(spv, q, k, v, do, cap=cap, scale=1.0, q_coords=qc, k_coords=kc, slopes=torch.tensor([slope, slope]).cuda())
+    dist = np.abs(arr(qc)[:, None, 1:] - arr(kc)[None, :, 1:]).sum(-1)
+    near = (dist == dist.min(1, keepdims=True)).astype(np.float64)
+    V = arr(v)
+    want = np.einsum("ij,jhd->ihd", near / near.sum(1, keepdims=True), V)
+    # equal weights, so their rounding cancels; e^-16 = 1e-7 of each key a step further off
+    n = nk * 2e-7 * (slope < 100) + (np.log2(nk) + 8) * EPS
+    tol = ref.UNIT[dtype] * np.abs(want) + n * np.abs(V).max()
+    assert not np.isnan(arr(got["out"])).any() and np.all(np.abs(arr(got["out"]) - want) <= tol)
+    lse = -slope * dist.min(1) + np.log(near.sum(1))
+    assert np.all(np.abs(arr(got["lse"]) - lse[:, None]) <= 4 * EPS * np.abs(lse[:, None]) + 1e-3)
+    for name in ("dq", "dk", "dv"):
+        assert bool(torch.isfinite(got[name].float()).all()), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("scale", [64.0, 4096.0, 1e6, 1e9])
+@pytest.mark.parametrize("nq,nk,climb", [(40, 500, False), (40, 500, True), (1, 6000, True), (300, 70, True)])
+def test_large_scales(spv, nq, nk, climb, scale, dtype):
+    """Products of small whole numbers times a large scale: the keys with the largest product have all the weight, however
+    often the largest so far moves up (climb: keys in ascending order)."""
+    print(f"{nq}x{nk} scale={scale} climb={climb} {dtype}", flush=True)
+    g = torch.Generator().manual_seed(12)
+    q = torch.randint(1, 3, (nq, 1, 32), generator=g).to(TD[dtype]).cuda()
+    k = torch.randint(-2, 3, (nk, 1, 32), generator=g).to(TD[dtype]).cuda()
+    if climb:
+        k = torch.randint(0, 2, (nk, 1, 32), generator=g).float().cuda()
+        k += torch.arange(nk, device="cuda").div(64, rounding_mode="floor")[:, None, None] - 3.0
+        k = k.to(TD[dtype])
+    v, do = rnd(2, nk, 1, 32, dtype=dtype), rnd(3, nq, 1, 32, dtype=dtype)
+    got = run(spv, q, k, v, do, scale=scale)
+    z = np.einsum("ihd,jhd->ij", arr(q), arr(k))
+    top = (z == z.max(1, keepdims=True)).astype(np.float64)
+    V = arr(v)
+    want = np.einsum("ij,jhd->ihd", top / top.sum(1, keepdims=True), V)
+    tol = ref.UNIT[dtype] * np.abs(want) + (np.log2(nk) + 8) * EPS * np.abs(V).max()
+    assert not np.isnan(arr(got["out"])).any() and np.all(np.abs(arr(got["out"]) - want) <= tol)
+    # finite wherever the definition's gradient, of some hundred times the scale, is in the type's range
+    want = ref.attention(arr(q), arr(k), V, [0, nq], [0, nk], scale, dout=arr(do))
+    for name in ("dq", "dk", "dv"):
+        held = torch.from_numpy(np.abs(want[name]) < 0.5 * torch.finfo(TD[dtype]).max)
+        assert bool(torch.isfinite(got[name].float().cpu()[held]).all()), name
