@@ -641,6 +641,8 @@ typedef struct spv_attention_params {
  *      ws: spv_attention_workspace_bytes(p, nq, nk, dt) bytes, 256-byte aligned
  *      (NULL where that is 0): few queries split their keys over the chip, and the
  *      parts are joined from there in a fixed order.
+ * A capped score is off by 2^-22 cap at most up to a cap of 8 (f32) or 64 (16-bit),
+ * beyond that by 2^-21 of itself, so a cap far above the scores changes nothing.
  * Errors: SPV_ERR_INVALID_ARG (null or misaligned pointers, sizes, strides, scale,
  *      cap, aliasing), SPV_ERR_UNSUPPORTED (D; over 2^22 workgroups of 32 rows),
  *      SPV_ERR_CAPACITY (ws too small).

@@ -49,7 +49,7 @@ __device__ inline float attn_unit(const AttnArgs& a) { return a.cap > 0.f ? 1.f 
 // [16384] x 8 heads of 32 with four 621 us, with three 685.
 constexpr int attn_waves(int dt, int DP) { return dt == SPV_F32 || DP > 64 ? 2 : 4; }
 
-template <int DT, int DP, int KW, bool BIAS, bool CAP>
+template <int DT, int DP, int KW, bool BIAS, int CAP>
 __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     using T = Tile<DT, DP>;
     constexpr int RT = attn_rows(DT, DP, KW), KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
@@ -73,8 +73,8 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     const int64_t qi = t.first + q0 + x / G;
     uint4 qf[T::NF];
     T::load_cols(a.q, qi * a.ldq + (int64_t)head * a.D, live, a.D, h, qf);
-    const float cs = in_vgpr(a.scale * kLog2e), cz = in_vgpr(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f);
-    const float cap2 = a.cap * kLog2e, fall = in_vgpr(-2.f * cap2);
+    const float cs = in_vgpr(a.scale * kLog2e);
+    const Capped<CAP> capped(a);
     int4 qc{0, 0, 0, 0};
     float slope = 0.f;  // of the scores where there is a cap, else of the products
     if constexpr (BIAS)
@@ -154,10 +154,8 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
             }
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
-                // cap tanh(w) = cap - 2 cap / (exp(2 w) + 1), to an absolute error of 2^-22 cap
                 auto bend = [&](int r, float b) __attribute__((always_inline)) {
-                    const float ex = __builtin_amdgcn_exp2f(z[u][r] * cz);
-                    z[u][r] = fmaf(fall, __builtin_amdgcn_rcpf(ex + 1.f), b + (cap2 - m));
+                    z[u][r] = capped(z[u][r], b + (capped.lift - m));
                 };
                 if constexpr (CAP && BIAS)
                     lc.bias(s, row0 + 32 * u, h, far, place, slope, lift, bend);
@@ -382,10 +380,13 @@ void plan_attention_ws(Arena& a, AttnArgs& t) {
 template <int DT, int DP, int KW>
 static void attn_launch(hipStream_t s, const AttnArgs& a, const AttnShape& sh) {
     const dim3 g = attn_grid(sh, a.K);
-    if (a.slopes && a.cap > 0.f) k_attn<DT, DP, KW, true, true><<<g, 256, 0, s>>>(a);
-    else if (a.slopes) k_attn<DT, DP, KW, true, false><<<g, 256, 0, s>>>(a);
-    else if (a.cap > 0.f) k_attn<DT, DP, KW, false, true><<<g, 256, 0, s>>>(a);
-    else k_attn<DT, DP, KW, false, false><<<g, 256, 0, s>>>(a);
+    const int cap = attn_cap(a);
+    if (a.slopes && cap == kCapQuick) k_attn<DT, DP, KW, true, kCapQuick><<<g, 256, 0, s>>>(a);
+    else if (a.slopes && cap) k_attn<DT, DP, KW, true, kCapExact><<<g, 256, 0, s>>>(a);
+    else if (a.slopes) k_attn<DT, DP, KW, true, kNoCap><<<g, 256, 0, s>>>(a);
+    else if (cap == kCapQuick) k_attn<DT, DP, KW, false, kCapQuick><<<g, 256, 0, s>>>(a);
+    else if (cap) k_attn<DT, DP, KW, false, kCapExact><<<g, 256, 0, s>>>(a);
+    else k_attn<DT, DP, KW, false, kNoCap><<<g, 256, 0, s>>>(a);
 }
 template <int DT, int DP>
 static void attn_dp_launch(hipStream_t s, const AttnArgs& a, const AttnShape& sh) {

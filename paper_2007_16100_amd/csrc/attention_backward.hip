@@ -19,21 +19,6 @@
 
 namespace spv {
 
-// d score / d product, over scale and kBend, and the score itself from a product under a cap
-struct Capped {
-    float cz, cap2, fall;
-    __device__ explicit Capped(const AttnArgs& a)
-        : cz(in_vgpr(2.f * kLog2e * a.scale / a.cap)), cap2(a.cap * kLog2e), fall(in_vgpr(-2.f * cap2)) {}
-    // t = tanh(w) = 1 - 2 r with r = 1 / (exp(2 w) + 1): 1 - t^2 = 4 (r - r^2)
-    __device__ float operator()(float y, float rest, float& x) const {
-        const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * cz) + 1.f);
-        x = fmaf(fall, r, rest);
-        return fmaf(-r, r, r);
-    }
-};
-template <bool CAP>
-constexpr float kBend = CAP ? 4.f : 1.f;
-
 // A row's lse in units of log 2, as the weights are formed from it.  A float32 holds it to 2^-24 of itself, and a weight
 // exp2(s - lse) is off by as much: past kMaxLse by a factor, up to overflow.  Such a row, and one whose scores are all
 // minus infinity, has no gradient.
@@ -51,7 +36,7 @@ constexpr int dkv_waves(int dt, int DP, int KW) {
     return dt == SPV_F32 ? (DP > 32 ? 1 : 2) : DP > 96 || (DP > 64 && KW > 1) ? 1 : DP > 32 ? 2 : 3;
 }
 
-template <int DT, int DP, int KW, bool BIAS, bool CAP>
+template <int DT, int DP, int KW, bool BIAS, int CAP>
 __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     using T = Tile<DT, DP>;
     constexpr int RT = attn_rows(DT, DP, KW), KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
@@ -125,7 +110,7 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     }
     const float lift = slope * 8388608.f;
     const float cs = in_vgpr(a.scale * kLog2e);
-    const Capped capped(a);
+    const Capped<CAP> capped(a);
     f32x16 dref;
 #pragma unroll
     for (int r = 0; r < 16; ++r) dref[r] = -delta;
@@ -162,8 +147,8 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
             for (int u = 0; u < KS; ++u) {
                 auto grad = [&](int r, float b) __attribute__((always_inline)) {
                     if constexpr (CAP) {
-                        float x;
-                        const float bend = capped(z[u][r], b + (capped.cap2 - lse), x);
+                        float bend;
+                        const float x = capped(z[u][r], b + (capped.lift - lse), &bend);
                         z[u][r] = __builtin_amdgcn_exp2f(x) * d[u][r] * bend;
                     } else {
                         z[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], cs, -lse)) * d[u][r];
@@ -216,7 +201,7 @@ template <int DT>
 constexpr float kUp = DT == SPV_F16 ? 12.f : 0.f;
 
 // Columns are keys; the rows are the scan's queries, once for each head of the key head's group, in that order.
-template <int DT, int DP, int KW, bool BIAS, bool CAP>
+template <int DT, int DP, int KW, bool BIAS, int CAP>
 __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArgs a) {
     using T = Tile<DT, DP>;
     constexpr int RT = 32, KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
@@ -283,7 +268,7 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
     if (t0 < t1) load();
 
     const float cs = in_vgpr(a.scale * kLog2e), inv_cs = 1.f / cs;
-    const Capped capped(a);
+    const Capped<CAP> capped(a);
     Words far{0, 0};
     uint32_t place = 0;
     Cube cube{};
@@ -300,7 +285,7 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
             // a row past the end has no weight: its lse counts as infinite
             const bool in = tid < got;
             const float e = in ? kUp<DT> - row_lse(rl) : -INFINITY;
-            lr[s][0][tid] = CAP ? e + capped.cap2 : e * inv_cs;
+            lr[s][0][tid] = CAP ? e + capped.lift : e * inv_cs;
             lr[s][1][tid] = -rd;
             if constexpr (BIAS) lc.put(s, tid, cq, in, cube);
         }
@@ -340,8 +325,8 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
                 f32x16 p;
                 auto grad = [&](int r, float b) __attribute__((always_inline)) {
                     if constexpr (CAP) {
-                        float x;
-                        const float bend = capped(z[u][r], b + rest[CAP ? u : 0][r], x);
+                        float bend;
+                        const float x = capped(z[u][r], b + rest[CAP ? u : 0][r], &bend);
                         p[r] = __builtin_amdgcn_exp2f(x);
                         z[u][r] = p[r] * d[u][r] * bend;
                     } else {
@@ -434,7 +419,7 @@ void plan_attention_backward_ws(Arena& a, AttnArgs& t) {
     if (pq || pk) t.part = a.take<float>(pq > pk ? pq : pk);
 }
 
-template <int DT, int DP, int KW, bool BIAS, bool CAP>
+template <int DT, int DP, int KW, bool BIAS, int CAP>
 static void launch_side(hipStream_t s, const AttnArgs& a, const AttnShape& sh, bool keys) {
     const dim3 g = attn_grid(sh, a.K);
     if (keys) k_attn_dkv<DT, DP, KW, BIAS, CAP><<<g, 256, 0, s>>>(a);
@@ -442,10 +427,13 @@ static void launch_side(hipStream_t s, const AttnArgs& a, const AttnShape& sh, b
 }
 template <int DT, int DP, int KW>
 static void launch_kw(hipStream_t s, const AttnArgs& a, const AttnShape& sh, bool keys) {
-    if (a.slopes && a.cap > 0.f) launch_side<DT, DP, KW, true, true>(s, a, sh, keys);
-    else if (a.slopes) launch_side<DT, DP, KW, true, false>(s, a, sh, keys);
-    else if (a.cap > 0.f) launch_side<DT, DP, KW, false, true>(s, a, sh, keys);
-    else launch_side<DT, DP, KW, false, false>(s, a, sh, keys);
+    const int cap = attn_cap(a);
+    if (a.slopes && cap == kCapQuick) launch_side<DT, DP, KW, true, kCapQuick>(s, a, sh, keys);
+    else if (a.slopes && cap) launch_side<DT, DP, KW, true, kCapExact>(s, a, sh, keys);
+    else if (a.slopes) launch_side<DT, DP, KW, true, kNoCap>(s, a, sh, keys);
+    else if (cap == kCapQuick) launch_side<DT, DP, KW, false, kCapQuick>(s, a, sh, keys);
+    else if (cap) launch_side<DT, DP, KW, false, kCapExact>(s, a, sh, keys);
+    else launch_side<DT, DP, KW, false, kNoCap>(s, a, sh, keys);
 }
 template <int DT, int DP>
 static void launch_dp(hipStream_t s, const AttnArgs& a, const AttnShape& sh, bool keys) {

@@ -368,6 +368,48 @@ struct Tile {
     }
 };
 
+// Scores under a cap, cap tanh(w) with w = scale z / cap, and 4 / kBend of their slope 1 - tanh(w)^2.
+// kCapQuick: tanh(w) = 1 - 2 r, r = 1 / (exp(2 w) + 1), slope 4 (r - r^2).  Near zero it cancels: a score is off by 2^-22
+// cap whatever its size.  In 16-bit types that is 1.5e-5 at a cap of 64, a thirtieth of float16's half step; in float32
+// 2e-6 at 8, as much as the other roundings of a score (cap 5, [1457, 1544] x 3 heads: out is off by 4.5e-7, as by 4.7e-7
+// with the exact form, and a training step takes 175 us, 208 with that).
+// kCapExact, for larger caps: with e = exp(-2 |w|), |tanh(w)| = (1 - e) / (1 + e) and slope 4 e / (1 + e)^2; below a
+// quarter, where 1 - e cancels, an odd polynomial (through three nodes of Chebyshev's in w^2; 1e-8).  Off by 5 2^-24
+// of itself at most, for eleven more instructions a score.
+constexpr int kNoCap = 0, kCapQuick = 1, kCapExact = 2;
+constexpr float quick_cap(int dt) { return dt == SPV_F32 ? 8.f : 64.f; }
+inline int attn_cap(const AttnArgs& a) {
+    return !(a.cap > 0.f) ? kNoCap : a.cap <= quick_cap(a.dt) ? kCapQuick : kCapExact;
+}
+template <int CAP>
+constexpr float kBend = CAP ? 4.f : 1.f;
+template <int CAP>
+struct Capped {
+    float cz, cw, cap2, fall, lift;  // lift: what a score is added to beside its bias
+    __device__ explicit Capped(const AttnArgs& a) {
+        cw = a.scale / a.cap;
+        cz = in_vgpr((CAP == kCapQuick ? 2.f : -2.f) * kLog2e * cw);
+        cap2 = a.cap * kLog2e;
+        fall = in_vgpr(-2.f * cap2);
+        lift = CAP == kCapQuick ? cap2 : 0.f;
+    }
+    // the score of product z in units of log 2, added to rest (which has lift in it)
+    __device__ float operator()(float z, float rest, float* bend = nullptr) const {
+        if constexpr (CAP == kCapQuick) {
+            const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z * cz) + 1.f);
+            if (bend) *bend = fmaf(-r, r, r);
+            return fmaf(fall, r, rest);
+        } else {
+            const float w = z * cw, v = w * w, e = __builtin_amdgcn_exp2f(fabsf(z) * cz);
+            const float r = __builtin_amdgcn_rcpf(e + 1.f);
+            const float low = fmaf(w * v, fmaf(v, fmaf(v, -0.05197494f, 0.13328699f), -0.33333317f), w);
+            const float t = fabsf(w) < 0.25f ? low : copysignf((1.f - e) * r, w);
+            if (bend) *bend = e * r * r;
+            return fmaf(t, cap2, rest);
+        }
+    }
+};
+
 // the values of the lane's 16 of 32 rows, from LDS.  A product of the values with ones gives the same without the reads,
 // but two of those are a third of a tile's matrix cycles: dk and dv of [3451, 3654, 1963, 2195] x 8 heads of 32, 185 us
 // that way, 174 so.

@@ -52,6 +52,37 @@ def rms(got, want):
     return np.sqrt(((g - want) ** 2).sum() / (want ** 2).sum())
 
 
+# -- caps ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("nq,nk", [(70, 513), (3, 4000)])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("cap", [1.0, 20.0, 50.0, 80.0, 1e3, 1e4, 1e6])
+def test_a_caps_error_is_relative_to_the_score(spv, cap, bias, nq, nk, dtype):
+    """Scores of ordinary size under caps up to the largest: where a cap is far above them it changes nothing.
+
+    In float32 a weight takes a product of D steps (5 EPS in the root of the mean square), a tanh to a few EPS of scores
+    of a few units (5), an exponent of up to 16 rounded once or twice (8) and its exponential (1): 11 EPS together.  The
+    backward has lse's rounding too, and delta's.  In 16 bits the result's rounding is 0.5 u, that of the weights and of
+    the scores' gradients as much again."""
+    print(f"cap={cap} bias={bias} {nq}x{nk} {dtype}", flush=True)
+    q, k, v, do = (rnd(i, n, h, 32, dtype=dtype) for i, (n, h) in enumerate(((nq, 2), (nk, 1), (nk, 1), (nq, 2))))
+    kw = dict(cap=cap)
+    opt = [None, None, None]
+    if bias:
+        g = torch.Generator().manual_seed(5)
+        kw["q_coords"], kw["k_coords"] = (torch.randint(-9, 9, (n, 4), generator=g).to(torch.int32).cuda()
+                                          for n in (nq, nk))
+        kw["slopes"] = torch.tensor([0.0625, 0.03125]).cuda()
+        opt = [kw["q_coords"].cpu().numpy(), kw["k_coords"].cpu().numpy(), arr(kw["slopes"])]
+    got = run(spv, q, k, v, do, **kw)
+    want = ref.attention(arr(q), arr(k), arr(v), [0, nq], [0, nk], float(np.float32(32 ** -0.5)), cap, *opt, arr(do), dtype)
+    tol = 16 * EPS if dtype == "f32" else ref.UNIT[dtype]
+    for n in ("out", "dq", "dk", "dv"):
+        bound = tol if n == "out" or dtype != "f32" else 2 * tol
+        assert rms(got[n], want[n]) <= bound, (n, rms(got[n], want[n]) / bound)
+
+
 # -- scores of minus infinity ------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
