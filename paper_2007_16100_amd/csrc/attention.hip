@@ -10,7 +10,9 @@ namespace spv {
 // heads; a workgroup takes the columns of one scan and one key head.  Scores are kept in units of log 2.  A column's
 // reference m moves (and the sums are scaled) only when a score passes it by more than kLead: weights of up to
 // 2^kLead lose nothing in float32 sums or 16-bit weights, and after the first tiles m hardly ever moves.
-// The bias, over scale, is what the products are added to; a cap's tanh stands between them, so it is added after.
+// The bias, over scale, is what the products are added to, unless a cap's tanh stands between them or (float32) D roundings
+// at the bias's size would show: 400 voxels from every key, at a slope of a half, out was off by up to 7e-5 so, by 6e-6 with
+// the bias added after the product.
 //
 // In 16 bits at 32 channels a score costs two matrix products of 32 channels but seven vector instructions (distance,
 // bias, reference, exponential, maximum, sum, rounding), of which the exponential counts double: those bound it, not the
@@ -22,7 +24,8 @@ namespace spv {
 // 211 x 3 heads in float32: 9.5 us a call.  In float32 the products (64 cycles each) bound it: [1457, 1544] x 3 heads,
 // cap and bias, 47 us, where 288 workgroups lie on 256 units.
 constexpr float kLead = 8.f;
-// A reference is base + m: base in the units that the products come in (of the scores, under a cap), m in units of log 2.
+// A reference is base + m: base in the units that the products come in (of the scores, where the bias is added after), m in
+// units of log 2.
 // One of up to kNear is all in m, and weights are exp2(z cs - m) in one step.  A larger one is a base, the largest z
 // itself, and is taken off z first: rounded to a float, m = base cs would be off by more than the weights' range, the
 // same for every key but enough to overflow or lose them all.
@@ -43,7 +46,7 @@ struct Reference {
     }
 };
 // units of log 2 in one of the base's
-__device__ inline float attn_unit(const AttnArgs& a) { return a.cap > 0.f ? 1.f : a.scale * kLog2e; }
+__device__ inline float attn_unit(const AttnArgs& a) { return attn_after(a.dt, a.slopes, a.cap > 0.f) ? 1.f : a.scale * kLog2e; }
 
 // Waves per SIMD that the registers have to leave room for.  [8192] x 4 heads of 128 with two 217 us, with one 350;
 // [16384] x 8 heads of 32 with four 621 us, with three 685.
@@ -53,6 +56,7 @@ template <int DT, int DP, int KW, bool BIAS, int CAP>
 __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     using T = Tile<DT, DP>;
     constexpr int RT = attn_rows(DT, DP, KW), KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
+    constexpr bool AFTER = attn_after(DT, BIAS, CAP);  // z becomes the score, in units of log 2
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
     __shared__ __align__(16) Places<BIAS ? KT : 32> lc;
     __shared__ uint32_t box[4][3];
@@ -76,7 +80,7 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     const float cs = in_vgpr(a.scale * kLog2e);
     const Capped<CAP> capped(a);
     int4 qc{0, 0, 0, 0};
-    float slope = 0.f;  // of the scores where there is a cap, else of the products
+    float slope = 0.f;  // of the scores where the bias is added after, else of the products
     if constexpr (BIAS)
         if (live) {
             qc = *(const int4*)(a.q_coords + 4 * qi);
@@ -108,7 +112,7 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     Cube cube{};
     if constexpr (BIAS) {
         qc = voxel_clamp(qc);
-        slope = CAP ? slope * kLog2e : slope / a.scale;
+        slope = AFTER ? slope * kLog2e : slope / a.scale;
         cube = columns_cube(qc, live, box);
         cube.place(qc, place);
         far = voxel_words(qc);
@@ -122,11 +126,11 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
             if (tid < KT) lc.put(s, tid, ck, tid < got, cube);
     };
 
-    // weights of scores (relative to m already under a cap) over their base
+    // weights of scores (relative to m already where they are AFTER) over their base
     auto weights = [](const f32x16& z, float cs, float m) __attribute__((always_inline)) {
         f32x16 p;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(CAP ? z[r] : fmaf(z[r], cs, -m));
+        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(AFTER ? z[r] : fmaf(z[r], cs, -m));
         return T::weights(p);
     };
     f32x16 o[T::NB];
@@ -147,7 +151,7 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
                 f32x16 b{};
-                if constexpr (BIAS && !CAP)
+                if constexpr (BIAS && !AFTER)
                     lc.bias(s, row0 + 32 * u, h, far, place, slope, lift,
                             [&](int r, float x) __attribute__((always_inline)) { b[r] = x; });
                 z[u] = T::rows_dot(lk[s] + (row0 + 32 * u) * T::LD, lane, qf, b);
@@ -155,9 +159,9 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
                 auto bend = [&](int r, float b) __attribute__((always_inline)) {
-                    z[u][r] = capped(z[u][r], b + (capped.lift - m));
+                    z[u][r] = CAP ? capped(z[u][r], b + (capped.lift - m)) : fmaf(z[u][r], cs, b - m);
                 };
-                if constexpr (CAP && BIAS)
+                if constexpr (AFTER && BIAS)
                     lc.bias(s, row0 + 32 * u, h, far, place, slope, lift, bend);
                 else if constexpr (CAP)
 #pragma unroll
@@ -172,23 +176,23 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
                 float top = z[u][0];
 #pragma unroll
                 for (int r = 1; r < 16; ++r) top = fmaxf(top, z[u][r]);
-                if (__any((CAP ? top - base : fmaf(top - base, cs, -m)) > kLead)) {
+                if (__any((AFTER ? top - base : fmaf(top - base, cs, -m)) > kLead)) {
                     top = half_max(top);
-                    const float past = CAP ? top - base : fmaf(top - base, cs, -m), old_m = m, old_base = base;
+                    const float past = AFTER ? top - base : fmaf(top - base, cs, -m), old_m = m, old_base = base;
                     if (past > kLead) {
-                        const float to = CAP ? top + m : top * cs;
+                        const float to = AFTER ? top + m : top * cs;
                         const bool near = fabsf(to) <= kNear;
                         m = near ? to : 0.f;
-                        base = near ? 0.f : CAP ? to : top;
+                        base = near ? 0.f : AFTER ? to : top;
                     }
-                    const float f = __builtin_amdgcn_exp2f(fmaf(old_base - base, CAP ? 1.f : cs, old_m - m));
+                    const float f = __builtin_amdgcn_exp2f(fmaf(old_base - base, AFTER ? 1.f : cs, old_m - m));
                     based = __any(base != 0.f);
                     l *= f;
 #pragma unroll
                     for (int b = 0; b < T::NB; ++b)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) o[b][r] *= f;
-                    if constexpr (CAP)
+                    if constexpr (AFTER)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) z[u][r] += old_m - m;
                 }
@@ -223,7 +227,7 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
         __syncthreads();
         if (kw) return;
         p += N;
-        const float unit = CAP ? 1.f : cs;
+        const float unit = AFTER ? 1.f : cs;
         float top = -INFINITY, top_base = kNoScore;
         auto count = [&](float m, float l, float base) __attribute__((always_inline)) {
             if (l != 0.f) top = fmaxf(top, fmaf(base, unit, m)), top_base = fmaxf(top_base, base);
@@ -260,7 +264,7 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
     }
     T::store_cols(a.out, qi * a.ldo + (int64_t)head * a.D, a.D, h, o, l != 0.f ? 1.f / l : 0.f);
     if (a.lse && h == 0)
-        a.lse[row] = l != 0.f ? fmaf(base, CAP ? 1.f : cs, m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+        a.lse[row] = l != 0.f ? fmaf(base, AFTER ? 1.f : cs, m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
 // The parts of a row joined under their largest reference: WR waves a row, a lane for each four channels of one of

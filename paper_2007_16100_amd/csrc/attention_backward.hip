@@ -5,7 +5,8 @@
 // also forms delta), and dk, dv with the keys in the columns.  One kernel for all three would save two products of
 // seven, but either add dq in the order that workgroups happen to run in, or hold it for every part of the keys.
 // -delta is what the products dout . v are added to; the bias, over scale, or (keys in the columns) the rows' -lse are
-// what the products q . k are added to, unless a cap's tanh stands between.
+// what the products q . k are added to, unless a cap's tanh stands between or (float32) the roundings at their size of each
+// step of the product would show (dv of 300 x 300 heads of 128: 1.7e-6 that way, 5.7e-7 so).
 //
 // In 16 bits dz is rounded to the type before its two products, and out, which delta is formed of, comes in rounded:
 // dq and dk of bf16 are off by 2.6e-3 (root of the mean square against 64 bits), their own last rounding alone by 1.7e-3.
@@ -40,6 +41,7 @@ template <int DT, int DP, int KW, bool BIAS, int CAP>
 __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     using T = Tile<DT, DP>;
     constexpr int RT = attn_rows(DT, DP, KW), KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
+    constexpr bool AFTER = attn_after(DT, BIAS, CAP);
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
     __shared__ __align__(16) Places<BIAS ? KT : 32> lc;
     __shared__ uint32_t box[4][3];
@@ -64,7 +66,7 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     uint4 of[T::NF];
     T::load_cols(a.out, qi * a.ldo + (int64_t)head * a.D, live, a.D, h, of);
     int4 qc{0, 0, 0, 0};
-    float slope = 0.f;  // of the scores where there is a cap, else of the products
+    float slope = 0.f;  // of the scores where the bias is added after, else of the products
     if (live) {
         lse = a.lse[qi * a.H + head];
         if constexpr (BIAS) {
@@ -103,7 +105,7 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     Cube cube{};
     if constexpr (BIAS) {
         qc = voxel_clamp(qc);
-        slope = CAP ? slope * kLog2e : slope / a.scale;
+        slope = AFTER ? slope * kLog2e : slope / a.scale;
         cube = columns_cube(qc, live, box);
         cube.place(qc, place);
         far = voxel_words(qc);
@@ -138,7 +140,7 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
             for (int u = 0; u < KS; ++u) {
                 d[u] = T::rows_dot(lv[s] + (row0 + 32 * u) * T::LD, lane, df, dref);
                 f32x16 b{};
-                if constexpr (BIAS && !CAP)
+                if constexpr (BIAS && !AFTER)
                     lc.bias(s, row0 + 32 * u, h, far, place, slope, lift,
                             [&](int r, float x) __attribute__((always_inline)) { b[r] = x; });
                 z[u] = T::rows_dot(lk[s] + (row0 + 32 * u) * T::LD, lane, qf, b);
@@ -151,10 +153,10 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
                         const float x = capped(z[u][r], b + (capped.lift - lse), &bend);
                         z[u][r] = __builtin_amdgcn_exp2f(x) * d[u][r] * bend;
                     } else {
-                        z[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], cs, -lse)) * d[u][r];
+                        z[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], cs, AFTER ? b - lse : -lse)) * d[u][r];
                     }
                 };
-                if constexpr (CAP && BIAS)
+                if constexpr (AFTER && BIAS)
                     lc.bias(s, row0 + 32 * u, h, far, place, slope, lift, grad);
                 else
 #pragma unroll
@@ -205,6 +207,7 @@ template <int DT, int DP, int KW, bool BIAS, int CAP>
 __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArgs a) {
     using T = Tile<DT, DP>;
     constexpr int RT = 32, KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
+    constexpr bool AFTER = CAP || DT == SPV_F32;  // the row's -lse is added after the product
     __shared__ __align__(16) char lq[2][KT * T::LD], ld[2][KT * T::LD];
     __shared__ __align__(16) Places<BIAS ? KT : 32> lc;
     __shared__ uint32_t box[4][3];
@@ -285,7 +288,7 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
             // a row past the end has no weight: its lse counts as infinite
             const bool in = tid < got;
             const float e = in ? kUp<DT> - row_lse(rl) : -INFINITY;
-            lr[s][0][tid] = CAP ? e + capped.lift : e * inv_cs;
+            lr[s][0][tid] = CAP ? e + capped.lift : AFTER ? e : e * inv_cs;
             lr[s][1][tid] = -rd;
             if constexpr (BIAS) lc.put(s, tid, cq, in, cube);
         }
@@ -308,12 +311,12 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
                 slope = in_vgpr(a.slopes[kh * G + g_now] * kLog2e);
                 lift = slope * 8388608.f;
             }
-            f32x16 z[KS], d[KS], rest[CAP ? KS : 1];
+            f32x16 z[KS], d[KS], rest[AFTER ? KS : 1];
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
                 z[u] = row_values(&lr[s][0][row0 + 32 * u], h);
                 d[u] = row_values(&lr[s][1][row0 + 32 * u], h);
-                if constexpr (CAP) {
+                if constexpr (AFTER) {
                     rest[u] = z[u];
                     z[u] = f32x16{};
                 }
@@ -326,11 +329,12 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
                 auto grad = [&](int r, float b) __attribute__((always_inline)) {
                     if constexpr (CAP) {
                         float bend;
-                        const float x = capped(z[u][r], b + rest[CAP ? u : 0][r], &bend);
+                        const float x = capped(z[u][r], b + rest[AFTER ? u : 0][r], &bend);
                         p[r] = __builtin_amdgcn_exp2f(x);
                         z[u][r] = p[r] * d[u][r] * bend;
                     } else {
-                        p[r] = __builtin_amdgcn_exp2f(BIAS ? fmaf(z[u][r], cs, b) : z[u][r] * cs);
+                        const float y = AFTER ? (BIAS ? b + rest[u][r] : rest[u][r]) : b;
+                        p[r] = __builtin_amdgcn_exp2f(AFTER || BIAS ? fmaf(z[u][r], cs, y) : z[u][r] * cs);
                         z[u][r] = p[r] * d[u][r];
                     }
                     if constexpr (DT == SPV_F16) z[u][r] *= down;

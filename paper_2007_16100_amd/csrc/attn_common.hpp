@@ -381,6 +381,8 @@ constexpr float quick_cap(int dt) { return dt == SPV_F32 ? 8.f : 64.f; }
 inline int attn_cap(const AttnArgs& a) {
     return !(a.cap > 0.f) ? kNoCap : a.cap <= quick_cap(a.dt) ? kCapQuick : kCapExact;
 }
+// the bias is added after the product and what a cap makes of it, not what the product is added to
+__host__ __device__ constexpr bool attn_after(int dt, bool bias, bool cap) { return cap || (dt == SPV_F32 && bias); }
 template <int CAP>
 constexpr float kBend = CAP ? 4.f : 1.f;
 template <int CAP>

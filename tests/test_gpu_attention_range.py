@@ -193,3 +193,42 @@ def test_large_scales(spv, nq, nk, climb, scale, dtype):
     for name in ("dq", "dk", "dv"):
         held = torch.from_numpy(np.abs(want[name]) < 0.5 * torch.finfo(TD[dtype]).max)
         assert bool(torch.isfinite(got[name].float().cpu()[held]).all()), name
+
+
+# -- float32 -----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("nq,nk", [(50, 300), (2, 5000)])
+def test_float32_scores_far_below_zero(spv, nq, nk, D):
+    """Tokens some 400 voxels from every key, at a slope of a half: the scores' sums are rounded a constant number of times
+    at their size X (in units of log 2), not once for each of the product's D steps.  Three roundings of at most EPS X,
+    evenly spread, are EPS X in the root of the mean square, so 1.5 EPS X ln 2 of the weights, and the products' own."""
+    print(f"{nq}x{nk} D={D}", flush=True)
+    g = torch.Generator().manual_seed(13)
+    q, k, v, do = (rnd(i, n, 1, D) for i, n in enumerate((nq, nk, nk, nq)))
+    kc = torch.randint(-4, 4, (nk, 4), generator=g).to(torch.int32).cuda()
+    qc = torch.randint(-4, 4, (nq, 4), generator=g).to(torch.int32).cuda()
+    qc[:, 1] += 400
+    slopes = torch.tensor([0.5]).cuda()
+    got = run(spv, q, k, v, do, q_coords=qc, k_coords=kc, slopes=slopes)
+    want = ref.attention(arr(q), arr(k), arr(v), [0, nq], [0, nk], float(np.float32(D ** -0.5)), 0.0, qc.cpu().numpy(),
+                         kc.cpu().numpy(), arr(slopes), arr(do))
+    X = 200 * 1.4427
+    bound = 1.5 * EPS * X * np.log(2.0) + 16 * EPS
+    for n in ("out", "dq", "dk", "dv"):
+        print(n, rms(got[n], want[n]) / EPS, bound / EPS, flush=True)
+    assert rms(got["out"], want["out"]) <= bound
+    for n in ("dq", "dk", "dv"):  # lse is rounded at that size too
+        assert rms(got[n], want[n]) <= 1.5 * bound, n
+
+
+@pytest.mark.parametrize("nq,nk", [(300, 300), (700, 3)])
+def test_float32_gradients_without_a_bias(spv, nq, nk):
+    """dv of heads of 128 channels: the weights' exponents, up to 16, are rounded three times (11 EPS), their products
+    5 EPS, sums of some hundred rows 9."""
+    q, k, v, do = (rnd(i, n, 1, 128) for i, n in enumerate((nq, nk, nk, nq)))
+    got = run(spv, q, k, v, do)
+    want = ref.attention(arr(q), arr(k), arr(v), [0, nq], [0, nk], float(np.float32(128 ** -0.5)), dout=arr(do))
+    for n in ("out", "dq", "dk", "dv"):
+        print(n, rms(got[n], want[n]) / EPS, flush=True)
+    assert rms(got["dv"], want["dv"]) <= 24 * EPS
