@@ -9,7 +9,8 @@ namespace spv {
 // Columns are (query, head of a key head's group) pairs, so shared key heads are staged once for all of their query
 // heads; a workgroup takes the columns of one scan and one key head.  Scores are kept in units of log 2.  A column's
 // reference m moves (and the sums are scaled) only when a score passes it by more than kLead: weights of up to
-// 2^kLead lose nothing in float32 sums or 16-bit weights, and after the first tiles m hardly ever moves.
+// 2^kLead lose nothing in float32 sums or 16-bit weights, and after the first tiles m hardly ever moves.  It moves to kLift
+// below the score: in float16 the largest weights are 2^7 to 2^15, and those of 2^-21 of the largest still normal numbers.
 // The bias, over scale, is what the products are added to, unless a cap's tanh stands between them or (float32) D roundings
 // at the bias's size would show: 400 voxels from every key, at a slope of a half, out was off by up to 7e-5 so, by 6e-6 with
 // the bias added after the product.
@@ -23,7 +24,10 @@ namespace spv {
 // and three more instructions.  One query over 88,119 keys x 8 heads of 32: 18 us in 64 parts, 3.8 TB/s with the join.
 // 211 x 3 heads in float32: 9.5 us a call.  In float32 the products (64 cycles each) bound it: [1457, 1544] x 3 heads,
 // cap and bias, 47 us, where 288 workgroups lie on 256 units.
-constexpr float kLead = 8.f;
+template <int DT>
+constexpr float kLead = DT == SPV_F16 ? 15.f : 8.f;
+template <int DT>
+constexpr float kLift = DT == SPV_F16 ? 7.f : 0.f;
 // A reference is base + m: base in the units that the products come in (of the scores, where the bias is added after), m in
 // units of log 2.
 // One of up to kNear is all in m, and weights are exp2(z cs - m) in one step.  A larger one is a base, the largest z
@@ -37,10 +41,11 @@ constexpr float kNoScore = -3.402823466e38f;
 struct Reference {
     float base, m;
     __device__ Reference(float top, float top_base) {
-        const bool near = fabsf(top) <= kNear;
-        base = near ? 0.f : top_base;
-        m = near ? top : 0.f;
+        base = far(top) ? top_base : 0.f;
+        m = far(top) ? 0.f : top;
     }
+    // no reference without a base is as large, lifted or not
+    static __device__ bool far(float top) { return !(fabsf(top) <= 2.f * kNear); }
     __device__ float factor(float b, float mm, float unit) const {
         return __builtin_amdgcn_exp2f(fmaf(b - base, unit, mm - m));
     }
@@ -176,13 +181,13 @@ __global__ __launch_bounds__(256, attn_waves(DT, DP)) void k_attn(AttnArgs a) {
                 float top = z[u][0];
 #pragma unroll
                 for (int r = 1; r < 16; ++r) top = fmaxf(top, z[u][r]);
-                if (__any((AFTER ? top - base : fmaf(top - base, cs, -m)) > kLead)) {
+                if (__any((AFTER ? top - base : fmaf(top - base, cs, -m)) > kLead<DT>)) {
                     top = half_max(top);
                     const float past = AFTER ? top - base : fmaf(top - base, cs, -m), old_m = m, old_base = base;
-                    if (past > kLead) {
+                    if (past > kLead<DT>) {
                         const float to = AFTER ? top + m : top * cs;
                         const bool near = fabsf(to) <= kNear;
-                        m = near ? to : 0.f;
+                        m = near ? to - kLift<DT> : 0.f;
                         base = near ? 0.f : AFTER ? to : top;
                     }
                     const float f = __builtin_amdgcn_exp2f(fmaf(old_base - base, AFTER ? 1.f : cs, old_m - m));
@@ -294,7 +299,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int parts) {
 #pragma unroll
         for (int x = 0; x < WR; ++x) m = fmaxf(m, sm[rw * WR + x]);
     }
-    if (fabsf(m) > kNear) {  // the same in all of a row's waves
+    if (Reference::far(m)) {  // the same in all of a row's waves
 #pragma unroll
         for (int x = 32; x > 0; x >>= 1) base = fmaxf(base, __shfl_xor(base, x, 64));
         if constexpr (WR > 1) {

@@ -232,3 +232,25 @@ def test_float32_gradients_without_a_bias(spv, nq, nk):
     for n in ("out", "dq", "dk", "dv"):
         print(n, rms(got[n], want[n]) / EPS, flush=True)
     assert rms(got["dv"], want["dv"]) <= 24 * EPS
+
+
+# -- float16 -----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("nq", [1, 40])
+@pytest.mark.parametrize("nk", [3000, 60000])
+@pytest.mark.parametrize("score", [-12.0, -15.0, -17.5])
+def test_f16_many_small_weights(spv, score, nk, nq):
+    """One key at score 0 and thousands far below it: their weights, e^-17.5 each, are counted together.  Rounding one to
+    float16 is off by 2^-11 of itself or, below the normal numbers, by 2^-25 of the largest that fits; the largest here
+    is multiplied as 2^7 or more."""
+    print(f"{nq}x{nk} score={score}", flush=True)
+    q, k = torch.zeros(nq, 1, 32).half().cuda(), torch.zeros(nk, 1, 32).half().cuda()
+    q[..., 0] = 1.0
+    k[1:, :, 0] = score
+    v = torch.ones(nk, 1, 32).half().cuda()
+    v[0] = 0.0
+    got = run(spv, q, k, v, scale=1.0)
+    w = (nk - 1) * np.exp(score)
+    want = w / (1 + w)
+    tol = (nk - 1) * 2.0 ** -32 + 2.0 ** -11 * want * 2 + 2.0 ** -24
+    assert np.all(np.abs(arr(got["out"]) - want) <= tol), (float(arr(got["out"]).mean()), want, tol)
