@@ -37,6 +37,42 @@ constexpr int dkv_waves(int dt, int DP, int KW) {
     return dt == SPV_F32 ? (DP > 32 ? 1 : 2) : DP > 96 || (DP > 64 && KW > 1) ? 1 : DP > 32 ? 2 : 3;
 }
 
+// Float16 holds dz neither where weights are small (below 6e-5 in fewer than eleven bits, below 3e-8 not at all) nor where
+// dout . v passes 65,504.  So a column's dz are multiplied as 2^up dz, and its sums scaled back at the end: up is lowered,
+// and the sums so far with it, whenever one passes 2^15, to leave the largest at 2^8.  It starts where the first rows
+// lower it, unless all of them are below 2^-45.  Finding the largest takes a tenth of a training step: 310 -> 341 us at
+// [3451, 3654, 1963, 2195] x 8 heads of 32, and dq of 60 queries over 6720 keys at dout of 1e-4 was off by 8e-2
+// without it, where rounding the exact result gives 8e-3, as now.
+constexpr int kUpMost = 60;
+// true: up of some column of the wave was lowered
+template <int N>
+__device__ inline bool lower(f32x16& z, f32x16 (&o)[N], int& up) {
+    float top = fabsf(z[0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, fabsf(z[r]));
+    if (!__any(top > 32768.f)) return false;
+    top = half_max(top);
+    int by = top > 32768.f ? (int)(__float_as_uint(top) >> 23) - 127 - 8 : 0;
+    if (by > up + 200) by = up + 200;  // infinities stay what they are
+    const float f = __builtin_amdgcn_ldexpf(1.f, -by);
+    up -= by;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z[r] *= f;
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[b][r] *= f;
+    return true;
+}
+template <int N>
+__device__ inline void scale_back(f32x16 (&o)[N], int up) {
+    const float f = __builtin_amdgcn_ldexpf(1.f, -up);
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[b][r] *= f;
+}
+
 template <int DT, int DP, int KW, bool BIAS, int CAP>
 __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     using T = Tile<DT, DP>;
@@ -113,6 +149,8 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     const float lift = slope * 8388608.f;
     const float cs = in_vgpr(a.scale * kLog2e);
     const Capped<CAP> capped(a);
+    int up = DT == SPV_F16 ? kUpMost : 0;
+    float rest = (float)up - lse;  // what a weight's exponent is beside the score
     f32x16 dref;
 #pragma unroll
     for (int r = 0; r < 16; ++r) dref[r] = -delta;
@@ -150,10 +188,10 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
                 auto grad = [&](int r, float b) __attribute__((always_inline)) {
                     if constexpr (CAP) {
                         float bend;
-                        const float x = capped(z[u][r], b + (capped.lift - lse), &bend);
+                        const float x = capped(z[u][r], b + (capped.lift + rest), &bend);
                         z[u][r] = __builtin_amdgcn_exp2f(x) * d[u][r] * bend;
                     } else {
-                        z[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], cs, AFTER ? b - lse : -lse)) * d[u][r];
+                        z[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], cs, AFTER ? b + rest : rest)) * d[u][r];
                     }
                 };
                 if constexpr (AFTER && BIAS)
@@ -168,6 +206,8 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
                     for (int r = 0; r < 16; ++r)
                         if (8 * (r / 4) + 4 * h + r % 4 >= end) z[u][r] = 0.f;
                 }
+                if constexpr (DT == SPV_F16)
+                    if (lower(z[u], o, up)) rest = (float)up - lse;
                 T::add_weighted(lk[s] + (row0 + 32 * u) * T::LD, lane, T::weights(z[u]), o);
             }
         }
@@ -177,6 +217,7 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
         }
         __syncthreads();
     }
+    if constexpr (DT == SPV_F16) scale_back(o, up);
     if constexpr (KW > 1) {
         // the waves of a block of columns add up (the tiles' LDS is free by now)
         static_assert(2 * KT * T::LD >= CW * (KW - 1) * T::NB * 16 * 256, "a wave's sums have room");
@@ -197,8 +238,7 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
 }
 
 // The weights are at most 1 and, over long scans, far below float16's smallest normal number (6e-5): in that type they
-// are multiplied as 2^12 p (and may be some times 1 where scores of millions round).  dz is not scaled: its size is
-// that of dout, which a caller may have scaled up.
+// are multiplied as 2^12 p (and may be some times 1 where scores of millions round).
 template <int DT>
 constexpr float kUp = DT == SPV_F16 ? 12.f : 0.f;
 
@@ -294,6 +334,8 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
         }
     };
     constexpr float down = DT == SPV_F16 ? 1.f / 4096.f : 1.f;  // 2^-kUp
+    int up = DT == SPV_F16 ? kUpMost : 0;
+    float lift_z = __builtin_amdgcn_ldexpf(down, up);  // 2^up, less the weights' kUp
     f32x16 ok[T::NB], ov[T::NB];
 #pragma unroll
     for (int b = 0; b < T::NB; ++b) ok[b] = ov[b] = f32x16{};
@@ -337,7 +379,7 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
                         p[r] = __builtin_amdgcn_exp2f(AFTER || BIAS ? fmaf(z[u][r], cs, y) : z[u][r] * cs);
                         z[u][r] = p[r] * d[u][r];
                     }
-                    if constexpr (DT == SPV_F16) z[u][r] *= down;
+                    if constexpr (DT == SPV_F16) z[u][r] *= lift_z;
                 };
                 if constexpr (BIAS)
                     lc.bias(s, row0 + 32 * u, h, far, place, slope, lift, grad);
@@ -345,6 +387,8 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
 #pragma unroll
                     for (int r = 0; r < 16; ++r) grad(r, 0.f);
                 T::add_weighted(ld[s] + (row0 + 32 * u) * T::LD, lane, T::weights(p), ov);
+                if constexpr (DT == SPV_F16)
+                    if (lower(z[u], ok, up)) lift_z = __builtin_amdgcn_ldexpf(down, up);
                 T::add_weighted(lq[s] + (row0 + 32 * u) * T::LD, lane, T::weights(z[u]), ok);
             }
         }
@@ -355,6 +399,7 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
         }
         __syncthreads();
     }
+    if constexpr (DT == SPV_F16) scale_back(ok, up);
     if constexpr (KW > 1) {
         // the waves of a block of columns add up (the tiles' LDS is free by now)
         static_assert(2 * KT * T::LD >= CW * (KW - 1) * T::NB * 16 * 256, "a wave's sums have room");

@@ -254,3 +254,35 @@ def test_f16_many_small_weights(spv, score, nk, nq):
     want = w / (1 + w)
     tol = (nk - 1) * 2.0 ** -32 + 2.0 ** -11 * want * 2 + 2.0 ** -24
     assert np.all(np.abs(arr(got["out"]) - want) <= tol), (float(arr(got["out"]).mean()), want, tol)
+
+
+# -- gradients in float16 -----------------------------------------------------------------
+
+@pytest.mark.parametrize("std", [1e-4, 1e-3, 1e-2, 1.0])
+@pytest.mark.parametrize("nq,nk", [(1500, 1500), (60, 6720), (2500, 40)])
+def test_f16_small_gradients(spv, nq, nk, std):
+    """Incoming gradients from 1e-4 up over long scans: dz, some 1e-8 each, keeps its eleven bits until it is summed.  Each
+    gradient is off by the rounding of its weights and of dz (u each, as out's) and by its own last rounding, half a
+    subnormal step where it is that small."""
+    print(f"{nq}x{nk} std={std}", flush=True)
+    q, k, v = (rnd(i, n, 2, 64, dtype="f16") for i, n in enumerate((nq, nk, nk)))
+    do = rnd(3, nq, 2, 64, std=std, dtype="f16")
+    got = run(spv, q, k, v, do)
+    want = ref.attention(arr(q), arr(k), arr(v), [0, nq], [0, nk], 0.125, dout=arr(do), dtype="f16")
+    for n in ("dq", "dk", "dv"):
+        err, w = arr(got[n]) - want[n], want[n]
+        # of a subnormal result: evenly spread over a step of 2^-24
+        bound = 2 * ref.UNIT["f16"] * np.sqrt((w ** 2).sum()) + np.sqrt(w.size) * 2.0 ** -24 / np.sqrt(12.0)
+        print(n, np.sqrt((err ** 2).sum()) / bound, flush=True)
+        assert np.sqrt((err ** 2).sum()) <= bound, n
+
+
+@pytest.mark.parametrize("nq,nk", [(3, 3), (200, 300), (5, 4000)])
+def test_f16_gradients_past_its_range_on_the_way(spv, nq, nk):
+    """Gradients scaled up: products dout . v of more than 65,504 whose dq and dk are in range again."""
+    q, k = (rnd(i, n, 1, 64, std=2.0 ** -6, dtype="f16") for i, n in enumerate((nq, nk)))
+    v, do = rnd(2, nk, 1, 64, std=128.0, dtype="f16"), rnd(3, nq, 1, 64, std=128.0, dtype="f16")
+    got = run(spv, q, k, v, do)
+    want = ref.attention(arr(q), arr(k), arr(v), [0, nq], [0, nk], 0.125, dout=arr(do), dtype="f16")
+    for n in ("dq", "dk", "dv"):
+        assert rms(got[n], want[n]) <= 4 * ref.UNIT["f16"], (n, rms(got[n], want[n]))
