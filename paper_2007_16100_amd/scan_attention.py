@@ -25,6 +25,13 @@ def scan_offsets(coords: torch.Tensor, scans: int) -> torch.Tensor:
     return torch.searchsorted(b, torch.arange(scans + 1, dtype=b.dtype, device=b.device), out_int32=True)
 
 
+def _rows(t: torch.Tensor, width: int, dtype: torch.dtype, name: str, rows: Optional[int] = None):
+    """Refuses what the calls would read past: t must be contiguous [rows][width] of dtype."""
+    if t.dim() != 2 or t.shape[1] != width or t.dtype != dtype or not t.is_contiguous() or \
+            (rows is not None and t.shape[0] != rows):
+        raise ValueError(f"{name} must be contiguous [{'rows' if rows is None else rows}][{width}] of {dtype}")
+
+
 class ScanAttention:
     """params: gamma, beta [C] f32; Wq [C][H D], Wk, Wv [C][Hkv D], Wo [H D][C] of the features' type."""
 
@@ -33,10 +40,19 @@ class ScanAttention:
         self.P = {n: t.contiguous() for n, t in params.items()}
         self.C, width = self.P["Wq"].shape
         self.H, self.K = heads, heads if kv_heads is None else kv_heads
+        if self.H <= 0 or self.K <= 0 or self.H % self.K:
+            raise ValueError("heads must be a multiple of the key heads")
         if width % heads or self.P["Wk"].shape != (self.C, self.K * (width // heads)) or \
                 self.P["Wv"].shape != self.P["Wk"].shape or self.P["Wo"].shape != (width, self.C):
             raise ValueError("the weights do not fit the heads")
-        self.D = width // heads
+        self.D, self.dtype = width // heads, self.P["Wq"].dtype
+        if self.dtype not in (torch.float32, torch.bfloat16, torch.float16) or \
+                any(self.P[n].dtype != self.dtype for n in ("Wk", "Wv", "Wo")):
+            raise ValueError("the weights must be of one type, float32, bfloat16 or float16")
+        for n, t in (("gamma", self.P["gamma"]), ("beta", self.P["beta"]), ("slopes", slopes)):
+            size = heads if n == "slopes" else self.C
+            if t is not None and (t.dtype != torch.float32 or t.shape != (size,)):
+                raise ValueError(f"{n} must be float32 [{size}]")
         self.cap, self.slopes, self.eps = cap, slopes, eps
         self.ws: Dict[str, tuple] = {}
 
@@ -63,7 +79,16 @@ class ScanAttention:
         save (a dict): receives what backward() reads."""
         P, own = self.P, tokens is None
         t = x if own else tokens
+        _rows(x, self.C, self.dtype, "x")
+        if not own:
+            _rows(tokens, self.C, self.dtype, "tokens")
+            if token_off is None:
+                raise ValueError("tokens come with their scans' ranges, token_off")
         n, m = x.shape[0], t.shape[0]
+        if self.slopes is not None:
+            for c, r, name in ((coords, n, "coords"),) if own else ((coords, n, "coords"), (token_coords, m, "token_coords")):
+                if c is None or c.dtype != torch.int32 or c.dim() != 2 or c.shape[1] != 4 or c.shape[0] < r:
+                    raise ValueError(f"slopes come with {name}, int32 [{r}][4]")
         h = spv.spv_layer_norm(x, P["gamma"], P["beta"], self.eps)
         ht = h if own else spv.spv_layer_norm(t, P["gamma"], P["beta"], self.eps)
         q = self._linear(ht, P["Wq"]).view(m, self.H, self.D)
@@ -87,6 +112,7 @@ class ScanAttention:
             raise ValueError("backward takes the voxels' own queries")
         P, x, h, p = self.P, saved["x"], saved["h"], saved["p"]
         n, width, kv = x.shape[0], self.H * self.D, self.K * self.D
+        _rows(dy, self.C, self.dtype, "dy", n)
         g = {}
         wide = (max(self.C, width), max(self.C, width))
         lin = self._ws("linear", wide, lambda: spv.Workspace.for_linear_backward(*wide))
