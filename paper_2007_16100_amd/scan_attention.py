@@ -11,6 +11,7 @@ Every step runs in libspv's kernels; the module only sequences the calls and hol
 """
 from __future__ import annotations
 
+import threading
 from typing import Dict, Optional
 
 import torch
@@ -33,7 +34,9 @@ def _rows(t: torch.Tensor, width: int, dtype: torch.dtype, name: str, rows: Opti
 
 
 class ScanAttention:
-    """params: gamma, beta [C] f32; Wq [C][H D], Wk, Wv [C][Hkv D], Wo [H D][C] of the features' type."""
+    """params: gamma, beta [C] f32; Wq [C][H D], Wk, Wv [C][Hkv D], Wo [H D][C] of the features' type.
+
+    Calls on several streams or from several threads may overlap: the layer keeps workspaces for each."""
 
     def __init__(self, params: Dict[str, torch.Tensor], heads: int, kv_heads: Optional[int] = None, cap: float = 0.0,
                  slopes: Optional[torch.Tensor] = None, eps: float = 1e-5):
@@ -54,14 +57,16 @@ class ScanAttention:
             if t is not None and (t.dtype != torch.float32 or t.shape != (size,)):
                 raise ValueError(f"{n} must be float32 [{size}]")
         self.cap, self.slopes, self.eps = cap, slopes, eps
-        self.ws: Dict[str, tuple] = {}
+        self.ws: Dict[tuple, tuple] = {}
 
     def _ws(self, name: str, sizes: tuple, make) -> spv.Workspace:
-        """The workspace `name` for a call of these sizes: the last one where it served them, or is large enough."""
-        last = self.ws.get(name)
+        """The current stream's and thread's workspace `name` for a call of these sizes: the last one where it served
+        them, or is large enough."""
+        key = (name, spv._stream().value, threading.get_ident())
+        last = self.ws.get(key)
         if last is None or last[0] != sizes:
             w = make()
-            last = self.ws[name] = (sizes, w if last is None or w.nbytes > last[1].nbytes else last[1])
+            last = self.ws[key] = (sizes, w if last is None or w.nbytes > last[1].nbytes else last[1])
         return last[1]
 
     def _linear(self, x, W, res=None):
