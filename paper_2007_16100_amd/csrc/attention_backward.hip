@@ -32,10 +32,42 @@ __device__ inline float row_lse(float lse) {
 // Waves per SIMD that the registers have to leave room for: as many as cost no or few spills.  [8192] x 4 heads of 128,
 // dq with two 254 us, with one 421; [9000] x 8 heads of 96, forward and backward, with two in dk, dv 1908 us, with one
 // 2319; [4096] x 4 heads of 64 in float32 with two everywhere 1026 us, with one 773.
-constexpr int dq_waves(int dt, int DP) { return dt == SPV_F32 ? (DP > 64 ? 1 : 2) : DP > 32 ? 2 : 3; }
+constexpr int dq_waves(int dt, int DP, int cap) {
+    return dt == SPV_F32 ? (DP > 64 ? 1 : 2) : DP > 96 || (DP > 64 && cap) ? 1 : DP > 32 || cap ? 2 : 3;
+}
 constexpr int dkv_waves(int dt, int DP, int KW) {
     return dt == SPV_F32 ? (DP > 32 ? 1 : 2) : DP > 96 || (DP > 64 && KW > 1) ? 1 : DP > 32 ? 2 : 3;
 }
+
+// The weights are at most 1 and, over long scans, far below float16's smallest normal number (6e-5): in that type they
+// are multiplied as 2^12 p (and may be some times 1 where scores of millions round).
+template <int DT>
+constexpr float kUp = DT == SPV_F16 ? 12.f : 0.f;
+
+// In 16 bits delta, formed of the rounded out, is off by an error e, every dz of a row by p e ds/dz, and dq by e times the
+// sum of p ds/dz k.  That is more than dq itself where keys and values lie around a mean: with both around 4 dq of bf16 was
+// off by 0.6, now by 2.4e-3.  The row shows e: the sum over its keys of p (dout . v - delta) is -e where it would be zero.
+// So one more product gives the sum of p ds/dz k, and e times it is taken off; dk takes the corrected delta.  What
+// rounding dz to the type adds to the sum of dz k for the mean key is taken off the same way: without a cap the sum
+// of dz as they are multiplied has both in it, under one (where the sum of dz need not be zero) they are counted apart.
+// A training step of [3451, 3654, 1963, 2195] x 8 heads of 32, bf16: 303 -> 327 us.
+struct DqSums {
+    float s[3] = {0.f, 0.f, 0.f};  // of dz as multiplied; of dz; under a cap of p (dout . v - delta)
+    float p = 0.f;                 // of p ds/dz
+    __device__ inline void halves() {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) s[i] = half_sum(s[i]);
+        p = half_sum(p);
+    }
+    __device__ inline void scale(float f, float fp) { s[0] *= f, s[1] *= f, s[2] *= f, p *= fp; }
+    // -e, for delta
+    __device__ inline float error(bool cap) const { return cap ? s[2] : s[1]; }
+    // what the sum of p ds/dz k is taken off times
+    __device__ inline float off(bool cap) const { return cap ? s[2] + (p > 0.f ? (s[0] - s[1]) / p : 0.f) : s[0]; }
+    // a wave's, 64 floats apart
+    __device__ inline void put(float* l) const { l[0] = s[0], l[64] = s[1], l[128] = s[2], l[192] = p; }
+    __device__ inline void add(const float* l) { s[0] += l[0], s[1] += l[64], s[2] += l[128], p += l[192]; }
+};
 
 // Float16 holds dz neither where weights are small (below 6e-5 in fewer than eleven bits, below 3e-8 not at all) nor where
 // dout . v passes 65,504.  So a column's dz are multiplied as 2^up dz, and its sums scaled back at the end: up is lowered,
@@ -45,8 +77,8 @@ constexpr int dkv_waves(int dt, int DP, int KW) {
 // without it, where rounding the exact result gives 8e-3, as now.
 constexpr int kUpMost = 60;
 // true: up of some column of the wave was lowered
-template <int N>
-__device__ inline bool lower(f32x16& z, f32x16 (&o)[N], int& up) {
+template <int N, int M>
+__device__ inline bool lower(f32x16& z, f32x16 (&o)[N], int& up, float (&sums)[M]) {
     float top = fabsf(z[0]);
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(top, fabsf(z[r]));
@@ -56,6 +88,8 @@ __device__ inline bool lower(f32x16& z, f32x16 (&o)[N], int& up) {
     if (by > up + 200) by = up + 200;  // infinities stay what they are
     const float f = __builtin_amdgcn_ldexpf(1.f, -by);
     up -= by;
+#pragma unroll
+    for (int i = 0; i < M; ++i) sums[i] *= f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) z[r] *= f;
 #pragma unroll
@@ -74,13 +108,15 @@ __device__ inline void scale_back(f32x16 (&o)[N], int up) {
 }
 
 template <int DT, int DP, int KW, bool BIAS, int CAP>
-__global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
+__global__ __launch_bounds__(256, dq_waves(DT, DP, CAP)) void k_attn_dq(AttnArgs a) {
     using T = Tile<DT, DP>;
     constexpr int RT = attn_rows(DT, DP, KW), KT = RT * KW, KS = RT / 32, CW = 4 / KW, BM = 32 * CW;
-    constexpr bool AFTER = attn_after(DT, BIAS, CAP);
+    constexpr bool AFTER = attn_after(DT, BIAS, CAP), LOW = DT != SPV_F32;
+    constexpr bool WIDE = LOW && DP > 64;  // -delta is added after the product: 16 registers less
     __shared__ __align__(16) char lk[2][KT * T::LD], lv[2][KT * T::LD];
     __shared__ __align__(16) Places<BIAS ? KT : 32> lc;
     __shared__ uint32_t box[4][3];
+    __shared__ float ls[LOW && KW > 1 ? 4 * CW * (KW - 1) : 1][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), cw = wave / KW, kw = wave % KW;
     const int c = lane & 31, h = lane >> 5;
     const Share sh = attn_share(a);
@@ -135,7 +171,6 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
 #pragma unroll
     for (int s = 0; s < T::NF; ++s) delta = T::frag_dot(df[s], of[s], delta);
     delta = half_sum(delta);
-    if (live && h == 0 && sh.part == 0 && kw == 0) a.delta[qi * a.H + head] = delta;
     Words far{0, 0};
     uint32_t place = 0;
     Cube cube{};
@@ -150,10 +185,11 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
     const float cs = in_vgpr(a.scale * kLog2e);
     const Capped<CAP> capped(a);
     int up = DT == SPV_F16 ? kUpMost : 0;
+    float lift_p = __builtin_amdgcn_ldexpf(1.f, (int)kUp<DT> - up);
     float rest = (float)up - lse;  // what a weight's exponent is beside the score
     f32x16 dref;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dref[r] = -delta;
+    for (int r = 0; r < 16; ++r) dref[r] = WIDE ? 0.f : -delta;
 
     auto store = [&](int s) __attribute__((always_inline)) {
         sk.store(lk[s], tid);
@@ -161,9 +197,10 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
         if constexpr (BIAS)
             if (tid < KT) lc.put(s, tid, ck, tid < got, cube);
     };
-    f32x16 o[T::NB];
+    f32x16 o[T::NB], mean[T::NB];  // sums of dz k and (16 bits) of the weights of its error, p ds/dz, times k
 #pragma unroll
-    for (int b = 0; b < T::NB; ++b) o[b] = f32x16{};
+    for (int b = 0; b < T::NB; ++b) o[b] = mean[b] = f32x16{};
+    DqSums sums;
     if (t0 < t1) {
         store(0);
         if (t0 + 1 < t1) load();
@@ -185,30 +222,51 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
             }
 #pragma unroll
             for (int u = 0; u < KS; ++u) {
+                f32x16 p, free;  // weights times ds/dz, p (dout . v - delta) free of it
+                const int end = left - 32 * u;
                 auto grad = [&](int r, float b) __attribute__((always_inline)) {
                     if constexpr (CAP) {
                         float bend;
-                        const float x = capped(z[u][r], b + (capped.lift + rest), &bend);
-                        z[u][r] = __builtin_amdgcn_exp2f(x) * d[u][r] * bend;
+                        const float x = capped(z[u][r], b + (capped.lift + rest), &bend), w = __builtin_amdgcn_exp2f(x);
+                        p[r] = w * bend;
+                        free[r] = w * (WIDE ? d[u][r] - delta : d[u][r]);
+                        z[u][r] = free[r] * bend;
                     } else {
-                        z[u][r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], cs, AFTER ? b + rest : rest)) * d[u][r];
+                        p[r] = __builtin_amdgcn_exp2f(fmaf(z[u][r], cs, AFTER ? b + rest : rest));
                     }
+                    if constexpr (!CAP) z[u][r] = p[r] * (WIDE ? d[u][r] - delta : d[u][r]);
+                    if constexpr (DT == SPV_F16) p[r] *= lift_p;
                 };
                 if constexpr (AFTER && BIAS)
                     lc.bias(s, row0 + 32 * u, h, far, place, slope, lift, grad);
                 else
 #pragma unroll
                     for (int r = 0; r < 16; ++r) grad(r, 0.f);
-                const int end = left - 32 * u;
-                if (end < 32) {  // keys past the scan's end: their rows are zero, but not their weights
+                if (end < 32) {  // keys past the scan's end: their rows are zero, but not their weights, which may pass any bound
                     asm volatile("");  // a branch, not selects on every tile
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (8 * (r / 4) + 4 * h + r % 4 >= end) z[u][r] = 0.f;
+                        if (8 * (r / 4) + 4 * h + r % 4 >= end) z[u][r] = p[r] = free[r] = 0.f;
                 }
+                if constexpr (LOW && CAP)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sums.s[2] += free[r];
                 if constexpr (DT == SPV_F16)
-                    if (lower(z[u], o, up)) rest = (float)up - lse;
-                T::add_weighted(lk[s] + (row0 + 32 * u) * T::LD, lane, T::weights(z[u]), o);
+                    if (lower(z[u], o, up, sums.s)) {
+                        rest = (float)up - lse;
+                        lift_p = __builtin_amdgcn_ldexpf(1.f, (int)kUp<DT> - up);
+                    }
+                const typename T::Weights w = T::weights(z[u]);
+                if constexpr (LOW) {
+                    const typename T::Weights wp = T::weights(p);
+                    sums.s[0] = T::sum(w, sums.s[0]);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sums.s[1] += z[u][r];
+                    if constexpr (CAP) sums.p = T::sum(wp, sums.p);
+                    T::add_weighted(lk[s] + (row0 + 32 * u) * T::LD, lane, w, o, &wp, mean);
+                } else {
+                    T::add_weighted(lk[s] + (row0 + 32 * u) * T::LD, lane, w, o);
+                }
             }
         }
         if (i + 1 < t1) {
@@ -217,30 +275,85 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP)) void k_attn_dq(AttnArgs a) {
         }
         __syncthreads();
     }
-    if constexpr (DT == SPV_F16) scale_back(o, up);
+    if constexpr (DT == SPV_F16) {
+        scale_back(o, up);
+        scale_back(mean, (int)kUp<DT>);
+        sums.scale(__builtin_amdgcn_ldexpf(1.f, -up), __builtin_amdgcn_ldexpf(1.f, -(int)kUp<DT>));
+    }
+    if constexpr (LOW) sums.halves();
     if constexpr (KW > 1) {
         // the waves of a block of columns add up (the tiles' LDS is free by now)
         static_assert(2 * KT * T::LD >= CW * (KW - 1) * T::NB * 16 * 256, "a wave's sums have room");
         constexpr int N = T::NB * 16 * 64;
-        float* p = (float*)&lk[0][0] + cw * (KW - 1) * N;
-        if (kw) lds_put(p + (kw - 1) * N, lane, o);
+        float *p = (float*)&lk[0][0] + cw * (KW - 1) * N, *pm = (float*)&lv[0][0] + cw * (KW - 1) * N;
+        if (kw) {
+            lds_put(p + (kw - 1) * N, lane, o);
+            if constexpr (LOW) {
+                lds_put(pm + (kw - 1) * N, lane, mean);
+                sums.put(&ls[4 * (cw * (KW - 1) + kw - 1)][lane]);
+            }
+        }
         __syncthreads();
         if (kw) return;
 #pragma unroll
-        for (int w = 1; w < KW; ++w) lds_add(p + (w - 1) * N, lane, 1.f, o);
+        for (int w = 1; w < KW; ++w) {
+            lds_add(p + (w - 1) * N, lane, 1.f, o);
+            if constexpr (LOW) {
+                lds_add(pm + (w - 1) * N, lane, 1.f, mean);
+                sums.add(&ls[4 * (cw * (KW - 1) + w - 1)][lane]);
+            }
+        }
     }
     if (!live) return;
     const float f = a.scale * kBend<CAP>;
-    if (a.part)
-        Tile<SPV_F32, DP>::store_cols(a.part, (((int64_t)sh.part * a.nq + qi) * a.H + head) * a.D, a.D, h, o, f);
-    else
-        T::store_cols(a.dq, qi * a.lddq + (int64_t)head * a.D, a.D, h, o, f);
+    const int64_t row = qi * a.H + head;
+    if (a.part) {
+        const int64_t at = (int64_t)sh.part * a.nq * a.H + row;
+        if (h == 0 && sh.part == 0) a.delta[row] = delta;
+        if constexpr (LOW) {
+            if (h == 0) *(float4*)(a.part_ml + 4 * at) = make_float4(sums.s[0], sums.s[1], sums.s[2], sums.p);
+            Tile<SPV_F32, DP>::store_cols(a.part, (2 * at + 1) * a.D, a.D, h, mean, f);
+            Tile<SPV_F32, DP>::store_cols(a.part, 2 * at * a.D, a.D, h, o, f);
+        } else {
+            Tile<SPV_F32, DP>::store_cols(a.part, at * a.D, a.D, h, o, f);
+        }
+        return;
+    }
+    if constexpr (LOW) {
+        const float off = sums.off(CAP);
+#pragma unroll
+        for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[b][r] = fmaf(-off, mean[b][r], o[b][r]);
+        delta += sums.error(CAP);
+    }
+    if (h == 0) a.delta[row] = delta;
+    T::store_cols(a.dq, qi * a.lddq + (int64_t)head * a.D, a.D, h, o, f);
 }
 
-// The weights are at most 1 and, over long scans, far below float16's smallest normal number (6e-5): in that type they
-// are multiplied as 2^12 p (and may be some times 1 where scores of millions round).
+// dq from the parts of its sums (16-bit types), and the rows' delta; four channels a thread
 template <int DT>
-constexpr float kUp = DT == SPV_F16 ? 12.f : 0.f;
+__global__ __launch_bounds__(256) void k_attn_dq_join(AttnArgs a, int parts) {
+    const int w = a.D / 4;
+    const int64_t id = blockIdx.x * (int64_t)256 + threadIdx.x, row = id / w, rows = a.nq * a.H, qi = row / a.H;
+    if (qi >= a.nq || qi < a.q_off[0] || qi >= a.q_off[a.B]) return;  // past the end, or a row of no scan
+    const int d = (int)(id - row * w) * 4;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f), m = s;
+    DqSums sums;
+    for (int q = 0; q < parts; ++q) {
+        const int64_t at = q * rows + row;
+        const float4 x = *(const float4*)(a.part + 2 * at * a.D + d), y = *(const float4*)(a.part + (2 * at + 1) * a.D + d);
+        const float4 z = *(const float4*)(a.part_ml + 4 * at);
+        s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+        m.x += y.x, m.y += y.y, m.z += y.z, m.w += y.w;
+        sums.s[0] += z.x, sums.s[1] += z.y, sums.s[2] += z.z, sums.p += z.w;
+    }
+    const bool cap = a.cap > 0.f;
+    const float off = -sums.off(cap);
+    *(uint2*)((uint16_t*)a.dq + qi * a.lddq + (row - qi * a.H) * a.D + d) =
+        make_uint2(pack2<DT>(fmaf(off, m.x, s.x), fmaf(off, m.y, s.y)), pack2<DT>(fmaf(off, m.z, s.z), fmaf(off, m.w, s.w)));
+    if (d == 0) a.delta[row] += sums.error(cap);
+}
 
 // Columns are keys; the rows are the scan's queries, once for each head of the key head's group, in that order.
 template <int DT, int DP, int KW, bool BIAS, int CAP>
@@ -335,7 +448,7 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
     };
     constexpr float down = DT == SPV_F16 ? 1.f / 4096.f : 1.f;  // 2^-kUp
     int up = DT == SPV_F16 ? kUpMost : 0;
-    float lift_z = __builtin_amdgcn_ldexpf(down, up);  // 2^up, less the weights' kUp
+    float lift_z = __builtin_amdgcn_ldexpf(down, up), none[1] = {0.f};  // 2^up, less the weights' kUp
     f32x16 ok[T::NB], ov[T::NB];
 #pragma unroll
     for (int b = 0; b < T::NB; ++b) ok[b] = ov[b] = f32x16{};
@@ -388,7 +501,7 @@ __global__ __launch_bounds__(256, dkv_waves(DT, DP, KW)) void k_attn_dkv(AttnArg
                     for (int r = 0; r < 16; ++r) grad(r, 0.f);
                 T::add_weighted(ld[s] + (row0 + 32 * u) * T::LD, lane, T::weights(p), ov);
                 if constexpr (DT == SPV_F16)
-                    if (lower(z[u], ok, up)) lift_z = __builtin_amdgcn_ldexpf(down, up);
+                    if (lower(z[u], ok, up, none)) lift_z = __builtin_amdgcn_ldexpf(down, up);
                 T::add_weighted(lq[s] + (row0 + 32 * u) * T::LD, lane, T::weights(z[u]), ok);
             }
         }
@@ -463,9 +576,11 @@ void plan_attention_backward_ws(Arena& a, AttnArgs& t) {
     t.delta = a.take<float>((size_t)t.nq * (size_t)t.H);
     const AttnShape q = dq_shape(t), k = dkv_shape(t);
     // the two kernels use the parts one after the other
-    const size_t pq = q.parts > 1 ? (size_t)q.parts * (size_t)t.nq * (size_t)t.H * (size_t)t.D : 0;
+    const size_t rows = q.parts > 1 ? (size_t)q.parts * (size_t)t.nq * (size_t)t.H : 0;
+    const size_t pq = rows * (size_t)t.D * (t.dt == SPV_F32 ? 1 : 2);
     const size_t pk = k.parts > 1 ? (size_t)k.parts * (size_t)t.nk * (size_t)t.K * (size_t)t.D * 2 : 0;
     if (pq || pk) t.part = a.take<float>(pq > pk ? pq : pk);
+    if (rows && t.dt != SPV_F32) t.part_ml = a.take<float>(4 * rows);
 }
 
 template <int DT, int DP, int KW, bool BIAS, int CAP>
@@ -503,6 +618,10 @@ static void backward_dt(hipStream_t s, const AttnArgs& a, bool keys) {
         case 128: launch_dp<DT, 128>(s, t, sh, keys); break;
     }
     if (sh.parts < 2) return;
+    if (!keys && DT != SPV_F32) {
+        if constexpr (DT != SPV_F32) k_attn_dq_join<DT><<<blocks_for(a.nq * a.H * a.D / 4, 256), 256, 0, s>>>(a, sh.parts);
+        return;
+    }
     if (!keys) {
         k_attn_add_parts<DT><<<blocks_for(a.nq * a.H * a.D / 4, 256), 256, 0, s>>>(a.part, sh.parts, a.nq, a.H, a.D,
                                                                                    a.q_off, a.B, a.dq, a.lddq);

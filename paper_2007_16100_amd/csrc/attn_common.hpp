@@ -320,7 +320,9 @@ struct Tile {
 
     // o[b] + (channels 32 b .. 32 b + 31 of the 32 rows at lds, transposed) . weights: lane (c, h) of o[b] holds
     // channels 32 b + 8 (i / 4) + 4 h + i % 4 of column c
-    static __device__ inline void add_weighted(const char* lds, int lane, const Weights& w, f32x16 (&o)[NB]) {
+    // (16-bit types: o2 the same with weights w2, of the same reads)
+    static __device__ inline void add_weighted(const char* lds, int lane, const Weights& w, f32x16 (&o)[NB],
+                                               const Weights* w2 = nullptr, f32x16* o2 = nullptr) {
         if constexpr (W) {
             const char* a = lds + (lane >> 5) * 4 * LD + (lane & 31) * 4;
 #pragma unroll
@@ -345,6 +347,7 @@ struct Tile {
                     const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(a + (16 * k + 8) * LD + 64 * b));
                     const i16x8 x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                     o[b] = mfma32x32x16<DT>(__builtin_bit_cast(uint4, x), w.f[k], o[b]);
+                    if (w2) o2[b] = mfma32x32x16<DT>(__builtin_bit_cast(uint4, x), w2->f[k], o2[b]);
                 }
         }
     }

@@ -27,12 +27,12 @@ def test_every_form_is_built(built):  # noqa: F811
 
 
 def test_attention_kernels_keep_their_registers(built):  # noqa: F811
-    """Up to 96 channels a form without a cap spills a few registers at most, one with a cap some dozens; the widest heads
-    more: a change that makes a form spill shows here.  All fit a compute unit's LDS."""
+    """Up to 96 channels a form spills some dozens of registers at most (with the exact cap up to a hundred), the widest
+    heads more: a change that makes a form spill shows here.  All fit a compute unit's LDS."""
     for name in ("k_attn", "k_attn_dq", "k_attn_dkv"):
         for (dt, dp, kw, bias, cap), k in attention(built, name).items():
             form = (name, dt, dp, kw, bias, cap)
             assert k[".group_segment_fixed_size"] <= LDS, form
             spills = k[".vgpr_spill_count"]
-            most = (8, 64, 128) if dp < 128 else (160, 160, 256)
+            most = (64, 64, 128) if dp < 128 else (160, 160, 256)
             assert spills <= most[cap], (form, spills)

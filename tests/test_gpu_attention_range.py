@@ -286,3 +286,31 @@ def test_f16_gradients_past_its_range_on_the_way(spv, nq, nk):
     want = ref.attention(arr(q), arr(k), arr(v), [0, nq], [0, nk], 0.125, dout=arr(do), dtype="f16")
     for n in ("dq", "dk", "dv"):
         assert rms(got[n], want[n]) <= 4 * ref.UNIT["f16"], (n, rms(got[n], want[n]))
+
+
+# -- means --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("k_mean,v_mean", [(0.0, 4.0), (4.0, 0.0), (4.0, 4.0), (16.0, 4.0)])
+@pytest.mark.parametrize("cap", [0.0, 30.0, 100.0])
+@pytest.mark.parametrize("nq,nk,H,K,D", [(400, 1200, 1, 1, 32), (2, 6000, 2, 1, 64), (700, 45, 4, 2, 40), (90, 300, 1, 1, 96),
+                                         (90, 300, 1, 1, 128)])
+def test_gradients_of_keys_and_values_around_a_mean(spv, nq, nk, H, K, D, k_mean, v_mean, cap, dtype):
+    """Keys and values that share a mean, as a layer's with biases do, or one without that centres its input: the rows of
+    p (dout . v - delta) sum to zero, so nothing that is the same for all keys reaches dq.  A gradient is off by its own
+    rounding and that of the weights or dz, 0.43 u each in the root of the mean square, 0.6 u together."""
+    print(f"{nq}x{nk} H={H} K={K} D={D} means {k_mean} {v_mean} cap={cap} {dtype}", flush=True)
+    q, do = rnd(0, nq, H, D, dtype=dtype), rnd(3, nq, H, D, dtype=dtype)
+    k, v = ((rnd(i, nk, K, D) + m).to(TD[dtype]) for i, m in ((1, k_mean), (2, v_mean)))
+    bias, opt = {}, [None, None, None]
+    if D == 40:
+        g = torch.Generator().manual_seed(5)
+        bias["q_coords"], bias["k_coords"] = (torch.randint(-9, 9, (n, 4), generator=g).to(torch.int32).cuda()
+                                              for n in (nq, nk))
+        bias["slopes"] = torch.tensor([0.25, 0.125, 0.0625, 0.03125]).cuda()
+        opt = [bias["q_coords"].cpu().numpy(), bias["k_coords"].cpu().numpy(), arr(bias["slopes"])]
+    got = run(spv, q, k, v, do, cap=cap, **bias)
+    want = ref.attention(arr(q), arr(k), arr(v), [0, nq], [0, nk], float(np.float32(D ** -0.5)), cap, *opt, arr(do), dtype)
+    for n in ("dq", "dk", "dv"):
+        print(n, rms(got[n], want[n]) / ref.UNIT[dtype], flush=True)
+        assert rms(got[n], want[n]) <= ref.UNIT[dtype], n
