@@ -653,7 +653,11 @@ typedef struct spv_attention_params {
  *   dq_i = scale sum_j dz_ij k_j,  dk_j = scale sum_i dz_ij q_i
  * (shared key heads sum over their query heads; scale, cap and slopes are
  * constants).  p is formed from lse as float32 holds it, so it is off by 2^-24 |lse|
- * of itself; a row whose |lse| passes 2.9e6 gives and gets no gradient.  Deterministic: no atomics, every sum in a fixed order.
+ * of itself; a row whose |lse| passes 2.9e6 gives and gets no gradient.  In 16-bit
+ * types p and dz are rounded to the type before their products (dz of f16 under a
+ * power of two of its own for each column), and delta, from the rounded out, is
+ * corrected by the sum over j of ds_ij that it leaves.  Deterministic: no atomics,
+ * every sum in a fixed order.
  * In:  the forward's inputs, out and lse; dout [nq][lddo] (dt).
  * Out: dq [nq][lddq], dk [nk][lddk], dv [nk][lddv] (dt), no input, rows strided and
  *      aligned as the inputs'.  A key of a scan without queries gets 0; rows of no

@@ -12,27 +12,33 @@ namespace spv {
 // 2^kLead lose nothing in float32 sums or 16-bit weights, and after the first tiles m hardly ever moves.  It moves to kLift
 // below the score: in float16 the largest weights are 2^7 to 2^15, and those of 2^-21 of the largest still normal numbers.
 // The bias, over scale, is what the products are added to, unless a cap's tanh stands between them or (float32) D roundings
-// at the bias's size would show: 400 voxels from every key, at a slope of a half, out was off by up to 7e-5 so, by 6e-6 with
-// the bias added after the product.
+// at the bias's size would show: 400 voxels from every key, at a slope of a half, out was off by up to 7e-5 so, by 6e-6
+// with the bias added after the product.
+//
+// In 16 bits the weights are rounded to the type before they multiply the values, and the sum they are divided by is of
+// the rounded ones: out of bf16 is off by 2.1e-3 (one query over 88,119 keys 2.4e-3) in the root of the mean square against
+// 64 bits, its own last rounding alone by 1.7e-3.  Two halves of a weight would leave that alone, for half of the products
+// again and two more instructions a score.
 //
 // In 16 bits at 32 channels a score costs two matrix products of 32 channels but seven vector instructions (distance,
-// bias, reference, exponential, maximum, sum, rounding), of which the exponential counts double: those bound it, not the
-// products.  They keep the vector units busy 82% of the time at [16384] x 8 heads.
-// [3451, 3654, 1963, 2195] x 8 heads of 32, bf16, bias: 90 us (scores alone: 50 - 60; products: 29); its 720 workgroups
-// leave two to three waves a SIMD, which wait at barriers and for each other's products.
-// Four scans of 26,881 in all x 4 heads of 64 on 2, f16, cap and bias: 474 us; a cap adds an exponential, a reciprocal
+// bias, reference, exponential, maximum, sum, rounding), of which the exponential counts double.
+// [3451, 3654, 1963, 2195] x 8 heads of 32, bf16, bias: 92 us, of which the scores' instructions take 50 - 60 and the
+// products, beside them, 29.  The vector units are busy 70% of the time, the matrix units 17%; 720 workgroups leave 2.5
+// waves a SIMD, of scans of unequal length, which wait at barriers and for each other's products.  (At [16384] x 8 heads
+// the vector units were busy 82%.)
+// Four scans of 26,881 in all x 4 heads of 64 on 2, f16, cap and bias: 475 us; a cap adds an exponential, a reciprocal
 // and three more instructions.  One query over 88,119 keys x 8 heads of 32: 18 us in 64 parts, 3.8 TB/s with the join.
-// 211 x 3 heads in float32: 9.5 us a call.  In float32 the products (64 cycles each) bound it: [1457, 1544] x 3 heads,
-// cap and bias, 47 us, where 288 workgroups lie on 256 units.
+// 211 x 3 heads in float32: 9.5 us a call.  [1457, 1544] x 3 heads in float32, cap and bias: 48 us, where 285 workgroups
+// lie on 256 units, one wave to a SIMD: its products (36% of the cycles), its vector instructions (23%) and the waits for
+// LDS and memory follow one another.
 template <int DT>
 constexpr float kLead = DT == SPV_F16 ? 15.f : 8.f;
 template <int DT>
 constexpr float kLift = DT == SPV_F16 ? 7.f : 0.f;
 // A reference is base + m: base in the units that the products come in (of the scores, where the bias is added after), m in
-// units of log 2.
-// One of up to kNear is all in m, and weights are exp2(z cs - m) in one step.  A larger one is a base, the largest z
-// itself, and is taken off z first: rounded to a float, m = base cs would be off by more than the weights' range, the
-// same for every key but enough to overflow or lose them all.
+// units of log 2.  One of up to kNear is all in m, and weights are exp2(z cs - m) in one step.  A larger one is a base, the
+// largest z itself, and is taken off z first: rounded to a float, m = base cs would be off by more than the weights'
+// range, the same for every key but enough to overflow or lose them all.
 constexpr float kNear = 1024.f;
 // the base of a column without a finite score so far: one of minus infinity has no weight under it, and any finite one
 // passes it
@@ -51,7 +57,9 @@ struct Reference {
     }
 };
 // units of log 2 in one of the base's
-__device__ inline float attn_unit(const AttnArgs& a) { return attn_after(a.dt, a.slopes, a.cap > 0.f) ? 1.f : a.scale * kLog2e; }
+__device__ inline float attn_unit(const AttnArgs& a) {
+    return attn_after(a.dt, a.slopes, a.cap > 0.f) ? 1.f : a.scale * kLog2e;
+}
 
 // Waves per SIMD that the registers have to leave room for.  [8192] x 4 heads of 128 with two 217 us, with one 350;
 // [16384] x 8 heads of 32 with four 621 us, with three 685.
@@ -324,7 +332,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int parts) {
                 const int s = s0 + u * NP;
                 v[u] = s < parts ? ml[s * rows] : make_float4(0.f, 0.f, 0.f, 0.f);
                 // sums of no key are not written
-                p[u] = v[u].y != 0.f ? *(const float4*)(a.part + (s * rows + row) * a.D + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+                p[u] = v[u].y != 0.f ? *(const float4*)(a.part + (s * rows + row) * a.D + d)
+                                     : make_float4(0.f, 0.f, 0.f, 0.f);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {

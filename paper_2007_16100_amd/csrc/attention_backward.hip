@@ -8,14 +8,17 @@
 // what the products q . k are added to, unless a cap's tanh stands between or (float32) the roundings at their size of each
 // step of the product would show (dv of 300 x 300 heads of 128: 1.7e-6 that way, 5.7e-7 so).
 //
-// In 16 bits dz is rounded to the type before its two products, and out, which delta is formed of, comes in rounded:
-// dq and dk of bf16 are off by 2.6e-3 (root of the mean square against 64 bits), their own last rounding alone by 1.7e-3.
-// An exact delta takes one more product of p and k, and brings 2.4e-3.
+// In 16 bits p and dz are rounded to the type before their products: dq of bf16 is off by 2.3e-3 (root of the mean square
+// against 64 bits), dk and dv by 2.4e-3, their own last rounding alone by 1.7e-3.  Two halves of dz would bring dq and dk
+// to 1.7e-3, for 21 us more in each kernel at the size below.  Out, which delta is formed of, comes in rounded too: see
+// DqSums.
 //
-// [3451, 3654, 1963, 2195] x 8 heads of 32, bf16, bias: dq 106 us, dk and dv 141.  As in the forward the vector
-// instructions of a score bound dq; dk and dv have two accumulators of a column, so two or three waves a SIMD, and wait
-// for LDS and the matrix unit in turn.  [1457, 1544] x 3 heads in float32, cap and bias: dq 61 us, dk and dv 75, by the
-// products, with 288 workgroups on 256 units.
+// [3451, 3654, 1963, 2195] x 8 heads of 32, bf16, bias: a training step takes 328 us; in a kernel trace of a cold start the
+// forward takes 105 of it, dq 131, dk and dv 140.  The vector units are busy 67% of the time in dq, 55% in dk and dv, the
+// matrix units 27 and 25%.  Dk and dv have two accumulators of a column, so 2.5 waves a SIMD, which wait for LDS (its
+// index unit active 45%) and the matrix unit in turn, with a barrier every 32 rows.
+// [1457, 1544] x 3 heads in float32, cap and bias: dq 60 us, dk and dv 76; 285 workgroups, one wave to a SIMD, whose
+// products (44 and 47% of the cycles), vector instructions (21 and 18%) and waits follow one another.
 #include "attn_common.hpp"
 
 namespace spv {
@@ -29,9 +32,11 @@ __device__ inline float row_lse(float lse) {
     return fabsf(e) > kMaxLse ? INFINITY : e;
 }
 
-// Waves per SIMD that the registers have to leave room for: as many as cost no or few spills.  [8192] x 4 heads of 128,
-// dq with two 254 us, with one 421; [9000] x 8 heads of 96, forward and backward, with two in dk, dv 1908 us, with one
-// 2319; [4096] x 4 heads of 64 in float32 with two everywhere 1026 us, with one 773.
+// Waves per SIMD that the registers have to leave room for, each the faster of two.  Some forms spill all the same: up to
+// 96 channels dozens of registers with a bias and a cap, at 128 in float32 with a bias over a hundred.  Backward of [8192]
+// in bf16: 4 heads of 128, one wave in dq 806 us, two 1103; 8 heads of 96 two 754, one 984, but under a cap one 1211, two
+// 1325; 8 heads of 32 under a cap two 596, three 1720.  [9000] x 8 heads of 96, forward and backward, with two in dk, dv
+// 1908 us, with one 2319 (before dq had its fourth product); [4096] x 4 heads of 64 in float32 with two everywhere 1026 us, with one 773.
 constexpr int dq_waves(int dt, int DP, int cap) {
     return dt == SPV_F32 ? (DP > 64 ? 1 : 2) : DP > 96 || (DP > 64 && cap) ? 1 : DP > 32 || cap ? 2 : 3;
 }
@@ -46,7 +51,7 @@ constexpr float kUp = DT == SPV_F16 ? 12.f : 0.f;
 
 // In 16 bits delta, formed of the rounded out, is off by an error e, every dz of a row by p e ds/dz, and dq by e times the
 // sum of p ds/dz k.  That is more than dq itself where keys and values lie around a mean: with both around 4 dq of bf16 was
-// off by 0.6, now by 2.4e-3.  The row shows e: the sum over its keys of p (dout . v - delta) is -e where it would be zero.
+// off by 0.6, now by 2.3e-3.  The row shows e: the sum over its keys of p (dout . v - delta) is -e where it would be zero.
 // So one more product gives the sum of p ds/dz k, and e times it is taken off; dk takes the corrected delta.  What
 // rounding dz to the type adds to the sum of dz k for the mean key is taken off the same way: without a cap the sum
 // of dz as they are multiplied has both in it, under one (where the sum of dz need not be zero) they are counted apart.
@@ -242,7 +247,8 @@ __global__ __launch_bounds__(256, dq_waves(DT, DP, CAP)) void k_attn_dq(AttnArgs
                 else
 #pragma unroll
                     for (int r = 0; r < 16; ++r) grad(r, 0.f);
-                if (end < 32) {  // keys past the scan's end: their rows are zero, but not their weights, which may pass any bound
+                // keys past the scan's end: their rows are zero, but not their weights, which may pass any bound
+                if (end < 32) {
                     asm volatile("");  // a branch, not selects on every tile
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
@@ -351,7 +357,8 @@ __global__ __launch_bounds__(256) void k_attn_dq_join(AttnArgs a, int parts) {
     const bool cap = a.cap > 0.f;
     const float off = -sums.off(cap);
     *(uint2*)((uint16_t*)a.dq + qi * a.lddq + (row - qi * a.H) * a.D + d) =
-        make_uint2(pack2<DT>(fmaf(off, m.x, s.x), fmaf(off, m.y, s.y)), pack2<DT>(fmaf(off, m.z, s.z), fmaf(off, m.w, s.w)));
+        make_uint2(pack2<DT>(fmaf(off, m.x, s.x), fmaf(off, m.y, s.y)),
+                   pack2<DT>(fmaf(off, m.z, s.z), fmaf(off, m.w, s.w)));
     if (d == 0) a.delta[row] += sums.error(cap);
 }
 

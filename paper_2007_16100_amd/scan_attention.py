@@ -129,7 +129,9 @@ class ScanAttention:
         for name, d, w in (("Wq", dq, width), ("Wk", dk, kv), ("Wv", dv, kv)):
             d = d.view(n, w)
             _, g[name] = spv.spv_linear_backward(lin, h, P[name], d, want_dx=False)
-            dh = self._linear(d, P[name].t().contiguous(), res=dh)  # the three products add up in the residual
+            # The three products add up in the residual.  In 16 bits each sum is rounded (bf16 off by 2.3e-3, one rounding
+            # 1.7e-3): the linear kernel takes up to 256 inputs, so not the three side by side.
+            dh = self._linear(d, P[name].t().contiguous(), res=dh)
         wn = self._ws("norm", (n,), lambda: spv.Workspace.for_layer_norm_backward(n, self.C))
         g["x"], g["gamma"], g["beta"] = spv.spv_layer_norm_backward(wn, dh, x, P["gamma"], self.eps, dres=dy)
         return g
