@@ -36,7 +36,8 @@ __device__ inline float row_lse(float lse) {
 // 96 channels dozens of registers with a bias and a cap, at 128 in float32 with a bias over a hundred.  Backward of [8192]
 // in bf16: 4 heads of 128, one wave in dq 806 us, two 1103; 8 heads of 96 two 754, one 984, but under a cap one 1211, two
 // 1325; 8 heads of 32 under a cap two 596, three 1720.  [9000] x 8 heads of 96, forward and backward, with two in dk, dv
-// 1908 us, with one 2319 (before dq had its fourth product); [4096] x 4 heads of 64 in float32 with two everywhere 1026 us, with one 773.
+// 1908 us, with one 2319 (before dq had its fourth product); [4096] x 4 heads of 64 in float32 with two everywhere 1026
+// us, with one 773.
 constexpr int dq_waves(int dt, int DP, int cap) {
     return dt == SPV_F32 ? (DP > 64 ? 1 : 2) : DP > 96 || (DP > 64 && cap) ? 1 : DP > 32 || cap ? 2 : 3;
 }

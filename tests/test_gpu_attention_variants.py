@@ -1,11 +1,10 @@
 """Every form of the attention kernels that a large call runs, at sizes a float64 reference can follow: many short and a
 few longer scans, so that there are workgroups enough for one wave or two on a block of columns.  shape() is the rule by
 which a call takes its form, written out again; each test asserts what its sizes reach, in both directions."""
-import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_attention import TD, Case, arr, spv, within  # noqa: F401 (spv: a fixture)
+from tests.test_gpu_attention import Case, spv  # noqa: F401 (spv: a fixture)
 
 pytestmark = pytest.mark.gpu
 
