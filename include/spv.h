@@ -676,6 +676,127 @@ spv_status spv_attention_backward(void* stream, void* ws, size_t ws_bytes, const
                                   const float* lse, const void* dout, int64_t lddo, void* dq, int64_t lddq,
                                   void* dk, int64_t lddk, void* dv, int64_t lddv, spv_dtype dt);
 
+/* Rotary positions: pairs of a head's channels turn with the axes of its voxel's
+ * coordinates, so that a product of two rotated heads depends on where the voxels
+ * stand to each other, along x, y and z apart. */
+typedef struct spv_rope_params {
+    int32_t D;           /* channels of a head: a multiple of 8 in 8 .. 128 */
+    int32_t sections[3]; /* pairs that turn with x, with y and with z, in this order; >= 0, P = their sum in 1 .. D / 2 */
+    int32_t halves;      /* pair p is channels (2 p, 2 p + 1); nonzero: (p, p + P) */
+    const float* freqs;  /* [P] f32, device: radians a voxel */
+} spv_rope_params;
+
+/*
+ * spv_rope -- every head of q and of k rotated by its row's coordinates: for pair p
+ * of the axis a that its section gives, theta = c_a * freqs[p],
+ *   (u, w) -> (u cos theta - w sin theta, u sin theta + w cos theta);
+ * channels past 2 P stay as they are.  inverse: by -theta, which is the backward
+ * (gradients of the rotated rows in, of the rows out).  theta is reduced to an
+ * eighth of a turn in float64 (off by 2^-51 |theta| at most), sine and cosine and the rotation are float32,
+ * one rounding to dt.
+ * In:  coords [n][4] i32 (b, x, y, z), 16-byte aligned (outside the voxel range: its
+ *      nearest end); m_dev: device row count (NULL = n); q [n][ldq] with H heads, k
+ *      [n][ldk] with Hkv heads or NULL (Hkv = 0), rows strided and 16-byte aligned as
+ *      spv_attention's.
+ * Out: q_out [n][ldqo], k_out [n][ldko] (dt; rows < count): each its own input (with the
+ *      same stride) or apart from both inputs.  No workspace.
+ * Errors: SPV_ERR_INVALID_ARG (null or misaligned pointers, sizes, sections, strides,
+ *      aliasing), SPV_ERR_UNSUPPORTED (D).
+ */
+spv_status spv_rope(void* stream, const spv_rope_params* p, const int32_t* coords, const int64_t* m_dev, int64_t n,
+                    const void* q, int64_t ldq, int32_t H, const void* k, int64_t ldk, int32_t Hkv,
+                    void* q_out, int64_t ldqo, void* k_out, int64_t ldko, int32_t inverse, spv_dtype dt);
+
+/* Rows in 8 bits, for the activations that a backward pass reads again.  A block is 32
+ * channels of a row (the last one may be shorter) and has one exponent byte:
+ *   E = max(floor(log2 max |x|) - 6, E0),  E0 = -126 (f16: -24),  exps = E + 127,
+ *   code = x 2^-E to the nearest whole number (ties to even), in -127 .. 127;
+ *   what is read back is code * 2^E, exact in the type it came from.
+ * The maximum is over the block's finite values; a value that is not finite has code
+ * -128 and reads as NaN.  A value is off by 2^E / 2 at most, by 2^E above 127.5 2^E:
+ * at most 2^-6 of the block's largest.  E0 is where 2^E and 127 * 2^E stop being
+ * exact in the type: smaller values fade out. */
+#define SPV_CHECKPOINT8_BLOCK 32
+
+/*
+ * spv_checkpoint8 -- rows into 8 bits.
+ * In:  x [m_cap][C] (dt); m_dev: device row count (NULL = m_cap).
+ * Out: codes [m_cap][C] i8, exps [m_cap][ceil(C / 32)] u8 (rows < count).
+ * spv_checkpoint8_read -- back: out [m_cap][C], in the type dt that they came from (a
+ * code that is too large for another type is infinite in it).
+ * Any width; 16-byte aligned rows of a multiple of 8 channels are moved in wide
+ * accesses.  No workspace.
+ * Errors: SPV_ERR_INVALID_ARG (null pointers, sizes, x = out of another kind).
+ */
+spv_status spv_checkpoint8(void* stream, const void* x, const int64_t* m_dev, int64_t m_cap, int32_t C,
+                           int8_t* codes, uint8_t* exps, spv_dtype dt);
+spv_status spv_checkpoint8_read(void* stream, const int8_t* codes, const uint8_t* exps, const int64_t* m_dev,
+                                int64_t m_cap, int32_t C, void* out, spv_dtype dt);
+
+/*
+ * spv_linear_backward8 -- the weight gradient of a linear layer whose input rows were
+ * kept in 8 bits (spv_linear_backward's dW, from codes):
+ *   dW = in^T @ da (float32),  in = what spv_checkpoint8_read gives.
+ * 16-bit types run on matrix cores, to which the rows' values and da go as they are
+ * (both exact in the type), float32 on those for float32; sums are float32 over a workgroup's
+ * rows, and the workgroups' are added in fp64 in a fixed order: the same bits on every call.
+ * In:  codes [m_cap][Cin], exps [m_cap][ceil(Cin / 32)]; m_dev: device row count
+ *      (NULL = m_cap); da [m_cap][Cout] (dt).
+ * Out: dW [Cin][Cout] f32, all of it (0 without rows).
+ *      ws: spv_linear_backward8_workspace_bytes(m_cap, Cin, Cout) bytes, 256-byte aligned.
+ * Errors: SPV_ERR_INVALID_ARG, SPV_ERR_CAPACITY, SPV_ERR_UNSUPPORTED (Cin * Cout > 2^20).
+ */
+size_t spv_linear_backward8_workspace_bytes(int64_t m_cap, int32_t Cin, int32_t Cout);
+spv_status spv_linear_backward8(void* stream, void* ws, size_t ws_bytes, const int8_t* codes, const uint8_t* exps,
+                                const int64_t* m_dev, int64_t m_cap, int32_t Cin, const void* da, int32_t Cout,
+                                float* dW, spv_dtype dt);
+
+typedef enum spv_act {
+    SPV_ACT_NONE = 0,
+    SPV_ACT_RELU = 1, /* z > 0 ? z : 0, NaN stays; its derivative at 0 is 0 */
+    SPV_ACT_SILU = 2  /* z / (1 + exp(-z)) */
+} spv_act;
+
+/*
+ * spv_group_norm -- group norm of packed scans with an activation: over the rows of
+ * scan b (off[b] .. off[b+1] - 1) and the C / G channels of group g together,
+ *   out = act((x - mu_bg) * r_bg * gamma[c] + beta[c]),
+ *   mu = mean x,  r = 1 / sqrt(mean (x - mu)^2 + eps)
+ * float32, with deviations from the rows' own running mean (no cancellation where a
+ * scan sits far from zero), joined in fp64; one rounding to dt.  G = 1: one mean a
+ * scan; G = C: one a scan and channel; off = {0, m}: all rows together.
+ * In:  x [m][C] (dt); off [B + 1] i32 device, ascending (clamped to [0, m]); gamma,
+ *      beta [C] f32 or NULL (1, 0); eps > 0, finite; C a multiple of G.
+ * Out: out [m][C] (dt; may be x), rows of no scan not written; stat [B][G][2] f32 or
+ *      NULL: mu and r, the backward's input (0 for a scan without rows); codes, exps:
+ *      x in 8 bits as spv_checkpoint8 gives it (rows of a scan), or both NULL.
+ *      ws: spv_group_norm_workspace_bytes(m, C, G, B) bytes, 256-byte aligned.
+ * Errors: SPV_ERR_INVALID_ARG (null pointers, sizes, eps, act, C % G,
+ *      aliasing), SPV_ERR_CAPACITY, SPV_ERR_UNSUPPORTED (C > 65536, B > 2^24).
+ *
+ * spv_group_norm_backward -- with xh = (x - mu) r, z = xh gamma + beta, gz = dy act'(z),
+ * h = gz gamma and means over a scan's rows and a group's channels:
+ *   dx = r (h - mean h - xh mean(h xh)) (+ dres),  dgamma[c] = sum gz xh,  dbeta[c] = sum gz
+ * mu and r are the forward's (stat); x is given as it was, or in 8 bits (codes and
+ * exps, x NULL), which is what the rows' values then are everywhere above.  Float32 sums of a workgroup's rows,
+ * added in fp64 in a fixed order: the same bits on every call.
+ * In:  dy, dres (or NULL) [m][C] (dt).
+ * Out: dx [m][C] (dt; may be dy or dres; rows of no scan not written), dgamma, dbeta
+ *      [C] f32 (0 without rows); any may be NULL.
+ *      ws: spv_group_norm_backward_workspace_bytes(m, C, G, B) bytes.
+ * Errors: as spv_group_norm; x and codes both given or both missing.
+ */
+size_t spv_group_norm_workspace_bytes(int64_t m, int32_t C, int32_t G, int32_t B);
+spv_status spv_group_norm(void* stream, void* ws, size_t ws_bytes, const void* x, int64_t m, int32_t C,
+                          const int32_t* off, int32_t B, int32_t G, const float* gamma, const float* beta, float eps,
+                          spv_act act, void* out, float* stat, int8_t* codes, uint8_t* exps, spv_dtype dt);
+size_t spv_group_norm_backward_workspace_bytes(int64_t m, int32_t C, int32_t G, int32_t B);
+spv_status spv_group_norm_backward(void* stream, void* ws, size_t ws_bytes, const void* dy, const void* x,
+                                   const int8_t* codes, const uint8_t* exps, int64_t m, int32_t C,
+                                   const int32_t* off, int32_t B, int32_t G, const float* gamma, const float* beta,
+                                   const float* stat, spv_act act, const void* dres, void* dx, float* dgamma,
+                                   float* dbeta, spv_dtype dt);
+
 /* Parameters of the SPVConv block (Fig. 2): voxel branch = voxelize, n_convs
  * submanifold 3x3x3 convs C->C, each act(scale * conv + shift); point branch =
  * act(scale_p * (f @ Wp) + shift_p); fused by addition after devoxelization. */

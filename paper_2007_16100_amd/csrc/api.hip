@@ -887,6 +887,158 @@ spv_status spv_attention_backward(void* stream, void* ws, size_t ws_bytes, const
     return hip_check();
 }
 
+// one side of a rotation: an output that is its own input has the same stride
+static bool rope_side_ok(const void* in, int64_t ld, const void* out, int64_t ldo, int64_t channels, int64_t n,
+                         spv_dtype dt) {
+    if (!row_stride_ok(ld, channels, dt) || !row_stride_ok(ldo, channels, dt)) return false;
+    if ((n > 0 && (!in || !out)) || !aligned16(in) || !aligned16(out)) return false;
+    return !in || in != out || ld == ldo;
+}
+
+spv_status spv_rope(void* stream, const spv_rope_params* p, const int32_t* coords, const int64_t* m_dev, int64_t n,
+                    const void* q, int64_t ldq, int32_t H, const void* k, int64_t ldk, int32_t Hkv, void* q_out,
+                    int64_t ldqo, void* k_out, int64_t ldko, int32_t inverse, spv_dtype dt) {
+    if (!p || !valid_dt(dt) || H <= 0 || Hkv < 0 || H > 65535 || Hkv > 65535 || p->D <= 0 || n < 0 ||
+        n >= ((int64_t)1 << 31))
+        return SPV_ERR_INVALID_ARG;
+    if (p->D % 8 || p->D > 128) return SPV_ERR_UNSUPPORTED;
+    int64_t P = 0;
+    for (int a = 0; a < 3; ++a) {
+        if (p->sections[a] < 0) return SPV_ERR_INVALID_ARG;
+        P += p->sections[a];
+    }
+    if (P < 1 || 2 * P > p->D || !p->freqs) return SPV_ERR_INVALID_ARG;
+    if ((n > 0 && !coords) || !aligned16(coords)) return SPV_ERR_INVALID_ARG;
+    if (!rope_side_ok(q, ldq, q_out, ldqo, (int64_t)H * p->D, n, dt)) return SPV_ERR_INVALID_ARG;
+    if (Hkv > 0 && !rope_side_ok(k, ldk, k_out, ldko, (int64_t)Hkv * p->D, n, dt)) return SPV_ERR_INVALID_ARG;
+    if (Hkv == 0 && (k || k_out)) return SPV_ERR_INVALID_ARG;
+    if (Hkv > 0 && n > 0 && (q_out == k_out || q_out == k || k_out == q)) return SPV_ERR_INVALID_ARG;
+    if (n == 0) return SPV_OK;
+    RopeArgs a{{q, q_out, ldq, ldqo, H}, {k, k_out, ldk, ldko, Hkv}, coords, p->freqs, m_dev, n, p->D, (int)P,
+               p->sections[0], p->sections[1], p->halves != 0, inverse != 0, (int)dt};
+    launch_rope((hipStream_t)stream, a);
+    return hip_check();
+}
+
+static bool rows_ok(int64_t m, int32_t C, spv_dtype dt) {
+    return m >= 0 && m < ((int64_t)1 << 31) && C > 0 && valid_dt(dt);
+}
+
+spv_status spv_checkpoint8(void* stream, const void* x, const int64_t* m_dev, int64_t m_cap, int32_t C, int8_t* codes,
+                           uint8_t* exps, spv_dtype dt) {
+    if (!rows_ok(m_cap, C, dt)) return SPV_ERR_INVALID_ARG;
+    if (m_cap == 0) return SPV_OK;
+    if (!x || !codes || !exps || x == (const void*)codes || x == (const void*)exps || (void*)codes == (void*)exps)
+        return SPV_ERR_INVALID_ARG;
+    launch_checkpoint8((hipStream_t)stream, x, Saved8{codes, exps}, RowRange{m_cap, m_dev, nullptr, 0}, C, (int)dt);
+    return hip_check();
+}
+
+spv_status spv_checkpoint8_read(void* stream, const int8_t* codes, const uint8_t* exps, const int64_t* m_dev,
+                                int64_t m_cap, int32_t C, void* out, spv_dtype dt) {
+    if (!rows_ok(m_cap, C, dt)) return SPV_ERR_INVALID_ARG;
+    if (m_cap == 0) return SPV_OK;
+    if (!out || !codes || !exps || out == (const void*)codes || out == (const void*)exps) return SPV_ERR_INVALID_ARG;
+    launch_checkpoint8_read((hipStream_t)stream, Saved8{const_cast<int8_t*>(codes), const_cast<uint8_t*>(exps)}, out,
+                            m_dev, m_cap, C, (int)dt);
+    return hip_check();
+}
+
+size_t spv_linear_backward8_workspace_bytes(int64_t m_cap, int32_t Cin, int32_t Cout) {
+    if (!rows_ok(m_cap, Cin, SPV_F32) || Cout <= 0 || (int64_t)Cin * Cout > (1 << 20)) return 0;
+    Arena a(nullptr, 0);
+    plan_wgrad8_ws(a, m_cap, Cin, Cout);
+    return a.used;
+}
+
+spv_status spv_linear_backward8(void* stream, void* ws, size_t ws_bytes, const int8_t* codes, const uint8_t* exps,
+                                const int64_t* m_dev, int64_t m_cap, int32_t Cin, const void* da, int32_t Cout,
+                                float* dW, spv_dtype dt) {
+    if (!rows_ok(m_cap, Cin, dt) || Cout <= 0 || !dW || !ws_ok(ws)) return SPV_ERR_INVALID_ARG;
+    if ((int64_t)Cin * Cout > (1 << 20)) return SPV_ERR_UNSUPPORTED;
+    if (m_cap > 0 && (!codes || !exps || !da || (const void*)dW == da || (const void*)dW == (const void*)codes ||
+                      (const void*)dW == (const void*)exps))
+        return SPV_ERR_INVALID_ARG;
+    if (need(spv_linear_backward8_workspace_bytes(m_cap, Cin, Cout), ws_bytes)) return SPV_ERR_CAPACITY;
+    Arena a(ws, ws_bytes);
+    Wgrad8Args t{{const_cast<int8_t*>(codes), const_cast<uint8_t*>(exps)}, m_dev, m_cap, Cin, Cout, (int)dt, da, dW,
+                 plan_wgrad8_ws(a, m_cap, Cin, Cout)};
+    launch_wgrad8((hipStream_t)stream, t);
+    return hip_check();
+}
+
+// sizes that both directions of the group norm take
+static spv_status group_norm_sizes(int64_t m, int32_t C, int32_t G, int32_t B, spv_dtype dt) {
+    if (!rows_ok(m, C, dt) || G <= 0 || C % G || B < 0) return SPV_ERR_INVALID_ARG;
+    return C > 65536 || B > (1 << 24) ? SPV_ERR_UNSUPPORTED : SPV_OK;
+}
+static GnArgs group_norm_args(int64_t m, int32_t C, int32_t G, int32_t B, spv_dtype dt) {
+    GnArgs t{};
+    t.m = m, t.C = C, t.G = G, t.B = B, t.dt = (int)dt;
+    return t;
+}
+
+size_t spv_group_norm_workspace_bytes(int64_t m, int32_t C, int32_t G, int32_t B) {
+    if (group_norm_sizes(m, C, G, B, SPV_F32) != SPV_OK) return 0;
+    GnArgs t = group_norm_args(m, C, G, B, SPV_F32);
+    Arena a(nullptr, 0);
+    plan_group_norm_ws(a, t);
+    return a.used;
+}
+
+spv_status spv_group_norm(void* stream, void* ws, size_t ws_bytes, const void* x, int64_t m, int32_t C,
+                          const int32_t* off, int32_t B, int32_t G, const float* gamma, const float* beta, float eps,
+                          spv_act act, void* out, float* stat, int8_t* codes, uint8_t* exps, spv_dtype dt) {
+    const spv_status st = group_norm_sizes(m, C, G, B, dt);
+    if (st != SPV_OK) return st;
+    if (!valid_v(eps) || (int)act < SPV_ACT_NONE || (int)act > SPV_ACT_SILU || (B > 0 && !off) || !ws_ok(ws))
+        return SPV_ERR_INVALID_ARG;
+    if (m > 0 && (!x || !out)) return SPV_ERR_INVALID_ARG;
+    if (!codes != !exps || (codes && ((void*)codes == (void*)exps || x == (void*)codes || x == (void*)exps ||
+                                      out == (void*)codes || out == (void*)exps)))
+        return SPV_ERR_INVALID_ARG;
+    if (need(spv_group_norm_workspace_bytes(m, C, G, B), ws_bytes)) return SPV_ERR_CAPACITY;
+    if (B == 0) return SPV_OK;
+    GnArgs t = group_norm_args(m, C, G, B, dt);
+    t.x = x, t.saved = Saved8{codes, exps}, t.off = off, t.gamma = gamma, t.beta = beta, t.eps = eps, t.act = (int)act;
+    t.out = out, t.stat = stat;
+    Arena a(ws, ws_bytes);
+    plan_group_norm_ws(a, t);
+    launch_group_norm((hipStream_t)stream, t);
+    return hip_check();
+}
+
+size_t spv_group_norm_backward_workspace_bytes(int64_t m, int32_t C, int32_t G, int32_t B) {
+    if (group_norm_sizes(m, C, G, B, SPV_F32) != SPV_OK) return 0;
+    GnArgs t = group_norm_args(m, C, G, B, SPV_F32);
+    Arena a(nullptr, 0);
+    plan_group_norm_backward_ws(a, t);
+    return a.used;
+}
+
+spv_status spv_group_norm_backward(void* stream, void* ws, size_t ws_bytes, const void* dy, const void* x,
+                                   const int8_t* codes, const uint8_t* exps, int64_t m, int32_t C, const int32_t* off,
+                                   int32_t B, int32_t G, const float* gamma, const float* beta, const float* stat,
+                                   spv_act act, const void* dres, void* dx, float* dgamma, float* dbeta,
+                                   spv_dtype dt) {
+    const spv_status st = group_norm_sizes(m, C, G, B, dt);
+    if (st != SPV_OK) return st;
+    if ((int)act < SPV_ACT_NONE || (int)act > SPV_ACT_SILU || (B > 0 && (!off || !stat)) || !ws_ok(ws))
+        return SPV_ERR_INVALID_ARG;
+    if (!codes != !exps || (m > 0 && (!dy || !x == !codes))) return SPV_ERR_INVALID_ARG;
+    if (dx && (dx == x || dx == (const void*)codes || dx == (const void*)exps)) return SPV_ERR_INVALID_ARG;
+    if (need(spv_group_norm_backward_workspace_bytes(m, C, G, B), ws_bytes)) return SPV_ERR_CAPACITY;
+    if (!dx && !dgamma && !dbeta) return SPV_OK;
+    GnArgs t = group_norm_args(m, C, G, B, dt);
+    t.x = x, t.saved = Saved8{const_cast<int8_t*>(codes), const_cast<uint8_t*>(exps)}, t.off = off;
+    t.gamma = gamma, t.beta = beta, t.stat = const_cast<float*>(stat), t.act = (int)act;
+    t.dy = dy, t.dres = dres, t.dx = dx, t.dgamma = dgamma, t.dbeta = dbeta;
+    Arena a(ws, ws_bytes);
+    plan_group_norm_backward_ws(a, t);
+    launch_group_norm_backward((hipStream_t)stream, t);
+    return hip_check();
+}
+
 size_t spv_devoxelize_backward_workspace_bytes(int64_t n, int64_t m) {
     if (n < 0 || m < 0) return 0;
     Arena a(nullptr, 0);

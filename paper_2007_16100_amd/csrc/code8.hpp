@@ -1,0 +1,34 @@
+// code8.hpp -- rows in 8 bits: an exponent for each 32 channels of a row, codes of -127 .. 127 in steps of 2^E.
+#pragma once
+
+#include "conv_common.hpp"
+
+namespace spv {
+
+constexpr int kCodeBlock = SPV_CHECKPOINT8_BLOCK;
+__host__ __device__ inline int code_blocks(int C) { return (C + kCodeBlock - 1) / kCodeBlock; }
+
+// |x| where x is finite, else 0, as bits (which order as the values do)
+__device__ inline uint32_t finite_bits(float x) {
+    const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
+    return b < 0x7F800000u ? b : 0u;
+}
+// the exponent byte of a block whose largest finite |x| has these bits: a subnormal maximum counts as 2^-127
+template <int DT>
+__device__ inline int code_exp(uint32_t top) {
+    const int e = (int)(top >> 23) - 6, lowest = DT == SPV_F16 ? 127 - 24 : 1;
+    return e < lowest ? lowest : e;
+}
+// 2^(byte - 127) and its inverse, for bytes 1 .. 248
+__device__ inline float code_step(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+__device__ inline float code_rate(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
+// the code of x: products by a power of two are exact
+__device__ inline int code_of(float x, float rate) {
+    const float q = fminf(fmaxf(rintf(x * rate), -127.f), 127.f);
+    return finite_bits(x) == 0u && x != 0.f ? -128 : (int)q;
+}
+__device__ inline float code_value(int code, float step) {
+    return code == -128 ? __uint_as_float(0x7FC00000u) : (float)code * step;
+}
+
+}  // namespace spv

@@ -509,6 +509,74 @@ void launch_attention(hipStream_t s, const AttnArgs& a);
 void plan_attention_backward_ws(Arena& a, AttnArgs& t);
 void launch_attention_backward(hipStream_t s, const AttnArgs& a);
 
+// --- rotary positions (rope.hip) --------------------------------------------------------
+struct RopeSide {
+    const void* in;             // [n][ld], head h at h * D
+    void* out;                  // [n][ldo]
+    int64_t ld, ldo;
+    int heads;                  // 0: none
+};
+struct RopeArgs {
+    RopeSide q, k;
+    const int32_t* coords;      // [n][4]
+    const float* freqs;         // [P]
+    const int64_t* m_dev;
+    int64_t n;
+    int D, P, sx, sy;           // pairs in all, of x and of y
+    int halves, inverse, dt;
+};
+void launch_rope(hipStream_t s, const RopeArgs& a);
+
+// --- rows in 8 bits (checkpoint8.hip) -----------------------------------------------------
+struct Saved8 {
+    int8_t* codes;              // [m][C]
+    uint8_t* exps;              // [m][ceil(C / 32)]
+};
+// the first *m_dev of cap rows, or with off the rows off[0] .. off[B] - 1
+struct RowRange {
+    int64_t cap;
+    const int64_t* m_dev;
+    const int32_t* off;
+    int B;
+    __device__ int64_t begin() const;
+    __device__ int64_t end() const;
+};
+void launch_checkpoint8(hipStream_t s, const void* x, Saved8 to, const RowRange& rows, int C, int dt);
+void launch_checkpoint8_read(hipStream_t s, Saved8 from, void* out, const int64_t* m_dev, int64_t m_cap, int C, int dt);
+struct Wgrad8Args {
+    Saved8 in;
+    const int64_t* m_dev;
+    int64_t m_cap;
+    int Cin, Cout, dt;
+    const void* da;             // [m][Cout]
+    float* dW;                  // [Cin][Cout]
+    float* part;                // [workgroups][Cin][Cout]
+};
+float* plan_wgrad8_ws(Arena& a, int64_t m_cap, int Cin, int Cout);
+void launch_wgrad8(hipStream_t s, const Wgrad8Args& a);
+
+// --- group norm over packed scans (group_norm.hip) ----------------------------------------
+struct GnArgs {
+    const void* x;              // [m][C], or nullptr: saved
+    Saved8 saved;               // the backward's x, or the forward's output; codes nullptr: none
+    int64_t m;
+    int C, B, G, dt, act;
+    const int32_t* off;         // [B + 1]
+    const float *gamma, *beta;  // [C] or nullptr (1, 0)
+    float eps;
+    void* out;                  // [m][C]
+    float* stat;                // [B][G][2] mean and 1 / deviation
+    // backward
+    const void *dy, *dres;      // [m][C]; dres may be nullptr
+    void* dx;                   // [m][C] or nullptr
+    float *dgamma, *dbeta;      // [C] or nullptr
+    float* part;                // workspace
+};
+void plan_group_norm_ws(Arena& a, GnArgs& t);
+void launch_group_norm(hipStream_t s, const GnArgs& a);
+void plan_group_norm_backward_ws(Arena& a, GnArgs& t);
+void launch_group_norm_backward(hipStream_t s, const GnArgs& a);
+
 // weight packings a block call runs inside its voxelization's first launch
 constexpr int kMaxPackJobs = 3;
 // the convolution itself (one kernel); wpack must have been packed from W

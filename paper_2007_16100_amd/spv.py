@@ -25,7 +25,9 @@ SPV_OK, SPV_ERR_INVALID_ARG, SPV_ERR_CAPACITY, SPV_ERR_RANGE, SPV_ERR_NONFINITE,
     range(7)
 SPV_F32, SPV_BF16, SPV_F16 = 0, 1, 2
 SPV_DEVOX_CENTER, SPV_DEVOX_CORNER, SPV_DEVOX_NEAREST = 0, 1, 2
+SPV_CHECKPOINT8_BLOCK = 32
 
+_ACT = {"none": 0, "relu": 1, "silu": 2}
 _DT = {torch.float32: SPV_F32, torch.bfloat16: SPV_BF16, torch.float16: SPV_F16}
 
 # every symbol include/spv.h declares
@@ -40,7 +42,10 @@ EXPORTS = ("spv_workspace_bytes", "spv_voxelize", "spv_voxelize_onto", "spv_pack
            "spv_linear_backward_workspace_bytes", "spv_linear_backward",
            "spv_layer_norm", "spv_layer_norm_backward_workspace_bytes", "spv_layer_norm_backward",
            "spv_attention_workspace_bytes", "spv_attention", "spv_attention_backward_workspace_bytes",
-           "spv_attention_backward",
+           "spv_attention_backward", "spv_rope",
+           "spv_checkpoint8", "spv_checkpoint8_read", "spv_linear_backward8_workspace_bytes", "spv_linear_backward8",
+           "spv_group_norm_workspace_bytes", "spv_group_norm", "spv_group_norm_backward_workspace_bytes",
+           "spv_group_norm_backward",
            "spv_block_workspace_bytes", "spv_block", "spv_lookup", "spv_voxel_lookup", "spv_conv_kernel",
            "spv_sparse_conv_nbr_noalloc",
            "spv_block_conv_kernel", "spv_status_check", "spv_status_string", "spv_last_hip_error")
@@ -66,6 +71,10 @@ class AttentionParams(ct.Structure):
     _fields_ = [("H", ct.c_int32), ("Hkv", ct.c_int32), ("D", ct.c_int32), ("B", ct.c_int32), ("scale", ct.c_float),
                 ("cap", ct.c_float), ("q_off", ct.c_void_p), ("k_off", ct.c_void_p), ("q_coords", ct.c_void_p),
                 ("k_coords", ct.c_void_p), ("slopes", ct.c_void_p)]
+
+
+class RopeParams(ct.Structure):
+    _fields_ = [("D", ct.c_int32), ("sections", ct.c_int32 * 3), ("halves", ct.c_int32), ("freqs", ct.c_void_p)]
 
 
 _lib = None
@@ -131,6 +140,19 @@ def lib():
         L.spv_attention.argtypes = [vp, vp, sz, ap, vp, i64, i64, vp, i64, vp, i64, i64, vp, i64, vp, i32]
         L.spv_attention_backward.argtypes = [vp, vp, sz, ap, vp, i64, i64, vp, i64, vp, i64, i64, vp, i64, vp, vp, i64,
                                              vp, i64, vp, i64, vp, i64, i32]
+        L.spv_rope.argtypes = [vp, ct.POINTER(RopeParams), vp, vp, i64, vp, i64, i32, vp, i64, i32, vp, i64, vp, i64, i32,
+                               i32]
+        L.spv_checkpoint8.argtypes = [vp, vp, vp, i64, i32, vp, vp, i32]
+        L.spv_checkpoint8_read.argtypes = [vp, vp, vp, vp, i64, i32, vp, i32]
+        L.spv_linear_backward8_workspace_bytes.argtypes = [i64, i32, i32]
+        L.spv_linear_backward8_workspace_bytes.restype = sz
+        L.spv_linear_backward8.argtypes = [vp, vp, sz, vp, vp, vp, i64, i32, vp, i32, vp, i32]
+        for f in ("spv_group_norm_workspace_bytes", "spv_group_norm_backward_workspace_bytes"):
+            getattr(L, f).argtypes = [i64, i32, i32, i32]
+            getattr(L, f).restype = sz
+        L.spv_group_norm.argtypes = [vp, vp, sz, vp, i64, i32, vp, i32, i32, vp, vp, f32, i32, vp, vp, vp, vp, i32]
+        L.spv_group_norm_backward.argtypes = [vp, vp, sz, vp, vp, vp, vp, i64, i32, vp, i32, i32, vp, vp, vp, i32, vp,
+                                              vp, vp, vp, i32]
         L.spv_devoxelize.argtypes = [vp, vp, sz, vp, vp, i64, i32, vp, vp, i64, f32, i32, vp, i32, vp, i32, vp, vp,
                                      vp, i32, vp, i32, vp, vp]
         L.spv_devoxelize_nbr.argtypes = [vp, vp, sz, vp, vp, i64, vp, vp, i32, vp, vp, i64, f32, i32, vp, i32, vp,
@@ -154,8 +176,9 @@ def lib():
                   "spv_sparse_conv_dgrad", "spv_sparse_conv_dgrad_nbr", "spv_sparse_conv_wgrad",
                   "spv_voxelize_backward",
                   "spv_devoxelize_backward", "spv_epilogue_backward", "spv_linear_backward", "spv_devoxelize",
-                  "spv_layer_norm", "spv_layer_norm_backward", "spv_attention", "spv_attention_backward",
-                  "spv_block", "spv_lookup", "spv_voxel_lookup",
+                  "spv_layer_norm", "spv_layer_norm_backward", "spv_attention", "spv_attention_backward", "spv_rope",
+                  "spv_checkpoint8", "spv_checkpoint8_read", "spv_linear_backward8", "spv_group_norm",
+                  "spv_group_norm_backward", "spv_block", "spv_lookup", "spv_voxel_lookup",
                   "spv_sparse_conv_nbr_noalloc", "spv_status_check"):
             getattr(L, f).restype = ct.c_int
         _lib = L
@@ -241,6 +264,20 @@ class Workspace:
         need = max(lib().spv_attention_workspace_bytes(ct.byref(params), nq, nk, _DT[dtype]),
                    lib().spv_attention_backward_workspace_bytes(ct.byref(params), nq, nk, _DT[dtype]))
         return cls(need, device)
+
+    @classmethod
+    def for_linear_backward8(cls, m: int, Cin: int, Cout: int, device="cuda"):
+        return cls(lib().spv_linear_backward8_workspace_bytes(m, Cin, Cout), device)
+
+    @classmethod
+    def for_group_norm(cls, m: int, C: int, groups: int, scans: int, device="cuda"):
+        return cls(lib().spv_group_norm_workspace_bytes(m, C, groups, scans), device)
+
+    @classmethod
+    def for_group_norm_backward(cls, m: int, C: int, groups: int, scans: int, device="cuda"):
+        """Serves the forward call of the same sizes too."""
+        return cls(max(lib().spv_group_norm_workspace_bytes(m, C, groups, scans),
+                       lib().spv_group_norm_backward_workspace_bytes(m, C, groups, scans)), device)
 
     @classmethod
     def for_block(cls, max_points: int, C: int, device="cuda"):
@@ -788,6 +825,196 @@ def spv_attention_backward(ws: Workspace, params: AttentionParams, q: torch.Tens
                                       lddo, dq, lddq, dk, lddk, dv, lddv, _DT[dt])
     _chk(st, "spv_attention_backward")
     return tuple(grads)
+
+
+def make_rope_params(D: int, freqs: torch.Tensor, sections: Sequence[int], halves: bool = False) -> RopeParams:
+    """Parameters of a rotation of heads of D channels by voxel coordinates: sections = pairs of channels that turn
+    with x, y and z; freqs [their sum] float32, radians a voxel.  Pair p is channels (2 p, 2 p + 1), or with halves
+    (p, p + pairs).  The struct keeps a reference to freqs."""
+    if len(sections) != 3:
+        raise ValueError("sections are the pairs of x, y and z")
+    p = RopeParams(D, (ct.c_int32 * 3)(*sections), int(halves), _channels(freqs, sum(sections), "freqs"))
+    p._keep = freqs
+    return p
+
+
+def rope_freqs(sections: Sequence[int], longest: float = 100.0, device="cuda") -> torch.Tensor:
+    """Radians a voxel of the pairs of each axis: from 1 down towards 1 / longest, evenly in their logarithms."""
+    return torch.tensor([longest ** (-i / s) for s in sections for i in range(s)], dtype=torch.float32, device=device)
+
+
+def spv_rope(params: RopeParams, coords: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None,
+             inverse: bool = False, m_dev: Optional[torch.Tensor] = None,
+             outs: Optional[Sequence[torch.Tensor]] = None):
+    """q [n][H][D] (and k [n][Hkv][D]) rotated by the rows' coordinates [n][4]: q' or (q', k').  inverse: the
+    rotation back, which turns gradients of the rotated rows into the rows'.  q, k and outs (the tensors to write, which
+    may be q and k themselves) may be parts of wider rows."""
+    D, dt = params.D, q.dtype
+    sides = [q] if k is None else [q, k]
+    if outs is None:
+        outs = [torch.empty(t.shape, dtype=dt, device=t.device) for t in sides]
+    if len(outs) != len(sides) or any(o.shape != t.shape for o, t in zip(outs, sides)):
+        raise ValueError("outs must have the shapes of what is rotated")
+    n, qp, ldq = _heads(q, q.shape[1], D, dt, "q")
+    _, qo, ldqo = _heads(outs[0], q.shape[1], D, dt, "outs")
+    if coords.dtype != torch.int32 or coords.dim() != 2 or coords.shape[1] != 4 or coords.shape[0] < n:
+        raise ValueError(f"coords must be int32 [{n}][4]")
+    kp = ko = None
+    K = ldk = ldko = 0
+    if k is not None:
+        K = k.shape[1]
+        nk, kp, ldk = _heads(k, K, D, dt, "k")
+        _, ko, ldko = _heads(outs[1], K, D, dt, "outs")
+        if nk != n:
+            raise ValueError("q and k must have the same rows")
+    cp, count = _addr(coords), _count(m_dev)
+    st = lib().spv_rope(_stream(), ct.byref(params), cp, count, n, qp, ldq, q.shape[1], kp, ldk, K, qo, ldqo, ko, ldko,
+                        int(inverse), _DT[dt])
+    _chk(st, "spv_rope")
+    return outs[0] if k is None else tuple(outs)
+
+
+def _count(t: Optional[torch.Tensor]):
+    """Address of a device row count."""
+    if t is not None and (t.dtype != torch.int64 or t.numel() < 1):
+        raise ValueError("a row count is int64 [1]")
+    return _addr(t)
+
+
+@dataclass
+class Checkpoint8:
+    """Rows in 8 bits, as spv_checkpoint8 and spv_group_norm give them."""
+    codes: torch.Tensor     # [m, C] int8
+    exps: torch.Tensor      # [m, ceil(C / 32)] uint8
+    dtype: torch.dtype      # of the rows they came from
+
+    @classmethod
+    def empty(cls, m: int, C: int, dtype: torch.dtype, device="cuda"):
+        blocks = (C + SPV_CHECKPOINT8_BLOCK - 1) // SPV_CHECKPOINT8_BLOCK
+        return cls(torch.empty((m, C), dtype=torch.int8, device=device),
+                   torch.empty((m, blocks), dtype=torch.uint8, device=device), dtype)
+
+    def addresses(self):
+        m, C = self.codes.shape
+        if self.codes.dtype != torch.int8 or self.exps.dtype != torch.uint8 or \
+                self.exps.shape != (m, (C + SPV_CHECKPOINT8_BLOCK - 1) // SPV_CHECKPOINT8_BLOCK):
+            raise ValueError("a checkpoint is int8 [rows][channels] with uint8 [rows][blocks of 32 channels]")
+        return _addr(self.codes), _addr(self.exps)
+
+
+def spv_checkpoint8(x: torch.Tensor, m_dev: Optional[torch.Tensor] = None,
+                    out: Optional[Checkpoint8] = None) -> Checkpoint8:
+    """The rows x [m][C] in 8 bits, with an exponent for each 32 channels of a row."""
+    m, C = x.shape
+    if out is None:
+        out = Checkpoint8.empty(m, C, x.dtype, x.device)
+    elif out.codes.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("out must have x's shape and type")
+    codes, exps = out.addresses()
+    xp, count = _addr(x), _count(m_dev)
+    st = lib().spv_checkpoint8(_stream(), xp, count, m, C, codes, exps, _DT[x.dtype])
+    _chk(st, "spv_checkpoint8")
+    return out
+
+
+def spv_checkpoint8_read(saved: Checkpoint8, m_dev: Optional[torch.Tensor] = None,
+                         out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The rows [m][C] that a checkpoint stands for, in the type they came from."""
+    codes, exps = saved.addresses()
+    m, C = saved.codes.shape
+    if out is None:
+        out = torch.empty((m, C), dtype=saved.dtype, device=saved.codes.device)
+    elif out.shape != (m, C) or out.dtype != saved.dtype:
+        raise ValueError("out must have the rows' shape and type")
+    op, count = _addr(out), _count(m_dev)
+    st = lib().spv_checkpoint8_read(_stream(), codes, exps, count, m, C, op, _DT[saved.dtype])
+    _chk(st, "spv_checkpoint8_read")
+    return out
+
+
+def spv_linear_backward8(ws: Workspace, saved: Checkpoint8, da: torch.Tensor, m_dev: Optional[torch.Tensor] = None,
+                         out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dW [Cin][Cout] float32 of a linear layer whose input rows were kept in 8 bits, given its product's gradient
+    da [m][Cout]."""
+    codes, exps = saved.addresses()
+    m, Cin = saved.codes.shape
+    if da.dim() != 2 or da.shape[0] != m or da.dtype != saved.dtype:
+        raise ValueError(f"da must be [{m}][Cout] of {saved.dtype}")
+    Cout = da.shape[1]
+    if out is None:
+        out = torch.empty((Cin, Cout), dtype=torch.float32, device=da.device)
+    elif out.shape != (Cin, Cout) or out.dtype != torch.float32:
+        raise ValueError(f"out must be float32 [{Cin}][{Cout}]")
+    dap, op, count = _addr(da), _addr(out), _count(m_dev)
+    st = lib().spv_linear_backward8(_stream(), ws.ptr, ws.nbytes, codes, exps, count, m, Cin, dap, Cout, op,
+                                    _DT[da.dtype])
+    _chk(st, "spv_linear_backward8")
+    return out
+
+
+def _scans(off: torch.Tensor) -> int:
+    if off.dtype != torch.int32 or off.dim() != 1 or off.shape[0] < 1:
+        raise ValueError("off must be int32 [scans + 1]")
+    return off.shape[0] - 1
+
+
+def spv_group_norm(ws: Workspace, x: torch.Tensor, off: torch.Tensor, groups: int,
+                   gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                   act: str = "none", want_stat: bool = False, want_checkpoint: bool = False,
+                   out: Optional[torch.Tensor] = None):
+    """act(group norm) of x [m][C] over the rows of each scan (off [scans + 1]) and the channels of each of `groups`
+    groups; act is "none", "relu" or "silu".  y, or (y, stat), (y, checkpoint) or (y, stat, checkpoint): stat
+    [scans][groups][2] and either x or its checkpoint in 8 bits are what the backward reads."""
+    m, C = x.shape
+    B = _scans(off)
+    if act not in _ACT:
+        raise ValueError(f"act must be one of {', '.join(_ACT)}")
+    xp, gp, bp = _addr(x), _channels(gamma, C, "gamma"), _channels(beta, C, "beta")
+    if out is None:
+        out = torch.empty_like(x)
+    elif out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("out must have x's shape and type")
+    stat = torch.empty((B, groups, 2), dtype=torch.float32, device=x.device) if want_stat else None
+    saved = Checkpoint8.empty(m, C, x.dtype, x.device) if want_checkpoint else None
+    codes, exps = saved.addresses() if saved is not None else (None, None)
+    st = lib().spv_group_norm(_stream(), ws.ptr, ws.nbytes, xp, m, C, _addr(off), B, groups, gp, bp, eps, _ACT[act],
+                              _addr(out), _addr(stat), codes, exps, _DT[x.dtype])
+    _chk(st, "spv_group_norm")
+    got = (out, *(t for t in (stat, saved) if t is not None))
+    return got if len(got) > 1 else out
+
+
+def spv_group_norm_backward(ws: Workspace, dy: torch.Tensor, x, off: torch.Tensor, groups: int, stat: torch.Tensor,
+                            gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                            act: str = "none", dres: Optional[torch.Tensor] = None):
+    """(dx, dgamma, dbeta) of spv_group_norm, given its stat and x or x's checkpoint; dres: a gradient added to dx (the
+    residual branch's)."""
+    m, C = dy.shape
+    B = _scans(off)
+    if act not in _ACT:
+        raise ValueError(f"act must be one of {', '.join(_ACT)}")
+    codes = exps = xp = None
+    if isinstance(x, Checkpoint8):
+        if x.codes.shape != dy.shape or x.dtype != dy.dtype:
+            raise ValueError("the checkpoint must have dy's shape and type")
+        codes, exps = x.addresses()
+    else:
+        if x.shape != dy.shape or x.dtype != dy.dtype:
+            raise ValueError("x must have dy's shape and type")
+        xp = _addr(x)
+    if dres is not None and (dres.shape != dy.shape or dres.dtype != dy.dtype):
+        raise ValueError("dres must have dy's shape and type")
+    if stat.dtype != torch.float32 or stat.shape != (B, groups, 2):
+        raise ValueError(f"stat must be float32 [{B}][{groups}][2]")
+    gp, bp = _channels(gamma, C, "gamma"), _channels(beta, C, "beta")
+    dx = torch.empty_like(dy)
+    dgamma = torch.empty(C, dtype=torch.float32, device=dy.device)
+    dbeta = torch.empty_like(dgamma)
+    st = lib().spv_group_norm_backward(_stream(), ws.ptr, ws.nbytes, _addr(dy), xp, codes, exps, m, C, _addr(off), B,
+                                       groups, gp, bp, _addr(stat), _ACT[act], _addr(dres), dx.data_ptr(),
+                                       dgamma.data_ptr(), dbeta.data_ptr(), _DT[dy.dtype])
+    _chk(st, "spv_group_norm_backward")
+    return dx, dgamma, dbeta
 
 
 def spv_devoxelize(ws: Workspace, grid_coords: torch.Tensor, vfeat: torch.Tensor, xyz: torch.Tensor,

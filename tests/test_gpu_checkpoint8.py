@@ -1,0 +1,166 @@
+"""Rows in 8 bits and the weight gradient from them on the GPU: codes bit for bit, sums within bounds derived from the
+kernel's roundings (tests/voxel_ops_ref.py)."""
+import numpy as np
+import pytest
+import torch
+
+from tests import voxel_ops_ref as ref
+
+pytestmark = pytest.mark.gpu
+TD = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def spv():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2007_16100_amd import spv as s
+    s.lib()
+    return s
+
+
+def features(m, C, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(m, C, generator=g) * torch.exp(4 * torch.rand(m, 1, generator=g) - 2)
+    return x.to(TD[dtype]).cuda()
+
+
+def arr(t):
+    return t.detach().double().cpu().numpy()
+
+
+def same(spv, x, saved, dtype):
+    q, e, y = ref.codes(arr(x), dtype)
+    assert np.array_equal(saved.codes.cpu().numpy(), q) and np.array_equal(saved.exps.cpu().numpy(), e)
+    assert np.array_equal(arr(spv.spv_checkpoint8_read(saved)), y, equal_nan=True)
+
+
+SHAPES = [(1, 1), (1, 8), (3, 31), (5, 32), (5, 33), (7, 19), (2, 64), (64, 96), (129, 100), (1000, 96), (33, 40), (257, 256),
+          (9, 520), (3, 2049), (20011, 48), (0, 32)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m,C", SHAPES)
+def test_rows_into_8_bits_and_back(spv, m, C, dtype):
+    print(f"code8 m={m} C={C} {dtype}", flush=True)
+    x = features(m, C, dtype, 3 * m + C)
+    same(spv, x, spv.spv_checkpoint8(x), dtype)
+
+
+@pytest.mark.parametrize("C", [64, 37])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_values_at_the_ends(spv, dtype, C):
+    """Zeros, ties, values past 127.5 steps, the largest and the smallest of the type, and values that are not finite."""
+    td = TD[dtype]
+    info = torch.finfo(td)
+    x = torch.zeros(16, C, dtype=torch.float64)
+    x[1, :] = torch.arange(C, dtype=torch.float64) * 0.5 + 64.0  # ties at steps of 1
+    x[2, :5] = torch.tensor([127.75, 127.5, 127.4, -127.9, 1.0])
+    x[3, :3] = torch.tensor([info.max, -info.max, info.max / 2])
+    x[4, :3] = torch.tensor([info.tiny, -info.tiny / 2, info.smallest_normal])
+    x[5, :2] = torch.tensor([info.smallest_normal * info.eps, -3 * info.smallest_normal * info.eps])
+    x[6, :4] = torch.tensor([float("inf"), 1.0, -2.0, float("nan")])
+    x[7, :] = float("nan")
+    x[8, :] = -float("inf")
+    x[9, C - 1] = 5.0
+    x[10, :2] = torch.tensor([2.0 ** -14, 65504.0 if dtype == "f16" else 2.0 ** 100])
+    x[11, :] = -0.0
+    x = x.to(td).cuda()
+    saved = spv.spv_checkpoint8(x)
+    if dtype != "f16":  # subnormal numbers may count as 0 on either side: they are far below a step of 2^-126
+        assert int(saved.exps[5, 0]) == 1 and int(saved.codes[5].abs().max()) == 0
+    same(spv, x, saved, dtype)
+
+
+@pytest.mark.parametrize("C", [96, 50])
+def test_options(spv, C):
+    """A row count on the device, given outputs, odd pointers, another stream, a graph."""
+    x = features(300, C, "bf16", 1)
+    full = spv.spv_checkpoint8(x)
+    live = torch.tensor([211], dtype=torch.int64, device="cuda")
+    out = spv.Checkpoint8.empty(300, C, torch.bfloat16)
+    out.codes.fill_(3)
+    out.exps.fill_(9)
+    assert spv.spv_checkpoint8(x, m_dev=live, out=out) is out
+    assert torch.equal(out.codes[:211], full.codes[:211]) and bool((out.codes[211:] == 3).all())
+    assert torch.equal(out.exps[:211], full.exps[:211]) and bool((out.exps[211:] == 9).all())
+    y = torch.full_like(x, 7.0)
+    spv.spv_checkpoint8_read(full, m_dev=live, out=y)
+    whole = spv.spv_checkpoint8_read(full)
+    assert torch.equal(y[:211], whole[:211]) and bool((y[211:] == 7.0).all())
+    buf = torch.empty(300 * C + 1, dtype=x.dtype, device="cuda")
+    odd = buf[1:].view(300, C)
+    odd.copy_(x)
+    got = spv.spv_checkpoint8(odd)
+    assert torch.equal(got.codes, full.codes) and torch.equal(got.exps, full.exps)
+    spv.spv_checkpoint8_read(full, out=odd)
+    assert torch.equal(odd, whole)
+    codes = torch.empty(300 * C + 1, dtype=torch.int8, device="cuda")[1:].view(300, C)
+    exps = torch.empty(300 * full.exps.shape[1] + 1, dtype=torch.uint8, device="cuda")[1:].view(full.exps.shape)
+    off = spv.spv_checkpoint8(x, out=spv.Checkpoint8(codes, exps, x.dtype))
+    assert torch.equal(off.codes, full.codes) and torch.equal(off.exps, full.exps)
+    assert torch.equal(spv.spv_checkpoint8_read(off), whole)
+    da = features(300, 64, "bf16", 8)
+    ws = spv.Workspace.for_linear_backward8(300, C, 64)
+    want = spv.spv_linear_backward8(ws, full, da)
+    assert torch.equal(spv.spv_linear_backward8(ws, off, da), want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = spv.spv_linear_backward8(spv.Workspace.for_linear_backward8(300, C, 64), spv.spv_checkpoint8(x), da)
+    side.synchronize()
+    assert torch.equal(other, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        saved = spv.spv_checkpoint8(x)
+        dW = spv.spv_linear_backward8(ws, saved, da)
+        back = spv.spv_checkpoint8_read(saved)
+    for seed in (5, 6, 7):
+        x.copy_(features(300, C, "bf16", seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        now = spv.spv_checkpoint8(x)
+        assert torch.equal(back, spv.spv_checkpoint8_read(now))
+        assert torch.equal(dW, spv.spv_linear_backward8(spv.Workspace.for_linear_backward8(300, C, 64), now, da))
+
+
+WGRAD = [(0, 8, 8), (1, 1, 1), (1, 32, 32), (5, 19, 7), (31, 96, 96), (64, 64, 32), (100, 33, 65), (701, 96, 96), (1000, 128, 19),
+         (3001, 96, 64), (2049, 256, 256), (777, 19, 256), (513, 40, 48), (40, 1024, 1024), (70001, 32, 32), (12345, 160, 224)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m,Cin,Cout", WGRAD)
+def test_weight_gradient(spv, m, Cin, Cout, dtype):
+    print(f"wgrad8 m={m} {Cin} -> {Cout} {dtype}", flush=True)
+    x, da = features(m, Cin, dtype, m + Cin), features(m, Cout, dtype, m + Cout + 1)
+    saved = spv.spv_checkpoint8(x)
+    ws = spv.Workspace.for_linear_backward8(m, Cin, Cout)
+    dW = spv.spv_linear_backward8(ws, saved, da)
+    X, D = ref.codes(arr(x), dtype)[2], arr(da)
+    want = X.T @ D
+    err, tol = np.abs(arr(dW) - want), ref.wgrad_bound(X, D, want)
+    assert np.all(err <= tol), float(np.max(err / np.maximum(tol, 1e-300)))
+    # the roundings are of both signs: their root mean square is far below their sum
+    if m > 100:
+        scale = np.sqrt((X ** 2).T @ (D ** 2))
+        assert np.sqrt(np.mean((err / scale) ** 2)) <= 16 * ref.EPS * np.log2(m)
+    ws.buf.fill_(255)
+    assert torch.equal(spv.spv_linear_backward8(ws, saved, da), dW)
+
+
+@pytest.mark.parametrize("Cin,Cout", [(96, 96), (19, 33)])
+def test_weight_gradient_rows_under_a_device_count_and_nan(spv, Cin, Cout):
+    m, live = 1000, torch.tensor([613], dtype=torch.int64, device="cuda")
+    x, da = features(m, Cin, "bf16", 1), features(m, Cout, "bf16", 2)
+    ws = spv.Workspace.for_linear_backward8(m, Cin, Cout)
+    saved = spv.spv_checkpoint8(x)
+    da[613:] = float("nan")
+    got = spv.spv_linear_backward8(ws, saved, da, m_dev=live)
+    X, D = ref.codes(arr(x), "bf16")[2][:613], arr(da)[:613]
+    assert np.all(np.abs(arr(got) - X.T @ D) <= ref.wgrad_bound(X, D, X.T @ D))
+    live.zero_()
+    assert not bool(spv.spv_linear_backward8(ws, saved, da, m_dev=live).any())
+    # a value that is not finite reaches its own channel alone
+    x[5, 3], da[613:] = float("inf"), 0.0
+    got = spv.spv_linear_backward8(ws, spv.spv_checkpoint8(x), da)
+    assert bool(torch.isnan(got[3]).all()) and bool(torch.isfinite(torch.cat([got[:3], got[4:]])).all())
