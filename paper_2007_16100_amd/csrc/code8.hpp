@@ -31,4 +31,25 @@ __device__ inline float code_value(int code, float step) {
     return code == -128 ? __uint_as_float(0x7FC00000u) : (float)code * step;
 }
 
+// The codes of a lane's VEC channels of a block that LANES lanes hold (a power of two of them, next to each other); returns the
+// block's exponent byte.  All lanes of the wave call it.
+template <int DT, int VEC, int LANES>
+__device__ inline int code_block(const float (&x)[VEC], uint32_t (&w)[VEC / 4]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) top = max(top, finite_bits(x[e]));
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    const int byte = code_exp<DT>(top);
+    const float rate = code_rate(byte);
+#pragma unroll
+    for (int j = 0; j < VEC / 4; ++j) {
+        uint32_t q[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[e] = (uint32_t)code_of(x[4 * j + e], rate) & 0xFFu;
+        w[j] = (q[0] | (q[1] << 8)) | ((q[2] << 16) | (q[3] << 24));
+    }
+    return byte;
+}
+
 }  // namespace spv

@@ -3,6 +3,10 @@
 //   mu, r from the rows of a scan and the channels of a group together;
 //   gz = dy act'(z),  h = gz gamma,  dx = r (h - mean h - xh mean(h xh)) (+ dres),
 //   dgamma = sum gz xh,  dbeta = sum gz.
+//
+// A scan's statistics take all of its rows, so each direction reads its rows twice.  Rows are cut into tiles of one
+// scan each, one to a workgroup: a first kernel leaves a tile's sums of each group, a second joins those of the tile's scan
+// (each workgroup again: a few thousand numbers, and a launch less) and writes the rows.
 #include <type_traits>
 
 #include "attn_common.hpp"
@@ -10,10 +14,14 @@
 
 namespace spv {
 
+// exp and the reciprocal are the hardware's, each off by 2^-23 of itself at most, and the exponent's rounding adds |z| 2^-24
+__device__ inline float sigmoid(float z) {
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -kLog2e));
+}
 template <int ACT>
 __device__ inline float act_of(float z) {
     if constexpr (ACT == SPV_ACT_RELU) return z <= 0.f ? 0.f : z;
-    else if constexpr (ACT == SPV_ACT_SILU) return z / (1.f + expf(-z));
+    else if constexpr (ACT == SPV_ACT_SILU) return z * sigmoid(z);
     else return z;
 }
 template <int ACT>
@@ -21,13 +29,508 @@ __device__ inline float act_slope(float z) {
     if constexpr (ACT == SPV_ACT_RELU) {
         return z <= 0.f ? 0.f : 1.f;
     } else if constexpr (ACT == SPV_ACT_SILU) {
-        const float s = 1.f / (1.f + expf(-z));
+        const float s = sigmoid(z);
         return s * fmaf(z, 1.f - s, 1.f);
     } else {
         return 1.f;
     }
 }
 
+// ---------------------------------------------------------------------------
+// Tiles.  A thread holds VEC channels (16 bytes, or one where rows are odd or unaligned) of every R-th row of its
+// workgroup's tile, so what belongs to a channel stays in registers over the rows; R = kGnThreads / (C / VEC).
+// ---------------------------------------------------------------------------
+constexpr int kGnThreads = 512, kGnWaves = kGnThreads / 64;
+constexpr int kGnTiles = 512;  // tiles of one long scan: two workgroups a CU
+constexpr int kGnAhead = 4;    // rows a thread loads at a time
+
+template <int DT>
+constexpr int kGnVec = DT == SPV_F32 ? 4 : 8;
+
+// VEC channels as they are loaded, in float32 and stored
+template <int DT, int VEC>
+struct Chans {
+    using Raw = std::conditional_t<VEC == 1, float, uint4>;
+    static __device__ Raw load(const void* p, int64_t e) {
+        if constexpr (VEC == 1) return ld_feat<DT>(p, e);
+        else return *(const uint4*)((const char*)p + e * (16 / VEC));
+    }
+    static __device__ void unpack(const Raw& r, float (&x)[VEC]) {
+        if constexpr (VEC == 1) {
+            x[0] = r;
+        } else {
+            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (DT == SPV_F32) {
+                    x[j] = __uint_as_float(w[j]);
+                } else {
+                    x[2 * j] = from16<DT>(w[j] & 0xFFFF);
+                    x[2 * j + 1] = from16<DT>(w[j] >> 16);
+                }
+            }
+        }
+    }
+    static __device__ void store(void* p, int64_t e, const float (&x)[VEC]) {
+        if constexpr (VEC == 1) {
+            st_feat<DT>(p, e, x[0]);
+        } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (DT == SPV_F32) w[j] = __float_as_uint(x[j]);
+                else w[j] = pack2<DT>(x[2 * j], x[2 * j + 1]);
+            }
+            *(uint4*)((char*)p + e * (16 / VEC)) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+};
+
+// VEC channels of a row in 8 bits: VEC codes and their exponent
+template <int VEC>
+struct Codes {
+    struct Raw {
+        uint32_t w[VEC == 8 ? 2 : 1];
+        int e;
+    };
+    static __device__ Raw load(const Saved8& s, int64_t row, int C, int c) {
+        Raw r;
+        const int8_t* p = s.codes + row * C + c;
+        if constexpr (VEC == 8) {
+            const uint2 u = *(const uint2*)p;
+            r.w[0] = u.x, r.w[1] = u.y;
+        } else if constexpr (VEC == 4) {
+            r.w[0] = *(const uint32_t*)p;
+        } else {
+            r.w[0] = (uint8_t)*p;
+        }
+        r.e = s.exps[row * code_blocks(C) + c / kCodeBlock];
+        return r;
+    }
+    static __device__ void unpack(const Raw& r, float (&x)[VEC]) {
+        const float step = code_step(r.e);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[j] = code_value((int8_t)(r.w[j / 4] >> (8 * (j % 4))), step);
+    }
+};
+
+struct GnTile {
+    int b;            // scan
+    int64_t row0;     // first row
+    int rows;         // of the tile
+    int64_t n;        // rows of the scan
+    int64_t tile0;    // number of the scan's first tile
+    bool first;       // this is it
+};
+__device__ inline GnTile gn_tile(const GnArgs& a, int tile_rows, int64_t t) {
+    const ScanTile s = find_tile(a.off, a.m, a.off, a.m, a.B, 1, tile_rows, t);
+    GnTile g;
+    g.b = s.b;
+    g.row0 = s.first + s.col0;
+    const int64_t left = s.cols - s.col0;
+    g.rows = (int)(left < 0 ? 0 : left > tile_rows ? tile_rows : left);
+    g.n = s.cols;
+    g.tile0 = s.first / tile_rows + s.b;
+    g.first = t == g.tile0;
+    return g;
+}
+
+// sum over a wave
+__device__ inline double wave_sum(double v) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+__device__ inline float wave_sum(float v) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// mean and r of a group of scan b from its tiles' means and sums of squares, by a wave, in 64 bits
+__device__ inline float2 gn_join_stat(const float2* part, int G, int g, int64_t tile0, int64_t n, int tile_rows, int w,
+                                      float eps) {
+    const int lane = threadIdx.x & 63;
+    const int64_t tiles = (n + tile_rows - 1) / tile_rows;
+    double s = 0.0, q = 0.0;
+    for (int64_t t = lane; t < tiles; t += 64) {
+        const int64_t rows = n - t * tile_rows < tile_rows ? n - t * tile_rows : tile_rows;
+        s += (double)rows * (double)part[(tile0 + t) * G + g].x;
+    }
+    if (n == 0) return make_float2(0.f, 0.f);
+    const double mu = wave_sum(s) / (double)n;
+    for (int64_t t = lane; t < tiles; t += 64) {
+        const int64_t rows = n - t * tile_rows < tile_rows ? n - t * tile_rows : tile_rows;
+        const float2 p = part[(tile0 + t) * G + g];
+        const double d = (double)p.x - mu;
+        q += (double)p.y + (double)(rows * w) * d * d;
+    }
+    q = wave_sum(q) / ((double)n * (double)w);
+    return make_float2((float)mu, (float)(1.0 / sqrt(q + (double)eps)));
+}
+// the sums of a group of a scan from its tiles', over the count
+__device__ inline float2 gn_join_sums(const float2* part, int G, int g, int64_t tile0, int64_t n, int tile_rows, int w) {
+    const int64_t tiles = (n + tile_rows - 1) / tile_rows;
+    double s1 = 0.0, s2 = 0.0;
+    for (int64_t t = threadIdx.x & 63; t < tiles; t += 64) {
+        const float2 p = part[(tile0 + t) * G + g];
+        s1 += (double)p.x;
+        s2 += (double)p.y;
+    }
+    const double count = n > 0 ? (double)n * (double)w : 1.0;
+    return make_float2((float)(wave_sum(s1) / count), (float)(wave_sum(s2) / count));
+}
+
+// a wave takes a group of a scan
+template <bool STAT>
+__global__ __launch_bounds__(256) void k_gn_join(GnArgs a, int tile_rows) {
+    const int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (u >= (int64_t)a.B * a.G) return;
+    const int b = (int)(u / a.G), g = (int)(u % a.G);
+    const int64_t r0 = clamp_off(a.off[b], a.m), r1 = clamp_off(a.off[b + 1], a.m), n = r1 > r0 ? r1 - r0 : 0;
+    const float2 v = STAT ? gn_join_stat(a.tiles, a.G, g, r0 / tile_rows + b, n, tile_rows, a.C / a.G, a.eps)
+                          : gn_join_sums(a.tiles, a.G, g, r0 / tile_rows + b, n, tile_rows, a.C / a.G);
+    if ((threadIdx.x & 63) == 0) a.joined[u] = v;
+}
+
+// A tile's mean and sum of squared deviations of each group.  A thread keeps the running mean of each of its channels and
+// the squares of the deviations from it, four rows at a time: no cancellation however far from zero the rows sit.  The
+// threads of a channel are then joined two by two in LDS, and the channels of a group by a wave.
+template <int DT, int VEC>
+__global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_rows) {
+    using V = Chans<DT, VEC>;
+    __shared__ float s_mean[kGnThreads * VEC], s_sq[kGnThreads * VEC], s_n[kGnThreads];
+    const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
+    if (t.rows == 0) return;
+    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
+    float mean[VEC], sq[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) mean[e] = sq[e] = 0.f;
+    float n = 0.f;
+    if (row < R) {
+        const int64_t base = t.row0 * a.C + c;
+        int i = row;
+        for (; i + 3 * R < t.rows; i += 4 * R) {
+            typename V::Raw u[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[k] = V::load(a.x, base + (int64_t)(i + k * R) * a.C);
+            float x[4][VEC];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) V::unpack(u[k], x[k]);
+            const float f = 4.f * __builtin_amdgcn_rcpf(n + 4.f), g = n * f;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float mu = ((x[0][e] + x[1][e]) + (x[2][e] + x[3][e])) * 0.25f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float d = x[k][e] - mu;
+                    sq[e] = fmaf(d, d, sq[e]);
+                }
+                const float d = mu - mean[e];
+                mean[e] = fmaf(d, f, mean[e]);
+                sq[e] = fmaf(d * g, d, sq[e]);
+            }
+            n += 4.f;
+        }
+        for (; i < t.rows; i += R) {
+            float x[VEC];
+            V::unpack(V::load(a.x, base + (int64_t)i * a.C), x);
+            n += 1.f;
+            const float f = __builtin_amdgcn_rcpf(n);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float d = x[e] - mean[e];
+                mean[e] = fmaf(d, f, mean[e]);
+                sq[e] = fmaf(d, x[e] - mean[e], sq[e]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            s_mean[row * a.C + c + e] = mean[e];
+            s_sq[row * a.C + c + e] = sq[e];
+        }
+        if (c == 0) s_n[row] = n;
+    }
+    __syncthreads();
+    // rows k and k + half, while there are two; the first rows have the most
+    for (int k = R; k > 1;) {
+        const int half = (k + 1) / 2;
+        for (int j = threadIdx.x; j < (k - half) * a.C; j += kGnThreads) {
+            const int p = j / a.C, o = j + half * a.C;
+            const float na = s_n[p], nb = s_n[p + half];
+            if (nb > 0.f) {
+                const float d = s_mean[o] - s_mean[j], f = nb / (na + nb);
+                s_mean[j] = fmaf(d, f, s_mean[j]);
+                s_sq[j] += fmaf(d * d, na * f, s_sq[o]);
+            }
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < k - half) s_n[threadIdx.x] += s_n[threadIdx.x + half];
+        k = half;
+        __syncthreads();
+    }
+    const int w = a.C / a.G, lane = threadIdx.x & 63;
+    for (int g = threadIdx.x >> 6; g < a.G; g += kGnWaves) {
+        float s = 0.f, q = 0.f;
+        for (int j = lane; j < w; j += 64) s += s_mean[g * w + j];
+        const float mu = wave_sum(s) / (float)w;
+        for (int j = lane; j < w; j += 64) {
+            const float d = s_mean[g * w + j] - mu;
+            q += fmaf(d * d, (float)t.rows, s_sq[g * w + j]);
+        }
+        q = wave_sum(q);
+        if (lane == 0) a.tiles[(int64_t)blockIdx.x * a.G + g] = make_float2(mu, q);
+    }
+}
+
+// the rows' second pass: y, and x in 8 bits (CODE: whole blocks of 32 channels)
+template <int DT, int VEC, int ACT, bool CODE>
+__global__ __launch_bounds__(kGnThreads) void k_gn_tile_apply(GnArgs a, int tile_rows) {
+    using V = Chans<DT, VEC>;
+    __shared__ float2 s_stat[kGnThreads * VEC];  // at most as many groups as channels
+    const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
+    if (t.rows == 0 && !(t.first && a.stat)) return;
+    const int w = a.C / a.G;
+    if (a.joined) {
+        for (int g = threadIdx.x; g < a.G; g += kGnThreads) s_stat[g] = a.joined[(int64_t)t.b * a.G + g];
+    } else {
+        for (int g = threadIdx.x >> 6; g < a.G; g += kGnWaves) {
+            const float2 v = gn_join_stat(a.tiles, a.G, g, t.tile0, t.n, tile_rows, w, a.eps);
+            if ((threadIdx.x & 63) == 0) s_stat[g] = v;
+        }
+    }
+    __syncthreads();
+    if (t.first && a.stat)
+        for (int g = threadIdx.x; g < a.G; g += kGnThreads) ((float2*)a.stat)[(int64_t)t.b * a.G + g] = s_stat[g];
+    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
+    float mu[VEC], sc[VEC], be[VEC];
+    if (row < R)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float2 st = s_stat[(c + e) / w];
+            mu[e] = st.x;
+            sc[e] = st.y * (a.gamma ? a.gamma[c + e] : 1.f);
+            be[e] = a.beta ? a.beta[c + e] : 0.f;
+        }
+    const int64_t base = t.row0 * a.C + c;
+    // all threads take as many rounds: the maximum of a block goes between lanes
+    for (int i0 = 0; i0 < t.rows; i0 += kGnAhead * R) {
+        typename V::Raw u[kGnAhead];
+#pragma unroll
+        for (int k = 0; k < kGnAhead; ++k) {
+            const int i = i0 + k * R + row;
+            u[k] = row < R && i < t.rows ? V::load(a.x, base + (int64_t)i * a.C) : typename V::Raw{};
+        }
+#pragma unroll
+        for (int k = 0; k < kGnAhead; ++k) {
+            const int i = i0 + k * R + row;
+            const bool on = row < R && i < t.rows;
+            float x[VEC], y[VEC];
+            V::unpack(u[k], x);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) y[e] = act_of<ACT>(fmaf(x[e] - mu[e], sc[e], be[e]));
+            if (on) V::store(a.out, base + (int64_t)i * a.C, y);
+            if constexpr (CODE) {
+                uint32_t w8[VEC / 4];
+                const int byte = code_block<DT, VEC, kCodeBlock / VEC>(x, w8);
+                if (on) {
+                    int8_t* q = a.saved.codes + (t.row0 + i) * a.C + c;
+                    if constexpr (VEC == 8) *(uint2*)q = make_uint2(w8[0], w8[1]);
+                    else *(uint32_t*)q = w8[0];
+                    if (c % kCodeBlock == 0)
+                        a.saved.exps[(t.row0 + i) * (a.C / kCodeBlock) + c / kCodeBlock] = (uint8_t)byte;
+                }
+            }
+        }
+    }
+}
+
+// what a thread's channels of the backward need of a row's dy and x (or its codes)
+template <int DT, int VEC, bool X8>
+struct GnSource {
+    using V = Chans<DT, VEC>;
+    using RawX = std::conditional_t<X8, typename Codes<VEC>::Raw, typename V::Raw>;
+    static __device__ RawX load(const GnArgs& a, int64_t row, int c) {
+        if constexpr (X8) return Codes<VEC>::load(a.saved, row, a.C, c);
+        else return V::load(a.x, row * a.C + c);
+    }
+    static __device__ void unpack(const RawX& r, float (&x)[VEC]) {
+        if constexpr (X8) Codes<VEC>::unpack(r, x);
+        else V::unpack(r, x);
+    }
+};
+
+// a tile's sums of gz and gz xh, of each channel and (times gamma) of each group
+template <int DT, int VEC, int ACT, bool X8>
+__global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_rows) {
+    using V = Chans<DT, VEC>;
+    using S = GnSource<DT, VEC, X8>;
+    __shared__ float s_1[kGnThreads * VEC], s_2[kGnThreads * VEC];
+    const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
+    const int w = a.C / a.G;
+    float* cols = a.part + (int64_t)blockIdx.x * 2 * a.C;
+    if (t.rows == 0) {  // the join of the channels takes every tile
+        for (int c = threadIdx.x; c < 2 * a.C; c += kGnThreads) cols[c] = 0.f;
+        return;
+    }
+    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
+    if (row < R) {
+        float mu[VEC], r[VEC], ga[VEC], be[VEC], s1[VEC], s2[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float2 st = ((const float2*)a.stat)[(int64_t)t.b * a.G + (c + e) / w];
+            mu[e] = st.x;
+            r[e] = st.y;
+            ga[e] = a.gamma ? a.gamma[c + e] : 1.f;
+            be[e] = a.beta ? a.beta[c + e] : 0.f;
+            s1[e] = s2[e] = 0.f;
+        }
+        for (int i0 = row; i0 < t.rows; i0 += kGnAhead * R) {
+            typename V::Raw ud[kGnAhead];
+            typename S::RawX ux[kGnAhead];
+#pragma unroll
+            for (int k = 0; k < kGnAhead; ++k) {
+                const int i = i0 + k * R < t.rows ? i0 + k * R : i0;
+                ud[k] = V::load(a.dy, (t.row0 + i) * a.C + c);
+                ux[k] = S::load(a, t.row0 + i, c);
+            }
+#pragma unroll
+            for (int k = 0; k < kGnAhead; ++k) {
+                if (i0 + k * R >= t.rows) break;
+                float x[VEC], d[VEC];
+                V::unpack(ud[k], d);
+                S::unpack(ux[k], x);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float xh = (x[e] - mu[e]) * r[e], gz = d[e] * act_slope<ACT>(fmaf(xh, ga[e], be[e]));
+                    s1[e] += gz;
+                    s2[e] = fmaf(gz, xh, s2[e]);
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            s_1[row * a.C + c + e] = s1[e];
+            s_2[row * a.C + c + e] = s2[e];
+        }
+    }
+    __syncthreads();
+    for (int k = R; k > 1;) {
+        const int half = (k + 1) / 2;
+        for (int j = threadIdx.x; j < (k - half) * a.C; j += kGnThreads) {
+            s_1[j] += s_1[j + half * a.C];
+            s_2[j] += s_2[j + half * a.C];
+        }
+        k = half;
+        __syncthreads();
+    }
+    for (int j = threadIdx.x; j < 2 * a.C; j += kGnThreads) cols[j] = j < a.C ? s_1[j] : s_2[j - a.C];
+    const int lane = threadIdx.x & 63;
+    for (int g = threadIdx.x >> 6; g < a.G; g += kGnWaves) {
+        float p = 0.f, q = 0.f;
+        for (int j = g * w + lane; j < (g + 1) * w; j += 64) {
+            const float gj = a.gamma ? a.gamma[j] : 1.f;
+            p = fmaf(gj, s_1[j], p);
+            q = fmaf(gj, s_2[j], q);
+        }
+        p = wave_sum(p);
+        q = wave_sum(q);
+        if (lane == 0) a.tiles[(int64_t)blockIdx.x * a.G + g] = make_float2(p, q);
+    }
+}
+
+// dbeta and dgamma: 16 of the 2 C columns of the tiles' sums a workgroup, in 32 runs of consecutive tiles, in 64 bits
+__device__ inline void gn_join_channels(const GnArgs& a, int64_t tiles, int which) {
+    __shared__ double red[32][17];
+    const int col = threadIdx.x & 15, run = threadIdx.x >> 4, j = which * 16 + col;
+    const int64_t len = (tiles + 31) / 32, t0 = run * len, t1 = t0 + len < tiles ? t0 + len : tiles;
+    double s = 0.0;
+    if (j < 2 * a.C)
+        for (int64_t t = t0; t < t1; t += 8) {
+            float f[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = t + k < t1 ? a.part[(t + k) * 2 * a.C + j] : 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += (double)f[k];
+        }
+    red[run][col] = s;
+    __syncthreads();
+    if (run || j >= 2 * a.C) return;
+    for (int k = 1; k < 32; ++k) s += red[k][col];
+    float* out = j < a.C ? a.dbeta : a.dgamma;
+    if (out) out[j < a.C ? j : j - a.C] = (float)s;
+}
+
+__global__ __launch_bounds__(kGnThreads) void k_gn_channels(GnArgs a, int64_t tiles) {
+    gn_join_channels(a, tiles, (int)blockIdx.x);
+}
+
+// the rows' second pass: dx; the workgroups past the tiles join the channels
+template <int DT, int VEC, int ACT, bool X8>
+__global__ __launch_bounds__(kGnThreads) void k_gn_tile_dx(GnArgs a, int tile_rows, int64_t tiles) {
+    using V = Chans<DT, VEC>;
+    using S = GnSource<DT, VEC, X8>;
+    if ((int64_t)blockIdx.x >= tiles) {
+        gn_join_channels(a, tiles, (int)(blockIdx.x - tiles));
+        return;
+    }
+    __shared__ float2 s_mean[kGnThreads * VEC];
+    const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
+    if (t.rows == 0) return;
+    const int w = a.C / a.G;
+    if (a.joined) {
+        for (int g = threadIdx.x; g < a.G; g += kGnThreads) s_mean[g] = a.joined[(int64_t)t.b * a.G + g];
+    } else {
+        for (int g = threadIdx.x >> 6; g < a.G; g += kGnWaves) {
+            const float2 v = gn_join_sums(a.tiles, a.G, g, t.tile0, t.n, tile_rows, w);
+            if ((threadIdx.x & 63) == 0) s_mean[g] = v;
+        }
+    }
+    __syncthreads();
+    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
+    if (row >= R) return;
+    float mu[VEC], r[VEC], ga[VEC], be[VEC], m1[VEC], m2[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        const float2 st = ((const float2*)a.stat)[(int64_t)t.b * a.G + (c + e) / w], me = s_mean[(c + e) / w];
+        mu[e] = st.x;
+        r[e] = st.y;
+        ga[e] = a.gamma ? a.gamma[c + e] : 1.f;
+        be[e] = a.beta ? a.beta[c + e] : 0.f;
+        m1[e] = me.x;
+        m2[e] = me.y;
+    }
+    for (int i0 = row; i0 < t.rows; i0 += kGnAhead * R) {
+        typename V::Raw ud[kGnAhead], ur[kGnAhead];
+        typename S::RawX ux[kGnAhead];
+#pragma unroll
+        for (int k = 0; k < kGnAhead; ++k) {
+            const int i = i0 + k * R < t.rows ? i0 + k * R : i0;
+            ud[k] = V::load(a.dy, (t.row0 + i) * a.C + c);
+            ux[k] = S::load(a, t.row0 + i, c);
+            if (a.dres) ur[k] = V::load(a.dres, (t.row0 + i) * a.C + c);
+        }
+#pragma unroll
+        for (int k = 0; k < kGnAhead; ++k) {
+            if (i0 + k * R >= t.rows) break;
+            float x[VEC], d[VEC], q[VEC] = {};
+            V::unpack(ud[k], d);
+            S::unpack(ux[k], x);
+            if (a.dres) V::unpack(ur[k], q);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float xh = (x[e] - mu[e]) * r[e];
+                const float h = d[e] * act_slope<ACT>(fmaf(xh, ga[e], be[e])) * ga[e];
+                d[e] = fmaf(r[e], h - m1[e] - xh * m2[e], q[e]);
+            }
+            V::store(a.dx, (t.row0 + i0 + k * R) * a.C + c, d);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// rows too wide for a workgroup's threads, by elements: a workgroup takes a group or a channel of a scan
+// ---------------------------------------------------------------------------
 __device__ inline double block_sum(double v, double* red) {
     __syncthreads();
     red[threadIdx.x] = v;
@@ -46,29 +549,27 @@ __device__ inline float saved_x(const GnArgs& a, int64_t i, int c) {
     return code_value(a.saved.codes[i * a.C + c], code_step(a.saved.exps[i * code_blocks(a.C) + c / kCodeBlock]));
 }
 
-// a workgroup takes a group of a scan
 template <int DT>
 __global__ __launch_bounds__(256) void k_gn_stat(GnArgs a) {
     __shared__ double red[256];
-    const int b = blockIdx.x / a.G, g = blockIdx.x % a.G, w = a.C / a.G;
-    const int64_t r0 = clamp_off(a.off[b], a.m), r1 = clamp_off(a.off[b + 1], a.m);
-    const int64_t n = r1 > r0 ? (r1 - r0) * w : 0;
-    double s = 0.0;
-    for (int64_t t = threadIdx.x; t < n; t += 256) s += (double)ld_feat<DT>(a.x, (r0 + t / w) * a.C + g * w + t % w);
-    const double mu = n ? block_sum(s, red) / (double)n : 0.0;
-    s = 0.0;
-    for (int64_t t = threadIdx.x; t < n; t += 256) {
-        const double d = (double)ld_feat<DT>(a.x, (r0 + t / w) * a.C + g * w + t % w) - mu;
-        s += d * d;
-    }
-    s = block_sum(s, red);
-    if (threadIdx.x == 0) {
-        a.part[2 * blockIdx.x] = (float)mu;
-        a.part[2 * blockIdx.x + 1] = n ? (float)(1.0 / sqrt(s / (double)n + (double)a.eps)) : 0.f;
-        if (a.stat) {
-            a.stat[2 * blockIdx.x] = a.part[2 * blockIdx.x];
-            a.stat[2 * blockIdx.x + 1] = a.part[2 * blockIdx.x + 1];
+    const int w = a.C / a.G;
+    for (int64_t u = blockIdx.x; u < (int64_t)a.B * a.G; u += gridDim.x) {
+        const int b = (int)(u / a.G), g = (int)(u % a.G);
+        const int64_t r0 = clamp_off(a.off[b], a.m), r1 = clamp_off(a.off[b + 1], a.m);
+        const int64_t n = r1 > r0 ? (r1 - r0) * w : 0;
+        double s = 0.0, q = 0.0;
+        for (int64_t t = threadIdx.x; t < n; t += 256) s += (double)ld_feat<DT>(a.x, (r0 + t / w) * a.C + g * w + t % w);
+        const double mu = block_sum(s, red) / (double)(n ? n : 1);
+        for (int64_t t = threadIdx.x; t < n; t += 256) {
+            const double d = (double)ld_feat<DT>(a.x, (r0 + t / w) * a.C + g * w + t % w) - mu;
+            q += d * d;
         }
+        q = block_sum(q, red);
+        if (threadIdx.x) continue;
+        const float2 v = n ? make_float2((float)mu, (float)(1.0 / sqrt(q / (double)n + (double)a.eps)))
+                           : make_float2(0.f, 0.f);
+        a.joined[u] = v;
+        if (a.stat) ((float2*)a.stat)[u] = v;
     }
 }
 
@@ -90,35 +591,53 @@ __global__ __launch_bounds__(256) void k_gn_apply(GnArgs a) {
         const int b = scan_of(a, i);
         if (b < 0) continue;
         for (int c = threadIdx.x; c < a.C; c += 256) {
-            const float* st = a.part + 2 * ((int64_t)b * a.G + c / (a.C / a.G));
-            const float xh = (ld_feat<DT>(a.x, i * a.C + c) - st[0]) * st[1];
+            const float2 st = a.joined[(int64_t)b * a.G + c / (a.C / a.G)];
+            const float xh = (ld_feat<DT>(a.x, i * a.C + c) - st.x) * st.y;
             st_feat<DT>(a.out, i * a.C + c,
                         act_of<ACT>(fmaf(xh, a.gamma ? a.gamma[c] : 1.f, a.beta ? a.beta[c] : 0.f)));
         }
     }
 }
 
-// a workgroup takes a channel of a scan: sum gz and sum gz xh
+// sum gz and sum gz xh of a channel of a scan: part[b][C][2]
 template <int DT, int ACT>
 __global__ __launch_bounds__(256) void k_gn_sums(GnArgs a) {
     __shared__ double red[256];
-    const int b = blockIdx.x / a.C, c = blockIdx.x % a.C;
-    const int64_t r0 = clamp_off(a.off[b], a.m), r1 = clamp_off(a.off[b + 1], a.m);
-    const float* st = a.stat + 2 * ((int64_t)b * a.G + c / (a.C / a.G));
-    const float g = a.gamma ? a.gamma[c] : 1.f, be = a.beta ? a.beta[c] : 0.f;
-    double s1 = 0.0, s2 = 0.0;
-    for (int64_t i = r0 + threadIdx.x; i < r1; i += 256) {
-        const float xh = (saved_x<DT>(a, i, c) - st[0]) * st[1];
-        const float gz = ld_feat<DT>(a.dy, i * a.C + c) * act_slope<ACT>(fmaf(xh, g, be));
-        s1 += (double)gz;
-        s2 += (double)gz * xh;
+    for (int64_t u = blockIdx.x; u < (int64_t)a.B * a.C; u += gridDim.x) {
+        const int b = (int)(u / a.C), c = (int)(u % a.C);
+        const int64_t r0 = clamp_off(a.off[b], a.m), r1 = clamp_off(a.off[b + 1], a.m);
+        const float2 st = ((const float2*)a.stat)[(int64_t)b * a.G + c / (a.C / a.G)];
+        const float g = a.gamma ? a.gamma[c] : 1.f, be = a.beta ? a.beta[c] : 0.f;
+        double s1 = 0.0, s2 = 0.0;
+        for (int64_t i = r0 + threadIdx.x; i < r1; i += 256) {
+            const float xh = (saved_x<DT>(a, i, c) - st.x) * st.y;
+            const float gz = ld_feat<DT>(a.dy, i * a.C + c) * act_slope<ACT>(fmaf(xh, g, be));
+            s1 += (double)gz;
+            s2 += (double)gz * xh;
+        }
+        s1 = block_sum(s1, red);
+        s2 = block_sum(s2, red);
+        if (threadIdx.x == 0) ((float2*)a.part)[u] = make_float2((float)s1, (float)s2);
     }
-    s1 = block_sum(s1, red);
-    s2 = block_sum(s2, red);
-    if (threadIdx.x == 0) {
-        a.part[2 * (int64_t)blockIdx.x] = (float)s1;
-        a.part[2 * (int64_t)blockIdx.x + 1] = (float)s2;
+}
+
+// a wave takes a group of a scan: the means of h and h xh
+__global__ __launch_bounds__(256) void k_gn_groups(GnArgs a) {
+    const int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (u >= (int64_t)a.B * a.G) return;
+    const int b = (int)(u / a.G), w = a.C / a.G, c0 = (int)(u % a.G) * w;
+    const int64_t n = clamp_off(a.off[b + 1], a.m) - clamp_off(a.off[b], a.m);
+    double m1 = 0.0, m2 = 0.0;
+    for (int c = c0 + (threadIdx.x & 63); c < c0 + w; c += 64) {
+        const float2 p = ((const float2*)a.part)[(int64_t)b * a.C + c];
+        const float g = a.gamma ? a.gamma[c] : 1.f;
+        m1 += (double)g * p.x;
+        m2 += (double)g * p.y;
     }
+    m1 = wave_sum(m1);
+    m2 = wave_sum(m2);
+    const double count = n > 0 ? (double)n * (double)w : 1.0;
+    if ((threadIdx.x & 63) == 0) a.joined[u] = make_float2((float)(m1 / count), (float)(m2 / count));
 }
 
 template <int DT, int ACT>
@@ -127,19 +646,12 @@ __global__ __launch_bounds__(256) void k_gn_dx(GnArgs a) {
     for (int64_t i = blockIdx.x; i < a.m; i += gridDim.x) {
         const int b = scan_of(a, i);
         if (b < 0) continue;
-        const float n = (float)(clamp_off(a.off[b + 1], a.m) - clamp_off(a.off[b], a.m)) * (float)w;
         for (int c = threadIdx.x; c < a.C; c += 256) {
-            const int g0 = c / w * w;
-            float m1 = 0.f, m2 = 0.f;
-            for (int j = g0; j < g0 + w; ++j) {
-                const float gj = a.gamma ? a.gamma[j] : 1.f;
-                m1 = fmaf(gj, a.part[2 * ((int64_t)b * a.C + j)], m1);
-                m2 = fmaf(gj, a.part[2 * ((int64_t)b * a.C + j) + 1], m2);
-            }
-            const float* st = a.stat + 2 * ((int64_t)b * a.G + c / w);
-            const float g = a.gamma ? a.gamma[c] : 1.f, xh = (saved_x<DT>(a, i, c) - st[0]) * st[1];
+            const int64_t u = (int64_t)b * a.G + c / w;
+            const float2 st = ((const float2*)a.stat)[u], me = a.joined[u];
+            const float g = a.gamma ? a.gamma[c] : 1.f, xh = (saved_x<DT>(a, i, c) - st.x) * st.y;
             const float h = ld_feat<DT>(a.dy, i * a.C + c) * act_slope<ACT>(fmaf(xh, g, a.beta ? a.beta[c] : 0.f)) * g;
-            float d = st[1] * (h - m1 / n - xh * (m2 / n));
+            float d = st.y * (h - me.x - xh * me.y);
             if (a.dres) d += ld_feat<DT>(a.dres, i * a.C + c);
             st_feat<DT>(a.dx, i * a.C + c, d);
         }
@@ -151,44 +663,116 @@ __global__ __launch_bounds__(256) void k_gn_params(GnArgs a) {
     if (c >= a.C) return;
     double s1 = 0.0, s2 = 0.0;
     for (int b = 0; b < a.B; ++b) {
-        s1 += (double)a.part[2 * ((int64_t)b * a.C + c)];
-        s2 += (double)a.part[2 * ((int64_t)b * a.C + c) + 1];
+        const float2 p = ((const float2*)a.part)[(int64_t)b * a.C + c];
+        s1 += (double)p.x;
+        s2 += (double)p.y;
     }
     if (a.dbeta) a.dbeta[c] = (float)s1;
     if (a.dgamma) a.dgamma[c] = (float)s2;
 }
 
-void plan_group_norm_ws(Arena& a, GnArgs& t) { t.part = a.take<float>((size_t)2 * t.B * t.G); }
-void plan_group_norm_backward_ws(Arena& a, GnArgs& t) { t.part = a.take<float>((size_t)2 * t.B * t.C); }
+// ---------------------------------------------------------------------------
 
-// f(type, activation) for those of a
+// Rows of a tile: kGnTiles tiles for a long scan, and 8192 values at least, a few rows a thread.
+static int gn_tile_rows(int64_t m, int C) {
+    const int64_t few = (8191 + C) / C, many = (m + kGnTiles - 1) / kGnTiles;
+    return (int)(few > many ? few : many);
+}
+static int64_t gn_tiles(int64_t m, int C, int B) { return m / gn_tile_rows(m, C) + B; }
+// A workgroup joins its scan's tiles itself up to this many numbers, else a kernel does it for all
+constexpr int64_t kGnJoin = 8192;
+static bool gn_join_apart(const GnArgs& a) { return gn_tiles(a.m, a.C, 1) * a.G > kGnJoin; }
+
+static void gn_ws(Arena& a, GnArgs& t) {
+    t.tiles = a.take<float2>((size_t)gn_tiles(t.m, t.C, t.B) * t.G);
+    t.joined = a.take<float2>((size_t)t.B * t.G);
+}
+void plan_group_norm_ws(Arena& a, GnArgs& t) { gn_ws(a, t); }
+void plan_group_norm_backward_ws(Arena& a, GnArgs& t) {
+    gn_ws(a, t);
+    t.part = a.take<float>((size_t)gn_tiles(t.m, t.C, t.B) * 2 * t.C);
+}
+
+template <int V>
+using Num = std::integral_constant<int, V>;
+// f(type, channels a thread, activation); 0 channels: rows too wide for the tiles
 template <class F>
 static void gn_kinds(const GnArgs& a, F&& f) {
-    auto act = [&](auto dt) {
-        if (a.act == SPV_ACT_RELU) f(dt, std::integral_constant<int, SPV_ACT_RELU>{});
-        else if (a.act == SPV_ACT_SILU) f(dt, std::integral_constant<int, SPV_ACT_SILU>{});
-        else f(dt, std::integral_constant<int, SPV_ACT_NONE>{});
+    const bool aligned = (((uintptr_t)a.x | (uintptr_t)a.out | (uintptr_t)a.dy | (uintptr_t)a.dres | (uintptr_t)a.dx) & 15u) == 0;
+    auto act = [&](auto dt, auto vec) {
+        if (a.act == SPV_ACT_RELU) f(dt, vec, Num<SPV_ACT_RELU>{});
+        else if (a.act == SPV_ACT_SILU) f(dt, vec, Num<SPV_ACT_SILU>{});
+        else f(dt, vec, Num<SPV_ACT_NONE>{});
     };
-    if (a.dt == SPV_F32) act(std::integral_constant<int, SPV_F32>{});
-    else if (a.dt == SPV_BF16) act(std::integral_constant<int, SPV_BF16>{});
-    else act(std::integral_constant<int, SPV_F16>{});
+    auto wide = [&](auto dt) {
+        constexpr int V = kGnVec<decltype(dt)::value>;
+        if (aligned && ((uintptr_t)a.saved.codes % V) == 0 && a.C % V == 0 && a.C / V <= kGnThreads) act(dt, Num<V>{});
+        else if (a.C <= kGnThreads) act(dt, Num<1>{});
+        else act(dt, Num<0>{});
+    };
+    if (a.dt == SPV_F32) wide(Num<SPV_F32>{});
+    else if (a.dt == SPV_BF16) wide(Num<SPV_BF16>{});
+    else wide(Num<SPV_F16>{});
 }
+static unsigned gn_grid(int64_t n) { return (unsigned)(n < 1 ? 1 : n > 65536 ? 65536 : n); }
 
-void launch_group_norm(hipStream_t s, const GnArgs& a) {
-    const unsigned rows = (unsigned)(a.m < 1 ? 1 : a.m > 65536 ? 65536 : a.m);
-    // before out, which may be x
-    if (a.saved.codes && a.m) launch_checkpoint8(s, a.x, a.saved, RowRange{a.m, nullptr, a.off, a.B}, a.C, a.dt);
-    gn_kinds(a, [&](auto dt, auto act) {
-        k_gn_stat<decltype(dt)::value><<<(unsigned)(a.B * a.G), 256, 0, s>>>(a);
-        if (a.m) k_gn_apply<decltype(dt)::value, decltype(act)::value><<<rows, 256, 0, s>>>(a);
+void launch_group_norm(hipStream_t s, const GnArgs& given) {
+    gn_kinds(given, [&](auto dt, auto vec, auto act) {
+        constexpr int DT = decltype(dt)::value, VEC = decltype(vec)::value, ACT = decltype(act)::value;
+        GnArgs a = given;
+        const bool code = VEC > 1 && a.C % kCodeBlock == 0 && a.saved.codes;
+        // before out, which may be x
+        if (a.saved.codes && !code && a.m)
+            launch_checkpoint8(s, a.x, a.saved, RowRange{a.m, nullptr, a.off, a.B}, a.C, a.dt);
+        if constexpr (VEC == 0) {
+            k_gn_stat<DT><<<gn_grid((int64_t)a.B * a.G), 256, 0, s>>>(a);
+            if (a.m) k_gn_apply<DT, ACT><<<gn_grid(a.m), 256, 0, s>>>(a);
+        } else {
+            const int rows = gn_tile_rows(a.m, a.C);
+            const unsigned tiles = (unsigned)gn_tiles(a.m, a.C, a.B);
+            k_gn_tile_stat<DT, VEC><<<tiles, kGnThreads, 0, s>>>(a, rows);
+            if (gn_join_apart(a)) k_gn_join<true><<<(unsigned)(((int64_t)a.B * a.G + 3) / 4), 256, 0, s>>>(a, rows);
+            else a.joined = nullptr;
+            if constexpr (VEC > 1) {
+                if (code) {
+                    k_gn_tile_apply<DT, VEC, ACT, true><<<tiles, kGnThreads, 0, s>>>(a, rows);
+                    return;
+                }
+            }
+            k_gn_tile_apply<DT, VEC, ACT, false><<<tiles, kGnThreads, 0, s>>>(a, rows);
+        }
     });
 }
+
+template <int DT, int VEC, int ACT, bool X8>
+static void gn_backward_tiles(hipStream_t s, GnArgs a) {
+    const int rows = gn_tile_rows(a.m, a.C);
+    const int64_t tiles = gn_tiles(a.m, a.C, a.B);
+    const unsigned join = a.dgamma || a.dbeta ? (unsigned)((2 * a.C + 15) / 16) : 0;
+    k_gn_tile_sums<DT, VEC, ACT, X8><<<(unsigned)tiles, kGnThreads, 0, s>>>(a, rows);
+    if (a.dx && gn_join_apart(a)) k_gn_join<false><<<(unsigned)(((int64_t)a.B * a.G + 3) / 4), 256, 0, s>>>(a, rows);
+    else a.joined = nullptr;
+    if (a.dx) k_gn_tile_dx<DT, VEC, ACT, X8><<<(unsigned)tiles + join, kGnThreads, 0, s>>>(a, rows, tiles);
+    else k_gn_channels<<<join, kGnThreads, 0, s>>>(a, tiles);
+}
 void launch_group_norm_backward(hipStream_t s, const GnArgs& a) {
-    const unsigned rows = (unsigned)(a.m < 1 ? 1 : a.m > 65536 ? 65536 : a.m);
-    gn_kinds(a, [&](auto dt, auto act) {
-        if (a.B) k_gn_sums<decltype(dt)::value, decltype(act)::value><<<(unsigned)(a.B * a.C), 256, 0, s>>>(a);
+    if (a.B == 0) {
         if (a.dgamma || a.dbeta) k_gn_params<<<(unsigned)((a.C + 255) / 256), 256, 0, s>>>(a);
-        if (a.dx && a.m && a.B) k_gn_dx<decltype(dt)::value, decltype(act)::value><<<rows, 256, 0, s>>>(a);
+        return;
+    }
+    gn_kinds(a, [&](auto dt, auto vec, auto act) {
+        constexpr int DT = decltype(dt)::value, VEC = decltype(vec)::value, ACT = decltype(act)::value;
+        if constexpr (VEC == 0) {
+            k_gn_sums<DT, ACT><<<gn_grid((int64_t)a.B * a.C), 256, 0, s>>>(a);
+            if (a.dgamma || a.dbeta) k_gn_params<<<(unsigned)((a.C + 255) / 256), 256, 0, s>>>(a);
+            if (!a.dx || !a.m) return;
+            k_gn_groups<<<(unsigned)(((int64_t)a.B * a.G + 3) / 4), 256, 0, s>>>(a);
+            k_gn_dx<DT, ACT><<<gn_grid(a.m), 256, 0, s>>>(a);
+        } else if (a.x || !a.saved.codes) {
+            gn_backward_tiles<DT, VEC, ACT, false>(s, a);
+        } else {
+            gn_backward_tiles<DT, VEC, ACT, true>(s, a);
+        }
     });
 }
 

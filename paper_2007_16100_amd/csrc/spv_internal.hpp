@@ -570,7 +570,10 @@ struct GnArgs {
     const void *dy, *dres;      // [m][C]; dres may be nullptr
     void* dx;                   // [m][C] or nullptr
     float *dgamma, *dbeta;      // [C] or nullptr
-    float* part;                // workspace
+    // workspace
+    float2* tiles;              // [tiles][G] mean and squares, or the backward's sums
+    float2* joined;             // [B][G] the same of a scan, as mean and r, or means
+    float* part;                // [tiles][2][C] the backward's sums of channels
 };
 void plan_group_norm_ws(Arena& a, GnArgs& t);
 void launch_group_norm(hipStream_t s, const GnArgs& a);
