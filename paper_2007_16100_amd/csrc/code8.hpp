@@ -2,6 +2,7 @@
 #pragma once
 
 #include "conv_common.hpp"
+#include "lanes.hpp"
 
 namespace spv {
 
@@ -32,14 +33,13 @@ __device__ inline float code_value(int code, float step) {
 }
 
 // The codes of a lane's VEC channels of a block that LANES lanes hold (a power of two of them, next to each other); returns the
-// block's exponent byte.  All lanes of the wave call it.
+// block's exponent byte.  All lanes of a block call it.
 template <int DT, int VEC, int LANES>
 __device__ inline int code_block(const float (&x)[VEC], uint32_t (&w)[VEC / 4]) {
     uint32_t top = 0;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) top = max(top, finite_bits(x[e]));
-#pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    top = lanes_max<LANES>(top);
     const int byte = code_exp<DT>(top);
     const float rate = code_rate(byte);
 #pragma unroll

@@ -42,7 +42,6 @@ __device__ inline float act_slope(float z) {
 // ---------------------------------------------------------------------------
 constexpr int kGnThreads = 512, kGnWaves = kGnThreads / 64;
 constexpr int kGnTiles = 512;  // tiles of one long scan: two workgroups a CU
-constexpr int kGnAhead = 4;    // rows a thread loads at a time
 
 template <int DT>
 constexpr int kGnVec = DT == SPV_F32 ? 4 : 8;
@@ -93,9 +92,10 @@ struct Codes {
         uint32_t w[VEC == 8 ? 2 : 1];
         int e;
     };
-    static __device__ Raw load(const Saved8& s, int64_t row, int C, int c) {
+    // at element e, whose block is number block
+    static __device__ Raw load(const Saved8& s, int64_t e, int64_t block) {
         Raw r;
-        const int8_t* p = s.codes + row * C + c;
+        const int8_t* p = s.codes + e;
         if constexpr (VEC == 8) {
             const uint2 u = *(const uint2*)p;
             r.w[0] = u.x, r.w[1] = u.y;
@@ -104,7 +104,7 @@ struct Codes {
         } else {
             r.w[0] = (uint8_t)*p;
         }
-        r.e = s.exps[row * code_blocks(C) + c / kCodeBlock];
+        r.e = s.exps[block];
         return r;
     }
     static __device__ void unpack(const Raw& r, float (&x)[VEC]) {
@@ -135,51 +135,84 @@ __device__ inline GnTile gn_tile(const GnArgs& a, int tile_rows, int64_t t) {
     return g;
 }
 
-// sum over a wave
-__device__ inline double wave_sum(double v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-__device__ inline float wave_sum(float v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-
-// mean and r of a group of scan b from its tiles' means and sums of squares, by a wave, in 64 bits
+// Mean and r of a group of a scan of n rows from its tiles' means and sums of squares, by a wave.  Deviations are from
+// the first tile's mean, whose distance from the mean of all, squared, is at most (tiles) times the variance: what
+// cancels in 64 bits is a few thousand of their units.
 __device__ inline float2 gn_join_stat(const float2* part, int G, int g, int64_t tile0, int64_t n, int tile_rows, int w,
                                       float eps) {
     const int lane = threadIdx.x & 63;
     const int64_t tiles = (n + tile_rows - 1) / tile_rows;
-    double s = 0.0, q = 0.0;
-    for (int64_t t = lane; t < tiles; t += 64) {
-        const int64_t rows = n - t * tile_rows < tile_rows ? n - t * tile_rows : tile_rows;
-        s += (double)rows * (double)part[(tile0 + t) * G + g].x;
-    }
     if (n == 0) return make_float2(0.f, 0.f);
-    const double mu = wave_sum(s) / (double)n;
-    for (int64_t t = lane; t < tiles; t += 64) {
-        const int64_t rows = n - t * tile_rows < tile_rows ? n - t * tile_rows : tile_rows;
-        const float2 p = part[(tile0 + t) * G + g];
-        const double d = (double)p.x - mu;
-        q += (double)p.y + (double)(rows * w) * d * d;
+    part += tile0 * G + g;
+    const float first = part[0].x;
+    const double per = 1.0 / (double)n;
+    double s = 0.0, q = 0.0;
+    for (int64_t t0 = 0; t0 < tiles; t0 += 256) {
+        float2 p[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t t = t0 + k * 64 + lane;
+            p[k] = part[(t < tiles ? t : 0) * G];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t t = t0 + k * 64 + lane, left = n - t * tile_rows;
+            const double rows = (double)(left < tile_rows ? left : tile_rows), d = (double)p[k].x - (double)first;
+            if (t < tiles) {
+                s += rows * d;
+                q += fma(rows * w * d, d, (double)p[k].y);
+            }
+        }
     }
-    q = wave_sum(q) / ((double)n * (double)w);
-    return make_float2((float)mu, (float)(1.0 / sqrt(q + (double)eps)));
+    s = wave_sum(s) * per;
+    q = wave_sum(q) * per / (double)w - s * s;
+    return make_float2((float)((double)first + s), 1.f / sqrtf((float)(q > 0.0 ? q : q == q ? 0.0 : q) + eps));
 }
 // the sums of a group of a scan from its tiles', over the count
 __device__ inline float2 gn_join_sums(const float2* part, int G, int g, int64_t tile0, int64_t n, int tile_rows, int w) {
     const int64_t tiles = (n + tile_rows - 1) / tile_rows;
+    const double per = n > 0 ? 1.0 / ((double)n * (double)w) : 0.0;
     double s1 = 0.0, s2 = 0.0;
-    for (int64_t t = threadIdx.x & 63; t < tiles; t += 64) {
-        const float2 p = part[(tile0 + t) * G + g];
-        s1 += (double)p.x;
-        s2 += (double)p.y;
+    part += tile0 * G + g;
+    for (int64_t t0 = 0; t0 < tiles; t0 += 256) {
+        float2 p[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t t = t0 + k * 64 + (threadIdx.x & 63);
+            p[k] = t < tiles ? part[t * G] : make_float2(0.f, 0.f);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            s1 += (double)p[k].x;
+            s2 += (double)p[k].y;
+        }
     }
-    const double count = n > 0 ? (double)n * (double)w : 1.0;
-    return make_float2((float)(wave_sum(s1) / count), (float)(wave_sum(s2) / count));
+    return make_float2((float)(wave_sum(s1) * per), (float)(wave_sum(s2) * per));
 }
+
+// A thread's rows of a tile (row, row + R, ..), U at a time, the next U asked for before the present ones are used.
+// ask() comes before whatever the first rows can be waited for during.  A row past the end is asked for as row 0.
+template <int U, class Raw>
+struct GnRows {
+    int row, R, rows;
+    Raw u[U];
+    template <class L>
+    __device__ void ask(int i0, Raw (&to)[U], L&& load) const {
+#pragma unroll
+        for (int k = 0; k < U; ++k) to[k] = load(i0 + k * R < rows ? i0 + k * R : 0);
+    }
+    // use(first row, rows asked for); rows from `rows` on are not the thread's
+    template <class L, class F>
+    __device__ void run(L&& load, F&& use) {
+        for (int i0 = row; i0 < rows; i0 += U * R) {
+            Raw next[U];
+            if (i0 + U * R < rows) ask(i0 + U * R, next, load);
+            use(i0, u);
+#pragma unroll
+            for (int k = 0; k < U; ++k) u[k] = next[k];
+        }
+    }
+};
 
 // a wave takes a group of a scan
 template <bool STAT>
@@ -199,87 +232,107 @@ __global__ __launch_bounds__(256) void k_gn_join(GnArgs a, int tile_rows) {
 template <int DT, int VEC>
 __global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_rows) {
     using V = Chans<DT, VEC>;
-    __shared__ float s_mean[kGnThreads * VEC], s_sq[kGnThreads * VEC], s_n[kGnThreads];
+    __shared__ float s_mean[kGnThreads * VEC], s_sq[kGnThreads * VEC], s_n[2][kGnThreads];
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
     if (t.rows == 0) return;
     const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
-    float mean[VEC], sq[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) mean[e] = sq[e] = 0.f;
-    float n = 0.f;
     if (row < R) {
-        const int64_t base = t.row0 * a.C + c;
-        int i = row;
-        for (; i + 3 * R < t.rows; i += 4 * R) {
-            typename V::Raw u[4];
+        float mean[VEC], sq[VEC], n = 0.f;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) u[k] = V::load(a.x, base + (int64_t)(i + k * R) * a.C);
+        for (int e = 0; e < VEC; ++e) mean[e] = sq[e] = 0.f;
+        const int64_t base = t.row0 * a.C + c;
+        auto load = [&](int i) { return V::load(a.x, base + (int64_t)i * a.C); };
+        GnRows<4, typename V::Raw> rows{row, R, t.rows};
+        rows.ask(row, rows.u, load);
+        rows.run(load, [&](int i0, const typename V::Raw(&u)[4]) {
             float x[4][VEC];
 #pragma unroll
             for (int k = 0; k < 4; ++k) V::unpack(u[k], x[k]);
-            const float f = 4.f * __builtin_amdgcn_rcpf(n + 4.f), g = n * f;
+            if (i0 + 3 * R < t.rows) {
+                const float f = 4.f * __builtin_amdgcn_rcpf(n + 4.f), g = n * f;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float mu = ((x[0][e] + x[1][e]) + (x[2][e] + x[3][e])) * 0.25f;
+                for (int e = 0; e < VEC; ++e) {
+                    const float mu = ((x[0][e] + x[1][e]) + (x[2][e] + x[3][e])) * 0.25f;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float d = x[k][e] - mu;
-                    sq[e] = fmaf(d, d, sq[e]);
+                    for (int k = 0; k < 4; ++k) {
+                        const float d = x[k][e] - mu;
+                        sq[e] = fmaf(d, d, sq[e]);
+                    }
+                    const float d = mu - mean[e];
+                    mean[e] = fmaf(d, f, mean[e]);
+                    sq[e] = fmaf(d * g, d, sq[e]);
                 }
-                const float d = mu - mean[e];
-                mean[e] = fmaf(d, f, mean[e]);
-                sq[e] = fmaf(d * g, d, sq[e]);
+                n += 4.f;
+                return;
             }
-            n += 4.f;
-        }
-        for (; i < t.rows; i += R) {
-            float x[VEC];
-            V::unpack(V::load(a.x, base + (int64_t)i * a.C), x);
-            n += 1.f;
-            const float f = __builtin_amdgcn_rcpf(n);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float d = x[e] - mean[e];
-                mean[e] = fmaf(d, f, mean[e]);
-                sq[e] = fmaf(d, x[e] - mean[e], sq[e]);
+            for (int k = 0; k < 3; ++k) {
+                if (i0 + k * R >= t.rows) break;
+                n += 1.f;
+                const float f = __builtin_amdgcn_rcpf(n);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float d = x[k][e] - mean[e];
+                    mean[e] = fmaf(d, f, mean[e]);
+                    sq[e] = fmaf(d, x[k][e] - mean[e], sq[e]);
+                }
             }
-        }
+        });
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             s_mean[row * a.C + c + e] = mean[e];
             s_sq[row * a.C + c + e] = sq[e];
         }
-        if (c == 0) s_n[row] = n;
+        if (c == 0) s_n[0][row] = n;
     }
     __syncthreads();
-    // rows k and k + half, while there are two; the first rows have the most
-    for (int k = R; k > 1;) {
-        const int half = (k + 1) / 2;
-        for (int j = threadIdx.x; j < (k - half) * a.C; j += kGnThreads) {
-            const int p = j / a.C, o = j + half * a.C;
-            const float na = s_n[p], nb = s_n[p + half];
-            if (nb > 0.f) {
-                const float d = s_mean[o] - s_mean[j], f = nb / (na + nb);
-                s_mean[j] = fmaf(d, f, s_mean[j]);
-                s_sq[j] += fmaf(d * d, na * f, s_sq[o]);
+    // four rows into one, while there are several: rows k, k + q, k + 2 q, k + 3 q, the first of which holds the most
+    int which = 0;
+    for (int k = R; k > 1; which ^= 1) {
+        const int q = (k + 3) / 4;
+        for (int j = threadIdx.x; j < q * a.C; j += kGnThreads) {
+            const int p = j / a.C;
+            float n = s_n[which][p], mean = s_mean[j], sq = s_sq[j];
+#pragma unroll
+            for (int h = 1; h < 4; ++h) {
+                if (p + h * q >= k) break;
+                const int o = j + h * q * a.C;
+                const float nb = s_n[which][p + h * q];
+                if (nb > 0.f) {
+                    const float d = s_mean[o] - mean, f = nb * __builtin_amdgcn_rcpf(n + nb);
+                    mean = fmaf(d, f, mean);
+                    sq += fmaf(d * d, n * f, s_sq[o]);
+                    n += nb;
+                }
             }
+            s_mean[j] = mean;
+            s_sq[j] = sq;
+            if (j == p * a.C) s_n[which ^ 1][p] = n;
         }
-        __syncthreads();
-        if ((int)threadIdx.x < k - half) s_n[threadIdx.x] += s_n[threadIdx.x + half];
-        k = half;
+        k = q;
         __syncthreads();
     }
     const int w = a.C / a.G, lane = threadIdx.x & 63;
     for (int g = threadIdx.x >> 6; g < a.G; g += kGnWaves) {
         float s = 0.f, q = 0.f;
         for (int j = lane; j < w; j += 64) s += s_mean[g * w + j];
-        const float mu = wave_sum(s) / (float)w;
+        const float mu = lanes_sum<64>(s) / (float)w;
         for (int j = lane; j < w; j += 64) {
             const float d = s_mean[g * w + j] - mu;
             q += fmaf(d * d, (float)t.rows, s_sq[g * w + j]);
         }
-        q = wave_sum(q);
+        q = lanes_sum<64>(q);
         if (lane == 0) a.tiles[(int64_t)blockIdx.x * a.G + g] = make_float2(mu, q);
+    }
+}
+
+// gamma and beta of a thread's channels
+template <int VEC>
+__device__ inline void gn_channels(const GnArgs& a, int c, bool on, float (&ga)[VEC], float (&be)[VEC]) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        ga[e] = on && a.gamma ? a.gamma[c + e] : 1.f;
+        be[e] = on && a.beta ? a.beta[c + e] : 0.f;
     }
 }
 
@@ -288,8 +341,15 @@ template <int DT, int VEC, int ACT, bool CODE>
 __global__ __launch_bounds__(kGnThreads) void k_gn_tile_apply(GnArgs a, int tile_rows) {
     using V = Chans<DT, VEC>;
     __shared__ float2 s_stat[kGnThreads * VEC];  // at most as many groups as channels
+    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
+    float ga[VEC], be[VEC];
+    gn_channels<VEC>(a, c, row < R, ga, be);
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
     if (t.rows == 0 && !(t.first && a.stat)) return;
+    const int64_t base = t.row0 * a.C + c;
+    auto load = [&](int i) { return V::load(a.x, base + (int64_t)i * a.C); };
+    GnRows<4, typename V::Raw> rows{row, R, row < R ? t.rows : 0};
+    if (rows.rows) rows.ask(row, rows.u, load);
     const int w = a.C / a.G;
     if (a.joined) {
         for (int g = threadIdx.x; g < a.G; g += kGnThreads) s_stat[g] = a.joined[(int64_t)t.b * a.G + g];
@@ -302,47 +362,34 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_apply(GnArgs a, int tile
     __syncthreads();
     if (t.first && a.stat)
         for (int g = threadIdx.x; g < a.G; g += kGnThreads) ((float2*)a.stat)[(int64_t)t.b * a.G + g] = s_stat[g];
-    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
-    float mu[VEC], sc[VEC], be[VEC];
-    if (row < R)
+    if (row >= R) return;  // whole blocks of 32 channels
+    float mu[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float2 st = s_stat[(c + e) / w];
-            mu[e] = st.x;
-            sc[e] = st.y * (a.gamma ? a.gamma[c + e] : 1.f);
-            be[e] = a.beta ? a.beta[c + e] : 0.f;
-        }
-    const int64_t base = t.row0 * a.C + c;
-    // all threads take as many rounds: the maximum of a block goes between lanes
-    for (int i0 = 0; i0 < t.rows; i0 += kGnAhead * R) {
-        typename V::Raw u[kGnAhead];
+    for (int e = 0; e < VEC; ++e) {
+        const float2 st = s_stat[(c + e) / w];
+        mu[e] = st.x;
+        ga[e] *= st.y;
+    }
+    rows.run(load, [&](int i0, const typename V::Raw(&u)[4]) {
 #pragma unroll
-        for (int k = 0; k < kGnAhead; ++k) {
-            const int i = i0 + k * R + row;
-            u[k] = row < R && i < t.rows ? V::load(a.x, base + (int64_t)i * a.C) : typename V::Raw{};
-        }
-#pragma unroll
-        for (int k = 0; k < kGnAhead; ++k) {
-            const int i = i0 + k * R + row;
-            const bool on = row < R && i < t.rows;
+        for (int k = 0; k < 4; ++k) {
+            if (i0 + k * R >= t.rows) break;
+            const int64_t e = base + (int64_t)(i0 + k * R) * a.C;
             float x[VEC], y[VEC];
             V::unpack(u[k], x);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) y[e] = act_of<ACT>(fmaf(x[e] - mu[e], sc[e], be[e]));
-            if (on) V::store(a.out, base + (int64_t)i * a.C, y);
+            for (int j = 0; j < VEC; ++j) y[j] = act_of<ACT>(fmaf(x[j] - mu[j], ga[j], be[j]));
+            V::store(a.out, e, y);
             if constexpr (CODE) {
                 uint32_t w8[VEC / 4];
                 const int byte = code_block<DT, VEC, kCodeBlock / VEC>(x, w8);
-                if (on) {
-                    int8_t* q = a.saved.codes + (t.row0 + i) * a.C + c;
-                    if constexpr (VEC == 8) *(uint2*)q = make_uint2(w8[0], w8[1]);
-                    else *(uint32_t*)q = w8[0];
-                    if (c % kCodeBlock == 0)
-                        a.saved.exps[(t.row0 + i) * (a.C / kCodeBlock) + c / kCodeBlock] = (uint8_t)byte;
-                }
+                int8_t* q = a.saved.codes + e;
+                if constexpr (VEC == 8) *(uint2*)q = make_uint2(w8[0], w8[1]);
+                else *(uint32_t*)q = w8[0];
+                if (c % kCodeBlock == 0) a.saved.exps[e / kCodeBlock] = (uint8_t)byte;
             }
         }
-    }
+    });
 }
 
 // what a thread's channels of the backward need of a row's dy and x (or its codes)
@@ -350,9 +397,21 @@ template <int DT, int VEC, bool X8>
 struct GnSource {
     using V = Chans<DT, VEC>;
     using RawX = std::conditional_t<X8, typename Codes<VEC>::Raw, typename V::Raw>;
-    static __device__ RawX load(const GnArgs& a, int64_t row, int c) {
-        if constexpr (X8) return Codes<VEC>::load(a.saved, row, a.C, c);
-        else return V::load(a.x, row * a.C + c);
+    struct Raw {
+        typename V::Raw dy;
+        RawX x;
+    };
+    struct RawRes : Raw {
+        typename V::Raw res;
+    };
+    // row i of a tile, from the elements and blocks of its first row
+    static __device__ Raw load(const GnArgs& a, int64_t base, int64_t block, int i) {
+        const int64_t e = base + (int64_t)i * a.C;
+        Raw r;
+        r.dy = V::load(a.dy, e);
+        if constexpr (X8) r.x = Codes<VEC>::load(a.saved, e, block + (int64_t)i * code_blocks(a.C));
+        else r.x = V::load(a.x, e);
+        return r;
     }
     static __device__ void unpack(const RawX& r, float (&x)[VEC]) {
         if constexpr (X8) Codes<VEC>::unpack(r, x);
@@ -366,6 +425,9 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
     using V = Chans<DT, VEC>;
     using S = GnSource<DT, VEC, X8>;
     __shared__ float s_1[kGnThreads * VEC], s_2[kGnThreads * VEC];
+    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
+    float ga[VEC], be[VEC];
+    gn_channels<VEC>(a, c, row < R, ga, be);
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
     const int w = a.C / a.G;
     float* cols = a.part + (int64_t)blockIdx.x * 2 * a.C;
@@ -373,33 +435,26 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
         for (int c = threadIdx.x; c < 2 * a.C; c += kGnThreads) cols[c] = 0.f;
         return;
     }
-    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
     if (row < R) {
-        float mu[VEC], r[VEC], ga[VEC], be[VEC], s1[VEC], s2[VEC];
+        float mu[VEC], r[VEC], s1[VEC], s2[VEC];
+        const int64_t base = t.row0 * a.C + c, block = t.row0 * code_blocks(a.C) + c / kCodeBlock;
+        auto load = [&](int i) { return S::load(a, base, block, i); };
+        GnRows<2, typename S::Raw> rows{row, R, t.rows};
+        rows.ask(row, rows.u, load);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             const float2 st = ((const float2*)a.stat)[(int64_t)t.b * a.G + (c + e) / w];
             mu[e] = st.x;
             r[e] = st.y;
-            ga[e] = a.gamma ? a.gamma[c + e] : 1.f;
-            be[e] = a.beta ? a.beta[c + e] : 0.f;
             s1[e] = s2[e] = 0.f;
         }
-        for (int i0 = row; i0 < t.rows; i0 += kGnAhead * R) {
-            typename V::Raw ud[kGnAhead];
-            typename S::RawX ux[kGnAhead];
+        rows.run(load, [&](int i0, const typename S::Raw(&u)[2]) {
 #pragma unroll
-            for (int k = 0; k < kGnAhead; ++k) {
-                const int i = i0 + k * R < t.rows ? i0 + k * R : i0;
-                ud[k] = V::load(a.dy, (t.row0 + i) * a.C + c);
-                ux[k] = S::load(a, t.row0 + i, c);
-            }
-#pragma unroll
-            for (int k = 0; k < kGnAhead; ++k) {
+            for (int k = 0; k < 2; ++k) {
                 if (i0 + k * R >= t.rows) break;
                 float x[VEC], d[VEC];
-                V::unpack(ud[k], d);
-                S::unpack(ux[k], x);
+                V::unpack(u[k].dy, d);
+                S::unpack(u[k].x, x);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const float xh = (x[e] - mu[e]) * r[e], gz = d[e] * act_slope<ACT>(fmaf(xh, ga[e], be[e]));
@@ -407,7 +462,7 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
                     s2[e] = fmaf(gz, xh, s2[e]);
                 }
             }
-        }
+        });
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             s_1[row * a.C + c + e] = s1[e];
@@ -416,12 +471,20 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
     }
     __syncthreads();
     for (int k = R; k > 1;) {
-        const int half = (k + 1) / 2;
-        for (int j = threadIdx.x; j < (k - half) * a.C; j += kGnThreads) {
-            s_1[j] += s_1[j + half * a.C];
-            s_2[j] += s_2[j + half * a.C];
+        const int q = (k + 3) / 4;
+        for (int j = threadIdx.x; j < q * a.C; j += kGnThreads) {
+            const int p = j / a.C;
+            float u = s_1[j], v = s_2[j];
+#pragma unroll
+            for (int h = 1; h < 4; ++h) {
+                if (p + h * q >= k) break;
+                u += s_1[j + h * q * a.C];
+                v += s_2[j + h * q * a.C];
+            }
+            s_1[j] = u;
+            s_2[j] = v;
         }
-        k = half;
+        k = q;
         __syncthreads();
     }
     for (int j = threadIdx.x; j < 2 * a.C; j += kGnThreads) cols[j] = j < a.C ? s_1[j] : s_2[j - a.C];
@@ -433,8 +496,8 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
             p = fmaf(gj, s_1[j], p);
             q = fmaf(gj, s_2[j], q);
         }
-        p = wave_sum(p);
-        q = wave_sum(q);
+        p = lanes_sum<64>(p);
+        q = lanes_sum<64>(q);
         if (lane == 0) a.tiles[(int64_t)blockIdx.x * a.G + g] = make_float2(p, q);
     }
 }
@@ -467,7 +530,7 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_channels(GnArgs a, int64_t ti
 
 // the rows' second pass: dx; the workgroups past the tiles join the channels
 template <int DT, int VEC, int ACT, bool X8>
-__global__ __launch_bounds__(kGnThreads) void k_gn_tile_dx(GnArgs a, int tile_rows, int64_t tiles) {
+__global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile_rows, int64_t tiles) {
     using V = Chans<DT, VEC>;
     using S = GnSource<DT, VEC, X8>;
     if ((int64_t)blockIdx.x >= tiles) {
@@ -475,9 +538,30 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_dx(GnArgs a, int tile_ro
         return;
     }
     __shared__ float2 s_mean[kGnThreads * VEC];
+    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
+    float ga[VEC], be[VEC];
+    gn_channels<VEC>(a, c, row < R, ga, be);
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
     if (t.rows == 0) return;
+    const int64_t base = t.row0 * a.C + c, block = t.row0 * code_blocks(a.C) + c / kCodeBlock;
+    auto load = [&](int i) {
+        typename S::RawRes r;
+        (typename S::Raw&)r = S::load(a, base, block, i);
+        if (a.dres) r.res = V::load(a.dres, base + (int64_t)i * a.C);
+        return r;
+    };
+    GnRows<2, typename S::RawRes> rows{row, R, row < R ? t.rows : 0};
     const int w = a.C / a.G;
+    float mu[VEC], r[VEC], m1[VEC], m2[VEC];
+    if (row < R) {
+        rows.ask(row, rows.u, load);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float2 st = ((const float2*)a.stat)[(int64_t)t.b * a.G + (c + e) / w];
+            mu[e] = st.x;
+            r[e] = st.y;
+        }
+    }
     if (a.joined) {
         for (int g = threadIdx.x; g < a.G; g += kGnThreads) s_mean[g] = a.joined[(int64_t)t.b * a.G + g];
     } else {
@@ -487,45 +571,30 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_dx(GnArgs a, int tile_ro
         }
     }
     __syncthreads();
-    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
     if (row >= R) return;
-    float mu[VEC], r[VEC], ga[VEC], be[VEC], m1[VEC], m2[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-        const float2 st = ((const float2*)a.stat)[(int64_t)t.b * a.G + (c + e) / w], me = s_mean[(c + e) / w];
-        mu[e] = st.x;
-        r[e] = st.y;
-        ga[e] = a.gamma ? a.gamma[c + e] : 1.f;
-        be[e] = a.beta ? a.beta[c + e] : 0.f;
+        const float2 me = s_mean[(c + e) / w];
         m1[e] = me.x;
         m2[e] = me.y;
     }
-    for (int i0 = row; i0 < t.rows; i0 += kGnAhead * R) {
-        typename V::Raw ud[kGnAhead], ur[kGnAhead];
-        typename S::RawX ux[kGnAhead];
+    rows.run(load, [&](int i0, const typename S::RawRes(&u)[2]) {
 #pragma unroll
-        for (int k = 0; k < kGnAhead; ++k) {
-            const int i = i0 + k * R < t.rows ? i0 + k * R : i0;
-            ud[k] = V::load(a.dy, (t.row0 + i) * a.C + c);
-            ux[k] = S::load(a, t.row0 + i, c);
-            if (a.dres) ur[k] = V::load(a.dres, (t.row0 + i) * a.C + c);
-        }
-#pragma unroll
-        for (int k = 0; k < kGnAhead; ++k) {
+        for (int k = 0; k < 2; ++k) {
             if (i0 + k * R >= t.rows) break;
             float x[VEC], d[VEC], q[VEC] = {};
-            V::unpack(ud[k], d);
-            S::unpack(ux[k], x);
-            if (a.dres) V::unpack(ur[k], q);
+            V::unpack(u[k].dy, d);
+            S::unpack(u[k].x, x);
+            if (a.dres) V::unpack(u[k].res, q);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const float xh = (x[e] - mu[e]) * r[e];
                 const float h = d[e] * act_slope<ACT>(fmaf(xh, ga[e], be[e])) * ga[e];
                 d[e] = fmaf(r[e], h - m1[e] - xh * m2[e], q[e]);
             }
-            V::store(a.dx, (t.row0 + i0 + k * R) * a.C + c, d);
+            V::store(a.dx, base + (int64_t)(i0 + k * R) * a.C, d);
         }
-    }
+    });
 }
 
 // ---------------------------------------------------------------------------

@@ -1,0 +1,57 @@
+// lanes.hpp -- exchanges between the lanes of a wave in vector registers (a lane's partner through DPP and the swaps of
+// rows of 16 and of 32 lanes), without the trip through LDS that a shuffle takes.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+namespace spv {
+
+template <int CTRL>
+__device__ inline int dpp(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, true);
+}
+// f(own, partner's) over groups of N lanes (a power of two), the same result in each lane of a group: lanes 1 and 2 apart,
+// then, of equal quads and eights, the mirrored one; then rows of 16 and halves of the wave
+template <int N, class F>
+__device__ inline int lanes_join(int v, F&& f) {
+    if constexpr (N >= 2) v = f(v, dpp<0xB1>(v));
+    if constexpr (N >= 4) v = f(v, dpp<0x4E>(v));
+    if constexpr (N >= 8) v = f(v, dpp<0x141>(v));
+    if constexpr (N >= 16) v = f(v, dpp<0x140>(v));
+    if constexpr (N >= 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = f((int)p[0], (int)p[1]);
+    }
+    if constexpr (N >= 64) {
+        const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = f((int)p[0], (int)p[1]);
+    }
+    return v;
+}
+template <int N>
+__device__ inline float lanes_sum(float v) {
+    return __int_as_float(
+        lanes_join<N>(__float_as_int(v), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
+}
+template <int N>
+__device__ inline uint32_t lanes_max(uint32_t v) {
+    return (uint32_t)lanes_join<N>((int)v, [](int a, int b) { return (int)max((uint32_t)a, (uint32_t)b); });
+}
+// of a whole wave, in 64 bits
+__device__ inline double wave_sum(double v) {
+    auto pair = [](int lo, int hi) { return __hiloint2double(hi, lo); };
+    v += pair(dpp<0xB1>(__double2loint(v)), dpp<0xB1>(__double2hiint(v)));
+    v += pair(dpp<0x4E>(__double2loint(v)), dpp<0x4E>(__double2hiint(v)));
+    v += pair(dpp<0x141>(__double2loint(v)), dpp<0x141>(__double2hiint(v)));
+    v += pair(dpp<0x140>(__double2loint(v)), dpp<0x140>(__double2hiint(v)));
+    {
+        const auto l = __builtin_amdgcn_permlane16_swap(__double2loint(v), __double2loint(v), false, false);
+        const auto h = __builtin_amdgcn_permlane16_swap(__double2hiint(v), __double2hiint(v), false, false);
+        v = pair((int)l[0], (int)h[0]) + pair((int)l[1], (int)h[1]);
+    }
+    const auto l = __builtin_amdgcn_permlane32_swap(__double2loint(v), __double2loint(v), false, false);
+    const auto h = __builtin_amdgcn_permlane32_swap(__double2hiint(v), __double2hiint(v), false, false);
+    return pair((int)l[0], (int)h[0]) + pair((int)l[1], (int)h[1]);
+}
+
+}  // namespace spv
