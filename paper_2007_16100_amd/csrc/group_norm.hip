@@ -41,7 +41,7 @@ __device__ inline float act_slope(float z) {
 // workgroup's tile, so what belongs to a channel stays in registers over the rows; R = kGnThreads / (C / VEC).
 // ---------------------------------------------------------------------------
 constexpr int kGnThreads = 512, kGnWaves = kGnThreads / 64;
-constexpr int kGnTiles = 512;  // tiles of one long scan: two workgroups a CU
+constexpr int kGnTiles = 240;  // tiles of one long scan: with the scans' first ones a workgroup a CU
 
 template <int DT>
 constexpr int kGnVec = DT == SPV_F32 ? 4 : 8;
@@ -114,79 +114,104 @@ struct Codes {
     }
 };
 
+// a thread's channels of a vector, or `other` of each
+template <int VEC>
+__device__ inline void gn_channels(const float* p, int c, float other, float (&v)[VEC]) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = other;
+    if (p) __builtin_memcpy(v, p + c, sizeof(v));
+}
+
 struct GnTile {
     int b;            // scan
     int64_t row0;     // first row
     int rows;         // of the tile
-    int64_t n;        // rows of the scan
+    uint32_t n;       // rows of the scan
     int64_t tile0;    // number of the scan's first tile
     bool first;       // this is it
 };
-__device__ inline GnTile gn_tile(const GnArgs& a, int tile_rows, int64_t t) {
-    const ScanTile s = find_tile(a.off, a.m, a.off, a.m, a.B, 1, tile_rows, t);
+// Scan b's first tile is number off[b] / tile_rows + b: known without a pass over the scans, with room for every
+// scan's tiles.  Tile t's scan is found with 63 intervals a step.
+__device__ inline GnTile gn_tile(const GnArgs& a, uint32_t tile_rows, uint32_t t) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = a.B, step, k;
+    uint32_t o, tile;
+    do {
+        step = (hi - lo + 62) / 63;
+        const int at = lo + step * lane;
+        o = at <= hi ? (uint32_t)clamp_off(a.off[at], a.m) : 0u;
+        tile = o / tile_rows + (uint32_t)at;
+        k = __popcll(__ballot(at < hi && tile <= t));
+        k = uniform(k > 0 ? k - 1 : 0);
+        lo += step * k;
+        hi = lo + step < hi ? lo + step : hi;
+    } while (step > 1);
     GnTile g;
-    g.b = s.b;
-    g.row0 = s.first + s.col0;
-    const int64_t left = s.cols - s.col0;
-    g.rows = (int)(left < 0 ? 0 : left > tile_rows ? tile_rows : left);
-    g.n = s.cols;
-    g.tile0 = s.first / tile_rows + s.b;
-    g.first = t == g.tile0;
+    g.b = uniform(lo);
+    const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)o, k), end = (uint32_t)__builtin_amdgcn_readlane((int)o, k + 1);
+    g.tile0 = (uint32_t)__builtin_amdgcn_readlane((int)tile, k);
+    g.n = end > first ? end - first : 0u;
+    const uint32_t done = (t - (uint32_t)g.tile0) * tile_rows;  // t is at least tile0, or past all of the scans
+    g.row0 = first + done;
+    g.rows = t >= (uint32_t)g.tile0 && done < g.n ? (int)(g.n - done < tile_rows ? g.n - done : tile_rows) : 0;
+    g.first = t == (uint32_t)g.tile0;
     return g;
 }
 
-// Mean and r of a group of a scan of n rows from its tiles' means and sums of squares, by a wave.  Deviations are from
-// the first tile's mean, whose distance from the mean of all, squared, is at most (tiles) times the variance: what
-// cancels in 64 bits is a few thousand of their units.
-__device__ inline float2 gn_join_stat(const float2* part, int G, int g, int64_t tile0, int64_t n, int tile_rows, int w,
-                                      float eps) {
-    const int lane = threadIdx.x & 63;
-    const int64_t tiles = (n + tile_rows - 1) / tile_rows;
-    if (n == 0) return make_float2(0.f, 0.f);
-    part += tile0 * G + g;
-    const float first = part[0].x;
-    const double per = 1.0 / (double)n;
-    double s = 0.0, q = 0.0;
-    for (int64_t t0 = 0; t0 < tiles; t0 += 256) {
-        float2 p[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int64_t t = t0 + k * 64 + lane;
-            p[k] = part[(t < tiles ? t : 0) * G];
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int64_t t = t0 + k * 64 + lane, left = n - t * tile_rows;
-            const double rows = (double)(left < tile_rows ? left : tile_rows), d = (double)p[k].x - (double)first;
-            if (t < tiles) {
-                s += rows * d;
-                q += fma(rows * w * d, d, (double)p[k].y);
-            }
-        }
+// The tiles of a group of a scan, taken by a wave: four a lane are asked for by the constructor, before whatever
+// else the workgroup has to wait for, the others in turn.
+struct GnGroup {
+    const float2* part;
+    int64_t stride, tiles;
+    float2 p[4];
+    __device__ GnGroup(const GnArgs& a, int g, int64_t tile0, uint32_t n, uint32_t tile_rows)
+        : part(a.tiles + tile0 * a.G + g), stride(a.G), tiles((n + tile_rows - 1) / tile_rows) {
+        ask(0);
     }
-    s = wave_sum(s) * per;
-    q = wave_sum(q) * per / (double)w - s * s;
-    return make_float2((float)((double)first + s), 1.f / sqrtf((float)(q > 0.0 ? q : q == q ? 0.0 : q) + eps));
-}
-// the sums of a group of a scan from its tiles', over the count
-__device__ inline float2 gn_join_sums(const float2* part, int G, int g, int64_t tile0, int64_t n, int tile_rows, int w) {
-    const int64_t tiles = (n + tile_rows - 1) / tile_rows;
-    const double per = n > 0 ? 1.0 / ((double)n * (double)w) : 0.0;
-    double s1 = 0.0, s2 = 0.0;
-    part += tile0 * G + g;
-    for (int64_t t0 = 0; t0 < tiles; t0 += 256) {
-        float2 p[4];
+    __device__ void ask(int64_t t0) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int64_t t = t0 + k * 64 + (threadIdx.x & 63);
-            p[k] = t < tiles ? part[t * G] : make_float2(0.f, 0.f);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            s1 += (double)p[k].x;
-            s2 += (double)p[k].y;
+            p[k] = t < tiles ? part[t * stride] : make_float2(0.f, 0.f);
         }
     }
+    // f(tile, its numbers) for the lane's tiles, zeros past the last
+    template <class F>
+    __device__ void each(F&& f) {
+        for (int64_t t0 = 0;;) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f(t0 + k * 64 + (threadIdx.x & 63), p[k]);
+            t0 += 256;
+            if (t0 >= tiles) break;
+            ask(t0);
+        }
+    }
+};
+// Mean and r of a group of a scan of n rows from its tiles' means and sums of squares.  Deviations are from
+// the first tile's mean, whose distance from the mean of all, squared, is at most (tiles) times the variance: what
+// cancels in 64 bits is a few thousand of their units.
+__device__ inline float2 gn_join_stat(GnGroup& t, uint32_t n, uint32_t tile_rows, int w, float eps) {
+    if (n == 0) return make_float2(0.f, 0.f);
+    const double first = (double)__int_as_float(uniform(__float_as_int(t.p[0].x))), per = 1.0 / (double)n;
+    double s = 0.0, q = 0.0;
+    t.each([&](int64_t i, const float2& p) {
+        const int64_t left = (int64_t)n - i * tile_rows;
+        const double rows = (double)(left < 0 ? 0 : left < tile_rows ? left : tile_rows), d = (double)p.x - first;
+        s = fma(rows, d, s);
+        q += fma(rows * w * d, d, (double)p.y);
+    });
+    s = wave_sum(s) * per;
+    q = wave_sum(q) * per / (double)w - s * s;
+    return make_float2((float)(first + s), 1.f / sqrtf((float)(q > 0.0 ? q : q == q ? 0.0 : q) + eps));
+}
+// the sums of a group of a scan from its tiles', over the count
+__device__ inline float2 gn_join_sums(GnGroup& t, uint32_t n, int w) {
+    const double per = n > 0 ? 1.0 / ((double)n * (double)w) : 0.0;
+    double s1 = 0.0, s2 = 0.0;
+    t.each([&](int64_t, const float2& p) {
+        s1 += (double)p.x;
+        s2 += (double)p.y;
+    });
     return make_float2((float)(wave_sum(s1) * per), (float)(wave_sum(s2) * per));
 }
 
@@ -216,25 +241,54 @@ struct GnRows {
 
 // a wave takes a group of a scan
 template <bool STAT>
-__global__ __launch_bounds__(256) void k_gn_join(GnArgs a, int tile_rows) {
+__global__ __launch_bounds__(256) void k_gn_join(GnArgs a, uint32_t tile_rows) {
     const int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (u >= (int64_t)a.B * a.G) return;
     const int b = (int)(u / a.G), g = (int)(u % a.G);
-    const int64_t r0 = clamp_off(a.off[b], a.m), r1 = clamp_off(a.off[b + 1], a.m), n = r1 > r0 ? r1 - r0 : 0;
-    const float2 v = STAT ? gn_join_stat(a.tiles, a.G, g, r0 / tile_rows + b, n, tile_rows, a.C / a.G, a.eps)
-                          : gn_join_sums(a.tiles, a.G, g, r0 / tile_rows + b, n, tile_rows, a.C / a.G);
+    const uint32_t r0 = (uint32_t)clamp_off(a.off[b], a.m), r1 = (uint32_t)clamp_off(a.off[b + 1], a.m);
+    const uint32_t n = r1 > r0 ? r1 - r0 : 0u;
+    GnGroup t(a, g, (int64_t)(r0 / tile_rows) + b, n, tile_rows);
+    const float2 v = STAT ? gn_join_stat(t, n, tile_rows, a.C / a.G, a.eps) : gn_join_sums(t, n, a.C / a.G);
     if ((threadIdx.x & 63) == 0) a.joined[u] = v;
 }
 
+// The groups of a tile of `rows` rows, joined from the units' means and squares: val[R][C / unit], L lanes a group.
+// A thread's row holds every R-th one.
+template <int L>
+__device__ inline void gn_units(const GnArgs& a, int rows, int R, int w, int unit, const float2* val) {
+    const int l = threadIdx.x & (L - 1), per = w / unit, units = a.C / unit, all = R * per;
+    const int least = rows / R, more = rows - least * R;  // a thread's row has least rows, the first ones one more
+    const float inv = 1.f / ((float)rows * (float)per), by = 1.f / (float)per;
+    for (int g0 = 0; g0 < a.G; g0 += kGnThreads / L) {  // all lanes take part in the sums
+        const int g = g0 + (int)threadIdx.x / L;
+        const float2* v = val + (g < a.G ? g : 0) * per;
+        const float first = v[0].x;  // equal values give their mean exactly
+        float s = 0.f, q = 0.f;
+        for (int j = l; j < all; j += L) {
+            const int r = (int)(((float)j + 0.5f) * by);
+            s = fmaf((float)(least + (r < more)), v[r * units + (j - r * per)].x - first, s);
+        }
+        const float mu = fmaf(lanes_sum<L>(s), inv, first);
+        for (int j = l; j < all; j += L) {
+            const int r = (int)(((float)j + 0.5f) * by);
+            const float2 p = v[r * units + (j - r * per)];
+            const float d = p.x - mu;
+            q += fmaf(d * d, (float)((least + (r < more)) * unit), p.y);
+        }
+        q = lanes_sum<L>(q);
+        if (l == 0 && g < a.G) a.tiles[(int64_t)blockIdx.x * a.G + g] = make_float2(mu, q);
+    }
+}
+
 // A tile's mean and sum of squared deviations of each group.  A thread keeps the running mean of each of its channels and
-// the squares of the deviations from it, four rows at a time: no cancellation however far from zero the rows sit.  The
-// threads of a channel are then joined two by two in LDS, and the channels of a group by a wave.
+// the squares of the deviations from it, four rows at a time: no cancellation however far from zero the rows sit.
 template <int DT, int VEC>
 __global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_rows) {
     using V = Chans<DT, VEC>;
-    __shared__ float s_mean[kGnThreads * VEC], s_sq[kGnThreads * VEC], s_n[2][kGnThreads];
+    __shared__ float2 s_val[kGnThreads * VEC];
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
     if (t.rows == 0) return;
+    const int w = a.C / a.G, unit = VEC > 1 && w % VEC == 0 ? VEC : VEC > 2 && w % 4 == 0 ? 4 : VEC > 1 && w % 2 == 0 ? 2 : 1;
     const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
     if (row < R) {
         float mean[VEC], sq[VEC], n = 0.f;
@@ -278,62 +332,26 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_
                 }
             }
         });
+        // equal counts: units of two, four and eight channels, while a group is made of those
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            s_mean[row * a.C + c + e] = mean[e];
-            s_sq[row * a.C + c + e] = sq[e];
+        for (int h = 1; h < VEC; h *= 2) {
+            if (w % (2 * h)) break;
+#pragma unroll
+            for (int e = 0; e + h < VEC; e += 2 * h) {
+                const float d = mean[e + h] - mean[e];
+                mean[e] = fmaf(d, 0.5f, mean[e]);
+                sq[e] += fmaf(d * d, 0.5f * n * (float)h, sq[e + h]);
+            }
         }
-        if (c == 0) s_n[0][row] = n;
+        const int units = a.C / unit;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (e % unit == 0) s_val[row * units + (c + e) / unit] = make_float2(mean[e], sq[e]);
     }
     __syncthreads();
-    // four rows into one, while there are several: rows k, k + q, k + 2 q, k + 3 q, the first of which holds the most
-    int which = 0;
-    for (int k = R; k > 1; which ^= 1) {
-        const int q = (k + 3) / 4;
-        for (int j = threadIdx.x; j < q * a.C; j += kGnThreads) {
-            const int p = j / a.C;
-            float n = s_n[which][p], mean = s_mean[j], sq = s_sq[j];
-#pragma unroll
-            for (int h = 1; h < 4; ++h) {
-                if (p + h * q >= k) break;
-                const int o = j + h * q * a.C;
-                const float nb = s_n[which][p + h * q];
-                if (nb > 0.f) {
-                    const float d = s_mean[o] - mean, f = nb * __builtin_amdgcn_rcpf(n + nb);
-                    mean = fmaf(d, f, mean);
-                    sq += fmaf(d * d, n * f, s_sq[o]);
-                    n += nb;
-                }
-            }
-            s_mean[j] = mean;
-            s_sq[j] = sq;
-            if (j == p * a.C) s_n[which ^ 1][p] = n;
-        }
-        k = q;
-        __syncthreads();
-    }
-    const int w = a.C / a.G, lane = threadIdx.x & 63;
-    for (int g = threadIdx.x >> 6; g < a.G; g += kGnWaves) {
-        float s = 0.f, q = 0.f;
-        for (int j = lane; j < w; j += 64) s += s_mean[g * w + j];
-        const float mu = lanes_sum<64>(s) / (float)w;
-        for (int j = lane; j < w; j += 64) {
-            const float d = s_mean[g * w + j] - mu;
-            q += fmaf(d * d, (float)t.rows, s_sq[g * w + j]);
-        }
-        q = lanes_sum<64>(q);
-        if (lane == 0) a.tiles[(int64_t)blockIdx.x * a.G + g] = make_float2(mu, q);
-    }
-}
-
-// gamma and beta of a thread's channels
-template <int VEC>
-__device__ inline void gn_channels(const GnArgs& a, int c, bool on, float (&ga)[VEC], float (&be)[VEC]) {
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        ga[e] = on && a.gamma ? a.gamma[c + e] : 1.f;
-        be[e] = on && a.beta ? a.beta[c + e] : 0.f;
-    }
+    // a group's units of all the threads' rows, by 64 lanes or by 8
+    if (R * (w / unit) > 32) gn_units<64>(a, t.rows, R, w, unit, s_val);
+    else gn_units<8>(a, t.rows, R, w, unit, s_val);
 }
 
 // the rows' second pass: y, and x in 8 bits (CODE: whole blocks of 32 channels)
@@ -342,10 +360,13 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_apply(GnArgs a, int tile
     using V = Chans<DT, VEC>;
     __shared__ float2 s_stat[kGnThreads * VEC];  // at most as many groups as channels
     const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
-    float ga[VEC], be[VEC];
-    gn_channels<VEC>(a, c, row < R, ga, be);
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
     if (t.rows == 0 && !(t.first && a.stat)) return;
+    const int wave = threadIdx.x >> 6;
+    GnGroup first(a, wave < a.G ? wave : 0, t.tile0, a.joined ? 0u : t.n, tile_rows);
+    float ga[VEC], be[VEC];
+    gn_channels<VEC>(a.gamma, c, 1.f, ga);
+    gn_channels<VEC>(a.beta, c, 0.f, be);
     const int64_t base = t.row0 * a.C + c;
     auto load = [&](int i) { return V::load(a.x, base + (int64_t)i * a.C); };
     GnRows<4, typename V::Raw> rows{row, R, row < R ? t.rows : 0};
@@ -354,8 +375,9 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_apply(GnArgs a, int tile
     if (a.joined) {
         for (int g = threadIdx.x; g < a.G; g += kGnThreads) s_stat[g] = a.joined[(int64_t)t.b * a.G + g];
     } else {
-        for (int g = threadIdx.x >> 6; g < a.G; g += kGnWaves) {
-            const float2 v = gn_join_stat(a.tiles, a.G, g, t.tile0, t.n, tile_rows, w, a.eps);
+        for (int g = wave; g < a.G; g += kGnWaves) {
+            if (g != wave) first = GnGroup(a, g, t.tile0, t.n, tile_rows);
+            const float2 v = gn_join_stat(first, t.n, tile_rows, w, a.eps);
             if ((threadIdx.x & 63) == 0) s_stat[g] = v;
         }
     }
@@ -419,6 +441,21 @@ struct GnSource {
     }
 };
 
+// mean and r of a thread's channels
+template <int VEC>
+__device__ inline void gn_stat(const GnArgs& a, int b, int c, int w, float (&mu)[VEC], float (&r)[VEC]) {
+    const float2* st = (const float2*)a.stat + (int64_t)b * a.G;
+    int g = c / w, left = w - (c - g * w);  // channels of the group that are still to come
+    float2 v[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        v[e] = st[g];
+        if (--left == 0 && g + 1 < a.G) ++g, left = w;
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) mu[e] = v[e].x, r[e] = v[e].y;
+}
+
 // a tile's sums of gz and gz xh, of each channel and (times gamma) of each group
 template <int DT, int VEC, int ACT, bool X8>
 __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_rows) {
@@ -426,8 +463,6 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
     using S = GnSource<DT, VEC, X8>;
     __shared__ float s_1[kGnThreads * VEC], s_2[kGnThreads * VEC];
     const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
-    float ga[VEC], be[VEC];
-    gn_channels<VEC>(a, c, row < R, ga, be);
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
     const int w = a.C / a.G;
     float* cols = a.part + (int64_t)blockIdx.x * 2 * a.C;
@@ -436,18 +471,16 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
         return;
     }
     if (row < R) {
-        float mu[VEC], r[VEC], s1[VEC], s2[VEC];
+        float mu[VEC], r[VEC], ga[VEC], be[VEC], s1[VEC], s2[VEC];
         const int64_t base = t.row0 * a.C + c, block = t.row0 * code_blocks(a.C) + c / kCodeBlock;
         auto load = [&](int i) { return S::load(a, base, block, i); };
         GnRows<2, typename S::Raw> rows{row, R, t.rows};
+        gn_channels<VEC>(a.gamma, c, 1.f, ga);
+        gn_channels<VEC>(a.beta, c, 0.f, be);
+        gn_stat<VEC>(a, t.b, c, w, mu, r);
         rows.ask(row, rows.u, load);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float2 st = ((const float2*)a.stat)[(int64_t)t.b * a.G + (c + e) / w];
-            mu[e] = st.x;
-            r[e] = st.y;
-            s1[e] = s2[e] = 0.f;
-        }
+        for (int e = 0; e < VEC; ++e) s1[e] = s2[e] = 0.f;
         rows.run(load, [&](int i0, const typename S::Raw(&u)[2]) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -528,21 +561,21 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_channels(GnArgs a, int64_t ti
     gn_join_channels(a, tiles, (int)blockIdx.x);
 }
 
-// the rows' second pass: dx; the workgroups past the tiles join the channels
+// the rows' second pass: dx; the first workgroups join the channels
 template <int DT, int VEC, int ACT, bool X8>
-__global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile_rows, int64_t tiles) {
+__global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile_rows, int64_t tiles, unsigned join) {
     using V = Chans<DT, VEC>;
     using S = GnSource<DT, VEC, X8>;
-    if ((int64_t)blockIdx.x >= tiles) {
-        gn_join_channels(a, tiles, (int)(blockIdx.x - tiles));
+    if (blockIdx.x < join) {
+        gn_join_channels(a, tiles, (int)blockIdx.x);
         return;
     }
     __shared__ float2 s_mean[kGnThreads * VEC];
     const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
-    float ga[VEC], be[VEC];
-    gn_channels<VEC>(a, c, row < R, ga, be);
-    const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
+    const GnTile t = gn_tile(a, tile_rows, blockIdx.x - join);
     if (t.rows == 0) return;
+    const int wave = threadIdx.x >> 6;
+    GnGroup first(a, wave < a.G ? wave : 0, t.tile0, a.joined ? 0u : t.n, tile_rows);
     const int64_t base = t.row0 * a.C + c, block = t.row0 * code_blocks(a.C) + c / kCodeBlock;
     auto load = [&](int i) {
         typename S::RawRes r;
@@ -552,21 +585,17 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
     };
     GnRows<2, typename S::RawRes> rows{row, R, row < R ? t.rows : 0};
     const int w = a.C / a.G;
-    float mu[VEC], r[VEC], m1[VEC], m2[VEC];
-    if (row < R) {
-        rows.ask(row, rows.u, load);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float2 st = ((const float2*)a.stat)[(int64_t)t.b * a.G + (c + e) / w];
-            mu[e] = st.x;
-            r[e] = st.y;
-        }
-    }
+    float mu[VEC], r[VEC], ga[VEC], be[VEC], m1[VEC], m2[VEC];
+    gn_channels<VEC>(a.gamma, c, 1.f, ga);
+    gn_channels<VEC>(a.beta, c, 0.f, be);
+    gn_stat<VEC>(a, t.b, c, w, mu, r);
+    if (row < R) rows.ask(row, rows.u, load);
     if (a.joined) {
         for (int g = threadIdx.x; g < a.G; g += kGnThreads) s_mean[g] = a.joined[(int64_t)t.b * a.G + g];
     } else {
-        for (int g = threadIdx.x >> 6; g < a.G; g += kGnWaves) {
-            const float2 v = gn_join_sums(a.tiles, a.G, g, t.tile0, t.n, tile_rows, w);
+        for (int g = wave; g < a.G; g += kGnWaves) {
+            if (g != wave) first = GnGroup(a, g, t.tile0, t.n, tile_rows);
+            const float2 v = gn_join_sums(first, t.n, w);
             if ((threadIdx.x & 63) == 0) s_mean[g] = v;
         }
     }
@@ -821,7 +850,7 @@ static void gn_backward_tiles(hipStream_t s, GnArgs a) {
     k_gn_tile_sums<DT, VEC, ACT, X8><<<(unsigned)tiles, kGnThreads, 0, s>>>(a, rows);
     if (a.dx && gn_join_apart(a)) k_gn_join<false><<<(unsigned)(((int64_t)a.B * a.G + 3) / 4), 256, 0, s>>>(a, rows);
     else a.joined = nullptr;
-    if (a.dx) k_gn_tile_dx<DT, VEC, ACT, X8><<<(unsigned)tiles + join, kGnThreads, 0, s>>>(a, rows, tiles);
+    if (a.dx) k_gn_tile_dx<DT, VEC, ACT, X8><<<(unsigned)tiles + join, kGnThreads, 0, s>>>(a, rows, tiles, join);
     else k_gn_channels<<<join, kGnThreads, 0, s>>>(a, tiles);
 }
 void launch_group_norm_backward(hipStream_t s, const GnArgs& a) {
