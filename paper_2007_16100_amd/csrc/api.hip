@@ -940,7 +940,7 @@ spv_status spv_checkpoint8_read(void* stream, const int8_t* codes, const uint8_t
     if (m_cap == 0) return SPV_OK;
     if (!out || !codes || !exps || out == (const void*)codes || out == (const void*)exps) return SPV_ERR_INVALID_ARG;
     launch_checkpoint8_read((hipStream_t)stream, Saved8{const_cast<int8_t*>(codes), const_cast<uint8_t*>(exps)}, out,
-                            m_dev, m_cap, C, (int)dt);
+                            RowRange{m_cap, m_dev, nullptr, 0}, C, (int)dt);
     return hip_check();
 }
 

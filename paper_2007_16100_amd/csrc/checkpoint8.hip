@@ -8,106 +8,389 @@ namespace spv {
 __device__ inline int64_t RowRange::begin() const { return off ? clamp_off(off[0], cap) : 0; }
 __device__ inline int64_t RowRange::end() const { return off ? clamp_off(off[B], cap) : clamp_rows(m_dev, cap); }
 
-// a thread takes a block of 32 channels
+// Half a wave takes a block of 32 channels of a row, a lane a channel: any width and alignment.
+template <int DT>
+__global__ __launch_bounds__(256) void k_code8_any(const void* x, Saved8 to, RowRange rows, int C) {
+    const int nb = code_blocks(C), l = threadIdx.x & 31;
+    const int64_t end = rows.end(), step = (int64_t)gridDim.x * 8;
+    for (int64_t i = rows.begin() + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < end; i += step)
+        for (int b = 0; b < nb; ++b) {
+            const int c = b * kCodeBlock + l;
+            const float v = c < C ? ld_feat<DT>(x, i * C + c) : 0.f;
+            const int byte = code_exp<DT>(lanes_max<32>(finite_bits(v)));
+            if (c < C) to.codes[i * C + c] = (int8_t)code_of(v, code_rate(byte));
+            if (l == 0) to.exps[i * nb + b] = (uint8_t)byte;
+        }
+}
+template <int DT>
+__global__ __launch_bounds__(256) void k_code8_read_any(Saved8 from, void* out, RowRange rows, int C) {
+    const int nb = code_blocks(C), l = threadIdx.x & 31;
+    const int64_t end = rows.end(), step = (int64_t)gridDim.x * 8;
+    for (int64_t i = rows.begin() + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < end; i += step)
+        for (int b = 0; b < nb; ++b) {
+            const int c = b * kCodeBlock + l;
+            if (c < C) st_feat<DT>(out, i * C + c, code_value(from.codes[i * C + c], code_step(from.exps[i * nb + b])));
+        }
+}
+
+// Rows of whole blocks: the blocks of all rows are one after the other.  A thread takes 16 bytes of x, four times over.
+template <int DT>
+constexpr int kCodeVec = DT == SPV_F32 ? 4 : 8;
+constexpr int kCodeAhead = 4;
+
 template <int DT>
 __global__ __launch_bounds__(256) void k_code8(const void* x, Saved8 to, RowRange rows, int C) {
-    const int nb = code_blocks(C);
-    const int64_t end = rows.end() * nb;
-    for (int64_t t = rows.begin() * nb + (int64_t)blockIdx.x * 256 + threadIdx.x; t < end; t += (int64_t)gridDim.x * 256) {
-        const int64_t i = t / nb;
-        const int c0 = (int)(t % nb) * kCodeBlock, c1 = c0 + kCodeBlock < C ? c0 + kCodeBlock : C;
-        uint32_t top = 0;
-        for (int c = c0; c < c1; ++c) top = max(top, finite_bits(ld_feat<DT>(x, i * C + c)));
-        const int e = code_exp<DT>(top);
-        const float rate = code_rate(e);
-        to.exps[t] = (uint8_t)e;
-        for (int c = c0; c < c1; ++c) to.codes[i * C + c] = (int8_t)code_of(ld_feat<DT>(x, i * C + c), rate);
+    constexpr int V = kCodeVec<DT>, LANES = kCodeBlock / V;
+    const int64_t per = C / V, end = rows.end() * per;  // vectors
+    const int64_t t0 = rows.begin() * per + (int64_t)blockIdx.x * (256 * kCodeAhead) + threadIdx.x;
+    uint4 u[kCodeAhead];
+#pragma unroll
+    for (int k = 0; k < kCodeAhead; ++k) {
+        const int64_t t = t0 + k * 256;
+        u[k] = t < end ? ((const uint4*)x)[t] : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < kCodeAhead; ++k) {
+        const int64_t t = t0 + k * 256;
+        float f[V];
+        uint32_t w[V / 4];
+        unpack16<DT>(u[k], f);
+        const int byte = code_block<DT, V, LANES>(f, w);
+        if (t >= end) break;  // whole blocks
+        if constexpr (V == 8) ((uint2*)to.codes)[t] = make_uint2(w[0], w[1]);
+        else ((uint32_t*)to.codes)[t] = w[0];
+        if (t % LANES == 0) to.exps[t / LANES] = (uint8_t)byte;
+    }
+}
+template <int DT>
+__global__ __launch_bounds__(256) void k_code8_read(Saved8 from, void* out, RowRange rows, int C) {
+    constexpr int V = kCodeVec<DT>, LANES = kCodeBlock / V;
+    const int64_t end = rows.end() * (C / V), t0 = (int64_t)blockIdx.x * (256 * kCodeAhead) + threadIdx.x;
+    uint32_t w[kCodeAhead][V / 4];
+    int e[kCodeAhead];
+#pragma unroll
+    for (int k = 0; k < kCodeAhead; ++k) {
+        const int64_t t = t0 + k * 256;
+        if (t >= end) continue;
+        __builtin_memcpy(w[k], (const char*)__builtin_assume_aligned(from.codes, V) + t * V, V);
+        e[k] = from.exps[t / LANES];
+    }
+#pragma unroll
+    for (int k = 0; k < kCodeAhead; ++k) {
+        const int64_t t = t0 + k * 256;
+        if (t >= end) break;
+        float f[V];
+        const float step = code_step(e[k]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = code_value((int8_t)(w[k][j / 4] >> (8 * (j % 4))), step);
+        ((uint4*)out)[t] = pack16<DT>(f);
     }
 }
 
 template <int DT>
-__global__ __launch_bounds__(256) void k_code8_read(Saved8 from, void* out, const int64_t* m_dev, int64_t m_cap, int C) {
-    const int64_t all = clamp_rows(m_dev, m_cap) * C;
-    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < all; t += (int64_t)gridDim.x * 256) {
-        const int64_t i = t / C;
-        const int c = (int)(t % C);
-        st_feat<DT>(out, t, code_value(from.codes[t], code_step(from.exps[i * code_blocks(C) + c / kCodeBlock])));
-    }
+static bool code8_wide(const void* x, const Saved8& s, int C) {
+    return C % kCodeBlock == 0 && (uintptr_t)x % 16 == 0 && (uintptr_t)s.codes % kCodeVec<DT> == 0;
 }
-
-static unsigned grid_for(int64_t threads) {
-    const int64_t g = (threads + 255) / 256;
-    return (unsigned)(g < 1 ? 1 : g > 65536 ? 65536 : g);
+static unsigned grid_rows(int64_t m) {
+    const int64_t g = (m + 7) / 8;
+    return (unsigned)(g < 1 ? 1 : g > 16384 ? 16384 : g);
+}
+template <int DT>
+static unsigned grid_vecs(int64_t m, int C) {
+    const int64_t per = 256 * kCodeAhead;
+    return (unsigned)((m * (C / kCodeVec<DT>) + per - 1) / per);
+}
+template <int DT>
+static void code8(hipStream_t s, const void* x, const Saved8& to, const RowRange& rows, int C) {
+    if (code8_wide<DT>(x, to, C) && rows.cap * C < ((int64_t)1 << 40))
+        k_code8<DT><<<grid_vecs<DT>(rows.cap, C), 256, 0, s>>>(x, to, rows, C);
+    else
+        k_code8_any<DT><<<grid_rows(rows.cap), 256, 0, s>>>(x, to, rows, C);
+}
+template <int DT>
+static void code8_read(hipStream_t s, const Saved8& from, void* out, const RowRange& rows, int C) {
+    if (code8_wide<DT>(out, from, C) && rows.cap * C < ((int64_t)1 << 40))
+        k_code8_read<DT><<<grid_vecs<DT>(rows.cap, C), 256, 0, s>>>(from, out, rows, C);
+    else
+        k_code8_read_any<DT><<<grid_rows(rows.cap), 256, 0, s>>>(from, out, rows, C);
 }
 void launch_checkpoint8(hipStream_t s, const void* x, Saved8 to, const RowRange& rows, int C, int dt) {
-    const unsigned g = grid_for(rows.cap * code_blocks(C));
-    if (dt == SPV_F32) k_code8<SPV_F32><<<g, 256, 0, s>>>(x, to, rows, C);
-    else if (dt == SPV_BF16) k_code8<SPV_BF16><<<g, 256, 0, s>>>(x, to, rows, C);
-    else k_code8<SPV_F16><<<g, 256, 0, s>>>(x, to, rows, C);
+    if (dt == SPV_F32) code8<SPV_F32>(s, x, to, rows, C);
+    else if (dt == SPV_BF16) code8<SPV_BF16>(s, x, to, rows, C);
+    else code8<SPV_F16>(s, x, to, rows, C);
 }
-void launch_checkpoint8_read(hipStream_t s, Saved8 from, void* out, const int64_t* m_dev, int64_t m_cap, int C, int dt) {
-    const unsigned g = grid_for(m_cap * C);
-    if (dt == SPV_F32) k_code8_read<SPV_F32><<<g, 256, 0, s>>>(from, out, m_dev, m_cap, C);
-    else if (dt == SPV_BF16) k_code8_read<SPV_BF16><<<g, 256, 0, s>>>(from, out, m_dev, m_cap, C);
-    else k_code8_read<SPV_F16><<<g, 256, 0, s>>>(from, out, m_dev, m_cap, C);
+void launch_checkpoint8_read(hipStream_t s, Saved8 from, void* out, const RowRange& rows, int C, int dt) {
+    if (dt == SPV_F32) code8_read<SPV_F32>(s, from, out, rows, C);
+    else if (dt == SPV_BF16) code8_read<SPV_BF16>(s, from, out, rows, C);
+    else code8_read<SPV_F16>(s, from, out, rows, C);
 }
 
 // ---------------------------------------------------------------------------
-// dW = in^T da: a workgroup takes 32 x 32 of dW over every S-th chunk of 32 rows
+// dW = in^T da.  A workgroup takes TM x TN tiles of 32 x 32 of dW and a share of the rows, its waves some of those each,
+// with nothing between them but the sum at the end.  The shares' sums go to the workspace and are joined in 64 bits.
 // ---------------------------------------------------------------------------
-constexpr int kWg8Rows = 32;
+constexpr int kWg8Waves = 4;
+constexpr int kWg8Step = 32;   // rows of a wave's step
+constexpr int kWg8Most = 3;    // tiles of a side of a workgroup's block
+constexpr int kWg8Groups = 256;  // workgroups, as far as the rows go
+
+// tiles of a side: the fewest padded, then the most
+static int wgrad8_side(int C) {
+    const int t = (C + 31) / 32;
+    int best = 1;
+    for (int k = 2; k <= kWg8Most; ++k)
+        if ((t + k - 1) / k * k <= (t + best - 1) / best * best) best = k;
+    return best;
+}
+static int wgrad8_blocks(int C) { return ((C + 31) / 32 + wgrad8_side(C) - 1) / wgrad8_side(C); }
 static int wgrad8_parts(int64_t m_cap, int Cin, int Cout) {
-    const int64_t tiles = (int64_t)((Cin + 31) / 32) * ((Cout + 31) / 32), chunks = (m_cap + kWg8Rows - 1) / kWg8Rows;
-    int64_t s = (1024 + tiles - 1) / tiles;
-    if (s > chunks) s = chunks;
+    const int64_t blocks = (int64_t)wgrad8_blocks(Cin) * wgrad8_blocks(Cout);
+    const int64_t rows = (m_cap + kWg8Waves * kWg8Step - 1) / (kWg8Waves * kWg8Step);
+    int64_t s = kWg8Groups / blocks;
+    if (s >= 8) s = s / 8 * 8;  // shares of the same rows on one die
+    if (s > rows) s = rows;
     return (int)(s < 1 ? 1 : s);
 }
 float* plan_wgrad8_ws(Arena& a, int64_t m_cap, int Cin, int Cout) {
     return a.take<float>((size_t)wgrad8_parts(m_cap, Cin, Cout) * Cin * Cout);
 }
 
-template <int DT>
-__global__ __launch_bounds__(256) void k_wgrad8(Wgrad8Args a) {
-    __shared__ float xs[kWg8Rows][33], ds[kWg8Rows][33];
-    const int ci = blockIdx.y * 32, co = blockIdx.z * 32, tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    const int64_t m = clamp_rows(a.m_dev, a.m_cap);
-    float acc[4] = {};
-    for (int64_t r0 = (int64_t)blockIdx.x * kWg8Rows; r0 < m; r0 += (int64_t)gridDim.x * kWg8Rows) {
-        __syncthreads();
-        for (int r = ty; r < kWg8Rows; r += 8) {
-            const int64_t i = r0 + r;
-            xs[r][tx] = i < m && ci + tx < a.Cin ? code_value(a.in.codes[i * a.Cin + ci + tx],
-                                                              code_step(a.in.exps[i * code_blocks(a.Cin) + blockIdx.y]))
-                                                 : 0.f;
-            ds[r][tx] = i < m && co + tx < a.Cout ? ld_feat<DT>(a.da, i * a.Cout + co + tx) : 0.f;
-        }
-        __syncthreads();
-        for (int r = 0; r < kWg8Rows; ++r)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = fmaf(xs[r][ty + 8 * j], ds[r][tx], acc[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (ci + ty + 8 * j < a.Cin && co + tx < a.Cout)
-            a.part[((int64_t)blockIdx.x * a.Cin + ci + ty + 8 * j) * a.Cout + co + tx] = acc[j];
+struct Wg8Block {
+    int part, ci, co;   // share of the rows, first channels
+    int64_t r0, r1;     // the wave's rows
+};
+// the shares come first in the grid, so that the blocks of one share, which read the same rows, run on one die
+template <int TM, int TN>
+__device__ inline Wg8Block wg8_block(const Wgrad8Args& a, int parts) {
+    Wg8Block b;
+    b.part = (int)(blockIdx.x % (unsigned)parts);
+    const int nm = (a.Cin + 32 * TM - 1) / (32 * TM), block = (int)(blockIdx.x / (unsigned)parts);
+    b.ci = block % nm * (32 * TM);
+    b.co = block / nm * (32 * TN);
+    const int64_t m = clamp_rows(a.m_dev, a.m_cap), steps = (m + kWg8Step - 1) / kWg8Step;
+    const int64_t waves = (int64_t)parts * kWg8Waves, w = (int64_t)b.part * kWg8Waves + uniform((int)(threadIdx.x >> 6));
+    b.r0 = steps * w / waves * kWg8Step;
+    b.r1 = steps * (w + 1) / waves * kWg8Step;
+    if (b.r1 > m) b.r1 = m;
+    return b;
 }
 
-__global__ __launch_bounds__(256) void k_wgrad8_join(const float* part, int parts, int64_t n, float* dW) {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (t >= n) return;
+// the waves' sums of a block, one after the other in LDS, and then to the share's part of the workspace
+template <int TM, int TN>
+__device__ inline void wg8_store(const Wgrad8Args& a, const Wg8Block& b, const f32x16 (&acc)[TM][TN], float* lds) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, h = lane >> 5;
+    for (int w = 0; w < kWg8Waves; ++w) {
+        __syncthreads();
+        if (wave == w)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float* p = lds + (32 * i + 8 * (e / 4) + 4 * h + e % 4) * (32 * TN) + 32 * j + c;
+                        *p = w ? *p + acc[i][j][e] : acc[i][j][e];
+                    }
+    }
+    __syncthreads();
+    float* out = a.part + (int64_t)b.part * a.Cin * a.Cout;
+    for (int t = threadIdx.x; t < 32 * TM * 32 * TN; t += 64 * kWg8Waves) {
+        const int i = b.ci + t / (32 * TN), j = b.co + t % (32 * TN);
+        if (i < a.Cin && j < a.Cout) out[(int64_t)i * a.Cout + j] = lds[t];
+    }
+}
+
+// 16-bit types, 16 channels a time: a wave brings 32 rows of codes, as values of the type, and of da into its own part of LDS
+// (the next 32 are on the way) and reads both back transposed: the matrix cores sum over rows.
+template <int DT, int TM, int TN>
+__global__ __launch_bounds__(64 * kWg8Waves, TM * TN > 6 ? 1 : 2) void k_wgrad8(Wgrad8Args a, int parts) {
+    constexpr int BM = 32 * TM, BN = 32 * TN, LM = 2 * BM + 16, LN = 2 * BN + 16;  // bytes from row to row in LDS
+    constexpr int QM = BM / 16, QN = BN / 8;                     // 16-byte chunks of a row
+    constexpr int KM = kWg8Step * QM / 64, KN = kWg8Step * QN / 64;  // of a lane
+    constexpr int SIZE = kWg8Step * (LM + LN);
+    constexpr int LDS = kWg8Waves * SIZE > BM * BN * 4 ? kWg8Waves * SIZE : BM * BN * 4;
+    typedef short i16x8 __attribute__((ext_vector_type(8)));
+    typedef __attribute__((address_space(3))) i16x4 lds4;
+    __shared__ __align__(16) char lds[LDS];
+    const Wg8Block b = wg8_block<TM, TN>(a, parts);
+    const int lane = threadIdx.x & 63, nb = code_blocks(a.Cin);
+    char *lx = lds + (threadIdx.x >> 6) * SIZE, *ld = lx + kWg8Step * LM;
+    f32x16 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    uint4 ux[KM], ud[KN];
+    int ue[KM];
+    auto ask = [&](int64_t r0) {
+#pragma unroll
+        for (int k = 0; k < KM; ++k) {
+            const int t = lane + 64 * k, c = b.ci + t % QM * 16;
+            const int64_t r = r0 + t / QM;
+            const bool on = r < b.r1 && c < a.Cin;
+            ux[k] = on ? *(const uint4*)(a.in.codes + r * a.Cin + c) : make_uint4(0, 0, 0, 0);
+            ue[k] = on ? a.in.exps[r * nb + c / kCodeBlock] : 1;
+        }
+#pragma unroll
+        for (int k = 0; k < KN; ++k) {
+            const int t = lane + 64 * k, c = b.co + t % QN * 8;
+            const int64_t r = r0 + t / QN;
+            ud[k] = r < b.r1 && c < a.Cout ? *(const uint4*)((const uint16_t*)a.da + r * a.Cout + c)
+                                           : make_uint4(0, 0, 0, 0);
+        }
+    };
+    if (b.r0 < b.r1) ask(b.r0);
+    for (int64_t r0 = b.r0; r0 < b.r1; r0 += kWg8Step) {
+#pragma unroll
+        for (int k = 0; k < KM; ++k) {
+            const int t = lane + 64 * k;
+            const uint32_t w[4] = {ux[k].x, ux[k].y, ux[k].z, ux[k].w};
+            const float step = code_step(ue[k]);
+            uint32_t v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t q = w[e / 2] >> (16 * (e % 2));
+                v[e] = pack2<DT>(code_value((int8_t)q, step), code_value((int8_t)(q >> 8), step));
+            }
+            uint4* p = (uint4*)(lx + t / QM * LM + t % QM * 32);
+            p[0] = make_uint4(v[0], v[1], v[2], v[3]);
+            p[1] = make_uint4(v[4], v[5], v[6], v[7]);
+        }
+#pragma unroll
+        for (int k = 0; k < KN; ++k) {
+            const int t = lane + 64 * k;
+            *(uint4*)(ld + t / QN * LN + t % QN * 16) = ud[k];
+        }
+        if (r0 + kWg8Step < b.r1) ask(r0 + kWg8Step);
+        lds_wait();
+        // lanes 16 g .. 16 g + 15 read four rows of 16 channels, and each gets its channel of the four
+        const int t = lane & 15, g = lane >> 4, row = 4 * (g >> 1) + (t >> 2), at = (16 * (g & 1) + 4 * (t & 3)) * 2;
+        auto transposed = [&](const char* p, int LD) {
+            const uint32_t q = lds_addr(p) + row * LD + at;
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)q);
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(q + 8 * LD));
+            return __builtin_bit_cast(uint4, (i16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+#pragma unroll
+        for (int k = 0; k < kWg8Step / 16; ++k) {
+            uint4 x[TM], d[TN];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) x[i] = transposed(lx + 16 * k * LM + 64 * i, LM);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) d[j] = transposed(ld + 16 * k * LN + 64 * j, LN);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = mfma32x32x16<DT>(x[i], d[j], acc[i][j]);
+        }
+        lds_wait();
+    }
+    wg8_store<TM, TN>(a, b, acc, (float*)lds);
+}
+
+// float32, and 16-bit types of other widths and alignments, in products of float32: a lane's operands are a channel of a row
+// each, as memory has them.
+template <int DT, int TM, int TN>
+__global__ __launch_bounds__(64 * kWg8Waves, TM * TN > 6 ? 1 : 2) void k_wgrad8_any(Wgrad8Args a, int parts) {
+    __shared__ float lds[32 * TM * 32 * TN];
+    const Wg8Block b = wg8_block<TM, TN>(a, parts);
+    const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5, nb = code_blocks(a.Cin);
+    f32x16 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    constexpr int U = 4;
+    for (int64_t r0 = b.r0; r0 < b.r1; r0 += 2 * U) {
+        int q[U][TM], e[U][TM];
+        float d[U][TN];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t r = r0 + 2 * u + h;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int k = b.ci + 32 * i + c;
+                const bool on = r < b.r1 && k < a.Cin;
+                q[u][i] = on ? a.in.codes[r * a.Cin + k] : 0;
+                e[u][i] = on ? a.in.exps[r * nb + k / kCodeBlock] : 1;
+            }
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int k = b.co + 32 * j + c;
+                d[u][j] = r < b.r1 && k < a.Cout ? ld_feat<DT>(a.da, r * a.Cout + k) : 0.f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const float x = code_value(q[u][i], code_step(e[u][i]));
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, d[u][j], acc[i][j], 0, 0, 0);
+            }
+    }
+    wg8_store<TM, TN>(a, b, acc, lds);
+}
+
+// adds the shares in 64 bits: 16 of n numbers a workgroup, in 32 runs of consecutive shares
+__global__ __launch_bounds__(512) void k_wgrad8_join(const float* __restrict__ part, int parts, int64_t n, float* __restrict__ dW) {
+    __shared__ double red[32][17];
+    const int col = threadIdx.x & 15, run = threadIdx.x >> 4, len = (parts + 31) / 32;
+    const int64_t t = (int64_t)blockIdx.x * 16 + col;
+    const int p0 = run * len, p1 = p0 + len < parts ? p0 + len : parts;
     double s = 0.0;
-    for (int p = 0; p < parts; ++p) s += (double)part[p * n + t];
+    if (t < n)
+        for (int p = p0; p < p1; p += 8) {
+            float f[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = p + k < p1 ? part[(int64_t)(p + k) * n + t] : 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += (double)f[k];
+        }
+    red[run][col] = s;
+    __syncthreads();
+    if (run || t >= n) return;
+    for (int k = 1; k < 32; ++k) s += red[k][col];
     dW[t] = (float)s;
 }
 
+template <int DT, int TM, int TN>
+static void wgrad8(hipStream_t s, const Wgrad8Args& a, int parts) {
+    const unsigned g = (unsigned)(parts * wgrad8_blocks(a.Cin) * wgrad8_blocks(a.Cout));
+    if constexpr (DT != SPV_F32) {
+        if (a.Cin % 16 == 0 && a.Cout % 8 == 0 && (((uintptr_t)a.in.codes | (uintptr_t)a.da) & 15u) == 0) {
+            k_wgrad8<DT, TM, TN><<<g, 64 * kWg8Waves, 0, s>>>(a, parts);
+            return;
+        }
+    }
+    k_wgrad8_any<DT, TM, TN><<<g, 64 * kWg8Waves, 0, s>>>(a, parts);
+}
+template <int DT, int TM>
+static void wgrad8_n(hipStream_t s, const Wgrad8Args& a, int parts) {
+    const int n = wgrad8_side(a.Cout);
+    if (n == 1) wgrad8<DT, TM, 1>(s, a, parts);
+    else if (n == 2) wgrad8<DT, TM, 2>(s, a, parts);
+    else wgrad8<DT, TM, 3>(s, a, parts);
+}
+template <int DT>
+static void wgrad8_m(hipStream_t s, const Wgrad8Args& a, int parts) {
+    const int n = wgrad8_side(a.Cin);
+    if (n == 1) wgrad8_n<DT, 1>(s, a, parts);
+    else if (n == 2) wgrad8_n<DT, 2>(s, a, parts);
+    else wgrad8_n<DT, 3>(s, a, parts);
+}
 void launch_wgrad8(hipStream_t s, const Wgrad8Args& a) {
     const int parts = wgrad8_parts(a.m_cap, a.Cin, a.Cout);
-    const dim3 g((unsigned)parts, (unsigned)((a.Cin + 31) / 32), (unsigned)((a.Cout + 31) / 32));
-    if (a.dt == SPV_F32) k_wgrad8<SPV_F32><<<g, 256, 0, s>>>(a);
-    else if (a.dt == SPV_BF16) k_wgrad8<SPV_BF16><<<g, 256, 0, s>>>(a);
-    else k_wgrad8<SPV_F16><<<g, 256, 0, s>>>(a);
+    if (a.dt == SPV_F32) wgrad8_m<SPV_F32>(s, a, parts);
+    else if (a.dt == SPV_BF16) wgrad8_m<SPV_BF16>(s, a, parts);
+    else wgrad8_m<SPV_F16>(s, a, parts);
     const int64_t n = (int64_t)a.Cin * a.Cout;
-    k_wgrad8_join<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a.part, parts, n, a.dW);
+    k_wgrad8_join<<<(unsigned)((n + 15) / 16), 512, 0, s>>>(a.part, parts, n, a.dW);
 }
 
 }  // namespace spv

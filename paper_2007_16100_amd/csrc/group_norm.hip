@@ -55,33 +55,12 @@ struct Chans {
         else return *(const uint4*)((const char*)p + e * (16 / VEC));
     }
     static __device__ void unpack(const Raw& r, float (&x)[VEC]) {
-        if constexpr (VEC == 1) {
-            x[0] = r;
-        } else {
-            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (DT == SPV_F32) {
-                    x[j] = __uint_as_float(w[j]);
-                } else {
-                    x[2 * j] = from16<DT>(w[j] & 0xFFFF);
-                    x[2 * j + 1] = from16<DT>(w[j] >> 16);
-                }
-            }
-        }
+        if constexpr (VEC == 1) x[0] = r;
+        else unpack16<DT>(r, x);
     }
     static __device__ void store(void* p, int64_t e, const float (&x)[VEC]) {
-        if constexpr (VEC == 1) {
-            st_feat<DT>(p, e, x[0]);
-        } else {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (DT == SPV_F32) w[j] = __float_as_uint(x[j]);
-                else w[j] = pack2<DT>(x[2 * j], x[2 * j + 1]);
-            }
-            *(uint4*)((char*)p + e * (16 / VEC)) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        if constexpr (VEC == 1) st_feat<DT>(p, e, x[0]);
+        else *(uint4*)((char*)p + e * (16 / VEC)) = pack16<DT>(x);
     }
 };
 

@@ -1,8 +1,8 @@
 // lanes.hpp -- exchanges between the lanes of a wave in vector registers (a lane's partner through DPP and the swaps of
-// rows of 16 and of 32 lanes), without the trip through LDS that a shuffle takes.
+// rows of 16 and of 32 lanes), without the trip through LDS that a shuffle takes; and the 16 bytes a lane moves.
 #pragma once
 
-#include <hip/hip_runtime.h>
+#include "spv_common.hpp"
 
 namespace spv {
 
@@ -52,6 +52,33 @@ __device__ inline double wave_sum(double v) {
     const auto l = __builtin_amdgcn_permlane32_swap(__double2loint(v), __double2loint(v), false, false);
     const auto h = __builtin_amdgcn_permlane32_swap(__double2hiint(v), __double2hiint(v), false, false);
     return pair((int)l[0], (int)h[0]) + pair((int)l[1], (int)h[1]);
+}
+
+// 16 bytes of channels in float32, and back with one rounding
+template <int DT, int V>
+__device__ inline void unpack16(const uint4& r, float (&x)[V]) {
+    static_assert(V == (DT == SPV_F32 ? 4 : 8), "16 bytes");
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (DT == SPV_F32) {
+            x[j] = __uint_as_float(w[j]);
+        } else {
+            x[2 * j] = from16<DT>(w[j] & 0xFFFF);
+            x[2 * j + 1] = from16<DT>(w[j] >> 16);
+        }
+    }
+}
+template <int DT, int V>
+__device__ inline uint4 pack16(const float (&x)[V]) {
+    static_assert(V == (DT == SPV_F32 ? 4 : 8), "16 bytes");
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (DT == SPV_F32) w[j] = __float_as_uint(x[j]);
+        else w[j] = pack2<DT>(x[2 * j], x[2 * j + 1]);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 }  // namespace spv

@@ -2,6 +2,7 @@
 //   theta = c_a freqs[p],  (u, w) -> (u cos theta - w sin theta, u sin theta + w cos theta),
 // c_a the row's coordinate on the axis whose section holds p.  The inverse turns by -theta.
 #include "conv_common.hpp"
+#include "lanes.hpp"
 
 namespace spv {
 
@@ -18,31 +19,6 @@ __device__ inline float2 cos_sin(int c, float f) {
     const int n = (int)q & 3;
     const float a = n & 1 ? s : k, b = n & 1 ? k : s;
     return make_float2(n == 1 || n == 2 ? -a : a, n & 2 ? -b : b);
-}
-
-// 16 bytes of channels
-template <int DT, int V>
-__device__ inline void unpack_v(const uint4& r, float (&x)[V]) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if constexpr (DT == SPV_F32) {
-            x[j] = __uint_as_float(w[j]);
-        } else {
-            x[2 * j] = from16<DT>(w[j] & 0xFFFF);
-            x[2 * j + 1] = from16<DT>(w[j] >> 16);
-        }
-    }
-}
-template <int DT, int V>
-__device__ inline uint4 pack_v(const float (&x)[V]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if constexpr (DT == SPV_F32) w[j] = __float_as_uint(x[j]);
-        else w[j] = pack2<DT>(x[2 * j], x[2 * j + 1]);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 __device__ inline int voxel_axis(const int32_t* c) {
@@ -112,8 +88,8 @@ __global__ __launch_bounds__(256) void k_rope_rows(RopeArgs a, RopeUnits un) {
             if constexpr (HALVES) {
                 if (t.two) {
                     float x[V], y[V];
-                    unpack_v<DT>(t.v[0], x);
-                    unpack_v<DT>(t.v[1], y);
+                    unpack16<DT>(t.v[0], x);
+                    unpack16<DT>(t.v[1], y);
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
                         const float2 q = cs[t.c + e];
@@ -121,12 +97,12 @@ __global__ __launch_bounds__(256) void k_rope_rows(RopeArgs a, RopeUnits un) {
                         x[e] = u * q.x - w * q.y;
                         y[e] = u * q.y + w * q.x;
                     }
-                    *(uint4*)(t.out + (int64_t)a.P * (16 / V)) = pack_v<DT>(y);
-                    t.v[0] = pack_v<DT>(x);
+                    *(uint4*)(t.out + (int64_t)a.P * (16 / V)) = pack16<DT>(y);
+                    t.v[0] = pack16<DT>(x);
                 }
             } else if (t.c < 2 * a.P) {
                 float x[V];
-                unpack_v<DT>(t.v[0], x);
+                unpack16<DT>(t.v[0], x);
 #pragma unroll
                 for (int e = 0; e < V; e += 2) {
                     const int p = (t.c + e) / 2;
@@ -136,7 +112,7 @@ __global__ __launch_bounds__(256) void k_rope_rows(RopeArgs a, RopeUnits un) {
                     x[e] = u * q.x - w * q.y;
                     x[e + 1] = u * q.y + w * q.x;
                 }
-                t.v[0] = pack_v<DT>(x);
+                t.v[0] = pack16<DT>(x);
             }
             *(uint4*)t.out = t.v[0];
         }

@@ -542,7 +542,7 @@ struct RowRange {
     __device__ int64_t end() const;
 };
 void launch_checkpoint8(hipStream_t s, const void* x, Saved8 to, const RowRange& rows, int C, int dt);
-void launch_checkpoint8_read(hipStream_t s, Saved8 from, void* out, const int64_t* m_dev, int64_t m_cap, int C, int dt);
+void launch_checkpoint8_read(hipStream_t s, Saved8 from, void* out, const RowRange& rows, int C, int dt);
 struct Wgrad8Args {
     Saved8 in;
     const int64_t* m_dev;

@@ -103,7 +103,9 @@ def test_options(spv, C):
     da = features(300, 64, "bf16", 8)
     ws = spv.Workspace.for_linear_backward8(300, C, 64)
     want = spv.spv_linear_backward8(ws, full, da)
-    assert torch.equal(spv.spv_linear_backward8(ws, off, da), want)
+    X, D = arr(whole), arr(da)
+    for got in (want, spv.spv_linear_backward8(ws, off, da)):  # other alignments may add up in another order
+        assert np.all(np.abs(arr(got) - X.T @ D) <= ref.wgrad_bound(X, D, X.T @ D))
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
