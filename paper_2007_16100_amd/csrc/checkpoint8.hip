@@ -129,10 +129,11 @@ void launch_checkpoint8_read(hipStream_t s, Saved8 from, void* out, const RowRan
 // dW = in^T da.  A workgroup takes TM x TN tiles of 32 x 32 of dW and a share of the rows, its waves some of those each,
 // with nothing between them but the sum at the end.  The shares' sums go to the workspace and are joined in 64 bits.
 // ---------------------------------------------------------------------------
-constexpr int kWg8Waves = 4;
-constexpr int kWg8Step = 32;   // rows of a wave's step
-constexpr int kWg8Most = 3;    // tiles of a side of a workgroup's block
+constexpr int kWg8Step = 32;     // rows of a wave's step
+constexpr int kWg8Most = 3;      // tiles of a side of a workgroup's block
 constexpr int kWg8Groups = 256;  // workgroups, as far as the rows go
+// waves of a workgroup: as many as the registers allow, for what they have on the way from memory
+constexpr int wg8_waves(int tiles) { return tiles <= 4 ? 8 : 4; }
 
 // tiles of a side: the fewest padded, then the most
 static int wgrad8_side(int C) {
@@ -145,74 +146,91 @@ static int wgrad8_side(int C) {
 static int wgrad8_blocks(int C) { return ((C + 31) / 32 + wgrad8_side(C) - 1) / wgrad8_side(C); }
 static int wgrad8_parts(int64_t m_cap, int Cin, int Cout) {
     const int64_t blocks = (int64_t)wgrad8_blocks(Cin) * wgrad8_blocks(Cout);
-    const int64_t rows = (m_cap + kWg8Waves * kWg8Step - 1) / (kWg8Waves * kWg8Step);
     int64_t s = kWg8Groups / blocks;
     if (s >= 8) s = s / 8 * 8;  // shares of the same rows on one die
-    if (s > rows) s = rows;
+    const int64_t steps = (m_cap + kWg8Step - 1) / kWg8Step;
+    if (s > steps) s = steps;
     return (int)(s < 1 ? 1 : s);
 }
+// numbers of a share: whole tiles
+static int64_t wgrad8_numbers(int Cin, int Cout) {
+    return (int64_t)wgrad8_blocks(Cin) * wgrad8_side(Cin) * wgrad8_blocks(Cout) * wgrad8_side(Cout) * 1024;
+}
 float* plan_wgrad8_ws(Arena& a, int64_t m_cap, int Cin, int Cout) {
-    return a.take<float>((size_t)wgrad8_parts(m_cap, Cin, Cout) * Cin * Cout);
+    return a.take<float>((size_t)wgrad8_parts(m_cap, Cin, Cout) * wgrad8_numbers(Cin, Cout));
 }
 
 struct Wg8Block {
-    int part, ci, co;   // share of the rows, first channels
+    int part, block;    // share of the rows, block of dW
+    int ci, co;         // its first channels
     int64_t r0, r1;     // the wave's rows
 };
 // the shares come first in the grid, so that the blocks of one share, which read the same rows, run on one die
-template <int TM, int TN>
+template <int TM, int TN, int STEP>
 __device__ inline Wg8Block wg8_block(const Wgrad8Args& a, int parts) {
+    constexpr int NW = wg8_waves(TM * TN);
     Wg8Block b;
     b.part = (int)(blockIdx.x % (unsigned)parts);
-    const int nm = (a.Cin + 32 * TM - 1) / (32 * TM), block = (int)(blockIdx.x / (unsigned)parts);
-    b.ci = block % nm * (32 * TM);
-    b.co = block / nm * (32 * TN);
-    const int64_t m = clamp_rows(a.m_dev, a.m_cap), steps = (m + kWg8Step - 1) / kWg8Step;
-    const int64_t waves = (int64_t)parts * kWg8Waves, w = (int64_t)b.part * kWg8Waves + uniform((int)(threadIdx.x >> 6));
-    b.r0 = steps * w / waves * kWg8Step;
-    b.r1 = steps * (w + 1) / waves * kWg8Step;
+    b.block = (int)(blockIdx.x / (unsigned)parts);
+    const int nm = (a.Cin + 32 * TM - 1) / (32 * TM);
+    b.ci = b.block % nm * (32 * TM);
+    b.co = b.block / nm * (32 * TN);
+    const int64_t m = clamp_rows(a.m_dev, a.m_cap), steps = (m + STEP - 1) / STEP;
+    const int64_t waves = (int64_t)parts * NW, w = (int64_t)b.part * NW + uniform((int)(threadIdx.x >> 6));
+    b.r0 = steps * w / waves * STEP;
+    b.r1 = steps * (w + 1) / waves * STEP;
     if (b.r1 > m) b.r1 = m;
     return b;
 }
 
-// the waves' sums of a block, one after the other in LDS, and then to the share's part of the workspace
+// A tile of 32 x 32 as it lies in LDS and in the workspace: column c's 32 rows one after the other, four rows (q of eight) at
+// place q ^ (c / 2) % 8, so that the lanes of a wave, a column each, meet in no bank.
+__device__ inline int wg8_place(int c, int q) { return c * 32 + 4 * (q ^ ((c >> 1) & 7)); }
+
+// The waves' sums of a block, added up in LDS, and then to the share's part of the workspace.  There is a round for each
+// wave, in which it adds every NW-th tile, another wave's next: the order of a tile's sum is the same on every call.
 template <int TM, int TN>
 __device__ inline void wg8_store(const Wgrad8Args& a, const Wg8Block& b, const f32x16 (&acc)[TM][TN], float* lds) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, h = lane >> 5;
-    for (int w = 0; w < kWg8Waves; ++w) {
+    constexpr int NW = wg8_waves(TM * TN);
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), c = lane & 31, h = lane >> 5;
+    for (int w = 0; w < NW; ++w) {
         __syncthreads();
-        if (wave == w)
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
+            for (int j = 0; j < TN; ++j) {
+                if (((i * TN + j - wave - w) & (NW - 1)) != 0) continue;
+                float* p = lds + (i * TN + j) * 1024;
+                float4 v[4];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float* p = lds + (32 * i + 8 * (e / 4) + 4 * h + e % 4) * (32 * TN) + 32 * j + c;
-                        *p = w ? *p + acc[i][j][e] : acc[i][j][e];
-                    }
+                for (int q = 0; q < 4; ++q)
+                    v[q] = w ? *(const float4*)(p + wg8_place(c, 2 * q + h)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *(float4*)(p + wg8_place(c, 2 * q + h)) =
+                        make_float4(v[q].x + acc[i][j][4 * q], v[q].y + acc[i][j][4 * q + 1],
+                                    v[q].z + acc[i][j][4 * q + 2], v[q].w + acc[i][j][4 * q + 3]);
+            }
     }
     __syncthreads();
-    float* out = a.part + (int64_t)b.part * a.Cin * a.Cout;
-    for (int t = threadIdx.x; t < 32 * TM * 32 * TN; t += 64 * kWg8Waves) {
-        const int i = b.ci + t / (32 * TN), j = b.co + t % (32 * TN);
-        if (i < a.Cin && j < a.Cout) out[(int64_t)i * a.Cout + j] = lds[t];
-    }
+    const int64_t n = (int64_t)((a.Cin + 32 * TM - 1) / (32 * TM)) * ((a.Cout + 32 * TN - 1) / (32 * TN)) * (TM * TN * 1024);
+    float4* out = (float4*)(a.part + b.part * n + (int64_t)b.block * (TM * TN * 1024));
+    for (int t = threadIdx.x; t < TM * TN * 256; t += 64 * NW) out[t] = ((const float4*)lds)[t];
 }
 
 // 16-bit types, 16 channels a time: a wave brings 32 rows of codes, as values of the type, and of da into its own part of LDS
 // (the next 32 are on the way) and reads both back transposed: the matrix cores sum over rows.
 template <int DT, int TM, int TN>
-__global__ __launch_bounds__(64 * kWg8Waves, TM * TN > 6 ? 1 : 2) void k_wgrad8(Wgrad8Args a, int parts) {
+__global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void k_wgrad8(Wgrad8Args a, int parts) {
     constexpr int BM = 32 * TM, BN = 32 * TN, LM = 2 * BM + 16, LN = 2 * BN + 16;  // bytes from row to row in LDS
     constexpr int QM = BM / 16, QN = BN / 8;                     // 16-byte chunks of a row
     constexpr int KM = kWg8Step * QM / 64, KN = kWg8Step * QN / 64;  // of a lane
     constexpr int SIZE = kWg8Step * (LM + LN);
-    constexpr int LDS = kWg8Waves * SIZE > BM * BN * 4 ? kWg8Waves * SIZE : BM * BN * 4;
+    constexpr int NW = wg8_waves(TM * TN), LDS = NW * SIZE > BM * BN * 4 ? NW * SIZE : BM * BN * 4;
     typedef short i16x8 __attribute__((ext_vector_type(8)));
     typedef __attribute__((address_space(3))) i16x4 lds4;
     __shared__ __align__(16) char lds[LDS];
-    const Wg8Block b = wg8_block<TM, TN>(a, parts);
+    const Wg8Block b = wg8_block<TM, TN, kWg8Step>(a, parts);
     const int lane = threadIdx.x & 63, nb = code_blocks(a.Cin);
     char *lx = lds + (threadIdx.x >> 6) * SIZE, *ld = lx + kWg8Step * LM;
     f32x16 acc[TM][TN];
@@ -291,11 +309,12 @@ __global__ __launch_bounds__(64 * kWg8Waves, TM * TN > 6 ? 1 : 2) void k_wgrad8(
 }
 
 // float32, and 16-bit types of other widths and alignments, in products of float32: a lane's operands are a channel of a row
-// each, as memory has them.
+// each, as memory has them.  Rows and channels past the ends are read as the last ones, and count as 0.
 template <int DT, int TM, int TN>
-__global__ __launch_bounds__(64 * kWg8Waves, TM * TN > 6 ? 1 : 2) void k_wgrad8_any(Wgrad8Args a, int parts) {
-    __shared__ float lds[32 * TM * 32 * TN];
-    const Wg8Block b = wg8_block<TM, TN>(a, parts);
+__global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void k_wgrad8_any(Wgrad8Args a, int parts) {
+    constexpr int U = 4, STEP = 2 * U;
+    __shared__ __align__(16) float lds[TM * TN * 1024];
+    const Wg8Block b = wg8_block<TM, TN, STEP>(a, parts);
     const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5, nb = code_blocks(a.Cin);
     f32x16 acc[TM][TN];
 #pragma unroll
@@ -304,59 +323,83 @@ __global__ __launch_bounds__(64 * kWg8Waves, TM * TN > 6 ? 1 : 2) void k_wgrad8_
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    constexpr int U = 4;
-    for (int64_t r0 = b.r0; r0 < b.r1; r0 += 2 * U) {
-        int q[U][TM], e[U][TM];
-        float d[U][TN];
+    int q[U][TM], x[U][TM];
+    float d[U][TN];
+    auto ask = [&](int64_t r0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t r = r0 + 2 * u + h;
+            const int64_t at = r0 + 2 * u + h, r = at < b.r1 ? at : b.r1 - 1;
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                const int k = b.ci + 32 * i + c;
-                const bool on = r < b.r1 && k < a.Cin;
-                q[u][i] = on ? a.in.codes[r * a.Cin + k] : 0;
-                e[u][i] = on ? a.in.exps[r * nb + k / kCodeBlock] : 1;
+                const int k = b.ci + 32 * i + c < a.Cin ? b.ci + 32 * i + c : a.Cin - 1;
+                q[u][i] = a.in.codes[r * a.Cin + k];
+                x[u][i] = a.in.exps[r * nb + k / kCodeBlock];
             }
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
-                const int k = b.co + 32 * j + c;
-                d[u][j] = r < b.r1 && k < a.Cout ? ld_feat<DT>(a.da, r * a.Cout + k) : 0.f;
+                const int k = b.co + 32 * j + c < a.Cout ? b.co + 32 * j + c : a.Cout - 1;
+                d[u][j] = ld_feat<DT>(a.da, r * a.Cout + k);
             }
         }
+    };
+    if (b.r0 < b.r1) ask(b.r0);
+    for (int64_t r0 = b.r0; r0 < b.r1; r0 += STEP) {
+        float f[U][TM], g[U][TN];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool on = r0 + 2 * u + h < b.r1;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) f[u][i] = on ? code_value(q[u][i], code_step(x[u][i])) : 0.f;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) g[u][j] = on ? d[u][j] : 0.f;
+        }
+        if (r0 + STEP < b.r1) ask(r0 + STEP);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const float x = code_value(q[u][i], code_step(e[u][i]));
+            for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, d[u][j], acc[i][j], 0, 0, 0);
-            }
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[u][i], g[u][j], acc[i][j], 0, 0, 0);
     }
     wg8_store<TM, TN>(a, b, acc, lds);
 }
 
-// adds the shares in 64 bits: 16 of n numbers a workgroup, in 32 runs of consecutive shares
-__global__ __launch_bounds__(512) void k_wgrad8_join(const float* __restrict__ part, int parts, int64_t n, float* __restrict__ dW) {
-    __shared__ double red[32][17];
+// adds the shares of the n numbers in 64 bits, 64 of them a workgroup, in 32 runs of consecutive shares; each is then put
+// where it belongs in dW (blocks of TM x TN tiles, those of a column of blocks one after the other)
+__global__ __launch_bounds__(512) void k_wgrad8_join(const float* __restrict__ part, int parts, int64_t n, int TM, int TN, int Cin,
+                                                     int Cout, float* __restrict__ dW) {
+    __shared__ double red[32][65];
     const int col = threadIdx.x & 15, run = threadIdx.x >> 4, len = (parts + 31) / 32;
-    const int64_t t = (int64_t)blockIdx.x * 16 + col;
     const int p0 = run * len, p1 = p0 + len < parts ? p0 + len : parts;
-    double s = 0.0;
-    if (t < n)
-        for (int p = p0; p < p1; p += 8) {
-            float f[8];
+    const float4* from = (const float4*)(part + (int64_t)blockIdx.x * 64) + col;
+    double s[4] = {};
+    for (int p = p0; p < p1; p += 8) {
+        float4 f[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = p + k < p1 ? part[(int64_t)(p + k) * n + t] : 0.f;
+        for (int k = 0; k < 8; ++k)
+            f[k] = p + k < p1 ? from[(int64_t)(p + k) * (n / 4)] : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s += (double)f[k];
+        for (int k = 0; k < 8; ++k) {
+            s[0] += (double)f[k].x;
+            s[1] += (double)f[k].y;
+            s[2] += (double)f[k].z;
+            s[3] += (double)f[k].w;
         }
-    red[run][col] = s;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) red[run][4 * col + e] = s[e];
     __syncthreads();
-    if (run || t >= n) return;
-    for (int k = 1; k < 32; ++k) s += red[k][col];
-    dW[t] = (float)s;
+    for (int k = 16; k > 0; k /= 2) {  // 16 rows of 64 by 512 threads
+        for (int t = threadIdx.x; t < k * 64; t += 512) red[t / 64][t % 64] += red[t / 64 + k][t % 64];
+        __syncthreads();
+    }
+    if (threadIdx.x >= 64) return;
+    const int64_t t = (int64_t)blockIdx.x * 64 + threadIdx.x;
+    const int tile = (int)(t / 1024), c = (int)(t % 1024) / 32, q = (int)(t % 32) / 4 ^ ((c >> 1) & 7);
+    const int block = tile / (TM * TN), in = tile % (TM * TN), nm = (Cin + 32 * TM - 1) / (32 * TM);
+    const int i = (block % nm * TM + in / TN) * 32 + 4 * q + (int)(t % 4), j = (block / nm * TN + in % TN) * 32 + c;
+    if (i < Cin && j < Cout) dW[(int64_t)i * Cout + j] = (float)red[0][threadIdx.x];
 }
 
 template <int DT, int TM, int TN>
@@ -364,11 +407,11 @@ static void wgrad8(hipStream_t s, const Wgrad8Args& a, int parts) {
     const unsigned g = (unsigned)(parts * wgrad8_blocks(a.Cin) * wgrad8_blocks(a.Cout));
     if constexpr (DT != SPV_F32) {
         if (a.Cin % 16 == 0 && a.Cout % 8 == 0 && (((uintptr_t)a.in.codes | (uintptr_t)a.da) & 15u) == 0) {
-            k_wgrad8<DT, TM, TN><<<g, 64 * kWg8Waves, 0, s>>>(a, parts);
+            k_wgrad8<DT, TM, TN><<<g, 64 * wg8_waves(TM * TN), 0, s>>>(a, parts);
             return;
         }
     }
-    k_wgrad8_any<DT, TM, TN><<<g, 64 * kWg8Waves, 0, s>>>(a, parts);
+    k_wgrad8_any<DT, TM, TN><<<g, 64 * wg8_waves(TM * TN), 0, s>>>(a, parts);
 }
 template <int DT, int TM>
 static void wgrad8_n(hipStream_t s, const Wgrad8Args& a, int parts) {
@@ -389,8 +432,9 @@ void launch_wgrad8(hipStream_t s, const Wgrad8Args& a) {
     if (a.dt == SPV_F32) wgrad8_m<SPV_F32>(s, a, parts);
     else if (a.dt == SPV_BF16) wgrad8_m<SPV_BF16>(s, a, parts);
     else wgrad8_m<SPV_F16>(s, a, parts);
-    const int64_t n = (int64_t)a.Cin * a.Cout;
-    k_wgrad8_join<<<(unsigned)((n + 15) / 16), 512, 0, s>>>(a.part, parts, n, a.dW);
+    const int64_t n = wgrad8_numbers(a.Cin, a.Cout);
+    k_wgrad8_join<<<(unsigned)(n / 64), 512, 0, s>>>(a.part, parts, n, wgrad8_side(a.Cin), wgrad8_side(a.Cout), a.Cin, a.Cout,
+                                                     a.dW);
 }
 
 }  // namespace spv
