@@ -80,9 +80,7 @@ __global__ __launch_bounds__(256) void k_code8_read(Saved8 from, void* out, RowR
         const int64_t t = t0 + k * 256;
         if (t >= end) break;
         float f[V];
-        const float step = code_step(e[k]);
-#pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = code_value((int8_t)(w[k][j / 4] >> (8 * (j % 4))), step);
+        code_values(w[k], code_step(e[k]), f);
         ((uint4*)out)[t] = pack16<DT>(f);
     }
 }
@@ -240,24 +238,53 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    // what a lane brings of a step, from its first row: channels past the ends are read as the last ones and not stored
     uint4 ux[KM], ud[KN];
     int ue[KM];
+    uint32_t atx[KM], ate[KM], atd[KN];
+#pragma unroll
+    for (int k = 0; k < KM; ++k) {
+        const int t = lane + 64 * k, c = b.ci + t % QM * 16 < a.Cin ? b.ci + t % QM * 16 : a.Cin - 16;
+        atx[k] = (uint32_t)(t / QM * a.Cin + c);
+        ate[k] = (uint32_t)(t / QM * nb + c / kCodeBlock);
+    }
+#pragma unroll
+    for (int k = 0; k < KN; ++k) {
+        const int t = lane + 64 * k, c = b.co + t % QN * 8 < a.Cout ? b.co + t % QN * 8 : a.Cout - 8;
+        atd[k] = (uint32_t)(t / QN * a.Cout + c) * 2u;
+    }
     auto ask = [&](int64_t r0) {
+        const int8_t* px = a.in.codes + r0 * a.Cin;
+        const uint8_t* pe = a.in.exps + r0 * nb;
+        const char* pd = (const char*)a.da + r0 * a.Cout * 2;
+        if (r0 + kWg8Step <= b.r1) {
 #pragma unroll
-        for (int k = 0; k < KM; ++k) {
-            const int t = lane + 64 * k, c = b.ci + t % QM * 16;
-            const int64_t r = r0 + t / QM;
-            const bool on = r < b.r1 && c < a.Cin;
-            ux[k] = on ? *(const uint4*)(a.in.codes + r * a.Cin + c) : make_uint4(0, 0, 0, 0);
-            ue[k] = on ? a.in.exps[r * nb + c / kCodeBlock] : 1;
-        }
+            for (int k = 0; k < KM; ++k) {
+                ux[k] = *(const uint4*)(px + atx[k]);
+                ue[k] = pe[ate[k]];
+            }
 #pragma unroll
-        for (int k = 0; k < KN; ++k) {
-            const int t = lane + 64 * k, c = b.co + t % QN * 8;
-            const int64_t r = r0 + t / QN;
-            ud[k] = r < b.r1 && c < a.Cout ? *(const uint4*)((const uint16_t*)a.da + r * a.Cout + c)
-                                           : make_uint4(0, 0, 0, 0);
+            for (int k = 0; k < KN; ++k) ud[k] = *(const uint4*)(pd + atd[k]);
+        } else {  // rows past the end count as 0
+            const int rows = (int)(b.r1 - r0);
+#pragma unroll
+            for (int k = 0; k < KM; ++k) {
+                const bool on = (lane + 64 * k) / QM < rows;
+                ux[k] = on ? *(const uint4*)(px + atx[k]) : make_uint4(0, 0, 0, 0);
+                ue[k] = on ? pe[ate[k]] : 1;
+            }
+#pragma unroll
+            for (int k = 0; k < KN; ++k)
+                ud[k] = (lane + 64 * k) / QN < rows ? *(const uint4*)(pd + atd[k]) : make_uint4(0, 0, 0, 0);
         }
+    };
+    // lanes 16 g .. 16 g + 15 read four rows of 16 channels, and each gets its channel of the four
+    const int tl = lane & 15, tg = lane >> 4, row = 4 * (tg >> 1) + (tl >> 2), at = (16 * (tg & 1) + 4 * (tl & 3)) * 2;
+    auto transposed = [&](const char* p, int LD) {
+        const uint32_t q = lds_addr(p) + row * LD + at;
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)q);
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(q + 8 * LD));
+        return __builtin_bit_cast(uint4, (i16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
     if (b.r0 < b.r1) ask(b.r0);
     for (int64_t r0 = b.r0; r0 < b.r1; r0 += kWg8Step) {
@@ -265,13 +292,11 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
         for (int k = 0; k < KM; ++k) {
             const int t = lane + 64 * k;
             const uint32_t w[4] = {ux[k].x, ux[k].y, ux[k].z, ux[k].w};
-            const float step = code_step(ue[k]);
+            float f[16];
+            code_values(w, code_step(ue[k]), f);
             uint32_t v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t q = w[e / 2] >> (16 * (e % 2));
-                v[e] = pack2<DT>(code_value((int8_t)q, step), code_value((int8_t)(q >> 8), step));
-            }
+            for (int e = 0; e < 8; ++e) v[e] = pack2<DT>(f[2 * e], f[2 * e + 1]);
             uint4* p = (uint4*)(lx + t / QM * LM + t % QM * 32);
             p[0] = make_uint4(v[0], v[1], v[2], v[3]);
             p[1] = make_uint4(v[4], v[5], v[6], v[7]);
@@ -283,14 +308,6 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
         }
         if (r0 + kWg8Step < b.r1) ask(r0 + kWg8Step);
         lds_wait();
-        // lanes 16 g .. 16 g + 15 read four rows of 16 channels, and each gets its channel of the four
-        const int t = lane & 15, g = lane >> 4, row = 4 * (g >> 1) + (t >> 2), at = (16 * (g & 1) + 4 * (t & 3)) * 2;
-        auto transposed = [&](const char* p, int LD) {
-            const uint32_t q = lds_addr(p) + row * LD + at;
-            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)q);
-            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(q + 8 * LD));
-            return __builtin_bit_cast(uint4, (i16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        };
 #pragma unroll
         for (int k = 0; k < kWg8Step / 16; ++k) {
             uint4 x[TM], d[TN];

@@ -32,6 +32,27 @@ __device__ inline float code_value(int code, float step) {
     return code == -128 ? __uint_as_float(0x7FC00000u) : (float)code * step;
 }
 
+// What 4 N codes stand for: a byte counted from -128 takes a conversion and two exact steps.  A code of -128 (a zero byte
+// then) is looked for in all of them at once.
+template <int N>
+__device__ inline void code_values(const uint32_t (&w)[N], float step, float (&x)[4 * N]) {
+    uint32_t u[N], none = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        u[j] = w[j] ^ 0x80808080u;
+        none |= (u[j] - 0x01010101u) & ~u[j] & 0x80808080u;  // not 0 where there is a zero byte
+        x[4 * j] = ((float)(u[j] & 0xFFu) - 128.f) * step;
+        x[4 * j + 1] = ((float)((u[j] >> 8) & 0xFFu) - 128.f) * step;
+        x[4 * j + 2] = ((float)((u[j] >> 16) & 0xFFu) - 128.f) * step;
+        x[4 * j + 3] = ((float)(u[j] >> 24) - 128.f) * step;
+    }
+    if (none) {
+#pragma unroll
+        for (int e = 0; e < 4 * N; ++e)
+            if (((u[e / 4] >> (8 * (e % 4))) & 0xFFu) == 0u) x[e] = __uint_as_float(0x7FC00000u);
+    }
+}
+
 // The codes of a lane's VEC channels of a block that LANES lanes hold (a power of two of them, next to each other); returns the
 // block's exponent byte.  All lanes of a block call it.
 template <int DT, int VEC, int LANES>

@@ -87,9 +87,8 @@ struct Codes {
         return r;
     }
     static __device__ void unpack(const Raw& r, float (&x)[VEC]) {
-        const float step = code_step(r.e);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) x[j] = code_value((int8_t)(r.w[j / 4] >> (8 * (j % 4))), step);
+        if constexpr (VEC == 1) x[0] = code_value((int8_t)r.w[0], code_step(r.e));
+        else code_values(r.w, code_step(r.e), x);
     }
 };
 
