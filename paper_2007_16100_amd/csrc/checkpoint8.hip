@@ -185,20 +185,22 @@ __device__ inline Wg8Block wg8_block(const Wgrad8Args& a, int parts) {
 // place q ^ (c / 2) % 8, so that the lanes of a wave, a column each, meet in no bank.
 __device__ inline int wg8_place(int c, int q) { return c * 32 + 4 * (q ^ ((c >> 1) & 7)); }
 
-// The waves' sums of a block, added up in LDS, and then to the share's part of the workspace.  There is a round for each
-// wave, in which it adds every NW-th tile, another wave's next: the order of a tile's sum is the same on every call.
+// The waves' sums of a block, added up in LDS, and then to the share's part of the workspace.  Four waves share an image of
+// the block; in each of four rounds a wave adds every fourth tile, another wave's next: the order of a tile's sum is the same
+// on every call.
 template <int TM, int TN>
 __device__ inline void wg8_store(const Wgrad8Args& a, const Wg8Block& b, const f32x16 (&acc)[TM][TN], float* lds) {
     constexpr int NW = wg8_waves(TM * TN);
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), c = lane & 31, h = lane >> 5;
-    for (int w = 0; w < NW; ++w) {
+    float* image = lds + (wave >> 2) * (TM * TN * 1024);
+    for (int w = 0; w < 4; ++w) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
-                if (((i * TN + j - wave - w) & (NW - 1)) != 0) continue;
-                float* p = lds + (i * TN + j) * 1024;
+                if (((i * TN + j - wave - w) & 3) != 0) continue;
+                float* p = image + (i * TN + j) * 1024;
                 float4 v[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
@@ -213,7 +215,14 @@ __device__ inline void wg8_store(const Wgrad8Args& a, const Wg8Block& b, const f
     __syncthreads();
     const int64_t n = (int64_t)((a.Cin + 32 * TM - 1) / (32 * TM)) * ((a.Cout + 32 * TN - 1) / (32 * TN)) * (TM * TN * 1024);
     float4* out = (float4*)(a.part + b.part * n + (int64_t)b.block * (TM * TN * 1024));
-    for (int t = threadIdx.x; t < TM * TN * 256; t += 64 * NW) out[t] = ((const float4*)lds)[t];
+    for (int t = threadIdx.x; t < TM * TN * 256; t += 64 * NW) {
+        float4 v = ((const float4*)lds)[t];
+        if constexpr (NW == 8) {
+            const float4 u = ((const float4*)lds)[t + TM * TN * 256];
+            v = make_float4(v.x + u.x, v.y + u.y, v.z + u.z, v.w + u.w);
+        }
+        out[t] = v;
+    }
 }
 
 // 16-bit types, 16 channels a time: a wave brings 32 rows of codes, as values of the type, and of da into its own part of LDS
@@ -224,7 +233,7 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
     constexpr int QM = BM / 16, QN = BN / 8;                     // 16-byte chunks of a row
     constexpr int KM = kWg8Step * QM / 64, KN = kWg8Step * QN / 64;  // of a lane
     constexpr int SIZE = kWg8Step * (LM + LN);
-    constexpr int NW = wg8_waves(TM * TN), LDS = NW * SIZE > BM * BN * 4 ? NW * SIZE : BM * BN * 4;
+    constexpr int NW = wg8_waves(TM * TN), SUMS = NW / 4 * BM * BN * 4, LDS = NW * SIZE > SUMS ? NW * SIZE : SUMS;
     typedef short i16x8 __attribute__((ext_vector_type(8)));
     typedef __attribute__((address_space(3))) i16x4 lds4;
     __shared__ __align__(16) char lds[LDS];
@@ -330,7 +339,7 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
 template <int DT, int TM, int TN>
 __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void k_wgrad8_any(Wgrad8Args a, int parts) {
     constexpr int U = 4, STEP = 2 * U;
-    __shared__ __align__(16) float lds[TM * TN * 1024];
+    __shared__ __align__(16) float lds[wg8_waves(TM * TN) / 4 * TM * TN * 1024];
     const Wg8Block b = wg8_block<TM, TN, STEP>(a, parts);
     const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5, nb = code_blocks(a.Cin);
     f32x16 acc[TM][TN];

@@ -54,14 +54,32 @@ __device__ inline void code_values(const uint32_t (&w)[N], float step, float (&x
 }
 
 // The codes of a lane's VEC channels of a block that LANES lanes hold (a power of two of them, next to each other); returns the
-// block's exponent byte.  All lanes of a block call it.
+// block's exponent byte.  All lanes of a block call it.  Where all values are finite a code is the low byte of x 2^-E plus
+// 1.5 2^23, whose addition rounds to a whole number, ties to even.
 template <int DT, int VEC, int LANES>
 __device__ inline int code_block(const float (&x)[VEC], uint32_t (&w)[VEC / 4]) {
     uint32_t top = 0;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) top = max(top, finite_bits(x[e]));
+    for (int e = 0; e < VEC; ++e) top = max(top, __float_as_uint(x[e]) & 0x7FFFFFFFu);
     top = lanes_max<LANES>(top);
-    const int byte = code_exp<DT>(top);
+    if (top < 0x7F800000u) {
+        const int byte = code_exp<DT>(top);
+        const float rate = code_rate(byte);
+#pragma unroll
+        for (int j = 0; j < VEC / 4; ++j) {
+            uint32_t q[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                q[e] = __float_as_uint(__builtin_amdgcn_fmed3f(x[4 * j + e] * rate, -127.f, 127.f) + 12582912.f);
+            w[j] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[3], q[2], 0x0C0C0400u),
+                                         __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u), 0x05040100u);
+        }
+        return byte;
+    }
+    top = 0;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) top = max(top, finite_bits(x[e]));
+    const int byte = code_exp<DT>(lanes_max<LANES>(top));
     const float rate = code_rate(byte);
 #pragma unroll
     for (int j = 0; j < VEC / 4; ++j) {
