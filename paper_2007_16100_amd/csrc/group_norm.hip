@@ -136,41 +136,45 @@ __device__ inline GnTile gn_tile(const GnArgs& a, uint32_t tile_rows, uint32_t t
     return g;
 }
 
-// The tiles of a group of a scan, taken by a wave: four a lane are asked for by the constructor, before whatever
-// else the workgroup has to wait for, the others in turn.
+// The tiles of a group of a scan, taken by a wave, or where scans have few tiles by 8 lanes: four a lane are asked for by the
+// constructor, before whatever else the workgroup has to wait for, the others in turn.
 struct GnGroup {
     const float2* part;
     int64_t stride, tiles;
+    int lanes;
+    float first;  // the mean of the first tile
     float2 p[4];
+    // group g of a thread that has none (past G): as group 0
     __device__ GnGroup(const GnArgs& a, int g, int64_t tile0, uint32_t n, uint32_t tile_rows)
-        : part(a.tiles + tile0 * a.G + g), stride(a.G), tiles((n + tile_rows - 1) / tile_rows) {
+        : part(a.tiles + tile0 * a.G + (g < a.G ? g : 0)), stride(a.G), tiles((n + tile_rows - 1) / tile_rows),
+          lanes(a.few_tiles ? 8 : 64) {
+        first = tiles > 0 ? part[0].x : 0.f;
         ask(0);
     }
+    __device__ int64_t tile(int64_t t0, int k) const { return t0 + k * lanes + (threadIdx.x & (lanes - 1)); }
     __device__ void ask(int64_t t0) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int64_t t = t0 + k * 64 + (threadIdx.x & 63);
-            p[k] = t < tiles ? part[t * stride] : make_float2(0.f, 0.f);
-        }
+        for (int k = 0; k < 4; ++k) p[k] = tile(t0, k) < tiles ? part[tile(t0, k) * stride] : make_float2(0.f, 0.f);
     }
     // f(tile, its numbers) for the lane's tiles, zeros past the last
     template <class F>
     __device__ void each(F&& f) {
         for (int64_t t0 = 0;;) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) f(t0 + k * 64 + (threadIdx.x & 63), p[k]);
-            t0 += 256;
+            for (int k = 0; k < 4; ++k) f(tile(t0, k), p[k]);
+            t0 += 4 * lanes;
             if (t0 >= tiles) break;
             ask(t0);
         }
     }
+    __device__ double sum(double v) const { return lanes_sum(v, lanes == 64); }
 };
 // Mean and r of a group of a scan of n rows from its tiles' means and sums of squares.  Deviations are from
 // the first tile's mean, whose distance from the mean of all, squared, is at most (tiles) times the variance: what
 // cancels in 64 bits is a few thousand of their units.
 __device__ inline float2 gn_join_stat(GnGroup& t, uint32_t n, uint32_t tile_rows, int w, float eps) {
     if (n == 0) return make_float2(0.f, 0.f);
-    const double first = (double)__int_as_float(uniform(__float_as_int(t.p[0].x))), per = 1.0 / (double)n;
+    const double first = (double)t.first, per = 1.0 / (double)n;
     double s = 0.0, q = 0.0;
     t.each([&](int64_t i, const float2& p) {
         const int64_t left = (int64_t)n - i * tile_rows;
@@ -178,8 +182,8 @@ __device__ inline float2 gn_join_stat(GnGroup& t, uint32_t n, uint32_t tile_rows
         s = fma(rows, d, s);
         q += fma(rows * w * d, d, (double)p.y);
     });
-    s = wave_sum(s) * per;
-    q = wave_sum(q) * per / (double)w - s * s;
+    s = t.sum(s) * per;
+    q = t.sum(q) * per / (double)w - s * s;
     return make_float2((float)(first + s), 1.f / sqrtf((float)(q > 0.0 ? q : q == q ? 0.0 : q) + eps));
 }
 // the sums of a group of a scan from its tiles', over the count
@@ -190,7 +194,21 @@ __device__ inline float2 gn_join_sums(GnGroup& t, uint32_t n, int w) {
         s1 += (double)p.x;
         s2 += (double)p.y;
     });
-    return make_float2((float)(wave_sum(s1) * per), (float)(wave_sum(s2) * per));
+    return make_float2((float)(t.sum(s1) * per), (float)(t.sum(s2) * per));
+}
+// All groups of a tile's scan into LDS, the thread's first one asked for already: f(group's tiles) is what is stored.
+template <class F>
+__device__ inline void gn_join_all(const GnArgs& a, const GnTile& t, uint32_t tile_rows, GnGroup& first, float2* out, F&& f) {
+    if (a.joined) {
+        for (int g = threadIdx.x; g < a.G; g += kGnThreads) out[g] = a.joined[(int64_t)t.b * a.G + g];
+        return;
+    }
+    const int lanes = first.lanes, own = (int)threadIdx.x / lanes;
+    for (int g0 = 0; g0 < a.G; g0 += kGnThreads / lanes) {  // all lanes take part in the sums
+        if (g0) first = GnGroup(a, g0 + own, t.tile0, t.n, tile_rows);
+        const float2 v = f(first);
+        if ((threadIdx.x & (lanes - 1)) == 0 && g0 + own < a.G) out[g0 + own] = v;
+    }
 }
 
 // A thread's rows of a tile (row, row + R, ..), U at a time, the next U asked for before the present ones are used.
@@ -340,8 +358,7 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_apply(GnArgs a, int tile
     const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
     if (t.rows == 0 && !(t.first && a.stat)) return;
-    const int wave = threadIdx.x >> 6;
-    GnGroup first(a, wave < a.G ? wave : 0, t.tile0, a.joined ? 0u : t.n, tile_rows);
+    GnGroup first(a, (int)threadIdx.x / (a.few_tiles ? 8 : 64), t.tile0, a.joined ? 0u : t.n, tile_rows);
     float ga[VEC], be[VEC];
     gn_channels<VEC>(a.gamma, c, 1.f, ga);
     gn_channels<VEC>(a.beta, c, 0.f, be);
@@ -350,15 +367,7 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_apply(GnArgs a, int tile
     GnRows<4, typename V::Raw> rows{row, R, row < R ? t.rows : 0};
     if (rows.rows) rows.ask(row, rows.u, load);
     const int w = a.C / a.G;
-    if (a.joined) {
-        for (int g = threadIdx.x; g < a.G; g += kGnThreads) s_stat[g] = a.joined[(int64_t)t.b * a.G + g];
-    } else {
-        for (int g = wave; g < a.G; g += kGnWaves) {
-            if (g != wave) first = GnGroup(a, g, t.tile0, t.n, tile_rows);
-            const float2 v = gn_join_stat(first, t.n, tile_rows, w, a.eps);
-            if ((threadIdx.x & 63) == 0) s_stat[g] = v;
-        }
-    }
+    gn_join_all(a, t, tile_rows, first, s_stat, [&](GnGroup& g) { return gn_join_stat(g, t.n, tile_rows, w, a.eps); });
     __syncthreads();
     if (t.first && a.stat)
         for (int g = threadIdx.x; g < a.G; g += kGnThreads) ((float2*)a.stat)[(int64_t)t.b * a.G + g] = s_stat[g];
@@ -552,8 +561,7 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
     const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x - join);
     if (t.rows == 0) return;
-    const int wave = threadIdx.x >> 6;
-    GnGroup first(a, wave < a.G ? wave : 0, t.tile0, a.joined ? 0u : t.n, tile_rows);
+    GnGroup first(a, (int)threadIdx.x / (a.few_tiles ? 8 : 64), t.tile0, a.joined ? 0u : t.n, tile_rows);
     const int64_t base = t.row0 * a.C + c, block = t.row0 * code_blocks(a.C) + c / kCodeBlock;
     auto load = [&](int i) {
         typename S::RawRes r;
@@ -568,15 +576,7 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
     gn_channels<VEC>(a.beta, c, 0.f, be);
     gn_stat<VEC>(a, t.b, c, w, mu, r);
     if (row < R) rows.ask(row, rows.u, load);
-    if (a.joined) {
-        for (int g = threadIdx.x; g < a.G; g += kGnThreads) s_mean[g] = a.joined[(int64_t)t.b * a.G + g];
-    } else {
-        for (int g = wave; g < a.G; g += kGnWaves) {
-            if (g != wave) first = GnGroup(a, g, t.tile0, t.n, tile_rows);
-            const float2 v = gn_join_sums(first, t.n, w);
-            if ((threadIdx.x & 63) == 0) s_mean[g] = v;
-        }
-    }
+    gn_join_all(a, t, tile_rows, first, s_mean, [&](GnGroup& g) { return gn_join_sums(g, t.n, w); });
     __syncthreads();
     if (row >= R) return;
 #pragma unroll
@@ -602,6 +602,67 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
             V::store(a.dx, base + (int64_t)(i0 + k * R) * a.C, d);
         }
     });
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: a workgroup takes a group of a scan, all of it in its threads' registers: the mean, the deviations from it and
+// the output in one launch.
+// ---------------------------------------------------------------------------
+constexpr int kGnHeld = 24;  // values a thread holds
+// values in all up to which that is done: 701 x 96 in float32 takes 6.9 us with 8 groups (8.2 in tiles), in bf16 with 96 groups 4.5
+// (13.8); 8000 x 32 with 32 groups, whose rows are then read 4 bytes at a time, 14.4 (10.0)
+constexpr int64_t kGnFew = 1 << 17;
+
+__device__ inline float block_sum(float v, float* red) {
+    v = lanes_sum<64>(v);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s = red[0];
+#pragma unroll
+    for (int w = 1; w < kGnWaves; ++w) s += red[w];
+    return s;
+}
+
+template <int DT, int ACT>
+__global__ __launch_bounds__(kGnThreads) void k_gn_few(GnArgs a, uint32_t by_w) {
+    __shared__ float red[2][kGnWaves];
+    const int b = (int)(blockIdx.x / (unsigned)a.G), g = (int)(blockIdx.x % (unsigned)a.G), w = a.C / a.G;
+    const int64_t r0 = clamp_off(a.off[b], a.m), r1 = clamp_off(a.off[b + 1], a.m);
+    const int n = r1 > r0 ? (int)(r1 - r0) * w : 0;
+    if (n == 0) {
+        if (threadIdx.x == 0 && a.stat) ((float2*)a.stat)[blockIdx.x] = make_float2(0.f, 0.f);
+        return;
+    }
+    const int64_t base = r0 * a.C + g * w;
+    const float first = ld_feat<DT>(a.x, base);  // equal values give their mean exactly
+    float x[kGnHeld];
+    int at[kGnHeld], c[kGnHeld];  // from the group's first value: rows * C is at most kGnHeld kGnThreads G
+    float s = 0.f, q = 0.f;
+#pragma unroll
+    for (int k = 0; k < kGnHeld; ++k) {
+        if (k * kGnThreads >= n) break;
+        const int t = (int)threadIdx.x + k * kGnThreads, i = t < n ? t : 0, r = by_w ? (int)__umulhi((uint32_t)i, by_w) : i;
+        c[k] = i - r * w;
+        at[k] = r * a.C + c[k];
+        x[k] = ld_feat<DT>(a.x, base + at[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kGnHeld; ++k)
+        if ((int)threadIdx.x + k * kGnThreads < n) s += x[k] - first;
+    const float mu = first + block_sum(s, red[0]) / (float)n;
+#pragma unroll
+    for (int k = 0; k < kGnHeld; ++k) {
+        if ((int)threadIdx.x + k * kGnThreads >= n) break;
+        x[k] -= mu;
+        q = fmaf(x[k], x[k], q);
+    }
+    const float rd = 1.f / sqrtf(block_sum(q, red[1]) / (float)n + a.eps);
+    if (threadIdx.x == 0 && a.stat) ((float2*)a.stat)[blockIdx.x] = make_float2(mu, rd);
+#pragma unroll
+    for (int k = 0; k < kGnHeld; ++k)
+        if ((int)threadIdx.x + k * kGnThreads < n)
+            st_feat<DT>(a.out, base + at[k],
+                        act_of<ACT>(fmaf(x[k] * rd, a.gamma ? a.gamma[g * w + c[k]] : 1.f, a.beta ? a.beta[g * w + c[k]] : 0.f)));
 }
 
 // ---------------------------------------------------------------------------
@@ -710,8 +771,8 @@ __global__ __launch_bounds__(256) void k_gn_groups(GnArgs a) {
         m1 += (double)g * p.x;
         m2 += (double)g * p.y;
     }
-    m1 = wave_sum(m1);
-    m2 = wave_sum(m2);
+    m1 = lanes_sum(m1, true);
+    m2 = lanes_sum(m2, true);
     const double count = n > 0 ? (double)n * (double)w : 1.0;
     if ((threadIdx.x & 63) == 0) a.joined[u] = make_float2((float)(m1 / count), (float)(m2 / count));
 }
@@ -755,9 +816,16 @@ static int gn_tile_rows(int64_t m, int C) {
     return (int)(few > many ? few : many);
 }
 static int64_t gn_tiles(int64_t m, int C, int B) { return m / gn_tile_rows(m, C) + B; }
-// A workgroup joins its scan's tiles itself up to this many numbers, else a kernel does it for all
-constexpr int64_t kGnJoin = 8192;
-static bool gn_join_apart(const GnArgs& a) { return gn_tiles(a.m, a.C, 1) * a.G > kGnJoin; }
+// A workgroup joins its scan's tiles itself: up to 32 of them by 8 lanes a group (64 groups at a time), more by a wave, up to
+// four times over.  Beyond, a launch of its own is shorter.
+static bool gn_few_tiles(const GnArgs& a) { return gn_tiles(a.m, a.C, 1) <= 32; }
+static bool gn_join_apart(const GnArgs& a) { return !gn_few_tiles(a) && a.G > 4 * kGnWaves; }
+
+// All groups of all scans fit a workgroup's registers each (no scan has more than m rows), and there are few values: rows are
+// read a group's channels at a time.  (Whether codes are asked for makes no difference to the other outputs.)
+static bool gn_few(const GnArgs& a) {
+    return a.m * (a.C / a.G) <= (int64_t)kGnHeld * kGnThreads && a.m * a.C <= kGnFew && (int64_t)a.B * a.G <= 4096;
+}
 
 static void gn_ws(Arena& a, GnArgs& t) {
     t.tiles = a.take<float2>((size_t)gn_tiles(t.m, t.C, t.B) * t.G);
@@ -796,16 +864,23 @@ void launch_group_norm(hipStream_t s, const GnArgs& given) {
     gn_kinds(given, [&](auto dt, auto vec, auto act) {
         constexpr int DT = decltype(dt)::value, VEC = decltype(vec)::value, ACT = decltype(act)::value;
         GnArgs a = given;
-        const bool code = VEC > 1 && a.C % kCodeBlock == 0 && a.saved.codes;
+        const bool code = VEC > 1 && a.C % kCodeBlock == 0 && a.saved.codes && !gn_few(a);
         // before out, which may be x
         if (a.saved.codes && !code && a.m)
             launch_checkpoint8(s, a.x, a.saved, RowRange{a.m, nullptr, a.off, a.B}, a.C, a.dt);
+        if (gn_few(a)) {
+            const int w = a.C / a.G;
+            const uint32_t by = w > 1 ? (uint32_t)((((uint64_t)1 << 32) + (uint64_t)w - 1) / (uint64_t)w) : 0u;
+            k_gn_few<DT, ACT><<<(unsigned)(a.B * a.G), kGnThreads, 0, s>>>(a, by);
+            return;
+        }
         if constexpr (VEC == 0) {
             k_gn_stat<DT><<<gn_grid((int64_t)a.B * a.G), 256, 0, s>>>(a);
             if (a.m) k_gn_apply<DT, ACT><<<gn_grid(a.m), 256, 0, s>>>(a);
         } else {
             const int rows = gn_tile_rows(a.m, a.C);
             const unsigned tiles = (unsigned)gn_tiles(a.m, a.C, a.B);
+            a.few_tiles = gn_few_tiles(a);
             k_gn_tile_stat<DT, VEC><<<tiles, kGnThreads, 0, s>>>(a, rows);
             if (gn_join_apart(a)) k_gn_join<true><<<(unsigned)(((int64_t)a.B * a.G + 3) / 4), 256, 0, s>>>(a, rows);
             else a.joined = nullptr;
@@ -824,6 +899,7 @@ template <int DT, int VEC, int ACT, bool X8>
 static void gn_backward_tiles(hipStream_t s, GnArgs a) {
     const int rows = gn_tile_rows(a.m, a.C);
     const int64_t tiles = gn_tiles(a.m, a.C, a.B);
+    a.few_tiles = gn_few_tiles(a);
     const unsigned join = a.dgamma || a.dbeta ? (unsigned)((2 * a.C + 15) / 16) : 0;
     k_gn_tile_sums<DT, VEC, ACT, X8><<<(unsigned)tiles, kGnThreads, 0, s>>>(a, rows);
     if (a.dx && gn_join_apart(a)) k_gn_join<false><<<(unsigned)(((int64_t)a.B * a.G + 3) / 4), 256, 0, s>>>(a, rows);

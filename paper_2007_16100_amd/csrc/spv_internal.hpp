@@ -574,6 +574,7 @@ struct GnArgs {
     float2* tiles;              // [tiles][G] mean and squares, or the backward's sums
     float2* joined;             // [B][G] the same of a scan, as mean and r, or means
     float* part;                // [tiles][2][C] the backward's sums of channels
+    int few_tiles;              // no scan has more than 32
 };
 void plan_group_norm_ws(Arena& a, GnArgs& t);
 void launch_group_norm(hipStream_t s, const GnArgs& a);

@@ -33,13 +33,49 @@ def _rows(t: torch.Tensor, width: int, dtype: torch.dtype, name: str, rows: Opti
         raise ValueError(f"{name} must be contiguous [{'rows' if rows is None else rows}][{width}] of {dtype}")
 
 
-class ScanAttention:
-    """params: gamma, beta [C] f32; Wq [C][H D], Wk, Wv [C][Hkv D], Wo [H D][C] of the features' type.
+class ScanLayer:
+    """What the layers over packed scans share: calls on several streams or from several threads may overlap, as a layer
+    keeps workspaces for each."""
 
-    Calls on several streams or from several threads may overlap: the layer keeps workspaces for each."""
+    def __init__(self):
+        self.ws: Dict[tuple, tuple] = {}
+
+    def _ws(self, name: str, sizes: tuple, make) -> spv.Workspace:
+        """The current stream's and thread's workspace `name` for a call of these sizes: the last one where it served
+        them, or is large enough."""
+        key = (name, spv._stream().value, threading.get_ident())
+        last = self.ws.get(key)
+        if last is None or last[0] != sizes:
+            w = make()
+            last = self.ws[key] = (sizes, w if last is None or w.nbytes > last[1].nbytes else last[1])
+        return last[1]
+
+    def _product(self, x, W, res=None, widest=0):
+        """x W (+ res), in workspaces for up to `widest` channels."""
+        sizes = (max(x.shape[0], 1), max(*W.shape, widest))
+        ws = self._ws("ops", sizes, lambda: spv.Workspace.for_ops(*sizes))
+        return spv.spv_linear(ws, x, W, res=res)[: x.shape[0]]
+
+    def _weight_gradient(self, kept, W, d, widest=0):
+        """dW of kept W, given the product's gradient: kept is the rows or their checkpoint in 8 bits."""
+        if isinstance(kept, torch.Tensor):
+            wide = (max(*W.shape, widest),) * 2
+            ws = self._ws("linear", wide, lambda: spv.Workspace.for_linear_backward(*wide))
+            return spv.spv_linear_backward(ws, kept, W, d, want_dx=False)[1]
+        sizes = (d.shape[0], *W.shape)
+        ws = self._ws(f"linear8 {W.shape[0]} {W.shape[1]}", sizes, lambda: spv.Workspace.for_linear_backward8(*sizes))
+        return spv.spv_linear_backward8(ws, kept, d)
+
+
+class ScanAttention(ScanLayer):
+    """params: gamma, beta [C] f32; Wq [C][H D], Wk, Wv [C][Hkv D], Wo [H D][C] of the features' type.
+    rope: spv.make_rope_params of the heads' channels.  keep8: what save holds of x and of the normalized rows for the
+    backward is in 8 bits (half of bf16's); q, k, v and the output stay, as the softmax's weights are formed from them anew."""
 
     def __init__(self, params: Dict[str, torch.Tensor], heads: int, kv_heads: Optional[int] = None, cap: float = 0.0,
-                 slopes: Optional[torch.Tensor] = None, eps: float = 1e-5):
+                 slopes: Optional[torch.Tensor] = None, eps: float = 1e-5, rope: Optional[spv.RopeParams] = None,
+                 keep8: bool = False):
+        super().__init__()
         self.P = {n: t.contiguous() for n, t in params.items()}
         self.C, width = self.P["Wq"].shape
         self.H, self.K = heads, heads if kv_heads is None else kv_heads
@@ -56,23 +92,12 @@ class ScanAttention:
             size = heads if n == "slopes" else self.C
             if t is not None and (t.dtype != torch.float32 or t.shape != (size,)):
                 raise ValueError(f"{n} must be float32 [{size}]")
-        self.cap, self.slopes, self.eps = cap, slopes, eps
-        self.ws: Dict[tuple, tuple] = {}
-
-    def _ws(self, name: str, sizes: tuple, make) -> spv.Workspace:
-        """The current stream's and thread's workspace `name` for a call of these sizes: the last one where it served
-        them, or is large enough."""
-        key = (name, spv._stream().value, threading.get_ident())
-        last = self.ws.get(key)
-        if last is None or last[0] != sizes:
-            w = make()
-            last = self.ws[key] = (sizes, w if last is None or w.nbytes > last[1].nbytes else last[1])
-        return last[1]
+        if rope is not None and rope.D != self.D:
+            raise ValueError(f"rope must be of heads of {self.D} channels")
+        self.cap, self.slopes, self.eps, self.rope, self.keep8 = cap, slopes, eps, rope, keep8
 
     def _linear(self, x, W, res=None):
-        sizes = (max(x.shape[0], 1), max(self.C, self.H * self.D))
-        ws = self._ws("ops", sizes, lambda: spv.Workspace.for_ops(*sizes))
-        return spv.spv_linear(ws, x, W, res=res)[: x.shape[0]]
+        return self._product(x, W, res, max(self.C, self.H * self.D))
 
     def _attention_ws(self, p, m, n, dtype):
         return self._ws("attention", (m, n, p.B), lambda: spv.Workspace.for_attention_backward(p, m, n, dtype))
@@ -90,15 +115,20 @@ class ScanAttention:
             if token_off is None:
                 raise ValueError("tokens come with their scans' ranges, token_off")
         n, m = x.shape[0], t.shape[0]
-        if self.slopes is not None:
+        if self.slopes is not None or self.rope is not None:
             for c, r, name in ((coords, n, "coords"),) if own else ((coords, n, "coords"), (token_coords, m, "token_coords")):
                 if c is None or c.dtype != torch.int32 or c.dim() != 2 or c.shape[1] != 4 or c.shape[0] < r:
-                    raise ValueError(f"slopes come with {name}, int32 [{r}][4]")
+                    raise ValueError(f"slopes and rope come with {name}, int32 [{r}][4]")
         h = spv.spv_layer_norm(x, P["gamma"], P["beta"], self.eps)
         ht = h if own else spv.spv_layer_norm(t, P["gamma"], P["beta"], self.eps)
         q = self._linear(ht, P["Wq"]).view(m, self.H, self.D)
         k = self._linear(h, P["Wk"]).view(n, self.K, self.D)
         v = self._linear(h, P["Wv"]).view(n, self.K, self.D)
+        if self.rope is not None and own:
+            spv.spv_rope(self.rope, coords, q, k, outs=(q, k))
+        elif self.rope is not None:
+            spv.spv_rope(self.rope, token_coords, q, outs=(q,))
+            spv.spv_rope(self.rope, coords, k, outs=(k,))
         bias = self.slopes is not None
         p = spv.make_attention_params(self.H, self.K, self.D, off if own else token_off, off, cap=self.cap,
                                       q_coords=(coords if own else token_coords) if bias else None,
@@ -108,7 +138,8 @@ class ScanAttention:
             o = spv.spv_attention(ws, p, q, k, v)
         else:
             o, lse = spv.spv_attention(ws, p, q, k, v, want_lse=True)
-            save.update(x=x, h=h, q=q, k=k, v=v, o=o, lse=lse, p=p, own=own)
+            kept = (spv.spv_checkpoint8(x), spv.spv_checkpoint8(h)) if self.keep8 else (x, h)
+            save.update(x=kept[0], h=kept[1], q=q, k=k, v=v, o=o, lse=lse, p=p, own=own, coords=coords)
         return self._linear(o.view(m, self.H * self.D), P["Wo"], res=t)
 
     def backward(self, saved: dict, dy: torch.Tensor) -> Dict[str, torch.Tensor]:
@@ -116,7 +147,7 @@ class ScanAttention:
         if not saved["own"]:
             raise ValueError("backward takes the voxels' own queries")
         P, x, h, p = self.P, saved["x"], saved["h"], saved["p"]
-        n, width, kv = x.shape[0], self.H * self.D, self.K * self.D
+        n, width, kv = saved["q"].shape[0], self.H * self.D, self.K * self.D
         _rows(dy, self.C, self.dtype, "dy", n)
         g = {}
         wide = (max(self.C, width), max(self.C, width))
@@ -125,13 +156,17 @@ class ScanAttention:
         ws = self._attention_ws(p, n, n, x.dtype)
         dq, dk, dv = spv.spv_attention_backward(ws, p, saved["q"], saved["k"], saved["v"], saved["o"], saved["lse"],
                                                 do[:n].view(n, self.H, self.D))
+        if self.rope is not None:
+            spv.spv_rope(self.rope, saved["coords"], dq, dk, inverse=True, outs=(dq, dk))
         dh = None
         for name, d, w in (("Wq", dq, width), ("Wk", dk, kv), ("Wv", dv, kv)):
             d = d.view(n, w)
-            _, g[name] = spv.spv_linear_backward(lin, h, P[name], d, want_dx=False)
+            g[name] = self._weight_gradient(h, P[name], d, max(self.C, width))
             # The three products add up in the residual.  In 16 bits each sum is rounded (bf16 off by 2.3e-3, one rounding
             # 1.7e-3): the linear kernel takes up to 256 inputs, so not the three side by side.
             dh = self._linear(d, P[name].t().contiguous(), res=dh)
+        if self.keep8:
+            x = spv.spv_checkpoint8_read(x)
         wn = self._ws("norm", (n,), lambda: spv.Workspace.for_layer_norm_backward(n, self.C))
         g["x"], g["gamma"], g["beta"] = spv.spv_layer_norm_backward(wn, dh, x, P["gamma"], self.eps, dres=dy)
         return g

@@ -852,11 +852,12 @@ def spv_rope(params: RopeParams, coords: torch.Tensor, q: torch.Tensor, k: Optio
     D, dt = params.D, q.dtype
     sides = [q] if k is None else [q, k]
     if outs is None:
-        outs = [torch.empty(t.shape, dtype=dt, device=t.device) for t in sides]
-    if len(outs) != len(sides) or any(o.shape != t.shape for o, t in zip(outs, sides)):
+        outs = [t.new_empty(t.shape) for t in sides]
+    elif len(outs) != len(sides) or any(o.shape != t.shape for o, t in zip(outs, sides)):
         raise ValueError("outs must have the shapes of what is rotated")
-    n, qp, ldq = _heads(q, q.shape[1], D, dt, "q")
-    _, qo, ldqo = _heads(outs[0], q.shape[1], D, dt, "outs")
+    H = q.shape[1]
+    n, qp, ldq = _heads(q, H, D, dt, "q")
+    _, qo, ldqo = _heads(outs[0], H, D, dt, "outs")
     if coords.dtype != torch.int32 or coords.dim() != 2 or coords.shape[1] != 4 or coords.shape[0] < n:
         raise ValueError(f"coords must be int32 [{n}][4]")
     kp = ko = None
@@ -868,7 +869,7 @@ def spv_rope(params: RopeParams, coords: torch.Tensor, q: torch.Tensor, k: Optio
         if nk != n:
             raise ValueError("q and k must have the same rows")
     cp, count = _addr(coords), _count(m_dev)
-    st = lib().spv_rope(_stream(), ct.byref(params), cp, count, n, qp, ldq, q.shape[1], kp, ldk, K, qo, ldqo, ko, ldko,
+    st = lib().spv_rope(_stream(), ct.byref(params), cp, count, n, qp, ldq, H, kp, ldk, K, qo, ldqo, ko, ldko,
                         int(inverse), _DT[dt])
     _chk(st, "spv_rope")
     return outs[0] if k is None else tuple(outs)
@@ -894,6 +895,14 @@ class Checkpoint8:
         return cls(torch.empty((m, C), dtype=torch.int8, device=device),
                    torch.empty((m, blocks), dtype=torch.uint8, device=device), dtype)
 
+    @classmethod
+    def _like(cls, x: torch.Tensor):
+        """A new one for rows like x, and its addresses."""
+        m, C = x.shape
+        codes = x.new_empty((m, C), dtype=torch.int8)
+        exps = x.new_empty((m, (C + SPV_CHECKPOINT8_BLOCK - 1) // SPV_CHECKPOINT8_BLOCK), dtype=torch.uint8)
+        return cls(codes, exps, x.dtype), codes.data_ptr(), exps.data_ptr()
+
     def addresses(self):
         m, C = self.codes.shape
         if self.codes.dtype != torch.int8 or self.exps.dtype != torch.uint8 or \
@@ -907,10 +916,11 @@ def spv_checkpoint8(x: torch.Tensor, m_dev: Optional[torch.Tensor] = None,
     """The rows x [m][C] in 8 bits, with an exponent for each 32 channels of a row."""
     m, C = x.shape
     if out is None:
-        out = Checkpoint8.empty(m, C, x.dtype, x.device)
+        out, codes, exps = Checkpoint8._like(x)
     elif out.codes.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("out must have x's shape and type")
-    codes, exps = out.addresses()
+    else:
+        codes, exps = out.addresses()
     xp, count = _addr(x), _count(m_dev)
     st = lib().spv_checkpoint8(_stream(), xp, count, m, C, codes, exps, _DT[x.dtype])
     _chk(st, "spv_checkpoint8")
@@ -923,7 +933,7 @@ def spv_checkpoint8_read(saved: Checkpoint8, m_dev: Optional[torch.Tensor] = Non
     codes, exps = saved.addresses()
     m, C = saved.codes.shape
     if out is None:
-        out = torch.empty((m, C), dtype=saved.dtype, device=saved.codes.device)
+        out = saved.codes.new_empty((m, C), dtype=saved.dtype)
     elif out.shape != (m, C) or out.dtype != saved.dtype:
         raise ValueError("out must have the rows' shape and type")
     op, count = _addr(out), _count(m_dev)
@@ -942,7 +952,7 @@ def spv_linear_backward8(ws: Workspace, saved: Checkpoint8, da: torch.Tensor, m_
         raise ValueError(f"da must be [{m}][Cout] of {saved.dtype}")
     Cout = da.shape[1]
     if out is None:
-        out = torch.empty((Cin, Cout), dtype=torch.float32, device=da.device)
+        out = da.new_empty((Cin, Cout), dtype=torch.float32)
     elif out.shape != (Cin, Cout) or out.dtype != torch.float32:
         raise ValueError(f"out must be float32 [{Cin}][{Cout}]")
     dap, op, count = _addr(da), _addr(out), _count(m_dev)
@@ -975,8 +985,7 @@ def spv_group_norm(ws: Workspace, x: torch.Tensor, off: torch.Tensor, groups: in
     elif out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("out must have x's shape and type")
     stat = torch.empty((B, groups, 2), dtype=torch.float32, device=x.device) if want_stat else None
-    saved = Checkpoint8.empty(m, C, x.dtype, x.device) if want_checkpoint else None
-    codes, exps = saved.addresses() if saved is not None else (None, None)
+    saved, codes, exps = Checkpoint8._like(x) if want_checkpoint else (None, None, None)
     st = lib().spv_group_norm(_stream(), ws.ptr, ws.nbytes, xp, m, C, _addr(off), B, groups, gp, bp, eps, _ACT[act],
                               _addr(out), _addr(stat), codes, exps, _DT[x.dtype])
     _chk(st, "spv_group_norm")
@@ -1008,7 +1017,7 @@ def spv_group_norm_backward(ws: Workspace, dy: torch.Tensor, x, off: torch.Tenso
         raise ValueError(f"stat must be float32 [{B}][{groups}][2]")
     gp, bp = _channels(gamma, C, "gamma"), _channels(beta, C, "beta")
     dx = torch.empty_like(dy)
-    dgamma = torch.empty(C, dtype=torch.float32, device=dy.device)
+    dgamma = dy.new_empty(C, dtype=torch.float32)
     dbeta = torch.empty_like(dgamma)
     st = lib().spv_group_norm_backward(_stream(), ws.ptr, ws.nbytes, _addr(dy), xp, codes, exps, m, C, _addr(off), B,
                                        groups, gp, bp, _addr(stat), _ACT[act], _addr(dres), dx.data_ptr(),

@@ -1,0 +1,233 @@
+"""The attention layer with rotary positions and rows kept in 8 bits, and the pre-activation layer with group norm, against the
+same layers in float64 with their gradients from autograd; and a training step of both, one after the other."""
+import numpy as np
+import pytest
+import torch
+
+from tests import voxel_ops_ref as ref
+
+pytestmark = pytest.mark.gpu
+TD = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+# the framework's normwise bounds of chains of layers (16-bit: rounded between the layers)
+TOL = {"f32": 1e-5, "bf16": 2e-2, "f16": 4e-3}
+LENS = [300, 0, 211, 1]
+
+
+@pytest.fixture(scope="module")
+def spv():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2007_16100_amd import spv as s
+    s.lib()
+    return s
+
+
+def normwise(got, want):
+    return ((got.detach().double().cpu() - want).abs().max() / want.abs().max()).item()
+
+
+def voxels(lens, seed):
+    g = torch.Generator().manual_seed(seed)
+    c = torch.randint(-60, 60, (sum(lens), 4), generator=g, dtype=torch.int32)
+    c[:, 0] = torch.repeat_interleave(torch.arange(len(lens)), torch.tensor(lens))
+    return c.cuda(), torch.tensor(np.cumsum([0, *lens]), dtype=torch.int32).cuda()
+
+
+def draws(seed, dtype):
+    g = torch.Generator().manual_seed(seed)
+
+    def normal(*shape, std=1.0, to=None):
+        return (torch.randn(*shape, generator=g) * std).to(to or TD[dtype]).cuda()
+    return normal
+
+
+def attention_params(C, H, K, D, dtype, seed):
+    r = draws(seed, dtype)
+    return dict(gamma=1 + r(C, std=0.1, to=torch.float32), beta=r(C, std=0.1, to=torch.float32), Wq=r(C, H * D, std=C ** -0.5),
+                Wk=r(C, K * D, std=C ** -0.5), Wv=r(C, K * D, std=C ** -0.5), Wo=r(H * D, C, std=(H * D) ** -0.5))
+
+
+def mlp_params(C, F, dtype, seed):
+    r = draws(seed, dtype)
+    return dict(gamma1=1 + r(C, std=0.1, to=torch.float32), beta1=r(C, std=0.1, to=torch.float32),
+                gamma2=1 + r(F, std=0.1, to=torch.float32), beta2=r(F, std=0.1, to=torch.float32), W1=r(C, F, std=C ** -0.5),
+                W2=r(F, C, std=F ** -0.5))
+
+
+def turn(t, heads, coords, freqs, sections):
+    """Rotary positions in float64, pairs of neighbours."""
+    n, P = t.shape[0], sum(sections)
+    axis = [1 + a for a, s in enumerate(sections) for _ in range(s)]
+    x = t.view(n, heads, -1)
+    z = torch.view_as_complex(x[..., :2 * P].reshape(n, heads, P, 2))
+    z = z * torch.polar(torch.ones(n, P, dtype=torch.float64), coords[:, axis].double() * freqs.double())[:, None]
+    return torch.cat([torch.view_as_real(z).reshape(n, heads, 2 * P), x[..., 2 * P:]], -1).reshape(n, -1)
+
+
+def plain_attention(P, x, H, K, off, coords, freqs, sections, tokens=None, t_off=None, t_coords=None):
+    def ln(t):
+        return torch.nn.functional.layer_norm(t, t.shape[1:], P["gamma"], P["beta"], 1e-5)
+    if tokens is None:
+        tokens, t_off, t_coords = x, off, coords
+    h = ln(x)
+    q, k, v = turn(ln(tokens) @ P["Wq"], H, t_coords, freqs, sections), turn(h @ P["Wk"], K, coords, freqs, sections), h @ P["Wv"]
+    D, rows = q.shape[1] // H, []
+    for b in range(len(off) - 1):
+        i, j = slice(t_off[b], t_off[b + 1]), slice(off[b], off[b + 1])
+        heads = []
+        for a in range(H):
+            c = slice(a // (H // K) * D, (a // (H // K) + 1) * D)
+            heads.append(torch.softmax(q[i, a * D:(a + 1) * D] @ k[j, c].T / D ** 0.5, 1) @ v[j, c])
+        rows.append(torch.cat(heads, 1))
+    return tokens + torch.cat(rows) @ P["Wo"]
+
+
+def plain_mlp(P, x, groups, off, act):
+    f = dict(none=lambda t: t, relu=torch.relu, silu=torch.nn.functional.silu)[act]
+
+    def norm(t, g, b):
+        rows = []
+        for i, j in zip(off, off[1:]):
+            r = t[i:j].reshape(j - i, groups, t.shape[1] // groups)
+            if j > i:
+                r = (r - r.mean((0, 2), keepdim=True)) / torch.sqrt(r.var((0, 2), unbiased=False, keepdim=True) + 1e-5)
+            rows.append(r.reshape(j - i, t.shape[1]))
+        return f(torch.cat(rows) * g + b)
+    return x + norm(norm(x, P["gamma1"], P["beta1"]) @ P["W1"], P["gamma2"], P["beta2"]) @ P["W2"]
+
+
+def leaves(P, x):
+    return {k: t.double().cpu().clone().requires_grad_() for k, t in P.items()}, x.double().cpu().requires_grad_()
+
+
+def compare(grads, want, Pd, xd, dy, tol, step=0.0):
+    """A vector given as [rows][channels] (one for each row) has its gradient's terms there: they are off by some dozens of
+    float32 roundings of their own size each, also where they add up to nothing (as for a shift that a later norm takes
+    off); with rows in 8 bits by up to `step` of it too, of either sign as values fall between the codes: four
+    standard deviations of their sum at most."""
+    names = list(Pd)
+    for k, r in zip(names + ["x"], torch.autograd.grad(want, [Pd[k] for k in names] + [xd], dy.double().cpu())):
+        terms = 0.0
+        if r.shape != grads[k].shape:
+            terms = 64 * ref.EPS * r.abs().sum(0).max().item() + 4 * step * (r ** 2).sum(0).max().item() ** 0.5
+            r = r.sum(0)
+        err = (grads[k].detach().double().cpu() - r).abs().max().item()
+        print(k, err / r.abs().max().item(), flush=True)
+        assert err <= tol * (2 if k != "x" else 1) * r.abs().max().item() + terms, k
+
+
+@pytest.mark.parametrize("dtype,C,H,K,sections", [("bf16", 128, 4, 4, (6, 6, 4)), ("f16", 96, 3, 1, (4, 4, 4)),
+                                                  ("f32", 64, 2, 2, (5, 5, 6))])
+def test_attention_with_rotary_positions(spv, dtype, C, H, K, sections):
+    from paper_2007_16100_amd.scan_attention import ScanAttention
+    coords, off = voxels(LENS, 1)
+    n, D, r = coords.shape[0], C // H, draws(7, dtype)
+    P, freqs = attention_params(C, H, K, D, dtype, C), spv.rope_freqs(sections, 50.0)
+    rope = spv.make_rope_params(D, freqs, sections)
+    x, dy, saved = r(n, C), r(n, C), {}
+    layer = ScanAttention(P, H, K, rope=rope)
+    y = layer.forward(x, off, coords, save=saved)
+    grads = layer.backward(saved, dy)
+    Pd, xd = leaves(P, x)
+    args = (H, K, off.tolist(), coords.cpu(), freqs.cpu(), sections)
+    want = plain_attention(Pd, xd, *args)
+    assert normwise(y, want.detach()) <= TOL[dtype]
+    compare(grads, want, Pd, xd, dy, TOL[dtype])
+    # the same scores with the map's frame moved: a rotation by the same angles on both sides
+    moved = coords + torch.tensor([0, 3000, -7000, 40], dtype=torch.int32, device="cuda")
+    assert normwise(layer.forward(x, off, moved), want.detach()) <= TOL[dtype]
+    # two tokens a scan (none of the empty one's): a serving step
+    t_off = torch.tensor([0, 2, 2, 4, 6], dtype=torch.int32).cuda()
+    tok, tc = r(6, C), voxels([2, 0, 2, 2], 5)[0]
+    got = layer.forward(x, off, coords, tok, t_off, tc)
+    with torch.no_grad():
+        want = plain_attention(Pd, xd, *args, tok.double().cpu(), t_off.tolist(), tc.cpu())
+    assert normwise(got, want) <= TOL[dtype]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_attention_from_rows_in_8_bits(spv, dtype):
+    """The same output; weight gradients and the layer norm's are those of the rows read back."""
+    from paper_2007_16100_amd.scan_attention import ScanAttention
+    coords, off = voxels(LENS, 2)
+    n, C, H, K, D, r = coords.shape[0], 128, 4, 2, 32, draws(8, dtype)
+    P, x, dy = attention_params(C, H, K, D, dtype, 3), r(n, C), r(n, C)
+    rope = spv.make_rope_params(D, spv.rope_freqs((6, 6, 4)), (6, 6, 4))
+    whole, held = {}, {}
+    layer, small = ScanAttention(P, H, K, rope=rope), ScanAttention(P, H, K, rope=rope, keep8=True)
+    assert torch.equal(layer.forward(x, off, coords, save=whole), small.forward(x, off, coords, save=held))
+    assert isinstance(held["x"], spv.Checkpoint8) and isinstance(held["h"], spv.Checkpoint8)
+    back = {k: spv.spv_checkpoint8_read(held[k]) for k in "xh"}
+    want, got = layer.backward(dict(whole, **back), dy), small.backward(held, dy)
+    for k in ("Wo", "x", "gamma", "beta"):
+        assert torch.equal(got[k], want[k]), k
+    rows = back["h"].double().cpu().numpy()
+    for k in ("Wq", "Wk", "Wv"):  # the same sums in another order: at most the rows' roundings of their terms
+        bound = 4 * n * ref.EPS * (np.abs(rows).sum(0).max() * 8 * want[k].abs().max().item())
+        assert (got[k] - want[k]).abs().max().item() <= bound
+        assert normwise(got[k], want[k].double().cpu()) <= 1e-5
+
+
+@pytest.mark.parametrize("keep8", [False, True])
+@pytest.mark.parametrize("dtype,C,F,groups,act", [("bf16", 96, 192, 8, "silu"), ("f16", 128, 64, 16, "silu"),
+                                                  ("f32", 32, 96, 4, "silu"), ("f32", 64, 64, 64, "none")])
+def test_mlp_and_gradients(spv, dtype, C, F, groups, act, keep8):
+    from paper_2007_16100_amd.scan_mlp import ScanMLP
+    lens = [300, 0, 211, 64]
+    off = torch.tensor(np.cumsum([0, *lens]), dtype=torch.int32).cuda()
+    n, r, P = sum(lens), draws(C, dtype), mlp_params(C, F, dtype, C + F)
+    x, dy, saved = r(n, C), r(n, C), {}
+    layer = ScanMLP(P, groups, act, keep8=keep8)
+    y = layer.forward(x, off, save=saved)
+    assert torch.equal(y, layer.forward(x, off))
+    grads = layer.backward(saved, dy)
+    if keep8:
+        assert all(isinstance(saved[k], spv.Checkpoint8) for k in ("in1", "out1", "in2", "out2"))
+        # the gradients of the same layer from the rows read back, which differ by orders of sums alone; the statistics
+        # are the forward's in both
+        back = {k: spv.spv_checkpoint8_read(saved[k]) for k in ("in1", "out1", "in2", "out2")}
+        want = layer.backward(dict(saved, **back), dy)
+        for k, t in want.items():
+            if k[0] == "W":
+                assert normwise(grads[k], t.double().cpu()) <= 1e-5, k
+            else:
+                assert torch.equal(grads[k], t), k
+    Pd, xd = leaves({k: t if k[0] == "W" else t.expand(n, -1) for k, t in P.items()}, x)
+    want = plain_mlp(Pd, xd, groups, off.tolist(), act)
+    assert normwise(y, want.detach()) <= TOL[dtype]
+    # a value in 8 bits is off by 2^-7 of the largest of its 32 at most (2^-6 above 127.5 steps): xh by that times the largest
+    # |xh| (some 4), and as much in the sums of the backward that it multiplies
+    step = 4 * 2.0 ** -7 if keep8 else 0.0
+    compare(grads, want, Pd, xd, dy, TOL[dtype] + step, step)
+
+
+def test_a_training_step_of_both_layers_in_a_graph(spv):
+    """Attention and the pre-activation layer one after the other, forward and backward, captured and replayed next to eager
+    steps of the same layers: every replay gives the eager gradients of its inputs."""
+    from paper_2007_16100_amd.scan_attention import ScanAttention
+    from paper_2007_16100_amd.scan_mlp import ScanMLP
+    coords, off = voxels(LENS, 4)
+    n, C, H = coords.shape[0], 96, 3
+    rope = spv.make_rope_params(32, spv.rope_freqs((6, 6, 4)), (6, 6, 4))
+    att = ScanAttention(attention_params(C, H, H, 32, "bf16", 1), H, rope=rope, keep8=True)
+    mlp = ScanMLP(mlp_params(C, 192, "bf16", 2), 8, keep8=True)
+
+    def step(x, dy):
+        a, b = {}, {}
+        y = mlp.forward(att.forward(x, off, coords, save=a), off, save=b)
+        g = mlp.backward(b, dy)
+        return [y, *g.values(), *att.backward(a, g["x"]).values()]
+    r = draws(3, "bf16")
+    x, dy = r(n, C), r(n, C)
+    step(x, dy)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(x, dy)
+    for _ in range(3):
+        x.copy_(r(n, C))
+        dy.copy_(r(n, C))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, step(x, dy)):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()

@@ -1,0 +1,70 @@
+"""What the layers with rotary positions, group norm and rows kept in 8 bits refuse before any kernel runs."""
+import pytest
+import torch
+
+from paper_2007_16100_amd import scan_attention, scan_mlp, spv
+from paper_2007_16100_amd.scan_attention import ScanAttention
+from paper_2007_16100_amd.scan_mlp import ScanMLP
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture
+def no_calls(monkeypatch):
+    """Every call that would launch a kernel or take device memory fails the test."""
+    def fail(name):
+        def f(*a, **k):
+            raise AssertionError(f"{name} was called")
+        return f
+    for name in [n for n in dir(spv) if n.startswith("spv_")] + ["Workspace"]:
+        monkeypatch.setattr(scan_attention.spv, name, fail(name))
+
+
+def mlp(C=64, F=128, dtype=BF, **other):
+    P = dict(gamma1=torch.ones(C), beta1=torch.zeros(C), gamma2=torch.ones(F), beta2=torch.zeros(F),
+             W1=torch.zeros(C, F, dtype=dtype), W2=torch.zeros(F, C, dtype=dtype))
+    return dict(P, **other)
+
+
+@pytest.mark.parametrize("other", [
+    dict(W2=torch.zeros(128, 32, dtype=BF)), dict(W2=torch.zeros(128, 64)), dict(gamma1=torch.ones(128)),
+    dict(gamma2=torch.ones(128, dtype=BF)), dict(beta1=torch.ones(64, 1)), dict(beta2=torch.ones(64)),
+    dict(W1=torch.zeros(64, 128, dtype=torch.float64), W2=torch.zeros(128, 64, dtype=torch.float64))])
+def test_parameters_of_other_types_and_widths(no_calls, other):
+    with pytest.raises(ValueError):
+        ScanMLP(mlp(**other), 8)
+
+
+@pytest.mark.parametrize("groups,act", [(0, "silu"), (-2, "silu"), (3, "silu"), (128, "silu"), (8, "gelu"), (8, None)])
+def test_groups_and_activations(no_calls, groups, act):
+    with pytest.raises(ValueError):
+        ScanMLP(mlp(), groups, act)
+
+
+def test_features_and_gradients_that_do_not_fit(no_calls):
+    layer, off, x = ScanMLP(mlp(), 8), torch.tensor([0, 10], dtype=torch.int32), torch.zeros(10, 64, dtype=BF)
+    for bad in (x.float(), x[:, :32], x.t(), x.view(2, 5, 64), x.half()):
+        with pytest.raises(ValueError):
+            layer.forward(bad, off)
+    for dy in (x[:9], x.float(), torch.zeros(10, 32, dtype=BF)):
+        with pytest.raises(ValueError):
+            layer.backward(dict(in1=x, off=off), dy)
+        with pytest.raises(ValueError):
+            layer.backward(dict(in1=spv.Checkpoint8.empty(10, 64, BF, "cpu"), off=off), dy)
+
+
+def attention(**kw):
+    P = dict(gamma=torch.ones(64), beta=torch.zeros(64), Wq=torch.zeros(64, 64, dtype=BF), Wk=torch.zeros(64, 32, dtype=BF),
+             Wv=torch.zeros(64, 32, dtype=BF), Wo=torch.zeros(64, 64, dtype=BF))
+    return ScanAttention(P, 4, 2, **kw)
+
+
+def test_rotary_positions_without_coordinates(no_calls):
+    with pytest.raises(ValueError):
+        attention(rope=spv.RopeParams(32))
+    layer, off = attention(rope=spv.RopeParams(16)), torch.tensor([0, 10], dtype=torch.int32)
+    x, tok, c = torch.zeros(10, 64, dtype=BF), torch.zeros(2, 64, dtype=BF), torch.zeros(10, 4, dtype=torch.int32)
+    for kw in (dict(), dict(coords=c[:9]), dict(coords=c.long()), dict(coords=c, tokens=tok, token_off=off),
+               dict(coords=c, tokens=tok, token_off=off, token_coords=c[:1])):
+        with pytest.raises(ValueError):
+            layer.forward(x, off, **kw)
