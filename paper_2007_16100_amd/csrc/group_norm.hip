@@ -24,15 +24,16 @@ __device__ inline float act_of(float z) {
     else if constexpr (ACT == SPV_ACT_SILU) return z * sigmoid(z);
     else return z;
 }
+// d act'(z); ReLU's is d or 0, also where d is not finite
 template <int ACT>
-__device__ inline float act_slope(float z) {
+__device__ inline float act_grad(float d, float z) {
     if constexpr (ACT == SPV_ACT_RELU) {
-        return z <= 0.f ? 0.f : 1.f;
+        return z <= 0.f ? 0.f : d;
     } else if constexpr (ACT == SPV_ACT_SILU) {
         const float s = sigmoid(z);
-        return s * fmaf(z, 1.f - s, 1.f);
+        return d * (s * fmaf(z, 1.f - s, 1.f));
     } else {
-        return 1.f;
+        return d;
     }
 }
 
@@ -477,7 +478,7 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
                 S::unpack(u[k].x, x);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const float xh = (x[e] - mu[e]) * r[e], gz = d[e] * act_slope<ACT>(fmaf(xh, ga[e], be[e]));
+                    const float xh = (x[e] - mu[e]) * r[e], gz = act_grad<ACT>(d[e], fmaf(xh, ga[e], be[e]));
                     s1[e] += gz;
                     s2[e] = fmaf(gz, xh, s2[e]);
                 }
@@ -596,7 +597,7 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const float xh = (x[e] - mu[e]) * r[e];
-                const float h = d[e] * act_slope<ACT>(fmaf(xh, ga[e], be[e])) * ga[e];
+                const float h = act_grad<ACT>(d[e], fmaf(xh, ga[e], be[e])) * ga[e];
                 d[e] = fmaf(r[e], h - m1[e] - xh * m2[e], q[e]);
             }
             V::store(a.dx, base + (int64_t)(i0 + k * R) * a.C, d);
@@ -748,7 +749,7 @@ __global__ __launch_bounds__(256) void k_gn_sums(GnArgs a) {
         double s1 = 0.0, s2 = 0.0;
         for (int64_t i = r0 + threadIdx.x; i < r1; i += 256) {
             const float xh = (saved_x<DT>(a, i, c) - st.x) * st.y;
-            const float gz = ld_feat<DT>(a.dy, i * a.C + c) * act_slope<ACT>(fmaf(xh, g, be));
+            const float gz = act_grad<ACT>(ld_feat<DT>(a.dy, i * a.C + c), fmaf(xh, g, be));
             s1 += (double)gz;
             s2 += (double)gz * xh;
         }
@@ -787,7 +788,7 @@ __global__ __launch_bounds__(256) void k_gn_dx(GnArgs a) {
             const int64_t u = (int64_t)b * a.G + c / w;
             const float2 st = ((const float2*)a.stat)[u], me = a.joined[u];
             const float g = a.gamma ? a.gamma[c] : 1.f, xh = (saved_x<DT>(a, i, c) - st.x) * st.y;
-            const float h = ld_feat<DT>(a.dy, i * a.C + c) * act_slope<ACT>(fmaf(xh, g, a.beta ? a.beta[c] : 0.f)) * g;
+            const float h = act_grad<ACT>(ld_feat<DT>(a.dy, i * a.C + c), fmaf(xh, g, a.beta ? a.beta[c] : 0.f)) * g;
             float d = st.y * (h - me.x - xh * me.y);
             if (a.dres) d += ld_feat<DT>(a.dres, i * a.C + c);
             st_feat<DT>(a.dx, i * a.C + c, d);

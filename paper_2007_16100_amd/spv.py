@@ -827,6 +827,47 @@ def spv_attention_backward(ws: Workspace, params: AttentionParams, q: torch.Tens
     return tuple(grads)
 
 
+def _here() -> int:
+    """The current device, whose current stream the calls below run on: their tensors have to be there."""
+    return torch.cuda.current_device()
+
+
+def _stream_of(dev: int):
+    return ct.c_void_p(_raw_stream(dev)) if _raw_stream is not None else _stream()
+
+
+def _at(t: Optional[torch.Tensor], dev: int):
+    """_addr of a tensor on device dev."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise ValueError(f"libspv takes tensors of the current device, cuda:{dev}")
+    if not t.is_contiguous():
+        raise ValueError("libspv takes contiguous tensors")
+    return t.data_ptr()
+
+
+def _vector(t: Optional[torch.Tensor], C: int, name: str, dev: int):
+    """_channels of a tensor on device dev."""
+    if t is not None and (t.dtype != torch.float32 or t.shape != (C,)):
+        raise ValueError(f"{name} must be float32 [{C}]")
+    return _at(t, dev)
+
+
+def _count(t: Optional[torch.Tensor], dev: int):
+    """Address of a device row count."""
+    if t is not None and (t.dtype != torch.int64 or t.numel() < 1):
+        raise ValueError("a row count is int64 [1]")
+    return _at(t, dev)
+
+
+def _rows_of(t: torch.Tensor, heads: int, D: int, dtype: torch.dtype, name: str, dev: int):
+    """_heads of a tensor on device dev."""
+    if t.get_device() != dev:
+        raise ValueError(f"libspv takes tensors of the current device, cuda:{dev}")
+    return _heads(t, heads, D, dtype, name)
+
+
 def make_rope_params(D: int, freqs: torch.Tensor, sections: Sequence[int], halves: bool = False) -> RopeParams:
     """Parameters of a rotation of heads of D channels by voxel coordinates: sections = pairs of channels that turn
     with x, y and z; freqs [their sum] float32, radians a voxel.  Pair p is channels (2 p, 2 p + 1), or with halves
@@ -834,7 +875,7 @@ def make_rope_params(D: int, freqs: torch.Tensor, sections: Sequence[int], halve
     if len(sections) != 3:
         raise ValueError("sections are the pairs of x, y and z")
     p = RopeParams(D, (ct.c_int32 * 3)(*sections), int(halves), _channels(freqs, sum(sections), "freqs"))
-    p._keep = freqs
+    p._keep, p._ref = freqs, ct.byref(p)
     return p
 
 
@@ -849,37 +890,36 @@ def spv_rope(params: RopeParams, coords: torch.Tensor, q: torch.Tensor, k: Optio
     """q [n][H][D] (and k [n][Hkv][D]) rotated by the rows' coordinates [n][4]: q' or (q', k').  inverse: the
     rotation back, which turns gradients of the rotated rows into the rows'.  q, k and outs (the tensors to write, which
     may be q and k themselves) may be parts of wider rows."""
-    D, dt = params.D, q.dtype
-    sides = [q] if k is None else [q, k]
-    if outs is None:
-        outs = [t.new_empty(t.shape) for t in sides]
-    elif len(outs) != len(sides) or any(o.shape != t.shape for o, t in zip(outs, sides)):
-        raise ValueError("outs must have the shapes of what is rotated")
-    H = q.shape[1]
-    n, qp, ldq = _heads(q, H, D, dt, "q")
-    _, qo, ldqo = _heads(outs[0], H, D, dt, "outs")
-    if coords.dtype != torch.int32 or coords.dim() != 2 or coords.shape[1] != 4 or coords.shape[0] < n:
-        raise ValueError(f"coords must be int32 [{n}][4]")
+    D, dt, H, dev = params.D, q.dtype, q.shape[1], _here()
+    n, qp, ldq = _rows_of(q, H, D, dt, "q", dev)
     kp = ko = None
     K = ldk = ldko = 0
     if k is not None:
         K = k.shape[1]
-        nk, kp, ldk = _heads(k, K, D, dt, "k")
-        _, ko, ldko = _heads(outs[1], K, D, dt, "outs")
+        nk, kp, ldk = _rows_of(k, K, D, dt, "k", dev)
         if nk != n:
             raise ValueError("q and k must have the same rows")
-    cp, count = _addr(coords), _count(m_dev)
-    st = lib().spv_rope(_stream(), ct.byref(params), cp, count, n, qp, ldq, H, kp, ldk, K, qo, ldqo, ko, ldko,
+    if coords.dtype != torch.int32 or coords.dim() != 2 or coords.shape[1] != 4 or coords.shape[0] < n:
+        raise ValueError(f"coords must be int32 [{n}][4]")
+    if params._keep.get_device() != dev:
+        raise ValueError(f"libspv takes tensors of the current device, cuda:{dev}")
+    cp, count = _at(coords, dev), _count(m_dev, dev)
+    if outs is None:
+        outs = (q.new_empty(q.shape),) if k is None else (q.new_empty(q.shape), k.new_empty(k.shape))
+        qo, ldqo = outs[0].data_ptr(), H * D
+        if k is not None:
+            ko, ldko = outs[1].data_ptr(), K * D
+    else:
+        sides = (q,) if k is None else (q, k)
+        if len(outs) != len(sides) or any(o.shape != t.shape for o, t in zip(outs, sides)):
+            raise ValueError("outs must have the shapes of what is rotated")
+        _, qo, ldqo = _rows_of(outs[0], H, D, dt, "outs", dev)
+        if k is not None:
+            _, ko, ldko = _rows_of(outs[1], K, D, dt, "outs", dev)
+    st = lib().spv_rope(_stream_of(dev), params._ref, cp, count, n, qp, ldq, H, kp, ldk, K, qo, ldqo, ko, ldko,
                         int(inverse), _DT[dt])
     _chk(st, "spv_rope")
     return outs[0] if k is None else tuple(outs)
-
-
-def _count(t: Optional[torch.Tensor]):
-    """Address of a device row count."""
-    if t is not None and (t.dtype != torch.int64 or t.numel() < 1):
-        raise ValueError("a row count is int64 [1]")
-    return _addr(t)
 
 
 @dataclass
@@ -903,26 +943,27 @@ class Checkpoint8:
         exps = x.new_empty((m, (C + SPV_CHECKPOINT8_BLOCK - 1) // SPV_CHECKPOINT8_BLOCK), dtype=torch.uint8)
         return cls(codes, exps, x.dtype), codes.data_ptr(), exps.data_ptr()
 
-    def addresses(self):
+    def addresses(self, dev: int):
         m, C = self.codes.shape
         if self.codes.dtype != torch.int8 or self.exps.dtype != torch.uint8 or \
                 self.exps.shape != (m, (C + SPV_CHECKPOINT8_BLOCK - 1) // SPV_CHECKPOINT8_BLOCK):
             raise ValueError("a checkpoint is int8 [rows][channels] with uint8 [rows][blocks of 32 channels]")
-        return _addr(self.codes), _addr(self.exps)
+        return _at(self.codes, dev), _at(self.exps, dev)
 
 
 def spv_checkpoint8(x: torch.Tensor, m_dev: Optional[torch.Tensor] = None,
                     out: Optional[Checkpoint8] = None) -> Checkpoint8:
     """The rows x [m][C] in 8 bits, with an exponent for each 32 channels of a row."""
     m, C = x.shape
+    dev = _here()
+    xp, count = _at(x, dev), _count(m_dev, dev)
     if out is None:
         out, codes, exps = Checkpoint8._like(x)
     elif out.codes.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("out must have x's shape and type")
     else:
-        codes, exps = out.addresses()
-    xp, count = _addr(x), _count(m_dev)
-    st = lib().spv_checkpoint8(_stream(), xp, count, m, C, codes, exps, _DT[x.dtype])
+        codes, exps = out.addresses(dev)
+    st = lib().spv_checkpoint8(_stream_of(dev), xp, count, m, C, codes, exps, _DT[x.dtype])
     _chk(st, "spv_checkpoint8")
     return out
 
@@ -930,14 +971,15 @@ def spv_checkpoint8(x: torch.Tensor, m_dev: Optional[torch.Tensor] = None,
 def spv_checkpoint8_read(saved: Checkpoint8, m_dev: Optional[torch.Tensor] = None,
                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The rows [m][C] that a checkpoint stands for, in the type they came from."""
-    codes, exps = saved.addresses()
+    dev = _here()
+    codes, exps = saved.addresses(dev)
     m, C = saved.codes.shape
     if out is None:
         out = saved.codes.new_empty((m, C), dtype=saved.dtype)
     elif out.shape != (m, C) or out.dtype != saved.dtype:
         raise ValueError("out must have the rows' shape and type")
-    op, count = _addr(out), _count(m_dev)
-    st = lib().spv_checkpoint8_read(_stream(), codes, exps, count, m, C, op, _DT[saved.dtype])
+    op, count = _at(out, dev), _count(m_dev, dev)
+    st = lib().spv_checkpoint8_read(_stream_of(dev), codes, exps, count, m, C, op, _DT[saved.dtype])
     _chk(st, "spv_checkpoint8_read")
     return out
 
@@ -946,7 +988,8 @@ def spv_linear_backward8(ws: Workspace, saved: Checkpoint8, da: torch.Tensor, m_
                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dW [Cin][Cout] float32 of a linear layer whose input rows were kept in 8 bits, given its product's gradient
     da [m][Cout]."""
-    codes, exps = saved.addresses()
+    dev = _here()
+    codes, exps = saved.addresses(dev)
     m, Cin = saved.codes.shape
     if da.dim() != 2 or da.shape[0] != m or da.dtype != saved.dtype:
         raise ValueError(f"da must be [{m}][Cout] of {saved.dtype}")
@@ -955,8 +998,8 @@ def spv_linear_backward8(ws: Workspace, saved: Checkpoint8, da: torch.Tensor, m_
         out = da.new_empty((Cin, Cout), dtype=torch.float32)
     elif out.shape != (Cin, Cout) or out.dtype != torch.float32:
         raise ValueError(f"out must be float32 [{Cin}][{Cout}]")
-    dap, op, count = _addr(da), _addr(out), _count(m_dev)
-    st = lib().spv_linear_backward8(_stream(), ws.ptr, ws.nbytes, codes, exps, count, m, Cin, dap, Cout, op,
+    dap, op, count = _at(da, dev), _at(out, dev), _count(m_dev, dev)
+    st = lib().spv_linear_backward8(_stream_of(dev), ws.ptr, ws.nbytes, codes, exps, count, m, Cin, dap, Cout, op,
                                     _DT[da.dtype])
     _chk(st, "spv_linear_backward8")
     return out
@@ -979,15 +1022,16 @@ def spv_group_norm(ws: Workspace, x: torch.Tensor, off: torch.Tensor, groups: in
     B = _scans(off)
     if act not in _ACT:
         raise ValueError(f"act must be one of {', '.join(_ACT)}")
-    xp, gp, bp = _addr(x), _channels(gamma, C, "gamma"), _channels(beta, C, "beta")
+    dev = _here()
+    xp, gp, bp = _at(x, dev), _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev)
     if out is None:
         out = torch.empty_like(x)
     elif out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("out must have x's shape and type")
     stat = torch.empty((B, groups, 2), dtype=torch.float32, device=x.device) if want_stat else None
     saved, codes, exps = Checkpoint8._like(x) if want_checkpoint else (None, None, None)
-    st = lib().spv_group_norm(_stream(), ws.ptr, ws.nbytes, xp, m, C, _addr(off), B, groups, gp, bp, eps, _ACT[act],
-                              _addr(out), _addr(stat), codes, exps, _DT[x.dtype])
+    st = lib().spv_group_norm(_stream_of(dev), ws.ptr, ws.nbytes, xp, m, C, _at(off, dev), B, groups, gp, bp, eps,
+                              _ACT[act], _at(out, dev), _at(stat, dev), codes, exps, _DT[x.dtype])
     _chk(st, "spv_group_norm")
     got = (out, *(t for t in (stat, saved) if t is not None))
     return got if len(got) > 1 else out
@@ -1002,26 +1046,28 @@ def spv_group_norm_backward(ws: Workspace, dy: torch.Tensor, x, off: torch.Tenso
     B = _scans(off)
     if act not in _ACT:
         raise ValueError(f"act must be one of {', '.join(_ACT)}")
+    dev = _here()
     codes = exps = xp = None
     if isinstance(x, Checkpoint8):
         if x.codes.shape != dy.shape or x.dtype != dy.dtype:
             raise ValueError("the checkpoint must have dy's shape and type")
-        codes, exps = x.addresses()
+        codes, exps = x.addresses(dev)
     else:
         if x.shape != dy.shape or x.dtype != dy.dtype:
             raise ValueError("x must have dy's shape and type")
-        xp = _addr(x)
+        xp = _at(x, dev)
     if dres is not None and (dres.shape != dy.shape or dres.dtype != dy.dtype):
         raise ValueError("dres must have dy's shape and type")
     if stat.dtype != torch.float32 or stat.shape != (B, groups, 2):
         raise ValueError(f"stat must be float32 [{B}][{groups}][2]")
-    gp, bp = _channels(gamma, C, "gamma"), _channels(beta, C, "beta")
+    dyp, offp, sp, rp = _at(dy, dev), _at(off, dev), _at(stat, dev), _at(dres, dev)
+    gp, bp = _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev)
     dx = torch.empty_like(dy)
     dgamma = dy.new_empty(C, dtype=torch.float32)
     dbeta = torch.empty_like(dgamma)
-    st = lib().spv_group_norm_backward(_stream(), ws.ptr, ws.nbytes, _addr(dy), xp, codes, exps, m, C, _addr(off), B,
-                                       groups, gp, bp, _addr(stat), _ACT[act], _addr(dres), dx.data_ptr(),
-                                       dgamma.data_ptr(), dbeta.data_ptr(), _DT[dy.dtype])
+    st = lib().spv_group_norm_backward(_stream_of(dev), ws.ptr, ws.nbytes, dyp, xp, codes, exps, m, C, offp, B, groups, gp,
+                                       bp, sp, _ACT[act], rp, dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(),
+                                       _DT[dy.dtype])
     _chk(st, "spv_group_norm_backward")
     return dx, dgamma, dbeta
 

@@ -143,7 +143,7 @@ def test_rows_of_no_scan_and_offsets_past_the_ends(spv):
         saved.codes.fill_(3)
         saved.exps.fill_(9)
         st = spv.lib().spv_group_norm(spv._stream(), ws.ptr, ws.nbytes, spv._ptr(x), m, C, spv._ptr(off), 3, G, None, None, 1e-5,
-                                      0, spv._ptr(y), None, *saved.addresses(), 1)
+                                      0, spv._ptr(y), None, *saved.addresses(0), 1)
         assert st == 0 and bool((saved.codes[:37] == 3).all()) and bool((saved.exps[460:] == 9).all())
         wide = torch.tensor([-50, 100, 100, 10 ** 6], dtype=torch.int32, device="cuda")
         check(spv, x, dy, res, g, b, wide, G, "relu", False, "bf16")

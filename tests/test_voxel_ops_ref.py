@@ -164,7 +164,7 @@ def test_group_norm_refusals():
 
 def test_binding_refusals(monkeypatch):
     """Shapes and types that the calls would read past."""
-    monkeypatch.setattr(spv, "_addr", lambda t: None if t is None else t.data_ptr())
+    monkeypatch.setattr(spv, "_here", lambda: -1)  # where the tensors of the CPU are
     monkeypatch.setattr(spv, "lib", lambda: (_ for _ in ()).throw(AssertionError("a call was made")))
     ws = type("W", (), dict(ptr=None, nbytes=0))()
     BF = torch.bfloat16
@@ -194,3 +194,19 @@ def test_binding_refusals(monkeypatch):
                dict(dres=x[:5]), dict(act="tanh")):
         with pytest.raises(ValueError):
             spv.spv_group_norm_backward(ws, x, kw.pop("x", x), off, 4, kw.pop("stat", stat), **kw)
+
+
+def test_tensors_of_another_device(monkeypatch):
+    """A call runs on the current device's stream; tensors of another one are refused before it."""
+    monkeypatch.setattr(spv, "_here", lambda: 0)
+    monkeypatch.setattr(spv, "lib", lambda: (_ for _ in ()).throw(AssertionError("a call was made")))
+    ws = type("W", (), dict(ptr=None, nbytes=0))()
+    x, off, c = torch.zeros(6, 64), torch.tensor([0, 6], dtype=torch.int32), torch.zeros(6, 4, dtype=torch.int32)
+    saved, p = spv.Checkpoint8.empty(6, 64, torch.float32, "cpu"), spv.RopeParams(32)
+    p._keep = torch.ones(16)
+    for f in (lambda: spv.spv_checkpoint8(x), lambda: spv.spv_checkpoint8_read(saved),
+              lambda: spv.spv_linear_backward8(ws, saved, x), lambda: spv.spv_group_norm(ws, x, off, 4),
+              lambda: spv.spv_group_norm_backward(ws, x, x, off, 4, torch.zeros(1, 4, 2)),
+              lambda: spv.spv_rope(p, c, x.view(6, 2, 32))):
+        with pytest.raises(ValueError, match="current device"):
+            f()
