@@ -166,3 +166,17 @@ def test_weight_gradient_rows_under_a_device_count_and_nan(spv, Cin, Cout):
     x[5, 3], da[613:] = float("inf"), 0.0
     got = spv.spv_linear_backward8(ws, spv.spv_checkpoint8(x), da)
     assert bool(torch.isnan(got[3]).all()) and bool(torch.isfinite(torch.cat([got[:3], got[4:]])).all())
+
+
+@pytest.mark.parametrize("dtype,e", [("f16", -18), ("f16", -24), ("bf16", -100), ("f32", -100)])
+@pytest.mark.parametrize("Cin,Cout", [(64, 32), (19, 33)])
+def test_weight_gradient_of_small_numbers(spv, Cin, Cout, dtype, e):
+    """Rows whose values are below a type's normal ones (float16's 2^-14) are multiplied as they are."""
+    m = 500
+    x = (features(m, Cin, "f32", 1) * 2.0 ** e).to(TD[dtype])
+    da = features(m, Cout, dtype, 2)
+    saved = spv.spv_checkpoint8(x)
+    same(spv, x, saved, dtype)
+    X, D = ref.codes(arr(x), dtype)[2], arr(da)
+    got = spv.spv_linear_backward8(spv.Workspace.for_linear_backward8(m, Cin, Cout), saved, da)
+    assert np.all(np.abs(arr(got) - X.T @ D) <= ref.wgrad_bound(X, D, X.T @ D) + ref.TINY["f32"])

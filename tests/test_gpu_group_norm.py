@@ -70,11 +70,15 @@ def check(spv, x, dy, res, g, b, off, G, act, ckpt, dtype):
 
 # lengths of the scans: one row, empty ones among them, many short ones, long ones
 LENS = {"one": [1], "mixed": [0, 1, 5, 300, 0, 33, 0], "even": [64, 64], "none": [0, 0], "short": [3, 1, 0, 2] * 60,
-        "long": [2777, 1, 1500]}
+        "long": [2777, 1, 1500], "crowd": [9, 0, 1, 4, 7] * 140, "many": [1, 0, 2, 1] * 1250, "six": [590, 10]}
 SHAPES = [(1, 1, "mixed"), (7, 7, "mixed"), (8, 1, "one"), (8, 8, "mixed"), (19, 1, "mixed"), (19, 19, "long"), (32, 4, "even"),
           (96, 8, "mixed"), (96, 96, "mixed"), (96, 1, "long"), (96, 8, "one"), (96, 8, "none"), (96, 8, "short"), (100, 4, "mixed"),
           (36, 4, "long"), (64, 2, "short"), (256, 16, "long"), (256, 256, "even"), (520, 8, "mixed"), (1030, 2, "even"),
-          (2049, 3, "one"), (2048, 32, "even"), (4096, 1, "even"), (5000, 5, "one"), (16, 16, "long")]
+          (2049, 3, "one"), (2048, 32, "even"), (4096, 1, "even"), (5000, 5, "one"), (16, 16, "long"),
+          # past what one launch takes: tiles joined by waves and by eights of lanes, by a launch of its own, searches over
+          # hundreds and thousands of scans, rows by elements and too wide for a workgroup
+          (96, 8, "crowd"), (96, 48, "crowd"), (96, 96, "crowd"), (51, 17, "crowd"), (51, 51, "crowd"), (32, 8, "many"),
+          (33, 3, "many"), (256, 256, "six"), (256, 1, "six"), (250, 125, "six"), (2049, 3, "even"), (1030, 515, "even")]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
