@@ -8,35 +8,56 @@ namespace spv {
 __device__ inline int64_t RowRange::begin() const { return off ? clamp_off(off[0], cap) : 0; }
 __device__ inline int64_t RowRange::end() const { return off ? clamp_off(off[B], cap) : clamp_rows(m_dev, cap); }
 
-// Half a wave takes a block of 32 channels of a row, a lane a channel: any width and alignment.
+constexpr int kCodeAhead = 4;  // loads a thread has on the way
+
+// Half a wave takes a block of 32 channels of kCodeAhead rows, a lane a channel: any width and alignment.
 template <int DT>
 __global__ __launch_bounds__(256) void k_code8_any(const void* x, Saved8 to, RowRange rows, int C) {
     const int nb = code_blocks(C), l = threadIdx.x & 31;
     const int64_t end = rows.end(), step = (int64_t)gridDim.x * 8;
-    for (int64_t i = rows.begin() + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < end; i += step)
+    for (int64_t i0 = rows.begin() + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i0 < end; i0 += kCodeAhead * step)
         for (int b = 0; b < nb; ++b) {
             const int c = b * kCodeBlock + l;
-            const float v = c < C ? ld_feat<DT>(x, i * C + c) : 0.f;
-            const int byte = code_exp<DT>(lanes_max<32>(finite_bits(v)));
-            if (c < C) to.codes[i * C + c] = (int8_t)code_of(v, code_rate(byte));
-            if (l == 0) to.exps[i * nb + b] = (uint8_t)byte;
+            float v[kCodeAhead];
+#pragma unroll
+            for (int k = 0; k < kCodeAhead; ++k) {
+                const int64_t i = i0 + k * step;
+                v[k] = c < C && i < end ? ld_feat<DT>(x, i * C + c) : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < kCodeAhead; ++k) {
+                const int64_t i = i0 + k * step;
+                const int byte = code_exp<DT>(lanes_max<32>(finite_bits(v[k])));
+                if (i >= end) break;
+                if (c < C) to.codes[i * C + c] = (int8_t)code_of(v[k], code_rate(byte));
+                if (l == 0) to.exps[i * nb + b] = (uint8_t)byte;
+            }
         }
 }
 template <int DT>
 __global__ __launch_bounds__(256) void k_code8_read_any(Saved8 from, void* out, RowRange rows, int C) {
     const int nb = code_blocks(C), l = threadIdx.x & 31;
     const int64_t end = rows.end(), step = (int64_t)gridDim.x * 8;
-    for (int64_t i = rows.begin() + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < end; i += step)
+    for (int64_t i0 = rows.begin() + (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i0 < end; i0 += kCodeAhead * step)
         for (int b = 0; b < nb; ++b) {
             const int c = b * kCodeBlock + l;
-            if (c < C) st_feat<DT>(out, i * C + c, code_value(from.codes[i * C + c], code_step(from.exps[i * nb + b])));
+            int q[kCodeAhead], e[kCodeAhead];
+#pragma unroll
+            for (int k = 0; k < kCodeAhead; ++k) {
+                const int64_t i = i0 + k * step;
+                const bool on = c < C && i < end;
+                q[k] = on ? from.codes[i * C + c] : 0;
+                e[k] = on ? from.exps[i * nb + b] : 1;
+            }
+#pragma unroll
+            for (int k = 0; k < kCodeAhead; ++k)
+                if (c < C && i0 + k * step < end) st_feat<DT>(out, (i0 + k * step) * C + c, code_value(q[k], code_step(e[k])));
         }
 }
 
 // Rows of whole blocks: the blocks of all rows are one after the other.  A thread takes 16 bytes of x, four times over.
 template <int DT>
 constexpr int kCodeVec = DT == SPV_F32 ? 4 : 8;
-constexpr int kCodeAhead = 4;
 
 template <int DT>
 __global__ __launch_bounds__(256) void k_code8(const void* x, Saved8 to, RowRange rows, int C) {
@@ -85,12 +106,66 @@ __global__ __launch_bounds__(256) void k_code8_read(Saved8 from, void* out, RowR
     }
 }
 
+// Rows of whole vectors whose last block is shorter: a row is nb blocks of LANES threads, those past its end idle, and a
+// workgroup takes 256 / (nb LANES) rows at a time, kCodeAhead times over.
 template <int DT>
-static bool code8_wide(const void* x, const Saved8& s, int C) {
-    return C % kCodeBlock == 0 && (uintptr_t)x % 16 == 0 && (uintptr_t)s.codes % kCodeVec<DT> == 0;
+__global__ __launch_bounds__(256) void k_code8_short(const void* x, Saved8 to, RowRange rows, int C) {
+    constexpr int V = kCodeVec<DT>, LANES = kCodeBlock / V;
+    const int nb = code_blocks(C), per = nb * LANES, R = 256 / per, row = (int)threadIdx.x / per, v = (int)threadIdx.x - row * per;
+    if (row >= R) return;  // whole blocks
+    const int64_t end = rows.end(), i0 = rows.begin() + (int64_t)blockIdx.x * (R * kCodeAhead) + row;
+    const bool on = v * V < C;
+    uint4 u[kCodeAhead];
+#pragma unroll
+    for (int k = 0; k < kCodeAhead; ++k) {
+        const int64_t i = i0 + k * R;
+        u[k] = on && i < end ? *(const uint4*)((const char*)x + (i * C + v * V) * (16 / V)) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < kCodeAhead; ++k) {
+        const int64_t i = i0 + k * R;
+        float f[V];
+        uint32_t w[V / 4];
+        unpack16<DT>(u[k], f);
+        const int byte = code_block<DT, V, LANES>(f, w);
+        if (i >= end) break;
+        if (on) __builtin_memcpy(__builtin_assume_aligned(to.codes + i * C + v * V, V), w, V);
+        if (v % LANES == 0) to.exps[i * nb + v / LANES] = (uint8_t)byte;
+    }
+}
+template <int DT>
+__global__ __launch_bounds__(256) void k_code8_read_short(Saved8 from, void* out, RowRange rows, int C) {
+    constexpr int V = kCodeVec<DT>, LANES = kCodeBlock / V;
+    const int nb = code_blocks(C), per = C / V, R = 256 / per, row = (int)threadIdx.x / per, v = (int)threadIdx.x - row * per;
+    const int64_t end = rows.end(), i0 = (int64_t)blockIdx.x * (R * kCodeAhead) + row;
+    uint32_t w[kCodeAhead][V / 4];
+    int e[kCodeAhead];
+#pragma unroll
+    for (int k = 0; k < kCodeAhead; ++k) {
+        const int64_t i = i0 + k * R;
+        if (row >= R || i >= end) continue;
+        __builtin_memcpy(w[k], __builtin_assume_aligned(from.codes + i * C + v * V, V), V);
+        e[k] = from.exps[i * nb + v / LANES];
+    }
+#pragma unroll
+    for (int k = 0; k < kCodeAhead; ++k) {
+        const int64_t i = i0 + k * R;
+        if (row >= R || i >= end) break;
+        float f[V];
+        code_values(w[k], code_step(e[k]), f);
+        *(uint4*)((char*)out + (i * C + v * V) * (16 / V)) = pack16<DT>(f);
+    }
+}
+
+// vectors of rows that are aligned and hold whole ones: 2 where blocks are whole too, 1 where a row's threads fit a workgroup
+template <int DT>
+static int code8_vectors(const void* x, const Saved8& s, const RowRange& rows, int C) {
+    constexpr int V = kCodeVec<DT>;
+    if (C % V || (uintptr_t)x % 16 || (uintptr_t)s.codes % V || rows.cap * C >= ((int64_t)1 << 40)) return 0;
+    return C % kCodeBlock == 0 ? 2 : code_blocks(C) * (kCodeBlock / V) <= 256 ? 1 : 0;
 }
 static unsigned grid_rows(int64_t m) {
-    const int64_t g = (m + 7) / 8;
+    const int64_t g = (m + 8 * kCodeAhead - 1) / (8 * kCodeAhead);
     return (unsigned)(g < 1 ? 1 : g > 16384 ? 16384 : g);
 }
 template <int DT>
@@ -98,19 +173,24 @@ static unsigned grid_vecs(int64_t m, int C) {
     const int64_t per = 256 * kCodeAhead;
     return (unsigned)((m * (C / kCodeVec<DT>) + per - 1) / per);
 }
+static unsigned grid_short(int64_t m, int threads) {
+    const int64_t rows = 256 / threads * kCodeAhead;
+    return (unsigned)((m + rows - 1) / rows);
+}
 template <int DT>
 static void code8(hipStream_t s, const void* x, const Saved8& to, const RowRange& rows, int C) {
-    if (code8_wide<DT>(x, to, C) && rows.cap * C < ((int64_t)1 << 40))
-        k_code8<DT><<<grid_vecs<DT>(rows.cap, C), 256, 0, s>>>(x, to, rows, C);
-    else
-        k_code8_any<DT><<<grid_rows(rows.cap), 256, 0, s>>>(x, to, rows, C);
+    const int v = code8_vectors<DT>(x, to, rows, C);
+    if (v == 2) k_code8<DT><<<grid_vecs<DT>(rows.cap, C), 256, 0, s>>>(x, to, rows, C);
+    else if (v == 1)
+        k_code8_short<DT><<<grid_short(rows.cap, code_blocks(C) * (kCodeBlock / kCodeVec<DT>)), 256, 0, s>>>(x, to, rows, C);
+    else k_code8_any<DT><<<grid_rows(rows.cap), 256, 0, s>>>(x, to, rows, C);
 }
 template <int DT>
 static void code8_read(hipStream_t s, const Saved8& from, void* out, const RowRange& rows, int C) {
-    if (code8_wide<DT>(out, from, C) && rows.cap * C < ((int64_t)1 << 40))
-        k_code8_read<DT><<<grid_vecs<DT>(rows.cap, C), 256, 0, s>>>(from, out, rows, C);
-    else
-        k_code8_read_any<DT><<<grid_rows(rows.cap), 256, 0, s>>>(from, out, rows, C);
+    const int v = code8_vectors<DT>(out, from, rows, C);
+    if (v == 2) k_code8_read<DT><<<grid_vecs<DT>(rows.cap, C), 256, 0, s>>>(from, out, rows, C);
+    else if (v == 1) k_code8_read_short<DT><<<grid_short(rows.cap, C / kCodeVec<DT>), 256, 0, s>>>(from, out, rows, C);
+    else k_code8_read_any<DT><<<grid_rows(rows.cap), 256, 0, s>>>(from, out, rows, C);
 }
 void launch_checkpoint8(hipStream_t s, const void* x, Saved8 to, const RowRange& rows, int C, int dt) {
     if (dt == SPV_F32) code8<SPV_F32>(s, x, to, rows, C);

@@ -212,6 +212,9 @@ __device__ inline void gn_join_all(const GnArgs& a, const GnTile& t, uint32_t ti
     }
 }
 
+// rows a thread asks for at a time: more of single channels, which are 2 or 4 bytes each
+constexpr int gn_ahead(int vec, int rows) { return vec == 1 ? 4 * rows : rows; }
+
 // A thread's rows of a tile (row, row + R, ..), U at a time, the next U asked for before the present ones are used.
 // ask() comes before whatever the first rows can be waited for during.  A row past the end is asked for as row 0.
 template <int U, class Raw>
@@ -293,9 +296,10 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_
         for (int e = 0; e < VEC; ++e) mean[e] = sq[e] = 0.f;
         const int64_t base = t.row0 * a.C + c;
         auto load = [&](int i) { return V::load(a.x, base + (int64_t)i * a.C); };
-        GnRows<4, typename V::Raw> rows{row, R, t.rows};
+        constexpr int U = gn_ahead(VEC, 4);
+        GnRows<U, typename V::Raw> rows{row, R, t.rows};
         rows.ask(row, rows.u, load);
-        rows.run(load, [&](int i0, const typename V::Raw(&u)[4]) {
+        auto four = [&](int i0, const typename V::Raw* u) {
             float x[4][VEC];
 #pragma unroll
             for (int k = 0; k < 4; ++k) V::unpack(u[k], x[k]);
@@ -328,6 +332,10 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_
                     sq[e] = fmaf(d, x[k][e] - mean[e], sq[e]);
                 }
             }
+        };
+        rows.run(load, [&](int i0, const typename V::Raw(&u)[U]) {
+#pragma unroll
+            for (int k = 0; k < U; k += 4) four(i0 + k * R, u + k);
         });
         // equal counts: units of two, four and eight channels, while a group is made of those
 #pragma unroll
@@ -365,7 +373,8 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_apply(GnArgs a, int tile
     gn_channels<VEC>(a.beta, c, 0.f, be);
     const int64_t base = t.row0 * a.C + c;
     auto load = [&](int i) { return V::load(a.x, base + (int64_t)i * a.C); };
-    GnRows<4, typename V::Raw> rows{row, R, row < R ? t.rows : 0};
+    constexpr int U = gn_ahead(VEC, 4);
+    GnRows<U, typename V::Raw> rows{row, R, row < R ? t.rows : 0};
     if (rows.rows) rows.ask(row, rows.u, load);
     const int w = a.C / a.G;
     gn_join_all(a, t, tile_rows, first, s_stat, [&](GnGroup& g) { return gn_join_stat(g, t.n, tile_rows, w, a.eps); });
@@ -380,9 +389,9 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_apply(GnArgs a, int tile
         mu[e] = st.x;
         ga[e] *= st.y;
     }
-    rows.run(load, [&](int i0, const typename V::Raw(&u)[4]) {
+    rows.run(load, [&](int i0, const typename V::Raw(&u)[U]) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < U; ++k) {
             if (i0 + k * R >= t.rows) break;
             const int64_t e = base + (int64_t)(i0 + k * R) * a.C;
             float x[VEC], y[VEC];
@@ -462,16 +471,17 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
         float mu[VEC], r[VEC], ga[VEC], be[VEC], s1[VEC], s2[VEC];
         const int64_t base = t.row0 * a.C + c, block = t.row0 * code_blocks(a.C) + c / kCodeBlock;
         auto load = [&](int i) { return S::load(a, base, block, i); };
-        GnRows<2, typename S::Raw> rows{row, R, t.rows};
+        constexpr int U = gn_ahead(VEC, 2);
+        GnRows<U, typename S::Raw> rows{row, R, t.rows};
         gn_channels<VEC>(a.gamma, c, 1.f, ga);
         gn_channels<VEC>(a.beta, c, 0.f, be);
         gn_stat<VEC>(a, t.b, c, w, mu, r);
         rows.ask(row, rows.u, load);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) s1[e] = s2[e] = 0.f;
-        rows.run(load, [&](int i0, const typename S::Raw(&u)[2]) {
+        rows.run(load, [&](int i0, const typename S::Raw(&u)[U]) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < U; ++k) {
                 if (i0 + k * R >= t.rows) break;
                 float x[VEC], d[VEC];
                 V::unpack(u[k].dy, d);
@@ -570,7 +580,8 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
         if (a.dres) r.res = V::load(a.dres, base + (int64_t)i * a.C);
         return r;
     };
-    GnRows<2, typename S::RawRes> rows{row, R, row < R ? t.rows : 0};
+    constexpr int U = gn_ahead(VEC, 2);
+    GnRows<U, typename S::RawRes> rows{row, R, row < R ? t.rows : 0};
     const int w = a.C / a.G;
     float mu[VEC], r[VEC], ga[VEC], be[VEC], m1[VEC], m2[VEC];
     gn_channels<VEC>(a.gamma, c, 1.f, ga);
@@ -586,9 +597,9 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
         m1[e] = me.x;
         m2[e] = me.y;
     }
-    rows.run(load, [&](int i0, const typename S::RawRes(&u)[2]) {
+    rows.run(load, [&](int i0, const typename S::RawRes(&u)[U]) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < U; ++k) {
             if (i0 + k * R >= t.rows) break;
             float x[VEC], d[VEC], q[VEC] = {};
             V::unpack(u[k].dy, d);
