@@ -31,7 +31,7 @@ __device__ inline float act_grad(float d, float z) {
         return z <= 0.f ? 0.f : d;
     } else if constexpr (ACT == SPV_ACT_SILU) {
         const float s = sigmoid(z);
-        return d * (s * fmaf(z, 1.f - s, 1.f));
+        return d * fmaf(s, fmaf(-z, s, z), s);  // s (1 + z (1 - s))
     } else {
         return d;
     }
@@ -438,7 +438,7 @@ struct GnSource {
     }
 };
 
-// mean and r of a thread's channels
+// r and -mean r of a thread's channels, so that xh is one fma (off by a rounding of mean r, as by one of the mean)
 template <int VEC>
 __device__ inline void gn_stat(const GnArgs& a, int b, int c, int w, float (&mu)[VEC], float (&r)[VEC]) {
     const float2* st = (const float2*)a.stat + (int64_t)b * a.G;
@@ -450,7 +450,7 @@ __device__ inline void gn_stat(const GnArgs& a, int b, int c, int w, float (&mu)
         if (--left == 0 && g + 1 < a.G) ++g, left = w;
     }
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) mu[e] = v[e].x, r[e] = v[e].y;
+    for (int e = 0; e < VEC; ++e) r[e] = v[e].y, mu[e] = -v[e].x * v[e].y;
 }
 
 // a tile's sums of gz and gz xh, of each channel and (times gamma) of each group
@@ -488,7 +488,7 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
                 S::unpack(u[k].x, x);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const float xh = (x[e] - mu[e]) * r[e], gz = act_grad<ACT>(d[e], fmaf(xh, ga[e], be[e]));
+                    const float xh = fmaf(x[e], r[e], mu[e]), gz = act_grad<ACT>(d[e], fmaf(xh, ga[e], be[e]));
                     s1[e] += gz;
                     s2[e] = fmaf(gz, xh, s2[e]);
                 }
@@ -533,11 +533,12 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
     }
 }
 
-// dbeta and dgamma: 16 of the 2 C columns of the tiles' sums a workgroup, in 32 runs of consecutive tiles, in 64 bits
+// dbeta and dgamma: 16 of the 2 C columns of the tiles' sums a workgroup, in runs of consecutive tiles, in 64 bits
 __device__ inline void gn_join_channels(const GnArgs& a, int64_t tiles, int which) {
-    __shared__ double red[32][17];
+    constexpr int RUNS = kGnThreads / 16;
+    __shared__ double red[RUNS][17];
     const int col = threadIdx.x & 15, run = threadIdx.x >> 4, j = which * 16 + col;
-    const int64_t len = (tiles + 31) / 32, t0 = run * len, t1 = t0 + len < tiles ? t0 + len : tiles;
+    const int64_t len = (tiles + RUNS - 1) / RUNS, t0 = run * len, t1 = t0 + len < tiles ? t0 + len : tiles;
     double s = 0.0;
     if (j < 2 * a.C)
         for (int64_t t = t0; t < t1; t += 8) {
@@ -550,7 +551,7 @@ __device__ inline void gn_join_channels(const GnArgs& a, int64_t tiles, int whic
     red[run][col] = s;
     __syncthreads();
     if (run || j >= 2 * a.C) return;
-    for (int k = 1; k < 32; ++k) s += red[k][col];
+    for (int k = 1; k < RUNS; ++k) s += red[k][col];
     float* out = j < a.C ? a.dbeta : a.dgamma;
     if (out) out[j < a.C ? j : j - a.C] = (float)s;
 }
@@ -607,9 +608,9 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
             if (a.dres) V::unpack(u[k].res, q);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const float xh = (x[e] - mu[e]) * r[e];
+                const float xh = fmaf(x[e], r[e], mu[e]);
                 const float h = act_grad<ACT>(d[e], fmaf(xh, ga[e], be[e])) * ga[e];
-                d[e] = fmaf(r[e], h - m1[e] - xh * m2[e], q[e]);
+                d[e] = fmaf(r[e], fmaf(-xh, m2[e], h - m1[e]), q[e]);
             }
             V::store(a.dx, base + (int64_t)(i0 + k * R) * a.C, d);
         }
@@ -620,6 +621,7 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
 // Few rows: a workgroup takes a group of a scan, all of it in its threads' registers: the mean, the deviations from it and
 // the output in one launch.
 // ---------------------------------------------------------------------------
+constexpr int kGnFewThreads = 512;
 constexpr int kGnHeld = 24;  // values a thread holds
 // values in all up to which that is done: 701 x 96 in float32 takes 6.9 us with 8 groups (8.2 in tiles), in bf16 with 96 groups 4.5
 // (13.8); 8000 x 32 with 32 groups, whose rows are then read 4 bytes at a time, 14.4 (10.0)
@@ -631,13 +633,13 @@ __device__ inline float block_sum(float v, float* red) {
     __syncthreads();
     float s = red[0];
 #pragma unroll
-    for (int w = 1; w < kGnWaves; ++w) s += red[w];
+    for (int w = 1; w < kGnFewThreads / 64; ++w) s += red[w];
     return s;
 }
 
 template <int DT, int ACT>
-__global__ __launch_bounds__(kGnThreads) void k_gn_few(GnArgs a, uint32_t by_w) {
-    __shared__ float red[2][kGnWaves];
+__global__ __launch_bounds__(kGnFewThreads) void k_gn_few(GnArgs a, uint32_t by_w) {
+    __shared__ float red[2][kGnFewThreads / 64];
     const int b = (int)(blockIdx.x / (unsigned)a.G), g = (int)(blockIdx.x % (unsigned)a.G), w = a.C / a.G;
     const int64_t r0 = clamp_off(a.off[b], a.m), r1 = clamp_off(a.off[b + 1], a.m);
     const int n = r1 > r0 ? (int)(r1 - r0) * w : 0;
@@ -648,23 +650,23 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_few(GnArgs a, uint32_t by_w) 
     const int64_t base = r0 * a.C + g * w;
     const float first = ld_feat<DT>(a.x, base);  // equal values give their mean exactly
     float x[kGnHeld];
-    int at[kGnHeld], c[kGnHeld];  // from the group's first value: rows * C is at most kGnHeld kGnThreads G
+    int at[kGnHeld], c[kGnHeld];  // from the group's first value: rows * C is at most kGnHeld kGnFewThreads G
     float s = 0.f, q = 0.f;
 #pragma unroll
     for (int k = 0; k < kGnHeld; ++k) {
-        if (k * kGnThreads >= n) break;
-        const int t = (int)threadIdx.x + k * kGnThreads, i = t < n ? t : 0, r = by_w ? (int)__umulhi((uint32_t)i, by_w) : i;
+        if (k * kGnFewThreads >= n) break;
+        const int t = (int)threadIdx.x + k * kGnFewThreads, i = t < n ? t : 0, r = by_w ? (int)__umulhi((uint32_t)i, by_w) : i;
         c[k] = i - r * w;
         at[k] = r * a.C + c[k];
         x[k] = ld_feat<DT>(a.x, base + at[k]);
     }
 #pragma unroll
     for (int k = 0; k < kGnHeld; ++k)
-        if ((int)threadIdx.x + k * kGnThreads < n) s += x[k] - first;
+        if ((int)threadIdx.x + k * kGnFewThreads < n) s += x[k] - first;
     const float mu = first + block_sum(s, red[0]) / (float)n;
 #pragma unroll
     for (int k = 0; k < kGnHeld; ++k) {
-        if ((int)threadIdx.x + k * kGnThreads >= n) break;
+        if ((int)threadIdx.x + k * kGnFewThreads >= n) break;
         x[k] -= mu;
         q = fmaf(x[k], x[k], q);
     }
@@ -672,7 +674,7 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_few(GnArgs a, uint32_t by_w) 
     if (threadIdx.x == 0 && a.stat) ((float2*)a.stat)[blockIdx.x] = make_float2(mu, rd);
 #pragma unroll
     for (int k = 0; k < kGnHeld; ++k)
-        if ((int)threadIdx.x + k * kGnThreads < n)
+        if ((int)threadIdx.x + k * kGnFewThreads < n)
             st_feat<DT>(a.out, base + at[k],
                         act_of<ACT>(fmaf(x[k] * rd, a.gamma ? a.gamma[g * w + c[k]] : 1.f, a.beta ? a.beta[g * w + c[k]] : 0.f)));
 }
@@ -836,7 +838,7 @@ static bool gn_join_apart(const GnArgs& a) { return !gn_few_tiles(a) && a.G > 4 
 // All groups of all scans fit a workgroup's registers each (no scan has more than m rows), and there are few values: rows are
 // read a group's channels at a time.  (Whether codes are asked for makes no difference to the other outputs.)
 static bool gn_few(const GnArgs& a) {
-    return a.m * (a.C / a.G) <= (int64_t)kGnHeld * kGnThreads && a.m * a.C <= kGnFew && (int64_t)a.B * a.G <= 4096;
+    return a.m * (a.C / a.G) <= (int64_t)kGnHeld * kGnFewThreads && a.m * a.C <= kGnFew && (int64_t)a.B * a.G <= 4096;
 }
 
 static void gn_ws(Arena& a, GnArgs& t) {
@@ -883,7 +885,7 @@ void launch_group_norm(hipStream_t s, const GnArgs& given) {
         if (gn_few(a)) {
             const int w = a.C / a.G;
             const uint32_t by = w > 1 ? (uint32_t)((((uint64_t)1 << 32) + (uint64_t)w - 1) / (uint64_t)w) : 0u;
-            k_gn_few<DT, ACT><<<(unsigned)(a.B * a.G), kGnThreads, 0, s>>>(a, by);
+            k_gn_few<DT, ACT><<<(unsigned)(a.B * a.G), kGnFewThreads, 0, s>>>(a, by);
             return;
         }
         if constexpr (VEC == 0) {
