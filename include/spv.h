@@ -681,7 +681,7 @@ spv_status spv_attention_backward(void* stream, void* ws, size_t ws_bytes, const
  * stand to each other, along x, y and z apart. */
 typedef struct spv_rope_params {
     int32_t D;           /* channels of a head: a multiple of 8 in 8 .. 128 */
-    int32_t sections[3]; /* pairs that turn with x, with y and with z, in this order; >= 0, P = their sum in 1 .. D / 2 */
+    int32_t sections[3]; /* pairs that turn with x, y and z, in this order; >= 0, P (their sum) in 1 .. D / 2 */
     int32_t halves;      /* pair p is channels (2 p, 2 p + 1); nonzero: (p, p + P) */
     const float* freqs;  /* [P] f32, device: radians a voxel */
 } spv_rope_params;
@@ -692,8 +692,8 @@ typedef struct spv_rope_params {
  *   (u, w) -> (u cos theta - w sin theta, u sin theta + w cos theta);
  * channels past 2 P stay as they are.  inverse: by -theta, which is the backward
  * (gradients of the rotated rows in, of the rows out).  theta is reduced to an
- * eighth of a turn in float64 (off by 2^-51 |theta| at most), sine and cosine and the rotation are float32,
- * one rounding to dt.
+ * eighth of a turn in float64 (off by 2^-51 |theta| at most); sine, cosine and the
+ * rotation are float32, with one rounding to dt.
  * In:  coords [n][4] i32 (b, x, y, z), 16-byte aligned (outside the voxel range: its
  *      nearest end); m_dev: device row count (NULL = n); q [n][ldq] with H heads, k
  *      [n][ldk] with Hkv heads or NULL (Hkv = 0), rows strided and 16-byte aligned as
@@ -713,9 +713,9 @@ spv_status spv_rope(void* stream, const spv_rope_params* p, const int32_t* coord
  *   code = x 2^-E to the nearest whole number (ties to even), in -127 .. 127;
  *   what is read back is code * 2^E, exact in the type it came from.
  * The maximum is over the block's finite values; a value that is not finite has code
- * -128 and reads as NaN.  A value is off by 2^E / 2 at most, by 2^E above 127.5 2^E:
- * at most 2^-6 of the block's largest.  E0 is where 2^E and 127 * 2^E stop being
- * exact in the type: smaller values fade out. */
+ * -128 and reads as NaN.  A value is off by 2^E / 2 at most, above 127.5 2^E by less
+ * than 2^E: by 2^-7 of the block's largest.  E0 is where 2^E stops being exact in
+ * the type: smaller values fade out. */
 #define SPV_CHECKPOINT8_BLOCK 32
 
 /*
@@ -724,9 +724,9 @@ spv_status spv_rope(void* stream, const spv_rope_params* p, const int32_t* coord
  * Out: codes [m_cap][C] i8, exps [m_cap][ceil(C / 32)] u8 (rows < count).
  * spv_checkpoint8_read -- back: out [m_cap][C], in the type dt that they came from (a
  * code that is too large for another type is infinite in it).
- * Any width; 16-byte aligned rows of a multiple of 8 channels are moved in wide
- * accesses.  No workspace.
- * Errors: SPV_ERR_INVALID_ARG (null pointers, sizes, x = out of another kind).
+ * Any width and alignment; aligned rows (x and out 16 bytes, codes 8) of a multiple of
+ * 8 channels (f32: 4) are moved 16 bytes at a time.  No workspace.
+ * Errors: SPV_ERR_INVALID_ARG (null pointers, sizes, aliasing).
  */
 spv_status spv_checkpoint8(void* stream, const void* x, const int64_t* m_dev, int64_t m_cap, int32_t C,
                            int8_t* codes, uint8_t* exps, spv_dtype dt);
@@ -737,9 +737,11 @@ spv_status spv_checkpoint8_read(void* stream, const int8_t* codes, const uint8_t
  * spv_linear_backward8 -- the weight gradient of a linear layer whose input rows were
  * kept in 8 bits (spv_linear_backward's dW, from codes):
  *   dW = in^T @ da (float32),  in = what spv_checkpoint8_read gives.
- * 16-bit types run on matrix cores, to which the rows' values and da go as they are
- * (both exact in the type), float32 on those for float32; sums are float32 over a workgroup's
- * rows, and the workgroups' are added in fp64 in a fixed order: the same bits on every call.
+ * 16-byte aligned codes and da of 16-bit types with Cin a multiple of 16 and Cout of 8
+ * run on those types' matrix cores, to which the rows' values and da go as they are
+ * (both exact in the type), float32 and the others on those for float32; sums are
+ * float32 over a workgroup's rows, and the workgroups' are added in fp64 in a fixed
+ * order: the same bits on every call.
  * In:  codes [m_cap][Cin], exps [m_cap][ceil(Cin / 32)]; m_dev: device row count
  *      (NULL = m_cap); da [m_cap][Cout] (dt).
  * Out: dW [Cin][Cout] f32, all of it (0 without rows).
@@ -762,9 +764,12 @@ typedef enum spv_act {
  * scan b (off[b] .. off[b+1] - 1) and the C / G channels of group g together,
  *   out = act((x - mu_bg) * r_bg * gamma[c] + beta[c]),
  *   mu = mean x,  r = 1 / sqrt(mean (x - mu)^2 + eps)
- * float32, with deviations from the rows' own running mean (no cancellation where a
- * scan sits far from zero), joined in fp64; one rounding to dt.  G = 1: one mean a
- * scan; G = C: one a scan and channel; off = {0, m}: all rows together.
+ * float32, with deviations from the rows' own mean (no cancellation where a scan sits
+ * far from zero), joined in fp64; one rounding to dt.  G = 1: one mean a scan; G = C:
+ * one a scan and channel; off = {0, m}: all rows together.  Equal values give
+ * act(beta).  Any width and alignment; 16-byte aligned rows of a multiple of 8
+ * channels (f32: 4), up to 4096 (f32: 2048), are moved 16 bytes at a time, up to 512
+ * others by elements; wider ones take plain kernels.
  * In:  x [m][C] (dt); off [B + 1] i32 device, ascending (clamped to [0, m]); gamma,
  *      beta [C] f32 or NULL (1, 0); eps > 0, finite; C a multiple of G.
  * Out: out [m][C] (dt; may be x), rows of no scan not written; stat [B][G][2] f32 or
@@ -778,8 +783,9 @@ typedef enum spv_act {
  * h = gz gamma and means over a scan's rows and a group's channels:
  *   dx = r (h - mean h - xh mean(h xh)) (+ dres),  dgamma[c] = sum gz xh,  dbeta[c] = sum gz
  * mu and r are the forward's (stat); x is given as it was, or in 8 bits (codes and
- * exps, x NULL), which is what the rows' values then are everywhere above.  Float32 sums of a workgroup's rows,
- * added in fp64 in a fixed order: the same bits on every call.
+ * exps, x NULL), which is what the rows' values then are everywhere above.  Float32
+ * sums of a workgroup's rows, added in fp64 in a fixed order: the same bits on every
+ * call.
  * In:  dy, dres (or NULL) [m][C] (dt).
  * Out: dx [m][C] (dt; may be dy or dres; rows of no scan not written), dgamma, dbeta
  *      [C] f32 (0 without rows); any may be NULL.

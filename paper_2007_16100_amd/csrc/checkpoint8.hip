@@ -55,7 +55,8 @@ __global__ __launch_bounds__(256) void k_code8_read_any(Saved8 from, void* out, 
         }
 }
 
-// Rows of whole blocks: the blocks of all rows are one after the other.  A thread takes 16 bytes of x, four times over.
+// Rows of whole blocks: the blocks of all rows are one after the other.  A thread takes 16 bytes of x, four times
+// over.  Bound by memory: 300,007 x 96 in bf16, 57.6 MB and 29.7, take 14.8 us into codes and 14.1 back.
 template <int DT>
 constexpr int kCodeVec = DT == SPV_F32 ? 4 : 8;
 
@@ -106,8 +107,8 @@ __global__ __launch_bounds__(256) void k_code8_read(Saved8 from, void* out, RowR
     }
 }
 
-// Rows of whole vectors whose last block is shorter: a row is nb blocks of LANES threads, those past its end idle, and a
-// workgroup takes 256 / (nb LANES) rows at a time, kCodeAhead times over.
+// Rows of whole vectors whose last block is shorter: a row is nb blocks of LANES threads, those past its end idle,
+// and a workgroup takes 256 / (nb LANES) rows at a time, kCodeAhead times over.
 template <int DT>
 __global__ __launch_bounds__(256) void k_code8_short(const void* x, Saved8 to, RowRange rows, int C) {
     constexpr int V = kCodeVec<DT>, LANES = kCodeBlock / V;
@@ -157,7 +158,8 @@ __global__ __launch_bounds__(256) void k_code8_read_short(Saved8 from, void* out
     }
 }
 
-// vectors of rows that are aligned and hold whole ones: 2 where blocks are whole too, 1 where a row's threads fit a workgroup
+// vectors of rows that are aligned and hold whole ones: 2 where blocks are whole too, 1 where a row's threads fit a
+// workgroup
 template <int DT>
 static int code8_vectors(const void* x, const Saved8& s, const RowRange& rows, int C) {
     constexpr int V = kCodeVec<DT>;
@@ -204,13 +206,19 @@ void launch_checkpoint8_read(hipStream_t s, Saved8 from, void* out, const RowRan
 }
 
 // ---------------------------------------------------------------------------
-// dW = in^T da.  A workgroup takes TM x TN tiles of 32 x 32 of dW and a share of the rows, its waves some of those each,
-// with nothing between them but the sum at the end.  The shares' sums go to the workspace and are joined in 64 bits.
+// dW = in^T da.  A workgroup takes TM x TN tiles of 32 x 32 of dW and a share of the rows, its waves some of those
+// each, with nothing between them but the sum at the end.  The shares' sums go to the workspace and are joined in 64
+// bits. 88,119 x 96 -> 96 in bf16: 12.7 us and 5.0 for the join; 26,881 x 256 -> 256 in f16: 15.0 and 4.6 (matrix
+// cores busy 12% of the time, vector units 43%: a code takes four steps to become a value, in each of the four
+// columns of blocks that read it).
 // ---------------------------------------------------------------------------
 constexpr int kWg8Step = 32;     // rows of a wave's step
 constexpr int kWg8Most = 3;      // tiles of a side of a workgroup's block
-constexpr int kWg8Groups = 256;  // workgroups, as far as the rows go
-// waves of a workgroup: as many as the registers allow, for what they have on the way from memory
+// Workgroups, as far as the rows go: one a CU.  Each leaves a share of dW (88,119 x 96 -> 96 with the codes' making
+// takes 24.9 us with 128 shares, 23.6 with 256, 31.8 with 512; 26,881 x 256 -> 256 31.3, 24.9, 29.5).
+constexpr int kWg8Groups = 256;
+// waves of a workgroup: eight where a wave's sums leave room for two on a SIMD (26,881 x 256 -> 256 32 -> 28 us with
+// four tiles; nine tiles, 144 registers of sums, 23.8 -> 28.4)
 constexpr int wg8_waves(int tiles) { return tiles <= 4 ? 8 : 4; }
 
 // tiles of a side: the fewest padded, then the most
@@ -261,13 +269,13 @@ __device__ inline Wg8Block wg8_block(const Wgrad8Args& a, int parts) {
     return b;
 }
 
-// A tile of 32 x 32 as it lies in LDS and in the workspace: column c's 32 rows one after the other, four rows (q of eight) at
-// place q ^ (c / 2) % 8, so that the lanes of a wave, a column each, meet in no bank.
+// A tile of 32 x 32 as it lies in LDS and in the workspace: column c's 32 rows one after the other, four rows (q of
+// eight) at place q ^ (c / 2) % 8, so that the lanes of a wave, a column each, meet in no bank.
 __device__ inline int wg8_place(int c, int q) { return c * 32 + 4 * (q ^ ((c >> 1) & 7)); }
 
-// The waves' sums of a block, added up in LDS, and then to the share's part of the workspace.  Four waves share an image of
-// the block; in each of four rounds a wave adds every fourth tile, another wave's next: the order of a tile's sum is the same
-// on every call.
+// The waves' sums of a block, added up in LDS, and then to the share's part of the workspace.  Four waves share an
+// image of the block; in each of four rounds a wave adds every fourth tile, another wave's next: the order of a
+// tile's sum is the same on every call.
 template <int TM, int TN>
 __device__ inline void wg8_store(const Wgrad8Args& a, const Wg8Block& b, const f32x16 (&acc)[TM][TN], float* lds) {
     constexpr int NW = wg8_waves(TM * TN);
@@ -305,8 +313,8 @@ __device__ inline void wg8_store(const Wgrad8Args& a, const Wg8Block& b, const f
     }
 }
 
-// 16-bit types, 16 channels a time: a wave brings 32 rows of codes, as values of the type, and of da into its own part of LDS
-// (the next 32 are on the way) and reads both back transposed: the matrix cores sum over rows.
+// 16-bit types, 16 channels at a time: a wave brings 32 rows of codes, as values of the type, and of da into its own
+// part of LDS (the next 32 are on the way) and reads both back transposed: the matrix cores sum over rows.
 template <int DT, int TM, int TN>
 __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void k_wgrad8(Wgrad8Args a, int parts) {
     constexpr int BM = 32 * TM, BN = 32 * TN, LM = 2 * BM + 16, LN = 2 * BN + 16;  // bytes from row to row in LDS
@@ -414,8 +422,8 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
     wg8_store<TM, TN>(a, b, acc, (float*)lds);
 }
 
-// float32, and 16-bit types of other widths and alignments, in products of float32: a lane's operands are a channel of a row
-// each, as memory has them.  Rows and channels past the ends are read as the last ones, and count as 0.
+// float32, and 16-bit types of other widths and alignments, in products of float32: a lane's operands are a channel
+// of a row each, as memory has them.  Rows and channels past the ends are read as the last ones, and count as 0.
 template <int DT, int TM, int TN>
 __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void k_wgrad8_any(Wgrad8Args a, int parts) {
     constexpr int U = 4, STEP = 2 * U;
@@ -471,8 +479,8 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
     wg8_store<TM, TN>(a, b, acc, lds);
 }
 
-// adds the shares of the n numbers in 64 bits, 64 of them a workgroup, in 32 runs of consecutive shares; each is then put
-// where it belongs in dW (blocks of TM x TN tiles, those of a column of blocks one after the other)
+// adds the shares of the n numbers in 64 bits, 64 of them a workgroup, in 32 runs of consecutive shares; each is then
+// put where it belongs in dW (blocks of TM x TN tiles, those of a column of blocks one after the other)
 __global__ __launch_bounds__(512) void k_wgrad8_join(const float* __restrict__ part, int parts, int64_t n, int TM, int TN, int Cin,
                                                      int Cout, float* __restrict__ dW) {
     __shared__ double red[32][65];

@@ -32,8 +32,8 @@ __device__ inline float code_value(int code, float step) {
     return code == -128 ? __uint_as_float(0x7FC00000u) : (float)code * step;
 }
 
-// What 4 N codes stand for: a byte counted from -128 takes a conversion and two exact steps.  A code of -128 (a zero byte
-// then) is looked for in all of them at once.
+// What 4 N codes stand for: a byte counted from -128 takes a conversion and two exact steps.  A code of -128 (a zero
+// byte then) is looked for in all of them at once.
 template <int N>
 __device__ inline void code_values(const uint32_t (&w)[N], float step, float (&x)[4 * N]) {
     uint32_t u[N], none = 0;
@@ -53,9 +53,9 @@ __device__ inline void code_values(const uint32_t (&w)[N], float step, float (&x
     }
 }
 
-// The codes of a lane's VEC channels of a block that LANES lanes hold (a power of two of them, next to each other); returns the
-// block's exponent byte.  All lanes of a block call it.  Where all values are finite a code is the low byte of x 2^-E plus
-// 1.5 2^23, whose addition rounds to a whole number, ties to even.
+// The codes of a lane's VEC channels of a block that LANES lanes hold (a power of two of them, next to each other);
+// returns the block's exponent byte.  All lanes of a block call it.  Where all values are finite a code is the low
+// byte of x 2^-E plus 1.5 2^23, whose addition rounds to a whole number, ties to even.
 template <int DT, int VEC, int LANES>
 __device__ inline int code_block(const float (&x)[VEC], uint32_t (&w)[VEC / 4]) {
     uint32_t top = 0;

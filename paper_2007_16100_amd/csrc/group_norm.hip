@@ -5,8 +5,14 @@
 //   dgamma = sum gz xh,  dbeta = sum gz.
 //
 // A scan's statistics take all of its rows, so each direction reads its rows twice.  Rows are cut into tiles of one
-// scan each, one to a workgroup: a first kernel leaves a tile's sums of each group, a second joins those of the tile's scan
-// (each workgroup again: a few thousand numbers, and a launch less) and writes the rows.
+// scan each, one to a workgroup: a first kernel leaves a tile's sums of each group, a second joins those of the
+// tile's scan (each workgroup again: a few thousand numbers, and a launch less) and writes the rows.  (One kernel
+// that keeps its rows over a barrier of all workgroups would read them once, but two such kernels on two streams
+// could each wait for room that the other holds.)
+//
+// Bound by memory, where rows are many: 300,007 x 96 in bf16 takes 35 us, 173 MB at 4.9 TB/s (a copy reaches 5.1): 13
+// for the statistics, 20 for the rows.  A training step of 88,119 x 96 with the residual's gradient, 152 MB, 42 us:
+// 9, 10, 13 and 15, of which 4 each are the launch, the search for the tile, the join and the last waves.
 #include <type_traits>
 
 #include "attn_common.hpp"
@@ -14,7 +20,8 @@
 
 namespace spv {
 
-// exp and the reciprocal are the hardware's, each off by 2^-23 of itself at most, and the exponent's rounding adds |z| 2^-24
+// exp and the reciprocal are the hardware's, each off by 2^-23 of itself at most, and the exponent's rounding adds
+// |z| 2^-24
 __device__ inline float sigmoid(float z) {
     return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -kLog2e));
 }
@@ -42,7 +49,11 @@ __device__ inline float act_grad(float d, float z) {
 // workgroup's tile, so what belongs to a channel stays in registers over the rows; R = kGnThreads / (C / VEC).
 // ---------------------------------------------------------------------------
 constexpr int kGnThreads = 512, kGnWaves = kGnThreads / 64;
-constexpr int kGnTiles = 240;  // tiles of one long scan: with the scans' first ones a workgroup a CU
+// Tiles of one long scan: with the scans' first ones and the workgroups that join the channels, about one a CU.  What
+// a workgroup does besides its rows (some 4 us, at the start and the end) is not hidden by a second one that does the
+// same: 240, 384 and 512 tiles take 39, 40 and 45 us for 300,007 x 96 in bf16 (512 being more than fit at once) and
+// 51, 61 and 61 for the training step of 88,119 x 96.
+constexpr int kGnTiles = 240;
 
 template <int DT>
 constexpr int kGnVec = DT == SPV_F32 ? 4 : 8;
@@ -137,8 +148,8 @@ __device__ inline GnTile gn_tile(const GnArgs& a, uint32_t tile_rows, uint32_t t
     return g;
 }
 
-// The tiles of a group of a scan, taken by a wave, or where scans have few tiles by 8 lanes: four a lane are asked for by the
-// constructor, before whatever else the workgroup has to wait for, the others in turn.
+// The tiles of a group of a scan, taken by a wave, or where scans have few tiles by 8 lanes: four a lane are asked
+// for by the constructor, before whatever else the workgroup has to wait for, the others in turn.
 struct GnGroup {
     const float2* part;
     int64_t stride, tiles;
@@ -213,6 +224,7 @@ __device__ inline void gn_join_all(const GnArgs& a, const GnTile& t, uint32_t ti
 }
 
 // rows a thread asks for at a time: more of single channels, which are 2 or 4 bytes each
+// (300,007 x 19 in 19 groups 23 -> 21 us)
 constexpr int gn_ahead(int vec, int rows) { return vec == 1 ? 4 * rows : rows; }
 
 // A thread's rows of a tile (row, row + R, ..), U at a time, the next U asked for before the present ones are used.
@@ -280,8 +292,8 @@ __device__ inline void gn_units(const GnArgs& a, int rows, int R, int w, int uni
     }
 }
 
-// A tile's mean and sum of squared deviations of each group.  A thread keeps the running mean of each of its channels and
-// the squares of the deviations from it, four rows at a time: no cancellation however far from zero the rows sit.
+// A tile's mean and sum of squared deviations of each group.  A thread keeps the running mean of each of its channels
+// and the squares of the deviations from it, four rows at a time: no cancellation however far from zero the rows sit.
 template <int DT, int VEC>
 __global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_rows) {
     using V = Chans<DT, VEC>;
@@ -561,6 +573,7 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_channels(GnArgs a, int64_t ti
 }
 
 // the rows' second pass: dx; the first workgroups join the channels
+// (128 registers: room for the joins' workgroups beside those of the tiles)
 template <int DT, int VEC, int ACT, bool X8>
 __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile_rows, int64_t tiles, unsigned join) {
     using V = Chans<DT, VEC>;
@@ -618,13 +631,13 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
 }
 
 // ---------------------------------------------------------------------------
-// Few rows: a workgroup takes a group of a scan, all of it in its threads' registers: the mean, the deviations from it and
-// the output in one launch.
+// Few rows: a workgroup takes a group of a scan, all of it in its threads' registers: the mean, the deviations from
+// it and the output in one launch.
 // ---------------------------------------------------------------------------
 constexpr int kGnFewThreads = 512;
 constexpr int kGnHeld = 24;  // values a thread holds
-// values in all up to which that is done: 701 x 96 in float32 takes 6.9 us with 8 groups (8.2 in tiles), in bf16 with 96 groups 4.5
-// (13.8); 8000 x 32 with 32 groups, whose rows are then read 4 bytes at a time, 14.4 (10.0)
+// values in all up to which that is done: 701 x 96 in float32 takes 6.9 us with 8 groups (8.2 in tiles), in bf16 with
+// 96 groups 4.5 (13.8); 8000 x 32 with 32 groups, whose rows are then read 4 bytes at a time, 14.4 (10.0)
 constexpr int64_t kGnFew = 1 << 17;
 
 __device__ inline float block_sum(float v, float* red) {
@@ -830,13 +843,16 @@ static int gn_tile_rows(int64_t m, int C) {
     return (int)(few > many ? few : many);
 }
 static int64_t gn_tiles(int64_t m, int C, int B) { return m / gn_tile_rows(m, C) + B; }
-// A workgroup joins its scan's tiles itself: up to 32 of them by 8 lanes a group (64 groups at a time), more by a wave, up to
-// four times over.  Beyond, a launch of its own is shorter.
+// A workgroup joins its scan's tiles itself: up to 32 of them by 8 lanes a group, 64 groups at a time (2000 x 96 in
+// 96 groups takes 14.5 us, 23.5 by a wave a group and 15.3 by a launch of its own), more by a wave, up to twice over.
+// Beyond, a launch of its own is shorter: 100,000 x 96 in bf16 15.4 against 17.1 us with 8 groups, 18.5 and 17.9 with
+// 24, 38.1 and 21.5 with 96.
 static bool gn_few_tiles(const GnArgs& a) { return gn_tiles(a.m, a.C, 1) <= 32; }
-static bool gn_join_apart(const GnArgs& a) { return !gn_few_tiles(a) && a.G > 4 * kGnWaves; }
+static bool gn_join_apart(const GnArgs& a) { return !gn_few_tiles(a) && a.G > 2 * kGnWaves; }
 
-// All groups of all scans fit a workgroup's registers each (no scan has more than m rows), and there are few values: rows are
-// read a group's channels at a time.  (Whether codes are asked for makes no difference to the other outputs.)
+// All groups of all scans fit a workgroup's registers each (no scan has more than m rows), and there are few values:
+// rows are read a group's channels at a time.  (Whether codes are asked for makes no difference to the other
+// outputs.)
 static bool gn_few(const GnArgs& a) {
     return a.m * (a.C / a.G) <= (int64_t)kGnHeld * kGnFewThreads && a.m * a.C <= kGnFew && (int64_t)a.B * a.G <= 4096;
 }

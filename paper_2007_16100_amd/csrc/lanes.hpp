@@ -10,8 +10,8 @@ template <int CTRL>
 __device__ inline int dpp(int v) {
     return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, true);
 }
-// f(own, partner's) over groups of N lanes (a power of two), the same result in each lane of a group: lanes 1 and 2 apart,
-// then, of equal quads and eights, the mirrored one; then rows of 16 and halves of the wave
+// f(own, partner's) over groups of N lanes (a power of two), the same result in each lane of a group: lanes 1 and 2
+// apart, then, of equal quads and eights, the mirrored one; then rows of 16 and halves of the wave
 template <int N, class F>
 __device__ inline int lanes_join(int v, F&& f) {
     if constexpr (N >= 2) v = f(v, dpp<0xB1>(v));

@@ -48,8 +48,9 @@ __device__ inline int over(int i, uint32_t by, int n) { return by ? (int)__umulh
 constexpr int kRopeAhead = 4;  // units a thread asks for before it waits
 constexpr int kRopeRows = 64;  // of a workgroup at most
 
-// A workgroup takes some rows: its threads form the sines and cosines of all their pairs once for all heads, in LDS, while
-// their first vectors are on the way.  Bound by memory: 88,119 rows of 16 heads of 32 in bf16, 180 MB, take 34 us.
+// A workgroup takes some rows: its threads form the sines and cosines of all their pairs once for all heads, in LDS,
+// while their first vectors are on the way.  Bound by memory: 88,119 rows of 16 heads of 32 in bf16, 180 MB, take 34
+// us.
 template <int DT, bool HALVES>
 __global__ __launch_bounds__(256) void k_rope_rows(RopeArgs a, RopeUnits un) {
     constexpr int V = DT == SPV_F32 ? 4 : 8, NV = HALVES ? 2 : 1;
@@ -127,8 +128,8 @@ __global__ __launch_bounds__(256) void k_rope_rows(RopeArgs a, RopeUnits un) {
     }
 }
 
-// Pairs of halves that vectors do not hold whole (P no multiple of theirs), and rows of millions of channels: a thread takes
-// pairs of single channels, those that stay two by two.
+// Pairs of halves that vectors do not hold whole (P no multiple of theirs), and rows of millions of channels: a
+// thread takes pairs of single channels, those that stay two by two.
 template <int DT>
 __global__ __launch_bounds__(256) void k_rope_pairs(RopeArgs a, RopeUnits un) {
     extern __shared__ float2 table[];  // [rows][P]
