@@ -104,6 +104,32 @@ struct Codes {
     }
 };
 
+__device__ inline int over(int i, uint32_t by) { return by ? (int)__umulhi((uint32_t)i, by) : i; }
+
+// a thread's row of R and its first channel (row R: it has none)
+template <int VEC>
+struct GnThread {
+    int row, c;
+    __device__ explicit GnThread(const GnShape& s)
+        : row(over((int)threadIdx.x, s.by_nv)), c(((int)threadIdx.x - row * s.nv) * VEC) {}
+};
+
+// the two numbers of a thread's channels' groups
+template <int VEC, class F>
+__device__ inline void gn_of_groups(const GnShape& s, const float2* groups, int c, F&& f) {
+    if (VEC == 1 || s.whole) {
+        const float2 v = groups[over(c, s.by_w)];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f(e, v);
+    } else {
+        float2 v[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] = groups[over(c + e, s.by_w)];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f(e, v[e]);
+    }
+}
+
 // a thread's channels of a vector, or `other` of each
 template <int VEC>
 __device__ inline void gn_channels(const float* p, int c, float other, float (&v)[VEC]) {
@@ -267,25 +293,26 @@ __global__ __launch_bounds__(256) void k_gn_join(GnArgs a, uint32_t tile_rows) {
 // The groups of a tile of `rows` rows, joined from the units' means and squares: val[R][C / unit], L lanes a group.
 // A thread's row holds every R-th one.
 template <int L>
-__device__ inline void gn_units(const GnArgs& a, int rows, int R, int w, int unit, const float2* val) {
-    const int l = threadIdx.x & (L - 1), per = w / unit, units = a.C / unit, all = R * per;
+__device__ inline void gn_units(const GnArgs& a, int rows, const float2* val) {
+    const GnShape& sh = a.sh;
+    const int l = threadIdx.x & (L - 1), R = sh.R, per = sh.per, units = sh.units, all = R * per;
     const int least = rows / R, more = rows - least * R;  // a thread's row has least rows, the first ones one more
-    const float inv = 1.f / ((float)rows * (float)per), by = 1.f / (float)per;
+    const float inv = 1.f / ((float)rows * (float)per);
     for (int g0 = 0; g0 < a.G; g0 += kGnThreads / L) {  // all lanes take part in the sums
         const int g = g0 + (int)threadIdx.x / L;
         const float2* v = val + (g < a.G ? g : 0) * per;
         const float first = v[0].x;  // equal values give their mean exactly
         float s = 0.f, q = 0.f;
         for (int j = l; j < all; j += L) {
-            const int r = (int)(((float)j + 0.5f) * by);
+            const int r = over(j, sh.by_per);
             s = fmaf((float)(least + (r < more)), v[r * units + (j - r * per)].x - first, s);
         }
         const float mu = fmaf(lanes_sum<L>(s), inv, first);
         for (int j = l; j < all; j += L) {
-            const int r = (int)(((float)j + 0.5f) * by);
+            const int r = over(j, sh.by_per);
             const float2 p = v[r * units + (j - r * per)];
             const float d = p.x - mu;
-            q += fmaf(d * d, (float)((least + (r < more)) * unit), p.y);
+            q += fmaf(d * d, (float)((least + (r < more)) * sh.unit), p.y);
         }
         q = lanes_sum<L>(q);
         if (l == 0 && g < a.G) a.tiles[(int64_t)blockIdx.x * a.G + g] = make_float2(mu, q);
@@ -300,8 +327,8 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_
     __shared__ float2 s_val[kGnThreads * VEC];
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
     if (t.rows == 0) return;
-    const int w = a.C / a.G, unit = VEC > 1 && w % VEC == 0 ? VEC : VEC > 2 && w % 4 == 0 ? 4 : VEC > 1 && w % 2 == 0 ? 2 : 1;
-    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
+    const GnThread<VEC> th(a.sh);
+    const int R = a.sh.R, row = th.row, c = th.c, unit = a.sh.unit;
     if (row < R) {
         float mean[VEC], sq[VEC], n = 0.f;
 #pragma unroll
@@ -352,7 +379,7 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_
         // equal counts: units of two, four and eight channels, while a group is made of those
 #pragma unroll
         for (int h = 1; h < VEC; h *= 2) {
-            if (w % (2 * h)) break;
+            if (unit < 2 * h) break;
 #pragma unroll
             for (int e = 0; e + h < VEC; e += 2 * h) {
                 const float d = mean[e + h] - mean[e];
@@ -360,15 +387,15 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_
                 sq[e] += fmaf(d * d, 0.5f * n * (float)h, sq[e + h]);
             }
         }
-        const int units = a.C / unit;
+        const int shift = unit >> 1 ? unit >> 2 ? unit >> 3 ? 3 : 2 : 1 : 0;
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-            if (e % unit == 0) s_val[row * units + (c + e) / unit] = make_float2(mean[e], sq[e]);
+            if ((e & (unit - 1)) == 0) s_val[row * a.sh.units + ((c + e) >> shift)] = make_float2(mean[e], sq[e]);
     }
     __syncthreads();
     // a group's units of all the threads' rows, by 64 lanes or by 8
-    if (R * (w / unit) > 32) gn_units<64>(a, t.rows, R, w, unit, s_val);
-    else gn_units<8>(a, t.rows, R, w, unit, s_val);
+    if (R * a.sh.per > 32) gn_units<64>(a, t.rows, s_val);
+    else gn_units<8>(a, t.rows, s_val);
 }
 
 // the rows' second pass: y, and x in 8 bits (CODE: whole blocks of 32 channels)
@@ -376,7 +403,8 @@ template <int DT, int VEC, int ACT, bool CODE>
 __global__ __launch_bounds__(kGnThreads) void k_gn_tile_apply(GnArgs a, int tile_rows) {
     using V = Chans<DT, VEC>;
     __shared__ float2 s_stat[kGnThreads * VEC];  // at most as many groups as channels
-    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
+    const GnThread<VEC> th(a.sh);
+    const int R = a.sh.R, row = th.row, c = th.c, w = a.sh.w;
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
     if (t.rows == 0 && !(t.first && a.stat)) return;
     GnGroup first(a, (int)threadIdx.x / (a.few_tiles ? 8 : 64), t.tile0, a.joined ? 0u : t.n, tile_rows);
@@ -388,19 +416,13 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_apply(GnArgs a, int tile
     constexpr int U = gn_ahead(VEC, 4);
     GnRows<U, typename V::Raw> rows{row, R, row < R ? t.rows : 0};
     if (rows.rows) rows.ask(row, rows.u, load);
-    const int w = a.C / a.G;
     gn_join_all(a, t, tile_rows, first, s_stat, [&](GnGroup& g) { return gn_join_stat(g, t.n, tile_rows, w, a.eps); });
     __syncthreads();
     if (t.first && a.stat)
         for (int g = threadIdx.x; g < a.G; g += kGnThreads) ((float2*)a.stat)[(int64_t)t.b * a.G + g] = s_stat[g];
     if (row >= R) return;  // whole blocks of 32 channels
     float mu[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        const float2 st = s_stat[(c + e) / w];
-        mu[e] = st.x;
-        ga[e] *= st.y;
-    }
+    gn_of_groups<VEC>(a.sh, s_stat, c, [&](int e, const float2& st) { mu[e] = st.x, ga[e] *= st.y; });
     rows.run(load, [&](int i0, const typename V::Raw(&u)[U]) {
 #pragma unroll
         for (int k = 0; k < U; ++k) {
@@ -452,17 +474,9 @@ struct GnSource {
 
 // r and -mean r of a thread's channels, so that xh is one fma (off by a rounding of mean r, as by one of the mean)
 template <int VEC>
-__device__ inline void gn_stat(const GnArgs& a, int b, int c, int w, float (&mu)[VEC], float (&r)[VEC]) {
-    const float2* st = (const float2*)a.stat + (int64_t)b * a.G;
-    int g = c / w, left = w - (c - g * w);  // channels of the group that are still to come
-    float2 v[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        v[e] = st[g];
-        if (--left == 0 && g + 1 < a.G) ++g, left = w;
-    }
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) r[e] = v[e].y, mu[e] = -v[e].x * v[e].y;
+__device__ inline void gn_stat(const GnArgs& a, int b, int c, float (&mu)[VEC], float (&r)[VEC]) {
+    gn_of_groups<VEC>(a.sh, (const float2*)a.stat + (int64_t)b * a.G, c,
+                      [&](int e, const float2& st) { r[e] = st.y, mu[e] = -st.x * st.y; });
 }
 
 // a tile's sums of gz and gz xh, of each channel and (times gamma) of each group
@@ -470,10 +484,11 @@ template <int DT, int VEC, int ACT, bool X8>
 __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_rows) {
     using V = Chans<DT, VEC>;
     using S = GnSource<DT, VEC, X8>;
-    __shared__ float s_1[kGnThreads * VEC], s_2[kGnThreads * VEC];
-    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
+    constexpr int N = kGnThreads * VEC;
+    __shared__ float s_sum[2 * N];  // [gz, gz xh][R][C]
+    const GnThread<VEC> th(a.sh);
+    const int R = a.sh.R, row = th.row, c = th.c, w = a.sh.w;
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x);
-    const int w = a.C / a.G;
     float* cols = a.part + (int64_t)blockIdx.x * 2 * a.C;
     if (t.rows == 0) {  // the join of the channels takes every tile
         for (int c = threadIdx.x; c < 2 * a.C; c += kGnThreads) cols[c] = 0.f;
@@ -487,7 +502,7 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
         GnRows<U, typename S::Raw> rows{row, R, t.rows};
         gn_channels<VEC>(a.gamma, c, 1.f, ga);
         gn_channels<VEC>(a.beta, c, 0.f, be);
-        gn_stat<VEC>(a, t.b, c, w, mu, r);
+        gn_stat<VEC>(a, t.b, c, mu, r);
         rows.ask(row, rows.u, load);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) s1[e] = s2[e] = 0.f;
@@ -508,36 +523,39 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
         });
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            s_1[row * a.C + c + e] = s1[e];
-            s_2[row * a.C + c + e] = s2[e];
+            s_sum[row * a.C + c + e] = s1[e];
+            s_sum[N + row * a.C + c + e] = s2[e];
         }
     }
     __syncthreads();
-    for (int k = R; k > 1;) {
-        const int q = (k + 3) / 4;
-        for (int j = threadIdx.x; j < q * a.C; j += kGnThreads) {
-            const int p = j / a.C;
-            float u = s_1[j], v = s_2[j];
-#pragma unroll
-            for (int h = 1; h < 4; ++h) {
-                if (p + h * q >= k) break;
-                u += s_1[j + h * q * a.C];
-                v += s_2[j + h * q * a.C];
-            }
-            s_1[j] = u;
-            s_2[j] = v;
+    // a column of R numbers by as many threads as there are, each every so many rows; a thread writes to a row of its own
+    const int parts = a.sh.parts;
+    for (int j = threadIdx.x; j < 2 * a.C * parts; j += kGnThreads) {
+        const int p = over(j, a.sh.by_cols), k = j - p * 2 * a.C;
+        float* v = s_sum + (k < a.C ? k : N + k - a.C);
+        float u = 0.f;
+        for (int i = p; i < R; i += parts) u += v[i * a.C];
+        v[p * a.C] = u;
+        if (parts == 1) cols[k] = u;
+    }
+    __syncthreads();
+    if (parts > 1) {
+        for (int k = threadIdx.x; k < 2 * a.C; k += kGnThreads) {
+            float* v = s_sum + (k < a.C ? k : N + k - a.C);
+            float u = v[0];
+            for (int i = 1; i < parts; ++i) u += v[i * a.C];
+            v[0] = u;
+            cols[k] = u;
         }
-        k = q;
         __syncthreads();
     }
-    for (int j = threadIdx.x; j < 2 * a.C; j += kGnThreads) cols[j] = j < a.C ? s_1[j] : s_2[j - a.C];
     const int lane = threadIdx.x & 63;
     for (int g = threadIdx.x >> 6; g < a.G; g += kGnWaves) {
         float p = 0.f, q = 0.f;
         for (int j = g * w + lane; j < (g + 1) * w; j += 64) {
             const float gj = a.gamma ? a.gamma[j] : 1.f;
-            p = fmaf(gj, s_1[j], p);
-            q = fmaf(gj, s_2[j], q);
+            p = fmaf(gj, s_sum[j], p);
+            q = fmaf(gj, s_sum[N + j], q);
         }
         p = lanes_sum<64>(p);
         q = lanes_sum<64>(q);
@@ -583,7 +601,8 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
         return;
     }
     __shared__ float2 s_mean[kGnThreads * VEC];
-    const int nv = a.C / VEC, R = kGnThreads / nv, row = threadIdx.x / nv, c = ((int)threadIdx.x - row * nv) * VEC;
+    const GnThread<VEC> th(a.sh);
+    const int R = a.sh.R, row = th.row, c = th.c, w = a.sh.w;
     const GnTile t = gn_tile(a, tile_rows, blockIdx.x - join);
     if (t.rows == 0) return;
     GnGroup first(a, (int)threadIdx.x / (a.few_tiles ? 8 : 64), t.tile0, a.joined ? 0u : t.n, tile_rows);
@@ -596,21 +615,15 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
     };
     constexpr int U = gn_ahead(VEC, 2);
     GnRows<U, typename S::RawRes> rows{row, R, row < R ? t.rows : 0};
-    const int w = a.C / a.G;
     float mu[VEC], r[VEC], ga[VEC], be[VEC], m1[VEC], m2[VEC];
     gn_channels<VEC>(a.gamma, c, 1.f, ga);
     gn_channels<VEC>(a.beta, c, 0.f, be);
-    gn_stat<VEC>(a, t.b, c, w, mu, r);
+    gn_stat<VEC>(a, t.b, c, mu, r);
     if (row < R) rows.ask(row, rows.u, load);
     gn_join_all(a, t, tile_rows, first, s_mean, [&](GnGroup& g) { return gn_join_sums(g, t.n, w); });
     __syncthreads();
     if (row >= R) return;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        const float2 me = s_mean[(c + e) / w];
-        m1[e] = me.x;
-        m2[e] = me.y;
-    }
+    gn_of_groups<VEC>(a.sh, s_mean, c, [&](int e, const float2& me) { m1[e] = me.x, m2[e] = me.y; });
     rows.run(load, [&](int i0, const typename S::RawRes(&u)[U]) {
 #pragma unroll
         for (int k = 0; k < U; ++k) {
@@ -857,6 +870,19 @@ static bool gn_few(const GnArgs& a) {
     return a.m * (a.C / a.G) <= (int64_t)kGnHeld * kGnFewThreads && a.m * a.C <= kGnFew && (int64_t)a.B * a.G <= 4096;
 }
 
+static uint32_t gn_by(int64_t n) { return n > 1 ? (uint32_t)((((uint64_t)1 << 32) + (uint64_t)n - 1) / (uint64_t)n) : 0u; }
+static GnShape gn_shape(int C, int G, int vec) {
+    GnShape s{};
+    s.nv = C / vec, s.R = kGnThreads / s.nv, s.w = C / G, s.whole = s.w % vec == 0;
+    s.unit = 1;
+    while (2 * s.unit <= vec && s.w % (2 * s.unit) == 0) s.unit *= 2;
+    s.per = s.w / s.unit, s.units = C / s.unit;
+    s.parts = kGnThreads / (2 * C);
+    s.parts = s.parts < 1 ? 1 : s.parts > s.R ? s.R : s.parts;
+    s.by_nv = gn_by(s.nv), s.by_w = gn_by(s.w), s.by_per = gn_by(s.per), s.by_cols = gn_by(2 * C);
+    return s;
+}
+
 static void gn_ws(Arena& a, GnArgs& t) {
     t.tiles = a.take<float2>((size_t)gn_tiles(t.m, t.C, t.B) * t.G);
     t.joined = a.take<float2>((size_t)t.B * t.G);
@@ -900,14 +926,14 @@ void launch_group_norm(hipStream_t s, const GnArgs& given) {
             launch_checkpoint8(s, a.x, a.saved, RowRange{a.m, nullptr, a.off, a.B}, a.C, a.dt);
         if (gn_few(a)) {
             const int w = a.C / a.G;
-            const uint32_t by = w > 1 ? (uint32_t)((((uint64_t)1 << 32) + (uint64_t)w - 1) / (uint64_t)w) : 0u;
-            k_gn_few<DT, ACT><<<(unsigned)(a.B * a.G), kGnFewThreads, 0, s>>>(a, by);
+            k_gn_few<DT, ACT><<<(unsigned)(a.B * a.G), kGnFewThreads, 0, s>>>(a, gn_by(w));
             return;
         }
         if constexpr (VEC == 0) {
             k_gn_stat<DT><<<gn_grid((int64_t)a.B * a.G), 256, 0, s>>>(a);
             if (a.m) k_gn_apply<DT, ACT><<<gn_grid(a.m), 256, 0, s>>>(a);
         } else {
+            a.sh = gn_shape(a.C, a.G, VEC);
             const int rows = gn_tile_rows(a.m, a.C);
             const unsigned tiles = (unsigned)gn_tiles(a.m, a.C, a.B);
             a.few_tiles = gn_few_tiles(a);
@@ -930,6 +956,7 @@ static void gn_backward_tiles(hipStream_t s, GnArgs a) {
     const int rows = gn_tile_rows(a.m, a.C);
     const int64_t tiles = gn_tiles(a.m, a.C, a.B);
     a.few_tiles = gn_few_tiles(a);
+    a.sh = gn_shape(a.C, a.G, VEC);
     const unsigned join = a.dgamma || a.dbeta ? (unsigned)((2 * a.C + 15) / 16) : 0;
     k_gn_tile_sums<DT, VEC, ACT, X8><<<(unsigned)tiles, kGnThreads, 0, s>>>(a, rows);
     if (a.dx && gn_join_apart(a)) k_gn_join<false><<<(unsigned)(((int64_t)a.B * a.G + 3) / 4), 256, 0, s>>>(a, rows);

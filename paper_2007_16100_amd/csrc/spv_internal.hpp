@@ -556,6 +556,15 @@ float* plan_wgrad8_ws(Arena& a, int64_t m_cap, int Cin, int Cout);
 void launch_wgrad8(hipStream_t s, const Wgrad8Args& a);
 
 // --- group norm over packed scans (group_norm.hip) ----------------------------------------
+// how the threads of a workgroup share a row, and quotients by its numbers as products (2^32 over each, rounded up; 0 for 1)
+struct GnShape {
+    int nv, R;                  // threads of a row, rows at a time
+    int w;                      // channels of a group
+    int whole;                  // a thread's channels are of one group
+    int unit, per, units;       // channels whose statistics are joined in a thread; units of a group and of a row
+    int parts;                  // threads that add up a column of R numbers
+    uint32_t by_nv, by_w, by_per, by_cols;
+};
 struct GnArgs {
     const void* x;              // [m][C], or nullptr: saved
     Saved8 saved;               // the backward's x, or the forward's output; codes nullptr: none
@@ -575,6 +584,7 @@ struct GnArgs {
     float2* joined;             // [B][G] the same of a scan, as mean and r, or means
     float* part;                // [tiles][2][C] the backward's sums of channels
     int few_tiles;              // no scan has more than 32
+    GnShape sh;
 };
 void plan_group_norm_ws(Arena& a, GnArgs& t);
 void launch_group_norm(hipStream_t s, const GnArgs& a);
