@@ -251,20 +251,21 @@ struct Wg8Block {
     int ci, co;         // its first channels
     int64_t r0, r1;     // the wave's rows
 };
-// the shares come first in the grid, so that the blocks of one share, which read the same rows, run on one die
+// the shares come first in the grid, so that the blocks of one share, which read the same rows, run on one die; a wave has
+// its share's part of the steps, the first waves of all one more where they do not come out even
 template <int TM, int TN, int STEP>
-__device__ inline Wg8Block wg8_block(const Wgrad8Args& a, int parts) {
+__device__ inline Wg8Block wg8_block(const Wgrad8Args& a) {
     constexpr int NW = wg8_waves(TM * TN);
     Wg8Block b;
-    b.part = (int)(blockIdx.x % (unsigned)parts);
-    b.block = (int)(blockIdx.x / (unsigned)parts);
-    const int nm = (a.Cin + 32 * TM - 1) / (32 * TM);
-    b.ci = b.block % nm * (32 * TM);
-    b.co = b.block / nm * (32 * TN);
-    const int64_t m = clamp_rows(a.m_dev, a.m_cap), steps = (m + STEP - 1) / STEP;
-    const int64_t waves = (int64_t)parts * NW, w = (int64_t)b.part * NW + uniform((int)(threadIdx.x >> 6));
-    b.r0 = steps * w / waves * STEP;
-    b.r1 = steps * (w + 1) / waves * STEP;
+    b.part = (int)blockIdx.x;
+    b.block = (int)(blockIdx.z * gridDim.y + blockIdx.y);
+    b.ci = (int)blockIdx.y * (32 * TM);
+    b.co = (int)blockIdx.z * (32 * TN);
+    const int64_t m = clamp_rows(a.m_dev, a.m_cap);
+    const uint32_t steps = (uint32_t)((m + STEP - 1) / STEP), waves = gridDim.x * NW;
+    const uint32_t w = blockIdx.x * NW + (uint32_t)uniform((int)(threadIdx.x >> 6)), each = steps / waves, more = steps - each * waves;
+    b.r0 = (int64_t)(w * each + (w < more ? w : more)) * STEP;
+    b.r1 = b.r0 + (int64_t)(each + (w < more)) * STEP;
     if (b.r1 > m) b.r1 = m;
     return b;
 }
@@ -301,7 +302,7 @@ __device__ inline void wg8_store(const Wgrad8Args& a, const Wg8Block& b, const f
             }
     }
     __syncthreads();
-    const int64_t n = (int64_t)((a.Cin + 32 * TM - 1) / (32 * TM)) * ((a.Cout + 32 * TN - 1) / (32 * TN)) * (TM * TN * 1024);
+    const int64_t n = (int64_t)gridDim.y * gridDim.z * (TM * TN * 1024);
     float4* out = (float4*)(a.part + b.part * n + (int64_t)b.block * (TM * TN * 1024));
     for (int t = threadIdx.x; t < TM * TN * 256; t += 64 * NW) {
         float4 v = ((const float4*)lds)[t];
@@ -316,7 +317,7 @@ __device__ inline void wg8_store(const Wgrad8Args& a, const Wg8Block& b, const f
 // 16-bit types, 16 channels at a time: a wave brings 32 rows of codes, as values of the type, and of da into its own
 // part of LDS (the next 32 are on the way) and reads both back transposed: the matrix cores sum over rows.
 template <int DT, int TM, int TN>
-__global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void k_wgrad8(Wgrad8Args a, int parts) {
+__global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void k_wgrad8(Wgrad8Args a) {
     constexpr int BM = 32 * TM, BN = 32 * TN, LM = 2 * BM + 16, LN = 2 * BN + 16;  // bytes from row to row in LDS
     constexpr int QM = BM / 16, QN = BN / 8;                     // 16-byte chunks of a row
     constexpr int KM = kWg8Step * QM / 64, KN = kWg8Step * QN / 64;  // of a lane
@@ -325,7 +326,7 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
     typedef short i16x8 __attribute__((ext_vector_type(8)));
     typedef __attribute__((address_space(3))) i16x4 lds4;
     __shared__ __align__(16) char lds[LDS];
-    const Wg8Block b = wg8_block<TM, TN, kWg8Step>(a, parts);
+    const Wg8Block b = wg8_block<TM, TN, kWg8Step>(a);
     const int lane = threadIdx.x & 63, nb = code_blocks(a.Cin);
     char *lx = lds + (threadIdx.x >> 6) * SIZE, *ld = lx + kWg8Step * LM;
     f32x16 acc[TM][TN];
@@ -425,10 +426,10 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
 // float32, and 16-bit types of other widths and alignments, in products of float32: a lane's operands are a channel
 // of a row each, as memory has them.  Rows and channels past the ends are read as the last ones, and count as 0.
 template <int DT, int TM, int TN>
-__global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void k_wgrad8_any(Wgrad8Args a, int parts) {
+__global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void k_wgrad8_any(Wgrad8Args a) {
     constexpr int U = 4, STEP = 2 * U;
     __shared__ __align__(16) float lds[wg8_waves(TM * TN) / 4 * TM * TN * 1024];
-    const Wg8Block b = wg8_block<TM, TN, STEP>(a, parts);
+    const Wg8Block b = wg8_block<TM, TN, STEP>(a);
     const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5, nb = code_blocks(a.Cin);
     f32x16 acc[TM][TN];
 #pragma unroll
@@ -518,14 +519,14 @@ __global__ __launch_bounds__(512) void k_wgrad8_join(const float* __restrict__ p
 
 template <int DT, int TM, int TN>
 static void wgrad8(hipStream_t s, const Wgrad8Args& a, int parts) {
-    const unsigned g = (unsigned)(parts * wgrad8_blocks(a.Cin) * wgrad8_blocks(a.Cout));
+    const dim3 g((unsigned)parts, (unsigned)wgrad8_blocks(a.Cin), (unsigned)wgrad8_blocks(a.Cout));
     if constexpr (DT != SPV_F32) {
         if (a.Cin % 16 == 0 && a.Cout % 8 == 0 && (((uintptr_t)a.in.codes | (uintptr_t)a.da) & 15u) == 0) {
-            k_wgrad8<DT, TM, TN><<<g, 64 * wg8_waves(TM * TN), 0, s>>>(a, parts);
+            k_wgrad8<DT, TM, TN><<<g, 64 * wg8_waves(TM * TN), 0, s>>>(a);
             return;
         }
     }
-    k_wgrad8_any<DT, TM, TN><<<g, 64 * wg8_waves(TM * TN), 0, s>>>(a, parts);
+    k_wgrad8_any<DT, TM, TN><<<g, 64 * wg8_waves(TM * TN), 0, s>>>(a);
 }
 template <int DT, int TM>
 static void wgrad8_n(hipStream_t s, const Wgrad8Args& a, int parts) {
