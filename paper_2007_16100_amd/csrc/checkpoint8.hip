@@ -219,7 +219,7 @@ constexpr int kWg8Most = 3;      // tiles of a side of a workgroup's block
 constexpr int kWg8Groups = 256;
 // waves of a workgroup: eight where a wave's sums leave room for two on a SIMD (26,881 x 256 -> 256 32 -> 28 us with
 // four tiles; nine tiles, 144 registers of sums, 23.8 -> 28.4)
-constexpr int wg8_waves(int tiles) { return tiles <= 4 ? 8 : 4; }
+constexpr int wg8_waves(int dt, int tm, int tn) { return tm * tn <= 4 && !(dt == SPV_F32 && tn == 3) ? 8 : 4; }
 
 // tiles of a side: the fewest padded, then the most
 static int wgrad8_side(int C) {
@@ -253,9 +253,8 @@ struct Wg8Block {
 };
 // the shares come first in the grid, so that the blocks of one share, which read the same rows, run on one die; a wave has
 // its share's part of the steps, the first waves of all one more where they do not come out even
-template <int TM, int TN, int STEP>
+template <int TM, int TN, int NW, int STEP>
 __device__ inline Wg8Block wg8_block(const Wgrad8Args& a) {
-    constexpr int NW = wg8_waves(TM * TN);
     Wg8Block b;
     b.part = (int)blockIdx.x;
     b.block = (int)(blockIdx.z * gridDim.y + blockIdx.y);
@@ -277,9 +276,8 @@ __device__ inline int wg8_place(int c, int q) { return c * 32 + 4 * (q ^ ((c >> 
 // The waves' sums of a block, added up in LDS, and then to the share's part of the workspace.  Four waves share an
 // image of the block; in each of four rounds a wave adds every fourth tile, another wave's next: the order of a
 // tile's sum is the same on every call.
-template <int TM, int TN>
+template <int NW, int TM, int TN>
 __device__ inline void wg8_store(const Wgrad8Args& a, const Wg8Block& b, const f32x16 (&acc)[TM][TN], float* lds) {
-    constexpr int NW = wg8_waves(TM * TN);
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), c = lane & 31, h = lane >> 5;
     float* image = lds + (wave >> 2) * (TM * TN * 1024);
     for (int w = 0; w < 4; ++w) {
@@ -314,19 +312,35 @@ __device__ inline void wg8_store(const Wgrad8Args& a, const Wg8Block& b, const f
     }
 }
 
-// 16-bit types, 16 channels at a time: a wave brings 32 rows of codes, as values of the type, and of da into its own
-// part of LDS (the next 32 are on the way) and reads both back transposed: the matrix cores sum over rows.
+// A float32 number as three of bf16 (8 bits each, cut off, the last one what is left): their sum is the number, down to
+// 2^-126 or so.  One that is not finite is the first of the three.
+__device__ inline void three_parts(float d, uint32_t (&p)[3]) {
+    const bool finite = (__float_as_uint(d) & 0x7F800000u) != 0x7F800000u;
+    const uint32_t top = __float_as_uint(d) & 0xFFFF0000u;
+    const float r = d - __uint_as_float(top);
+    const uint32_t mid = __float_as_uint(r) & 0xFFFF0000u;
+    p[0] = finite || d == d ? top : 0x7FC00000u;
+    p[1] = finite ? mid : 0u;
+    p[2] = finite ? __float_as_uint(r - __uint_as_float(mid)) : 0u;
+}
+
+// 16 channels of codes and 16 bytes of da at a time: a wave brings 32 rows of codes, as values of the type, and of da into
+// its own part of LDS (the next 32 are on the way) and reads both back transposed: the matrix cores sum over rows.  With
+// float32 the values are multiplied as bf16, which holds them (7 bits), by da in three parts of bf16: every product is
+// exact, and three of them take a third of the time of one of float32's own.
 template <int DT, int TM, int TN>
-__global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void k_wgrad8(Wgrad8Args a) {
+__global__ __launch_bounds__(64 * wg8_waves(DT, TM, TN), TM * TN > 6 ? 1 : 2) void k_wgrad8(Wgrad8Args a) {
+    constexpr bool W = DT == SPV_F32;
+    constexpr int MT = W ? SPV_BF16 : DT, PARTS = W ? 3 : 1, SZ = W ? 4 : 2, E = 16 / SZ;  // type of the products
     constexpr int BM = 32 * TM, BN = 32 * TN, LM = 2 * BM + 16, LN = 2 * BN + 16;  // bytes from row to row in LDS
-    constexpr int QM = BM / 16, QN = BN / 8;                     // 16-byte chunks of a row
+    constexpr int QM = BM / 16, QN = BN / E;                         // 16-byte chunks of a row
     constexpr int KM = kWg8Step * QM / 64, KN = kWg8Step * QN / 64;  // of a lane
-    constexpr int SIZE = kWg8Step * (LM + LN);
-    constexpr int NW = wg8_waves(TM * TN), SUMS = NW / 4 * BM * BN * 4, LDS = NW * SIZE > SUMS ? NW * SIZE : SUMS;
+    constexpr int PART = kWg8Step * LN, SIZE = kWg8Step * LM + PARTS * PART;
+    constexpr int NW = wg8_waves(DT, TM, TN), SUMS = NW / 4 * BM * BN * 4, LDS = NW * SIZE > SUMS ? NW * SIZE : SUMS;
     typedef short i16x8 __attribute__((ext_vector_type(8)));
     typedef __attribute__((address_space(3))) i16x4 lds4;
     __shared__ __align__(16) char lds[LDS];
-    const Wg8Block b = wg8_block<TM, TN, kWg8Step>(a);
+    const Wg8Block b = wg8_block<TM, TN, NW, kWg8Step>(a);
     const int lane = threadIdx.x & 63, nb = code_blocks(a.Cin);
     char *lx = lds + (threadIdx.x >> 6) * SIZE, *ld = lx + kWg8Step * LM;
     f32x16 acc[TM][TN];
@@ -348,13 +362,13 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
     }
 #pragma unroll
     for (int k = 0; k < KN; ++k) {
-        const int t = lane + 64 * k, c = b.co + t % QN * 8 < a.Cout ? b.co + t % QN * 8 : a.Cout - 8;
-        atd[k] = (uint32_t)(t / QN * a.Cout + c) * 2u;
+        const int t = lane + 64 * k, c = b.co + t % QN * E < a.Cout ? b.co + t % QN * E : a.Cout - E;
+        atd[k] = (uint32_t)(t / QN * a.Cout + c) * SZ;
     }
     auto ask = [&](int64_t r0) {
         const int8_t* px = a.in.codes + r0 * a.Cin;
         const uint8_t* pe = a.in.exps + r0 * nb;
-        const char* pd = (const char*)a.da + r0 * a.Cout * 2;
+        const char* pd = (const char*)a.da + r0 * a.Cout * SZ;
         if (r0 + kWg8Step <= b.r1) {
 #pragma unroll
             for (int k = 0; k < KM; ++k) {
@@ -394,7 +408,7 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
             code_values(w, code_step(ue[k]), f);
             uint32_t v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = pack2<DT>(f[2 * e], f[2 * e + 1]);
+            for (int e = 0; e < 8; ++e) v[e] = pack2<MT>(f[2 * e], f[2 * e + 1]);
             uint4* p = (uint4*)(lx + t / QM * LM + t % QM * 32);
             p[0] = make_uint4(v[0], v[1], v[2], v[3]);
             p[1] = make_uint4(v[4], v[5], v[6], v[7]);
@@ -402,7 +416,19 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
 #pragma unroll
         for (int k = 0; k < KN; ++k) {
             const int t = lane + 64 * k;
-            *(uint4*)(ld + t / QN * LN + t % QN * 16) = ud[k];
+            char* p = ld + t / QN * LN + t % QN * (2 * E);
+            if constexpr (W) {
+                const uint32_t w[4] = {ud[k].x, ud[k].y, ud[k].z, ud[k].w};
+                uint32_t q[4][3];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) three_parts(__uint_as_float(w[e]), q[e]);
+#pragma unroll
+                for (int h = 0; h < 3; ++h)  // the upper halves of two words
+                    *(uint2*)(p + h * PART) = make_uint2(__builtin_amdgcn_perm(q[1][h], q[0][h], 0x07060302u),
+                                                         __builtin_amdgcn_perm(q[3][h], q[2][h], 0x07060302u));
+            } else {
+                *(uint4*)p = ud[k];
+            }
         }
         if (r0 + kWg8Step < b.r1) ask(r0 + kWg8Step);
         lds_wait();
@@ -412,24 +438,27 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
 #pragma unroll
             for (int i = 0; i < TM; ++i) x[i] = transposed(lx + 16 * k * LM + 64 * i, LM);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) d[j] = transposed(ld + 16 * k * LN + 64 * j, LN);
+            for (int h = PARTS - 1; h >= 0; --h) {  // the smallest first
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+                for (int j = 0; j < TN; ++j) d[j] = transposed(ld + h * PART + 16 * k * LN + 64 * j, LN);
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = mfma32x32x16<DT>(x[i], d[j], acc[i][j]);
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma32x32x16<MT>(x[i], d[j], acc[i][j]);
+            }
         }
         lds_wait();
     }
-    wg8_store<TM, TN>(a, b, acc, (float*)lds);
+    wg8_store<NW>(a, b, acc, (float*)lds);
 }
 
-// float32, and 16-bit types of other widths and alignments, in products of float32: a lane's operands are a channel
+// Other widths and alignments, in products of float32: a lane's operands are a channel
 // of a row each, as memory has them.  Rows and channels past the ends are read as the last ones, and count as 0.
 template <int DT, int TM, int TN>
-__global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void k_wgrad8_any(Wgrad8Args a) {
-    constexpr int U = 4, STEP = 2 * U;
-    __shared__ __align__(16) float lds[wg8_waves(TM * TN) / 4 * TM * TN * 1024];
-    const Wg8Block b = wg8_block<TM, TN, STEP>(a);
+__global__ __launch_bounds__(64 * wg8_waves(DT, TM, TN), TM * TN > 6 ? 1 : 2) void k_wgrad8_any(Wgrad8Args a) {
+    constexpr int U = 4, STEP = 2 * U, NW = wg8_waves(DT, TM, TN);
+    __shared__ __align__(16) float lds[NW / 4 * TM * TN * 1024];
+    const Wg8Block b = wg8_block<TM, TN, NW, STEP>(a);
     const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5, nb = code_blocks(a.Cin);
     f32x16 acc[TM][TN];
 #pragma unroll
@@ -477,7 +506,7 @@ __global__ __launch_bounds__(64 * wg8_waves(TM * TN), TM * TN > 6 ? 1 : 2) void 
                 for (int j = 0; j < TN; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[u][i], g[u][j], acc[i][j], 0, 0, 0);
     }
-    wg8_store<TM, TN>(a, b, acc, lds);
+    wg8_store<NW>(a, b, acc, lds);
 }
 
 // adds the shares of the n numbers in 64 bits, 64 of them a workgroup, in 32 runs of consecutive shares; each is then
@@ -520,13 +549,11 @@ __global__ __launch_bounds__(512) void k_wgrad8_join(const float* __restrict__ p
 template <int DT, int TM, int TN>
 static void wgrad8(hipStream_t s, const Wgrad8Args& a, int parts) {
     const dim3 g((unsigned)parts, (unsigned)wgrad8_blocks(a.Cin), (unsigned)wgrad8_blocks(a.Cout));
-    if constexpr (DT != SPV_F32) {
-        if (a.Cin % 16 == 0 && a.Cout % 8 == 0 && (((uintptr_t)a.in.codes | (uintptr_t)a.da) & 15u) == 0) {
-            k_wgrad8<DT, TM, TN><<<g, 64 * wg8_waves(TM * TN), 0, s>>>(a);
-            return;
-        }
-    }
-    k_wgrad8_any<DT, TM, TN><<<g, 64 * wg8_waves(TM * TN), 0, s>>>(a);
+    if (a.Cin % 16 == 0 && a.Cout % (DT == SPV_F32 ? 4 : 8) == 0 &&
+        (((uintptr_t)a.in.codes | (uintptr_t)a.da) & 15u) == 0)
+        k_wgrad8<DT, TM, TN><<<g, 64 * wg8_waves(DT, TM, TN), 0, s>>>(a);
+    else
+        k_wgrad8_any<DT, TM, TN><<<g, 64 * wg8_waves(DT, TM, TN), 0, s>>>(a);
 }
 template <int DT, int TM>
 static void wgrad8_n(hipStream_t s, const Wgrad8Args& a, int parts) {
