@@ -737,11 +737,11 @@ spv_status spv_checkpoint8_read(void* stream, const int8_t* codes, const uint8_t
  * spv_linear_backward8 -- the weight gradient of a linear layer whose input rows were
  * kept in 8 bits (spv_linear_backward's dW, from codes):
  *   dW = in^T @ da (float32),  in = what spv_checkpoint8_read gives.
- * 16-byte aligned codes and da of 16-bit types with Cin a multiple of 16 and Cout of 8
- * run on those types' matrix cores, to which the rows' values and da go as they are
- * (both exact in the type), float32 and the others on those for float32; sums are
- * float32 over a workgroup's rows, and the workgroups' are added in fp64 in a fixed
- * order: the same bits on every call.
+ * 16-byte aligned codes and da with Cin a multiple of 16 and Cout of 8 (f32: 4) run on
+ * the 16-bit matrix cores: the rows' values are exact there, 16-bit da goes as it is,
+ * float32 da (of many rows) in three parts that add up to it.  Other widths and
+ * alignments, and few rows of float32, run on those for float32.  Sums are float32 over a workgroup's rows, and the workgroups' are
+ * added in fp64 in a fixed order: the same bits on every call.
  * In:  codes [m_cap][Cin], exps [m_cap][ceil(Cin / 32)]; m_dev: device row count
  *      (NULL = m_cap); da [m_cap][Cout] (dt).
  * Out: dW [Cin][Cout] f32, all of it (0 without rows).

@@ -452,7 +452,7 @@ __global__ __launch_bounds__(64 * wg8_waves(DT, TM, TN), TM * TN > 6 ? 1 : 2) vo
     wg8_store<NW>(a, b, acc, (float*)lds);
 }
 
-// Other widths and alignments, in products of float32: a lane's operands are a channel
+// Other widths and alignments, and few rows of float32, in products of float32: a lane's operands are a channel
 // of a row each, as memory has them.  Rows and channels past the ends are read as the last ones, and count as 0.
 template <int DT, int TM, int TN>
 __global__ __launch_bounds__(64 * wg8_waves(DT, TM, TN), TM * TN > 6 ? 1 : 2) void k_wgrad8_any(Wgrad8Args a) {
@@ -549,7 +549,10 @@ __global__ __launch_bounds__(512) void k_wgrad8_join(const float* __restrict__ p
 template <int DT, int TM, int TN>
 static void wgrad8(hipStream_t s, const Wgrad8Args& a, int parts) {
     const dim3 g((unsigned)parts, (unsigned)wgrad8_blocks(a.Cin), (unsigned)wgrad8_blocks(a.Cout));
-    if (a.Cin % 16 == 0 && a.Cout % (DT == SPV_F32 ? 4 : 8) == 0 &&
+    // float32: rows enough for a wave's steps of 32 (96 -> 96, 1024 waves: 701 rows take 12.1 us in three parts, 10.0 in
+    // float32's products; 12,000 18.0 and 17.6; 256 -> 256, 128 waves: 701 12.8 and 12.2, 12,000 19.3 and 35.3)
+    const bool rows = DT != SPV_F32 || a.m_cap >= (int64_t)12 * parts * wg8_waves(DT, TM, TN);
+    if (rows && a.Cin % 16 == 0 && a.Cout % (DT == SPV_F32 ? 4 : 8) == 0 &&
         (((uintptr_t)a.in.codes | (uintptr_t)a.da) & 15u) == 0)
         k_wgrad8<DT, TM, TN><<<g, 64 * wg8_waves(DT, TM, TN), 0, s>>>(a);
     else

@@ -35,7 +35,8 @@ def _rows(t: torch.Tensor, width: int, dtype: torch.dtype, name: str, rows: Opti
 
 class ScanLayer:
     """What the layers over packed scans share: calls on several streams or from several threads may overlap, as a layer
-    keeps workspaces for each."""
+    keeps workspaces for each.  Graphs captured on one stream use that stream's: their replays must not overlap each other
+    or its calls."""
 
     def __init__(self):
         self.ws: Dict[tuple, tuple] = {}

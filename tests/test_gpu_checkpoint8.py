@@ -183,20 +183,23 @@ def test_weight_gradient_of_small_numbers(spv, Cin, Cout, dtype, e):
 
 
 @pytest.mark.parametrize("Cin,Cout", [(32, 32), (96, 64), (19, 33)])
-def test_weight_gradient_keeps_float32(spv, Cin, Cout):
-    """A single row's products are da's own 24 bits times the codes' seven, over the range of float32: up to three roundings.
-    What is not finite in da stays in its column as it is."""
-    x = features(1, Cin, "f32", 3)
-    x[0, 0] = 1.0
+@pytest.mark.parametrize("m", [1, 30000])
+def test_weight_gradient_keeps_float32(spv, Cin, Cout, m):
+    """A single row's products (among rows of zeros) are da's own 24 bits times the codes' seven, over the range of float32: up
+    to three roundings.  What is not finite in da stays in its column as it is."""
+    x = torch.zeros(m, Cin, device="cuda")
+    x[-1:] = features(1, Cin, "f32", 3)
+    x[-1, 0] = 1.0
     g = torch.Generator().manual_seed(4)
-    da = (torch.randn(1, Cout, generator=g) * 10.0 ** (60 * torch.rand(1, Cout, generator=g) - 30)).cuda()
-    ws, saved = spv.Workspace.for_linear_backward8(1, Cin, Cout), spv.spv_checkpoint8(x)
-    X, D = ref.codes(arr(x), "f32")[2], arr(da)
+    da = torch.zeros(m, Cout, device="cuda")
+    da[-1:] = torch.randn(1, Cout, generator=g) * 10.0 ** (60 * torch.rand(1, Cout, generator=g) - 30)
+    ws, saved = spv.Workspace.for_linear_backward8(m, Cin, Cout), spv.spv_checkpoint8(x)
+    X, D = ref.codes(arr(x[-1:]), "f32")[2], arr(da[-1:])
     want = X.T @ D
     got = spv.spv_linear_backward8(ws, saved, da)
     assert np.all(np.abs(arr(got) - want) <= 3 * ref.EPS * np.abs(want) + ref.TINY["f32"])
-    da[0, 1], da[0, 5], da[0, 7] = float("inf"), float("-inf"), float("nan")
-    da[0, 8] = torch.tensor([0x7F800001], dtype=torch.int32).view(torch.float32)[0]
+    da[-1, 1], da[-1, 5], da[-1, 7] = float("inf"), float("-inf"), float("nan")
+    da[-1, 8] = torch.tensor([0x7F800001], dtype=torch.int32).view(torch.float32)[0]
     bad = spv.spv_linear_backward8(ws, saved, da)
     assert bad[0, 1] == float("inf") and bad[0, 5] == float("-inf") and bool(torch.isnan(bad[0, 7:9]).all())
     keep = [j for j in range(Cout) if j not in (1, 5, 7, 8)]

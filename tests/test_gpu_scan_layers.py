@@ -231,3 +231,19 @@ def test_a_training_step_of_both_layers_in_a_graph(spv):
         for a, b in zip(got, step(x, dy)):
             assert torch.equal(a, b)
         torch.cuda.synchronize()
+
+
+def test_layers_on_scans_without_voxels(spv):
+    """A batch of which nothing is left: outputs and gradients of no rows, weight gradients of zeros."""
+    from paper_2007_16100_amd.scan_attention import ScanAttention
+    from paper_2007_16100_amd.scan_mlp import ScanMLP
+    C, off, coords = 96, torch.zeros(3, dtype=torch.int32).cuda(), torch.zeros(0, 4, dtype=torch.int32).cuda()
+    x = torch.zeros(0, C, dtype=torch.bfloat16).cuda()
+    rope = spv.make_rope_params(32, spv.rope_freqs((6, 6, 4)), (6, 6, 4))
+    for keep8 in (False, True):
+        for layer, args in ((ScanAttention(attention_params(C, 3, 3, 32, "bf16", 1), 3, rope=rope, keep8=keep8), (off, coords)),
+                            (ScanMLP(mlp_params(C, 192, "bf16", 2), 8, keep8=keep8), (off,))):
+            saved = {}
+            assert layer.forward(x, *args, save=saved).shape == (0, C)
+            g = layer.backward(saved, x)
+            assert g["x"].shape == (0, C) and not any(bool(t.any()) for k, t in g.items() if k != "x")

@@ -68,3 +68,49 @@ def test_rotary_positions_without_coordinates(no_calls):
                dict(coords=c, tokens=tok, token_off=off, token_coords=c[:1])):
         with pytest.raises(ValueError):
             layer.forward(x, off, **kw)
+
+
+def test_one_workspace_a_stream_and_thread(monkeypatch):
+    """The calls of a step, replaced by ones that note their workspace: two streams' and two threads' are apart."""
+    import ctypes as ct
+    import threading
+    import types
+    log = types.SimpleNamespace(used=[], stream=ct.c_void_p(None))
+
+    class Workspace:
+        def __init__(self, nbytes):
+            self.nbytes = nbytes
+    for n in ("for_ops", "for_linear_backward", "for_linear_backward8", "for_group_norm_backward"):
+        setattr(Workspace, n, classmethod(lambda cls, *sizes: cls(sum(sizes))))
+
+    def note(result):
+        def f(ws, *a, **k):
+            log.used.append(ws)
+            return result(*a, **k)
+        return f
+    fake = types.SimpleNamespace(
+        Workspace=Workspace, _stream=lambda: log.stream, Checkpoint8=spv.Checkpoint8,
+        spv_linear=note(lambda x, W, res=None: torch.zeros(x.shape[0], W.shape[1])),
+        spv_linear_backward=note(lambda x, W, da, want_dx=True: (None, torch.zeros_like(W))),
+        spv_group_norm=note(lambda x, *a, want_stat=False, want_checkpoint=False: (x, torch.zeros(1, 2, 2)) if want_stat else x),
+        spv_group_norm_backward=note(lambda dy, x, *a, dres=None: (dy, torch.zeros(1), torch.zeros(1))))
+    monkeypatch.setattr(scan_attention, "spv", fake)
+    monkeypatch.setattr(scan_mlp, "spv", fake)
+    layer = ScanMLP(mlp(8, 16, F32), 2)
+
+    def step():
+        log.used.clear()
+        saved, x = {}, torch.zeros(5, 8)
+        layer.forward(x, torch.tensor([0, 5], dtype=torch.int32), save=saved)
+        layer.backward(saved, x)
+        return [id(w) for w in log.used]
+    first = step()
+    assert first and step() == first
+    log.stream = ct.c_void_p(4096)
+    other = step()
+    assert len(other) == len(first) and not set(first) & set(other)
+    log.stream, got = ct.c_void_p(None), []
+    t = threading.Thread(target=lambda: got.extend(step()))
+    t.start()
+    t.join()
+    assert len(got) == len(first) and not set(first) & set(got)
