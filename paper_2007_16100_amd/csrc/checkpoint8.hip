@@ -513,7 +513,7 @@ __global__ __launch_bounds__(64 * wg8_waves(DT, TM, TN), TM * TN > 6 ? 1 : 2) vo
 // put where it belongs in dW (blocks of TM x TN tiles, those of a column of blocks one after the other)
 __global__ __launch_bounds__(512) void k_wgrad8_join(const float* __restrict__ part, int parts, int64_t n, int TM, int TN, int Cin,
                                                      int Cout, float* __restrict__ dW) {
-    __shared__ double red[32][65];
+    __shared__ double red[8][65];
     const int col = threadIdx.x & 15, run = threadIdx.x >> 4, len = (parts + 31) / 32;
     const int p0 = run * len, p1 = p0 + len < parts ? p0 + len : parts;
     const float4* from = (const float4*)(part + (int64_t)blockIdx.x * 64) + col;
@@ -532,18 +532,20 @@ __global__ __launch_bounds__(512) void k_wgrad8_join(const float* __restrict__ p
         }
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) red[run][4 * col + e] = s[e];
-    __syncthreads();
-    for (int k = 16; k > 0; k /= 2) {  // 16 rows of 64 by 512 threads
-        for (int t = threadIdx.x; t < k * 64; t += 512) red[t / 64][t % 64] += red[t / 64 + k][t % 64];
-        __syncthreads();
+    for (int e = 0; e < 4; ++e) {  // a wave's four runs, then the waves'
+        s[e] = rows_sum(s[e]);
+        if ((threadIdx.x & 63) < 16) red[threadIdx.x >> 6][4 * col + e] = s[e];
     }
+    __syncthreads();
     if (threadIdx.x >= 64) return;
+    double sum = red[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) sum += red[w][threadIdx.x];
     const int64_t t = (int64_t)blockIdx.x * 64 + threadIdx.x;
     const int tile = (int)(t / 1024), c = (int)(t % 1024) / 32, q = (int)(t % 32) / 4 ^ ((c >> 1) & 7);
     const int block = tile / (TM * TN), in = tile % (TM * TN), nm = (Cin + 32 * TM - 1) / (32 * TM);
     const int i = (block % nm * TM + in / TN) * 32 + 4 * q + (int)(t % 4), j = (block / nm * TN + in % TN) * 32 + c;
-    if (i < Cin && j < Cout) dW[(int64_t)i * Cout + j] = (float)red[0][threadIdx.x];
+    if (i < Cin && j < Cout) dW[(int64_t)i * Cout + j] = (float)sum;
 }
 
 template <int DT, int TM, int TN>

@@ -37,14 +37,9 @@ template <int N>
 __device__ inline uint32_t lanes_max(uint32_t v) {
     return (uint32_t)lanes_join<N>((int)v, [](int a, int b) { return (int)max((uint32_t)a, (uint32_t)b); });
 }
-// in 64 bits, over groups of 8 lanes or (wide) the whole wave
-__device__ inline double lanes_sum(double v, bool wide) {
+// of the four lanes 16 apart, in 64 bits
+__device__ inline double rows_sum(double v) {
     auto pair = [](int lo, int hi) { return __hiloint2double(hi, lo); };
-    v += pair(dpp<0xB1>(__double2loint(v)), dpp<0xB1>(__double2hiint(v)));
-    v += pair(dpp<0x4E>(__double2loint(v)), dpp<0x4E>(__double2hiint(v)));
-    v += pair(dpp<0x141>(__double2loint(v)), dpp<0x141>(__double2hiint(v)));
-    if (!wide) return v;
-    v += pair(dpp<0x140>(__double2loint(v)), dpp<0x140>(__double2hiint(v)));
     {
         const auto l = __builtin_amdgcn_permlane16_swap(__double2loint(v), __double2loint(v), false, false);
         const auto h = __builtin_amdgcn_permlane16_swap(__double2hiint(v), __double2hiint(v), false, false);
@@ -53,6 +48,16 @@ __device__ inline double lanes_sum(double v, bool wide) {
     const auto l = __builtin_amdgcn_permlane32_swap(__double2loint(v), __double2loint(v), false, false);
     const auto h = __builtin_amdgcn_permlane32_swap(__double2hiint(v), __double2hiint(v), false, false);
     return pair((int)l[0], (int)h[0]) + pair((int)l[1], (int)h[1]);
+}
+// over groups of 8 lanes or (wide) the whole wave, in 64 bits
+__device__ inline double lanes_sum(double v, bool wide) {
+    auto pair = [](int lo, int hi) { return __hiloint2double(hi, lo); };
+    v += pair(dpp<0xB1>(__double2loint(v)), dpp<0xB1>(__double2hiint(v)));
+    v += pair(dpp<0x4E>(__double2loint(v)), dpp<0x4E>(__double2hiint(v)));
+    v += pair(dpp<0x141>(__double2loint(v)), dpp<0x141>(__double2hiint(v)));
+    if (!wide) return v;
+    v += pair(dpp<0x140>(__double2loint(v)), dpp<0x140>(__double2hiint(v)));
+    return rows_sum(v);
 }
 
 // 16 bytes of channels in float32, and back with one rounding
