@@ -208,14 +208,14 @@ void launch_checkpoint8_read(hipStream_t s, Saved8 from, void* out, const RowRan
 // ---------------------------------------------------------------------------
 // dW = in^T da.  A workgroup takes TM x TN tiles of 32 x 32 of dW and a share of the rows, its waves some of those
 // each, with nothing between them but the sum at the end.  The shares' sums go to the workspace and are joined in 64
-// bits. 88,119 x 96 -> 96 in bf16: 12.7 us and 5.0 for the join; 26,881 x 256 -> 256 in f16: 15.0 and 4.6 (matrix
+// bits. 88,119 x 96 -> 96 in bf16: 12.9 us and 4.9 for the join; 26,881 x 256 -> 256 in f16: 15.1 and 4.2 (matrix
 // cores busy 12% of the time, vector units 43%: a code takes four steps to become a value, in each of the four
 // columns of blocks that read it).
 // ---------------------------------------------------------------------------
 constexpr int kWg8Step = 32;     // rows of a wave's step
 constexpr int kWg8Most = 3;      // tiles of a side of a workgroup's block
 // Workgroups, as far as the rows go: one a CU.  Each leaves a share of dW (88,119 x 96 -> 96 with the codes' making
-// takes 24.9 us with 128 shares, 23.6 with 256, 31.8 with 512; 26,881 x 256 -> 256 31.3, 24.9, 29.5).
+// takes 24.3 us with 128 shares, 23.0 with 256, 30.4 with 512; 26,881 x 256 -> 256 30.6, 24.2, 29.5).
 constexpr int kWg8Groups = 256;
 // waves of a workgroup: eight where a wave's sums leave room for two on a SIMD (26,881 x 256 -> 256 32 -> 28 us with
 // four tiles; nine tiles, 144 registers of sums, 23.8 -> 28.4)

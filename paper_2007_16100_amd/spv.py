@@ -905,7 +905,7 @@ def spv_rope(params: RopeParams, coords: torch.Tensor, q: torch.Tensor, k: Optio
         raise ValueError(f"libspv takes tensors of the current device, cuda:{dev}")
     cp, count = _at(coords, dev), _count(m_dev, dev)
     if outs is None:
-        outs = (q.new_empty(q.shape),) if k is None else (q.new_empty(q.shape), k.new_empty(k.shape))
+        outs = tuple(torch.empty_like(t, memory_format=torch.contiguous_format) for t in ((q,) if k is None else (q, k)))
         qo, ldqo = outs[0].data_ptr(), H * D
         if k is not None:
             ko, ldko = outs[1].data_ptr(), K * D
@@ -939,7 +939,7 @@ class Checkpoint8:
     def _like(cls, x: torch.Tensor):
         """A new one for rows like x, and its addresses."""
         m, C = x.shape
-        codes = x.new_empty((m, C), dtype=torch.int8)
+        codes = torch.empty_like(x, dtype=torch.int8, memory_format=torch.contiguous_format)
         exps = x.new_empty((m, (C + SPV_CHECKPOINT8_BLOCK - 1) // SPV_CHECKPOINT8_BLOCK), dtype=torch.uint8)
         return cls(codes, exps, x.dtype), codes.data_ptr(), exps.data_ptr()
 
@@ -975,7 +975,7 @@ def spv_checkpoint8_read(saved: Checkpoint8, m_dev: Optional[torch.Tensor] = Non
     codes, exps = saved.addresses(dev)
     m, C = saved.codes.shape
     if out is None:
-        out = saved.codes.new_empty((m, C), dtype=saved.dtype)
+        out = torch.empty_like(saved.codes, dtype=saved.dtype)
     elif out.shape != (m, C) or out.dtype != saved.dtype:
         raise ValueError("out must have the rows' shape and type")
     op, count = _at(out, dev), _count(m_dev, dev)
@@ -1028,7 +1028,7 @@ def spv_group_norm(ws: Workspace, x: torch.Tensor, off: torch.Tensor, groups: in
         out = torch.empty_like(x)
     elif out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("out must have x's shape and type")
-    stat = torch.empty((B, groups, 2), dtype=torch.float32, device=x.device) if want_stat else None
+    stat = x.new_empty((B, groups, 2), dtype=torch.float32) if want_stat else None
     saved, codes, exps = Checkpoint8._like(x) if want_checkpoint else (None, None, None)
     st = lib().spv_group_norm(_stream_of(dev), ws.ptr, ws.nbytes, xp, m, C, _at(off, dev), B, groups, gp, bp, eps,
                               _ACT[act], _at(out, dev), _at(stat, dev), codes, exps, _DT[x.dtype])
