@@ -35,15 +35,17 @@ def _rows(t: torch.Tensor, width: int, dtype: torch.dtype, name: str, rows: Opti
 
 class ScanLayer:
     """What the layers over packed scans share: calls on several streams or from several threads may overlap, as a layer
-    keeps workspaces for each.  Graphs captured on one stream use that stream's: their replays must not overlap each other
-    or its calls."""
+    keeps workspaces for each.  A captured call's are its graph's own, like the tensors it makes: kept ones would be another
+    graph's too, and let go for larger ones while a graph still writes to them."""
 
     def __init__(self):
         self.ws: Dict[tuple, tuple] = {}
 
     def _ws(self, name: str, sizes: tuple, make) -> spv.Workspace:
         """The current stream's and thread's workspace `name` for a call of these sizes: the last one where it served
-        them, or is large enough."""
+        them, or is large enough.  Under capture a new one, from the graph's memory."""
+        if torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing():
+            return make()
         key = (name, spv._stream().value, threading.get_ident())
         last = self.ws.get(key)
         if last is None or last[0] != sizes:

@@ -233,6 +233,42 @@ def test_a_training_step_of_both_layers_in_a_graph(spv):
         torch.cuda.synchronize()
 
 
+def test_two_graphs_on_the_stream_of_larger_eager_calls(spv):
+    """Two steps captured on a stream that has run the layer eagerly, and runs it on more rows afterwards: replays write to
+    nothing that others have taken since, and do not mix."""
+    from paper_2007_16100_amd.scan_mlp import ScanMLP
+    C, r = 96, draws(3, "bf16")
+    mlp = ScanMLP(mlp_params(C, 192, "bf16", 2), 8, keep8=True)
+
+    def step(x, off, dy):
+        saved = {}
+        return [mlp.forward(x, off, save=saved), *mlp.backward(saved, dy).values()]
+    small = [(r(n, C), torch.tensor([0, n // 3, n], dtype=torch.int32).cuda(), r(n, C)) for n in (701, 450)]
+    large = (r(9001, C), torch.tensor([0, 9001], dtype=torch.int32).cuda(), r(9001, C))
+    torch.cuda.synchronize()
+    s, graphs, got = torch.cuda.Stream(), [], []
+    with torch.cuda.stream(s):
+        want = [[t.clone() for t in step(*a)] for a in small]
+    s.synchronize()
+    for a in small:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            got.append(step(*a))
+        graphs.append(g)
+    with torch.cuda.stream(s):
+        step(*large)
+        taken = [torch.full((k << 10,), 7, dtype=torch.uint8, device="cuda") for k in (16, 64, 256, 1024) for _ in range(24)]
+        for _ in range(3):
+            for g in graphs:
+                g.replay()
+            s.synchronize()
+            for a, b in zip(got, want):
+                assert all(torch.equal(x, y) for x, y in zip(a, b))
+            assert all(bool((t == 7).all()) for t in taken)
+            step(*large)
+    s.synchronize()
+
+
 def test_layers_on_scans_without_voxels(spv):
     """A batch of which nothing is left: outputs and gradients of no rows, weight gradients of zeros."""
     from paper_2007_16100_amd.scan_attention import ScanAttention

@@ -70,10 +70,10 @@ def test_rotary_positions_without_coordinates(no_calls):
             layer.forward(x, off, **kw)
 
 
-def test_one_workspace_a_stream_and_thread(monkeypatch):
-    """The calls of a step, replaced by ones that note their workspace: two streams' and two threads' are apart."""
+@pytest.fixture
+def workspaces(monkeypatch):
+    """(log, step): a step of a layer whose calls are replaced by ones that note their workspace, in order of use."""
     import ctypes as ct
-    import threading
     import types
     log = types.SimpleNamespace(used=[], stream=ct.c_void_p(None))
 
@@ -103,7 +103,15 @@ def test_one_workspace_a_stream_and_thread(monkeypatch):
         saved, x = {}, torch.zeros(5, 8)
         layer.forward(x, torch.tensor([0, 5], dtype=torch.int32), save=saved)
         layer.backward(saved, x)
-        return [id(w) for w in log.used]
+        return list(log.used)
+    return log, step
+
+
+def test_one_workspace_a_stream_and_thread(workspaces):
+    """Two streams' and two threads' workspaces are apart."""
+    import ctypes as ct
+    import threading
+    log, step = workspaces
     first = step()
     assert first and step() == first
     log.stream = ct.c_void_p(4096)
@@ -114,3 +122,15 @@ def test_one_workspace_a_stream_and_thread(monkeypatch):
     t.start()
     t.join()
     assert len(got) == len(first) and not set(first) & set(got)
+
+
+def test_captured_calls_have_workspaces_of_their_own(workspaces, monkeypatch):
+    """A capture takes no workspace that the layer keeps, nor another capture's, and leaves none behind for later calls."""
+    log, step = workspaces
+    first, capturing = step(), [True]
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    one, two = step(), step()
+    assert not set(first) & set(one) and not set(first) & set(two) and not set(one) & set(two)
+    capturing[0] = False
+    assert step() == first
