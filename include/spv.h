@@ -777,7 +777,7 @@ typedef enum spv_act {
  *      x in 8 bits as spv_checkpoint8 gives it (rows of a scan), or both NULL.
  *      ws: spv_group_norm_workspace_bytes(m, C, G, B) bytes, 256-byte aligned.
  * Errors: SPV_ERR_INVALID_ARG (null pointers, sizes, eps, act, C % G,
- *      aliasing), SPV_ERR_CAPACITY, SPV_ERR_UNSUPPORTED (C > 65536, B > 2^24, B * G > 2^32).
+ *      aliasing), SPV_ERR_CAPACITY, SPV_ERR_UNSUPPORTED (C > 65536, B > 2^22, B * G > 2^25).
  *
  * spv_group_norm_backward -- with xh = (x - mu) r, z = xh gamma + beta, gz = dy act'(z),
  * h = gz gamma and means over a scan's rows and a group's channels:

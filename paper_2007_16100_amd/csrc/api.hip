@@ -967,10 +967,10 @@ spv_status spv_linear_backward8(void* stream, void* ws, size_t ws_bytes, const i
     return hip_check();
 }
 
-// sizes that both directions of the group norm take
+// sizes that both directions of the group norm take: a launch has room for 2^32 threads, 512 a scan, 64 one of its groups
 static spv_status group_norm_sizes(int64_t m, int32_t C, int32_t G, int32_t B, spv_dtype dt) {
     if (!rows_ok(m, C, dt) || G <= 0 || C % G || B < 0) return SPV_ERR_INVALID_ARG;
-    return C > 65536 || B > (1 << 24) || (int64_t)B * G > ((int64_t)1 << 32) ? SPV_ERR_UNSUPPORTED : SPV_OK;
+    return C > 65536 || B > (1 << 22) || (int64_t)B * G > (1 << 25) ? SPV_ERR_UNSUPPORTED : SPV_OK;
 }
 static GnArgs group_norm_args(int64_t m, int32_t C, int32_t G, int32_t B, spv_dtype dt) {
     GnArgs t{};

@@ -64,7 +64,7 @@ template <int DT>
 __global__ __launch_bounds__(256) void k_code8(const void* x, Saved8 to, RowRange rows, int C) {
     constexpr int V = kCodeVec<DT>, LANES = kCodeBlock / V;
     const int64_t per = C / V, end = rows.end() * per;  // vectors
-    const int64_t t0 = rows.begin() * per + (int64_t)blockIdx.x * (256 * kCodeAhead) + threadIdx.x;
+    const int64_t t0 = rows.begin() * per + group_of_grid() * (256 * kCodeAhead) + threadIdx.x;
     uint4 u[kCodeAhead];
 #pragma unroll
     for (int k = 0; k < kCodeAhead; ++k) {
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void k_code8(const void* x, Saved8 to, RowRang
 template <int DT>
 __global__ __launch_bounds__(256) void k_code8_read(Saved8 from, void* out, RowRange rows, int C) {
     constexpr int V = kCodeVec<DT>, LANES = kCodeBlock / V;
-    const int64_t end = rows.end() * (C / V), t0 = (int64_t)blockIdx.x * (256 * kCodeAhead) + threadIdx.x;
+    const int64_t end = rows.end() * (C / V), t0 = group_of_grid() * (256 * kCodeAhead) + threadIdx.x;
     uint32_t w[kCodeAhead][V / 4];
     int e[kCodeAhead];
 #pragma unroll
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256) void k_code8_short(const void* x, Saved8 to, R
     constexpr int V = kCodeVec<DT>, LANES = kCodeBlock / V;
     const int nb = code_blocks(C), per = nb * LANES, R = 256 / per, row = (int)threadIdx.x / per, v = (int)threadIdx.x - row * per;
     if (row >= R) return;  // whole blocks
-    const int64_t end = rows.end(), i0 = rows.begin() + (int64_t)blockIdx.x * (R * kCodeAhead) + row;
+    const int64_t end = rows.end(), i0 = rows.begin() + group_of_grid() * (R * kCodeAhead) + row;
     const bool on = v * V < C;
     uint4 u[kCodeAhead];
 #pragma unroll
@@ -138,7 +138,7 @@ template <int DT>
 __global__ __launch_bounds__(256) void k_code8_read_short(Saved8 from, void* out, RowRange rows, int C) {
     constexpr int V = kCodeVec<DT>, LANES = kCodeBlock / V;
     const int nb = code_blocks(C), per = C / V, R = 256 / per, row = (int)threadIdx.x / per, v = (int)threadIdx.x - row * per;
-    const int64_t end = rows.end(), i0 = (int64_t)blockIdx.x * (R * kCodeAhead) + row;
+    const int64_t end = rows.end(), i0 = group_of_grid() * (R * kCodeAhead) + row;
     uint32_t w[kCodeAhead][V / 4];
     int e[kCodeAhead];
 #pragma unroll
@@ -171,13 +171,13 @@ static unsigned grid_rows(int64_t m) {
     return (unsigned)(g < 1 ? 1 : g > 16384 ? 16384 : g);
 }
 template <int DT>
-static unsigned grid_vecs(int64_t m, int C) {
+static dim3 grid_vecs(int64_t m, int C) {
     const int64_t per = 256 * kCodeAhead;
-    return (unsigned)((m * (C / kCodeVec<DT>) + per - 1) / per);
+    return grid_of((m * (C / kCodeVec<DT>) + per - 1) / per);
 }
-static unsigned grid_short(int64_t m, int threads) {
+static dim3 grid_short(int64_t m, int threads) {
     const int64_t rows = 256 / threads * kCodeAhead;
-    return (unsigned)((m + rows - 1) / rows);
+    return grid_of((m + rows - 1) / rows);
 }
 template <int DT>
 static void code8(hipStream_t s, const void* x, const Saved8& to, const RowRange& rows, int C) {

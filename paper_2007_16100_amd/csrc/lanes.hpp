@@ -6,6 +6,15 @@
 
 namespace spv {
 
+// A launch's axis has room for 2^32 threads: workgroups of 256 are laid out in lines of 2^23.  Those past the last find
+// nothing to do.  (The length of a line read from the launch instead cost 300,007 x 96 into 8 bits and back 1.7 us of 29.)
+constexpr int kGridLine = 23;
+inline dim3 grid_of(int64_t groups) {
+    const int64_t line = (int64_t)1 << kGridLine;
+    return groups <= line ? dim3((unsigned)(groups < 1 ? 1 : groups)) : dim3((unsigned)line, (unsigned)((groups + line - 1) >> kGridLine));
+}
+__device__ inline int64_t group_of_grid() { return ((int64_t)blockIdx.y << kGridLine) + blockIdx.x; }
+
 template <int CTRL>
 __device__ inline int dpp(int v) {
     return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, true);

@@ -55,7 +55,7 @@ template <int DT, bool HALVES>
 __global__ __launch_bounds__(256) void k_rope_rows(RopeArgs a, RopeUnits un) {
     constexpr int V = DT == SPV_F32 ? 4 : 8, NV = HALVES ? 2 : 1;
     extern __shared__ float2 table[];  // [rows][P]
-    const int64_t m = clamp_rows(a.m_dev, a.n), row0 = (int64_t)blockIdx.x * un.rows;
+    const int64_t m = clamp_rows(a.m_dev, a.n), row0 = group_of_grid() * un.rows;
     if (row0 >= m) return;
     const int rows = (int)(m - row0 < un.rows ? m - row0 : un.rows), all = rows * un.row;
     struct Unit {
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256) void k_rope_rows(RopeArgs a, RopeUnits un) {
 template <int DT>
 __global__ __launch_bounds__(256) void k_rope_pairs(RopeArgs a, RopeUnits un) {
     extern __shared__ float2 table[];  // [rows][P]
-    const int64_t m = clamp_rows(a.m_dev, a.n), row0 = (int64_t)blockIdx.x * un.rows;
+    const int64_t m = clamp_rows(a.m_dev, a.n), row0 = group_of_grid() * un.rows;
     if (row0 >= m) return;
     const int rows = (int)(m - row0 < un.rows ? m - row0 : un.rows), all = rows * un.row;
     rope_table(a, row0, rows, table);
@@ -189,7 +189,7 @@ static void rope(hipStream_t s, const RopeArgs& a) {
     };
     u.by_row = by(u.row, (int64_t)u.rows * u.row);
     u.by_head = by(u.head, u.row);
-    const unsigned g = (unsigned)((a.n + u.rows - 1) / u.rows);
+    const dim3 g = grid_of((a.n + u.rows - 1) / u.rows);
     const size_t lds = (size_t)u.rows * a.P * sizeof(float2);  // 32 KiB at most
     if (!wide) k_rope_pairs<DT><<<g, 256, lds, s>>>(a, u);
     else if (a.halves) k_rope_rows<DT, true><<<g, 256, lds, s>>>(a, u);

@@ -69,3 +69,62 @@ def test_rotary_positions(spv):
     want = spv.spv_rope(p, c[-LAST:].contiguous(), q[-LAST:].contiguous())
     got = spv.spv_rope(p, c, q, outs=(q,))
     assert torch.equal(got[-LAST:], want) and not bool(got[:-LAST].any())
+
+
+def test_more_workgroups_than_an_axis_of_the_grid_holds(spv):
+    """2^24 workgroups of 256 threads and more: short heads, and float32 rows of one vector."""
+    n = (1 << 30) + 1000
+    q = torch.zeros(n, 1, 8, dtype=torch.bfloat16, device="cuda")
+    c = torch.zeros(n, 4, dtype=torch.int32, device="cuda")
+    p = spv.make_rope_params(8, spv.rope_freqs((2, 1, 1)), (2, 1, 1))
+    places = (0, (1 << 29) - LAST, 1 << 29, n - LAST)
+    for i, r0 in enumerate(places):
+        q[r0:r0 + LAST] = rows(5 + i, (LAST, 1, 8))
+        c[r0:r0 + LAST] = torch.randint(-500, 500, (LAST, 4), generator=torch.Generator().manual_seed(i), dtype=torch.int32).cuda()
+    want = [spv.spv_rope(p, c[r0:r0 + LAST].contiguous(), q[r0:r0 + LAST].contiguous()) for r0 in places]
+    spv.spv_rope(p, c, q, outs=(q,))
+    for r0, w in zip(places, want):
+        assert torch.equal(q[r0:r0 + LAST], w)
+    del q, c
+    m = (1 << 31) - 1
+    x = torch.zeros(m, 4, device="cuda")
+    places = (0, (1 << 30) - LAST, 1 << 30, m - LAST)
+    for i, r0 in enumerate(places):
+        x[r0:r0 + LAST] = rows(9 + i, (LAST, 4), torch.float32)
+    saved = spv.spv_checkpoint8(x)
+    want = [spv.spv_checkpoint8(x[r0:r0 + LAST].contiguous()) for r0 in places]
+    for r0, w in zip(places, want):
+        assert torch.equal(saved.codes[r0:r0 + LAST], w.codes) and torch.equal(saved.exps[r0:r0 + LAST], w.exps)
+    spv.spv_checkpoint8_read(saved, out=x)
+    for r0, w in zip(places, want):
+        assert torch.equal(x[r0:r0 + LAST], spv.spv_checkpoint8_read(w))
+
+
+def test_group_norm_of_as_many_scans_as_it_takes(spv):
+    """2^22 scans of one row and two by turns: the first and the last ones are what they are alone."""
+    B, G, E = 1 << 22, 2, 2.0 ** -24
+    off = (torch.arange(B + 1) * 3 // 2).to(torch.int32).cuda()
+    m = B * 3 // 2
+    x = torch.randn(m, 8, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    ws = spv.Workspace.for_group_norm_backward(m, 8, G, B)
+    y, stat = spv.spv_group_norm(ws, x, off, G, want_stat=True)
+    dx, dgamma, dbeta = spv.spv_group_norm_backward(ws, x, x, off, G, stat)
+    for r0, b in ((0, 0), (m - 3000, B - 2000)):
+        o, few, st = (off[b:b + 2001] - r0).contiguous(), x[r0:r0 + 3000].contiguous(), stat[b:b + 2000].contiguous()
+        w = spv.Workspace.for_group_norm_backward(3000, 8, G, 2000)
+        yw, sw = spv.spv_group_norm(w, few, o, G, want_stat=True)
+        X, Y, R = float(few.abs().max()), float(yw.abs().max()), float(sw[..., 1].max())
+        # of 8 values at most: a mean and a deviation off by d, r by d R + 16 E of itself, each side
+        d = 10 * E * X
+        assert (st[..., 0] - sw[..., 0]).abs().max() <= 2 * d
+        assert ((st[..., 1] - sw[..., 1]) / sw[..., 1]).abs().max() <= 2 * (d * R + 16 * E)
+        assert (y[r0:r0 + 3000] - yw).abs().max() <= 2 * (R * d + (d * R + 16 * E) * Y)
+        # from the same stat: xh = x r - mu r off by h, the means by 8 E X and X h + 8 E X Y
+        h = 3 * E * X * R
+        dw = spv.spv_group_norm_backward(w, few, few, o, G, st)[0]
+        assert (dx[r0:r0 + 3000] - dw).abs().max() <= 2 * R * X * (9 * E + 2 * h * Y + 8 * E * Y * Y + 4 * E * (2 + Y * Y))
+    mu, r = (t.repeat_interleave(off.diff().long(), 0).repeat_interleave(4, 1).double() for t in (stat[..., 0], stat[..., 1]))
+    xd, yd = x.double(), y.double()
+    # a term x xh: xh off by roundings of x r, of mu r and of itself
+    assert ((dgamma.double() - (xd * yd).sum(0)).abs() <= 8 * E * (xd.abs() * ((xd.abs() + mu.abs()) * r + yd.abs())).sum(0)).all()
+    assert ((dbeta.double() - xd.sum(0)).abs() <= 8 * E * xd.abs().sum(0)).all()

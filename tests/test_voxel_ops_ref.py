@@ -157,6 +157,7 @@ def test_group_norm_refusals():
         assert f(nb=8) == spv.SPV_ERR_CAPACITY
         assert f(C=65538, G=1) == spv.SPV_ERR_UNSUPPORTED
         assert f(B=(1 << 24) + 1) == spv.SPV_ERR_UNSUPPORTED
+        assert f(B=(1 << 22) + 1) == f(B=1 << 17, C=512, G=512) == spv.SPV_ERR_UNSUPPORTED  # past a launch's 2^32 threads
     assert fwd(B=0, off=None) == spv.SPV_OK
     for f in (L.spv_group_norm_workspace_bytes, L.spv_group_norm_backward_workspace_bytes):
         assert f(10, 8, 3, 1) == 0 and f(-1, 8, 2, 1) == 0 and f(0, 8, 2, 0) >= 0
