@@ -472,11 +472,13 @@ struct GnSource {
     }
 };
 
-// r and -mean r of a thread's channels, so that xh is one fma (off by a rounding of mean r, as by one of the mean)
+// Mean and r of a thread's channels.  Both kernels form x - mean first, as the forward does: it is 0 where a group's values
+// are equal, and z is beta there.  (x r - mean r in one step leaves the rounding of mean r instead, of either sign, and
+// ReLU then lets half of such groups' gradients through.)
 template <int VEC>
 __device__ inline void gn_stat(const GnArgs& a, int b, int c, float (&mu)[VEC], float (&r)[VEC]) {
     gn_of_groups<VEC>(a.sh, (const float2*)a.stat + (int64_t)b * a.G, c,
-                      [&](int e, const float2& st) { r[e] = st.y, mu[e] = -st.x * st.y; });
+                      [&](int e, const float2& st) { mu[e] = st.x, r[e] = st.y; });
 }
 
 // a tile's sums of gz and gz xh, of each channel and (times gamma) of each group
@@ -495,17 +497,17 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
         return;
     }
     if (row < R) {
-        float mu[VEC], r[VEC], ga[VEC], be[VEC], s1[VEC], s2[VEC];
+        float mu[VEC], r[VEC], gr[VEC], be[VEC], s1[VEC], s2[VEC];
         const int64_t base = t.row0 * a.C + c, block = t.row0 * code_blocks(a.C) + c / kCodeBlock;
         auto load = [&](int i) { return S::load(a, base, block, i); };
         constexpr int U = gn_ahead(VEC, 2);
         GnRows<U, typename S::Raw> rows{row, R, t.rows};
-        gn_channels<VEC>(a.gamma, c, 1.f, ga);
+        rows.ask(row, rows.u, load);
+        gn_channels<VEC>(a.gamma, c, 1.f, gr);
         gn_channels<VEC>(a.beta, c, 0.f, be);
         gn_stat<VEC>(a, t.b, c, mu, r);
-        rows.ask(row, rows.u, load);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) s1[e] = s2[e] = 0.f;
+        for (int e = 0; e < VEC; ++e) gr[e] *= r[e], s1[e] = s2[e] = 0.f;
         rows.run(load, [&](int i0, const typename S::Raw(&u)[U]) {
 #pragma unroll
             for (int k = 0; k < U; ++k) {
@@ -515,16 +517,16 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_sums(GnArgs a, int tile_
                 S::unpack(u[k].x, x);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const float xh = fmaf(x[e], r[e], mu[e]), gz = act_grad<ACT>(d[e], fmaf(xh, ga[e], be[e]));
+                    const float dev = x[e] - mu[e], gz = act_grad<ACT>(d[e], fmaf(dev, gr[e], be[e]));
                     s1[e] += gz;
-                    s2[e] = fmaf(gz, xh, s2[e]);
+                    s2[e] = fmaf(gz, dev, s2[e]);
                 }
             }
         });
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             s_sum[row * a.C + c + e] = s1[e];
-            s_sum[N + row * a.C + c + e] = s2[e];
+            s_sum[N + row * a.C + c + e] = s2[e] * r[e];  // r once a channel
         }
     }
     __syncthreads();
@@ -616,10 +618,10 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
     constexpr int U = gn_ahead(VEC, 2);
     GnRows<U, typename S::RawRes> rows{row, R, row < R ? t.rows : 0};
     float mu[VEC], r[VEC], ga[VEC], be[VEC], m1[VEC], m2[VEC];
+    if (row < R) rows.ask(row, rows.u, load);
     gn_channels<VEC>(a.gamma, c, 1.f, ga);
     gn_channels<VEC>(a.beta, c, 0.f, be);
     gn_stat<VEC>(a, t.b, c, mu, r);
-    if (row < R) rows.ask(row, rows.u, load);
     gn_join_all(a, t, tile_rows, first, s_mean, [&](GnGroup& g) { return gn_join_sums(g, t.n, w); });
     __syncthreads();
     if (row >= R) return;
@@ -634,7 +636,7 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
             if (a.dres) V::unpack(u[k].res, q);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const float xh = fmaf(x[e], r[e], mu[e]);
+                const float xh = (x[e] - mu[e]) * r[e];
                 const float h = act_grad<ACT>(d[e], fmaf(xh, ga[e], be[e])) * ga[e];
                 d[e] = fmaf(r[e], fmaf(-xh, m2[e], h - m1[e]), q[e]);
             }

@@ -231,3 +231,63 @@ def test_group_norm_on_another_stream_and_in_a_graph(spv):
         torch.cuda.synchronize()
         want, _ = step(spv, x, dy, res, g, b, off, G, "silu", True)
         assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+def equal_values(lens, C, G, seed, scale=1.0):
+    """Rows whose groups hold one value each a scan, a whole number of 64 .. 127 (either sign) times scale / 16: exact in every
+    type, and in 8 bits for powers of two."""
+    g = torch.Generator().manual_seed(seed)
+    v = torch.randint(64, 128, (len(lens), G), generator=g) * (1 - 2 * torch.randint(0, 2, (len(lens), G), generator=g))
+    return (v.double() * (scale / 16.0)).repeat_interleave(C // G, 1).repeat_interleave(torch.tensor(lens), 0)
+
+
+def check_equal(spv, x, dy, res, gamma, beta, off, G, act, ckpt, dtype):
+    """A group of equal values has xh = 0 to the last bit, in the forward and in the backward: y = act(beta), dgamma = 0, and
+    without beta ReLU lets no gradient through; the others' slopes at 0 are 1 and 1/2."""
+    m, C = x.shape
+    (y, stat, dx, dg, db), _ = step(spv, x, dy, res, gamma, beta, off, G, act, ckpt)
+    assert not bool(y.any()) and not bool(dg.any())
+    o, E = off.tolist(), ref.EPS
+    full = torch.tensor([b > a for a, b in zip(o, o[1:])], device="cuda")
+    r = 1.0 / np.sqrt(1e-5)
+    assert bool(((stat[full][..., 1].double() - r).abs() <= 4 * E * r).all())
+    if act == "relu":
+        assert not bool(db.any())
+        assert torch.equal(dx, torch.zeros_like(dx) if res is None else res)
+        return
+    slope = {"none": 1.0, "silu": 0.5}[act]
+    gz = arr(dy) * slope
+    h = gz * (1.0 if gamma is None else arr(gamma))
+    steps = 3 * min(m, 1024) + 16  # of a sum, as in the reference
+    tol = E * (steps + 8) * np.abs(gz).sum(0) + ref.TINY["f32"]
+    within(db, gz.sum(0), tol, "dbeta")
+    for i, j in zip(o, o[1:]):
+        if j <= i:
+            continue
+        t = h[i:j].reshape(j - i, G, C // G)
+        mean, size = (f(t).mean((0, 2), keepdims=True) for f in (np.asarray, np.abs))
+        want = (r * (t - mean)).reshape(j - i, C)
+        err = r * (E * (steps + 16) * size + 8 * E * np.abs(t)).reshape(j - i, C) + 8 * E * np.abs(want)
+        if res is not None:
+            want = want + arr(res[i:j])
+            err = err + E * np.abs(want)
+        within(dx[i:j], want, err + ref.UNIT[dtype] * (np.abs(want) + err) + ref.TINY[dtype], "dx")
+
+
+# scans of one row, of a few and of many tiles; vectors and elements, and rows too wide for a workgroup
+EQUAL = [(96, 1, [1] * 40 + [700, 0, 5]), (96, 8, [3, 1, 2000, 1]), (96, 96, [1, 0, 3000, 2]), (96, 96, [1] * 300), (19, 19, [1, 900]),
+         (51, 3, [1, 700, 0, 2]), (256, 16, [2500, 1]), (1030, 515, [1, 40, 2])]
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("act", ["relu", "silu", "none"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_equal_values_have_no_deviation_in_the_backward(spv, dtype, act, ckpt):
+    for k, (C, G, lens) in enumerate(EQUAL):
+        m = sum(lens)
+        print(f"equal values C={C} G={G} {dtype} {act} {ckpt}", flush=True)
+        x = equal_values(lens, C, G, 31 + k).to(TD[dtype]).cuda()
+        _, dy, res, gamma, beta = inputs(m, C, dtype, 7 + k)
+        gamma = gamma * torch.where(beta > 0, 1.0, -1.0)
+        for p in ((gamma, None, res), (None, torch.zeros_like(beta), None)):
+            check_equal(spv, x, dy, p[2], p[0], p[1], offsets(lens), G, act, ckpt, dtype)
