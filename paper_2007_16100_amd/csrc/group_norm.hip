@@ -309,10 +309,10 @@ __device__ inline void gn_units(const GnArgs& a, int rows, const float2* val) {
         }
         const float mu = fmaf(lanes_sum<L>(s), inv, first);
         for (int j = l; j < all; j += L) {
-            const int r = over(j, sh.by_per);
+            const int r = over(j, sh.by_per), n = least + (r < more);
             const float2 p = v[r * units + (j - r * per)];
-            const float d = p.x - mu;
-            q += fmaf(d * d, (float)((least + (r < more)) * sh.unit), p.y);
+            const float d = n ? p.x - mu : 0.f;  // a unit of no rows: mu's square may be infinite
+            q += fmaf(d * d, (float)(n * sh.unit), p.y);
         }
         q = lanes_sum<L>(q);
         if (l == 0 && g < a.G) a.tiles[(int64_t)blockIdx.x * a.G + g] = make_float2(mu, q);

@@ -291,3 +291,16 @@ def test_equal_values_have_no_deviation_in_the_backward(spv, dtype, act, ckpt):
         gamma = gamma * torch.where(beta > 0, 1.0, -1.0)
         for p in ((gamma, None, res), (None, torch.zeros_like(beta), None)):
             check_equal(spv, x, dy, p[2], p[0], p[1], offsets(lens), G, act, ckpt, dtype)
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("act", ["relu", "silu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_equal_values_in_tiles_of_few_rows(spv, dtype, act, ckpt):
+    """Values whose squares float32 does not hold (some 5e20), in tiles that have fewer rows than a workgroup takes at a time."""
+    for k, (C, G, lens) in enumerate([(96, 1, [3, 1, 2000, 1]), (96, 8, [5, 2500, 2]), (36, 4, [1, 4000, 7]), (51, 3, [1, 1500, 2])]):
+        m = sum(lens)
+        print(f"large equal values C={C} G={G} {dtype} {act} {ckpt}", flush=True)
+        x = equal_values(lens, C, G, 51 + k, 2.0 ** 66).to(TD[dtype]).cuda()
+        _, dy, res, gamma, _ = inputs(m, C, dtype, 17 + k)
+        check_equal(spv, x, dy, res, gamma, None, offsets(lens), G, act, ckpt, dtype)
