@@ -346,7 +346,8 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_
                 const float f = 4.f * __builtin_amdgcn_rcpf(n + 4.f), g = n * f;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const float mu = ((x[0][e] + x[1][e]) + (x[2][e] + x[3][e])) * 0.25f;
+                    // from the first: equal values give their mean exactly, the type's largest and smallest too
+                    const float mu = fmaf((x[1][e] - x[0][e]) + ((x[2][e] - x[0][e]) + (x[3][e] - x[0][e])), 0.25f, x[0][e]);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const float d = x[k][e] - mu;

@@ -304,3 +304,17 @@ def test_large_equal_values_in_tiles_of_few_rows(spv, dtype, act, ckpt):
         x = equal_values(lens, C, G, 51 + k, 2.0 ** 66).to(TD[dtype]).cuda()
         _, dy, res, gamma, _ = inputs(m, C, dtype, 17 + k)
         check_equal(spv, x, dy, res, gamma, None, offsets(lens), G, act, ckpt, dtype)
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("act", ["relu", "none"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_equal_values_at_the_end_of_the_type(spv, dtype, act, ckpt):
+    """Values of 1.7e38 to 3.37e38, where float32 and bf16 end (3.40e38 and 3.39e38): not even two add up in float32."""
+    for k, (C, G, lens) in enumerate([(96, 8, [1, 2500, 3]), (96, 96, [1, 3, 700]), (51, 3, [1, 1500, 4]), (36, 36, [40, 9, 1])]):
+        m = sum(lens)
+        print(f"equal values at the end C={C} G={G} {dtype} {act} {ckpt}", flush=True)
+        x = equal_values(lens, C, G, 71 + k, 2.0 ** 125).to(TD[dtype]).cuda()
+        assert bool(torch.isfinite(x).all()) and float(x.abs().min()) > 1.7e38
+        _, dy, res, gamma, _ = inputs(m, C, dtype, 27 + k)
+        check_equal(spv, x, dy, res, gamma, None, offsets(lens), G, act, ckpt, dtype)
