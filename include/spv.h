@@ -775,7 +775,8 @@ typedef enum spv_act {
  * Out: out [m][C] (dt; may be x), rows of no scan not written; stat [B][G][2] f32 or
  *      NULL: mu and r, the backward's input (0 for a scan without rows); codes, exps:
  *      x in 8 bits as spv_checkpoint8 gives it (rows of a scan), or both NULL.
- *      ws: spv_group_norm_workspace_bytes(m, C, G, B) bytes, 256-byte aligned.
+ *      ws: spv_group_norm_workspace_bytes(m, C, G, B) bytes, 256-byte aligned (never
+ *      fewer for more rows or scans, so one for the largest batch serves every other).
  * Errors: SPV_ERR_INVALID_ARG (null pointers, sizes, eps, act, C % G,
  *      aliasing), SPV_ERR_CAPACITY, SPV_ERR_UNSUPPORTED (C > 65536, B > 2^22, B * G > 2^25).
  *
@@ -789,7 +790,7 @@ typedef enum spv_act {
  * In:  dy, dres (or NULL) [m][C] (dt).
  * Out: dx [m][C] (dt; may be dy or dres; rows of no scan not written), dgamma, dbeta
  *      [C] f32 (0 without rows); any may be NULL.
- *      ws: spv_group_norm_backward_workspace_bytes(m, C, G, B) bytes.
+ *      ws: spv_group_norm_backward_workspace_bytes(m, C, G, B) bytes, likewise.
  * Errors: as spv_group_norm; x and codes both given or both missing.
  */
 size_t spv_group_norm_workspace_bytes(int64_t m, int32_t C, int32_t G, int32_t B);

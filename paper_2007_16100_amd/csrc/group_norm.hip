@@ -854,11 +854,18 @@ __global__ __launch_bounds__(256) void k_gn_params(GnArgs a) {
 // ---------------------------------------------------------------------------
 
 // Rows of a tile: kGnTiles tiles for a long scan, and 8192 values at least, a few rows a thread.
+static int64_t gn_least_rows(int C) { return (8191 + C) / C; }
 static int gn_tile_rows(int64_t m, int C) {
-    const int64_t few = (8191 + C) / C, many = (m + kGnTiles - 1) / kGnTiles;
+    const int64_t few = gn_least_rows(C), many = (m + kGnTiles - 1) / kGnTiles;
     return (int)(few > many ? few : many);
 }
 static int64_t gn_tiles(int64_t m, int C, int B) { return m / gn_tile_rows(m, C) + B; }
+// Room in the workspace: no fewer, and never less for more rows (gn_tiles falls where a tile gets a row more), so that a
+// workspace for the largest batch serves every smaller one.
+static size_t gn_room(int64_t m, int C, int B) {
+    const int64_t t = m / gn_least_rows(C);
+    return (size_t)((t < kGnTiles ? t : kGnTiles) + B);
+}
 // A workgroup joins its scan's tiles itself: up to 32 of them by 8 lanes a group, 64 groups at a time (2000 x 96 in
 // 96 groups takes 14.5 us, 23.5 by a wave a group and 15.3 by a launch of its own), more by a wave, up to twice over.
 // Beyond, a launch of its own is shorter: 100,000 x 96 in bf16 15.4 against 17.1 us with 8 groups, 18.5 and 17.9 with
@@ -887,13 +894,13 @@ static GnShape gn_shape(int C, int G, int vec) {
 }
 
 static void gn_ws(Arena& a, GnArgs& t) {
-    t.tiles = a.take<float2>((size_t)gn_tiles(t.m, t.C, t.B) * t.G);
+    t.tiles = a.take<float2>(gn_room(t.m, t.C, t.B) * t.G);
     t.joined = a.take<float2>((size_t)t.B * t.G);
 }
 void plan_group_norm_ws(Arena& a, GnArgs& t) { gn_ws(a, t); }
 void plan_group_norm_backward_ws(Arena& a, GnArgs& t) {
     gn_ws(a, t);
-    t.part = a.take<float>((size_t)gn_tiles(t.m, t.C, t.B) * 2 * t.C);
+    t.part = a.take<float>(gn_room(t.m, t.C, t.B) * 2 * t.C);
 }
 
 template <int V>

@@ -211,3 +211,15 @@ def test_tensors_of_another_device(monkeypatch):
               lambda: spv.spv_rope(p, c, x.view(6, 2, 32))):
         with pytest.raises(ValueError, match="current device"):
             f()
+
+
+@built
+@pytest.mark.parametrize("C,G,B", [(96, 8, 1), (96, 8, 4), (96, 96, 3), (4096, 1, 1), (19, 19, 2), (1, 1, 1), (5000, 5, 2)])
+def test_a_workspace_for_more_rows_serves_fewer(C, G, B):
+    """The bytes asked for never fall as rows are added: a program makes its workspace once, for its largest batch."""
+    L = spv.lib()
+    rows = sorted({*range(3000), *(240 * k + d for k in range(12, 1300) for d in (-1, 0, 1)), *(1 << k for k in range(12, 31))})
+    for f in (lambda m: L.spv_group_norm_workspace_bytes(m, C, G, B), lambda m: L.spv_group_norm_backward_workspace_bytes(m, C, G, B),
+              lambda m: L.spv_linear_backward8_workspace_bytes(m, min(C, 256), 64)):
+        sizes = [f(m) for m in rows]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[0] > 0
