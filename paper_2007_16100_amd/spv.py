@@ -847,6 +847,13 @@ def _at(t: Optional[torch.Tensor], dev: int):
     return t.data_ptr()
 
 
+def _ws_at(ws: Workspace, dev: int):
+    """Address of a workspace on device dev."""
+    if ws.buf.get_device() != dev:
+        raise ValueError(f"libspv takes a workspace of the current device, cuda:{dev}")
+    return ws.ptr
+
+
 def _vector(t: Optional[torch.Tensor], C: int, name: str, dev: int):
     """_channels of a tensor on device dev."""
     if t is not None and (t.dtype != torch.float32 or t.shape != (C,)):
@@ -998,8 +1005,8 @@ def spv_linear_backward8(ws: Workspace, saved: Checkpoint8, da: torch.Tensor, m_
         out = da.new_empty((Cin, Cout), dtype=torch.float32)
     elif out.shape != (Cin, Cout) or out.dtype != torch.float32:
         raise ValueError(f"out must be float32 [{Cin}][{Cout}]")
-    dap, op, count = _at(da, dev), _at(out, dev), _count(m_dev, dev)
-    st = lib().spv_linear_backward8(_stream_of(dev), ws.ptr, ws.nbytes, codes, exps, count, m, Cin, dap, Cout, op,
+    dap, op, count, wp = _at(da, dev), _at(out, dev), _count(m_dev, dev), _ws_at(ws, dev)
+    st = lib().spv_linear_backward8(_stream_of(dev), wp, ws.nbytes, codes, exps, count, m, Cin, dap, Cout, op,
                                     _DT[da.dtype])
     _chk(st, "spv_linear_backward8")
     return out
@@ -1028,10 +1035,11 @@ def spv_group_norm(ws: Workspace, x: torch.Tensor, off: torch.Tensor, groups: in
         out = torch.empty_like(x)
     elif out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError("out must have x's shape and type")
+    offp, wp = _at(off, dev), _ws_at(ws, dev)
     stat = x.new_empty((B, groups, 2), dtype=torch.float32) if want_stat else None
     saved, codes, exps = Checkpoint8._like(x) if want_checkpoint else (None, None, None)
-    st = lib().spv_group_norm(_stream_of(dev), ws.ptr, ws.nbytes, xp, m, C, _at(off, dev), B, groups, gp, bp, eps,
-                              _ACT[act], _at(out, dev), _at(stat, dev), codes, exps, _DT[x.dtype])
+    st = lib().spv_group_norm(_stream_of(dev), wp, ws.nbytes, xp, m, C, offp, B, groups, gp, bp, eps, _ACT[act],
+                              _at(out, dev), _at(stat, dev), codes, exps, _DT[x.dtype])
     _chk(st, "spv_group_norm")
     got = (out, *(t for t in (stat, saved) if t is not None))
     return got if len(got) > 1 else out
@@ -1061,11 +1069,11 @@ def spv_group_norm_backward(ws: Workspace, dy: torch.Tensor, x, off: torch.Tenso
     if stat.dtype != torch.float32 or stat.shape != (B, groups, 2):
         raise ValueError(f"stat must be float32 [{B}][{groups}][2]")
     dyp, offp, sp, rp = _at(dy, dev), _at(off, dev), _at(stat, dev), _at(dres, dev)
-    gp, bp = _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev)
+    gp, bp, wp = _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev), _ws_at(ws, dev)
     dx = torch.empty_like(dy)
     dgamma = dy.new_empty(C, dtype=torch.float32)
     dbeta = torch.empty_like(dgamma)
-    st = lib().spv_group_norm_backward(_stream_of(dev), ws.ptr, ws.nbytes, dyp, xp, codes, exps, m, C, offp, B, groups, gp,
+    st = lib().spv_group_norm_backward(_stream_of(dev), wp, ws.nbytes, dyp, xp, codes, exps, m, C, offp, B, groups, gp,
                                        bp, sp, _ACT[act], rp, dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(),
                                        _DT[dy.dtype])
     _chk(st, "spv_group_norm_backward")

@@ -223,3 +223,17 @@ def test_a_workspace_for_more_rows_serves_fewer(C, G, B):
               lambda m: L.spv_linear_backward8_workspace_bytes(m, min(C, 256), 64)):
         sizes = [f(m) for m in rows]
         assert all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[0] > 0
+
+
+def test_workspaces_of_another_device(monkeypatch):
+    """A workspace is where the call runs, too."""
+    monkeypatch.setattr(spv, "_here", lambda: -1)  # where the tensors of the CPU are
+    monkeypatch.setattr(spv, "lib", lambda: (_ for _ in ()).throw(AssertionError("a call was made")))
+    ws = spv.Workspace(1024, "meta")
+    ws.buf = type("Buffer", (), dict(get_device=lambda self: 1))()
+    x, off = torch.zeros(6, 64), torch.tensor([0, 6], dtype=torch.int32)
+    saved = spv.Checkpoint8.empty(6, 64, torch.float32, "cpu")
+    for f in (lambda: spv.spv_linear_backward8(ws, saved, x), lambda: spv.spv_group_norm(ws, x, off, 4),
+              lambda: spv.spv_group_norm_backward(ws, x, x, off, 4, torch.zeros(1, 4, 2))):
+        with pytest.raises(ValueError, match="workspace of the current device"):
+            f()
