@@ -18,6 +18,9 @@ import torch
 
 from . import spv
 
+# weights of which spv_linear_backward and spv_linear_backward8 form the gradient in one call
+LINEAR_BACKWARD_WEIGHTS, LINEAR_BACKWARD8_WEIGHTS = 1 << 16, 1 << 20
+
 
 def scan_offsets(coords: torch.Tensor, scans: int) -> torch.Tensor:
     """[scans + 1] int32: the first row of each scan in a voxel list [m][4] in canonical order (no
@@ -60,13 +63,20 @@ class ScanLayer:
         return spv.spv_linear(ws, x, W, res=res)[: x.shape[0]]
 
     def _weight_gradient(self, kept, W, d, widest=0):
-        """dW of kept W, given the product's gradient: kept is the rows or their checkpoint in 8 bits."""
-        if isinstance(kept, torch.Tensor):
-            wide = (max(*W.shape, widest),) * 2
-            ws = self._ws("linear", wide, lambda: spv.Workspace.for_linear_backward(*wide))
+        """dW of kept W, given the product's gradient: kept is the rows or their checkpoint in 8 bits.  The workspace is for up to
+        `widest` channels, or (None) for W alone."""
+        whole, (Cin, Cout) = isinstance(kept, torch.Tensor), W.shape
+        most = (LINEAR_BACKWARD_WEIGHTS if whole else LINEAR_BACKWARD8_WEIGHTS) // Cin
+        if Cout > most > 0:  # by blocks of outputs
+            step = most // 16 * 16 or most
+            return torch.cat([self._weight_gradient(kept, W[:, j:j + step].contiguous(), d[:, j:j + step].contiguous(), None)
+                              for j in range(0, Cout, step)], 1)
+        if whole:
+            name, sizes = (f"linear {Cin} {Cout}", (Cin, Cout)) if widest is None else ("linear", (max(Cin, Cout, widest),) * 2)
+            ws = self._ws(name, sizes, lambda: spv.Workspace.for_linear_backward(*sizes))
             return spv.spv_linear_backward(ws, kept, W, d, want_dx=False)[1]
-        sizes = (d.shape[0], *W.shape)
-        ws = self._ws(f"linear8 {W.shape[0]} {W.shape[1]}", sizes, lambda: spv.Workspace.for_linear_backward8(*sizes))
+        sizes = (d.shape[0], Cin, Cout)
+        ws = self._ws(f"linear8 {Cin} {Cout}", sizes, lambda: spv.Workspace.for_linear_backward8(*sizes))
         return spv.spv_linear_backward8(ws, kept, d)
 
 

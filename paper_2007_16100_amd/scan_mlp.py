@@ -20,7 +20,10 @@ from .scan_attention import ScanLayer, _rows
 class ScanMLP(ScanLayer):
     """params: gamma1, beta1 [C] and gamma2, beta2 [F] f32; W1 [C][F], W2 [F][C] of the features' type.  act is "none",
     "relu" or "silu"; keep8: save holds rows in 8 bits (half of bf16's).  Contiguous parameters are read where they are, others
-    copied once."""
+    copied once.
+
+    16-bit products run on the matrix cores from a multiple of 8 channels, up to 128 or 225 to 256, to 16, 32, 64, 96, 128 or 256;
+    others and float32's on a vector kernel."""
 
     def __init__(self, params: Dict[str, torch.Tensor], groups: int, act: str = "silu", eps: float = 1e-5,
                  keep8: bool = False):

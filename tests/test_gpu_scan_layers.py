@@ -283,3 +283,10 @@ def test_layers_on_scans_without_voxels(spv):
             assert layer.forward(x, *args, save=saved).shape == (0, C)
             g = layer.backward(saved, x)
             assert g["x"].shape == (0, C) and not any(bool(t.any()) for k, t in g.items() if k != "x")
+
+
+@pytest.mark.parametrize("keep8", [False, True])
+@pytest.mark.parametrize("dtype,C,F,groups", [("bf16", 256, 512, 8), ("f16", 272, 256, 16), ("f32", 300, 260, 4),
+                                              ("bf16", 1056, 1024, 32)])
+def test_mlp_of_more_weights_than_one_backward_call_takes(spv, dtype, C, F, groups, keep8):
+    test_mlp_and_gradients(spv, dtype, C, F, groups, "silu", keep8)

@@ -134,3 +134,42 @@ def test_captured_calls_have_workspaces_of_their_own(workspaces, monkeypatch):
     assert not set(first) & set(one) and not set(first) & set(two) and not set(one) & set(two)
     capturing[0] = False
     assert step() == first
+
+
+@pytest.mark.parametrize("C,F", [(256, 512), (512, 256), (300, 260), (64, 128)])
+def test_weight_gradients_of_wide_layers(workspaces, monkeypatch, C, F):
+    """The linear layer's backward takes 65,536 weights: a layer of more has its weight gradient by blocks of outputs, each in a
+    workspace that holds it."""
+    calls = []
+
+    def backward(ws, x, W, da, want_dx=True):
+        assert W.shape[0] * W.shape[1] <= 65536 and W.is_contiguous() and da.is_contiguous() and not want_dx
+        assert x.shape[1] == W.shape[0] and da.shape == (x.shape[0], W.shape[1]) and ws.nbytes >= sum(W.shape)
+        calls.append(W.shape)
+        return None, x.t() @ da
+    fake = scan_attention.spv
+    monkeypatch.setattr(fake, "spv_linear_backward", backward)
+    layer, off = ScanMLP(mlp(C, F, F32), 2), torch.tensor([0, 5], dtype=torch.int32)
+    x, dy, saved = torch.randn(5, C), torch.randn(5, C), {}
+    layer.forward(x, off, save=saved)
+    saved["out2"] = torch.randn(5, F)
+    g = layer.backward(saved, dy)
+    assert g["W2"].shape == (F, C) and torch.allclose(g["W2"], saved["out2"].t() @ dy, atol=1e-5)
+    assert g["W1"].shape == (C, F) and len(calls) == (2 if C * F <= 65536 else 4)
+
+
+def test_weight_gradients_of_wide_layers_from_8_bits(workspaces, monkeypatch):
+    """The same from 8 bits, of 2^20 weights a call."""
+    calls = []
+
+    def backward(ws, saved, da):
+        shape = (saved.codes.shape[1], da.shape[1])
+        assert shape[0] * shape[1] <= 1 << 20 and da.is_contiguous()
+        calls.append(shape)
+        return saved.codes.float().t() @ da
+    monkeypatch.setattr(scan_attention.spv, "spv_linear_backward8", backward, raising=False)
+    layer = ScanMLP(mlp(1100, 1000, F32), 2)
+    saved = spv.Checkpoint8(torch.randint(-127, 128, (5, 1100), dtype=torch.int8), torch.ones(5, 35, dtype=torch.uint8), F32)
+    d = torch.randn(5, 1000)
+    got = layer._weight_gradient(saved, layer.P["W1"], d)
+    assert calls == [(1100, 944), (1100, 56)] and torch.allclose(got, saved.codes.float().t() @ d, atol=1e-2)
