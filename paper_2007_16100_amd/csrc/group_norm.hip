@@ -346,14 +346,12 @@ __global__ __launch_bounds__(kGnThreads) void k_gn_tile_stat(GnArgs a, int tile_
                 const float f = 4.f * __builtin_amdgcn_rcpf(n + 4.f), g = n * f;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    // from the first: equal values give their mean exactly, the type's largest and smallest too
-                    const float mu = fmaf((x[1][e] - x[0][e]) + ((x[2][e] - x[0][e]) + (x[3][e] - x[0][e])), 0.25f, x[0][e]);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float d = x[k][e] - mu;
-                        sq[e] = fmaf(d, d, sq[e]);
-                    }
-                    const float d = mu - mean[e];
+                    // distances to the first: equal values give their mean exactly, the type's largest and smallest too;
+                    // the squares about the mean are what is left of those about the first, a quarter at least
+                    const float d1 = x[1][e] - x[0][e], d2 = x[2][e] - x[0][e], d3 = x[3][e] - x[0][e], s = (d1 + d2) + d3;
+                    const float m = s * 0.25f, d = (x[0][e] - mean[e]) + m;
+                    sq[e] = fmaf(d3, d3, fmaf(d2, d2, fmaf(d1, d1, sq[e])));
+                    sq[e] = fmaf(-s, m, sq[e]);
                     mean[e] = fmaf(d, f, mean[e]);
                     sq[e] = fmaf(d * g, d, sq[e]);
                 }
