@@ -740,8 +740,9 @@ spv_status spv_checkpoint8_read(void* stream, const int8_t* codes, const uint8_t
  * 16-byte aligned codes and da with Cin a multiple of 16 and Cout of 8 (f32: 4) run on
  * the 16-bit matrix cores: the rows' values are exact there, 16-bit da goes as it is,
  * float32 da (of many rows) in three parts that add up to it.  Other widths and
- * alignments, and few rows of float32, run on those for float32.  Sums are float32 over a workgroup's rows, and the workgroups' are
- * added in fp64 in a fixed order: the same bits on every call.
+ * alignments, and few rows of float32, run on those for float32.  Sums are float32
+ * over a workgroup's rows, and the workgroups' are added in fp64 in a fixed order:
+ * the same bits on every call.
  * In:  codes [m_cap][Cin], exps [m_cap][ceil(Cin / 32)]; m_dev: device row count
  *      (NULL = m_cap); da [m_cap][Cout] (dt).
  * Out: dW [Cin][Cout] f32, all of it (0 without rows).
@@ -767,9 +768,12 @@ typedef enum spv_act {
  * float32, with deviations from the rows' own mean (no cancellation where a scan sits
  * far from zero), joined in fp64; one rounding to dt.  G = 1: one mean a scan; G = C:
  * one a scan and channel; off = {0, m}: all rows together.  Equal values give
- * act(beta).  Any width and alignment; 16-byte aligned rows of a multiple of 8
- * channels (f32: 4), up to 4096 (f32: 2048), are moved 16 bytes at a time, up to 512
- * others by elements; wider ones take plain kernels.
+ * act(beta), and xh = 0 in the backward (from the rows, or codes that hold them
+ * exactly).  Deviations are squared in float32: where they pass some 1e19, r is 0.
+ * Any width and alignment; 16-byte aligned rows of a multiple of 8 channels (f32: 4),
+ * up to 4096 (f32: 2048), are moved 16 bytes at a time, up to 512 others by elements;
+ * wider ones take plain kernels, which are not meant for many rows (a workgroup reads
+ * a whole group of a scan).
  * In:  x [m][C] (dt); off [B + 1] i32 device, ascending (clamped to [0, m]); gamma,
  *      beta [C] f32 or NULL (1, 0); eps > 0, finite; C a multiple of G.
  * Out: out [m][C] (dt; may be x), rows of no scan not written; stat [B][G][2] f32 or

@@ -11,8 +11,9 @@
 // could each wait for room that the other holds.)
 //
 // Bound by memory, where rows are many: 300,007 x 96 in bf16 takes 35 us, 173 MB at 4.9 TB/s (a copy reaches 5.1): 13
-// for the statistics, 20 for the rows.  A training step of 88,119 x 96 with the residual's gradient, 152 MB, 42 us:
-// 9, 10, 13 and 15, of which 4 each are the launch, the search for the tile, the join and the last waves.
+// for the statistics, 20 for the rows.  A training step of 88,119 x 96 with the residual's gradient, 152 MB, 41 us:
+// 8, 10, 11 and 14 in a kernel trace (which adds some), of which 4 each are the launch, the search for the tile, the
+// join and the last waves.
 #include <type_traits>
 
 #include "attn_common.hpp"
@@ -51,8 +52,8 @@ __device__ inline float act_grad(float d, float z) {
 constexpr int kGnThreads = 512, kGnWaves = kGnThreads / 64;
 // Tiles of one long scan: with the scans' first ones and the workgroups that join the channels, about one a CU.  What
 // a workgroup does besides its rows (some 4 us, at the start and the end) is not hidden by a second one that does the
-// same: 240, 384 and 512 tiles take 39, 40 and 45 us for 300,007 x 96 in bf16 (512 being more than fit at once) and
-// 51, 61 and 61 for the training step of 88,119 x 96.
+// same: 240, 384 and 512 tiles take 35.4, 35.7 and 37.9 us for 300,007 x 96 in bf16 (512 being more than fit at once) and
+// 41.0, 44.4 and 44.9 for the training step of 88,119 x 96.
 constexpr int kGnTiles = 240;
 
 template <int DT>
@@ -650,8 +651,9 @@ __global__ __launch_bounds__(kGnThreads, 4) void k_gn_tile_dx(GnArgs a, int tile
 // ---------------------------------------------------------------------------
 constexpr int kGnFewThreads = 512;
 constexpr int kGnHeld = 24;  // values a thread holds
-// values in all up to which that is done: 701 x 96 in float32 takes 6.9 us with 8 groups (8.2 in tiles), in bf16 with
-// 96 groups 4.5 (13.8); 8000 x 32 with 32 groups, whose rows are then read 4 bytes at a time, 14.4 (10.0)
+// values in all up to which that is done: 701 x 96 in a graph takes 6.9 us in float32 with 8 groups (7.5 in tiles), in bf16
+// with 8 groups 9.2 (8.0: a thread's 17 loads of 2 bytes wait for each other) and with 96 groups 4.5 (13.6); 8000 x 32
+// with 32 groups, whose rows are then read 4 bytes at a time, 14.4 (10.0)
 constexpr int64_t kGnFew = 1 << 17;
 
 __device__ inline float block_sum(float v, float* red) {
@@ -707,7 +709,9 @@ __global__ __launch_bounds__(kGnFewThreads) void k_gn_few(GnArgs a, uint32_t by_
 }
 
 // ---------------------------------------------------------------------------
-// rows too wide for a workgroup's threads, by elements: a workgroup takes a group or a channel of a scan
+// Rows too wide for a workgroup's threads, by elements: a workgroup takes a group or a channel of a scan, all of its
+// rows.  Right, and not meant for many rows: 11,263 x 1028 in bf16 takes 5.3 ms with 4 groups and 21 with one (rows of 1024,
+// aligned, 0.02), the backward 0.14.
 // ---------------------------------------------------------------------------
 __device__ inline double block_sum(double v, double* red) {
     __syncthreads();
@@ -865,9 +869,9 @@ static size_t gn_room(int64_t m, int C, int B) {
     return (size_t)((t < kGnTiles ? t : kGnTiles) + B);
 }
 // A workgroup joins its scan's tiles itself: up to 32 of them by 8 lanes a group, 64 groups at a time (2000 x 96 in
-// 96 groups takes 14.5 us, 23.5 by a wave a group and 15.3 by a launch of its own), more by a wave, up to twice over.
-// Beyond, a launch of its own is shorter: 100,000 x 96 in bf16 15.4 against 17.1 us with 8 groups, 18.5 and 17.9 with
-// 24, 38.1 and 21.5 with 96.
+// 96 groups takes 14.2 us, 23.5 by a wave a group and 15.3 by a launch of its own), more by a wave, up to twice over.
+// Beyond, a launch of its own is shorter: 100,000 x 96 in bf16 14.9 against 16.7 us with 8 groups, 18.0 and 17.7 with
+// 24, 37.2 and 21.6 with 96.
 static bool gn_few_tiles(const GnArgs& a) { return gn_tiles(a.m, a.C, 1) <= 32; }
 static bool gn_join_apart(const GnArgs& a) { return !gn_few_tiles(a) && a.G > 2 * kGnWaves; }
 
